@@ -47,7 +47,7 @@ typedef enum {
     DBLP_ETIMEOUT = -5   /* reserved: no call in this library waits on the device */
 } dblp_status_t;
 
-typedef enum { DBLP_F32 = 0, DBLP_BF16 = 1 } dblp_dtype_t;
+typedef enum { DBLP_F32 = 0, DBLP_BF16 = 1, DBLP_F16 = 2 } dblp_dtype_t; /* F16: worker-side operators only, not plans */
 typedef enum { DBLP_LOSS_NONE = 0, DBLP_LOSS_IID = 1, DBLP_LOSS_GE = 2, DBLP_LOSS_MICROBURST = 3 } dblp_loss_kind_t;
 enum { DBLP_SUM = 0, DBLP_MEAN = 1, DBLP_OUT_BF16 = 2 }; /* flags of dblp_aggregate; OUT_BF16 only with dblp_aggregate_reduce_ex */
 
@@ -399,6 +399,94 @@ int dblp_round_host(const dblp_plan_t* plan, const void* const* grads_host, cons
 int dblp_round_until_stop(const dblp_plan_t* plan, const dblp_loss_model_t* model, uint64_t seed, uint32_t round,
                           uint32_t bound_ppm, uint32_t max_attempts, int early_stop, const dblp_device_buffers_t* dev,
                           uint32_t* attempts_used, uint32_t* all_ok_host, void* stream);
+
+/* ---- worker side: operators of the training step whose gradients a round carries -----------------------------------
+ * Algorithm 4 (worker): compute the gradient, send it, receive the mean, update.  These calls compute pieces of that
+ * gradient for token models: the embedding table and its gradient, dropout, attention and its gradient.  They need no
+ * plan; they run on the current device, whose memory all device pointers are in, allocate nothing, only enqueue work
+ * on the given stream, and the order of every floating-point addition is fixed by the arguments, so results repeat bit for bit.
+ * dtype arguments are dblp_dtype_t; strides are in elements and may be anything that keeps rows apart (inputs may also
+ * repeat: stride 0).  Zero-sized calls return DBLP_OK without touching memory. */
+
+/* dblp_embed: out[i, :] = scale * table[tokens[i], :], an fp32 multiply rounded once to out_dtype.
+ * table: rows x width, row stride table_stride.  tokens: n ids of token_bytes (4 or 8) bytes each, signed.  out: n rows,
+ * row stride out_stride.  A token equal to `padding` (any value outside [0, rows) = no padding id) gives a zero row.  A
+ * token outside [0, rows) that is not the padding id gives a zero row too and is counted in *bad_tokens (u64, device,
+ * accumulates; NULL = not counted); it never faults. */
+int dblp_embed(const void* table, int64_t table_stride, uint64_t rows, uint32_t width, int table_dtype,
+               const void* tokens, uint32_t token_bytes, uint64_t n, int64_t padding, float scale, void* out,
+               int64_t out_stride, int out_dtype, uint64_t* bad_tokens, void* stream);
+
+/* dblp_embed_grad: the table's gradient, dense.  For every row v
+ *     dtable[v, :] = round(scale * sum of dout[i, :] over the i with tokens[i] = v, ascending [+ dtable[v, :]])
+ * The sum is in fp32: the occurrences of all tokens, sorted by (token, i), are cut into tiles of 32; inside a tile a
+ * row's terms are added one after the other, and a row that spans several tiles adds their partial sums in tile order
+ * (from 8 partial sums on in 8 contiguous parts, joined in order).  Rows that no token names are written as zero.
+ * flags: DBLP_ACCUMULATE adds to what dtable holds (rows that no token names are not touched), e.g. the output layer's
+ * gradient of a tied table.  Padding and bad tokens contribute nothing (bad_tokens as above).
+ * ws: dblp_embed_grad_workspace_bytes() bytes, 256-byte aligned, contents need not be preserved.  n < 2^31, rows < 2^31. */
+enum { DBLP_ACCUMULATE = 1 };
+int dblp_embed_grad_workspace_bytes(uint64_t n, uint64_t rows, uint32_t width, size_t* bytes);
+int dblp_embed_grad(const void* dout, int64_t dout_stride, int dout_dtype, const void* tokens, uint32_t token_bytes,
+                    uint64_t n, int64_t padding, float scale, void* dtable, int64_t dtable_stride, uint64_t rows,
+                    uint32_t width, int dtable_dtype, uint32_t flags, uint64_t* bad_tokens, void* ws, size_t ws_bytes,
+                    void* stream);
+
+/* dblp_dropout: out = dropout(x) [+ residual], rows x cols, each with a row stride of its own; out may be x or residual.
+ * Element i = row * cols + col (whatever the strides) draws 16 bits: group i / 8 is one Philox4x32-10 draw with key =
+ * seed and counter = (group low, group high, 5 | site << 8, step), element i takes half i % 2 (low first) of word
+ * (i % 8) / 2.  It is dropped iff its bits are below t = floor(p * 65536); a kept element is scaled by
+ * 65536 / (65536 - t), the inverse of the share that is really kept, so the expectation is exact for every p.  The mask
+ * is never stored: dblp_dropout_grad draws it again.  p in [0, 1] (1 drops everything), site < 2^24; (seed, step, site)
+ * names a mask: site tells the dropouts of one training step apart.  residual NULL = none.  The product and the sum are
+ * fp32 (two roundings), the result is rounded once more to dtype. */
+int dblp_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* out,
+                 int64_t out_stride, uint64_t rows, uint32_t cols, int dtype, double p, uint64_t seed, uint32_t step,
+                 uint32_t site, void* stream);
+/* dx = the gradient of x given dout (the residual's gradient is dout itself).  dx may be dout. */
+int dblp_dropout_grad(const void* dout, int64_t dout_stride, void* dx, int64_t dx_stride, uint64_t rows, uint32_t cols,
+                      int dtype, double p, uint64_t seed, uint32_t step, uint32_t site, void* stream);
+
+/* Heads of a [batch, token, head, head_dim] tensor; the head_dim elements of a head are contiguous.  Data and strides
+ * (in elements; unused where the extent is 1) are multiples of 16 bytes.  Inputs may have stride 0 over batch or heads
+ * (broadcast); the sections of outputs must not overlap. */
+typedef struct {
+    void* data;
+    int64_t batch_stride, token_stride, head_stride;
+} dblp_heads_t;
+
+enum { DBLP_ATTENTION_CAUSAL = 1 };
+typedef struct {
+    uint32_t batch, q_tokens, k_tokens; /* extents of the tensors */
+    uint32_t q_heads, kv_heads;         /* kv_heads divides q_heads; query head h reads key head h / (q_heads / kv_heads) */
+    uint32_t head_dim;                  /* a multiple of 8, at most 128 */
+    int dtype;                          /* DBLP_BF16 or DBLP_F16 */
+    uint32_t flags;                     /* 0 or DBLP_ATTENTION_CAUSAL */
+    float scale;                        /* of the scores, usually 1 / sqrt(head_dim); finite, > 0 */
+    const int32_t* q_lens;              /* device, [batch]: tokens that count in each sequence; NULL = all.  Values are */
+    const int32_t* k_lens;              /* clamped to the extents; what lies beyond is never used, NaN included */
+} dblp_attention_t;
+
+/* dblp_attention, per sequence and head, with lq = q_lens[b] and lk = k_lens[b]:
+ *     s_ij = scale * <q_i, k_j>,  i < lq, j < lk, with DBLP_ATTENTION_CAUSAL also j <= i + lk - lq (the last query
+ *                                 sees every key)
+ *     lse_i = log sum_j exp(s_ij),  out_i = sum_j exp(s_ij - lse_i) v_j
+ * A query that sees no key, or lies beyond lq, gets out = 0 and lse = -infinity.  lse: fp32 [batch, q_heads, q_tokens],
+ * contiguous (NULL = not wanted).
+ * dblp_attention_grad: with D_i = <dout_i, out_i>, p_ij = exp(s_ij - lse_i) computed again from q, k and lse,
+ *     ds_ij = p_ij (<dout_i, v_j> - D_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+ *     dv_j = sum_i p_ij dout_i;  shared key heads sum over their query heads.
+ * out and lse are dblp_attention's for the same arguments.  Every element of dq, dk and dv is written (zero where
+ * nothing contributes).  Scores, statistics and accumulators are fp32; p and ds are rounded to dtype where they enter a
+ * product.
+ * ws: dblp_attention_workspace_bytes() bytes (fwd for dblp_attention, grad for dblp_attention_grad; either may be 0),
+ * 256-byte aligned, contents need not be preserved. */
+int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes);
+int dblp_attention(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
+                   const dblp_heads_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
+                        const dblp_heads_t* out, const dblp_heads_t* dout, const float* lse, const dblp_heads_t* dq,
+                        const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- diagnostics -----------------------------------------------------------------------------------------------*/
 const char* dblp_strerror(int status);

@@ -11,9 +11,10 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdblp.so")
 
-DBLP_F32, DBLP_BF16 = 0, 1
+DBLP_F32, DBLP_BF16, DBLP_F16 = 0, 1, 2
 DBLP_LOSS_NONE, DBLP_LOSS_IID, DBLP_LOSS_GE, DBLP_LOSS_MICROBURST = 0, 1, 2, 3
 DBLP_SUM, DBLP_MEAN, DBLP_OUT_BF16 = 0, 1, 2
+DBLP_ACCUMULATE, DBLP_ATTENTION_CAUSAL = 1, 1
 LOSS_KINDS = {"none": DBLP_LOSS_NONE, "iid": DBLP_LOSS_IID, "ge": DBLP_LOSS_GE, "microburst": DBLP_LOSS_MICROBURST}
 HDR_BYTES = 32
 COUNTER_FIELDS = ("n_arrived", "n_accepted", "n_dup", "n_stale", "n_invalid", "n_late")
@@ -47,6 +48,15 @@ class dblp_round_marks_t(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in MARK_FIELDS]
 
 
+class dblp_heads_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class dblp_attention_t(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("batch", "q_tokens", "k_tokens", "q_heads", "kv_heads", "head_dim")] + [
+        ("dtype", C.c_int), ("flags", C.c_uint32), ("scale", C.c_float), ("q_lens", C.c_void_p), ("k_lens", C.c_void_p)]
+
+
 class RoundMarks:
     """Timing events for the stages of a whole-round call (torch events; the library records them)."""
 
@@ -77,6 +87,8 @@ EXPORTS = ("dblp_plan_create", "dblp_plan_destroy", "dblp_plan_query", "dblp_pla
            "dblp_aggregate_book",
            "dblp_aggregate_claim", "dblp_aggregate_claim_grouped", "dblp_claim_workspace_bytes", "dblp_aggregate_bitmap", "dblp_aggregate_reduce", "dblp_aggregate_reduce_ex", "dblp_aggregate_reduce_atomic", "dblp_norm_scratch_count", "dblp_aggregate", "dblp_round_reset", "dblp_check_bound", "dblp_bound_ok", "dblp_clr",
            "dblp_select_bound", "dblp_round_send", "dblp_round_receive", "dblp_round_device", "dblp_round_host",
+           "dblp_embed", "dblp_embed_grad_workspace_bytes", "dblp_embed_grad", "dblp_dropout", "dblp_dropout_grad",
+           "dblp_attention_workspace_bytes", "dblp_attention", "dblp_attention_grad",
            "dblp_strerror", "dblp_last_error", "dblp_launch_count")
 
 
@@ -96,6 +108,17 @@ def lib():
         L.dblp_clr.argtypes = [C.c_double, C.c_double, C.c_double]
         L.dblp_loss_model_from_rates.argtypes = [C.c_int, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double,
                                                  C.c_uint64, C.POINTER(dblp_loss_model_t)]
+        vp, i64, u64, u32 = C.c_void_p, C.c_int64, C.c_uint64, C.c_uint32
+        L.dblp_embed.argtypes = [vp, i64, u64, u32, C.c_int, vp, u32, u64, i64, C.c_float, vp, i64, C.c_int, vp, vp]
+        L.dblp_embed_grad_workspace_bytes.argtypes = [u64, u64, u32, C.POINTER(C.c_size_t)]
+        L.dblp_embed_grad.argtypes = [vp, i64, C.c_int, vp, u32, u64, i64, C.c_float, vp, i64, u64, u32, C.c_int, u32, vp, vp,
+                                      C.c_size_t, vp]
+        L.dblp_dropout.argtypes = [vp, i64, vp, i64, vp, i64, u64, u32, C.c_int, C.c_double, u64, u32, u32, vp]
+        L.dblp_dropout_grad.argtypes = [vp, i64, vp, i64, u64, u32, C.c_int, C.c_double, u64, u32, u32, vp]
+        at, hd, sz = C.POINTER(dblp_attention_t), C.POINTER(dblp_heads_t), C.POINTER(C.c_size_t)
+        L.dblp_attention_workspace_bytes.argtypes = [at, sz, sz]
+        L.dblp_attention.argtypes = [at, hd, hd, hd, hd, vp, vp, C.c_size_t, vp]
+        L.dblp_attention_grad.argtypes = [at] + [hd] * 5 + [vp] + [hd] * 3 + [vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -398,6 +421,155 @@ def dblp_round_host(plan, grads_host, model, seed, round, bound_ppm, flags, dev,
                                  C.c_uint32(bound_ppm), C.c_uint32(flags), C.byref(b), _ptr(agg_host),
                                  _ptr(counters_host), _ptr(recv_cnt_host), _ptr(missing_cnt_host), _ptr(ok_host),
                                  _ptr(all_ok_host), _stream(stream)), "dblp_round_host")
+
+
+# ---- worker side -----------------------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: DBLP_F32, torch.bfloat16: DBLP_BF16, torch.float16: DBLP_F16}
+
+
+def _dtype(t):
+    if t.dtype not in _DTYPES:
+        raise ValueError("dtype %s: float32, bfloat16 or float16" % t.dtype)
+    return _DTYPES[t.dtype]
+
+
+def _on_device(*tensors):
+    """The library launches on the current device: every tensor has to be there."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError("a tensor on %s, which is not the current device" % t.device)
+
+
+def _require(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t, name):
+    """(address, row stride) of a 2-D tensor whose elements within a row are contiguous."""
+    _require(t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: 2-D, contiguous within a row" % name)
+    return t.data_ptr(), t.stride(0)
+
+
+def _flat_tokens(tokens):
+    _require(tokens.dim() == 1 and tokens.dtype in (torch.int32, torch.int64) and tokens.is_contiguous(),
+             "tokens: 1-D, contiguous, int32 or int64")
+    return tokens.data_ptr(), tokens.element_size(), tokens.shape[0]
+
+
+def _counter(t):
+    _require(t is None or (t.dtype == torch.int64 and t.numel() == 1), "bad_tokens: one int64")
+    return None if t is None else t.data_ptr()
+
+
+def _scratch(ws):
+    return (None, 0) if ws is None or ws.numel() == 0 else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def dblp_embed(table, tokens, out, scale=1.0, padding=-1, bad_tokens=None, stream=None):
+    """out[i] = scale * table[tokens[i]]; a zero row for the padding id and for ids outside the table."""
+    _on_device(table, tokens, out, bad_tokens)
+    tp, ts = _rows(table, "table")
+    op, os_ = _rows(out, "out")
+    kp, kb, n = _flat_tokens(tokens)
+    _require(out.shape == (n, table.shape[1]), "out: one row of the table's width per token")
+    _check(lib().dblp_embed(tp, ts, table.shape[0], table.shape[1], _dtype(table), kp, kb, n, padding, scale, op, os_,
+                            _dtype(out), _counter(bad_tokens), _stream(stream)), "dblp_embed")
+
+
+def dblp_embed_grad_workspace_bytes(n, rows, width):
+    b = C.c_size_t()
+    _check(lib().dblp_embed_grad_workspace_bytes(n, rows, width, C.byref(b)), "dblp_embed_grad_workspace_bytes")
+    return int(b.value)
+
+
+def dblp_embed_grad(dout, tokens, dtable, ws, scale=1.0, padding=-1, accumulate=False, bad_tokens=None, stream=None):
+    """dtable[v] = scale * sum of dout[i] over the i with tokens[i] = v (added to dtable with accumulate)."""
+    _on_device(dout, tokens, dtable, ws, bad_tokens)
+    dp, ds = _rows(dout, "dout")
+    tp, ts = _rows(dtable, "dtable")
+    kp, kb, n = _flat_tokens(tokens)
+    _require(dout.shape == (n, dtable.shape[1]), "dout: one row of the table's width per token")
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_embed_grad(dp, ds, _dtype(dout), kp, kb, n, padding, scale, tp, ts, dtable.shape[0], dtable.shape[1],
+                                 _dtype(dtable), DBLP_ACCUMULATE if accumulate else 0, _counter(bad_tokens), wp, wb,
+                                 _stream(stream)), "dblp_embed_grad")
+
+
+def dblp_dropout(x, out, p, seed, step, site, residual=None, stream=None):
+    """out = dropout(x) [+ residual]; (seed, step, site) names the mask."""
+    _on_device(x, out, residual)
+    xp, xs = _rows(x, "x")
+    op, os_ = _rows(out, "out")
+    rp, rs = (None, 0) if residual is None else _rows(residual, "residual")
+    _require(out.shape == x.shape and (residual is None or residual.shape == x.shape), "x, residual and out: one shape")
+    _require(out.dtype == x.dtype and (residual is None or residual.dtype == x.dtype), "x, residual and out: one dtype")
+    _check(lib().dblp_dropout(xp, xs, rp, rs, op, os_, x.shape[0], x.shape[1], _dtype(x), p, seed, step, site,
+                              _stream(stream)), "dblp_dropout")
+
+
+def dblp_dropout_grad(dout, dx, p, seed, step, site, stream=None):
+    """Gradient of dblp_dropout's x: the mask of (seed, step, site) drawn again."""
+    _on_device(dout, dx)
+    gp, gs = _rows(dout, "dout")
+    xp, xs = _rows(dx, "dx")
+    _require(dx.shape == dout.shape and dx.dtype == dout.dtype, "dout and dx: one shape and dtype")
+    _check(lib().dblp_dropout_grad(gp, gs, xp, xs, dx.shape[0], dx.shape[1], _dtype(dx), p, seed, step, site,
+                                   _stream(stream)), "dblp_dropout_grad")
+
+
+def _heads(t, name, like, batch, tokens, heads):
+    _require(t.dtype == like.dtype and tuple(t.shape) == (batch, tokens, heads, like.shape[3]),
+             "%s: shape %s, %s" % (name, (batch, tokens, heads, like.shape[3]), like.dtype))
+    sb, st, sh, sd = t.stride()
+    _require(sd == 1 or t.shape[3] == 1, "%s: the elements of a head are contiguous" % name)
+    return C.byref(dblp_heads_t(t.data_ptr(), sb, st, sh))
+
+
+def _attention(q, k, causal, scale, q_lens, k_lens):
+    _require(q.dim() == 4 and k.dim() == 4, "q and k: [batch, tokens, heads, head_dim]")
+    B, Sq, Hq, D = q.shape
+    for n in (q_lens, k_lens):
+        _require(n is None or (n.dtype == torch.int32 and n.shape == (B,) and n.is_contiguous()), "lengths: int32, one per sequence")
+    return dblp_attention_t(B, Sq, k.shape[1], Hq, k.shape[2], D, _dtype(q), DBLP_ATTENTION_CAUSAL if causal else 0,
+                            D ** -0.5 if scale is None and D else scale or 0.0, None if q_lens is None else q_lens.data_ptr(),
+                            None if k_lens is None else k_lens.data_ptr())
+
+
+def dblp_attention_workspace_bytes(q, k, causal=False):
+    """(bytes for dblp_attention, bytes for dblp_attention_grad) with tensors of these shapes."""
+    f, g = C.c_size_t(), C.c_size_t()
+    _check(lib().dblp_attention_workspace_bytes(C.byref(_attention(q, k, causal, None, None, None)), C.byref(f), C.byref(g)),
+           "dblp_attention_workspace_bytes")
+    return int(f.value), int(g.value)
+
+
+def dblp_attention(q, k, v, out, lse=None, ws=None, causal=False, scale=None, q_lens=None, k_lens=None, stream=None):
+    """q, out [batch, tokens, heads, head_dim]; k, v [batch, keys, key heads, head_dim]; lse fp32 [batch, heads, tokens]."""
+    _on_device(q, k, v, out, lse, ws, q_lens, k_lens)
+    a = _attention(q, k, causal, scale, q_lens, k_lens)
+    _require(lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (a.batch, a.q_heads, a.q_tokens) and
+                             lse.is_contiguous()), "lse: contiguous float32 [batch, heads, tokens]")
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_attention(C.byref(a), _heads(q, "q", q, a.batch, a.q_tokens, a.q_heads),
+                                _heads(k, "k", q, a.batch, a.k_tokens, a.kv_heads),
+                                _heads(v, "v", q, a.batch, a.k_tokens, a.kv_heads),
+                                _heads(out, "out", q, a.batch, a.q_tokens, a.q_heads), None if lse is None else lse.data_ptr(),
+                                wp, wb, _stream(stream)), "dblp_attention")
+
+
+def dblp_attention_grad(q, k, v, out, dout, lse, dq, dk, dv, ws, causal=False, scale=None, q_lens=None, k_lens=None,
+                        stream=None):
+    """Gradients of dblp_attention, from its inputs, its out and lse, and dout."""
+    _on_device(q, k, v, out, dout, lse, dq, dk, dv, ws, q_lens, k_lens)
+    a = _attention(q, k, causal, scale, q_lens, k_lens)
+    _require(lse.dtype == torch.float32 and tuple(lse.shape) == (a.batch, a.q_heads, a.q_tokens) and lse.is_contiguous(),
+             "lse: contiguous float32 [batch, heads, tokens]")
+    qh = [_heads(t, n, q, a.batch, a.q_tokens, a.q_heads) for t, n in ((q, "q"), (out, "out"), (dout, "dout"), (dq, "dq"))]
+    kh = [_heads(t, n, q, a.batch, a.k_tokens, a.kv_heads) for t, n in ((k, "k"), (v, "v"), (dk, "dk"), (dv, "dv"))]
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_attention_grad(C.byref(a), qh[0], kh[0], kh[1], qh[1], qh[2], lse.data_ptr(), qh[3], kh[2], kh[3], wp, wb,
+                                     _stream(stream)), "dblp_attention_grad")
 
 
 def dblp_launch_count():

@@ -17,7 +17,7 @@ constexpr unsigned long long kEmpty64 = ~0ull;
 constexpr uint32_t kMaxWorkersPerLaunch = 64;  // gradient pointers travel in the kernel parameter block
 
 // Purposes of a Philox draw: kept apart by the low byte of counter word 2.
-enum : uint32_t { kStreamPacket = 1, kStreamGeInit = 2, kStreamWindow = 3, kStreamPerm = 4 };
+enum : uint32_t { kStreamPacket = 1, kStreamGeInit = 2, kStreamWindow = 3, kStreamPerm = 4, kStreamDropout = 5 };
 
 void set_error(const char* fmt, ...);
 extern std::atomic<uint64_t> g_launches;
