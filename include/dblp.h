@@ -448,8 +448,8 @@ int dblp_dropout_grad(const void* dout, int64_t dout_stride, void* dx, int64_t d
                       int dtype, double p, uint64_t seed, uint32_t step, uint32_t site, void* stream);
 
 /* Heads of a [batch, token, head, head_dim] tensor; the head_dim elements of a head are contiguous.  Data and strides
- * (in elements; unused where the extent is 1) are multiples of 16 bytes.  Inputs may have stride 0 over batch or heads
- * (broadcast); the sections of outputs must not overlap. */
+ * (in elements; unused where the extent is 1) are multiples of 16 bytes.  Strides are not negative; inputs may have stride 0 over batch
+ * or heads (broadcast); the sections of outputs must not overlap. */
 typedef struct {
     void* data;
     int64_t batch_stride, token_stride, head_stride;
@@ -491,6 +491,10 @@ int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t* q, const 
 /* ---- diagnostics -----------------------------------------------------------------------------------------------*/
 const char* dblp_strerror(int status);
 const char* dblp_last_error(void);  /* HOST string, valid until the calling thread's next failing call */
+/* Waits inside kernels that gave up after their limit (about two seconds), on the current device since the library was
+ * loaded; 0 unless something is wrong, else the results of the calls before it are incomplete.  Reads the device:
+ * synchronises with the default stream. */
+int dblp_wait_timeouts(uint64_t* count);
 uint64_t dblp_launch_count(void);   /* kernels launched by this library since it was loaded */
 
 #ifdef __cplusplus

@@ -88,7 +88,7 @@ EXPORTS = ("dblp_plan_create", "dblp_plan_destroy", "dblp_plan_query", "dblp_pla
            "dblp_aggregate_claim", "dblp_aggregate_claim_grouped", "dblp_claim_workspace_bytes", "dblp_aggregate_bitmap", "dblp_aggregate_reduce", "dblp_aggregate_reduce_ex", "dblp_aggregate_reduce_atomic", "dblp_norm_scratch_count", "dblp_aggregate", "dblp_round_reset", "dblp_check_bound", "dblp_bound_ok", "dblp_clr",
            "dblp_select_bound", "dblp_round_send", "dblp_round_receive", "dblp_round_device", "dblp_round_host",
            "dblp_embed", "dblp_embed_grad_workspace_bytes", "dblp_embed_grad", "dblp_dropout", "dblp_dropout_grad",
-           "dblp_attention_workspace_bytes", "dblp_attention", "dblp_attention_grad",
+           "dblp_attention_workspace_bytes", "dblp_attention", "dblp_attention_grad", "dblp_wait_timeouts",
            "dblp_strerror", "dblp_last_error", "dblp_launch_count")
 
 
@@ -570,6 +570,12 @@ def dblp_attention_grad(q, k, v, out, dout, lse, dq, dk, dv, ws, causal=False, s
     wp, wb = _scratch(ws)
     _check(lib().dblp_attention_grad(C.byref(a), qh[0], kh[0], kh[1], qh[1], qh[2], lse.data_ptr(), qh[3], kh[2], kh[3], wp, wb,
                                      _stream(stream)), "dblp_attention_grad")
+
+
+def dblp_wait_timeouts():
+    n = C.c_uint64()
+    _check(lib().dblp_wait_timeouts(C.byref(n)), "dblp_wait_timeouts")
+    return int(n.value)
 
 
 def dblp_launch_count():

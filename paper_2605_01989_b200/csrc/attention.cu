@@ -1,147 +1,67 @@
-// dblp_attention and dblp_attention_grad, one warp a row: the plain arrangement, fp32 throughout.
+// dblp_attention, dblp_attention_grad: argument checks, tensor maps and the entry points.
 #include <math.h>
 
-#include "types.cuh"
+#include <mutex>
+
+#include "attention.cuh"
 
 namespace dblp {
 
-constexpr int kAttnWarps = 8;
-constexpr int kPerLane = 4;                 // head_dim <= 128
+static __device__ unsigned long long d_wait_timeouts;
 
-struct Heads {
-    void* p;
-    int64_t sb, st, sh;
-};
+constexpr int kMaxDevices = 64;
 
-struct AttnArgs {
-    Heads q, k, v, o, go, dq, dk, dv;
-    float *lse, *delta;
-    uint32_t B, Sq, Sk, Hq, Hkv, D, causal;
-    float scale;
-    const int32_t *q_lens, *k_lens;
-};
-
-__device__ __forceinline__ uint32_t length_of(const int32_t* lens, uint32_t b, uint32_t extent)
+unsigned long long* timeout_counter()
 {
-    return lens ? (uint32_t)min(max(lens[b], 0), (int32_t)extent) : extent;
-}
-
-template <typename T>
-__device__ __forceinline__ const T* row_of(const Heads& h, uint32_t b, uint32_t t, uint32_t head)
-{
-    return (const T*)h.p + (int64_t)b * h.sb + (int64_t)t * h.st + (int64_t)head * h.sh;
-}
-
-template <typename T>
-__device__ __forceinline__ void load_row(const T* p, uint32_t D, uint32_t lane, float* x)
-{
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) x[i] = lane + 32 * i < D ? to_f32(p[lane + 32 * i]) : 0.0f;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_row(const Heads& h, uint32_t b, uint32_t t, uint32_t head, uint32_t D, uint32_t lane, const float* x)
-{
-    T* p = const_cast<T*>(row_of<T>(h, b, t, head));
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-        if (lane + 32 * i < D) p[lane + 32 * i] = from_f32<T>(x[i]);
-}
-
-__device__ __forceinline__ float dot_rows(const float* a, const float* b)
-{
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) s += a[i] * b[i];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    return s;
-}
-
-// keys that query i sees: 0 .. result - 1
-__device__ __forceinline__ uint32_t keys_of(uint32_t i, uint32_t lq, uint32_t lk, uint32_t causal)
-{
-    if (i >= lq) return 0;
-    if (!causal) return lk;
-    const int64_t e = (int64_t)i + lk - lq + 1;
-    return e < 0 ? 0 : (uint32_t)e;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kAttnWarps * 32) k_attention(AttnArgs a)
-{
-    const uint32_t lane = threadIdx.x & 31, i = blockIdx.x * kAttnWarps + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-    if (i >= a.Sq) return;
-    const uint32_t hk = h / (a.Hq / a.Hkv), n = keys_of(i, length_of(a.q_lens, b, a.Sq), length_of(a.k_lens, b, a.Sk), a.causal);
-    float q[kPerLane], x[kPerLane], o[kPerLane] = {}, m = -INFINITY, l = 0.0f;
-    load_row(row_of<T>(a.q, b, i, h), a.D, lane, q);
-    for (uint32_t j = 0; j < n; ++j) {
-        load_row(row_of<T>(a.k, b, j, hk), a.D, lane, x);
-        const float s = dot_rows(q, x) * a.scale, mn = fmaxf(m, s), c = expf(m - mn), p = expf(s - mn);
-        load_row(row_of<T>(a.v, b, j, hk), a.D, lane, x);
-        l = l * c + p;
-        m = mn;
-#pragma unroll
-        for (int t = 0; t < kPerLane; ++t) o[t] = o[t] * c + p * x[t];
+    static std::atomic<void*> at[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return nullptr;
+    void* p = at[dev].load(std::memory_order_acquire);
+    if (!p) {
+        if (cudaGetSymbolAddress(&p, d_wait_timeouts) != cudaSuccess) return nullptr;
+        at[dev].store(p, std::memory_order_release);
     }
-#pragma unroll
-    for (int t = 0; t < kPerLane; ++t) o[t] = n ? o[t] / l : 0.0f;
-    store_row<T>(a.o, b, i, h, a.D, lane, o);
-    if (a.lse && lane == 0) a.lse[((uint64_t)b * a.Hq + h) * a.Sq + i] = n ? m + logf(l) : -INFINITY;
+    return (unsigned long long*)p;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kAttnWarps * 32) k_attention_dq(AttnArgs a)
+// The driver's encoder of tensor maps, looked up through the runtime (the library does not link the driver).
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encoder()
 {
-    const uint32_t lane = threadIdx.x & 31, i = blockIdx.x * kAttnWarps + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-    if (i >= a.Sq) return;
-    const uint32_t hk = h / (a.Hq / a.Hkv), n = keys_of(i, length_of(a.q_lens, b, a.Sq), length_of(a.k_lens, b, a.Sk), a.causal);
-    const uint64_t at = ((uint64_t)b * a.Hq + h) * a.Sq + i;
-    float q[kPerLane], x[kPerLane], g[kPerLane], dq[kPerLane] = {};
-    load_row(row_of<T>(a.q, b, i, h), a.D, lane, q);
-    load_row(row_of<T>(a.go, b, i, h), a.D, lane, g);
-    load_row(row_of<T>(a.o, b, i, h), a.D, lane, x);
-    const float delta = dot_rows(g, x), lse = a.lse[at];
-    if (lane == 0) a.delta[at] = delta;
-    for (uint32_t j = 0; j < n; ++j) {
-        load_row(row_of<T>(a.v, b, j, hk), a.D, lane, x);
-        const float dp = dot_rows(g, x);
-        load_row(row_of<T>(a.k, b, j, hk), a.D, lane, x);
-        const float ds = expf(dot_rows(q, x) * a.scale - lse) * (dp - delta);
-#pragma unroll
-        for (int t = 0; t < kPerLane; ++t) dq[t] += ds * x[t];
+    static std::atomic<void*> fn{nullptr};
+    void* f = fn.load(std::memory_order_acquire);
+    if (!f) {
+        cudaDriverEntryPointQueryResult st;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &st) != cudaSuccess ||
+            st != cudaDriverEntryPointSuccess)
+            return nullptr;
+        fn.store(f, std::memory_order_release);
     }
-#pragma unroll
-    for (int t = 0; t < kPerLane; ++t) dq[t] *= a.scale;
-    store_row<T>(a.dq, b, i, h, a.D, lane, dq);
+    return (EncodeTiled)f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kAttnWarps * 32) k_attention_dkv(AttnArgs a)
+// Boxes of 128 tokens x 64 columns; what lies outside the tensor reads as zero.
+int make_source(TileSource* t, const dblp_attention_t* a, const dblp_heads_t* h, uint32_t tokens, uint32_t nheads)
 {
-    const uint32_t lane = threadIdx.x & 31, j = blockIdx.x * kAttnWarps + (threadIdx.x >> 5), hk = blockIdx.y, b = blockIdx.z;
-    if (j >= a.Sk) return;
-    const uint32_t rep = a.Hq / a.Hkv, lq = length_of(a.q_lens, b, a.Sq), lk = length_of(a.k_lens, b, a.Sk);
-    float k[kPerLane], v[kPerLane], x[kPerLane], g[kPerLane], dk[kPerLane] = {}, dv[kPerLane] = {};
-    if (j < lk) {
-        load_row(row_of<T>(a.k, b, j, hk), a.D, lane, k);
-        load_row(row_of<T>(a.v, b, j, hk), a.D, lane, v);
-        const int64_t first = a.causal ? max((int64_t)0, (int64_t)j + lq - lk) : 0;
-        for (uint32_t h = hk * rep; h < hk * rep + rep; ++h)
-            for (uint32_t i = (uint32_t)first; i < lq; ++i) {
-                const uint64_t at = ((uint64_t)b * a.Hq + h) * a.Sq + i;
-                load_row(row_of<T>(a.q, b, i, h), a.D, lane, x);
-                load_row(row_of<T>(a.go, b, i, h), a.D, lane, g);
-                const float p = expf(dot_rows(x, k) * a.scale - a.lse[at]), ds = p * (dot_rows(g, v) - a.delta[at]) * a.scale;
-#pragma unroll
-                for (int t = 0; t < kPerLane; ++t) { dv[t] += p * g[t]; dk[t] += ds * x[t]; }
-            }
-    }
-    store_row<T>(a.dk, b, j, hk, a.D, lane, dk);
-    store_row<T>(a.dv, b, j, hk, a.D, lane, dv);
+    const EncodeTiled encode = encoder();
+    DBLP_REQUIRE(encode, DBLP_ECUDA, "attention: the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t unused = (cuuint64_t)a->head_dim * 2;
+    const bool hb = nheads > 1 && h->head_stride == 0, bb = a->batch > 1 && h->batch_stride == 0;
+    const cuuint64_t dims[4] = {a->head_dim, tokens, hb ? 1u : nheads, bb ? 1u : a->batch};
+    const cuuint64_t strides[3] = {tokens > 1 ? (cuuint64_t)h->token_stride * 2 : unused, dims[2] > 1 ? (cuuint64_t)h->head_stride * 2 : unused,
+                                   dims[3] > 1 ? (cuuint64_t)h->batch_stride * 2 : unused};
+    const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
+    const CUresult rc = encode(&t->map, a->dtype == DBLP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                               h->data, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    DBLP_REQUIRE(rc == CUDA_SUCCESS, DBLP_ECUDA, "attention: tensor map refused (driver error %d)", (int)rc);
+    t->mh = hb ? 0 : 1;
+    t->mb = bb ? 0 : 1;
+    return DBLP_OK;
 }
-
-static Heads heads(const dblp_heads_t* h) { return Heads{h->data, h->batch_stride, h->token_stride, h->head_stride}; }
 
 static int check_shape(const char* who, const dblp_attention_t* a)
 {
@@ -168,7 +88,7 @@ static int check_heads(const char* who, const char* name, const dblp_attention_t
     for (auto& d : dim) {
         if (d.extent <= 1) continue;
         aligned = aligned && d.stride % 8 == 0;
-        DBLP_REQUIRE(d.stride >= 0 && d.stride < (1ll << 39), DBLP_EINVAL, "%s: %s has a stride of %lld", who, name, (long long)d.stride);
+        DBLP_REQUIRE(d.stride >= (&d == &dim[1] && !output ? 1 : 0) && d.stride < (1ll << 39), DBLP_EINVAL, "%s: %s has a stride of %lld", who, name, (long long)d.stride);
     }
     DBLP_REQUIRE(aligned, DBLP_EALIGN, "%s: %s has data or a stride that is not a multiple of 16 bytes", who, name);
     if (output) {                                   // sorted by stride, each dimension must clear the ones below it
@@ -187,26 +107,9 @@ static int check_heads(const char* who, const char* name, const dblp_attention_t
     return DBLP_OK;
 }
 
-static AttnArgs make_args(const dblp_attention_t* a)
-{
-    AttnArgs r{};
-    r.B = a->batch; r.Sq = a->q_tokens; r.Sk = a->k_tokens; r.Hq = a->q_heads; r.Hkv = a->kv_heads; r.D = a->head_dim;
-    r.causal = a->flags & DBLP_ATTENTION_CAUSAL; r.scale = a->scale; r.q_lens = a->q_lens; r.k_lens = a->k_lens;
-    return r;
-}
-
 }  // namespace dblp
 
 using namespace dblp;
-
-extern "C" int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes)
-{
-    const int rc = check_shape("attention_workspace_bytes", a);
-    if (rc != DBLP_OK) return rc;
-    if (fwd_bytes) *fwd_bytes = 0;
-    if (grad_bytes) *grad_bytes = (size_t)a->batch * a->q_heads * a->q_tokens * 4;
-    return DBLP_OK;
-}
 
 #define DBLP_TRY(call)                      \
     do {                                    \
@@ -214,26 +117,35 @@ extern "C" int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t*
         if (rc_ != DBLP_OK) return rc_;     \
     } while (0)
 
+extern "C" int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes)
+{
+    DBLP_TRY(check_shape("attention_workspace_bytes", a));
+    if (fwd_bytes) *fwd_bytes = attention_forward_space(a);
+    if (grad_bytes) *grad_bytes = attention_backward_space(a);
+    return DBLP_OK;
+}
+
+static int check_space(const char* who, const void* ws, size_t ws_bytes, size_t need)
+{
+    DBLP_REQUIRE(need == 0 || ws, DBLP_EINVAL, "%s: the workspace is null", who);
+    DBLP_REQUIRE(need == 0 || ((uintptr_t)ws & 255) == 0, DBLP_EALIGN, "%s: the workspace is not 256-byte aligned", who);
+    DBLP_REQUIRE(ws_bytes >= need, DBLP_ECAPACITY, "%s: workspace of %zu bytes, needs %zu", who, ws_bytes, need);
+    return DBLP_OK;
+}
+
 extern "C" int dblp_attention(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                               const dblp_heads_t* out, float* lse, void* ws, size_t ws_bytes, void* stream)
 {
-    (void)ws; (void)ws_bytes;
     DBLP_TRY(check_shape("attention", a));
     if (a->batch == 0 || a->q_tokens == 0) return DBLP_OK;
     DBLP_TRY(check_heads("attention", "q", a, q, a->q_tokens, a->q_heads, false));
     DBLP_TRY(check_heads("attention", "out", a, out, a->q_tokens, a->q_heads, true));
-    AttnArgs r = make_args(a);
-    r.q = heads(q); r.o = heads(out); r.lse = lse;
     if (a->k_tokens) {
         DBLP_TRY(check_heads("attention", "k", a, k, a->k_tokens, a->kv_heads, false));
         DBLP_TRY(check_heads("attention", "v", a, v, a->k_tokens, a->kv_heads, false));
-        r.k = heads(k); r.v = heads(v);
     }
-    const dim3 grid((a->q_tokens + kAttnWarps - 1) / kAttnWarps, a->q_heads, a->batch);
-    if (a->dtype == DBLP_BF16) k_attention<__nv_bfloat16><<<grid, kAttnWarps * 32, 0, (cudaStream_t)stream>>>(r);
-    else k_attention<__half><<<grid, kAttnWarps * 32, 0, (cudaStream_t)stream>>>(r);
-    DBLP_LAUNCHED();
-    return DBLP_OK;
+    DBLP_TRY(check_space("attention", ws, ws_bytes, attention_forward_space(a)));
+    return attention_forward(a, q, k, v, out, lse, ws, (cudaStream_t)stream);
 }
 
 extern "C" int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
@@ -241,41 +153,30 @@ extern "C" int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t
                                    const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, size_t ws_bytes, void* stream)
 {
     DBLP_TRY(check_shape("attention_grad", a));
-    if (a->batch == 0) return DBLP_OK;
-    AttnArgs r = make_args(a);
+    if (a->batch == 0 || (a->q_tokens == 0 && a->k_tokens == 0)) return DBLP_OK;
     if (a->q_tokens) {
         DBLP_TRY(check_heads("attention_grad", "q", a, q, a->q_tokens, a->q_heads, false));
         DBLP_TRY(check_heads("attention_grad", "out", a, out, a->q_tokens, a->q_heads, false));
         DBLP_TRY(check_heads("attention_grad", "dout", a, dout, a->q_tokens, a->q_heads, false));
         DBLP_TRY(check_heads("attention_grad", "dq", a, dq, a->q_tokens, a->q_heads, true));
         DBLP_REQUIRE(lse, DBLP_EINVAL, "attention_grad: lse is null");
-        r.q = heads(q); r.o = heads(out); r.go = heads(dout); r.dq = heads(dq); r.lse = const_cast<float*>(lse);
     }
     if (a->k_tokens) {
         DBLP_TRY(check_heads("attention_grad", "k", a, k, a->k_tokens, a->kv_heads, false));
         DBLP_TRY(check_heads("attention_grad", "v", a, v, a->k_tokens, a->kv_heads, false));
         DBLP_TRY(check_heads("attention_grad", "dk", a, dk, a->k_tokens, a->kv_heads, true));
         DBLP_TRY(check_heads("attention_grad", "dv", a, dv, a->k_tokens, a->kv_heads, true));
-        r.k = heads(k); r.v = heads(v); r.dk = heads(dk); r.dv = heads(dv);
     }
-    size_t need = 0;
-    DBLP_TRY(dblp_attention_workspace_bytes(a, nullptr, &need));
-    DBLP_REQUIRE(need == 0 || (ws && ((uintptr_t)ws & 255) == 0), ws ? DBLP_EALIGN : DBLP_EINVAL,
-                 "attention_grad: the workspace is null or not 256-byte aligned");
-    DBLP_REQUIRE(ws_bytes >= need, DBLP_ECAPACITY, "attention_grad: workspace of %zu bytes, needs %zu", ws_bytes, need);
-    r.delta = (float*)ws;
-    cudaStream_t s = (cudaStream_t)stream;
-    const dim3 gq((a->q_tokens + kAttnWarps - 1) / kAttnWarps, a->q_heads, a->batch), gk((a->k_tokens + kAttnWarps - 1) / kAttnWarps, a->kv_heads, a->batch);
-    const bool bf = a->dtype == DBLP_BF16;
-    if (a->q_tokens) {
-        if (bf) k_attention_dq<__nv_bfloat16><<<gq, kAttnWarps * 32, 0, s>>>(r);
-        else k_attention_dq<__half><<<gq, kAttnWarps * 32, 0, s>>>(r);
-        DBLP_LAUNCHED();
-    }
-    if (a->k_tokens) {
-        if (bf) k_attention_dkv<__nv_bfloat16><<<gk, kAttnWarps * 32, 0, s>>>(r);
-        else k_attention_dkv<__half><<<gk, kAttnWarps * 32, 0, s>>>(r);
-        DBLP_LAUNCHED();
-    }
+    DBLP_TRY(check_space("attention_grad", ws, ws_bytes, attention_backward_space(a)));
+    return attention_backward(a, q, k, v, out, dout, lse, dq, dk, dv, ws, (cudaStream_t)stream);
+}
+
+extern "C" int dblp_wait_timeouts(uint64_t* count)
+{
+    DBLP_REQUIRE(count, DBLP_EINVAL, "wait_timeouts: null output");
+    unsigned long long* p = timeout_counter(), v = 0;
+    DBLP_REQUIRE(p, DBLP_ECUDA, "wait_timeouts: no device counter: %s", cudaGetErrorString(cudaGetLastError()));
+    DBLP_CUDA(cudaMemcpy(&v, p, sizeof(v), cudaMemcpyDeviceToHost));
+    *count = v;
     return DBLP_OK;
 }

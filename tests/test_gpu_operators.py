@@ -507,3 +507,7 @@ def test_gradient_is_the_difference_quotient():
         # each of the n gradient elements is off by about u of its size with a random sign; 8 standard deviations
         noise = 8 * 2 * U[F16] * (grad.double() * d).square().sum().sqrt().item() + 1e-4 * (grad.double() * d).abs().sum().item()
         assert abs((ends[0] - ends[1]) / (2 * eps) - along) <= noise
+
+
+def test_no_wait_ran_out():
+    assert dblp.dblp_wait_timeouts() == 0
