@@ -32,6 +32,44 @@ template <int DP> struct FwdSmem {
     static constexpr int kBytes = 1024 + TILE * (1 + STAGES);
 };
 
+// Scores from place `left` on become -infinity.
+template <int N> __device__ __forceinline__ void hide_from(uint32_t* x, uint32_t left)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if ((uint32_t)i >= left) x[i] = 0xFF800000u;
+}
+
+template <int N> __device__ __forceinline__ float largest(const uint32_t* x)
+{
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = __uint_as_float(x[i]);
+#pragma unroll
+    for (int i = 4; i < N; i += 8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            m[u] = i + 4 + u < N ? max3(m[u], __uint_as_float(x[i + u]), __uint_as_float(x[i + 4 + u])) : fmaxf(m[u], __uint_as_float(x[i + u]));
+    return max3(fmaxf(m[0], m[1]), m[2], m[3]);
+}
+
+// 32 scores -> 16 words of probabilities in tensor memory; their fp32 sum is added to `sum`.  Rounded to 16 bits because
+// that is the type of the product with v.
+template <typename T>
+__device__ __forceinline__ void probabilities(const uint32_t* x, float2 c2, float2 mc2, float2& sum, uint32_t dst)
+{
+    uint32_t p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float2 y = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, mc2);
+        y.x = exp2_fast(y.x);
+        y.y = exp2_fast(y.y);
+        sum = add2(sum, y);
+        p[i] = pack2<T>(y.x, y.y);
+    }
+    tmem_st16(dst, p);
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_constant__ FwdArgs a)
 {
@@ -142,7 +180,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(t_o, t_s + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
+                    mma_ts(t_o, t_s + 64 + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
                 mma_commit(&empty[st]);
                 if (j + 1 < nk) scores(j + 1);                  // overwrites p(j), which the product before has read by then
                 else mma_commit(&s_full);
@@ -162,55 +200,55 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, j & 1, g));
             if (!ok) break;
             tc_fence_after();
-            uint32_t x[128];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(t_s + lane_base + i * 32, x + i * 32);
-            tmem_wait_ld();
+            // All 128 scores for the maximum; the first 64 are then dropped and read again chunk by chunk, which keeps the
+            // thread below 168 registers.  p(j) goes to columns 64 .. 127 of s(j): those are in registers by then.
             const uint32_t left = seen > j * 128 ? seen - j * 128 : 0;
-            if (__any_sync(0xFFFFFFFFu, left < 128)) {
-#pragma unroll
-                for (int i = 0; i < 128; ++i)
-                    if ((uint32_t)i >= left) x[i] = 0xFF800000u;                                    // -infinity
+            const bool cut = __any_sync(0xFFFFFFFFu, left < 128);
+            uint32_t lo[64], hi[64];
+            tmem_ld32(t_s + lane_base, lo);
+            tmem_ld32(t_s + lane_base + 32, lo + 32);
+            tmem_ld32(t_s + lane_base + 64, hi);
+            tmem_ld32(t_s + lane_base + 96, hi + 32);
+            tmem_wait_ld<64>(lo);
+            tmem_loaded<64>(hi);
+            if (cut) {
+                hide_from<64>(lo, left);
+                hide_from<64>(hi, left > 64 ? left - 64 : 0);
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            const bool move = top > m + grow || (m == -INFINITY && top > m);
+            const float top = fmaxf(largest<64>(lo), largest<64>(hi));
+            const bool move = top > m + grow;                   // also from -infinity
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float alpha = move ? exp2_fast((m - top) * c) : 1.0f;                         // m = -infinity: 0
                 if (move) m = top;
                 l *= alpha;
                 if (j > 0) {
+#pragma unroll 1
+                    for (int i = 0; i < DP / 16; ++i) {
+                        uint32_t o[16];
+                        tmem_ld16(t_o + lane_base + i * 16, o);
+                        tmem_wait_ld<16>(o);
 #pragma unroll
-                    for (int i = 0; i < DP / 32; ++i) {
-                        uint32_t o[32];
-                        tmem_ld32(t_o + lane_base + i * 32, o);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int t = 0; t < 32; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * alpha);
-                        tmem_st32(t_o + lane_base + i * 32, o);
+                        for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * alpha);
+                        tmem_st16(t_o + lane_base + i * 16, o);
                     }
                 }
             }
             const float mc = m == -INFINITY ? 0.0f : -m * c;
             const float2 c2 = make_float2(c, c), mc2 = make_float2(mc, mc);
-            float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t p[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int e = half * 64 + 2 * i;
-                    float2 y = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, mc2);
-                    y.x = exp2_fast(y.x);
-                    y.y = exp2_fast(y.y);
-                    sum[i & 1] = add2(sum[i & 1], y);
-                    p[i] = pack2<T>(y.x, y.y);                  // 16 bits: the type of the product with v
-                }
-                tmem_st32(t_s + lane_base + half * 32, p);
-            }
-            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            float2 sum = make_float2(0.0f, 0.0f);
+            uint32_t again[32];
+            tmem_ld32(t_s + lane_base, again);
+            probabilities<T>(hi, c2, mc2, sum, t_s + lane_base + 96);
+            probabilities<T>(hi + 32, c2, mc2, sum, t_s + lane_base + 112);
+            tmem_wait_ld<32>(again);
+            uint32_t again2[32];
+            tmem_ld32(t_s + lane_base + 32, again2);
+            if (cut) hide_from<32>(again, left);
+            probabilities<T>(again, c2, mc2, sum, t_s + lane_base + 64);
+            tmem_wait_ld<32>(again2);
+            if (cut) hide_from<32>(again2, left > 32 ? left - 32 : 0);
+            probabilities<T>(again2, c2, mc2, sum, t_s + lane_base + 80);
+            l += sum.x + sum.y;
             tmem_wait_st();
             tc_fence_before();
             bar_arrive(&p_ready);
@@ -224,7 +262,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             for (int i = 0; i < DP / 32; ++i) {
                 uint32_t x[32];
                 tmem_ld32(t_o + lane_base + i * 32, x);
-                tmem_wait_ld();
+                tmem_wait_ld<32>(x);
 #pragma unroll
                 for (int t = 0; t < 32; t += 8) {
                     Vec8<T> w;
