@@ -1,129 +1,535 @@
-// dblp_attention_grad, one warp a row: the plain arrangement, fp32 throughout.
+// dblp_attention_grad on the tensor cores: one pass over the (key tile, query tile) pairs that recomputes the probabilities.
+//
+//   k_grad_rows   per query row D_i = <dout_i, out_i> and lse_i log2(e), padded to whole tiles: 2 x 4 bytes a row, so that
+//                 the main kernel needs neither out nor a reduction.
+//   k_grad        one block takes a share of the key tiles of one (sequence, key head) and walks, for each of them, over
+//                 all query tiles of the heads that share it.  With keys as rows and queries as columns:
+//                     s = k q^T          p = 2^(scale log2(e) s - lse log2(e))
+//                     dp = v dout^T      ds = p (dp - D)
+//                     dv += p dout       dk += ds q       dq(query tile) = ds^T k
+//                 p and ds are 16-bit left operands: p in tensor memory, ds in shared memory, where the same bytes are read
+//                 once along the rows (dk) and once across them (dq).  dk and dv stay in tensor memory until the key tile
+//                 is done and are written once; shared key heads sum in the same accumulator.
+//   k_grad_dq     adds the shares' dq, scales and rounds.
+// Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
+// two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
+// fill the machine; each costs a buffer of q's size in fp32.
+//   warps         0-7 p and ds (each thread one key and 64 queries), 8-11 dq to memory, 12 TMA, 13 products.
 #include <math.h>
 
 #include "attention.cuh"
 
 namespace dblp {
 
-constexpr int kAttnWarps = 8;
-constexpr int kPerLane = 4;                 // head_dim <= 128
+constexpr int kGradThreads = 448;
 
-struct AttnArgs {
-    Heads q, k, v, o, go, dq, dk, dv;
-    float *lse, *delta;
-    uint32_t B, Sq, Sk, Hq, Hkv, D, causal;
-    float scale;
-    const int32_t *q_lens, *k_lens;
+struct GradArgs {
+    TileSource q, k, v, go;
+    Heads dk, dv;
+    const float2* rows;        // [B][Hq][tiles][2][128]: lse log2(e) then D, as floats
+    float4* dq;                // [R][B][Hq][tiles][D / 4 of DP][128]
+    AttnShape s;
+    float scale, scale_log2;
+    uint32_t q_tiles, k_tiles, shares;
+    unsigned long long* timeouts;
 };
 
-template <typename T>
-__device__ __forceinline__ const T* row_of(const Heads& h, uint32_t b, uint32_t t, uint32_t head)
+// Key tile number n of share r: to and fro, so that under a causal mask the shares get like amounts of work.
+__device__ __forceinline__ uint32_t share_tile(uint32_t r, uint32_t n, uint32_t shares)
 {
-    return (const T*)h.p + (int64_t)b * h.sb + (int64_t)t * h.st + (int64_t)head * h.sh;
+    return n * shares + (n & 1 ? shares - 1 - r : r);
+}
+// First query tile that sees key tile j, and the number of query tiles that see any key.
+__device__ __forceinline__ uint32_t first_query_tile(uint32_t j, uint32_t lq, uint32_t lk, uint32_t causal)
+{
+    if (!causal) return 0;
+    const int32_t i = (int32_t)(j * 128 + lq) - (int32_t)lk;            // first query that sees key 128 j
+    return i > 0 ? (uint32_t)i / 128 : 0;
 }
 
+// ---- rows ------------------------------------------------------------------------------------------------------------
+// A warp takes four rows at a time, eight lanes a row, 16 bytes a load.
 template <typename T>
-__device__ __forceinline__ void load_row(const T* p, uint32_t D, uint32_t lane, float* x)
+__global__ void __launch_bounds__(256)
+k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict__ rows, AttnShape s, uint32_t q_tiles)
 {
+    const uint32_t lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z, lq = length_of(s.q_lens, b, s.Sq), lk = length_of(s.k_lens, b, s.Sk);
+    const uint32_t i = blockIdx.x * 32 + (threadIdx.x >> 5) * 4 + (lane >> 3);
+    const bool live = keys_of(i, lq, lk, s.causal) > 0;
+    float d = 0.0f;
+    if (live) {
+        const T* po = (const T*)o.p + (int64_t)b * o.sb + (int64_t)i * o.st + (int64_t)h * o.sh;
+        const T* pg = (const T*)go.p + (int64_t)b * go.sb + (int64_t)i * go.st + (int64_t)h * go.sh;
+        for (uint32_t c = (lane & 7) * 8; c < s.D; c += 64) {
+            Vec8<T> vo, vg;
+            float x[8], y[8];
+            vo.load(po + c);
+            vg.load(pg + c);
+            vo.get(x);
+            vg.get(y);
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) x[i] = lane + 32 * i < D ? to_f32(p[lane + 32 * i]) : 0.0f;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_row(const Heads& h, uint32_t b, uint32_t t, uint32_t head, uint32_t D, uint32_t lane, const float* x)
-{
-    T* p = const_cast<T*>(row_of<T>(h, b, t, head));
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-        if (lane + 32 * i < D) p[lane + 32 * i] = from_f32<T>(x[i]);
-}
-
-__device__ __forceinline__ float dot_rows(const float* a, const float* b)
-{
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) s += a[i] * b[i];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    return s;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kAttnWarps * 32) k_attention_dq(AttnArgs a)
-{
-    const uint32_t lane = threadIdx.x & 31, i = blockIdx.x * kAttnWarps + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-    if (i >= a.Sq) return;
-    const uint32_t hk = h / (a.Hq / a.Hkv), n = keys_of(i, length_of(a.q_lens, b, a.Sq), length_of(a.k_lens, b, a.Sk), a.causal);
-    const uint64_t at = ((uint64_t)b * a.Hq + h) * a.Sq + i;
-    float q[kPerLane], x[kPerLane], g[kPerLane], dq[kPerLane] = {};
-    load_row(row_of<T>(a.q, b, i, h), a.D, lane, q);
-    load_row(row_of<T>(a.go, b, i, h), a.D, lane, g);
-    load_row(row_of<T>(a.o, b, i, h), a.D, lane, x);
-    const float delta = dot_rows(g, x), lse = a.lse[at];
-    if (lane == 0) a.delta[at] = delta;
-    for (uint32_t j = 0; j < n; ++j) {
-        load_row(row_of<T>(a.v, b, j, hk), a.D, lane, x);
-        const float dp = dot_rows(g, x);
-        load_row(row_of<T>(a.k, b, j, hk), a.D, lane, x);
-        const float ds = expf(dot_rows(q, x) * a.scale - lse) * (dp - delta);
-#pragma unroll
-        for (int t = 0; t < kPerLane; ++t) dq[t] += ds * x[t];
+            for (int t = 0; t < 8; ++t) d += x[t] * y[t];
+        }
     }
 #pragma unroll
-    for (int t = 0; t < kPerLane; ++t) dq[t] *= a.scale;
-    store_row<T>(a.dq, b, i, h, a.D, lane, dq);
+    for (int t = 4; t; t >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, t);
+    if ((lane & 7) == 0 && i < q_tiles * 128) {
+        float* r = rows + (((uint64_t)b * s.Hq + h) * q_tiles + i / 128) * 256 + i % 128;
+        // rows that see nothing: 2^(s - infinity) = 0
+        r[0] = live ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i] * 1.4426950408889634f : INFINITY;
+        r[128] = live ? d : 0.0f;
+    }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kAttnWarps * 32) k_attention_dkv(AttnArgs a)
+// ---- main ------------------------------------------------------------------------------------------------------------
+template <int DP> struct GradSmem {
+    static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes;
+    static constexpr int NQ = 2, NG = DP == 64 ? 2 : 1;                 // stages of q (with its row values) and of dout
+    static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, ROWS = DS + 2 * (int)kBlockBytes;
+    static constexpr int kBytes = 1024 + ROWS + NQ * 1024;
+};
+
+__device__ __forceinline__ void add4(float4* p, float4 v)
 {
-    const uint32_t lane = threadIdx.x & 31, j = blockIdx.x * kAttnWarps + (threadIdx.x >> 5), hk = blockIdx.y, b = blockIdx.z;
-    if (j >= a.Sk) return;
-    const uint32_t rep = a.Hq / a.Hkv, lq = length_of(a.q_lens, b, a.Sq), lk = length_of(a.k_lens, b, a.Sk);
-    float k[kPerLane], v[kPerLane], x[kPerLane], g[kPerLane], dk[kPerLane] = {}, dv[kPerLane] = {};
-    if (j < lk) {
-        load_row(row_of<T>(a.k, b, j, hk), a.D, lane, k);
-        load_row(row_of<T>(a.v, b, j, hk), a.D, lane, v);
-        const int64_t first = a.causal ? max((int64_t)0, (int64_t)j + lq - lk) : 0;
-        for (uint32_t h = hk * rep; h < hk * rep + rep; ++h)
-            for (uint32_t i = (uint32_t)first; i < lq; ++i) {
-                const uint64_t at = ((uint64_t)b * a.Hq + h) * a.Sq + i;
-                load_row(row_of<T>(a.q, b, i, h), a.D, lane, x);
-                load_row(row_of<T>(a.go, b, i, h), a.D, lane, g);
-                const float p = expf(dot_rows(x, k) * a.scale - a.lse[at]), ds = p * (dot_rows(g, v) - a.delta[at]) * a.scale;
-#pragma unroll
-                for (int t = 0; t < kPerLane; ++t) { dv[t] += p * g[t]; dk[t] += ds * x[t]; }
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant__ GradArgs a)
+{
+    using L = GradSmem<DP>;
+    constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG;
+    constexpr bool kOwnDq = DP == 64;                          // dq has columns of its own; else it takes those of dp
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t kv_full, q_full[NQ], q_empty[NQ], g_full[NG], g_empty[NG], cut_full;
+    __shared__ uint64_t s_full, p_ready, dp_full, ds_ready, ds_free, dq_full, dq_free, acc_full, acc_free, idle;
+    __shared__ uint32_t tmem_slot, dead;
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t share = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const uint32_t lq = length_of(a.s.q_lens, b, a.s.Sq), lk = length_of(a.s.k_lens, b, a.s.Sk);
+    const uint32_t nq = (lq + 127) / 128, nk = lq ? (lk + 127) / 128 : 0;
+    // query tiles per head that key tile j meets
+    auto meets = [&](uint32_t j) -> uint32_t {
+        if (j >= nk) return 0;
+        const uint32_t i0 = first_query_tile(j, lq, lk, a.s.causal);
+        return i0 < nq ? nq - i0 : 0;
+    };
+
+    if (tid == 0) {
+        dead = 0;
+        for (uint64_t* p : {&kv_full, &cut_full, &s_full, &dp_full, &ds_free, &dq_full, &acc_full, &idle}) bar_init(p, 1);
+        for (int i = 0; i < NQ; ++i) { bar_init(&q_full[i], 1); bar_init(&q_empty[i], 1); }
+        for (int i = 0; i < NG; ++i) { bar_init(&g_full[i], 1); bar_init(&g_empty[i], 1); }
+        bar_init(&p_ready, 256);
+        bar_init(&ds_ready, 256);
+        bar_init(&acc_free, 256);
+        bar_init(&dq_free, 128);
+        fence_bar_init();
+    }
+    if (warp == 13) tmem_alloc<512>(&tmem_slot);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
+    const uint32_t t_dq = kOwnDq ? tmem + 384 : t_dp;
+    const Guard g{&dead, a.timeouts};
+
+    if (warp == 12) {                                           // ---- TMA
+        uint32_t n = 0, w = 0, cuts = 0;                        // pairs, key tiles with work, tiles that were cleared
+        bool ok = true;
+        // a tile whose rows from `first` on do not count but may hold anything
+        auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t first) {
+            if (lane == 0) {
+                bar_expect(&cut_full, L::TILE);
+                load_tile<NS>(dst, src, &cut_full, token, head, b);
             }
+            bar_drain(&cut_full, cuts++ & 1);
+            __syncwarp();
+            clear_rows<NS>(dst, first);
+            __syncwarp();
+        };
+        for (uint32_t m = 0; ok; ++m) {
+            const uint32_t j = share_tile(share, m, a.shares);
+            if (m * a.shares >= a.k_tiles) break;
+            const uint32_t per_head = meets(j);
+            if (per_head == 0) continue;
+            if (w) ok = __all_sync(0xFFFFFFFFu, bar_wait(&acc_full, (w - 1) & 1, g));   // products of the tile before are done
+            if (!ok) break;
+            const bool kcut = j * 128 + 128 > lk && lk < a.s.Sk;
+            if (kcut) load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
+            if (lane == 0) {
+                bar_expect(&kv_full, kcut ? L::TILE : 2 * L::TILE);
+                if (!kcut) load_tile<NS>(smem + L::K, a.k, &kv_full, j * 128, hk, b);
+                load_tile<NS>(smem + L::V, a.v, &kv_full, j * 128, hk, b);
+            }
+            ++w;
+            for (uint32_t t = 0; t < per_head * a.s.rep && ok; ++t, ++n) {
+                const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
+                const bool cut = i * 128 + 128 > lq && lq < a.s.Sq;
+                const uint32_t sq = n % NQ, sg = n % NG;
+                if (n >= NQ) ok = __all_sync(0xFFFFFFFFu, bar_wait(&q_empty[sq], (n / NQ - 1) & 1, g));
+                if (!ok) break;
+                uint8_t *dq_ = smem + L::Q + sq * L::TILE, *dg = smem + L::G + sg * L::TILE;
+                if (cut) load_cut(dq_, a.q, i * 128, h, lq - i * 128);
+                if (lane == 0) {
+                    bar_expect(&q_full[sq], (cut ? 0 : L::TILE) + 1024);
+                    if (!cut) load_tile<NS>(dq_, a.q, &q_full[sq], i * 128, h, b);
+                    bulk_load(smem + L::ROWS + sq * 1024, (const float*)a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &q_full[sq]);
+                }
+                if (n >= NG) ok = __all_sync(0xFFFFFFFFu, bar_wait(&g_empty[sg], (n / NG - 1) & 1, g));
+                if (!ok) { if (lane == 0) bar_drain(&q_full[sq], (n / NQ) & 1); break; }
+                if (cut) load_cut(dg, a.go, i * 128, h, lq - i * 128);
+                if (lane == 0) {
+                    if (cut) {
+                        bar_arrive(&g_full[sg]);
+                    } else {
+                        bar_expect(&g_full[sg], L::TILE);
+                        load_tile<NS>(dg, a.go, &g_full[sg], i * 128, h, b);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) {                                        // every copy lands before the block may end
+            if (w) bar_drain(&kv_full, (w - 1) & 1);
+            for (uint32_t x = n > NQ ? n - NQ : 0; x < n; ++x) bar_drain(&q_full[x % NQ], (x / NQ) & 1);
+            for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&g_full[x % NG], (x / NG) & 1);
+        }
+    } else if (warp == 13) {                                    // ---- products
+        if (lane == 0) {
+            constexpr uint32_t id_kk = mma_desc<T>(128, 128, false, false);     // s, dp
+            constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);       // dv, dk: right operand across its rows
+            constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);        // dq: both across their rows
+            const uint32_t base = smem_addr(smem);
+            uint32_t n = 0, w = 0;
+            bool ok = true;
+            auto scores = [&](uint32_t x) {
+                ok = ok && bar_wait(&q_full[x % NQ], (x / NQ) & 1, g);
+                if (!ok) return;
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
+                    mma_ss(t_s, desc_k(base + L::K + off), desc_k(base + L::Q + (x % NQ) * L::TILE + off), id_kk, kk > 0);
+                }
+                mma_commit(&s_full);
+            };
+            for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
+                const uint32_t pairs = meets(share_tile(share, m, a.shares)) * a.s.rep;
+                if (pairs == 0) continue;
+                ok = bar_wait(&kv_full, w & 1, g);
+                scores(n);
+                for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
+                    const uint32_t qa = base + L::Q + (n % NQ) * L::TILE, ga = base + L::G + (n % NG) * L::TILE;
+                    ok = bar_wait(&g_full[n % NG], (n / NG) & 1, g);
+                    if (ok && !kOwnDq && n) ok = bar_wait(&dq_free, (n - 1) & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk) {
+                        const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
+                        mma_ss(t_dp, desc_k(base + L::V + off), desc_k(ga + off), id_kk, kk > 0);
+                    }
+                    mma_commit(&dp_full);
+                    ok = bar_wait(&p_ready, n & 1, g);
+                    if (ok && t == 0 && w) ok = bar_wait(&acc_free, (w - 1) & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)              // p of queries 0-63 in columns 0-31, of 64-127 in 64-95
+                        mma_ts(t_dv, t_s + (kk / 4) * 64 + (kk % 4) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
+                    mma_commit(&g_empty[n % NG]);
+                    if (t + 1 < pairs) scores(n + 1);           // over p(n), which the product before has read by then
+                    ok = ok && bar_wait(&ds_ready, n & 1, g);
+                    if (ok && kOwnDq && n) ok = bar_wait(&dq_free, (n - 1) & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_ss(t_dq, desc_mn(base + L::DS + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
+                    mma_commit(&dq_full);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_ss(t_dk, desc_k(base + L::DS + (kk / 4) * kBlockBytes + (kk % 4) * 32), desc_mn(qa + kk * 2048, kBlockBytes), id_kv,
+                               t > 0 || kk > 0);
+                    mma_commit(&q_empty[n % NQ]);
+                    mma_commit(&ds_free);
+                }
+                if (ok) mma_commit(&acc_full);
+                ++w;
+            }
+            if (!ok) {                                          // products in flight end before the memory is freed
+                mma_commit(&idle);
+                bar_drain(&idle, 0);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 8) {                                     // ---- dq: tensor memory -> this share's buffer
+        const uint32_t lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
+        uint32_t n = 0;
+        bool ok = true;
+        for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
+            const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j);
+            for (uint32_t t = 0; t < per_head * a.s.rep; ++t, ++n) {
+                const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
+                float4* dst = a.dq + (((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * (DP / 4)) * 128 + row;
+                ok = __all_sync(0xFFFFFFFFu, bar_wait(&dq_full, n & 1, g));
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < DP; c += 64) {
+                    uint32_t x[64];
+                    tmem_ld32(t_dq + lane_base + c, x);
+                    tmem_ld32(t_dq + lane_base + c + 32, x + 32);
+                    tmem_wait_ld<64>(x);
+                    if (c + 64 == DP) {
+                        tc_fence_before();
+                        bar_arrive(&dq_free);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 64; e += 4) {
+                        const float4 v = make_float4(__uint_as_float(x[e]), __uint_as_float(x[e + 1]), __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+                        float4* p = dst + (c + e) / 4 * 128;
+                        if (m == 0) *p = v;                     // the share's first key tile is every query tile's first
+                        else add4(p, v);
+                    }
+                }
+            }
+        }
+    } else {                                                    // ---- p and ds: thread = key (lane of the tile), 64 queries
+        const uint32_t half = warp >> 2, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
+        const uint32_t my_s = t_s + lane_base + half * 64, my_dp = t_dp + lane_base + half * 64;
+        uint8_t* ds_row = smem + L::DS + half * kBlockBytes + row * 128;
+        const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
+        uint32_t n = 0, w = 0;
+        bool ok = true;
+        for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
+            const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * a.s.rep;
+            if (j >= a.k_tiles) continue;
+            const uint32_t key = j * 128 + row;
+            for (uint32_t t = 0; t < pairs; ++t, ++n) {
+                const uint32_t i = nq - per_head + t % per_head;
+                // queries [from, 64) of this thread's columns see the key
+                int32_t from = key < lk ? 0 : 64;
+                if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + half * 64));
+                const bool cut = __any_sync(0xFFFFFFFFu, from > 0);
+                const float4* lse4 = reinterpret_cast<const float4*>(smem + L::ROWS + (n % NQ) * 1024) + half * 16;
+                ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, n & 1, g) && bar_wait(&q_full[n % NQ], (n / NQ) & 1, g));
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t p[64];
+                tmem_ld32(my_s, p);
+                tmem_ld32(my_s + 32, p + 32);
+                tmem_wait_ld<64>(p);
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                    const float4 l4 = lse4[e / 4];
+                    float2 u = fma2(make_float2(__uint_as_float(p[e]), __uint_as_float(p[e + 1])), c2, make_float2(-l4.x, -l4.y));
+                    float2 v = fma2(make_float2(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])), c2, make_float2(-l4.z, -l4.w));
+                    p[e] = __float_as_uint(exp2_fast(u.x));
+                    p[e + 1] = __float_as_uint(exp2_fast(u.y));
+                    p[e + 2] = __float_as_uint(exp2_fast(v.x));
+                    p[e + 3] = __float_as_uint(exp2_fast(v.y));
+                }
+                if (cut) {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (e < from) p[e] = 0;
+                }
+                {
+                    uint32_t q16[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) q16[e] = pack2<T>(__uint_as_float(p[2 * e]), __uint_as_float(p[2 * e + 1]));
+                    tmem_st32(my_s, q16);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                bar_arrive(&p_ready);
+
+                ok = __all_sync(0xFFFFFFFFu, bar_wait(&dp_full, n & 1, g));
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t x[64];
+                tmem_ld32(my_dp, x);
+                tmem_ld32(my_dp + 32, x + 32);
+                tmem_wait_ld<64>(x);
+                const float4* d4 = lse4 + 32;
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                    const float4 d = d4[e / 4];
+                    const float2 u = mul2(make_float2(__uint_as_float(p[e]), __uint_as_float(p[e + 1])),
+                                          add2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), make_float2(-d.x, -d.y)));
+                    const float2 v = mul2(make_float2(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])),
+                                          add2(make_float2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), make_float2(-d.z, -d.w)));
+                    p[e] = __float_as_uint(u.x);
+                    p[e + 1] = __float_as_uint(u.y);
+                    p[e + 2] = __float_as_uint(v.x);
+                    p[e + 3] = __float_as_uint(v.y);
+                }
+                if (cut) {                                      // 0 * (dp of a row that does not count) may be NaN
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if (e < from) p[e] = 0;
+                }
+                if (n) ok = __all_sync(0xFFFFFFFFu, bar_wait(&ds_free, (n - 1) & 1, g));
+                if (!ok) break;
+#pragma unroll
+                for (int e = 0; e < 64; e += 8) {
+                    const uint4 u = make_uint4(pack2<T>(__uint_as_float(p[e]), __uint_as_float(p[e + 1])), pack2<T>(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])),
+                                               pack2<T>(__uint_as_float(p[e + 4]), __uint_as_float(p[e + 5])), pack2<T>(__uint_as_float(p[e + 6]), __uint_as_float(p[e + 7])));
+                    *reinterpret_cast<uint4*>(ds_row + (((e / 8) ^ (row & 7)) << 4)) = u;
+                }
+                fence_async_smem();
+                tc_fence_before();
+                bar_arrive(&ds_ready);
+            }
+            if (!ok) break;
+            // this key tile's gradients: the first four warps dv, the others dk
+            const Heads& hd = half ? a.dk : a.dv;
+            T* dst = (T*)hd.p + (int64_t)b * hd.sb + (int64_t)key * hd.st + (int64_t)hk * hd.sh;
+            const float f = half ? a.scale : 1.0f;
+            if (pairs) {
+                ok = __all_sync(0xFFFFFFFFu, bar_wait(&acc_full, w & 1, g));
+                if (!ok) break;
+                tc_fence_after();
+            }
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t x[32];
+                if (pairs) {
+                    tmem_ld32((half ? t_dk : t_dv) + lane_base + c, x);
+                    tmem_wait_ld<32>(x);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    Vec8<T> o;
+                    float y[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) y[u] = pairs ? __uint_as_float(x[e + u]) * f : 0.0f;
+                    o.set(y);
+                    if (key < a.s.Sk && (uint32_t)(c + e) < a.s.D) o.store(dst + c + e);
+                }
+            }
+            if (pairs) {
+                tc_fence_before();
+                bar_arrive(&acc_free);
+                ++w;
+            }
+        }
     }
-    store_row<T>(a.dk, b, j, hk, a.D, lane, dk);
-    store_row<T>(a.dv, b, j, hk, a.D, lane, dv);
+    __syncthreads();
+    if (warp == 13) {
+        tc_fence_after();
+        tmem_free<512>(tmem);
+    }
 }
 
-size_t attention_backward_space(const dblp_attention_t* a) { return (size_t)a->batch * a->q_heads * a->q_tokens * 4; }
+// ---- dq --------------------------------------------------------------------------------------------------------------
+// Thread: one query, 8 of its columns at a time.  Share r has a part of query tile i iff its first key tile, r, meets it.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part, Heads dq, AttnShape s, float scale, uint32_t q_tiles, uint32_t shares)
+{
+    const uint32_t i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row = threadIdx.x & 127, token = i * 128 + row;
+    const uint32_t lq = length_of(s.q_lens, b, s.Sq), lk = length_of(s.k_lens, b, s.Sk);
+    const uint32_t most = i * 128 < lq ? keys_of(min(lq, i * 128 + 128) - 1, lq, lk, s.causal) : 0, parts = min(shares, (most + 127) / 128);
+    if (token >= s.Sq) return;
+    T* dst = (T*)dq.p + (int64_t)b * dq.sb + (int64_t)token * dq.st + (int64_t)h * dq.sh;
+    const uint64_t stride = (uint64_t)s.B * s.Hq * q_tiles * (DP / 4) * 128;
+    const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row;
+#pragma unroll 4
+    for (uint32_t c = (threadIdx.x >> 7) * 8; c < s.D; c += 16) {
+        float y[8] = {};
+        for (uint32_t r = 0; r < parts; ++r) {
+            const float4 u = src[r * stride + c / 4 * 128], v = src[r * stride + (c / 4 + 1) * 128];
+            y[0] += u.x; y[1] += u.y; y[2] += u.z; y[3] += u.w;
+            y[4] += v.x; y[5] += v.y; y[6] += v.z; y[7] += v.w;
+        }
+#pragma unroll
+        for (int t = 0; t < 8; ++t) y[t] *= scale;
+        Vec8<T> o;
+        o.set(y);
+        o.store(dst + c);
+    }
+}
+
+// Shares per (sequence, key head): blocks run one to an SM, so the last round of blocks should be full; every further share
+// costs a pass over q's size in fp32.  Among R up to 8 (and no more than there are key tiles) take the least
+// rounds(R) / R, with 4 % for each share.
+static uint32_t shares_of(const dblp_attention_t* a)
+{
+    const uint64_t groups = (uint64_t)a->batch * a->kv_heads, tiles = (a->k_tokens + 127) / 128, sms = 148;
+    uint32_t best = 1;
+    double least = 1e300;
+    for (uint32_t r = 1; r <= 8 && r <= tiles; ++r) {
+        const double cost = (double)((groups * r + sms - 1) / sms) * (double)((tiles + r - 1) / r) * (1.0 + 0.04 * r);
+        if (cost < least) { least = cost; best = r; }
+    }
+    return best;
+}
+
+struct GradSpaceA {
+    uint64_t rows, dq, bytes;
+    explicit GradSpaceA(const dblp_attention_t* a)
+    {
+        const uint64_t tiles = (uint64_t)a->batch * a->q_heads * ((a->q_tokens + 127) / 128), dp = a->head_dim <= 64 ? 64 : 128;
+        rows = 0;
+        dq = tiles * 1024;
+        bytes = dq + (a->k_tokens ? shares_of(a) * tiles * 128 * dp * 4 : 0);
+    }
+};
+
+size_t attention_backward_space(const dblp_attention_t* a) { return GradSpaceA(a).bytes; }
+
+template <typename T, int DP>
+static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* lse, Heads dq, cudaStream_t s)
+{
+    const AttnShape& sh = r.s;
+    if (sh.Sq) {
+        k_grad_rows<T><<<dim3(r.q_tiles * 4, sh.Hq, sh.B), 256, 0, s>>>(o, go, lse, (float*)r.rows, sh, r.q_tiles);
+        DBLP_LAUNCHED();
+    }
+    if (sh.Sk) {
+        DBLP_CUDA(cudaFuncSetAttribute(k_grad<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, GradSmem<DP>::kBytes));
+        k_grad<T, DP><<<dim3(r.shares, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
+        DBLP_LAUNCHED();
+    }
+    if (sh.Sq) {
+        k_grad_dq<T, DP><<<dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s>>>(r.dq, dq, sh, r.scale, r.q_tiles, r.shares);
+        DBLP_LAUNCHED();
+    }
+    return DBLP_OK;
+}
 
 int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                        const dblp_heads_t* out, const dblp_heads_t* dout, const float* lse, const dblp_heads_t* dq,
                        const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, cudaStream_t s)
 {
-    AttnArgs r{};
-    r.B = a->batch; r.Sq = a->q_tokens; r.Sk = a->k_tokens; r.Hq = a->q_heads; r.Hkv = a->kv_heads; r.D = a->head_dim;
-    r.causal = a->flags & DBLP_ATTENTION_CAUSAL; r.scale = a->scale; r.q_lens = a->q_lens; r.k_lens = a->k_lens;
-    r.q = heads(q); r.k = heads(k); r.v = heads(v); r.o = heads(out); r.go = heads(dout);
-    r.dq = heads(dq); r.dk = heads(dk); r.dv = heads(dv); r.lse = const_cast<float*>(lse);
-    r.delta = (float*)ws;
-    const dim3 gq((a->q_tokens + kAttnWarps - 1) / kAttnWarps, a->q_heads, a->batch), gk((a->k_tokens + kAttnWarps - 1) / kAttnWarps, a->kv_heads, a->batch);
-    const bool bf = a->dtype == DBLP_BF16;
-    if (a->q_tokens) {
-        if (bf) k_attention_dq<__nv_bfloat16><<<gq, kAttnWarps * 32, 0, s>>>(r);
-        else k_attention_dq<__half><<<gq, kAttnWarps * 32, 0, s>>>(r);
-        DBLP_LAUNCHED();
-    }
-    if (a->k_tokens) {
-        if (bf) k_attention_dkv<__nv_bfloat16><<<gk, kAttnWarps * 32, 0, s>>>(r);
-        else k_attention_dkv<__half><<<gk, kAttnWarps * 32, 0, s>>>(r);
-        DBLP_LAUNCHED();
-    }
-    return DBLP_OK;
+    GradArgs r{};
+    int rc = DBLP_OK;
+    if (a->q_tokens) rc = make_source(&r.q, a, q, a->q_tokens, a->q_heads);
+    if (rc == DBLP_OK && a->q_tokens) rc = make_source(&r.go, a, dout, a->q_tokens, a->q_heads);
+    if (rc == DBLP_OK && a->k_tokens) rc = make_source(&r.k, a, k, a->k_tokens, a->kv_heads);
+    if (rc == DBLP_OK && a->k_tokens) rc = make_source(&r.v, a, v, a->k_tokens, a->kv_heads);
+    if (rc != DBLP_OK) return rc;
+    const GradSpaceA sp(a);
+    r.dk = heads(dk);
+    r.dv = heads(dv);
+    r.rows = (const float2*)((uint8_t*)ws + sp.rows);
+    r.dq = (float4*)((uint8_t*)ws + sp.dq);
+    r.s = shape_of(a);
+    r.scale = a->scale;
+    r.scale_log2 = (float)(a->scale * 1.4426950408889634);
+    r.q_tiles = (a->q_tokens + 127) / 128;
+    r.k_tiles = (a->k_tokens + 127) / 128;
+    r.shares = a->k_tokens ? shares_of(a) : 0;
+    r.timeouts = timeout_counter();
+    DBLP_REQUIRE(r.timeouts, DBLP_ECUDA, "attention_grad: device setup failed: %s", cudaGetErrorString(cudaGetLastError()));
+    const Heads o = heads(out), go = heads(dout), hq = heads(dq);
+    if (a->dtype == DBLP_BF16)
+        return a->head_dim <= 64 ? launch_backward<__nv_bfloat16, 64>(r, o, go, lse, hq, s) : launch_backward<__nv_bfloat16, 128>(r, o, go, lse, hq, s);
+    return a->head_dim <= 64 ? launch_backward<__half, 64>(r, o, go, lse, hq, s) : launch_backward<__half, 128>(r, o, go, lse, hq, s);
 }
 
 }  // namespace dblp
