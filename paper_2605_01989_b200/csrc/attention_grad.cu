@@ -1,7 +1,7 @@
 // dblp_attention_grad on the tensor cores: one pass over the (key tile, query tile) pairs that recomputes the probabilities.
 //
-//   k_grad_rows   per query row D_i = <dout_i, out_i> and lse_i log2(e), padded to whole tiles: 2 x 4 bytes a row, so that
-//                 the main kernel needs neither out nor a reduction.
+//   k_grad_rows   per query row -D_i = -<dout_i, out_i> and -lse_i log2(e), padded to whole tiles: 2 x 4 bytes a row, so
+//                 that the main kernel needs neither out nor a reduction.
 //   k_grad        one block takes a share of the key tiles of one (sequence, key head) and walks, for each of them, over
 //                 all query tiles of the heads that share it.  With keys as rows and queries as columns:
 //                     s = k q^T          p = 2^(scale log2(e) s - lse log2(e))
@@ -26,7 +26,7 @@ constexpr int kGradThreads = 448;
 struct GradArgs {
     TileSource q, k, v, go;
     Heads dk, dv;
-    const float2* rows;        // [B][Hq][tiles][2][128]: lse log2(e) then D, as floats
+    const float* rows;         // [B][Hq][tiles][2][128]: -lse log2(e), then -D
     float4* dq;                // [R][B][Hq][tiles][D / 4 of DP][128]
     AttnShape s;
     float scale, scale_log2;
@@ -76,8 +76,8 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
     if ((lane & 7) == 0 && i < q_tiles * 128) {
         float* r = rows + (((uint64_t)b * s.Hq + h) * q_tiles + i / 128) * 256 + i % 128;
         // rows that see nothing: 2^(s - infinity) = 0
-        r[0] = live ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i] * 1.4426950408889634f : INFINITY;
-        r[128] = live ? d : 0.0f;
+        r[0] = live ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i] * -1.4426950408889634f : -INFINITY;
+        r[128] = live ? -d : 0.0f;
     }
 }
 
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 if (lane == 0) {
                     bar_expect(&q_full[sq], (cut ? 0 : L::TILE) + 1024);
                     if (!cut) load_tile<NS>(dq_, a.q, &q_full[sq], i * 128, h, b);
-                    bulk_load(smem + L::ROWS + sq * 1024, (const float*)a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &q_full[sq]);
+                    bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &q_full[sq]);
                 }
                 if (n >= NG) ok = __all_sync(0xFFFFFFFFu, bar_wait(&g_empty[sg], (n / NG - 1) & 1, g));
                 if (!ok) { if (lane == 0) bar_drain(&q_full[sq], (n / NQ) & 1); break; }
@@ -216,23 +216,26 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 }
                 mma_commit(&s_full);
             };
+            auto dprobs = [&](uint32_t x) {
+                ok = ok && bar_wait(&g_full[x % NG], (x / NG) & 1, g);
+                if (ok && !kOwnDq && x) ok = bar_wait(&dq_free, (x - 1) & 1, g);
+                if (!ok) return;
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
+                    mma_ss(t_dp, desc_k(base + L::V + off), desc_k(base + L::G + (x % NG) * L::TILE + off), id_kk, kk > 0);
+                }
+                mma_commit(&dp_full);
+            };
             for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
                 const uint32_t pairs = meets(share_tile(share, m, a.shares)) * a.s.rep;
                 if (pairs == 0) continue;
                 ok = bar_wait(&kv_full, w & 1, g);
                 scores(n);
+                dprobs(n);
                 for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
                     const uint32_t qa = base + L::Q + (n % NQ) * L::TILE, ga = base + L::G + (n % NG) * L::TILE;
-                    ok = bar_wait(&g_full[n % NG], (n / NG) & 1, g);
-                    if (ok && !kOwnDq && n) ok = bar_wait(&dq_free, (n - 1) & 1, g);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) {
-                        const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                        mma_ss(t_dp, desc_k(base + L::V + off), desc_k(ga + off), id_kk, kk > 0);
-                    }
-                    mma_commit(&dp_full);
                     ok = bar_wait(&p_ready, n & 1, g);
                     if (ok && t == 0 && w) ok = bar_wait(&acc_free, (w - 1) & 1, g);
                     if (!ok) break;
@@ -243,6 +246,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     mma_commit(&g_empty[n % NG]);
                     if (t + 1 < pairs) scores(n + 1);           // over p(n), which the product before has read by then
                     ok = ok && bar_wait(&ds_ready, n & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (kOwnDq && t + 1 < pairs) dprobs(n + 1); // dp(n) has been read: the next pair need not wait for dq, dk
                     if (ok && kOwnDq && n) ok = bar_wait(&dq_free, (n - 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
@@ -256,6 +262,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                                t > 0 || kk > 0);
                     mma_commit(&q_empty[n % NQ]);
                     mma_commit(&ds_free);
+                    if (!kOwnDq && t + 1 < pairs) dprobs(n + 1);
                 }
                 if (ok) mma_commit(&acc_full);
                 ++w;
@@ -266,7 +273,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             }
         }
         __syncwarp();
-    } else if (warp >= 8) {                                     // ---- dq: tensor memory -> this share's buffer
+    } else if (warp >= 8 && warp < 12) {                        // ---- dq: tensor memory -> this share's buffer
         const uint32_t lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
         uint32_t n = 0;
         bool ok = true;
@@ -279,17 +286,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < DP; c += 64) {
-                    uint32_t x[64];
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t x[32];
                     tmem_ld32(t_dq + lane_base + c, x);
-                    tmem_ld32(t_dq + lane_base + c + 32, x + 32);
-                    tmem_wait_ld<64>(x);
-                    if (c + 64 == DP) {
+                    tmem_wait_ld<32>(x);
+                    if (c + 32 == DP) {
                         tc_fence_before();
                         bar_arrive(&dq_free);
                     }
 #pragma unroll
-                    for (int e = 0; e < 64; e += 4) {
+                    for (int e = 0; e < 32; e += 4) {
                         const float4 v = make_float4(__uint_as_float(x[e]), __uint_as_float(x[e + 1]), __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
                         float4* p = dst + (c + e) / 4 * 128;
                         if (m == 0) *p = v;                     // the share's first key tile is every query tile's first
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 }
             }
         }
-    } else {                                                    // ---- p and ds: thread = key (lane of the tile), 64 queries
+    } else if (warp < 8) {                                      // ---- p and ds: thread = key (lane of the tile), 64 queries
         const uint32_t half = warp >> 2, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
         const uint32_t my_s = t_s + lane_base + half * 64, my_dp = t_dp + lane_base + half * 64;
         uint8_t* ds_row = smem + L::DS + half * kBlockBytes + row * 128;
@@ -315,7 +321,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 int32_t from = key < lk ? 0 : 64;
                 if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + half * 64));
                 const bool cut = __any_sync(0xFFFFFFFFu, from > 0);
-                const float4* lse4 = reinterpret_cast<const float4*>(smem + L::ROWS + (n % NQ) * 1024) + half * 16;
                 ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, n & 1, g) && bar_wait(&q_full[n % NQ], (n / NQ) & 1, g));
                 if (!ok) break;
                 tc_fence_after();
@@ -323,26 +328,27 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 tmem_ld32(my_s, p);
                 tmem_ld32(my_s + 32, p + 32);
                 tmem_wait_ld<64>(p);
+                const float4* l4 = reinterpret_cast<const float4*>(smem + L::ROWS + (n % NQ) * 1024) + half * 16;
 #pragma unroll
-                for (int e = 0; e < 64; e += 4) {
-                    const float4 l4 = lse4[e / 4];
-                    float2 u = fma2(make_float2(__uint_as_float(p[e]), __uint_as_float(p[e + 1])), c2, make_float2(-l4.x, -l4.y));
-                    float2 v = fma2(make_float2(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])), c2, make_float2(-l4.z, -l4.w));
-                    p[e] = __float_as_uint(exp2_fast(u.x));
-                    p[e + 1] = __float_as_uint(exp2_fast(u.y));
-                    p[e + 2] = __float_as_uint(exp2_fast(v.x));
-                    p[e + 3] = __float_as_uint(exp2_fast(v.y));
-                }
-                if (cut) {
+                for (int part = 0; part < 64; part += 32) {
+                    uint32_t w16[16];
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e < from) p[e] = 0;
-                }
-                {
-                    uint32_t q16[32];
+                    for (int e = part; e < part + 32; e += 4) {
+                        const float4 l = l4[e / 4];
+                        const float2 u = fma2(pair(p[e], p[e + 1]), c2, make_float2(l.x, l.y)), v = fma2(pair(p[e + 2], p[e + 3]), c2, make_float2(l.z, l.w));
+                        p[e] = __float_as_uint(exp2_fast(u.x));
+                        p[e + 1] = __float_as_uint(exp2_fast(u.y));
+                        p[e + 2] = __float_as_uint(exp2_fast(v.x));
+                        p[e + 3] = __float_as_uint(exp2_fast(v.y));
+                    }
+                    if (cut) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) q16[e] = pack2<T>(__uint_as_float(p[2 * e]), __uint_as_float(p[2 * e + 1]));
-                    tmem_st32(my_s, q16);
+                        for (int e = part; e < part + 32; ++e)
+                            if (e < from) p[e] = 0;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w16[e] = pack2<T>(__uint_as_float(p[part + 2 * e]), __uint_as_float(p[part + 2 * e + 1]));
+                    tmem_st16(my_s + part / 2, w16);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -351,35 +357,31 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 ok = __all_sync(0xFFFFFFFFu, bar_wait(&dp_full, n & 1, g));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t x[64];
-                tmem_ld32(my_dp, x);
-                tmem_ld32(my_dp + 32, x + 32);
-                tmem_wait_ld<64>(x);
-                const float4* d4 = lse4 + 32;
-#pragma unroll
-                for (int e = 0; e < 64; e += 4) {
-                    const float4 d = d4[e / 4];
-                    const float2 u = mul2(make_float2(__uint_as_float(p[e]), __uint_as_float(p[e + 1])),
-                                          add2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), make_float2(-d.x, -d.y)));
-                    const float2 v = mul2(make_float2(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])),
-                                          add2(make_float2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), make_float2(-d.z, -d.w)));
-                    p[e] = __float_as_uint(u.x);
-                    p[e + 1] = __float_as_uint(u.y);
-                    p[e + 2] = __float_as_uint(v.x);
-                    p[e + 3] = __float_as_uint(v.y);
-                }
-                if (cut) {                                      // 0 * (dp of a row that does not count) may be NaN
-#pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e < from) p[e] = 0;
-                }
                 if (n) ok = __all_sync(0xFFFFFFFFu, bar_wait(&ds_free, (n - 1) & 1, g));
                 if (!ok) break;
 #pragma unroll
-                for (int e = 0; e < 64; e += 8) {
-                    const uint4 u = make_uint4(pack2<T>(__uint_as_float(p[e]), __uint_as_float(p[e + 1])), pack2<T>(__uint_as_float(p[e + 2]), __uint_as_float(p[e + 3])),
-                                               pack2<T>(__uint_as_float(p[e + 4]), __uint_as_float(p[e + 5])), pack2<T>(__uint_as_float(p[e + 6]), __uint_as_float(p[e + 7])));
-                    *reinterpret_cast<uint4*>(ds_row + (((e / 8) ^ (row & 7)) << 4)) = u;
+                for (int part = 0; part < 64; part += 16) {     // 16 columns at a time: p and dp at once would not fit in 128 registers
+                    uint32_t x[16];
+                    tmem_ld16(my_dp + part, x);
+                    tmem_wait_ld<16>(x);
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int f = 0; f < 8; f += 4) {
+                            const int at = part + e + f;
+                            const float4 d = l4[32 + at / 4];
+                            float2 u = mul2(pair(p[at], p[at + 1]), add2(pair(x[e + f], x[e + f + 1]), make_float2(d.x, d.y)));
+                            float2 v = mul2(pair(p[at + 2], p[at + 3]), add2(pair(x[e + f + 2], x[e + f + 3]), make_float2(d.z, d.w)));
+                            if (cut) {                          // 0 * (dp of a row that does not count) may be NaN
+                                u = make_float2(at < from ? 0.0f : u.x, at + 1 < from ? 0.0f : u.y);
+                                v = make_float2(at + 2 < from ? 0.0f : v.x, at + 3 < from ? 0.0f : v.y);
+                            }
+                            w[f / 2] = pack2<T>(u.x, u.y);
+                            w[f / 2 + 1] = pack2<T>(v.x, v.y);
+                        }
+                        *reinterpret_cast<uint4*>(ds_row + ((((part + e) / 8) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
                 }
                 fence_async_smem();
                 tc_fence_before();
@@ -516,7 +518,7 @@ int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const d
     const GradSpaceA sp(a);
     r.dk = heads(dk);
     r.dv = heads(dv);
-    r.rows = (const float2*)((uint8_t*)ws + sp.rows);
+    r.rows = (const float*)((uint8_t*)ws + sp.rows);
     r.dq = (float4*)((uint8_t*)ws + sp.dq);
     r.s = shape_of(a);
     r.scale = a->scale;

@@ -192,6 +192,7 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar)
 }
 
 // ---- arithmetic on pairs ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ float2 pair(uint32_t a, uint32_t b) { return make_float2(__uint_as_float(a), __uint_as_float(b)); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
     uint64_t r;
