@@ -125,8 +125,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         bool ok = true;
         for (uint32_t n = 0; n < 2 * nk && ok; ++n) {
             const uint32_t st = n % STAGES, use = n / STAGES, j = n >> 1;
-            if (use) ok = bar_wait(&empty[st], (use - 1) & 1, g);
-            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (use) ok = warp_wait(&empty[st], (use - 1) & 1, g);
             if (!ok) break;
             const bool is_v = n & 1, cut = is_v && j * 128 + 128 > lk && lk < a.s.Sk;
             uint8_t* dst = ring + st * L::TILE;
@@ -155,38 +154,39 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             for (uint32_t n = issued > (uint32_t)STAGES ? issued - STAGES : 0; n < issued; ++n) bar_drain(&full[n % STAGES], (n / STAGES) & 1);
         }
     } else if (warp == 5) {                                     // ---- products
-        if (lane == 0) {
+        {
+            const uint32_t leader = elect_leader();
             constexpr uint32_t id_s = mma_desc<T>(128, 128, false, false), id_o = mma_desc<T>(128, DP, false, true);
             const uint32_t qa = smem_addr(sq), ra = smem_addr(ring);
-            bool ok = bar_wait(&q_full, 0, g);
+            bool ok = warp_wait(&q_full, 0, g);
             auto scores = [&](uint32_t j) {
                 const uint32_t n = 2 * j, st = n % STAGES;
-                ok = ok && bar_wait(&full[st], (n / STAGES) & 1, g);
+                ok = ok && warp_wait(&full[st], (n / STAGES) & 1, g);
                 if (!ok) return;
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
                     const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(t_s, desc_k(qa + off), desc_k(ra + st * L::TILE + off), id_s, kk > 0);
+                    mma_ss(leader, t_s, desc_k(qa + off), desc_k(ra + st * L::TILE + off), id_s, kk > 0);
                 }
-                mma_commit(&empty[st]);
-                mma_commit(&s_full);
+                mma_commit(leader, &empty[st]);
+                mma_commit(leader, &s_full);
             };
             scores(0);
             for (uint32_t j = 0; j < nk && ok; ++j) {
                 const uint32_t n = 2 * j + 1, st = n % STAGES;
-                ok = bar_wait(&p_ready, j & 1, g) && bar_wait(&full[st], (n / STAGES) & 1, g);
+                ok = warp_wait(&p_ready, j & 1, g) && warp_wait(&full[st], (n / STAGES) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(t_o, t_s + 64 + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
-                mma_commit(&empty[st]);
+                    mma_ts(leader, t_o, t_s + 64 + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
+                mma_commit(leader, &empty[st]);
                 if (j + 1 < nk) scores(j + 1);                  // overwrites p(j), which the product before has read by then
-                else mma_commit(&s_full);
+                else mma_commit(leader, &s_full);
             }
             if (!ok) {                                          // products in flight end before the memory is freed
-                mma_commit(&idle);
+                mma_commit(leader, &idle);
                 bar_drain(&idle, 0);
             }
         }
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         float m = -INFINITY, l = 0.0f;
         bool ok = true;
         for (uint32_t j = 0; j < nk; ++j) {
-            ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, j & 1, g));
+            ok = warp_wait(&s_full, j & 1, g);
             if (!ok) break;
             tc_fence_after();
             // All 128 scores for the maximum; the first 64 are then dropped and read again chunk by chunk, which keeps the
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             tc_fence_before();
             bar_arrive(&p_ready);
         }
-        if (ok) ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, nk & 1, g));
+        if (ok) ok = warp_wait(&s_full, nk & 1, g);
         if (ok) {
             tc_fence_after();
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;

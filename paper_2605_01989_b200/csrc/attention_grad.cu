@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (m * a.shares >= a.k_tiles) break;
             const uint32_t per_head = meets(j);
             if (per_head == 0) continue;
-            if (w) ok = __all_sync(0xFFFFFFFFu, bar_wait(&acc_full, (w - 1) & 1, g));   // products of the tile before are done
+            if (w) ok = warp_wait(&acc_full, (w - 1) & 1, g);   // products of the tile before are done
             if (!ok) break;
             const bool kcut = j * 128 + 128 > lk && lk < a.s.Sk;
             if (kcut) load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
                 const bool cut = i * 128 + 128 > lq && lq < a.s.Sq;
                 const uint32_t sq = n % NQ, sg = n % NG;
-                if (n >= NQ) ok = __all_sync(0xFFFFFFFFu, bar_wait(&q_empty[sq], (n / NQ - 1) & 1, g));
+                if (n >= NQ) ok = warp_wait(&q_empty[sq], (n / NQ - 1) & 1, g);
                 if (!ok) break;
                 uint8_t *dq_ = smem + L::Q + sq * L::TILE, *dg = smem + L::G + sg * L::TILE;
                 if (cut) load_cut(dq_, a.q, i * 128, h, lq - i * 128);
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     if (!cut) load_tile<NS>(dq_, a.q, &q_full[sq], i * 128, h, b);
                     bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &q_full[sq]);
                 }
-                if (n >= NG) ok = __all_sync(0xFFFFFFFFu, bar_wait(&g_empty[sg], (n / NG - 1) & 1, g));
+                if (n >= NG) ok = warp_wait(&g_empty[sg], (n / NG - 1) & 1, g);
                 if (!ok) { if (lane == 0) bar_drain(&q_full[sq], (n / NQ) & 1); break; }
                 if (cut) load_cut(dg, a.go, i * 128, h, lq - i * 128);
                 if (lane == 0) {
@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&g_full[x % NG], (x / NG) & 1);
         }
     } else if (warp == 13) {                                    // ---- products
-        if (lane == 0) {
+        {
+            const uint32_t leader = elect_leader();
             constexpr uint32_t id_kk = mma_desc<T>(128, 128, false, false);     // s, dp
             constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);       // dv, dk: right operand across its rows
             constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);        // dq: both across their rows
@@ -206,69 +207,69 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             uint32_t n = 0, w = 0;
             bool ok = true;
             auto scores = [&](uint32_t x) {
-                ok = ok && bar_wait(&q_full[x % NQ], (x / NQ) & 1, g);
+                ok = ok && warp_wait(&q_full[x % NQ], (x / NQ) & 1, g);
                 if (!ok) return;
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
                     const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(t_s, desc_k(base + L::K + off), desc_k(base + L::Q + (x % NQ) * L::TILE + off), id_kk, kk > 0);
+                    mma_ss(leader, t_s, desc_k(base + L::K + off), desc_k(base + L::Q + (x % NQ) * L::TILE + off), id_kk, kk > 0);
                 }
-                mma_commit(&s_full);
+                mma_commit(leader, &s_full);
             };
             auto dprobs = [&](uint32_t x) {
-                ok = ok && bar_wait(&g_full[x % NG], (x / NG) & 1, g);
-                if (ok && !kOwnDq && x) ok = bar_wait(&dq_free, (x - 1) & 1, g);
+                ok = ok && warp_wait(&g_full[x % NG], (x / NG) & 1, g);
+                if (ok && !kOwnDq && x) ok = warp_wait(&dq_free, (x - 1) & 1, g);
                 if (!ok) return;
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
                     const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(t_dp, desc_k(base + L::V + off), desc_k(base + L::G + (x % NG) * L::TILE + off), id_kk, kk > 0);
+                    mma_ss(leader, t_dp, desc_k(base + L::V + off), desc_k(base + L::G + (x % NG) * L::TILE + off), id_kk, kk > 0);
                 }
-                mma_commit(&dp_full);
+                mma_commit(leader, &dp_full);
             };
             for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
                 const uint32_t pairs = meets(share_tile(share, m, a.shares)) * a.s.rep;
                 if (pairs == 0) continue;
-                ok = bar_wait(&kv_full, w & 1, g);
+                ok = warp_wait(&kv_full, w & 1, g);
                 scores(n);
                 dprobs(n);
                 for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
                     const uint32_t qa = base + L::Q + (n % NQ) * L::TILE, ga = base + L::G + (n % NG) * L::TILE;
-                    ok = bar_wait(&p_ready, n & 1, g);
-                    if (ok && t == 0 && w) ok = bar_wait(&acc_free, (w - 1) & 1, g);
+                    ok = warp_wait(&p_ready, n & 1, g);
+                    if (ok && t == 0 && w) ok = warp_wait(&acc_free, (w - 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)              // p of queries 0-63 in columns 0-31, of 64-127 in 64-95
-                        mma_ts(t_dv, t_s + (kk / 4) * 64 + (kk % 4) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
-                    mma_commit(&g_empty[n % NG]);
+                        mma_ts(leader, t_dv, t_s + (kk / 4) * 64 + (kk % 4) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
+                    mma_commit(leader, &g_empty[n % NG]);
                     if (t + 1 < pairs) scores(n + 1);           // over p(n), which the product before has read by then
-                    ok = ok && bar_wait(&ds_ready, n & 1, g);
+                    ok = ok && warp_wait(&ds_ready, n & 1, g);
                     if (!ok) break;
                     tc_fence_after();
                     if (kOwnDq && t + 1 < pairs) dprobs(n + 1); // dp(n) has been read: the next pair need not wait for dq, dk
-                    if (ok && kOwnDq && n) ok = bar_wait(&dq_free, (n - 1) & 1, g);
+                    if (ok && kOwnDq && n) ok = warp_wait(&dq_free, (n - 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
-                        mma_ss(t_dq, desc_mn(base + L::DS + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
-                    mma_commit(&dq_full);
+                        mma_ss(leader, t_dq, desc_mn(base + L::DS + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
+                    mma_commit(leader, &dq_full);
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
-                        mma_ss(t_dk, desc_k(base + L::DS + (kk / 4) * kBlockBytes + (kk % 4) * 32), desc_mn(qa + kk * 2048, kBlockBytes), id_kv,
+                        mma_ss(leader, t_dk, desc_k(base + L::DS + (kk / 4) * kBlockBytes + (kk % 4) * 32), desc_mn(qa + kk * 2048, kBlockBytes), id_kv,
                                t > 0 || kk > 0);
-                    mma_commit(&q_empty[n % NQ]);
-                    mma_commit(&ds_free);
+                    mma_commit(leader, &q_empty[n % NQ]);
+                    mma_commit(leader, &ds_free);
                     if (!kOwnDq && t + 1 < pairs) dprobs(n + 1);
                 }
-                if (ok) mma_commit(&acc_full);
+                if (ok) mma_commit(leader, &acc_full);
                 ++w;
             }
             if (!ok) {                                          // products in flight end before the memory is freed
-                mma_commit(&idle);
+                mma_commit(leader, &idle);
                 bar_drain(&idle, 0);
             }
         }
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             for (uint32_t t = 0; t < per_head * a.s.rep; ++t, ++n) {
                 const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
                 float4* dst = a.dq + (((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * (DP / 4)) * 128 + row;
-                ok = __all_sync(0xFFFFFFFFu, bar_wait(&dq_full, n & 1, g));
+                ok = warp_wait(&dq_full, n & 1, g);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 int32_t from = key < lk ? 0 : 64;
                 if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + half * 64));
                 const bool cut = __any_sync(0xFFFFFFFFu, from > 0);
-                ok = __all_sync(0xFFFFFFFFu, bar_wait(&s_full, n & 1, g) && bar_wait(&q_full[n % NQ], (n / NQ) & 1, g));
+                ok = warp_wait(&s_full, n & 1, g) && warp_wait(&q_full[n % NQ], (n / NQ) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t p[64];
@@ -354,10 +355,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 tc_fence_before();
                 bar_arrive(&p_ready);
 
-                ok = __all_sync(0xFFFFFFFFu, bar_wait(&dp_full, n & 1, g));
+                ok = warp_wait(&dp_full, n & 1, g);
                 if (!ok) break;
                 tc_fence_after();
-                if (n) ok = __all_sync(0xFFFFFFFFu, bar_wait(&ds_free, (n - 1) & 1, g));
+                if (n) ok = warp_wait(&ds_free, (n - 1) & 1, g);
                 if (!ok) break;
 #pragma unroll
                 for (int part = 0; part < 64; part += 16) {     // 16 columns at a time: p and dp at once would not fit in 128 registers
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             T* dst = (T*)hd.p + (int64_t)b * hd.sb + (int64_t)key * hd.st + (int64_t)hk * hd.sh;
             const float f = half ? a.scale : 1.0f;
             if (pairs) {
-                ok = __all_sync(0xFFFFFFFFu, bar_wait(&acc_full, w & 1, g));
+                ok = warp_wait(&acc_full, w & 1, g);
                 if (!ok) break;
                 tc_fence_after();
             }
