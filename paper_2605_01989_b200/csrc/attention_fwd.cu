@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         bar_init(&idle, 1);
         for (int i = 0; i < STAGES; ++i) { bar_init(&full[i], 1); bar_init(&empty[i], 1); }
         bar_init(&s_full, 1);
-        bar_init(&p_ready, 128);
+        bar_init(&p_ready, 4);
         fence_bar_init();
     }
     if (warp == 5) tmem_alloc<256>(&tmem_slot);
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             l += sum.x + sum.y;
             tmem_wait_st();
             tc_fence_before();
-            bar_arrive(&p_ready);
+            warp_arrive(&p_ready);
         }
         if (ok) ok = warp_wait(&s_full, nk & 1, g);
         if (ok) {

@@ -14,20 +14,21 @@
 // Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
 // two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
-//   warps         0-7 p and ds (each thread one key and 64 queries), 8-11 dq to memory, 12 TMA, 13 products.
+//   warps         0-15 p, ds and dq's way to memory (each thread one key and 32 queries), 16 TMA, 17 products.
 #include <math.h>
 
 #include "attention.cuh"
 
 namespace dblp {
 
-constexpr int kGradThreads = 448;
+constexpr int kGradThreads = 576;
+constexpr uint32_t kPairWarps = 16, kTmaWarp = 16, kMmaWarp = 17;
 
 struct GradArgs {
     TileSource q, k, v, go;
     Heads dk, dv;
     const float* rows;         // [B][Hq][tiles][2][128]: -lse log2(e), then -D
-    float4* dq;                // [R][B][Hq][tiles][D / 4 of DP][128]
+    float4* dq;                // [R][B][Hq][tiles][4][DP / 4][32]: query 32 a + l, columns 4 c .. 4 c + 3 at [a][c][l]
     AttnShape s;
     float scale, scale_log2;
     uint32_t q_tiles, k_tiles, shares;
@@ -84,15 +85,18 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
 // ---- main ------------------------------------------------------------------------------------------------------------
 template <int DP> struct GradSmem {
     static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes;
-    static constexpr int NQ = 2, NG = DP == 64 ? 2 : 1;                 // stages of q (with its row values) and of dout
+    static constexpr int NQ = DP == 64 ? 4 : 2, NG = DP == 64 ? 3 : 1;  // stages of q (with its row values) and of dout
     static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, ROWS = DS + 2 * (int)kBlockBytes;
-    static constexpr int kBytes = 1024 + ROWS + NQ * 1024;
+    static constexpr int STAGE = ROWS + NQ * 1024;                      // dq on its way out: 2 KB a warp
+    static constexpr int BARS = STAGE + (int)kPairWarps * 2048, kBytes = BARS + 256;
 };
 
-__device__ __forceinline__ void add4(float4* p, float4 v)
-{
-    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
-}
+struct GradBars {
+    uint64_t kv_full, q_full[4], q_empty[4], g_full[3], g_empty[3], cut_full;
+    uint64_t s_full, p_ready, dp_full, ds_ready, ds_free, dq_full, dq_free, acc_full, acc_free, idle;
+    uint32_t tmem_slot, dead;
+};
+static_assert(sizeof(GradBars) <= 256, "");
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant__ GradArgs a)
@@ -100,11 +104,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     using L = GradSmem<DP>;
     constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG;
     constexpr bool kOwnDq = DP == 64;                          // dq has columns of its own; else it takes those of dp
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full, q_full[NQ], q_empty[NQ], g_full[NG], g_empty[NG], cut_full;
-    __shared__ uint64_t s_full, p_ready, dp_full, ds_ready, ds_free, dq_full, dq_free, acc_full, acc_free, idle;
-    __shared__ uint32_t tmem_slot, dead;
-    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t smem[];          // the whole of the block's shared memory, so at an even kilobyte
+    GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t share = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
@@ -118,34 +119,34 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     };
 
     if (tid == 0) {
-        dead = 0;
-        for (uint64_t* p : {&kv_full, &cut_full, &s_full, &dp_full, &ds_free, &dq_full, &acc_full, &idle}) bar_init(p, 1);
-        for (int i = 0; i < NQ; ++i) { bar_init(&q_full[i], 1); bar_init(&q_empty[i], 1); }
-        for (int i = 0; i < NG; ++i) { bar_init(&g_full[i], 1); bar_init(&g_empty[i], 1); }
-        bar_init(&p_ready, 256);
-        bar_init(&ds_ready, 256);
-        bar_init(&acc_free, 256);
-        bar_init(&dq_free, 128);
+        s.dead = 0;
+        for (uint64_t* p : {&s.kv_full, &s.cut_full, &s.s_full, &s.dp_full, &s.ds_free, &s.dq_full, &s.acc_full, &s.idle}) bar_init(p, 1);
+        for (int i = 0; i < NQ; ++i) { bar_init(&s.q_full[i], 1); bar_init(&s.q_empty[i], 1); }
+        for (int i = 0; i < NG; ++i) { bar_init(&s.g_full[i], 1); bar_init(&s.g_empty[i], 1); }
+        bar_init(&s.p_ready, kPairWarps);
+        bar_init(&s.ds_ready, kPairWarps);
+        bar_init(&s.acc_free, kPairWarps);
+        bar_init(&s.dq_free, kPairWarps);
         fence_bar_init();
     }
-    if (warp == 13) tmem_alloc<512>(&tmem_slot);
+    if (warp == kMmaWarp) tmem_alloc<512>(&s.tmem_slot);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
+    const uint32_t tmem = s.tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
     const uint32_t t_dq = kOwnDq ? tmem + 384 : t_dp;
-    const Guard g{&dead, a.timeouts};
+    const Guard g{&s.dead, a.timeouts};
 
-    if (warp == 12) {                                           // ---- TMA
+    if (warp == kTmaWarp) {                                       // ---- TMA
         uint32_t n = 0, w = 0, cuts = 0;                        // pairs, key tiles with work, tiles that were cleared
         bool ok = true;
         // a tile whose rows from `first` on do not count but may hold anything
         auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t first) {
             if (lane == 0) {
-                bar_expect(&cut_full, L::TILE);
-                load_tile<NS>(dst, src, &cut_full, token, head, b);
+                bar_expect(&s.cut_full, L::TILE);
+                load_tile<NS>(dst, src, &s.cut_full, token, head, b);
             }
-            bar_drain(&cut_full, cuts++ & 1);
+            bar_drain(&s.cut_full, cuts++ & 1);
             __syncwarp();
             clear_rows<NS>(dst, first);
             __syncwarp();
@@ -155,49 +156,49 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (m * a.shares >= a.k_tiles) break;
             const uint32_t per_head = meets(j);
             if (per_head == 0) continue;
-            if (w) ok = warp_wait(&acc_full, (w - 1) & 1, g);   // products of the tile before are done
+            if (w) ok = warp_wait(&s.acc_full, (w - 1) & 1, g);   // products of the tile before are done
             if (!ok) break;
             const bool kcut = j * 128 + 128 > lk && lk < a.s.Sk;
             if (kcut) load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
             if (lane == 0) {
-                bar_expect(&kv_full, kcut ? L::TILE : 2 * L::TILE);
-                if (!kcut) load_tile<NS>(smem + L::K, a.k, &kv_full, j * 128, hk, b);
-                load_tile<NS>(smem + L::V, a.v, &kv_full, j * 128, hk, b);
+                bar_expect(&s.kv_full, kcut ? L::TILE : 2 * L::TILE);
+                if (!kcut) load_tile<NS>(smem + L::K, a.k, &s.kv_full, j * 128, hk, b);
+                load_tile<NS>(smem + L::V, a.v, &s.kv_full, j * 128, hk, b);
             }
             ++w;
             for (uint32_t t = 0; t < per_head * a.s.rep && ok; ++t, ++n) {
                 const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
                 const bool cut = i * 128 + 128 > lq && lq < a.s.Sq;
                 const uint32_t sq = n % NQ, sg = n % NG;
-                if (n >= NQ) ok = warp_wait(&q_empty[sq], (n / NQ - 1) & 1, g);
+                if (n >= NQ) ok = warp_wait(&s.q_empty[sq], (n / NQ - 1) & 1, g);
                 if (!ok) break;
                 uint8_t *dq_ = smem + L::Q + sq * L::TILE, *dg = smem + L::G + sg * L::TILE;
                 if (cut) load_cut(dq_, a.q, i * 128, h, lq - i * 128);
                 if (lane == 0) {
-                    bar_expect(&q_full[sq], (cut ? 0 : L::TILE) + 1024);
-                    if (!cut) load_tile<NS>(dq_, a.q, &q_full[sq], i * 128, h, b);
-                    bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &q_full[sq]);
+                    bar_expect(&s.q_full[sq], (cut ? 0 : L::TILE) + 1024);
+                    if (!cut) load_tile<NS>(dq_, a.q, &s.q_full[sq], i * 128, h, b);
+                    bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &s.q_full[sq]);
                 }
-                if (n >= NG) ok = warp_wait(&g_empty[sg], (n / NG - 1) & 1, g);
-                if (!ok) { if (lane == 0) bar_drain(&q_full[sq], (n / NQ) & 1); break; }
+                if (n >= NG) ok = warp_wait(&s.g_empty[sg], (n / NG - 1) & 1, g);
+                if (!ok) { if (lane == 0) bar_drain(&s.q_full[sq], (n / NQ) & 1); break; }
                 if (cut) load_cut(dg, a.go, i * 128, h, lq - i * 128);
                 if (lane == 0) {
                     if (cut) {
-                        bar_arrive(&g_full[sg]);
+                        bar_arrive(&s.g_full[sg]);
                     } else {
-                        bar_expect(&g_full[sg], L::TILE);
-                        load_tile<NS>(dg, a.go, &g_full[sg], i * 128, h, b);
+                        bar_expect(&s.g_full[sg], L::TILE);
+                        load_tile<NS>(dg, a.go, &s.g_full[sg], i * 128, h, b);
                     }
                 }
                 __syncwarp();
             }
         }
         if (lane == 0) {                                        // every copy lands before the block may end
-            if (w) bar_drain(&kv_full, (w - 1) & 1);
-            for (uint32_t x = n > NQ ? n - NQ : 0; x < n; ++x) bar_drain(&q_full[x % NQ], (x / NQ) & 1);
-            for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&g_full[x % NG], (x / NG) & 1);
+            if (w) bar_drain(&s.kv_full, (w - 1) & 1);
+            for (uint32_t x = n > NQ ? n - NQ : 0; x < n; ++x) bar_drain(&s.q_full[x % NQ], (x / NQ) & 1);
+            for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&s.g_full[x % NG], (x / NG) & 1);
         }
-    } else if (warp == 13) {                                    // ---- products
+    } else if (warp == kMmaWarp) {                                 // ---- products
         {
             const uint32_t leader = elect_leader();
             constexpr uint32_t id_kk = mma_desc<T>(128, 128, false, false);     // s, dp
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             uint32_t n = 0, w = 0;
             bool ok = true;
             auto scores = [&](uint32_t x) {
-                ok = ok && warp_wait(&q_full[x % NQ], (x / NQ) & 1, g);
+                ok = ok && warp_wait(&s.q_full[x % NQ], (x / NQ) & 1, g);
                 if (!ok) return;
                 tc_fence_after();
 #pragma unroll
@@ -215,11 +216,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
                     mma_ss(leader, t_s, desc_k(base + L::K + off), desc_k(base + L::Q + (x % NQ) * L::TILE + off), id_kk, kk > 0);
                 }
-                mma_commit(leader, &s_full);
+                mma_commit(leader, &s.s_full);
             };
             auto dprobs = [&](uint32_t x) {
-                ok = ok && warp_wait(&g_full[x % NG], (x / NG) & 1, g);
-                if (ok && !kOwnDq && x) ok = warp_wait(&dq_free, (x - 1) & 1, g);
+                ok = ok && warp_wait(&s.g_full[x % NG], (x / NG) & 1, g);
+                if (ok && !kOwnDq && x) ok = warp_wait(&s.dq_free, (x - 1) & 1, g);
                 if (!ok) return;
                 tc_fence_after();
 #pragma unroll
@@ -227,114 +228,126 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
                     mma_ss(leader, t_dp, desc_k(base + L::V + off), desc_k(base + L::G + (x % NG) * L::TILE + off), id_kk, kk > 0);
                 }
-                mma_commit(leader, &dp_full);
+                mma_commit(leader, &s.dp_full);
             };
             for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
                 const uint32_t pairs = meets(share_tile(share, m, a.shares)) * a.s.rep;
                 if (pairs == 0) continue;
-                ok = warp_wait(&kv_full, w & 1, g);
+                ok = warp_wait(&s.kv_full, w & 1, g);
                 scores(n);
                 dprobs(n);
                 for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
                     const uint32_t qa = base + L::Q + (n % NQ) * L::TILE, ga = base + L::G + (n % NG) * L::TILE;
-                    ok = warp_wait(&p_ready, n & 1, g);
-                    if (ok && t == 0 && w) ok = warp_wait(&acc_free, (w - 1) & 1, g);
+                    ok = warp_wait(&s.p_ready, n & 1, g);
+                    if (ok && t == 0 && w) ok = warp_wait(&s.acc_free, (w - 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)              // p of queries 0-63 in columns 0-31, of 64-127 in 64-95
-                        mma_ts(leader, t_dv, t_s + (kk / 4) * 64 + (kk % 4) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
-                    mma_commit(leader, &g_empty[n % NG]);
+                    for (int kk = 0; kk < 8; ++kk)              // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
+                        mma_ts(leader, t_dv, t_s + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
+                    mma_commit(leader, &s.g_empty[n % NG]);
                     if (t + 1 < pairs) scores(n + 1);           // over p(n), which the product before has read by then
-                    ok = ok && warp_wait(&ds_ready, n & 1, g);
+                    ok = ok && warp_wait(&s.ds_ready, n & 1, g);
                     if (!ok) break;
                     tc_fence_after();
                     if (kOwnDq && t + 1 < pairs) dprobs(n + 1); // dp(n) has been read: the next pair need not wait for dq, dk
-                    if (ok && kOwnDq && n) ok = warp_wait(&dq_free, (n - 1) & 1, g);
+                    if (ok && kOwnDq && n) ok = warp_wait(&s.dq_free, (n - 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
                         mma_ss(leader, t_dq, desc_mn(base + L::DS + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
-                    mma_commit(leader, &dq_full);
+                    mma_commit(leader, &s.dq_full);
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
                         mma_ss(leader, t_dk, desc_k(base + L::DS + (kk / 4) * kBlockBytes + (kk % 4) * 32), desc_mn(qa + kk * 2048, kBlockBytes), id_kv,
                                t > 0 || kk > 0);
-                    mma_commit(leader, &q_empty[n % NQ]);
-                    mma_commit(leader, &ds_free);
+                    mma_commit(leader, &s.q_empty[n % NQ]);
+                    mma_commit(leader, &s.ds_free);
                     if (!kOwnDq && t + 1 < pairs) dprobs(n + 1);
                 }
-                if (ok) mma_commit(leader, &acc_full);
+                if (ok) mma_commit(leader, &s.acc_full);
                 ++w;
             }
             if (!ok) {                                          // products in flight end before the memory is freed
-                mma_commit(leader, &idle);
-                bar_drain(&idle, 0);
+                mma_commit(leader, &s.idle);
+                bar_drain(&s.idle, 0);
             }
         }
         __syncwarp();
-    } else if (warp >= 8 && warp < 12) {                        // ---- dq: tensor memory -> this share's buffer
-        const uint32_t lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
-        uint32_t n = 0;
-        bool ok = true;
-        for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
-            const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j);
-            for (uint32_t t = 0; t < per_head * a.s.rep; ++t, ++n) {
-                const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
-                float4* dst = a.dq + (((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * (DP / 4)) * 128 + row;
-                ok = warp_wait(&dq_full, n & 1, g);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int c = 0; c < DP; c += 32) {
-                    uint32_t x[32];
-                    tmem_ld32(t_dq + lane_base + c, x);
-                    tmem_wait_ld<32>(x);
-                    if (c + 32 == DP) {
-                        tc_fence_before();
-                        bar_arrive(&dq_free);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 v = make_float4(__uint_as_float(x[e]), __uint_as_float(x[e + 1]), __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
-                        float4* p = dst + (c + e) / 4 * 128;
-                        if (m == 0) *p = v;                     // the share's first key tile is every query tile's first
-                        else add4(p, v);
-                    }
-                }
-            }
-        }
-    } else if (warp < 8) {                                      // ---- p and ds: thread = key (lane of the tile), 64 queries
-        const uint32_t half = warp >> 2, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
-        const uint32_t my_s = t_s + lane_base + half * 64, my_dp = t_dp + lane_base + half * 64;
-        uint8_t* ds_row = smem + L::DS + half * kBlockBytes + row * 128;
+    } else {                                                    // ---- p and ds: thread = key (lane of the tile), 32 queries
+        const uint32_t grp = warp >> 2, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
+        const uint32_t my_s = t_s + lane_base + grp * 32, my_dp = t_dp + lane_base + grp * 32;
+        uint8_t* ds_row = smem + L::DS + (grp >> 1) * kBlockBytes + row * 128;
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
+        float4* stage = reinterpret_cast<float4*>(smem + L::STAGE + warp * 2048);
         uint32_t n = 0, w = 0;
         bool ok = true;
+
+        // dq of pair x to this share's buffer: this warp takes 32 queries and DP / 4 columns, 16 columns at a time through
+        // shared memory; the memory system adds them.  `first`: nothing is there yet.  The additions of the last visit to a
+        // query tile are done before those of this one begin: all groups but the pair before's are complete, and with one
+        // pair a key tile (`lone`) those too.
+        constexpr int PIECES = DP / 64;
+        float4* dq_at = nullptr;
+        bool dq_first = false, dq_lone = false;
+        auto drain = [&](uint32_t x) {
+            ok = warp_wait(&s.dq_full, x & 1, g);
+            if (!ok) return;
+            tc_fence_after();
+            if (lane == 0) {
+                if (dq_lone) bulk_wait<0>();
+                else bulk_wait<PIECES>();
+            }
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                uint32_t v[16];
+                tmem_ld16(t_dq + lane_base + (grp * PIECES + c) * 16, v);
+                if (lane == 0) bulk_wait_read<0>();             // the piece that was here has left
+                __syncwarp();
+                tmem_wait_ld<16>(v);
+                if (c + 1 == PIECES) {
+                    tc_fence_before();
+                    warp_arrive(&s.dq_free);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    stage[e * 32 + lane] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (dq_first) bulk_store(dq_at + c * 128, stage, 2048);
+                    else bulk_add_f32(dq_at + c * 128, stage, 2048);
+                    bulk_commit();
+                }
+            }
+        };
+
         for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
             const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * a.s.rep;
             if (j >= a.k_tiles) continue;
             const uint32_t key = j * 128 + row;
-            for (uint32_t t = 0; t < pairs; ++t, ++n) {
-                const uint32_t i = nq - per_head + t % per_head;
-                // queries [from, 64) of this thread's columns see the key
-                int32_t from = key < lk ? 0 : 64;
-                if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + half * 64));
+            for (uint32_t t = 0, i = nq - per_head, h = hk * a.s.rep; t < pairs; ++t, ++n) {
+                if (!kOwnDq && n) {                             // dp of this pair comes where dq of the last one is
+                    drain(n - 1);
+                    if (!ok) break;
+                }
+                // queries [from, 32) of this thread's columns see the key
+                int32_t from = key < lk ? 0 : 32;
+                if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + grp * 32));
                 const bool cut = __any_sync(0xFFFFFFFFu, from > 0);
-                ok = warp_wait(&s_full, n & 1, g) && warp_wait(&q_full[n % NQ], (n / NQ) & 1, g);
+                ok = warp_wait(&s.s_full, n & 1, g) && warp_wait(&s.q_full[n % NQ], (n / NQ) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t p[64];
+                uint32_t p[32];
                 tmem_ld32(my_s, p);
-                tmem_ld32(my_s + 32, p + 32);
-                tmem_wait_ld<64>(p);
-                const float4* l4 = reinterpret_cast<const float4*>(smem + L::ROWS + (n % NQ) * 1024) + half * 16;
+                const float4* l4 = reinterpret_cast<const float4*>(smem + L::ROWS + (n % NQ) * 1024) + grp * 8;
+                tmem_wait_ld<32>(p);
 #pragma unroll
-                for (int part = 0; part < 64; part += 32) {
-                    uint32_t w16[16];
+                for (int part = 0; part < 32; part += 16) {
+                    uint32_t w8[8];
 #pragma unroll
-                    for (int e = part; e < part + 32; e += 4) {
+                    for (int e = part; e < part + 16; e += 4) {
                         const float4 l = l4[e / 4];
                         const float2 u = fma2(pair(p[e], p[e + 1]), c2, make_float2(l.x, l.y)), v = fma2(pair(p[e + 2], p[e + 3]), c2, make_float2(l.z, l.w));
                         p[e] = __float_as_uint(exp2_fast(u.x));
@@ -344,24 +357,31 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     }
                     if (cut) {
 #pragma unroll
-                        for (int e = part; e < part + 32; ++e)
+                        for (int e = part; e < part + 16; ++e)
                             if (e < from) p[e] = 0;
                     }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w16[e] = pack2<T>(__uint_as_float(p[part + 2 * e]), __uint_as_float(p[part + 2 * e + 1]));
-                    tmem_st16(my_s + part / 2, w16);
+                    for (int e = 0; e < 8; ++e) w8[e] = pack2<T>(__uint_as_float(p[part + 2 * e]), __uint_as_float(p[part + 2 * e + 1]));
+                    tmem_st8(my_s + part / 2, w8);
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                bar_arrive(&p_ready);
+                warp_arrive(&s.p_ready);
 
-                ok = warp_wait(&dp_full, n & 1, g);
+                if (kOwnDq && n) {
+                    drain(n - 1);
+                    if (!ok) break;
+                }
+                dq_at = a.dq + ((((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * 4 + (warp & 3)) * (DP / 4) + grp * (DP / 16)) * 32;
+                dq_first = m == 0;                              // the share's first key tile is the first to meet every query tile
+                dq_lone = pairs == 1;
+                if (++i == nq) { i = nq - per_head; ++h; }
+                ok = warp_wait(&s.dp_full, n & 1, g);
+                if (ok && n) ok = warp_wait(&s.ds_free, (n - 1) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
-                if (n) ok = warp_wait(&ds_free, (n - 1) & 1, g);
-                if (!ok) break;
 #pragma unroll
-                for (int part = 0; part < 64; part += 16) {     // 16 columns at a time: p and dp at once would not fit in 128 registers
+                for (int part = 0; part < 32; part += 16) {     // 16 columns at a time, for the sake of registers
                     uint32_t x[16];
                     tmem_ld16(my_dp + part, x);
                     tmem_wait_ld<16>(x);
@@ -381,32 +401,35 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                             w[f / 2] = pack2<T>(u.x, u.y);
                             w[f / 2 + 1] = pack2<T>(v.x, v.y);
                         }
-                        *reinterpret_cast<uint4*>(ds_row + ((((part + e) / 8) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(ds_row + ((((grp & 1) * 4 + (part + e) / 8) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
                 fence_async_smem();
                 tc_fence_before();
-                bar_arrive(&ds_ready);
+                warp_arrive(&s.ds_ready);
             }
             if (!ok) break;
-            // this key tile's gradients: the first four warps dv, the others dk
-            const Heads& hd = half ? a.dk : a.dv;
+            // this key tile's gradients: two groups dv, two dk, half of the columns each
+            const bool is_dk = grp >= 2;
+            const Heads& hd = is_dk ? a.dk : a.dv;
             T* dst = (T*)hd.p + (int64_t)b * hd.sb + (int64_t)key * hd.st + (int64_t)hk * hd.sh;
-            const float f = half ? a.scale : 1.0f;
+            const float f = is_dk ? a.scale : 1.0f;
+            const int c0 = (grp & 1) * (DP / 2);
             if (pairs) {
-                ok = warp_wait(&acc_full, w & 1, g);
+                ok = warp_wait(&s.acc_full, w & 1, g);
                 if (!ok) break;
                 tc_fence_after();
             }
 #pragma unroll
-            for (int c = 0; c < DP; c += 32) {
-                uint32_t x[32];
+            for (int cc = 0; cc < DP / 2; cc += 16) {
+                const int c = c0 + cc;
+                uint32_t x[16];
                 if (pairs) {
-                    tmem_ld32((half ? t_dk : t_dv) + lane_base + c, x);
-                    tmem_wait_ld<32>(x);
+                    tmem_ld16((is_dk ? t_dk : t_dv) + lane_base + c, x);
+                    tmem_wait_ld<16>(x);
                 }
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
+                for (int e = 0; e < 16; e += 8) {
                     Vec8<T> o;
                     float y[8];
 #pragma unroll
@@ -417,13 +440,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             }
             if (pairs) {
                 tc_fence_before();
-                bar_arrive(&acc_free);
+                warp_arrive(&s.acc_free);
                 ++w;
             }
         }
+        if (ok && n) drain(n - 1);
+        if (lane == 0) bulk_wait<0>();
     }
     __syncthreads();
-    if (warp == 13) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_free<512>(tmem);
     }
@@ -440,12 +465,12 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
     if (token >= s.Sq) return;
     T* dst = (T*)dq.p + (int64_t)b * dq.sb + (int64_t)token * dq.st + (int64_t)h * dq.sh;
     const uint64_t stride = (uint64_t)s.B * s.Hq * q_tiles * (DP / 4) * 128;
-    const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row;
+    const float4* src = part + ((((uint64_t)b * s.Hq + h) * q_tiles + i) * 4 + row / 32) * (DP / 4) * 32 + row % 32;
 #pragma unroll 4
     for (uint32_t c = (threadIdx.x >> 7) * 8; c < s.D; c += 16) {
         float y[8] = {};
         for (uint32_t r = 0; r < parts; ++r) {
-            const float4 u = src[r * stride + c / 4 * 128], v = src[r * stride + (c / 4 + 1) * 128];
+            const float4 u = src[r * stride + c / 4 * 32], v = src[r * stride + (c / 4 + 1) * 32];
             y[0] += u.x; y[1] += u.y; y[2] += u.z; y[3] += u.w;
             y[4] += v.x; y[5] += v.y; y[6] += v.z; y[7] += v.w;
         }

@@ -25,16 +25,23 @@ __device__ __forceinline__ void bar_arrive(uint64_t* b)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
 }
+// One arrival for a warp: arrivals on one barrier are served one after the other, 512 of them cost thousands of cycles.
+__device__ __forceinline__ void warp_arrive(uint64_t* b)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(b);
+}
 __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
 }
+// The thread may sleep up to a millisecond before the answer is no: a polling warp would take issue slots from the others.
 __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok)
-                 : "r"(smem_addr(b)), "r"(parity)
+                 : "r"(smem_addr(b)), "r"(parity), "r"(1000000u)
                  : "memory");
     return ok != 0;
 }
@@ -49,7 +56,7 @@ struct Guard {
     unsigned long long* timeouts;       // device memory, one per device
 };
 
-static __device__ __noinline__ bool bar_wait_slow(uint64_t* b, uint32_t parity, Guard g)
+__device__ __forceinline__ bool bar_wait_slow(uint64_t* b, uint32_t parity, Guard g)
 {
     const long long t0 = clock64();
     for (;;) {
@@ -72,7 +79,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, const Gu
     return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, g));
 }
 // For copies that were issued and must land before the block ends: bounded by itself, whatever the flag says.
-static __device__ __noinline__ void bar_drain(uint64_t* b, uint32_t parity)
+__device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
 {
     const long long t0 = clock64();
     while (!bar_try(b, parity) && clock64() - t0 < kWaitCycles) {}
@@ -92,6 +99,19 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar))
                  : "memory");
 }
+// shared -> global, plain or added in fp32 by the memory system; grouped per issuing thread
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_add_f32(void* dst, const void* src, uint32_t bytes)
+{
+    asm volatile("cp.reduce.async.bulk.global.shared::cta.bulk_group.add.f32 [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// at most N groups of this thread still read shared memory / are not yet written
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+template <int N> __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
@@ -158,6 +178,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r)
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
                  "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
                  "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t* r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
 
