@@ -10,7 +10,8 @@
 //                 p and ds are 16-bit left operands: p in tensor memory, ds in shared memory, where the same bytes are read
 //                 once along the rows (dk) and once across them (dq).  dk and dv stay in tensor memory until the key tile
 //                 is done and are written once; shared key heads sum in the same accumulator.
-//   k_grad_dq     adds the shares' dq, scales and rounds.
+//   k_grad_dq     adds the shares' dq, scales and rounds; k_grad_dkv does the same for key heads whose query heads were
+//                 split into groups.
 // Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
 // two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
@@ -31,7 +32,8 @@ struct GradArgs {
     float4* dq;                // [R][B][Hq][tiles][4][DP / 4][32]: query 32 a + l, columns 4 c .. 4 c + 3 at [a][c][l]
     AttnShape s;
     float scale, scale_log2;
-    uint32_t q_tiles, k_tiles, shares;
+    float* dkv;                // [G][2][B][Hkv][k_tiles * 128][DP]: dv, dk of one head group; null when G = 1
+    uint32_t q_tiles, k_tiles, shares, groups, group_heads;
     unsigned long long* timeouts;
 };
 
@@ -108,7 +110,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t share = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const uint32_t share = blockIdx.x % a.shares, group = blockIdx.x / a.shares, hk = blockIdx.y, b = blockIdx.z;
+    const uint32_t heads = a.group_heads, h0 = hk * a.s.rep + group * heads;        // this block's query heads
     const uint32_t lq = length_of(a.s.q_lens, b, a.s.Sq), lk = length_of(a.s.k_lens, b, a.s.Sk);
     const uint32_t nq = (lq + 127) / 128, nk = lq ? (lk + 127) / 128 : 0;
     // query tiles per head that key tile j meets
@@ -166,8 +169,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 load_tile<NS>(smem + L::V, a.v, &s.kv_full, j * 128, hk, b);
             }
             ++w;
-            for (uint32_t t = 0; t < per_head * a.s.rep && ok; ++t, ++n) {
-                const uint32_t h = hk * a.s.rep + t / per_head, i = nq - per_head + t % per_head;
+            for (uint32_t t = 0; t < per_head * heads && ok; ++t, ++n) {
+                const uint32_t h = h0 + t / per_head, i = nq - per_head + t % per_head;
                 const bool cut = i * 128 + 128 > lq && lq < a.s.Sq;
                 const uint32_t sq = n % NQ, sg = n % NG;
                 if (n >= NQ) ok = warp_wait(&s.q_empty[sq], (n / NQ - 1) & 1, g);
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 mma_commit(leader, &s.dp_full);
             };
             for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
-                const uint32_t pairs = meets(share_tile(share, m, a.shares)) * a.s.rep;
+                const uint32_t pairs = meets(share_tile(share, m, a.shares)) * heads;
                 if (pairs == 0) continue;
                 ok = warp_wait(&s.kv_full, w & 1, g);
                 scores(n);
@@ -324,10 +327,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         };
 
         for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
-            const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * a.s.rep;
+            const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * heads;
             if (j >= a.k_tiles) continue;
             const uint32_t key = j * 128 + row;
-            for (uint32_t t = 0, i = nq - per_head, h = hk * a.s.rep; t < pairs; ++t, ++n) {
+            for (uint32_t t = 0, i = nq - per_head, h = h0; t < pairs; ++t, ++n) {
                 if (!kOwnDq && n) {                             // dp of this pair comes where dq of the last one is
                     drain(n - 1);
                     if (!ok) break;
@@ -413,6 +416,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             const bool is_dk = grp >= 2;
             const Heads& hd = is_dk ? a.dk : a.dv;
             T* dst = (T*)hd.p + (int64_t)b * hd.sb + (int64_t)key * hd.st + (int64_t)hk * hd.sh;
+            float* part = a.dkv + ((((uint64_t)(group * 2 + is_dk) * a.s.B + b) * a.s.Hkv + hk) * a.k_tiles * 128 + key) * DP;
             const float f = is_dk ? a.scale : 1.0f;
             const int c0 = (grp & 1) * (DP / 2);
             if (pairs) {
@@ -430,12 +434,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 }
 #pragma unroll
                 for (int e = 0; e < 16; e += 8) {
-                    Vec8<T> o;
                     float y[8];
 #pragma unroll
                     for (int u = 0; u < 8; ++u) y[u] = pairs ? __uint_as_float(x[e + u]) * f : 0.0f;
-                    o.set(y);
-                    if (key < a.s.Sk && (uint32_t)(c + e) < a.s.D) o.store(dst + c + e);
+                    if (a.dkv) {
+                        Vec8<float> o;
+                        o.set(y);
+                        o.store(part + c + e);
+                    } else if (key < a.s.Sk && (uint32_t)(c + e) < a.s.D) {
+                        Vec8<T> o;
+                        o.set(y);
+                        o.store(dst + c + e);
+                    }
                 }
             }
             if (pairs) {
@@ -482,29 +492,68 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
     }
 }
 
-// Shares per (sequence, key head): blocks run one to an SM, so the last round of blocks should be full; every further share
-// costs a pass over q's size in fp32.  Among R up to 8 (and no more than there are key tiles) take the least
-// rounds(R) / R, with 4 % for each share.
-static uint32_t shares_of(const dblp_attention_t* a)
+// dk and dv of shared key heads from their head groups, added in order.  Thread: 8 columns of one key; grid.z: batch, dv or dk.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) k_grad_dkv(const float* __restrict__ part, Heads dk, Heads dv, AttnShape s, uint32_t k_rows, uint32_t groups)
 {
-    const uint64_t groups = (uint64_t)a->batch * a->kv_heads, tiles = (a->k_tokens + 127) / 128, sms = 148;
-    uint32_t best = 1;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, c = at % (DP / 8) * 8, key = at / (DP / 8), hk = blockIdx.y, b = blockIdx.z >> 1, is_dk = blockIdx.z & 1;
+    if (key >= s.Sk || c >= s.D) return;
+    const uint64_t stride = 2ull * s.B * s.Hkv * k_rows * DP;
+    const float* src = part + ((((uint64_t)is_dk * s.B + b) * s.Hkv + hk) * k_rows + key) * DP + c;
+    float y[8] = {};
+    for (uint32_t g = 0; g < groups; ++g) {
+        Vec8<float> v;
+        float x[8];
+        v.load(src + g * stride);
+        v.get(x);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) y[t] += x[t];
+    }
+    const Heads& hd = is_dk ? dk : dv;
+    Vec8<T> o;
+    o.set(y);
+    o.store((T*)hd.p + (int64_t)b * hd.sb + (int64_t)key * hd.st + (int64_t)hk * hd.sh + c);
+}
+
+// How the work of one (sequence, key head) is cut: into R shares of its key tiles and, where query heads share it, G groups
+// of them.  Blocks run one to an SM, so time is about rounds x pairs a block; every share costs a pass over q's size in
+// fp32 (written, added to and read again), several groups one over k's and v's.  Microseconds from the measured 2.2 (head_dim
+// up to 64) and 3.5 a pair, and about 4 bytes a nanosecond.
+struct GradCut {
+    uint32_t shares, groups;
+};
+static GradCut cut_of(const dblp_attention_t* a)
+{
+    const uint64_t bk = (uint64_t)a->batch * a->kv_heads, kt = (a->k_tokens + 127) / 128, qt = (a->q_tokens + 127) / 128, sms = 148;
+    const uint32_t rep = a->q_heads / a->kv_heads;
+    const double dp = a->head_dim <= 64 ? 64 : 128, pair_us = a->head_dim <= 64 ? 2.2 : 3.5, half = a->flags & DBLP_ATTENTION_CAUSAL ? 0.5 : 1.0;
+    const double q_us = (double)a->batch * a->q_heads * qt * 128 * dp * 4 / 4e6, k_us = 2.0 * bk * kt * 128 * dp * 4 / 4e6;
+    GradCut best{1, 1};
     double least = 1e300;
-    for (uint32_t r = 1; r <= 8 && r <= tiles; ++r) {
-        const double cost = (double)((groups * r + sms - 1) / sms) * (double)((tiles + r - 1) / r) * (1.0 + 0.04 * r);
-        if (cost < least) { least = cost; best = r; }
+    for (uint32_t g = 1; g <= rep; ++g) {
+        if (rep % g || (g > 1 && a->batch > 32767)) continue;      // (grid limit of the final sum)
+        for (uint32_t r = 1; r <= 32 && r <= kt; ++r) {
+            const double rounds = (double)((bk * r * g + sms - 1) / sms);
+            const double us = rounds * (double)((kt + r - 1) / r) * (1.0 + qt * (rep / g) * half * pair_us) + r * half * 2 * q_us + (g > 1 ? g * k_us : 0.0);
+            if (us < least) { least = us; best = {r, g}; }
+        }
     }
     return best;
 }
 
 struct GradSpaceA {
-    uint64_t rows, dq, bytes;
-    explicit GradSpaceA(const dblp_attention_t* a)
+    uint64_t rows, dq, dkv, bytes;
+    GradCut cut;
+    explicit GradSpaceA(const dblp_attention_t* a) : cut{0, 1}
     {
         const uint64_t tiles = (uint64_t)a->batch * a->q_heads * ((a->q_tokens + 127) / 128), dp = a->head_dim <= 64 ? 64 : 128;
         rows = 0;
         dq = tiles * 1024;
-        bytes = dq + (a->k_tokens ? shares_of(a) * tiles * 128 * dp * 4 : 0);
+        dkv = bytes = dq;
+        if (!a->k_tokens) return;
+        cut = cut_of(a);
+        dkv = dq + cut.shares * tiles * 128 * dp * 4;
+        bytes = dkv + (cut.groups > 1 ? cut.groups * 2ull * a->batch * a->kv_heads * ((a->k_tokens + 127) / 128) * 128 * dp * 4 : 0);
     }
 };
 
@@ -520,7 +569,11 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
     }
     if (sh.Sk) {
         DBLP_CUDA(cudaFuncSetAttribute(k_grad<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, GradSmem<DP>::kBytes));
-        k_grad<T, DP><<<dim3(r.shares, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
+        k_grad<T, DP><<<dim3(r.shares * r.groups, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
+        DBLP_LAUNCHED();
+    }
+    if (sh.Sk && r.dkv) {
+        k_grad_dkv<T, DP><<<dim3((sh.Sk * (DP / 8) + 255) / 256, sh.Hkv, sh.B * 2), 256, 0, s>>>(r.dkv, r.dk, r.dv, sh, r.k_tiles * 128, r.groups);
         DBLP_LAUNCHED();
     }
     if (sh.Sq) {
@@ -551,7 +604,10 @@ int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const d
     r.scale_log2 = (float)(a->scale * 1.4426950408889634);
     r.q_tiles = (a->q_tokens + 127) / 128;
     r.k_tiles = (a->k_tokens + 127) / 128;
-    r.shares = a->k_tokens ? shares_of(a) : 0;
+    r.shares = sp.cut.shares;
+    r.groups = sp.cut.groups;
+    r.group_heads = r.s.rep / r.groups;
+    r.dkv = r.groups > 1 ? (float*)((uint8_t*)ws + sp.dkv) : nullptr;
     r.timeouts = timeout_counter();
     DBLP_REQUIRE(r.timeouts, DBLP_ECUDA, "attention_grad: device setup failed: %s", cudaGetErrorString(cudaGetLastError()));
     const Heads o = heads(out), go = heads(dout), hq = heads(dq);
