@@ -28,43 +28,55 @@ __device__ __forceinline__ float drop_one(const DropKey& k, uint32_t bits, float
     return bits >= k.t ? __fmul_rn(x, k.inv) : 0.0f;
 }
 
-// One thread per group of eight elements of contiguous rows (cols % 8 == 0 and 16-byte aligned rows, or everything one
-// row of n elements).  The last group of the one-row form may be short.
+// A thread takes kGroups<T> groups of eight elements of contiguous rows (cols % 8 == 0 and 16-byte aligned rows, or
+// everything one row of n elements), all loads before the first draw: one 16-byte load a thread leaves too few bytes in
+// flight (32768 x 6400 bf16: 176 us with one group, DRAM-bound with two).  The last group of the one-row form may be short.
+template <typename T> constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
+
 template <typename T, bool RES>
 __global__ void __launch_bounds__(kDropThreads)
 k_dropout(const T* x, int64_t xs, const T* res, int64_t rs, T* out, int64_t os, uint64_t n, uint32_t groups_per_row, DropKey k)
 {
-    const uint64_t g = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x, e0 = g * 8;
-    if (e0 >= n) return;
-    int64_t xo = e0, ro = e0, oo = e0;
-    if (groups_per_row) {
-        const uint64_t row = g / groups_per_row, c = (g - row * groups_per_row) * 8;
-        xo = (int64_t)row * xs + c; ro = (int64_t)row * rs + c; oo = (int64_t)row * os + c;
-    }
-    float v[8], r[8];
-    const bool full = n - e0 >= 8;
-    Vec8<T> vx, vr;
-    if (full) {
-        vx.load(x + xo);
-        if (RES) vr.load(res + ro);
-    }
-    const uint4 w = drop_draw(k, g);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    if (full) {
-        vx.get(v);
-        if (RES) vr.get(r);
+    constexpr int U = kGroups<T>;
+    const uint64_t g0 = (uint64_t)blockIdx.x * (kDropThreads * U) + threadIdx.x;
+    int64_t xo[U], ro[U], oo[U];
+    Vec8<T> vx[U], vr[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = drop_one(k, i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu, v[i]);
-            if (RES) v[i] = __fadd_rn(v[i], r[i]);
+    for (int u = 0; u < U; ++u) {
+        const uint64_t g = g0 + u * kDropThreads, e0 = g * 8;
+        xo[u] = ro[u] = oo[u] = (int64_t)e0;
+        if (groups_per_row) {
+            const uint64_t row = g / groups_per_row, c = (g - row * groups_per_row) * 8;
+            xo[u] = (int64_t)row * xs + c; ro[u] = (int64_t)row * rs + c; oo[u] = (int64_t)row * os + c;
         }
-        vx.set(v);
-        vx.store(out + oo);
-    } else {
-        for (int i = 0; i < (int)(n - e0); ++i) {
-            float y = drop_one(k, i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu, to_f32(x[xo + i]));
-            if (RES) y = __fadd_rn(y, to_f32(res[ro + i]));
-            out[oo + i] = from_f32<T>(y);
+        if (e0 + 8 <= n) {
+            vx[u].load(x + xo[u]);
+            if (RES) vr[u].load(res + ro[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint64_t g = g0 + u * kDropThreads, e0 = g * 8;
+        if (e0 >= n) break;
+        const uint4 w = drop_draw(k, g);
+        const uint32_t b[4] = {w.x, w.y, w.z, w.w};
+        if (e0 + 8 <= n) {
+            float v[8], r[8];
+            vx[u].get(v);
+            if (RES) vr[u].get(r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = drop_one(k, i & 1 ? b[i >> 1] >> 16 : b[i >> 1] & 0xFFFFu, v[i]);
+                if (RES) v[i] = __fadd_rn(v[i], r[i]);
+            }
+            vx[u].set(v);
+            vx[u].store(out + oo[u]);
+        } else {
+            for (int i = 0; i < (int)(n - e0); ++i) {
+                float y = drop_one(k, (b[i >> 1] >> (i & 1 ? 16 : 0)) & 0xFFFFu, to_f32(x[xo[u] + i]));
+                if (RES) y = __fadd_rn(y, to_f32(res[ro[u] + i]));
+                out[oo[u] + i] = from_f32<T>(y);
+            }
         }
     }
 }
@@ -95,14 +107,14 @@ static int launch_dropout(const T* x, int64_t xs, const T* res, int64_t rs, T* o
                           const DropKey& k, cudaStream_t s)
 {
     const uint64_t n = rows * cols, groups = (n + 7) / 8;
-    const unsigned grid = (unsigned)((groups + kDropThreads - 1) / kDropThreads);
+    const unsigned grid = (unsigned)((groups + kDropThreads - 1) / kDropThreads), gridv = (grid + kGroups<T> - 1) / kGroups<T>;
     const bool flat = rows == 1 || (xs == cols && os == cols && (!res || rs == cols));
     const bool vec = aligned16(x) && aligned16(out) && (!res || aligned16(res)) &&
                      (flat || (cols % 8 == 0 && xs % 8 == 0 && os % 8 == 0 && (!res || rs % 8 == 0)));
     if (vec) {
         const uint32_t gpr = flat ? 0 : cols / 8;
-        if (res) k_dropout<T, true><<<grid, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, gpr, k);
-        else k_dropout<T, false><<<grid, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, gpr, k);
+        if (res) k_dropout<T, true><<<gridv, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, gpr, k);
+        else k_dropout<T, false><<<gridv, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, gpr, k);
     } else {
         if (res) k_dropout_any<T, true><<<grid, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, cols, k);
         else k_dropout_any<T, false><<<grid, kDropThreads, 0, s>>>(x, xs, res, rs, out, os, n, cols, k);

@@ -6,11 +6,12 @@
 // pairs first makes every sum a run of the sorted list, so that nothing is added by atomics and each sum has one fixed
 // order.  The steps, all on the caller's stream:
 //   1. sort by (token, position): rank counting up to kRankMax tokens (one launch), else a radix sort by 8-bit digits (two
-//      launches a digit);
+//      launches a digit); a bitmap of the rows that occur comes with it;
 //   2. k_grad_tiles: the sorted list is cut into tiles of 32 positions whatever the runs' lengths, so a token that fills
 //      half the batch is spread over as many warps as any other rows are.  Runs inside a tile are finished; a run that
-//      crosses a tile's end leaves a partial sum.  Marks the rows that occur in a bitmap;
-//   3. k_grad_finish: joins the partial sums of crossing runs in tile order, and writes zeros to the rows that do not occur.
+//      crosses a tile's end leaves a partial sum.  Other warps of
+//      the launch write zeros to the rows that do not occur, so that reading dout and writing the table overlap;
+//   3. k_grad_join: joins the partial sums of crossing runs in tile order.
 // The floor is reading dout once and writing the table once.
 #include "types.cuh"
 
@@ -29,17 +30,18 @@ constexpr int kLookUnroll = 4;
 template <typename I, typename TI, typename TO, int G>
 __global__ void __launch_bounds__(kEmbedThreads)
 k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restrict__ tokens, uint64_t n, int64_t padding,
-        float scale, TO* __restrict__ out, int64_t os, uint32_t gpr, unsigned long long* bad)
+        float scale, TO* __restrict__ out, int64_t os, FastDiv gpr, unsigned long long* bad)
 {
-    const uint64_t items = n * gpr, base = (uint64_t)blockIdx.x * (kEmbedThreads * kLookUnroll) + threadIdx.x;
-    uint64_t row[kLookUnroll];
+    // n * groups < 2^32 a launch (the host cuts longer lists): the division by the row's groups is a multiply and a shift
+    const uint32_t items = (uint32_t)n * gpr.d, base = blockIdx.x * (kEmbedThreads * kLookUnroll) + threadIdx.x;
+    uint32_t row[kLookUnroll];
     uint32_t grp[kLookUnroll];
     int64_t tok[kLookUnroll];
 #pragma unroll
     for (int u = 0; u < kLookUnroll; ++u) {
-        const uint64_t it = base + (uint64_t)u * kEmbedThreads;
-        row[u] = it / gpr;
-        grp[u] = (uint32_t)(it - row[u] * gpr);
+        const uint32_t it = base + u * kEmbedThreads;
+        row[u] = gpr.div(it);
+        grp[u] = it - row[u] * gpr.d;
         tok[u] = it < items ? token_at(tokens, row[u]) : -1;
     }
     if constexpr (G == 8) {
@@ -50,7 +52,7 @@ k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restr
             if (tok[u] >= 0 && tok[u] < rows && tok[u] != padding) v[u].load(table + tok[u] * ts + grp[u] * 8);
 #pragma unroll
         for (int u = 0; u < kLookUnroll; ++u) {
-            if (base + (uint64_t)u * kEmbedThreads >= items) break;
+            if (base + u * kEmbedThreads >= items) break;
             const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
             if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
             Vec8<TO> o;
@@ -72,7 +74,7 @@ k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restr
             if (tok[u] >= 0 && tok[u] < rows && tok[u] != padding) v[u] = table[tok[u] * ts + grp[u]];
 #pragma unroll
         for (int u = 0; u < kLookUnroll; ++u) {
-            if (base + (uint64_t)u * kEmbedThreads >= items) break;
+            if (base + u * kEmbedThreads >= items) break;
             const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
             if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
             out[(int64_t)row[u] * os + grp[u]] = from_f32<TO>(live ? __fmul_rn(to_f32(v[u]), scale) : 0.0f);
@@ -94,14 +96,9 @@ __device__ __forceinline__ uint32_t key_of(const I* tokens, uint64_t i, int64_t 
     return (uint32_t)t;
 }
 
-__device__ __forceinline__ void clear_words(uint32_t* p, uint32_t words)
-{
-    for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < words; i += gridDim.x * blockDim.x) p[i] = 0;
-}
-
 // Stable rank by counting: a block takes 32 tokens, its 8 warps an eighth of all keys each, and lane l counts for token l
 // how many of them sort before it.  n^2 comparisons, but one launch and no dependent passes.
-constexpr uint32_t kRankMax = 8192;
+constexpr uint32_t kRankMax = 4096, kSeenWords = 128;
 
 template <typename I>
 __global__ void __launch_bounds__(256)
@@ -109,12 +106,25 @@ k_rank_sort(const I* __restrict__ tokens, uint32_t n, int64_t rows, int64_t padd
             uint32_t* __restrict__ pos, uint32_t* __restrict__ seen, uint32_t seen_words, unsigned long long* bad)
 {
     extern __shared__ uint32_t s_key[];                        // all n keys, padded to a multiple of 32 with all-ones
-    __shared__ uint32_t s_cnt[8][32];
-    clear_words(seen, seen_words);
+    __shared__ uint32_t s_cnt[8][32], s_seen[kSeenWords];
     const uint32_t n32 = (n + 31) & ~31u, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = blockIdx.x * 32 + lane;
     for (uint32_t i = threadIdx.x; i < n32; i += 256)
         s_key[i] = i < n ? key_of(tokens, i, rows, padding, i / 32 == blockIdx.x ? bad : nullptr) : 0xFFFFFFFFu;
     __syncthreads();
+    // The bitmap of the rows that occur: every block has all keys at hand and builds a share of the words.
+    for (uint32_t w0 = blockIdx.x * kSeenWords; w0 < seen_words; w0 += gridDim.x * kSeenWords) {
+        const uint32_t nw = min(kSeenWords, seen_words - w0);
+        for (uint32_t i = threadIdx.x; i < nw; i += 256) s_seen[i] = 0;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < n; i += 256) {
+            const uint32_t k = s_key[i], w = (k >> 5) - w0;
+            if (k < rows && w < nw) atomicOr(&s_seen[w], 1u << (k & 31));
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < nw; i += 256) seen[w0 + i] = s_seen[i];
+        __syncthreads();
+    }
+    if (blockIdx.x * 32 >= n32) return;                        // blocks for the bitmap alone
     const uint32_t key = s_key[mine], groups = n32 / 4, per = (groups + 7) / 8;
     const uint32_t lo = min(groups, warp * per), hi = min(groups, lo + per);
     const uint4* __restrict__ k4 = reinterpret_cast<const uint4*>(s_key);
@@ -145,10 +155,10 @@ k_rank_sort(const I* __restrict__ tokens, uint32_t n, int64_t rows, int64_t padd
     }
 }
 
-// One digit of the radix sort.  Block b owns the contiguous range of `per` items starting at b * per; table[d * blocks + b]
+// One digit of the radix sort.  Block b owns the contiguous range of `per` items starting at b * per; table[b * 256 + d]
 // is its count of digit d.
 constexpr int kRadix = 256;
-constexpr uint32_t kRadixBlocks = 148;
+constexpr uint32_t kRadixBlocks = 148, kRadixStage = 2048;     // blocks at most; items a block keeps in shared memory
 
 template <typename I, bool FIRST>
 __device__ __forceinline__ uint32_t radix_key(const I* tokens, const uint32_t* keys, uint32_t i, int64_t rows, int64_t padding,
@@ -165,29 +175,40 @@ k_radix_count(const I* __restrict__ tokens, const uint32_t* __restrict__ keys, u
 {
     __shared__ uint32_t s_hist[kRadix];
     s_hist[threadIdx.x] = 0;
-    if (FIRST) clear_words(seen, seen_words);
+    if (FIRST)
+        for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < seen_words; i += gridDim.x * 256) seen[i] = 0;
     __syncthreads();
     const uint32_t lo = blockIdx.x * per, hi = min(n, lo + per);
     for (uint32_t i = lo + threadIdx.x; i < hi; i += 256)
         atomicAdd(&s_hist[radix_key<I, FIRST>(tokens, keys, i, rows, padding, bad) >> shift & (kRadix - 1)], 1u);
     __syncthreads();
-    table[threadIdx.x * gridDim.x + blockIdx.x] = s_hist[threadIdx.x];
+    table[blockIdx.x * kRadix + threadIdx.x] = s_hist[threadIdx.x];
 }
 
 template <typename I, bool FIRST>
 __global__ void __launch_bounds__(256)
 k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos, uint32_t n,
                 uint32_t per, uint32_t shift, int64_t rows, int64_t padding, const uint32_t* __restrict__ table,
-                uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out)
+                uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out, uint32_t* __restrict__ seen)
 {
+    __shared__ uint32_t s_key[kRadixStage], s_pos[kRadixStage];
     __shared__ uint32_t s_warp[8][kRadix];                     // counts, then next free place, per warp and digit
     __shared__ uint32_t s_scan[8];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nb = gridDim.x;
     for (uint32_t i = tid; i < 8 * kRadix; i += 256) (&s_warp[0][0])[i] = 0;
+    const uint32_t blo = blockIdx.x * per, bhi = min(n, blo + per);
+    const bool staged = per <= kRadixStage;
+    if (staged)
+        for (uint32_t i = blo + tid; i < bhi; i += 256) {
+            s_key[i - blo] = radix_key<I, FIRST>(tokens, keys, i, rows, padding, nullptr);
+            s_pos[i - blo] = FIRST ? i : pos[i];
+        }
+    auto key_at = [&](uint32_t i) { return staged ? s_key[i - blo] : radix_key<I, FIRST>(tokens, keys, i, rows, padding, nullptr); };
     // place of this block's first item of digit `tid`: items of smaller digits, then those of earlier blocks
     uint32_t before = 0, total = 0;
+#pragma unroll 32
     for (uint32_t b = 0; b < nb; ++b) {
-        const uint32_t c = table[tid * nb + b];
+        const uint32_t c = table[b * kRadix + tid];
         before += b < blockIdx.x ? c : 0;
         total += c;
     }
@@ -202,10 +223,10 @@ k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys,
     uint32_t base = x - total + before;
     for (uint32_t w = 0; w < warp; ++w) base += s_scan[w];
     // a warp's share of the block's items is contiguous and a multiple of 32, so warp order is item order
-    const uint32_t blo = blockIdx.x * per, bhi = min(n, blo + per), wper = per / 8;
+    const uint32_t wper = per / 8;
     const uint32_t lo = min(bhi, blo + warp * wper), hi = min(bhi, lo + wper);
     for (uint32_t i = lo + lane; i < hi; i += 32)
-        atomicAdd(&s_warp[warp][radix_key<I, FIRST>(tokens, keys, i, rows, padding, nullptr) >> shift & (kRadix - 1)], 1u);
+        atomicAdd(&s_warp[warp][key_at(i) >> shift & (kRadix - 1)], 1u);
     __syncthreads();
     for (uint32_t w = 0; w < 8; ++w) {
         const uint32_t c = s_warp[w][tid];
@@ -218,13 +239,14 @@ k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys,
         const bool in = i < hi;
         const uint32_t active = __ballot_sync(0xFFFFFFFFu, in);
         if (in) {
-            const uint32_t key = radix_key<I, FIRST>(tokens, keys, i, rows, padding, nullptr);
+            const uint32_t key = key_at(i);
             const uint32_t d = key >> shift & (kRadix - 1), same = __match_any_sync(active, d);
             const uint32_t at = s_warp[warp][d] + __popc(same & ((1u << lane) - 1));
             __syncwarp(active);
             if ((same >> lane) == 1u) s_warp[warp][d] = at + 1;  // the highest lane of the digit
             keys_out[at] = key;
-            pos_out[at] = FIRST ? i : pos[i];
+            pos_out[at] = staged ? s_pos[i - blo] : FIRST ? i : pos[i];
+            if (FIRST && key < rows && !(*(volatile uint32_t*)&seen[key >> 5] >> (key & 31) & 1)) atomicOr(&seen[key >> 5], 1u << (key & 31));
         }
         __syncwarp();
     }
@@ -274,15 +296,38 @@ __device__ __forceinline__ void finish_row(T* p, float* acc, float scale, bool a
     store_group<T, G>(p, acc);
 }
 
+// Warps from `sum_warps` on write zeros to the rows that no token names, kZeroRows rows each.
+constexpr uint32_t kZeroRows = 4;
+
+template <typename TO, int G>
+__device__ __forceinline__ void zero_rows(uint32_t r0, const uint32_t* __restrict__ seen, uint32_t rows, uint32_t width, TO* __restrict__ dtable, int64_t ts)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    if (r0 >= rows) return;
+    uint32_t absent = ~seen[r0 >> 5] >> (r0 & 31) & ((1u << kZeroRows) - 1);
+    if (rows - r0 < kZeroRows) absent &= (1u << (rows - r0)) - 1;
+    float z[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) z[i] = 0.0f;
+    for (; absent; absent &= absent - 1) {
+        TO* p = dtable + (int64_t)(r0 + __ffs(absent) - 1) * ts;
+        for (uint32_t c = lane * G; c < width; c += 32 * G) store_group<TO, G>(p + c, z);
+    }
+}
+
 template <typename TI, typename TO, int G>
 __global__ void __launch_bounds__(kGradWarps * 32)
 k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
              uint32_t n, uint32_t rows, uint32_t width, uint32_t slabs, float scale, TO* __restrict__ dtable, int64_t ts,
-             uint32_t accumulate, float* __restrict__ part, uint32_t* __restrict__ seen)
+             uint32_t accumulate, float* __restrict__ part, const uint32_t* __restrict__ seen, uint64_t sum_warps)
 {
     constexpr int kAhead = G == 8 ? (sizeof(TI) == 2 ? 8 : 4) : 16;     // rows in flight a lane
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t w = (uint64_t)blockIdx.x * kGradWarps + (threadIdx.x >> 5);
+    if (w >= sum_warps) {
+        zero_rows<TO, G>((uint32_t)(w - sum_warps) * kZeroRows, seen, rows, width, dtable, ts);
+        return;
+    }
     const uint32_t tile = (uint32_t)(w / slabs), slab = (uint32_t)(w - (uint64_t)tile * slabs);
     const uint64_t p0 = (uint64_t)tile * kTile;
     if (p0 >= n) return;
@@ -291,8 +336,6 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
     const uint32_t prev = p0 ? keys[p0 - 1] : 0xFFFFFFFFu, next = p0 + cnt < n ? keys[p0 + cnt] : 0xFFFFFFFFu;
     const uint32_t live = __popc(__ballot_sync(0xFFFFFFFFu, key < rows));      // keys >= rows are at the end
     if (live == 0) return;
-    const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, key, 1);
-    if (slab == 0 && lane < live && key != (lane ? up : prev)) atomicOr(&seen[key >> 5], 1u << (key & 31));
 
     const uint32_t c0 = (slab * 32 + lane) * G;
     const bool in = c0 < width;
@@ -343,69 +386,81 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
     }
 }
 
-// Blocks below `join_blocks` take one (tile, slab) each: if a run begins in the tile and goes on, they add its partial
-// sums, slot 1 of this tile and slot 0 of the following ones, in 8 contiguous parts by 8 warps that are then joined in
-// order (runs over fewer than 8 tiles: by the first warp alone).  The other blocks write zeros to the rows whose bit is
-// not set, kZeroRows rows each.
-constexpr uint32_t kZeroRows = 32;
+// Joining a run that crosses tiles: slot 1 of the tile in which it begins, then slot 0 of each tile that continues it, in
+// tile order.  A tile continues a run when its first key is the key before it.
+// Short runs (up to kLongRun - 1 partial sums): one warp a (tile, slab), which ends at once unless a run begins in its tile
+// and goes on.  Longer ones: a run of kLongRun or more sums continues over at least one tile whose number is a multiple of 64;
+// the first such tile names the run, and a block adds it in 8 contiguous parts by 8 warps, joined in order.
+constexpr uint32_t kLongRun = 65;
+
+__device__ __forceinline__ bool continues(const uint32_t* __restrict__ keys, uint32_t tile, uint32_t tiles, uint32_t key)
+{
+    return tile > 0 && tile < tiles && keys[(uint64_t)tile * kTile] == key && keys[(uint64_t)tile * kTile - 1] == key;
+}
+
+// Tiles from `from` on, one after the other, that continue key's run.
+__device__ __forceinline__ uint32_t continued(const uint32_t* __restrict__ keys, uint32_t from, uint32_t tiles, uint32_t key)
+{
+    uint32_t more = 0;
+    for (uint32_t t = from;; t += 32) {
+        const uint32_t b = __ballot_sync(0xFFFFFFFFu, continues(keys, t + (threadIdx.x & 31), tiles, key));
+        more += b == 0xFFFFFFFFu ? 32 : __ffs(~b) - 1;
+        if (b != 0xFFFFFFFFu) return more;
+    }
+}
+
+// Terms lo .. hi - 1 of the run that begins in `tile`, columns c0 ..
+template <int G>
+__device__ __forceinline__ void add_terms(const float* __restrict__ part, uint32_t tile, uint32_t lo, uint32_t hi, uint32_t width, uint32_t c0, float* acc)
+{
+#pragma unroll 8
+    for (uint32_t m = lo; m < hi; ++m) {
+        float x[G];
+        load_group<float, G>(part + ((uint64_t)(tile + m) * 2 + (m == 0 ? 1 : 0)) * width + c0, x);
+#pragma unroll
+        for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], x[i]);
+    }
+}
 
 template <typename TO, int G>
 __global__ void __launch_bounds__(kGradWarps * 32)
-k_grad_finish(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32_t width, uint32_t slabs, float scale,
-              TO* __restrict__ dtable, int64_t ts, uint32_t accumulate, const float* __restrict__ part,
-              const uint32_t* __restrict__ seen, uint32_t join_blocks)
+k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32_t width, uint32_t slabs, float scale,
+            TO* __restrict__ dtable, int64_t ts, uint32_t accumulate, const float* __restrict__ part, uint32_t short_blocks)
 {
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (blockIdx.x >= join_blocks) {
-        const uint32_t r0 = (blockIdx.x - join_blocks) * kZeroRows;
-        uint32_t absent = ~seen[r0 >> 5];
-        if (rows - r0 < 32) absent &= (1u << (rows - r0)) - 1;
-        float z[G];
-#pragma unroll
-        for (int i = 0; i < G; ++i) z[i] = 0.0f;
-        for (uint32_t m = absent; m; m &= m - 1) {
-            TO* row = dtable + (int64_t)(r0 + __ffs(m) - 1) * ts;
-            for (uint32_t c = threadIdx.x * G; c < width; c += kGradWarps * 32 * G) store_group<TO, G>(row + c, z);
-        }
-        return;
-    }
     __shared__ float s_part[kGradWarps][32 * G];
-    const uint32_t tile = blockIdx.x / slabs, slab = blockIdx.x - tile * slabs, tiles = (n + kTile - 1) / kTile;
-    const uint64_t p0 = (uint64_t)tile * kTile;
-    if (p0 + kTile >= n) return;                                        // the last tile: nothing goes on
-    const uint32_t key = keys[p0 + kTile - 1];
-    if (key >= rows || keys[p0 + kTile] != key) return;
-    if (p0 && keys[p0 - 1] == key) return;                              // began in an earlier tile
-    // tiles after this one whose first key is still `key`
-    uint32_t more = 0;
-    for (uint32_t t = tile + 1; ; t += 32) {
-        const bool same = t + lane < tiles && keys[(uint64_t)(t + lane) * kTile] == key;
-        const uint32_t b = __ballot_sync(0xFFFFFFFFu, same);
-        more += b == 0xFFFFFFFFu ? 32 : __ffs(~b) - 1;
-        if (b != 0xFFFFFFFFu) break;
-    }
-    const uint32_t c0 = (slab * 32 + lane) * G, terms = more + 1;
-    const bool in = c0 < width;
-    const uint32_t parts = terms < 8 ? 1 : 8, per = (terms + parts - 1) / parts;
-    const uint32_t lo = min(terms, warp * per), hi = warp < parts ? min(terms, lo + per) : lo;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = (n + kTile - 1) / kTile;
     float acc[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) acc[i] = 0.0f;
-    if (in) {
-#pragma unroll 4
-        for (uint32_t m = lo; m < hi; ++m) {
-            const float* q = part + ((uint64_t)(tile + m) * 2 + (m == 0 ? 1 : 0)) * width + c0;
-            float x[G];
-            load_group<float, G>(q, x);
-#pragma unroll
-            for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], x[i]);
-        }
+    if (blockIdx.x < short_blocks) {
+        const uint64_t w = (uint64_t)blockIdx.x * kGradWarps + warp;
+        const uint32_t tile = (uint32_t)(w / slabs), slab = (uint32_t)(w - (uint64_t)tile * slabs), c0 = (slab * 32 + lane) * G;
+        if (tile + 1 >= tiles) return;                                  // nothing goes on from the last tile
+        const uint64_t end = (uint64_t)(tile + 1) * kTile;
+        const uint32_t key = keys[end - 1];
+        if (key >= rows || keys[end] != key || continues(keys, tile, tiles, key)) return;
+        const uint32_t terms = 1 + continued(keys, tile + 1, tiles, key);
+        if (terms >= kLongRun || c0 >= width) return;
+        add_terms<G>(part, tile, 0, terms, width, c0, acc);
+        finish_row<TO, G>(dtable + (int64_t)key * ts + c0, acc, scale, accumulate);
+        return;
     }
+    const uint32_t at = blockIdx.x - short_blocks, u = (at / slabs + 1) * 64, slab = at % slabs, c0 = (slab * 32 + lane) * G;
+    const uint32_t key = keys[(uint64_t)u * kTile];
+    if (key >= rows || !continues(keys, u, tiles, key) || continues(keys, u - 64, tiles, key)) return;
+    // u - 64 does not continue the run, so it begins in one of the 64 tiles before u
+    const uint32_t b0 = __ballot_sync(0xFFFFFFFFu, continues(keys, u - 1 - lane, tiles, key));
+    const uint32_t b1 = __ballot_sync(0xFFFFFFFFu, continues(keys, u - 33 - lane, tiles, key));
+    const uint32_t back = b0 != 0xFFFFFFFFu ? __ffs(~b0) - 1 : 32 + __ffs(~b1) - 1;
+    const uint32_t tile = u - back - 1, terms = 1 + back + continued(keys, u, tiles, key);
+    if (terms < kLongRun) return;
+    const uint32_t per = (terms + kGradWarps - 1) / kGradWarps, lo = min(terms, warp * per), hi = min(terms, lo + per);
+    if (c0 < width) add_terms<G>(part, tile, lo, hi, width, c0, acc);
 #pragma unroll
     for (int i = 0; i < G; ++i) s_part[warp][lane * G + i] = acc[i];
     __syncthreads();
-    if (warp || !in) return;
-    for (uint32_t p = 1; p < parts; ++p)
+    if (warp || c0 >= width) return;
+    for (int p = 1; p < kGradWarps; ++p)
 #pragma unroll
         for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], s_part[p][lane * G + i]);
     finish_row<TO, G>(dtable + (int64_t)key * ts + c0, acc, scale, accumulate);
@@ -437,12 +492,16 @@ static int sort_tokens(const I* tokens, uint32_t n, uint32_t rows, int64_t paddi
     const uint32_t seen_words = (rows + 31) / 32;
     if (n <= kRankMax) {
         const uint32_t n32 = (n + 31) & ~31u;
-        k_rank_sort<I><<<n32 / 32, 256, n32 * 4, s>>>(tokens, n, rows, padding, k[0], p[0], seen, seen_words, bad);
+        const uint32_t for_seen = (seen_words + kSeenWords - 1) / kSeenWords;
+        const uint32_t grid = n32 / 32 > for_seen ? n32 / 32 : for_seen < 148 ? for_seen : 148;
+        k_rank_sort<I><<<grid, 256, n32 * 4, s>>>(tokens, n, rows, padding, k[0], p[0], seen, seen_words, bad);
         DBLP_LAUNCHED();
         *keys = k[0]; *pos = p[0];
         return DBLP_OK;
     }
-    uint32_t per = (n + kRadixBlocks - 1) / kRadixBlocks;
+    // Every block reads all blocks' counts: up to 64 of them while a block's items fit in its shared memory, then more.
+    uint32_t per = (n + 63) / 64;
+    if (per > kRadixStage) per = (n + kRadixBlocks - 1) / kRadixBlocks > kRadixStage ? (n + kRadixBlocks - 1) / kRadixBlocks : kRadixStage;
     per = (per + 255) / 256 * 256;
     const uint32_t nb = (n + per - 1) / per;
     int from = 1;
@@ -451,11 +510,11 @@ static int sort_tokens(const I* tokens, uint32_t n, uint32_t rows, int64_t paddi
         if (shift == 0) {
             k_radix_count<I, true><<<nb, 256, 0, s>>>(tokens, nullptr, n, per, shift, rows, padding, table, seen, seen_words, bad);
             DBLP_LAUNCHED();
-            k_radix_scatter<I, true><<<nb, 256, 0, s>>>(tokens, nullptr, nullptr, n, per, shift, rows, padding, table, k[to], p[to]);
+            k_radix_scatter<I, true><<<nb, 256, 0, s>>>(tokens, nullptr, nullptr, n, per, shift, rows, padding, table, k[to], p[to], seen);
         } else {
-            k_radix_count<I, false><<<nb, 256, 0, s>>>(tokens, k[from], n, per, shift, rows, padding, table, seen, seen_words, nullptr);
+            k_radix_count<I, false><<<nb, 256, 0, s>>>(tokens, k[from], n, per, shift, rows, padding, table, nullptr, 0, nullptr);
             DBLP_LAUNCHED();
-            k_radix_scatter<I, false><<<nb, 256, 0, s>>>(tokens, k[from], p[from], n, per, shift, rows, padding, table, k[to], p[to]);
+            k_radix_scatter<I, false><<<nb, 256, 0, s>>>(tokens, k[from], p[from], n, per, shift, rows, padding, table, k[to], p[to], seen);
         }
         DBLP_LAUNCHED();
         from = to;
@@ -466,21 +525,21 @@ static int sort_tokens(const I* tokens, uint32_t n, uint32_t rows, int64_t paddi
 
 template <typename TI, typename TO, int G>
 static int launch_sums(const TI* dout, int64_t ds, const uint32_t* keys, const uint32_t* pos, uint32_t n, uint32_t rows, uint32_t width,
-                       float scale, TO* dtable, int64_t ts, uint32_t accumulate, float* part, uint32_t* seen, cudaStream_t s)
+                       float scale, TO* dtable, int64_t ts, uint32_t accumulate, float* part, const uint32_t* seen, cudaStream_t s)
 {
     const uint32_t slabs = (width + 32 * G - 1) / (32 * G), tiles = (n + kTile - 1) / kTile;
-    const uint64_t warps = (uint64_t)tiles * slabs, grid = (warps + kGradWarps - 1) / kGradWarps;
-    // join blocks exist where a run can cross tiles; zero blocks unless the rows are accumulated into
-    const uint64_t join = tiles > 1 ? warps : 0, zero = accumulate ? 0 : (rows + kZeroRows - 1) / kZeroRows;
-    DBLP_REQUIRE(grid < (1ull << 31) && join + zero < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
-    if (tiles) {
-        k_grad_tiles<TI, TO, G><<<(unsigned)grid, kGradWarps * 32, 0, s>>>(dout, ds, keys, pos, n, rows, width, slabs, scale, dtable, ts,
-                                                                         accumulate, part, seen);
-        DBLP_LAUNCHED();
-    }
-    if (join + zero) {
-        k_grad_finish<TO, G><<<(unsigned)(join + zero), kGradWarps * 32, 0, s>>>(keys, n, rows, width, slabs, scale, dtable, ts,
-                                                                               accumulate, part, seen, (uint32_t)join);
+    const uint64_t sums = (uint64_t)tiles * slabs, zeros = accumulate ? 0 : (rows + kZeroRows - 1) / kZeroRows;
+    const uint64_t sum_warps = (sums + kGradWarps - 1) / kGradWarps * kGradWarps;      // whole blocks of either kind
+    const uint64_t grid = (sum_warps + zeros + kGradWarps - 1) / kGradWarps;
+    DBLP_REQUIRE(grid < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
+    k_grad_tiles<TI, TO, G><<<(unsigned)grid, kGradWarps * 32, 0, s>>>(dout, ds, keys, pos, n, rows, width, slabs, scale, dtable, ts,
+                                                                     accumulate, part, seen, sum_warps);
+    DBLP_LAUNCHED();
+    if (tiles > 1) {                                                   // a run can cross tiles
+        const uint64_t brief = ((tiles - 1ull) * slabs + kGradWarps - 1) / kGradWarps, lengthy = (uint64_t)((tiles - 1) / 64) * slabs;
+        DBLP_REQUIRE(brief + lengthy < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
+        k_grad_join<TO, G><<<(unsigned)(brief + lengthy), kGradWarps * 32, 0, s>>>(keys, n, rows, width, slabs, scale, dtable, ts, accumulate,
+                                                                                  part, (uint32_t)brief);
         DBLP_LAUNCHED();
     }
     return DBLP_OK;
@@ -519,19 +578,24 @@ extern "C" int dblp_embed(const void* table, int64_t table_stride, uint64_t rows
     DBLP_REQUIRE((uintptr_t)table % tb == 0 && (uintptr_t)out % ob == 0, DBLP_EALIGN, "embed: a pointer is not aligned to its type");
     const bool vec = width % 8 == 0 && vector_rows(table, table_stride, rows, tb) && vector_rows(out, out_stride, n, ob);
     const uint32_t gpr = vec ? width / 8 : width;
-    const uint64_t grid = (n * gpr + kEmbedThreads * kLookUnroll - 1) / (kEmbedThreads * kLookUnroll);
-    DBLP_REQUIRE(grid < (1ull << 31), DBLP_ECAPACITY, "embed: too many elements in one call");
-    return with_type(table_dtype, [&](auto ti) {
-        return with_type(out_dtype, [&](auto to) {
+    const uint64_t most = 0xFFFF0000u / gpr;                            // tokens a launch: its items fit in 32 bits
+    return with_type(table_dtype, [&](auto ti) -> int {
+        return with_type(out_dtype, [&](auto to) -> int {
             using TI = decltype(ti);
             using TO = decltype(to);
             auto launch = [&](auto id) -> int {
                 using I = decltype(id);
-                if (vec) k_embed<I, TI, TO, 8><<<(unsigned)grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
-                    (const TI*)table, table_stride, (int64_t)rows, (const I*)tokens, n, padding, scale, (TO*)out, out_stride, gpr, (unsigned long long*)bad_tokens);
-                else k_embed<I, TI, TO, 1><<<(unsigned)grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
-                    (const TI*)table, table_stride, (int64_t)rows, (const I*)tokens, n, padding, scale, (TO*)out, out_stride, gpr, (unsigned long long*)bad_tokens);
-                DBLP_LAUNCHED();
+                for (uint64_t first = 0; first < n; first += most) {
+                    const uint64_t m = n - first < most ? n - first : most;
+                    const unsigned grid = (unsigned)((m * gpr + kEmbedThreads * kLookUnroll - 1) / (kEmbedThreads * kLookUnroll));
+                    const I* tk = (const I*)tokens + first;
+                    TO* o = (TO*)out + (int64_t)first * out_stride;
+                    if (vec) k_embed<I, TI, TO, 8><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
+                        (const TI*)table, table_stride, (int64_t)rows, tk, m, padding, scale, o, out_stride, FastDiv(gpr), (unsigned long long*)bad_tokens);
+                    else k_embed<I, TI, TO, 1><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
+                        (const TI*)table, table_stride, (int64_t)rows, tk, m, padding, scale, o, out_stride, FastDiv(gpr), (unsigned long long*)bad_tokens);
+                    DBLP_LAUNCHED();
+                }
                 return DBLP_OK;
             };
             return token_bytes == 4 ? launch(int32_t()) : launch(int64_t());
@@ -568,8 +632,8 @@ extern "C" int dblp_embed_grad(const void* dout, int64_t dout_stride, int dout_d
     DBLP_REQUIRE(ws_bytes >= sp.bytes, DBLP_ECAPACITY, "embed_grad: workspace of %zu bytes, needs %llu", ws_bytes, (unsigned long long)sp.bytes);
     uint8_t* w = (uint8_t*)ws;
     cudaStream_t s = (cudaStream_t)stream;
-    uint32_t* seen = (uint32_t*)(w + sp.seen);
     const uint32_t *keys = (const uint32_t*)(w + sp.keys[0]), *pos = (const uint32_t*)(w + sp.pos[0]);
+    uint32_t* seen = (uint32_t*)(w + sp.seen);
     if (n == 0) {
         DBLP_CUDA(cudaMemsetAsync(seen, 0, (rows + 31) / 32 * 4, s));
     } else {

@@ -511,3 +511,16 @@ def test_gradient_is_the_difference_quotient():
 
 def test_no_wait_ran_out():
     assert dblp.dblp_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("first", [0, 1, 31, 32, 33, 63 * 32, 64 * 32, 64 * 32 + 1, 64 * 32 - 1])
+@pytest.mark.parametrize("length", [1, 32, 33, 63 * 32, 64 * 32, 64 * 32 + 40, 65 * 32, 130 * 32, 200 * 32 + 5])
+def test_embed_grad_runs_of_every_length_at_every_place(first, length):
+    """One long run between two others, beginning and ending around tile boundaries of the sorted list."""
+    rows, width = 5, 16
+    tokens = torch.cat([torch.full((c,), v, dtype=torch.int32, device=DEV) for v, c in ((1, first), (2, length), (4, 50))])
+    tokens = tokens[torch.randperm(tokens.numel(), generator=torch.Generator().manual_seed(first + length)).to(DEV)]
+    dout = randn((tokens.numel(), width), F32, 77)
+    dtable = embed_grad(dout, tokens, rows, torch.full((rows, width), 5.0, device=DEV))
+    want, tol = grad_and_bound(dout, tokens, rows, 1.0, F32)
+    within(dtable, want, tol, "dtable")
