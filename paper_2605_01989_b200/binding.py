@@ -436,8 +436,15 @@ def _dtype(t):
 def _on_device(*tensors):
     """The library launches on the current device: every tensor has to be there."""
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        if t is not None and (t.get_device() < 0 or t.get_device() != torch._C._cuda_getDevice()):
             raise ValueError("a tensor on %s, which is not the current device" % t.device)
+
+
+def _raw_stream(stream):
+    """The stream's handle as a number; the current stream's without building a torch.cuda.Stream."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _require(ok, what):
@@ -446,35 +453,46 @@ def _require(ok, what):
 
 
 def _rows(t, name):
-    """(address, row stride) of a 2-D tensor whose elements within a row are contiguous."""
-    _require(t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: 2-D, contiguous within a row" % name)
-    return t.data_ptr(), t.stride(0)
+    """(address, row stride, rows, columns) of a 2-D tensor whose elements within a row are contiguous."""
+    if t.dim() != 2:
+        raise ValueError("%s: 2-D" % name)
+    (rows, cols), (rs, cs) = t.shape, t.stride()
+    if cs != 1 and cols > 1:
+        raise ValueError("%s: contiguous within a row" % name)
+    return t.data_ptr(), rs, rows, cols
+
+
+_TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 def _flat_tokens(tokens):
-    _require(tokens.dim() == 1 and tokens.dtype in (torch.int32, torch.int64) and tokens.is_contiguous(),
-             "tokens: 1-D, contiguous, int32 or int64")
-    return tokens.data_ptr(), tokens.element_size(), tokens.shape[0]
+    b = _TOKEN_BYTES.get(tokens.dtype)
+    if b is None or tokens.dim() != 1 or not tokens.is_contiguous():
+        raise ValueError("tokens: 1-D, contiguous, int32 or int64")
+    return tokens.data_ptr(), b, tokens.shape[0]
 
 
 def _counter(t):
-    _require(t is None or (t.dtype == torch.int64 and t.numel() == 1), "bad_tokens: one int64")
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    _require(t.dtype == torch.int64 and t.numel() == 1, "bad_tokens: one int64")
+    return t.data_ptr()
 
 
 def _scratch(ws):
-    return (None, 0) if ws is None or ws.numel() == 0 else (ws.data_ptr(), ws.numel() * ws.element_size())
+    return (None, 0) if ws is None or ws.numel() == 0 else (ws.data_ptr(), ws.nbytes)
 
 
 def dblp_embed(table, tokens, out, scale=1.0, padding=-1, bad_tokens=None, stream=None):
     """out[i] = scale * table[tokens[i]]; a zero row for the padding id and for ids outside the table."""
     _on_device(table, tokens, out, bad_tokens)
-    tp, ts = _rows(table, "table")
-    op, os_ = _rows(out, "out")
+    tp, ts, rows, width = _rows(table, "table")
+    op, os_, m, w = _rows(out, "out")
     kp, kb, n = _flat_tokens(tokens)
-    _require(out.shape == (n, table.shape[1]), "out: one row of the table's width per token")
-    _check(lib().dblp_embed(tp, ts, table.shape[0], table.shape[1], _dtype(table), kp, kb, n, padding, scale, op, os_,
-                            _dtype(out), _counter(bad_tokens), _stream(stream)), "dblp_embed")
+    if m != n or w != width:
+        raise ValueError("out: one row of the table's width per token")
+    _check(lib().dblp_embed(tp, ts, rows, width, _dtype(table), kp, kb, n, padding, scale, op, os_, _dtype(out),
+                            _counter(bad_tokens), _raw_stream(stream)), "dblp_embed")
 
 
 def dblp_embed_grad_workspace_bytes(n, rows, width):
@@ -486,60 +504,78 @@ def dblp_embed_grad_workspace_bytes(n, rows, width):
 def dblp_embed_grad(dout, tokens, dtable, ws, scale=1.0, padding=-1, accumulate=False, bad_tokens=None, stream=None):
     """dtable[v] = scale * sum of dout[i] over the i with tokens[i] = v (added to dtable with accumulate)."""
     _on_device(dout, tokens, dtable, ws, bad_tokens)
-    dp, ds = _rows(dout, "dout")
-    tp, ts = _rows(dtable, "dtable")
+    dp, ds, m, w = _rows(dout, "dout")
+    tp, ts, rows, width = _rows(dtable, "dtable")
     kp, kb, n = _flat_tokens(tokens)
-    _require(dout.shape == (n, dtable.shape[1]), "dout: one row of the table's width per token")
+    if m != n or w != width:
+        raise ValueError("dout: one row of the table's width per token")
     wp, wb = _scratch(ws)
-    _check(lib().dblp_embed_grad(dp, ds, _dtype(dout), kp, kb, n, padding, scale, tp, ts, dtable.shape[0], dtable.shape[1],
-                                 _dtype(dtable), DBLP_ACCUMULATE if accumulate else 0, _counter(bad_tokens), wp, wb,
-                                 _stream(stream)), "dblp_embed_grad")
+    _check(lib().dblp_embed_grad(dp, ds, _dtype(dout), kp, kb, n, padding, scale, tp, ts, rows, width, _dtype(dtable),
+                                 DBLP_ACCUMULATE if accumulate else 0, _counter(bad_tokens), wp, wb, _raw_stream(stream)),
+           "dblp_embed_grad")
 
 
 def dblp_dropout(x, out, p, seed, step, site, residual=None, stream=None):
     """out = dropout(x) [+ residual]; (seed, step, site) names the mask."""
     _on_device(x, out, residual)
-    xp, xs = _rows(x, "x")
-    op, os_ = _rows(out, "out")
-    rp, rs = (None, 0) if residual is None else _rows(residual, "residual")
-    _require(out.shape == x.shape and (residual is None or residual.shape == x.shape), "x, residual and out: one shape")
-    _require(out.dtype == x.dtype and (residual is None or residual.dtype == x.dtype), "x, residual and out: one dtype")
-    _check(lib().dblp_dropout(xp, xs, rp, rs, op, os_, x.shape[0], x.shape[1], _dtype(x), p, seed, step, site,
-                              _stream(stream)), "dblp_dropout")
+    xp, xs, rows, cols = _rows(x, "x")
+    op, os_, m, w = _rows(out, "out")
+    rp = rs = None
+    same = m == rows and w == cols and out.dtype == x.dtype
+    if residual is not None:
+        rp, rs, m, w = _rows(residual, "residual")
+        same = same and m == rows and w == cols and residual.dtype == x.dtype
+    if not same:
+        raise ValueError("x, residual and out: one shape and dtype")
+    _check(lib().dblp_dropout(xp, xs, rp, rs or 0, op, os_, rows, cols, _dtype(x), p, seed, step, site, _raw_stream(stream)),
+           "dblp_dropout")
 
 
 def dblp_dropout_grad(dout, dx, p, seed, step, site, stream=None):
     """Gradient of dblp_dropout's x: the mask of (seed, step, site) drawn again."""
     _on_device(dout, dx)
-    gp, gs = _rows(dout, "dout")
-    xp, xs = _rows(dx, "dx")
-    _require(dx.shape == dout.shape and dx.dtype == dout.dtype, "dout and dx: one shape and dtype")
-    _check(lib().dblp_dropout_grad(gp, gs, xp, xs, dx.shape[0], dx.shape[1], _dtype(dx), p, seed, step, site,
-                                   _stream(stream)), "dblp_dropout_grad")
+    gp, gs, rows, cols = _rows(dout, "dout")
+    xp, xs, m, w = _rows(dx, "dx")
+    if m != rows or w != cols or dx.dtype != dout.dtype:
+        raise ValueError("dout and dx: one shape and dtype")
+    _check(lib().dblp_dropout_grad(gp, gs, xp, xs, rows, cols, _dtype(dx), p, seed, step, site, _raw_stream(stream)),
+           "dblp_dropout_grad")
 
 
-def _heads(t, name, like, batch, tokens, heads):
-    _require(t.dtype == like.dtype and tuple(t.shape) == (batch, tokens, heads, like.shape[3]),
-             "%s: shape %s, %s" % (name, (batch, tokens, heads, like.shape[3]), like.dtype))
+def _heads(t, name, dtype, shape):
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError("%s: shape %s, %s" % (name, shape, dtype))
     sb, st, sh, sd = t.stride()
-    _require(sd == 1 or t.shape[3] == 1, "%s: the elements of a head are contiguous" % name)
+    if sd != 1 and shape[3] > 1:
+        raise ValueError("%s: the elements of a head are contiguous" % name)
     return C.byref(dblp_heads_t(t.data_ptr(), sb, st, sh))
 
 
 def _attention(q, k, causal, scale, q_lens, k_lens):
+    """(the call's description, q's shape, k's shape)"""
     _require(q.dim() == 4 and k.dim() == 4, "q and k: [batch, tokens, heads, head_dim]")
-    B, Sq, Hq, D = q.shape
+    qs, ks = q.shape, k.shape
+    B, Sq, Hq, D = qs
+    _require(ks[0] == B and ks[3] == D, "q and k: one batch and head_dim")
     for n in (q_lens, k_lens):
-        _require(n is None or (n.dtype == torch.int32 and n.shape == (B,) and n.is_contiguous()), "lengths: int32, one per sequence")
-    return dblp_attention_t(B, Sq, k.shape[1], Hq, k.shape[2], D, _dtype(q), DBLP_ATTENTION_CAUSAL if causal else 0,
-                            D ** -0.5 if scale is None and D else scale or 0.0, None if q_lens is None else q_lens.data_ptr(),
-                            None if k_lens is None else k_lens.data_ptr())
+        if n is not None and not (n.dtype == torch.int32 and n.shape == (B,) and n.is_contiguous()):
+            raise ValueError("lengths: int32, one per sequence")
+    if scale is None:
+        scale = D ** -0.5 if D else 0.0
+    return dblp_attention_t(B, Sq, ks[1], Hq, ks[2], D, _dtype(q), DBLP_ATTENTION_CAUSAL if causal else 0, scale,
+                            None if q_lens is None else q_lens.data_ptr(), None if k_lens is None else k_lens.data_ptr()), qs, ks
+
+
+def _lse(lse, qs):
+    if lse.dtype != torch.float32 or lse.shape != (qs[0], qs[2], qs[1]) or not lse.is_contiguous():
+        raise ValueError("lse: contiguous float32 [batch, heads, tokens]")
+    return lse.data_ptr()
 
 
 def dblp_attention_workspace_bytes(q, k, causal=False):
     """(bytes for dblp_attention, bytes for dblp_attention_grad) with tensors of these shapes."""
     f, g = C.c_size_t(), C.c_size_t()
-    _check(lib().dblp_attention_workspace_bytes(C.byref(_attention(q, k, causal, None, None, None)), C.byref(f), C.byref(g)),
+    _check(lib().dblp_attention_workspace_bytes(C.byref(_attention(q, k, causal, None, None, None)[0]), C.byref(f), C.byref(g)),
            "dblp_attention_workspace_bytes")
     return int(f.value), int(g.value)
 
@@ -547,29 +583,25 @@ def dblp_attention_workspace_bytes(q, k, causal=False):
 def dblp_attention(q, k, v, out, lse=None, ws=None, causal=False, scale=None, q_lens=None, k_lens=None, stream=None):
     """q, out [batch, tokens, heads, head_dim]; k, v [batch, keys, key heads, head_dim]; lse fp32 [batch, heads, tokens]."""
     _on_device(q, k, v, out, lse, ws, q_lens, k_lens)
-    a = _attention(q, k, causal, scale, q_lens, k_lens)
-    _require(lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (a.batch, a.q_heads, a.q_tokens) and
-                             lse.is_contiguous()), "lse: contiguous float32 [batch, heads, tokens]")
+    a, qs, ks = _attention(q, k, causal, scale, q_lens, k_lens)
+    dt = q.dtype
     wp, wb = _scratch(ws)
-    _check(lib().dblp_attention(C.byref(a), _heads(q, "q", q, a.batch, a.q_tokens, a.q_heads),
-                                _heads(k, "k", q, a.batch, a.k_tokens, a.kv_heads),
-                                _heads(v, "v", q, a.batch, a.k_tokens, a.kv_heads),
-                                _heads(out, "out", q, a.batch, a.q_tokens, a.q_heads), None if lse is None else lse.data_ptr(),
-                                wp, wb, _stream(stream)), "dblp_attention")
+    _check(lib().dblp_attention(C.byref(a), _heads(q, "q", dt, qs), _heads(k, "k", dt, ks), _heads(v, "v", dt, ks),
+                                _heads(out, "out", dt, qs), None if lse is None else _lse(lse, qs), wp, wb, _raw_stream(stream)),
+           "dblp_attention")
 
 
 def dblp_attention_grad(q, k, v, out, dout, lse, dq, dk, dv, ws, causal=False, scale=None, q_lens=None, k_lens=None,
                         stream=None):
     """Gradients of dblp_attention, from its inputs, its out and lse, and dout."""
     _on_device(q, k, v, out, dout, lse, dq, dk, dv, ws, q_lens, k_lens)
-    a = _attention(q, k, causal, scale, q_lens, k_lens)
-    _require(lse.dtype == torch.float32 and tuple(lse.shape) == (a.batch, a.q_heads, a.q_tokens) and lse.is_contiguous(),
-             "lse: contiguous float32 [batch, heads, tokens]")
-    qh = [_heads(t, n, q, a.batch, a.q_tokens, a.q_heads) for t, n in ((q, "q"), (out, "out"), (dout, "dout"), (dq, "dq"))]
-    kh = [_heads(t, n, q, a.batch, a.k_tokens, a.kv_heads) for t, n in ((k, "k"), (v, "v"), (dk, "dk"), (dv, "dv"))]
+    a, qs, ks = _attention(q, k, causal, scale, q_lens, k_lens)
+    dt = q.dtype
     wp, wb = _scratch(ws)
-    _check(lib().dblp_attention_grad(C.byref(a), qh[0], kh[0], kh[1], qh[1], qh[2], lse.data_ptr(), qh[3], kh[2], kh[3], wp, wb,
-                                     _stream(stream)), "dblp_attention_grad")
+    _check(lib().dblp_attention_grad(C.byref(a), _heads(q, "q", dt, qs), _heads(k, "k", dt, ks), _heads(v, "v", dt, ks),
+                                     _heads(out, "out", dt, qs), _heads(dout, "dout", dt, qs), _lse(lse, qs),
+                                     _heads(dq, "dq", dt, qs), _heads(dk, "dk", dt, ks), _heads(dv, "dv", dt, ks), wp, wb,
+                                     _raw_stream(stream)), "dblp_attention_grad")
 
 
 def dblp_wait_timeouts():

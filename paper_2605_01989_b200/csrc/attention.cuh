@@ -62,6 +62,19 @@ int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const d
                        const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, cudaStream_t s);
 size_t attention_backward_space(const dblp_attention_t* a);
 
+// Lets kernel K use `bytes` of shared memory on the current device; asked of the runtime once per kernel and device.
+template <auto K> inline cudaError_t allow_shared(int bytes)
+{
+    static std::atomic<unsigned long long> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_acq_rel);
+    return e;
+}
+
 unsigned long long* timeout_counter();     // of the current device; null after a CUDA error
 int make_source(TileSource* t, const dblp_attention_t* a, const dblp_heads_t* h, uint32_t tokens, uint32_t nheads);
 inline Heads heads(const dblp_heads_t* h) { return h ? Heads{h->data, h->batch_stride, h->token_stride, h->head_stride} : Heads{}; }

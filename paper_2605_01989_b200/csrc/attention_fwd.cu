@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
 
 template <typename T, int DP> static int launch_forward(const FwdArgs& r, cudaStream_t s)
 {
-    DBLP_CUDA(cudaFuncSetAttribute(k_attention<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<DP>::kBytes));
+    const cudaError_t e = allow_shared<k_attention<T, DP>>(FwdSmem<DP>::kBytes);
+    DBLP_CUDA(e);
     const dim3 grid((r.s.Sq + 127) / 128, r.s.Hq, r.s.B);
     k_attention<T, DP><<<grid, kFwdThreads, FwdSmem<DP>::kBytes, s>>>(r);
     DBLP_LAUNCHED();

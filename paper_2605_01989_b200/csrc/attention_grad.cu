@@ -568,7 +568,8 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
         DBLP_LAUNCHED();
     }
     if (sh.Sk) {
-        DBLP_CUDA(cudaFuncSetAttribute(k_grad<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, GradSmem<DP>::kBytes));
+        const cudaError_t e = allow_shared<k_grad<T, DP>>(GradSmem<DP>::kBytes);
+    DBLP_CUDA(e);
         k_grad<T, DP><<<dim3(r.shares * r.groups, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
         DBLP_LAUNCHED();
     }
