@@ -54,6 +54,11 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t first)
     fence_async_smem();
 }
 
+// dblp_attention for few queries a key head (attention_rows.cu)
+bool few_rows(const dblp_attention_t* a);
+size_t rows_space(const dblp_attention_t* a);
+int attention_rows(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
+                   const dblp_heads_t* out, float* lse, void* ws, cudaStream_t s);
 int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                       const dblp_heads_t* out, float* lse, void* ws, cudaStream_t s);
 size_t attention_forward_space(const dblp_attention_t* a);

@@ -295,11 +295,12 @@ template <typename T, int DP> static int launch_forward(const FwdArgs& r, cudaSt
     return DBLP_OK;
 }
 
-size_t attention_forward_space(const dblp_attention_t*) { return 0; }
+size_t attention_forward_space(const dblp_attention_t* a) { return few_rows(a) ? rows_space(a) : 0; }
 
 int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
-                      const dblp_heads_t* out, float* lse, void*, cudaStream_t s)
+                      const dblp_heads_t* out, float* lse, void* ws, cudaStream_t s)
 {
+    if (few_rows(a)) return attention_rows(a, q, k, v, out, lse, ws, s);
     FwdArgs r{};
     int rc = make_source(&r.q, a, q, a->q_tokens, a->q_heads);
     if (rc == DBLP_OK && a->k_tokens) rc = make_source(&r.k, a, k, a->k_tokens, a->kv_heads);
