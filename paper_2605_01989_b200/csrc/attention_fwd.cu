@@ -1,14 +1,15 @@
 // dblp_attention on the tensor cores.
 //
-// One block takes 128 queries of one head and walks over its keys in tiles of 128: s = q k^T into tensor memory, one thread
-// a row for the softmax, p back into tensor memory as the left operand of out += p v.  The running maximum and sum of a row
+// A work item is 128 queries of one head; a block walks over the item's keys in tiles of 128: s = q k^T into tensor memory, one
+// thread a row for the softmax, p back into tensor memory as the left operand of out += p v.  The running maximum and sum of a row
 // stay in its thread's registers, so nothing of size queries x keys exists.
 //   scores     x = scale * log2(e) * s, p = 2^(x - m), m any value near the row's maximum so far: out and the sum use the
 //              same m, so it cancels.  m moves only when the maximum has grown by more than 2^8, and only then is the
 //              accumulator rescaled; p stays below 2^8, exact enough in 16 bits and far from overflow.
 //   warps      0-3 softmax and epilogue, 4 TMA, 5 products.  Two blocks share an SM (96 KB of shared memory and 256 columns
-//              of tensor memory each), so that one's products run beside the other's exponentials and a block's start and
-//              end are hidden.
+//              of tensor memory each), so that one's products run beside the other's exponentials.  The blocks are persistent:
+//              q and the first k and v of the next item are loaded, and its first scores computed, while the last item's
+//              softmax and output are still under way.
 //   memory     k and v tiles pass through one ring, in the order in which the products use them.
 #include <math.h>
 
@@ -24,8 +25,28 @@ struct FwdArgs {
     float* lse;
     AttnShape s;
     float scale_log2;
+    uint32_t q_tiles, items, heads_together;
     unsigned long long* timeouts;
 };
+
+// Items in the order in which they are handed out: heads in groups whose k and v stay in L2
+// together, within a group by query tile; under a causal mask the last tiles, which see the most keys,
+// first.  Block x takes them to and fro, x, 2 grid - 1 - x, 2 grid + x, ...: like amounts of work for all.
+struct Item {
+    uint32_t qt, h, b;
+};
+__device__ __forceinline__ uint32_t item_number(uint32_t round) { return round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+__device__ __forceinline__ Item item_of(const FwdArgs& a, uint32_t x)
+{
+    const uint32_t heads = a.s.Hq * a.s.B, per = a.heads_together * a.q_tiles, g = x / per, first = g * a.heads_together;
+    const uint32_t n = min(a.heads_together, heads - first), y = x - g * per, t = y / n, hb = first + y - t * n;
+    return {a.s.causal ? a.q_tiles - 1 - t : t, hb % a.s.Hq, hb / a.s.Hq};
+}
+// Key tiles that a query tile's last query sees.
+__device__ __forceinline__ uint32_t key_tiles(const FwdArgs& a, uint32_t q0, uint32_t lq, uint32_t lk)
+{
+    return q0 < lq ? (keys_of(min(lq, q0 + 128) - 1, lq, lk, a.s.causal) + 127) / 128 : 0;
+}
 
 template <int DP> struct FwdSmem {
     static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes, STAGES = DP == 64 ? 5 : 2;
@@ -76,31 +97,19 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     using L = FwdSmem<DP>;
     constexpr int NS = L::NS, STAGES = L::STAGES;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t q_full, cut_full, full[STAGES], empty[STAGES], s_full, p_ready, idle;
+    __shared__ uint64_t q_full, q_empty, cut_full, full[STAGES], empty[STAGES], s_full, p_ready, o_full, o_free, idle;
     __shared__ uint32_t tmem_slot, dead;
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* sq = smem;
     uint8_t* ring = smem + L::TILE;
-
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    // a causal head's last queries see the most keys: start with them
-    const uint32_t qt = a.s.causal ? gridDim.x - 1 - blockIdx.x : blockIdx.x, h = blockIdx.y, b = blockIdx.z, hk = h / a.s.rep;
-    const uint32_t q0 = qt * 128, lq = length_of(a.s.q_lens, b, a.s.Sq), lk = length_of(a.s.k_lens, b, a.s.Sk);
-    const uint32_t most = q0 < lq ? keys_of(min(lq, q0 + 128) - 1, lq, lk, a.s.causal) : 0;      // of the tile's last query
-    const uint32_t nk = (most + 127) / 128;
-
-    if (nk == 0) {                                              // nothing to see: zeros
-        if (tid < 128 && q0 + tid < a.s.Sq) {
-            T* o = (T*)a.o.p + (int64_t)b * a.o.sb + (int64_t)(q0 + tid) * a.o.st + (int64_t)h * a.o.sh;
-            for (uint32_t c = 0; c < a.s.D; c += 8) *reinterpret_cast<uint4*>(o + c) = make_uint4(0, 0, 0, 0);
-            if (a.lse) a.lse[((uint64_t)b * a.s.Hq + h) * a.s.Sq + q0 + tid] = -INFINITY;
-        }
-        return;
-    }
 
     if (tid == 0) {
         dead = 0;
         bar_init(&q_full, 1);
+        bar_init(&q_empty, 1);
+        bar_init(&o_full, 1);
+        bar_init(&o_free, 4);
         bar_init(&cut_full, 1);
         bar_init(&idle, 1);
         for (int i = 0; i < STAGES; ++i) { bar_init(&full[i], 1); bar_init(&empty[i], 1); }
@@ -115,107 +124,129 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     const uint32_t tmem = tmem_slot, t_s = tmem, t_o = tmem + 128;
     const Guard g{&dead, a.timeouts};
 
-    if (warp == 4) {                                            // ---- TMA: k(0), v(0), k(1), ...
-        if (lane == 0) {
-            bar_expect(&q_full, L::TILE);
-            load_tile<NS>(sq, a.q, &q_full, q0, h, b);
-        }
-        const uint32_t tail = lk & 127;                         // rows of the last tile that count, if not all
-        uint32_t issued = 0;
+    if (warp == 4) {                                            // ---- TMA: q, k(0), v(0), k(1), ...
+        uint32_t n = 0, w = 0, cuts = 0;                        // tiles through the ring, items with work, tiles that were cleared
         bool ok = true;
-        for (uint32_t n = 0; n < 2 * nk && ok; ++n) {
-            const uint32_t st = n % STAGES, use = n / STAGES, j = n >> 1;
-            if (use) ok = warp_wait(&empty[st], (use - 1) & 1, g);
+        for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
+            const Item it = item_of(a, x);
+            const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk), hk = it.h / a.s.rep;
+            const uint32_t nk = key_tiles(a, it.qt * 128, lq, lk);
+            if (nk == 0) continue;
+            if (w) ok = warp_wait(&q_empty, (w - 1) & 1, g);
             if (!ok) break;
-            const bool is_v = n & 1, cut = is_v && j * 128 + 128 > lk && lk < a.s.Sk;
-            uint8_t* dst = ring + st * L::TILE;
-            if (!cut) {
-                if (lane == 0) {
-                    bar_expect(&full[st], L::TILE);
-                    load_tile<NS>(dst, is_v ? a.v : a.k, &full[st], j * 128, hk, b);
-                }
-                issued = n + 1;
-            } else {                                            // a v tile whose last rows do not count: clear them first
-                if (lane == 0) {
-                    bar_expect(&cut_full, L::TILE);
-                    load_tile<NS>(dst, a.v, &cut_full, j * 128, hk, b);
-                }
-                bar_drain(&cut_full, 0);                        // one such tile a block, the last
-                __syncwarp();
-                clear_rows<NS>(dst, tail);
-                __syncwarp();
-                if (lane == 0) bar_arrive(&full[st]);
-                issued = n + 1;
+            if (lane == 0) {
+                bar_expect(&q_full, L::TILE);
+                load_tile<NS>(sq, a.q, &q_full, it.qt * 128, it.h, it.b);
             }
-            __syncwarp();
+            ++w;
+            for (uint32_t t = 0; t < 2 * nk; ++t, ++n) {
+                const uint32_t st = n % STAGES, use = n / STAGES, j = t >> 1;
+                if (use) ok = warp_wait(&empty[st], (use - 1) & 1, g);
+                if (!ok) break;
+                const bool is_v = t & 1, cut = is_v && j * 128 + 128 > lk && lk < a.s.Sk;
+                uint8_t* dst = ring + st * L::TILE;
+                if (!cut) {
+                    if (lane == 0) {
+                        bar_expect(&full[st], L::TILE);
+                        load_tile<NS>(dst, is_v ? a.v : a.k, &full[st], j * 128, hk, it.b);
+                    }
+                } else {                                        // a v tile whose last rows do not count: clear them first
+                    if (lane == 0) {
+                        bar_expect(&cut_full, L::TILE);
+                        load_tile<NS>(dst, a.v, &cut_full, j * 128, hk, it.b);
+                    }
+                    bar_drain(&cut_full, cuts++ & 1);
+                    __syncwarp();
+                    clear_rows<NS>(dst, lk & 127);
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&full[st]);
+                }
+                __syncwarp();
+            }
         }
         if (lane == 0) {                                        // every copy lands before the block may end
-            bar_drain(&q_full, 0);
-            for (uint32_t n = issued > (uint32_t)STAGES ? issued - STAGES : 0; n < issued; ++n) bar_drain(&full[n % STAGES], (n / STAGES) & 1);
+            if (w) bar_drain(&q_full, (w - 1) & 1);
+            for (uint32_t x = n > (uint32_t)STAGES ? n - STAGES : 0; x < n; ++x) bar_drain(&full[x % STAGES], (x / STAGES) & 1);
         }
     } else if (warp == 5) {                                     // ---- products
-        {
-            const uint32_t leader = elect_leader();
-            constexpr uint32_t id_s = mma_desc<T>(128, 128, false, false), id_o = mma_desc<T>(128, DP, false, true);
-            const uint32_t qa = smem_addr(sq), ra = smem_addr(ring);
-            bool ok = warp_wait(&q_full, 0, g);
-            auto scores = [&](uint32_t j) {
-                const uint32_t n = 2 * j, st = n % STAGES;
-                ok = ok && warp_wait(&full[st], (n / STAGES) & 1, g);
-                if (!ok) return;
-                tc_fence_after();
+        const uint32_t leader = elect_leader();
+        constexpr uint32_t id_s = mma_desc<T>(128, 128, false, false), id_o = mma_desc<T>(128, DP, false, true);
+        const uint32_t qa = smem_addr(sq), ra = smem_addr(ring);
+        uint32_t n = 0, w = 0, tile = 0;
+        bool ok = true;
+        auto scores = [&](uint32_t at) {
+            const uint32_t st = at % STAGES;
+            ok = ok && warp_wait(&full[st], (at / STAGES) & 1, g);
+            if (!ok) return;
+            tc_fence_after();
 #pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk) {
-                    const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(leader, t_s, desc_k(qa + off), desc_k(ra + st * L::TILE + off), id_s, kk > 0);
-                }
-                mma_commit(leader, &empty[st]);
-                mma_commit(leader, &s_full);
-            };
-            scores(0);
-            for (uint32_t j = 0; j < nk && ok; ++j) {
-                const uint32_t n = 2 * j + 1, st = n % STAGES;
-                ok = warp_wait(&p_ready, j & 1, g) && warp_wait(&full[st], (n / STAGES) & 1, g);
+            for (int kk = 0; kk < DP / 16; ++kk) {
+                const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
+                mma_ss(leader, t_s, desc_k(qa + off), desc_k(ra + st * L::TILE + off), id_s, kk > 0);
+            }
+            mma_commit(leader, &empty[st]);
+            mma_commit(leader, &s_full);
+        };
+        for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
+            const Item it = item_of(a, x);
+            const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
+            const uint32_t nk = key_tiles(a, it.qt * 128, lq, lk);
+            if (nk == 0) continue;
+            ok = warp_wait(&q_full, w & 1, g);
+            scores(n);
+            if (ok && nk == 1) mma_commit(leader, &q_empty);
+            for (uint32_t j = 0; j < nk && ok; ++j, n += 2, ++tile) {
+                const uint32_t st = (n + 1) % STAGES;
+                ok = warp_wait(&p_ready, tile & 1, g) && warp_wait(&full[st], ((n + 1) / STAGES) & 1, g);
+                if (ok && j == 0 && w) ok = warp_wait(&o_free, (w - 1) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
                     mma_ts(leader, t_o, t_s + 64 + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
                 mma_commit(leader, &empty[st]);
-                if (j + 1 < nk) scores(j + 1);                  // overwrites p(j), which the product before has read by then
-                else mma_commit(leader, &s_full);
+                if (j + 1 < nk) scores(n + 2);                  // overwrites p(j), which the product before has read by then
+                else mma_commit(leader, &o_full);
+                if (ok && j + 2 == nk) mma_commit(leader, &q_empty);
             }
-            if (!ok) {                                          // products in flight end before the memory is freed
-                mma_commit(leader, &idle);
-                bar_drain(&idle, 0);
-            }
+            ++w;
+        }
+        if (!ok) {                                              // products in flight end before the memory is freed
+            mma_commit(leader, &idle);
+            bar_drain(&idle, 0);
         }
         __syncwarp();
     } else {                                                    // ---- softmax: one thread a row
-        const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal), lane_base = warp << 21;      // lane 32 * warp
+        const uint32_t lane_base = warp << 21;                  // lane 32 * warp
         const float c = a.scale_log2, grow = 8.0f / c;
-        float m = -INFINITY, l = 0.0f;
+        uint32_t w = 0, tile = 0;
         bool ok = true;
-        for (uint32_t j = 0; j < nk; ++j) {
-            ok = warp_wait(&s_full, j & 1, g);
+        for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
+        const Item it = item_of(a, x);
+        const uint32_t q0 = it.qt * 128, lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
+        const uint32_t nk = key_tiles(a, q0, lq, lk);
+        const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal);
+        float m = -INFINITY, l = 0.0f;
+        for (uint32_t j = 0; j < nk; ++j, ++tile) {
+            ok = warp_wait(&s_full, tile & 1, g);
             if (!ok) break;
             tc_fence_after();
-            // All 128 scores for the maximum; the first 64 are then dropped and read again chunk by chunk, which keeps the
-            // thread below 168 registers.  p(j) goes to columns 64 .. 127 of s(j): those are in registers by then.
+            // The maximum takes the scores in two halves; the first is read again chunk by chunk afterwards (a read of tensor
+            // memory takes about 30 cycles, a spilled register far more).  p(j) goes to columns 64 .. 127 of s(j): those are
+            // in registers by then.
             const uint32_t left = seen > j * 128 ? seen - j * 128 : 0;
             const bool cut = __any_sync(0xFFFFFFFFu, left < 128);
-            uint32_t lo[64], hi[64];
-            tmem_ld32(t_s + lane_base, lo);
-            tmem_ld32(t_s + lane_base + 32, lo + 32);
+            uint32_t hi[64];
+            tmem_ld32(t_s + lane_base, hi);
+            tmem_ld32(t_s + lane_base + 32, hi + 32);
+            tmem_wait_ld<64>(hi);
+            if (cut) hide_from<64>(hi, left);
+            float top = largest<64>(hi);
             tmem_ld32(t_s + lane_base + 64, hi);
             tmem_ld32(t_s + lane_base + 96, hi + 32);
-            tmem_wait_ld<64>(lo);
-            tmem_loaded<64>(hi);
-            if (cut) {
-                hide_from<64>(lo, left);
-                hide_from<64>(hi, left > 64 ? left - 64 : 0);
-            }
-            const float top = fmaxf(largest<64>(lo), largest<64>(hi));
+            tmem_wait_ld<64>(hi);
+            if (cut) hide_from<64>(hi, left > 64 ? left - 64 : 0);
+            top = fmaxf(top, largest<64>(hi));
             const bool move = top > m + grow;                   // also from -infinity
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float alpha = move ? exp2_fast((m - top) * c) : 1.0f;                         // m = -infinity: 0
@@ -253,29 +284,38 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             tc_fence_before();
             warp_arrive(&p_ready);
         }
-        if (ok) ok = warp_wait(&s_full, nk & 1, g);
-        if (ok) {
+        if (!ok) break;
+        if (nk) {
+            ok = warp_wait(&o_full, w & 1, g);
+            if (!ok) break;
             tc_fence_after();
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            T* o = (T*)a.o.p + (int64_t)b * a.o.sb + (int64_t)row * a.o.st + (int64_t)h * a.o.sh;
+            ++w;
+        }
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        T* o = (T*)a.o.p + (int64_t)it.b * a.o.sb + (int64_t)row * a.o.st + (int64_t)it.h * a.o.sh;
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                uint32_t x[32];
+        for (int i = 0; i < DP / 32; ++i) {
+            uint32_t x[32];
+            if (nk) {
                 tmem_ld32(t_o + lane_base + i * 32, x);
                 tmem_wait_ld<32>(x);
-#pragma unroll
-                for (int t = 0; t < 32; t += 8) {
-                    Vec8<T> w;
-                    float y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = seen ? __uint_as_float(x[t + e]) * inv : 0.0f;
-                    w.set(y);
-                    if (row < a.s.Sq && (uint32_t)(i * 32 + t) < a.s.D) w.store(o + i * 32 + t);
+                if (i + 1 == DP / 32) {
+                    tc_fence_before();
+                    warp_arrive(&o_free);
                 }
             }
-            if (a.lse && row < a.s.Sq)
-                a.lse[((uint64_t)b * a.s.Hq + h) * a.s.Sq + row] = seen ? (m * c + log2f(l)) * 0.693147180559945309f : -INFINITY;
-            tc_fence_before();
+#pragma unroll
+            for (int t = 0; t < 32; t += 8) {
+                Vec8<T> v;
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = seen ? __uint_as_float(x[t + e]) * inv : 0.0f;
+                v.set(y);
+                if (row < a.s.Sq && (uint32_t)(i * 32 + t) < a.s.D) v.store(o + i * 32 + t);
+            }
+        }
+        if (a.lse && row < a.s.Sq)
+            a.lse[((uint64_t)it.b * a.s.Hq + it.h) * a.s.Sq + row] = seen ? (m * c + log2f(l)) * 0.693147180559945309f : -INFINITY;
         }
     }
     __syncthreads();
@@ -289,7 +329,7 @@ template <typename T, int DP> static int launch_forward(const FwdArgs& r, cudaSt
 {
     const cudaError_t e = allow_shared<k_attention<T, DP>>(FwdSmem<DP>::kBytes);
     DBLP_CUDA(e);
-    const dim3 grid((r.s.Sq + 127) / 128, r.s.Hq, r.s.B);
+    const unsigned grid = r.items < 2 * 148 ? r.items : 2 * 148;       // two blocks an SM
     k_attention<T, DP><<<grid, kFwdThreads, FwdSmem<DP>::kBytes, s>>>(r);
     DBLP_LAUNCHED();
     return DBLP_OK;
@@ -310,6 +350,13 @@ int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const db
     r.lse = lse;
     r.s = shape_of(a);
     r.scale_log2 = (float)(a->scale * 1.4426950408889634);
+    r.q_tiles = (a->q_tokens + 127) / 128;
+    const uint64_t items = (uint64_t)r.q_tiles * a->q_heads * a->batch, kv_bytes = (uint64_t)a->k_tokens * a->head_dim * 4 + 1;
+    DBLP_REQUIRE(items < (1ull << 31), DBLP_ECAPACITY, "attention: 2^31 query tiles or more");
+    r.items = (uint32_t)items;
+    // heads that walk together: their k and v take at most 32 MB of the L2 (query heads that share one count it each)
+    const uint64_t heads = (uint64_t)a->q_heads * a->batch, fit = (32ull << 20) / kv_bytes;
+    r.heads_together = (uint32_t)(fit < 1 ? 1 : fit < heads ? fit : heads);
     r.timeouts = timeout_counter();
     DBLP_REQUIRE(r.timeouts, DBLP_ECUDA, "attention: device setup failed: %s", cudaGetErrorString(cudaGetLastError()));
     if (a->dtype == DBLP_BF16)
