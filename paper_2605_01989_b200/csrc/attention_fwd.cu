@@ -1,7 +1,8 @@
 // dblp_attention on the tensor cores.
 //
-// A work item is 128 queries of one head; a block walks over the item's keys in tiles of 128: s = q k^T into tensor memory, one
-// thread a row for the softmax, p back into tensor memory as the left operand of out += p v.  The running maximum and sum of a row
+// A work item is 128 queries of one head; a block walks over the item's keys in half tiles of 64: s = q k^T into one of two
+// buffers in tensor memory, one thread a row for the softmax, p back over s as the left operand of out += p v.  The products
+// of one buffer run while the softmax works on the other.  The running maximum and sum of a row
 // stay in its thread's registers, so nothing of size queries x keys exists.
 //   scores     x = scale * log2(e) * s, p = 2^(x - m), m any value near the row's maximum so far: out and the sum use the
 //              same m, so it cancels.  m moves only when the maximum has grown by more than 2^8, and only then is the
@@ -42,10 +43,10 @@ __device__ __forceinline__ Item item_of(const FwdArgs& a, uint32_t x)
     const uint32_t n = min(a.heads_together, heads - first), y = x - g * per, t = y / n, hb = first + y - t * n;
     return {a.s.causal ? a.q_tiles - 1 - t : t, hb % a.s.Hq, hb / a.s.Hq};
 }
-// Key tiles that a query tile's last query sees.
-__device__ __forceinline__ uint32_t key_tiles(const FwdArgs& a, uint32_t q0, uint32_t lq, uint32_t lk)
+// Half tiles of 64 keys that a query tile's last query sees.
+__device__ __forceinline__ uint32_t key_halves(const FwdArgs& a, uint32_t q0, uint32_t lq, uint32_t lk)
 {
-    return q0 < lq ? (keys_of(min(lq, q0 + 128) - 1, lq, lk, a.s.causal) + 127) / 128 : 0;
+    return q0 < lq ? (keys_of(min(lq, q0 + 128) - 1, lq, lk, a.s.causal) + 63) / 64 : 0;
 }
 
 template <int DP> struct FwdSmem {
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     using L = FwdSmem<DP>;
     constexpr int NS = L::NS, STAGES = L::STAGES;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t q_full, q_empty, cut_full, full[STAGES], empty[STAGES], s_full, p_ready, o_full, o_free, idle;
+    __shared__ uint64_t q_full, q_empty, cut_full, full[STAGES], empty[STAGES], s_full[2], p_ready[2], pv_done, o_full, o_free, idle;
     __shared__ uint32_t tmem_slot, dead;
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* sq = smem;
@@ -113,8 +114,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         bar_init(&cut_full, 1);
         bar_init(&idle, 1);
         for (int i = 0; i < STAGES; ++i) { bar_init(&full[i], 1); bar_init(&empty[i], 1); }
-        bar_init(&s_full, 1);
-        bar_init(&p_ready, 4);
+        for (int i = 0; i < 2; ++i) { bar_init(&s_full[i], 1); bar_init(&p_ready[i], 4); }
+        bar_init(&pv_done, 1);
         fence_bar_init();
     }
     if (warp == 5) tmem_alloc<256>(&tmem_slot);
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
             const Item it = item_of(a, x);
             const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk), hk = it.h / a.s.rep;
-            const uint32_t nk = key_tiles(a, it.qt * 128, lq, lk);
+            const uint32_t nk = (key_halves(a, it.qt * 128, lq, lk) + 1) / 2;
             if (nk == 0) continue;
             if (w) ok = warp_wait(&q_empty, (w - 1) & 1, g);
             if (!ok) break;
@@ -170,45 +171,51 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         }
     } else if (warp == 5) {                                     // ---- products
         const uint32_t leader = elect_leader();
-        constexpr uint32_t id_s = mma_desc<T>(128, 128, false, false), id_o = mma_desc<T>(128, DP, false, true);
+        constexpr uint32_t id_s = mma_desc<T>(128, 64, false, false), id_o = mma_desc<T>(128, DP, false, true);
         const uint32_t qa = smem_addr(sq), ra = smem_addr(ring);
-        uint32_t n = 0, w = 0, tile = 0;
+        uint32_t n = 0, w = 0, count = 0;                       // ring tiles and items before this one, halves in all
         bool ok = true;
-        auto scores = [&](uint32_t at) {
-            const uint32_t st = at % STAGES;
+        // scores of half tile h of an item of nh: 64 of the k tile's 128 rows, into buffer (count + h) % 2
+        auto scores = [&](uint32_t h, uint32_t nh) {
+            const uint32_t at = n + (h & ~1u), st = at % STAGES, to = (count + h) & 1;
             ok = ok && warp_wait(&full[st], (at / STAGES) & 1, g);
             if (!ok) return;
             tc_fence_after();
+            const uint32_t ka = ra + st * L::TILE + (h & 1) * (kBlockBytes / 2);
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
                 const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                mma_ss(leader, t_s, desc_k(qa + off), desc_k(ra + st * L::TILE + off), id_s, kk > 0);
+                mma_ss(leader, t_s + to * 64, desc_k(qa + off), desc_k(ka + off), id_s, kk > 0);
             }
-            mma_commit(leader, &empty[st]);
-            mma_commit(leader, &s_full);
+            if ((h & 1) || h + 1 == nh) mma_commit(leader, &empty[st]);
+            mma_commit(leader, &s_full[to]);
+            if (h + 1 == nh) mma_commit(leader, &q_empty);
         };
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
             const Item it = item_of(a, x);
             const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
-            const uint32_t nk = key_tiles(a, it.qt * 128, lq, lk);
-            if (nk == 0) continue;
+            const uint32_t nh = key_halves(a, it.qt * 128, lq, lk);
+            if (nh == 0) continue;
             ok = warp_wait(&q_full, w & 1, g);
-            scores(n);
-            if (ok && nk == 1) mma_commit(leader, &q_empty);
-            for (uint32_t j = 0; j < nk && ok; ++j, n += 2, ++tile) {
-                const uint32_t st = (n + 1) % STAGES;
-                ok = warp_wait(&p_ready, tile & 1, g) && warp_wait(&full[st], ((n + 1) / STAGES) & 1, g);
-                if (ok && j == 0 && w) ok = warp_wait(&o_free, (w - 1) & 1, g);
+            scores(0, nh);
+            if (nh > 1) scores(1, nh);
+            for (uint32_t h = 0; h < nh && ok; ++h) {
+                const uint32_t at = n + (h | 1), st = at % STAGES, from = (count + h) & 1;
+                ok = warp_wait(&p_ready[from], ((count + h) >> 1) & 1, g) && warp_wait(&full[st], (at / STAGES) & 1, g);
+                if (ok && h == 0 && w) ok = warp_wait(&o_free, (w - 1) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t va = ra + st * L::TILE + (h & 1) * (kBlockBytes / 2);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(leader, t_o, t_s + 64 + kk * 8, desc_mn(ra + st * L::TILE + kk * 2048, kBlockBytes), id_o, j > 0 || kk > 0);
-                mma_commit(leader, &empty[st]);
-                if (j + 1 < nk) scores(n + 2);                  // overwrites p(j), which the product before has read by then
-                else mma_commit(leader, &o_full);
-                if (ok && j + 2 == nk) mma_commit(leader, &q_empty);
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_ts(leader, t_o, t_s + from * 64 + kk * 8, desc_mn(va + kk * 2048, kBlockBytes), id_o, h > 0 || kk > 0);
+                if ((h & 1) || h + 1 == nh) mma_commit(leader, &empty[st]);
+                mma_commit(leader, &pv_done);
+                if (h + 1 == nh) mma_commit(leader, &o_full);
+                if (h + 2 < nh) scores(h + 2, nh);              // over p(h), which the product before has read by then
             }
+            n += (nh + 1) / 2 * 2;
+            count += nh;
             ++w;
         }
         if (!ok) {                                              // products in flight end before the memory is freed
@@ -219,40 +226,35 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     } else {                                                    // ---- softmax: one thread a row
         const uint32_t lane_base = warp << 21;                  // lane 32 * warp
         const float c = a.scale_log2, grow = 8.0f / c;
-        uint32_t w = 0, tile = 0;
+        uint32_t w = 0, count = 0;
         bool ok = true;
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
         const Item it = item_of(a, x);
         const uint32_t q0 = it.qt * 128, lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
-        const uint32_t nk = key_tiles(a, q0, lq, lk);
+        const uint32_t nh = key_halves(a, q0, lq, lk);
         const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal);
         float m = -INFINITY, l = 0.0f;
-        for (uint32_t j = 0; j < nk; ++j, ++tile) {
-            ok = warp_wait(&s_full, tile & 1, g);
+        for (uint32_t h = 0; h < nh; ++h, ++count) {
+            const uint32_t buf = count & 1, my_s = t_s + lane_base + buf * 64;
+            ok = warp_wait(&s_full[buf], (count >> 1) & 1, g);
             if (!ok) break;
             tc_fence_after();
-            // The maximum takes the scores in two halves; the first is read again chunk by chunk afterwards (a read of tensor
-            // memory takes about 30 cycles, a spilled register far more).  p(j) goes to columns 64 .. 127 of s(j): those are
-            // in registers by then.
-            const uint32_t left = seen > j * 128 ? seen - j * 128 : 0;
-            const bool cut = __any_sync(0xFFFFFFFFu, left < 128);
-            uint32_t hi[64];
-            tmem_ld32(t_s + lane_base, hi);
-            tmem_ld32(t_s + lane_base + 32, hi + 32);
-            tmem_wait_ld<64>(hi);
-            if (cut) hide_from<64>(hi, left);
-            float top = largest<64>(hi);
-            tmem_ld32(t_s + lane_base + 64, hi);
-            tmem_ld32(t_s + lane_base + 96, hi + 32);
-            tmem_wait_ld<64>(hi);
-            if (cut) hide_from<64>(hi, left > 64 ? left - 64 : 0);
-            top = fmaxf(top, largest<64>(hi));
+            uint32_t s[64];
+            tmem_ld32(my_s, s);
+            tmem_ld32(my_s + 32, s + 32);
+            tmem_wait_ld<64>(s);
+            const uint32_t left = seen > h * 64 ? seen - h * 64 : 0;
+            if (__any_sync(0xFFFFFFFFu, left < 64)) hide_from<64>(s, left);
+            const float top = largest<64>(s);
             const bool move = top > m + grow;                   // also from -infinity
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float alpha = move ? exp2_fast((m - top) * c) : 1.0f;                         // m = -infinity: 0
                 if (move) m = top;
                 l *= alpha;
-                if (j > 0) {
+                if (h > 0) {                                    // the product of the half before still adds to the accumulator
+                    ok = warp_wait(&pv_done, (count - 1) & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll 1
                     for (int i = 0; i < DP / 16; ++i) {
                         uint32_t o[16];
@@ -267,25 +269,15 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             const float mc = m == -INFINITY ? 0.0f : -m * c;
             const float2 c2 = make_float2(c, c), mc2 = make_float2(mc, mc);
             float2 sum = make_float2(0.0f, 0.0f);
-            uint32_t again[32];
-            tmem_ld32(t_s + lane_base, again);
-            probabilities<T>(hi, c2, mc2, sum, t_s + lane_base + 96);
-            probabilities<T>(hi + 32, c2, mc2, sum, t_s + lane_base + 112);
-            tmem_wait_ld<32>(again);
-            uint32_t again2[32];
-            tmem_ld32(t_s + lane_base + 32, again2);
-            if (cut) hide_from<32>(again, left);
-            probabilities<T>(again, c2, mc2, sum, t_s + lane_base + 64);
-            tmem_wait_ld<32>(again2);
-            if (cut) hide_from<32>(again2, left > 32 ? left - 32 : 0);
-            probabilities<T>(again2, c2, mc2, sum, t_s + lane_base + 80);
+            probabilities<T>(s, c2, mc2, sum, my_s);            // p(h) over s(h), which is in registers by now
+            probabilities<T>(s + 32, c2, mc2, sum, my_s + 16);
             l += sum.x + sum.y;
             tmem_wait_st();
             tc_fence_before();
-            warp_arrive(&p_ready);
+            warp_arrive(&p_ready[buf]);
         }
         if (!ok) break;
-        if (nk) {
+        if (nh) {
             ok = warp_wait(&o_full, w & 1, g);
             if (!ok) break;
             tc_fence_after();
@@ -295,10 +287,10 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         T* o = (T*)a.o.p + (int64_t)it.b * a.o.sb + (int64_t)row * a.o.st + (int64_t)it.h * a.o.sh;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i) {
-            uint32_t x[32];
-            if (nk) {
-                tmem_ld32(t_o + lane_base + i * 32, x);
-                tmem_wait_ld<32>(x);
+            uint32_t y32[32];
+            if (nh) {
+                tmem_ld32(t_o + lane_base + i * 32, y32);
+                tmem_wait_ld<32>(y32);
                 if (i + 1 == DP / 32) {
                     tc_fence_before();
                     warp_arrive(&o_free);
@@ -309,7 +301,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                 Vec8<T> v;
                 float y[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = seen ? __uint_as_float(x[t + e]) * inv : 0.0f;
+                for (int e = 0; e < 8; ++e) y[e] = seen ? __uint_as_float(y32[t + e]) * inv : 0.0f;
                 v.set(y);
                 if (row < a.s.Sq && (uint32_t)(i * 32 + t) < a.s.D) v.store(o + i * 32 + t);
             }
