@@ -76,16 +76,22 @@ template <int N> __device__ __forceinline__ float largest(const uint32_t* x)
 }
 
 // 32 scores -> 16 words of probabilities in tensor memory; their fp32 sum is added to `sum`.  Rounded to 16 bits because
-// that is the type of the product with v.
-template <typename T>
+// that is the type of the product with v.  With head_dim up to 64 the exponentials bound the kernel and a quarter of them is
+// computed off the special function unit (8192 x 8192, 16 heads: 438 us with none, 414 an eighth, 400 a quarter, 453 half);
+// with 128 the products do, and the extra instructions cost (271 -> 276 us causal on 4 key heads).
+template <typename T, int DP>
 __device__ __forceinline__ void probabilities(const uint32_t* x, float2 c2, float2 mc2, float2& sum, uint32_t dst)
 {
     uint32_t p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         float2 y = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, mc2);
-        y.x = exp2_fast(y.x);
-        y.y = exp2_fast(y.y);
+        if (DP == 64 && i % 4 == 3) {
+            y = exp2_pair(y);
+        } else {
+            y.x = exp2_fast(y.x);
+            y.y = exp2_fast(y.y);
+        }
         sum = add2(sum, y);
         p[i] = pack2<T>(y.x, y.y);
     }
@@ -269,8 +275,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             const float mc = m == -INFINITY ? 0.0f : -m * c;
             const float2 c2 = make_float2(c, c), mc2 = make_float2(mc, mc);
             float2 sum = make_float2(0.0f, 0.0f);
-            probabilities<T>(s, c2, mc2, sum, my_s);            // p(h) over s(h), which is in registers by now
-            probabilities<T>(s + 32, c2, mc2, sum, my_s + 16);
+            probabilities<T, DP>(s, c2, mc2, sum, my_s);            // p(h) over s(h), which is in registers by now
+            probabilities<T, DP>(s + 32, c2, mc2, sum, my_s + 16);
             l += sum.x + sum.y;
             tmem_wait_st();
             tc_fence_before();

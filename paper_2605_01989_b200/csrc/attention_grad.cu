@@ -15,21 +15,22 @@
 // Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
 // two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
-//   warps         0-15 p, ds and dq's way to memory (each thread one key and 32 queries), 16 TMA, 17 products.
+//   warps         0-7 p and ds of a pair's first 64 queries, 8-15 of the others (each thread one key and 32 queries), half a
+//                 step apart; both take dq out of tensor memory; 16 TMA, 17 products, 18 dq to memory.
 #include <math.h>
 
 #include "attention.cuh"
 
 namespace dblp {
 
-constexpr int kGradThreads = 576;
-constexpr uint32_t kPairWarps = 16, kTmaWarp = 16, kMmaWarp = 17;
+constexpr int kGradThreads = 608;
+constexpr uint32_t kPairWarps = 16, kTmaWarp = 16, kMmaWarp = 17, kOutWarp = 18;
 
 struct GradArgs {
     TileSource q, k, v, go;
     Heads dk, dv;
     const float* rows;         // [B][Hq][tiles][2][128]: -lse log2(e), then -D
-    float4* dq;                // [R][B][Hq][tiles][4][DP / 4][32]: query 32 a + l, columns 4 c .. 4 c + 3 at [a][c][l]
+    float* dq;                 // [R][B][Hq][tiles][DP / 64][4][16][32][4]: query 32 a + l, columns 64 d + 4 c .. at [d][a][c][l]
     AttnShape s;
     float scale, scale_log2;
     float* dkv;                // [G][2][B][Hkv][k_tiles * 128][DP]: dv, dk of one head group; null when G = 1
@@ -87,15 +88,16 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
 // ---- main ------------------------------------------------------------------------------------------------------------
 template <int DP> struct GradSmem {
     static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes;
-    static constexpr int NQ = DP == 64 ? 4 : 2, NG = DP == 64 ? 3 : 1;  // stages of q (with its row values) and of dout
-    static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, ROWS = DS + 2 * (int)kBlockBytes;
-    static constexpr int STAGE = ROWS + NQ * 1024;                      // dq on its way out: 2 KB a warp
-    static constexpr int BARS = STAGE + (int)kPairWarps * 2048, kBytes = BARS + 256;
+    // stages of q (with its row values), of dout, of ds; dq leaves through one piece of 128 queries x 64 columns in fp32
+    static constexpr int NQ = DP == 64 ? 3 : 2, NG = DP == 64 ? 2 : 1, ND = DP == 64 ? 2 : 1;
+    static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, STAGE = DS + ND * 2 * (int)kBlockBytes;
+    static constexpr int ROWS = STAGE + 32768, BARS = ROWS + NQ * 1024, kBytes = BARS + 256;
 };
+static_assert(GradSmem<64>::kBytes <= 232448 && GradSmem<128>::kBytes <= 232448, "");
 
 struct GradBars {
-    uint64_t kv_full, q_full[4], q_empty[4], g_full[3], g_empty[3], cut_full;
-    uint64_t s_full, p_ready, dp_full, ds_ready, ds_free, dq_full, dq_free, acc_full, acc_free, idle;
+    uint64_t kv_full, q_full[3], q_empty[3], g_full[2], g_empty[2], cut_full;
+    uint64_t s_full[2], p_ready[2], dp_full[2], ds_ready[2], ds_free[2], dq_full, dq_free, staged, stage_free, acc_full, acc_free, idle;
     uint32_t tmem_slot, dead;
 };
 static_assert(sizeof(GradBars) <= 256, "");
@@ -104,7 +106,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant__ GradArgs a)
 {
     using L = GradSmem<DP>;
-    constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG;
+    constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG, ND = L::ND, BATCHES = DP / 64;
     constexpr bool kOwnDq = DP == 64;                          // dq has columns of its own; else it takes those of dp
     extern __shared__ __align__(1024) uint8_t smem[];          // the whole of the block's shared memory, so at an even kilobyte
     GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
@@ -123,13 +125,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 
     if (tid == 0) {
         s.dead = 0;
-        for (uint64_t* p : {&s.kv_full, &s.cut_full, &s.s_full, &s.dp_full, &s.ds_free, &s.dq_full, &s.acc_full, &s.idle}) bar_init(p, 1);
+        for (uint64_t* p : {&s.kv_full, &s.cut_full, &s.dq_full, &s.stage_free, &s.acc_full, &s.idle}) bar_init(p, 1);
         for (int i = 0; i < NQ; ++i) { bar_init(&s.q_full[i], 1); bar_init(&s.q_empty[i], 1); }
         for (int i = 0; i < NG; ++i) { bar_init(&s.g_full[i], 1); bar_init(&s.g_empty[i], 1); }
-        bar_init(&s.p_ready, kPairWarps);
-        bar_init(&s.ds_ready, kPairWarps);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&s.s_full[i], 1);
+            bar_init(&s.dp_full[i], 1);
+            bar_init(&s.ds_free[i], 1);
+            bar_init(&s.p_ready[i], kPairWarps / 2);
+            bar_init(&s.ds_ready[i], kPairWarps / 2);
+        }
         bar_init(&s.acc_free, kPairWarps);
-        bar_init(&s.dq_free, kPairWarps);
+        bar_init(&s.dq_free, kOwnDq ? kPairWarps : kPairWarps / 2);
+        bar_init(&s.staged, kOwnDq ? kPairWarps : kPairWarps / 2);
         fence_bar_init();
     }
     if (warp == kMmaWarp) tmem_alloc<512>(&s.tmem_slot);
@@ -201,128 +209,185 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             for (uint32_t x = n > NQ ? n - NQ : 0; x < n; ++x) bar_drain(&s.q_full[x % NQ], (x / NQ) & 1);
             for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&s.g_full[x % NG], (x / NG) & 1);
         }
-    } else if (warp == kMmaWarp) {                                 // ---- products
-        {
-            const uint32_t leader = elect_leader();
-            constexpr uint32_t id_kk = mma_desc<T>(128, 128, false, false);     // s, dp
-            constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);       // dv, dk: right operand across its rows
-            constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);        // dq: both across their rows
-            const uint32_t base = smem_addr(smem);
-            uint32_t n = 0, w = 0;
-            bool ok = true;
-            auto scores = [&](uint32_t x) {
-                ok = ok && warp_wait(&s.q_full[x % NQ], (x / NQ) & 1, g);
+    } else if (warp == kMmaWarp) {                              // ---- products
+        // Each pair is done in two halves of 64 queries by two groups of warps that work half a step apart: one computes p
+        // while the other computes ds.  The order below follows them: p of the first half, ds of the second half of the pair
+        // before, ds of the first half, p of the second.
+        const uint32_t leader = elect_leader();
+        constexpr uint32_t id_kk = mma_desc<T>(128, 64, false, false);          // s, dp of a half
+        constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);           // dv, dk: right operand across its rows
+        constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);            // dq: both across their rows
+        const uint32_t base = smem_addr(smem);
+        uint32_t n = 0, w = 0;
+        bool ok = true;
+        // s (left k, right q) or dp (left v, right dout) of half e
+        auto half_scores = [&](uint32_t to, uint32_t left, uint32_t right, uint32_t e, uint64_t* done) {
+#pragma unroll
+            for (int kk = 0; kk < DP / 16; ++kk) {
+                const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
+                mma_ss(leader, to + e * 64, desc_k(left + off), desc_k(right + e * (kBlockBytes / 2) + off), id_kk, kk > 0);
+            }
+            mma_commit(leader, done);
+        };
+        auto q_at = [&](uint32_t x) { return base + L::Q + (x % NQ) * L::TILE; };
+        auto g_at = [&](uint32_t x) { return base + L::G + (x % NG) * L::TILE; };
+        auto ds_at = [&](uint32_t x) { return base + L::DS + (x % ND) * 2 * kBlockBytes; };
+        auto scores = [&](uint32_t x, uint32_t e) { half_scores(t_s, base + L::K, q_at(x), e, &s.s_full[e]); };
+        auto dprobs = [&](uint32_t x, uint32_t e) { half_scores(t_dp, base + L::V, g_at(x), e, &s.dp_full[e]); };
+        auto add_dv = [&](uint32_t x, uint32_t e, bool acc) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)                      // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
+                mma_ts(leader, t_dv, t_s + e * 64 + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(g_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
+                       acc || kk > 0);
+        };
+        auto add_dk = [&](uint32_t x, uint32_t e, bool acc) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+                mma_ss(leader, t_dk, desc_k(ds_at(x) + e * kBlockBytes + kk * 32), desc_mn(q_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
+                       acc || kk > 0);
+        };
+        // second half of pair x: its ds is there, so dk and dq can be completed; `more`: another pair of this key tile follows
+        auto finish = [&](uint32_t x, bool more) {
+            ok = ok && warp_wait(&s.ds_ready[1], x & 1, g);
+            if (ok && kOwnDq && x) ok = warp_wait(&s.dq_free, (x - 1) & 1, g);
+            if (!ok) return;
+            tc_fence_after();
+            if (kOwnDq && more) dprobs(x + 1, 1);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)
+                mma_ss(leader, t_dq, desc_mn(ds_at(x) + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
+            mma_commit(leader, &s.dq_full);
+            add_dk(x, 1, true);
+            mma_commit(leader, &s.q_empty[x % NQ]);
+            mma_commit(leader, &s.ds_free[x % ND]);
+            if (!kOwnDq && more) {                              // dp of the next pair comes where dq is
+                ok = warp_wait(&s.dq_free, x & 1, g);       // (its dout is there: dv of its first half came before)
                 if (!ok) return;
                 tc_fence_after();
-#pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk) {
-                    const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(leader, t_s, desc_k(base + L::K + off), desc_k(base + L::Q + (x % NQ) * L::TILE + off), id_kk, kk > 0);
-                }
-                mma_commit(leader, &s.s_full);
-            };
-            auto dprobs = [&](uint32_t x) {
-                ok = ok && warp_wait(&s.g_full[x % NG], (x / NG) & 1, g);
-                if (ok && !kOwnDq && x) ok = warp_wait(&s.dq_free, (x - 1) & 1, g);
-                if (!ok) return;
+                dprobs(x + 1, 0);
+                dprobs(x + 1, 1);
+            }
+        };
+        for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
+            const uint32_t pairs = meets(share_tile(share, m, a.shares)) * heads;
+            if (pairs == 0) continue;
+            ok = warp_wait(&s.kv_full, w & 1, g) && warp_wait(&s.q_full[n % NQ], (n / NQ) & 1, g);
+            if (!ok) break;
+            tc_fence_after();
+            scores(n, 0);
+            scores(n, 1);
+            ok = warp_wait(&s.g_full[n % NG], (n / NG) & 1, g);
+            if (ok && !kOwnDq && n) ok = warp_wait(&s.dq_free, (n - 1) & 1, g);
+            if (!ok) break;
+            tc_fence_after();
+            dprobs(n, 0);
+            dprobs(n, 1);
+            for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
+                const bool more = t + 1 < pairs;
+                ok = warp_wait(&s.p_ready[0], n & 1, g) && warp_wait(&s.g_full[n % NG], (n / NG) & 1, g);
+                if (ok && t == 0 && w) ok = warp_wait(&s.acc_free, (w - 1) & 1, g);
+                if (!ok) break;
                 tc_fence_after();
-#pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk) {
-                    const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                    mma_ss(leader, t_dp, desc_k(base + L::V + off), desc_k(base + L::G + (x % NG) * L::TILE + off), id_kk, kk > 0);
+                add_dv(n, 0, t > 0);
+                if (more && NQ > 2) {
+                    ok = warp_wait(&s.q_full[(n + 1) % NQ], ((n + 1) / NQ) & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(n + 1, 0);                           // over p, which the product before has read by then
                 }
-                mma_commit(leader, &s.dp_full);
-            };
-            for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
-                const uint32_t pairs = meets(share_tile(share, m, a.shares)) * heads;
-                if (pairs == 0) continue;
-                ok = warp_wait(&s.kv_full, w & 1, g);
-                scores(n);
-                dprobs(n);
-                for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
-                    const uint32_t qa = base + L::Q + (n % NQ) * L::TILE, ga = base + L::G + (n % NG) * L::TILE;
-                    ok = warp_wait(&s.p_ready, n & 1, g);
-                    if (ok && t == 0 && w) ok = warp_wait(&s.acc_free, (w - 1) & 1, g);
+                if (t > 0) finish(n - 1, true);                 // with two stages, q of the next pair comes into its place
+                ok = ok && warp_wait(&s.ds_ready[0], n & 1, g);
+                if (ok && kOwnDq && more) ok = warp_wait(&s.g_full[(n + 1) % NG], ((n + 1) / NG) & 1, g);
+                if (!ok) break;
+                tc_fence_after();
+                if (kOwnDq && more) dprobs(n + 1, 0);
+                add_dk(n, 0, t > 0);
+                ok = warp_wait(&s.p_ready[1], n & 1, g);
+                if (!ok) break;
+                tc_fence_after();
+                add_dv(n, 1, true);
+                mma_commit(leader, &s.g_empty[n % NG]);
+                if (more && NQ <= 2) {
+                    ok = warp_wait(&s.q_full[(n + 1) % NQ], ((n + 1) / NQ) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)              // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
-                        mma_ts(leader, t_dv, t_s + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(ga + kk * 2048, kBlockBytes), id_kv, t > 0 || kk > 0);
-                    mma_commit(leader, &s.g_empty[n % NG]);
-                    if (t + 1 < pairs) scores(n + 1);           // over p(n), which the product before has read by then
-                    ok = ok && warp_wait(&s.ds_ready, n & 1, g);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (kOwnDq && t + 1 < pairs) dprobs(n + 1); // dp(n) has been read: the next pair need not wait for dq, dk
-                    if (ok && kOwnDq && n) ok = warp_wait(&s.dq_free, (n - 1) & 1, g);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        mma_ss(leader, t_dq, desc_mn(base + L::DS + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
-                    mma_commit(leader, &s.dq_full);
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        mma_ss(leader, t_dk, desc_k(base + L::DS + (kk / 4) * kBlockBytes + (kk % 4) * 32), desc_mn(qa + kk * 2048, kBlockBytes), id_kv,
-                               t > 0 || kk > 0);
-                    mma_commit(leader, &s.q_empty[n % NQ]);
-                    mma_commit(leader, &s.ds_free);
-                    if (!kOwnDq && t + 1 < pairs) dprobs(n + 1);
+                    scores(n + 1, 0);
                 }
-                if (ok) mma_commit(leader, &s.acc_full);
-                ++w;
+                if (more) scores(n + 1, 1);
             }
-            if (!ok) {                                          // products in flight end before the memory is freed
-                mma_commit(leader, &s.idle);
-                bar_drain(&s.idle, 0);
-            }
+            finish(n - 1, false);
+            if (ok) mma_commit(leader, &s.acc_full);
+            ++w;
+        }
+        if (!ok) {                                              // products in flight end before the memory is freed
+            mma_commit(leader, &s.idle);
+            bar_drain(&s.idle, 0);
         }
         __syncwarp();
+    } else if (warp == kOutWarp) {                              // ---- dq: shared memory -> this share's buffer
+        uint32_t k = 0;
+        bool ok = true;
+        for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
+            const uint32_t per_head = meets(share_tile(share, m, a.shares)), pairs = per_head * heads;
+            for (uint32_t t = 0, i = nq - per_head, h = h0; t < pairs && ok; ++t) {
+                float* dst = a.dq + ((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * (128 * DP);
+                if (++i == nq) { i = nq - per_head; ++h; }
+                for (int c = 0; c < BATCHES; ++c, ++k) {
+                    ok = warp_wait(&s.staged, k & 1, g);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        // the additions of the last visit to this query tile are done before those of this one begin: all but
+                        // the pair before's are complete, and with one pair a key tile that one's too
+                        if (c == 0) {
+                            if (pairs > 1) bulk_wait<BATCHES>();
+                            else bulk_wait<0>();
+                        }
+                        // the share's first key tile is the first to meet every query tile it meets at all
+                        if (m == 0) bulk_store(dst + c * 8192, smem + L::STAGE, 32768);
+                        else bulk_add_f32(dst + c * 8192, smem + L::STAGE, 32768);
+                        bulk_commit();
+                        bulk_wait_read<0>();
+                        bar_arrive(&s.stage_free);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) bulk_wait<0>();
     } else {                                                    // ---- p and ds: thread = key (lane of the tile), 32 queries
-        const uint32_t grp = warp >> 2, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
+        const uint32_t grp = warp >> 2, e2 = warp >> 3, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
         const uint32_t my_s = t_s + lane_base + grp * 32, my_dp = t_dp + lane_base + grp * 32;
-        uint8_t* ds_row = smem + L::DS + (grp >> 1) * kBlockBytes + row * 128;
+        uint8_t* ds_row = smem + L::DS + e2 * kBlockBytes + row * 128;
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
-        float4* stage = reinterpret_cast<float4*>(smem + L::STAGE + warp * 2048);
+        float4* stage = reinterpret_cast<float4*>(smem + L::STAGE) + (warp & 3) * 512 + lane;
         uint32_t n = 0, w = 0;
         bool ok = true;
 
-        // dq of pair x to this share's buffer: this warp takes 32 queries and DP / 4 columns, 16 columns at a time through
-        // shared memory; the memory system adds them.  `first`: nothing is there yet.  The additions of the last visit to a
-        // query tile are done before those of this one begin: all groups but the pair before's are complete, and with one
-        // pair a key tile (`lone`) those too.
-        constexpr int PIECES = DP / 64;
-        float4* dq_at = nullptr;
-        bool dq_first = false, dq_lone = false;
+        // dq of pair x: tensor memory -> shared memory, 64 columns at a time.  With columns of its own all warps take 16 each,
+        // the groups at different points of their step; else the first group alone, at once, since dp waits for the columns.
+        constexpr int PIECES = kOwnDq ? 1 : 2;
         auto drain = [&](uint32_t x) {
             ok = warp_wait(&s.dq_full, x & 1, g);
             if (!ok) return;
             tc_fence_after();
-            if (lane == 0) {
-                if (dq_lone) bulk_wait<0>();
-                else bulk_wait<PIECES>();
-            }
 #pragma unroll
-            for (int c = 0; c < PIECES; ++c) {
-                uint32_t v[16];
-                tmem_ld16(t_dq + lane_base + (grp * PIECES + c) * 16, v);
-                if (lane == 0) bulk_wait_read<0>();             // the piece that was here has left
-                __syncwarp();
-                tmem_wait_ld<16>(v);
-                if (c + 1 == PIECES) {
+            for (int c = 0; c < BATCHES; ++c) {
+                uint32_t v[16 * PIECES];
+                const uint32_t col = (kOwnDq ? grp : grp * 2) * 16;
+#pragma unroll
+                for (int u = 0; u < PIECES; ++u) tmem_ld16(t_dq + lane_base + c * 64 + col + u * 16, v + 16 * u);
+                tmem_wait_ld<16 * PIECES>(v);
+                if (c + 1 == BATCHES) {
                     tc_fence_before();
                     warp_arrive(&s.dq_free);
                 }
+                const uint32_t k = x * BATCHES + c;
+                if (k) ok = warp_wait(&s.stage_free, (k - 1) & 1, g);
+                if (!ok) return;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    stage[e * 32 + lane] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                for (int e = 0; e < 4 * PIECES; ++e) stage[(col / 4 + e) * 32] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
                 fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if (dq_first) bulk_store(dq_at + c * 128, stage, 2048);
-                    else bulk_add_f32(dq_at + c * 128, stage, 2048);
-                    bulk_commit();
-                }
+                warp_arrive(&s.staged);
             }
         };
 
@@ -330,16 +395,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * heads;
             if (j >= a.k_tiles) continue;
             const uint32_t key = j * 128 + row;
-            for (uint32_t t = 0, i = nq - per_head, h = h0; t < pairs; ++t, ++n) {
-                if (!kOwnDq && n) {                             // dp of this pair comes where dq of the last one is
-                    drain(n - 1);
-                    if (!ok) break;
-                }
+            for (uint32_t t = 0, i = nq - per_head; t < pairs; ++t, ++n, i = i + 1 < nq ? i + 1 : nq - per_head) {
                 // queries [from, 32) of this thread's columns see the key
                 int32_t from = key < lk ? 0 : 32;
                 if (a.s.causal) from = max(from, (int32_t)(key + lq) - (int32_t)lk - (int32_t)(i * 128 + grp * 32));
                 const bool cut = __any_sync(0xFFFFFFFFu, from > 0);
-                ok = warp_wait(&s.s_full, n & 1, g) && warp_wait(&s.q_full[n % NQ], (n / NQ) & 1, g);
+                ok = warp_wait(&s.s_full[e2], n & 1, g) && warp_wait(&s.q_full[n % NQ], (n / NQ) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t p[32];
@@ -353,10 +414,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     for (int e = part; e < part + 16; e += 4) {
                         const float4 l = l4[e / 4];
                         const float2 u = fma2(pair(p[e], p[e + 1]), c2, make_float2(l.x, l.y)), v = fma2(pair(p[e + 2], p[e + 3]), c2, make_float2(l.z, l.w));
-                        p[e] = __float_as_uint(exp2_fast(u.x));
-                        p[e + 1] = __float_as_uint(exp2_fast(u.y));
-                        p[e + 2] = __float_as_uint(exp2_fast(v.x));
-                        p[e + 3] = __float_as_uint(exp2_fast(v.y));
+                        float2 y = make_float2(exp2_fast(u.x), exp2_fast(u.y)), z;
+                        if (DP == 64 && e % 8 == 4) z = exp2_pair(v);           // a quarter off the special function unit
+                        else z = make_float2(exp2_fast(v.x), exp2_fast(v.y));
+                        p[e] = __float_as_uint(y.x);
+                        p[e + 1] = __float_as_uint(y.y);
+                        p[e + 2] = __float_as_uint(z.x);
+                        p[e + 3] = __float_as_uint(z.y);
                     }
                     if (cut) {
 #pragma unroll
@@ -369,18 +433,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                warp_arrive(&s.p_ready);
+                warp_arrive(&s.p_ready[e2]);
 
-                if (kOwnDq && n) {
+                if (n && (kOwnDq ? e2 == 1 : e2 == 0)) {
                     drain(n - 1);
                     if (!ok) break;
                 }
-                dq_at = a.dq + ((((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * 4 + (warp & 3)) * (DP / 4) + grp * (DP / 16)) * 32;
-                dq_first = m == 0;                              // the share's first key tile is the first to meet every query tile
-                dq_lone = pairs == 1;
-                if (++i == nq) { i = nq - per_head; ++h; }
-                ok = warp_wait(&s.dp_full, n & 1, g);
-                if (ok && n) ok = warp_wait(&s.ds_free, (n - 1) & 1, g);
+                ok = warp_wait(&s.dp_full[e2], n & 1, g);
+                if (ok && n >= ND) ok = warp_wait(&s.ds_free[n % ND], (n / ND - 1) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -404,12 +464,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                             w[f / 2] = pack2<T>(u.x, u.y);
                             w[f / 2 + 1] = pack2<T>(v.x, v.y);
                         }
-                        *reinterpret_cast<uint4*>(ds_row + ((((grp & 1) * 4 + (part + e) / 8) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(ds_row + (n % ND) * 2 * kBlockBytes + ((((grp & 1) * 4 + (part + e) / 8) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
                 fence_async_smem();
                 tc_fence_before();
-                warp_arrive(&s.ds_ready);
+                warp_arrive(&s.ds_ready[e2]);
+                if (kOwnDq && n && e2 == 0) {
+                    drain(n - 1);
+                    if (!ok) break;
+                }
             }
             if (!ok) break;
             // this key tile's gradients: two groups dv, two dk, half of the columns each
@@ -454,8 +518,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 ++w;
             }
         }
-        if (ok && n) drain(n - 1);
-        if (lane == 0) bulk_wait<0>();
+        if (ok && n && (kOwnDq || e2 == 0)) drain(n - 1);
     }
     __syncthreads();
     if (warp == kMmaWarp) {
@@ -475,12 +538,13 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
     if (token >= s.Sq) return;
     T* dst = (T*)dq.p + (int64_t)b * dq.sb + (int64_t)token * dq.st + (int64_t)h * dq.sh;
     const uint64_t stride = (uint64_t)s.B * s.Hq * q_tiles * (DP / 4) * 128;
-    const float4* src = part + ((((uint64_t)b * s.Hq + h) * q_tiles + i) * 4 + row / 32) * (DP / 4) * 32 + row % 32;
+    const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row / 32 * 512 + row % 32;
 #pragma unroll 4
     for (uint32_t c = (threadIdx.x >> 7) * 8; c < s.D; c += 16) {
+        const uint32_t at = c / 64 * 2048 + c % 64 / 4 * 32;
         float y[8] = {};
         for (uint32_t r = 0; r < parts; ++r) {
-            const float4 u = src[r * stride + c / 4 * 32], v = src[r * stride + (c / 4 + 1) * 32];
+            const float4 u = src[r * stride + at], v = src[r * stride + at + 32];
             y[0] += u.x; y[1] += u.y; y[2] += u.z; y[3] += u.w;
             y[4] += v.x; y[5] += v.y; y[6] += v.z; y[7] += v.w;
         }
@@ -578,7 +642,7 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
         DBLP_LAUNCHED();
     }
     if (sh.Sq) {
-        k_grad_dq<T, DP><<<dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s>>>(r.dq, dq, sh, r.scale, r.q_tiles, r.shares);
+        k_grad_dq<T, DP><<<dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s>>>((const float4*)r.dq, dq, sh, r.scale, r.q_tiles, r.shares);
         DBLP_LAUNCHED();
     }
     return DBLP_OK;
@@ -599,7 +663,7 @@ int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const d
     r.dk = heads(dk);
     r.dv = heads(dv);
     r.rows = (const float*)((uint8_t*)ws + sp.rows);
-    r.dq = (float4*)((uint8_t*)ws + sp.dq);
+    r.dq = (float*)((uint8_t*)ws + sp.dq);
     r.s = shape_of(a);
     r.scale = a->scale;
     r.scale_log2 = (float)(a->scale * 1.4426950408889634);
