@@ -35,13 +35,13 @@ __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
 }
-// The thread may sleep up to a millisecond before the answer is no: a polling warp would take issue slots from the others.
+// (A time hint for the sleep, 200 ns to 1 ms, and test_wait were tried: 2 to 9 % slower in all kernels.)
 __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok)
-                 : "r"(smem_addr(b)), "r"(parity), "r"(1000000u)
+                 : "r"(smem_addr(b)), "r"(parity)
                  : "memory");
     return ok != 0;
 }
