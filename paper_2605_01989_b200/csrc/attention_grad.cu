@@ -16,21 +16,21 @@
 // two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
 //   warps         0-7 p and ds of a pair's first 64 queries, 8-15 of the others (each thread one key and 32 queries), half a
-//                 step apart; both take dq out of tensor memory; 16 TMA, 17 products, 18 dq to memory.
+//                 step apart; 16-19 dq to memory, 20 TMA, 21 products.
 #include <math.h>
 
 #include "attention.cuh"
 
 namespace dblp {
 
-constexpr int kGradThreads = 608;
-constexpr uint32_t kPairWarps = 16, kTmaWarp = 16, kMmaWarp = 17, kOutWarp = 18;
+constexpr int kGradThreads = 704;
+constexpr uint32_t kPairWarps = 16, kDqWarp = 16, kTmaWarp = 20, kMmaWarp = 21;
 
 struct GradArgs {
     TileSource q, k, v, go;
     Heads dk, dv;
     const float* rows;         // [B][Hq][tiles][2][128]: -lse log2(e), then -D
-    float* dq;                 // [R][B][Hq][tiles][DP / 32][4][8][32][4]: query 32 a + l, columns 32 d + 4 c .. at [d][a][c][l]
+    float* dq;                 // [R][B][Hq][tiles][4][DP / 4][32][4]: query 32 a + l, columns 4 c .. 4 c + 3 at [a][c][l]
     AttnShape s;
     float scale, scale_log2;
     float* dkv;                // [G][2][B][Hkv][k_tiles * 128][DP]: dv, dk of one head group; null when G = 1
@@ -88,7 +88,8 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
 // ---- main ------------------------------------------------------------------------------------------------------------
 template <int DP> struct GradSmem {
     static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes;
-    // stages of q (with its row values), of dout, of ds; dq leaves through two pieces of 128 queries x 32 columns in fp32
+    // stages of q (with its row values), of dout, of ds; dq leaves in pieces of 32 queries x 16 columns in fp32, four
+    // at a time for each of its warps
     static constexpr int NQ = DP == 64 ? 3 : 2, NG = DP == 64 ? 2 : 1, ND = DP == 64 ? 2 : 1;
     static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, STAGE = DS + ND * 2 * (int)kBlockBytes;
     static constexpr int ROWS = STAGE + 32768, BARS = ROWS + NQ * 1024, kBytes = BARS + 256;
@@ -97,7 +98,7 @@ static_assert(GradSmem<64>::kBytes <= 232448 && GradSmem<128>::kBytes <= 232448,
 
 struct GradBars {
     uint64_t kv_full, q_full[3], q_empty[3], g_full[2], g_empty[2], cut_full;
-    uint64_t s_full[2], p_ready[2], dp_full[2], ds_ready[2], ds_free[2], dq_full, dq_free, staged[2], stage_free[2], acc_full, acc_free, idle;
+    uint64_t s_full[2], p_ready[2], dp_full[2], ds_ready[2], ds_free[2], dq_full, dq_free, acc_full, acc_free, idle;
     uint32_t tmem_slot, dead;
 };
 static_assert(sizeof(GradBars) <= 256, "");
@@ -106,7 +107,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant__ GradArgs a)
 {
     using L = GradSmem<DP>;
-    constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG, ND = L::ND, BATCHES = DP / 32;
+    constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG, ND = L::ND;
     constexpr bool kOwnDq = DP == 64;                          // dq has columns of its own; else it takes those of dp
     extern __shared__ __align__(1024) uint8_t smem[];          // the whole of the block's shared memory, so at an even kilobyte
     GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 
     if (tid == 0) {
         s.dead = 0;
-        for (uint64_t* p : {&s.kv_full, &s.cut_full, &s.dq_full, &s.stage_free[0], &s.stage_free[1], &s.acc_full, &s.idle}) bar_init(p, 1);
+        for (uint64_t* p : {&s.kv_full, &s.cut_full, &s.dq_full, &s.acc_full, &s.idle}) bar_init(p, 1);
         for (int i = 0; i < NQ; ++i) { bar_init(&s.q_full[i], 1); bar_init(&s.q_empty[i], 1); }
         for (int i = 0; i < NG; ++i) { bar_init(&s.g_full[i], 1); bar_init(&s.g_empty[i], 1); }
         for (int i = 0; i < 2; ++i) {
@@ -136,9 +137,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             bar_init(&s.ds_ready[i], kPairWarps / 2);
         }
         bar_init(&s.acc_free, kPairWarps);
-        bar_init(&s.dq_free, kOwnDq ? kPairWarps : kPairWarps / 2);
-        bar_init(&s.staged[0], kPairWarps / 2);
-        bar_init(&s.staged[1], kPairWarps / 2);
+        bar_init(&s.dq_free, 4);
         fence_bar_init();
     }
     if (warp == kMmaWarp) tmem_alloc<512>(&s.tmem_slot);
@@ -325,33 +324,51 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             bar_drain(&s.idle, 0);
         }
         __syncwarp();
-    } else if (warp == kOutWarp) {                              // ---- dq: shared memory -> this share's buffer
-        uint32_t k = 0;
+    } else if (warp >= kDqWarp) {                               // ---- dq: tensor memory -> this share's buffer
+        // Each warp takes 32 queries.  Pieces go through shared memory and are added by the memory system: adding from
+        // registers kept the load/store unit busy and stalled every other warp behind it.
+        constexpr int CH = 4, PER = DP / 16;
+        const uint32_t quarter = warp & 3, lane_base = quarter << 21;
+        float4* stage = reinterpret_cast<float4*>(smem + L::STAGE + quarter * CH * 2048);
+        uint32_t n = 0;
         bool ok = true;
         for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
             const uint32_t per_head = meets(share_tile(share, m, a.shares)), pairs = per_head * heads;
-            for (uint32_t t = 0, i = nq - per_head, h = h0; t < pairs && ok; ++t) {
-                float* dst = a.dq + ((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * (128 * DP);
+            for (uint32_t t = 0, i = nq - per_head, h = h0; t < pairs; ++t, ++n) {
+                float* dst = a.dq + (((((uint64_t)share * a.s.B + b) * a.s.Hq + h) * a.q_tiles + i) * 4 + quarter) * (32 * DP);
                 if (++i == nq) { i = nq - per_head; ++h; }
-                for (int c = 0; c < BATCHES; ++c, ++k) {        // piece k passes through buffer k % 2
-                    ok = warp_wait(&s.staged[k & 1], (k >> 1) & 1, g);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        // the additions of the last visit to this query tile are done before those of this one begin: all but
-                        // the pair before's are complete, and with one pair a key tile that one's too
-                        if (c == 0) {
-                            if (pairs > 1) bulk_wait<BATCHES>();
-                            else bulk_wait<0>();
-                        }
-                        const uint8_t* from = smem + L::STAGE + (k & 1) * 16384;
-                        // the share's first key tile is the first to meet every query tile it meets at all
-                        if (m == 0) bulk_store(dst + c * 4096, from, 16384);
-                        else bulk_add_f32(dst + c * 4096, from, 16384);
-                        bulk_commit();
-                        bulk_wait_read<0>();
-                        bar_arrive(&s.stage_free[k & 1]);
-                    }
+                ok = warp_wait(&s.dq_full, n & 1, g);
+                if (!ok) break;
+                tc_fence_after();
+                // the additions of the last visit to this query tile are done before those of this one begin: all but those of
+                // the pair before are complete, and with one pair a key tile those too
+                if (lane == 0) {
+                    if (pairs > 1) bulk_wait<PER>();
+                    else bulk_wait<0>();
+                }
+#pragma unroll
+                for (int c = 0; c < PER; ++c) {
+                    uint32_t x[16];
+                    tmem_ld16(t_dq + lane_base + c * 16, x);
+                    if (lane == 0) bulk_wait_read<CH - 1>();    // the piece that was here has left
                     __syncwarp();
+                    tmem_wait_ld<16>(x);
+                    if (c + 1 == PER) {
+                        tc_fence_before();
+                        warp_arrive(&s.dq_free);
+                    }
+                    float4* to = stage + (c % CH) * 128 + lane;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        to[e * 32] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        // the share's first key tile is the first to meet every query tile it meets at all
+                        if (m == 0) bulk_store(dst + c * 512, stage + (c % CH) * 128, 2048);
+                        else bulk_add_f32(dst + c * 512, stage + (c % CH) * 128, 2048);
+                        bulk_commit();
+                    }
                 }
             }
         }
@@ -361,37 +378,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         const uint32_t my_s = t_s + lane_base + grp * 32, my_dp = t_dp + lane_base + grp * 32;
         uint8_t* ds_row = smem + L::DS + e2 * kBlockBytes + row * 128;
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
-        float4* stage = reinterpret_cast<float4*>(smem + L::STAGE) + (warp & 3) * 256 + (grp & 1) * 128 + lane;
         uint32_t n = 0, w = 0;
         bool ok = true;
-
-        // dq of pair x: tensor memory -> shared memory in pieces of 32 columns, 16 a warp.  With columns of its own each group
-        // takes one piece, at different points of their steps; else the first group takes all, at once, since dp waits for
-        // the columns.
-        auto drain = [&](uint32_t x) {
-            ok = warp_wait(&s.dq_full, x & 1, g);
-            if (!ok) return;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < (kOwnDq ? 1 : BATCHES); ++c) {
-                const uint32_t piece = kOwnDq ? e2 : c, k = x * BATCHES + piece;
-                uint32_t v[16];
-                tmem_ld16(t_dq + lane_base + piece * 32 + (grp & 1) * 16, v);
-                tmem_wait_ld<16>(v);
-                if (kOwnDq || c + 1 == BATCHES) {
-                    tc_fence_before();
-                    warp_arrive(&s.dq_free);
-                }
-                if (k >= 2) ok = warp_wait(&s.stage_free[k & 1], ((k >> 1) - 1) & 1, g);
-                if (!ok) return;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    stage[(k & 1) * 1024 + e * 32] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
-                fence_async_smem();
-                warp_arrive(&s.staged[k & 1]);
-            }
-        };
-
         for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
             const uint32_t j = share_tile(share, m, a.shares), per_head = meets(j), pairs = per_head * heads;
             if (j >= a.k_tiles) continue;
@@ -436,10 +424,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 tc_fence_before();
                 warp_arrive(&s.p_ready[e2]);
 
-                if (n && (kOwnDq ? e2 == 1 : e2 == 0)) {
-                    drain(n - 1);
-                    if (!ok) break;
-                }
                 ok = warp_wait(&s.dp_full[e2], n & 1, g);
                 if (ok && n >= ND) ok = warp_wait(&s.ds_free[n % ND], (n / ND - 1) & 1, g);
                 if (!ok) break;
@@ -471,10 +455,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 fence_async_smem();
                 tc_fence_before();
                 warp_arrive(&s.ds_ready[e2]);
-                if (kOwnDq && n && e2 == 0) {
-                    drain(n - 1);
-                    if (!ok) break;
-                }
             }
             if (!ok) break;
             // this key tile's gradients: two groups dv, two dk, half of the columns each
@@ -519,7 +499,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 ++w;
             }
         }
-        if (ok && n && (kOwnDq || e2 == 0)) drain(n - 1);
     }
     __syncthreads();
     if (warp == kMmaWarp) {
@@ -539,10 +518,10 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
     if (token >= s.Sq) return;
     T* dst = (T*)dq.p + (int64_t)b * dq.sb + (int64_t)token * dq.st + (int64_t)h * dq.sh;
     const uint64_t stride = (uint64_t)s.B * s.Hq * q_tiles * (DP / 4) * 128;
-    const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row / 32 * 256 + row % 32;
+    const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row / 32 * (DP / 4) * 32 + row % 32;
 #pragma unroll 4
     for (uint32_t c = (threadIdx.x >> 7) * 8; c < s.D; c += 16) {
-        const uint32_t at = c / 32 * 1024 + c % 32 / 4 * 32;
+        const uint32_t at = c / 4 * 32;
         float y[8] = {};
         for (uint32_t r = 0; r < parts; ++r) {
             const float4 u = src[r * stride + at], v = src[r * stride + at + 32];
