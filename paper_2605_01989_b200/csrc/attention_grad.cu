@@ -15,8 +15,8 @@
 // Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
 // two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
-//   warps         0-7 p and ds of a pair's first 64 queries, 8-15 of the others (each thread one key and 32 queries), half a
-//                 step apart; 16-19 dq to memory, 20 TMA, 21 products.
+//   warps         0-15 p and ds, each thread one key and 32 queries, with head_dim up to 64 in two groups half a step apart;
+//                 16-19 dq to memory, 20 TMA, 21 products.
 #include <math.h>
 
 #include "attention.cuh"
@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 {
     using L = GradSmem<DP>;
     constexpr int NS = L::NS, NQ = L::NQ, NG = L::NG, ND = L::ND;
+    constexpr int NE = DP == 64 ? 2 : 1;                       // groups that the queries of a pair are split into
     constexpr bool kOwnDq = DP == 64;                          // dq has columns of its own; else it takes those of dp
     extern __shared__ __align__(1024) uint8_t smem[];          // the whole of the block's shared memory, so at an even kilobyte
     GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
@@ -133,8 +134,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             bar_init(&s.s_full[i], 1);
             bar_init(&s.dp_full[i], 1);
             bar_init(&s.ds_free[i], 1);
-            bar_init(&s.p_ready[i], kPairWarps / 2);
-            bar_init(&s.ds_ready[i], kPairWarps / 2);
+            bar_init(&s.p_ready[i], kPairWarps / NE);
+            bar_init(&s.ds_ready[i], kPairWarps / NE);
         }
         bar_init(&s.acc_free, kPairWarps);
         bar_init(&s.dq_free, 4);
@@ -210,17 +211,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&s.g_full[x % NG], (x / NG) & 1);
         }
     } else if (warp == kMmaWarp) {                              // ---- products
-        // Each pair is done in two halves of 64 queries by two groups of warps that work half a step apart: one computes p
-        // while the other computes ds.  The order below follows them: p of the first half, ds of the second half of the pair
-        // before, ds of the first half, p of the second.
+        // head_dim up to 64: each pair is done in two halves of 64 queries by two groups of warps that work half a step apart,
+        // one computes p while the other computes ds.  The order below follows them: p of the first half, ds of the second
+        // half of the pair before, ds of the first half, p of the second.  With 128 there is no room for that: dq takes the
+        // columns of dp, so that dp of the next pair waits for dq in any case, and all warps take the whole pair together (8192
+        // tokens, 16 heads on 4, causal: 1.40 ms in halves).
         const uint32_t leader = elect_leader();
-        constexpr uint32_t id_kk = mma_desc<T>(128, 64, false, false);          // s, dp of a half
+        constexpr uint32_t id_kk = mma_desc<T>(128, 128 / NE, false, false);    // s, dp of a group
         constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);           // dv, dk: right operand across its rows
         constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);            // dq: both across their rows
         const uint32_t base = smem_addr(smem);
         uint32_t n = 0, w = 0;
         bool ok = true;
-        // s (left k, right q) or dp (left v, right dout) of half e
+        // s (left k, right q) or dp (left v, right dout) of group e
         auto half_scores = [&](uint32_t to, uint32_t left, uint32_t right, uint32_t e, uint64_t* done) {
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
@@ -236,19 +239,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         auto dprobs = [&](uint32_t x, uint32_t e) { half_scores(t_dp, base + L::V, g_at(x), e, &s.dp_full[e]); };
         auto add_dv = [&](uint32_t x, uint32_t e, bool acc) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)                      // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
+            for (int kk = 0; kk < 8 / NE; ++kk)                 // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
                 mma_ts(leader, t_dv, t_s + e * 64 + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(g_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
                        acc || kk > 0);
         };
         auto add_dk = [&](uint32_t x, uint32_t e, bool acc) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-                mma_ss(leader, t_dk, desc_k(ds_at(x) + e * kBlockBytes + kk * 32), desc_mn(q_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
+            for (int kk = 0; kk < 8 / NE; ++kk)
+                mma_ss(leader, t_dk, desc_k(ds_at(x) + (e + kk / 4) * kBlockBytes + kk % 4 * 32), desc_mn(q_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
                        acc || kk > 0);
         };
-        // second half of pair x: its ds is there, so dk and dq can be completed; `more`: another pair of this key tile follows
-        auto finish = [&](uint32_t x, bool more) {
-            ok = ok && warp_wait(&s.ds_ready[1], x & 1, g);
+        // last group of pair x: its ds is there, so dk and dq can be completed; `more`: another pair of this key tile follows
+        auto finish = [&](uint32_t x, bool more, bool acc) {
+            ok = ok && warp_wait(&s.ds_ready[NE - 1], x & 1, g);
             if (ok && kOwnDq && x) ok = warp_wait(&s.dq_free, (x - 1) & 1, g);
             if (!ok) return;
             tc_fence_after();
@@ -257,15 +260,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             for (int kk = 0; kk < 8; ++kk)
                 mma_ss(leader, t_dq, desc_mn(ds_at(x) + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
             mma_commit(leader, &s.dq_full);
-            add_dk(x, 1, true);
+            add_dk(x, NE - 1, acc);
             mma_commit(leader, &s.q_empty[x % NQ]);
             mma_commit(leader, &s.ds_free[x % ND]);
             if (!kOwnDq && more) {                              // dp of the next pair comes where dq is
-                ok = warp_wait(&s.dq_free, x & 1, g);       // (its dout is there: dv of its first half came before)
+                ok = warp_wait(&s.g_full[(x + 1) % NG], ((x + 1) / NG) & 1, g) && warp_wait(&s.dq_free, x & 1, g);
                 if (!ok) return;
                 tc_fence_after();
                 dprobs(x + 1, 0);
-                dprobs(x + 1, 1);
             }
         };
         for (uint32_t m = 0; ok && m * a.shares < a.k_tiles; ++m) {
@@ -274,48 +276,45 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             ok = warp_wait(&s.kv_full, w & 1, g) && warp_wait(&s.q_full[n % NQ], (n / NQ) & 1, g);
             if (!ok) break;
             tc_fence_after();
-            scores(n, 0);
-            scores(n, 1);
+            for (int e = 0; e < NE; ++e) scores(n, e);
             ok = warp_wait(&s.g_full[n % NG], (n / NG) & 1, g);
             if (ok && !kOwnDq && n) ok = warp_wait(&s.dq_free, (n - 1) & 1, g);
             if (!ok) break;
             tc_fence_after();
-            dprobs(n, 0);
-            dprobs(n, 1);
+            for (int e = 0; e < NE; ++e) dprobs(n, e);
             for (uint32_t t = 0; t < pairs && ok; ++t, ++n) {
                 const bool more = t + 1 < pairs;
-                ok = warp_wait(&s.p_ready[0], n & 1, g) && warp_wait(&s.g_full[n % NG], (n / NG) & 1, g);
+                ok = warp_wait(&s.p_ready[0], n & 1, g);
                 if (ok && t == 0 && w) ok = warp_wait(&s.acc_free, (w - 1) & 1, g);
                 if (!ok) break;
                 tc_fence_after();
                 add_dv(n, 0, t > 0);
-                if (more && NQ > 2) {
+                if (NE == 1) mma_commit(leader, &s.g_empty[n % NG]);
+                if (more) {
                     ok = warp_wait(&s.q_full[(n + 1) % NQ], ((n + 1) / NQ) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
                     scores(n + 1, 0);                           // over p, which the product before has read by then
                 }
-                if (t > 0) finish(n - 1, true);                 // with two stages, q of the next pair comes into its place
-                ok = ok && warp_wait(&s.ds_ready[0], n & 1, g);
-                if (ok && kOwnDq && more) ok = warp_wait(&s.g_full[(n + 1) % NG], ((n + 1) / NG) & 1, g);
-                if (!ok) break;
-                tc_fence_after();
-                if (kOwnDq && more) dprobs(n + 1, 0);
-                add_dk(n, 0, t > 0);
-                ok = warp_wait(&s.p_ready[1], n & 1, g);
-                if (!ok) break;
-                tc_fence_after();
-                add_dv(n, 1, true);
-                mma_commit(leader, &s.g_empty[n % NG]);
-                if (more && NQ <= 2) {
-                    ok = warp_wait(&s.q_full[(n + 1) % NQ], ((n + 1) / NQ) & 1, g);
+                if (NE == 1) {
+                    finish(n, more, t > 0);
+                } else {
+                    if (t > 0) finish(n - 1, true, true);
+                    ok = ok && warp_wait(&s.ds_ready[0], n & 1, g);
+                    if (ok && more) ok = warp_wait(&s.g_full[(n + 1) % NG], ((n + 1) / NG) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
-                    scores(n + 1, 0);
+                    if (more) dprobs(n + 1, 0);
+                    add_dk(n, 0, t > 0);
+                    ok = warp_wait(&s.p_ready[1], n & 1, g);
+                    if (!ok) break;
+                    tc_fence_after();
+                    add_dv(n, 1, true);
+                    mma_commit(leader, &s.g_empty[n % NG]);
+                    if (more) scores(n + 1, 1);
                 }
-                if (more) scores(n + 1, 1);
             }
-            finish(n - 1, false);
+            if (NE == 2) finish(n - 1, false, true);
             if (ok) mma_commit(leader, &s.acc_full);
             ++w;
         }
@@ -374,9 +373,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         }
         if (lane == 0) bulk_wait<0>();
     } else {                                                    // ---- p and ds: thread = key (lane of the tile), 32 queries
-        const uint32_t grp = warp >> 2, e2 = warp >> 3, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
+        const uint32_t grp = warp >> 2, e2 = NE == 2 ? warp >> 3 : 0, lane_base = (warp & 3) << 21, row = (warp & 3) * 32 + lane;
         const uint32_t my_s = t_s + lane_base + grp * 32, my_dp = t_dp + lane_base + grp * 32;
-        uint8_t* ds_row = smem + L::DS + e2 * kBlockBytes + row * 128;
+        uint8_t* ds_row = smem + L::DS + (grp >> 1) * kBlockBytes + row * 128;
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
         uint32_t n = 0, w = 0;
         bool ok = true;
