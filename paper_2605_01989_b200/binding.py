@@ -435,9 +435,14 @@ def _dtype(t):
 
 def _on_device(*tensors):
     """The library launches on the current device: every tensor has to be there."""
+    cur = -1
     for t in tensors:
-        if t is not None and (t.get_device() < 0 or t.get_device() != torch._C._cuda_getDevice()):
-            raise ValueError("a tensor on %s, which is not the current device" % t.device)
+        if t is not None:
+            dev = t.get_device()
+            if cur < 0 <= dev:
+                cur = torch._C._cuda_getDevice()
+            if dev < 0 or dev != cur:
+                raise ValueError("a tensor on %s, which is not the current device" % t.device)
 
 
 def _raw_stream(stream):

@@ -57,6 +57,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict__ rows, AttnShape s, uint32_t q_tiles)
 {
+    after_start();
     const uint32_t lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z, lq = length_of(s.q_lens, b, s.Sq), lk = length_of(s.k_lens, b, s.Sk);
     const uint32_t i = blockIdx.x * 32 + (threadIdx.x >> 5) * 4 + (lane >> 3);
     const bool live = keys_of(i, lq, lk, s.causal) > 0;
@@ -148,6 +149,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     const uint32_t tmem = s.tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
     const uint32_t t_dq = kOwnDq ? tmem + 384 : t_dp;
     const Guard g{&s.dead, a.timeouts};
+    after_start();
+    wait_before();                                              // the rows' values; what is above ran beside their kernel
 
     if (warp == kTmaWarp) {                                       // ---- TMA
         uint32_t n = 0, w = 0, cuts = 0;                        // pairs, key tiles with work, tiles that were cleared
@@ -511,6 +514,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part, Heads dq, AttnShape s, float scale, uint32_t q_tiles, uint32_t shares)
 {
+    wait_before();
     const uint32_t i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row = threadIdx.x & 127, token = i * 128 + row;
     const uint32_t lq = length_of(s.q_lens, b, s.Sq), lk = length_of(s.k_lens, b, s.Sk);
     const uint32_t most = i * 128 < lq ? keys_of(min(lq, i * 128 + 128) - 1, lq, lk, s.causal) : 0, parts = min(shares, (most + 127) / 128);
@@ -539,6 +543,8 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_grad_dkv(const float* __restrict__ part, Heads dk, Heads dv, AttnShape s, uint32_t k_rows, uint32_t groups)
 {
+    after_start();
+    wait_before();
     const uint32_t at = blockIdx.x * 256 + threadIdx.x, c = at % (DP / 8) * 8, key = at / (DP / 8), hk = blockIdx.y, b = blockIdx.z >> 1, is_dk = blockIdx.z & 1;
     if (key >= s.Sk || c >= s.D) return;
     const uint64_t stride = 2ull * s.B * s.Hkv * k_rows * DP;
@@ -612,18 +618,14 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
     }
     if (sh.Sk) {
         const cudaError_t e = allow_shared<k_grad<T, DP>>(GradSmem<DP>::kBytes);
-    DBLP_CUDA(e);
-        k_grad<T, DP><<<dim3(r.shares * r.groups, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
-        DBLP_LAUNCHED();
+        DBLP_CUDA(e);
+        DBLP_NEXT(launch_next(k_grad<T, DP>, dim3(r.shares * r.groups, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s, r));
+        if (r.dkv)
+            DBLP_NEXT(launch_next(k_grad_dkv<T, DP>, dim3((sh.Sk * (DP / 8) + 255) / 256, sh.Hkv, sh.B * 2), 256, 0, s, r.dkv, r.dk, r.dv, sh,
+                                  r.k_tiles * 128, r.groups));
     }
-    if (sh.Sk && r.dkv) {
-        k_grad_dkv<T, DP><<<dim3((sh.Sk * (DP / 8) + 255) / 256, sh.Hkv, sh.B * 2), 256, 0, s>>>(r.dkv, r.dk, r.dv, sh, r.k_tiles * 128, r.groups);
-        DBLP_LAUNCHED();
-    }
-    if (sh.Sq) {
-        k_grad_dq<T, DP><<<dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s>>>((const float4*)r.dq, dq, sh, r.scale, r.q_tiles, r.shares);
-        DBLP_LAUNCHED();
-    }
+    if (sh.Sq)
+        DBLP_NEXT(launch_next(k_grad_dq<T, DP>, dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s, (const float4*)r.dq, dq, sh, r.scale, r.q_tiles, r.shares));
     return DBLP_OK;
 }
 

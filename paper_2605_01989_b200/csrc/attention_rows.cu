@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_attention_rows(const __grid
     constexpr int GROUPS = 32 / LPK, STEP = kRowsWarps * GROUPS, DP = LPK * 8;
     constexpr int kRowsAhead = NR <= 4 ? 4 : 2;                 // keys a group takes at a time, with as many more in flight
     __shared__ float s_acc[kRowsWarps][NR][DP + 2];
+    after_start();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_key = lane % LPK, group = warp * GROUPS + lane / LPK, c = in_key * 8;
     const uint32_t hk = blockIdx.x, split = blockIdx.y, b = blockIdx.z, rows = a.s.Sq * a.s.rep;
     const uint32_t lq = length_of(a.s.q_lens, b, a.s.Sq), lk = length_of(a.s.k_lens, b, a.s.Sk);
@@ -182,6 +183,7 @@ __global__ void __launch_bounds__(128) k_attention_join(const __grid_constant__ 
 {
     constexpr int DP = LPK * 8, GROUPS = 128 / LPK;
     __shared__ float s_acc[GROUPS][DP + 2];
+    wait_before();
     const uint32_t rows = a.s.Sq * a.s.rep, row = blockIdx.x, group = threadIdx.x / LPK, c = threadIdx.x % LPK * 8;
     const uint64_t total = (uint64_t)a.s.B * a.s.Hkv * rows;
     const uint32_t per = (a.splits + GROUPS - 1) / GROUPS, lo = min(a.splits, group * per), hi = min(a.splits, lo + per);
@@ -234,8 +236,7 @@ template <typename T, int LPK> static int launch_rows(const RowsArgs& r, cudaStr
     else k_attention_rows<T, LPK, 8><<<grid, kRowsWarps * 32, 0, s>>>(r);
     DBLP_LAUNCHED();
     if (r.part) {
-        k_attention_join<T, LPK><<<r.s.B * r.s.Hkv * rows, 128, 0, s>>>(r);
-        DBLP_LAUNCHED();
+        DBLP_NEXT(launch_next(k_attention_join<T, LPK>, r.s.B * r.s.Hkv * rows, 128, 0, s, r));
     }
     return DBLP_OK;
 }

@@ -41,6 +41,17 @@ extern std::atomic<uint64_t> g_launches;
         }                                                                                       \
     } while (0)
 
+// A launch through the runtime's launch call, which gives the status itself.
+#define DBLP_NEXT(call)                                                                         \
+    do {                                                                                        \
+        const cudaError_t e_ = (call);                                                          \
+        dblp::g_launches.fetch_add(1, std::memory_order_relaxed);                               \
+        if (e_ != cudaSuccess) {                                                                \
+            dblp::set_error("kernel launch failed: %s (%s:%d)", cudaGetErrorString(e_), __FILE__, __LINE__); \
+            return DBLP_ECUDA;                                                                  \
+        }                                                                                       \
+    } while (0)
+
 #define DBLP_REQUIRE(cond, status, ...)                                                         \
     do {                                                                                        \
         if (!(cond)) {                                                                          \

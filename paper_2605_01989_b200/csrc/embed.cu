@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(256)
 k_rank_sort(const I* __restrict__ tokens, uint32_t n, int64_t rows, int64_t padding, uint32_t* __restrict__ keys,
             uint32_t* __restrict__ pos, uint32_t* __restrict__ seen, uint32_t seen_words, unsigned long long* bad)
 {
+    after_start();
     extern __shared__ uint32_t s_key[];                        // all n keys, padded to a multiple of 32 with all-ones
     __shared__ uint32_t s_cnt[8][32], s_seen[kSeenWords];
     const uint32_t n32 = (n + 31) & ~31u, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = blockIdx.x * 32 + lane;
@@ -174,6 +175,8 @@ k_radix_count(const I* __restrict__ tokens, const uint32_t* __restrict__ keys, u
               unsigned long long* bad)
 {
     __shared__ uint32_t s_hist[kRadix];
+    after_start();
+    wait_before();
     s_hist[threadIdx.x] = 0;
     if (FIRST)
         for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < seen_words; i += gridDim.x * 256) seen[i] = 0;
@@ -196,6 +199,8 @@ k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys,
     __shared__ uint32_t s_scan[8];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nb = gridDim.x;
     for (uint32_t i = tid; i < 8 * kRadix; i += 256) (&s_warp[0][0])[i] = 0;
+    after_start();
+    wait_before();
     const uint32_t blo = blockIdx.x * per, bhi = min(n, blo + per);
     const bool staged = per <= kRadixStage;
     if (staged)
@@ -322,6 +327,8 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
              uint32_t accumulate, float* __restrict__ part, const uint32_t* __restrict__ seen, uint64_t sum_warps)
 {
     constexpr int kAhead = G == 8 ? (sizeof(TI) == 2 ? 8 : 4) : 16;     // rows in flight a lane
+    after_start();
+    wait_before();
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t w = (uint64_t)blockIdx.x * kGradWarps + (threadIdx.x >> 5);
     if (w >= sum_warps) {
@@ -428,6 +435,7 @@ k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32
             TO* __restrict__ dtable, int64_t ts, uint32_t accumulate, const float* __restrict__ part, uint32_t short_blocks)
 {
     __shared__ float s_part[kGradWarps][32 * G];
+    wait_before();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = (n + kTile - 1) / kTile;
     float acc[G];
 #pragma unroll
@@ -510,13 +518,11 @@ static int sort_tokens(const I* tokens, uint32_t n, uint32_t rows, int64_t paddi
         if (shift == 0) {
             k_radix_count<I, true><<<nb, 256, 0, s>>>(tokens, nullptr, n, per, shift, rows, padding, table, seen, seen_words, bad);
             DBLP_LAUNCHED();
-            k_radix_scatter<I, true><<<nb, 256, 0, s>>>(tokens, nullptr, nullptr, n, per, shift, rows, padding, table, k[to], p[to], seen);
+            DBLP_NEXT(launch_next(k_radix_scatter<I, true>, nb, 256, 0, s, tokens, nullptr, nullptr, n, per, shift, rows, padding, table, k[to], p[to], seen));
         } else {
-            k_radix_count<I, false><<<nb, 256, 0, s>>>(tokens, k[from], n, per, shift, rows, padding, table, nullptr, 0, nullptr);
-            DBLP_LAUNCHED();
-            k_radix_scatter<I, false><<<nb, 256, 0, s>>>(tokens, k[from], p[from], n, per, shift, rows, padding, table, k[to], p[to], seen);
+            DBLP_NEXT(launch_next(k_radix_count<I, false>, nb, 256, 0, s, tokens, k[from], n, per, shift, rows, padding, table, nullptr, 0, nullptr));
+            DBLP_NEXT(launch_next(k_radix_scatter<I, false>, nb, 256, 0, s, tokens, k[from], p[from], n, per, shift, rows, padding, table, k[to], p[to], seen));
         }
-        DBLP_LAUNCHED();
         from = to;
     }
     *keys = k[from]; *pos = p[from];
@@ -532,15 +538,13 @@ static int launch_sums(const TI* dout, int64_t ds, const uint32_t* keys, const u
     const uint64_t sum_warps = (sums + kGradWarps - 1) / kGradWarps * kGradWarps;      // whole blocks of either kind
     const uint64_t grid = (sum_warps + zeros + kGradWarps - 1) / kGradWarps;
     DBLP_REQUIRE(grid < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
-    k_grad_tiles<TI, TO, G><<<(unsigned)grid, kGradWarps * 32, 0, s>>>(dout, ds, keys, pos, n, rows, width, slabs, scale, dtable, ts,
-                                                                     accumulate, part, seen, sum_warps);
-    DBLP_LAUNCHED();
+    DBLP_NEXT(launch_next(k_grad_tiles<TI, TO, G>, (unsigned)grid, kGradWarps * 32, 0, s, dout, ds, keys, pos, n, rows, width, slabs, scale, dtable,
+                          ts, accumulate, part, seen, sum_warps));
     if (tiles > 1) {                                                   // a run can cross tiles
         const uint64_t brief = ((tiles - 1ull) * slabs + kGradWarps - 1) / kGradWarps, lengthy = (uint64_t)((tiles - 1) / 64) * slabs;
         DBLP_REQUIRE(brief + lengthy < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
-        k_grad_join<TO, G><<<(unsigned)(brief + lengthy), kGradWarps * 32, 0, s>>>(keys, n, rows, width, slabs, scale, dtable, ts, accumulate,
-                                                                                  part, (uint32_t)brief);
-        DBLP_LAUNCHED();
+        DBLP_NEXT(launch_next(k_grad_join<TO, G>, (unsigned)(brief + lengthy), kGradWarps * 32, 0, s, keys, n, rows, width, slabs, scale, dtable, ts,
+                              accumulate, part, (uint32_t)brief));
     }
     return DBLP_OK;
 }

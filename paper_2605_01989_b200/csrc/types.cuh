@@ -107,6 +107,27 @@ struct FastDiv {
     }
 };
 
+// Kernels of one call that follow each other: each lets the next one be set up while it still runs (after_start), and waits for
+// the one before, results included, as its first step (wait_before).  Every block of every kernel in such a chain does both.
+__device__ __forceinline__ void after_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline cudaError_t launch_next(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A&&... args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 inline int element_bytes(int dtype) { return dtype == DBLP_F32 ? 4 : 2; }
 inline bool known_dtype(int dtype) { return dtype == DBLP_F32 || dtype == DBLP_BF16 || dtype == DBLP_F16; }
 
