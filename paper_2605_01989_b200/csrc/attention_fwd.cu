@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* sq = smem;
     uint8_t* ring = smem + L::TILE;
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
 
     if (tid == 0) {
         dead = 0;
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, t_s = tmem, t_o = tmem + 128;
+    const uint32_t tmem = uniform(tmem_slot), t_s = tmem, t_o = tmem + 128;
     const Guard g{&dead, a.timeouts};
 
     if (warp == 4) {                                            // ---- TMA: q, k(0), v(0), k(1), ...
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         bool ok = true;
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
             const Item it = item_of(a, x);
-            const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk), hk = it.h / a.s.rep;
+            const uint32_t lq = uniform(length_of(a.s.q_lens, it.b, a.s.Sq)), lk = uniform(length_of(a.s.k_lens, it.b, a.s.Sk)), hk = it.h / a.s.rep;
             const uint32_t nk = (key_halves(a, it.qt * 128, lq, lk) + 1) / 2;
             if (nk == 0) continue;
             if (w) ok = warp_wait(&q_empty, (w - 1) & 1, g);
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         };
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
             const Item it = item_of(a, x);
-            const uint32_t lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
+            const uint32_t lq = uniform(length_of(a.s.q_lens, it.b, a.s.Sq)), lk = uniform(length_of(a.s.k_lens, it.b, a.s.Sk));
             const uint32_t nh = key_halves(a, it.qt * 128, lq, lk);
             if (nh == 0) continue;
             ok = warp_wait(&q_full, w & 1, g);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         bool ok = true;
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
         const Item it = item_of(a, x);
-        const uint32_t q0 = it.qt * 128, lq = length_of(a.s.q_lens, it.b, a.s.Sq), lk = length_of(a.s.k_lens, it.b, a.s.Sk);
+        const uint32_t q0 = it.qt * 128, lq = uniform(length_of(a.s.q_lens, it.b, a.s.Sq)), lk = uniform(length_of(a.s.k_lens, it.b, a.s.Sk));
         const uint32_t nh = key_halves(a, q0, lq, lk);
         const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal);
         float m = -INFINITY, l = 0.0f;

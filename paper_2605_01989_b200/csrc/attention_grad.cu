@@ -114,10 +114,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     extern __shared__ __align__(1024) uint8_t smem[];          // the whole of the block's shared memory, so at an even kilobyte
     GradBars& s = *reinterpret_cast<GradBars*>(smem + L::BARS);
 
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const uint32_t share = blockIdx.x % a.shares, group = blockIdx.x / a.shares, hk = blockIdx.y, b = blockIdx.z;
     const uint32_t heads = a.group_heads, h0 = hk * a.s.rep + group * heads;        // this block's query heads
-    const uint32_t lq = length_of(a.s.q_lens, b, a.s.Sq), lk = length_of(a.s.k_lens, b, a.s.Sk);
+    const uint32_t lq = uniform(length_of(a.s.q_lens, b, a.s.Sq)), lk = uniform(length_of(a.s.k_lens, b, a.s.Sk));
     const uint32_t nq = (lq + 127) / 128, nk = lq ? (lk + 127) / 128 : 0;
     // query tiles per head that key tile j meets
     auto meets = [&](uint32_t j) -> uint32_t {
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s.tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
+    const uint32_t tmem = uniform(s.tmem_slot), t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
     const uint32_t t_dq = kOwnDq ? tmem + 384 : t_dp;
     const Guard g{&s.dead, a.timeouts};
     after_start();

@@ -85,6 +85,10 @@ __device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
     while (!bar_try(b, parity) && clock64() - t0 < kWaitCycles) {}
 }
 
+// A value that is the same in all lanes, in a form from which the compiler sees that: loops and branches on it, and the
+// operands of the products inside them, then stay in uniform registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+
 // ---- TMA -------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tma_tile(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3)
 {
