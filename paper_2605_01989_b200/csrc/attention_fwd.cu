@@ -176,7 +176,6 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             for (uint32_t x = n > (uint32_t)STAGES ? n - STAGES : 0; x < n; ++x) bar_drain(&full[x % STAGES], (x / STAGES) & 1);
         }
     } else if (warp == 5) {                                     // ---- products
-        const uint32_t leader = elect_leader();
         constexpr uint32_t id_s = mma_desc<T>(128, 64, false, false), id_o = mma_desc<T>(128, DP, false, true);
         const uint32_t qa = smem_addr(sq), ra = smem_addr(ring);
         uint32_t n = 0, w = 0, count = 0;                       // ring tiles and items before this one, halves in all
@@ -191,11 +190,11 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
                 const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                mma_ss(leader, t_s + to * 64, desc_k(qa + off), desc_k(ka + off), id_s, kk > 0);
+                mma_ss(t_s + to * 64, desc_k(qa + off), desc_k(ka + off), id_s, kk > 0);
             }
-            if ((h & 1) || h + 1 == nh) mma_commit(leader, &empty[st]);
-            mma_commit(leader, &s_full[to]);
-            if (h + 1 == nh) mma_commit(leader, &q_empty);
+            if ((h & 1) || h + 1 == nh) mma_commit(&empty[st]);
+            mma_commit(&s_full[to]);
+            if (h + 1 == nh) mma_commit(&q_empty);
         };
         for (uint32_t round = 0, x; (x = item_number(round)) < a.items && ok; ++round) {
             const Item it = item_of(a, x);
@@ -214,10 +213,10 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                 const uint32_t va = ra + st * L::TILE + (h & 1) * (kBlockBytes / 2);
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
-                    mma_ts(leader, t_o, t_s + from * 64 + kk * 8, desc_mn(va + kk * 2048, kBlockBytes), id_o, h > 0 || kk > 0);
-                if ((h & 1) || h + 1 == nh) mma_commit(leader, &empty[st]);
-                mma_commit(leader, &pv_done);
-                if (h + 1 == nh) mma_commit(leader, &o_full);
+                    mma_ts(t_o, t_s + from * 64 + kk * 8, desc_mn(va + kk * 2048, kBlockBytes), id_o, h > 0 || kk > 0);
+                if ((h & 1) || h + 1 == nh) mma_commit(&empty[st]);
+                mma_commit(&pv_done);
+                if (h + 1 == nh) mma_commit(&o_full);
                 if (h + 2 < nh) scores(h + 2, nh);              // over p(h), which the product before has read by then
             }
             n += (nh + 1) / 2 * 2;
@@ -225,7 +224,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             ++w;
         }
         if (!ok) {                                              // products in flight end before the memory is freed
-            mma_commit(leader, &idle);
+            mma_commit(&idle);
             bar_drain(&idle, 0);
         }
         __syncwarp();

@@ -219,7 +219,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         // half of the pair before, ds of the first half, p of the second.  With 128 there is no room for that: dq takes the
         // columns of dp, so that dp of the next pair waits for dq in any case, and all warps take the whole pair together (8192
         // tokens, 16 heads on 4, causal: 1.40 ms in halves).
-        const uint32_t leader = elect_leader();
         constexpr uint32_t id_kk = mma_desc<T>(128, 128 / NE, false, false);    // s, dp of a group
         constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);           // dv, dk: right operand across its rows
         constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);            // dq: both across their rows
@@ -231,9 +230,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
                 const uint32_t off = (kk / 4) * kBlockBytes + (kk % 4) * 32;
-                mma_ss(leader, to + e * 64, desc_k(left + off), desc_k(right + e * (kBlockBytes / 2) + off), id_kk, kk > 0);
+                mma_ss(to + e * 64, desc_k(left + off), desc_k(right + e * (kBlockBytes / 2) + off), id_kk, kk > 0);
             }
-            mma_commit(leader, done);
+            mma_commit(done);
         };
         auto q_at = [&](uint32_t x) { return base + L::Q + (x % NQ) * L::TILE; };
         auto g_at = [&](uint32_t x) { return base + L::G + (x % NG) * L::TILE; };
@@ -243,13 +242,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         auto add_dv = [&](uint32_t x, uint32_t e, bool acc) {
 #pragma unroll
             for (int kk = 0; kk < 8 / NE; ++kk)                 // p of queries 32 g .. 32 g + 31 in columns 32 g .. 32 g + 15
-                mma_ts(leader, t_dv, t_s + e * 64 + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(g_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
+                mma_ts(t_dv, t_s + e * 64 + (kk / 2) * 32 + (kk % 2) * 8, desc_mn(g_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
                        acc || kk > 0);
         };
         auto add_dk = [&](uint32_t x, uint32_t e, bool acc) {
 #pragma unroll
             for (int kk = 0; kk < 8 / NE; ++kk)
-                mma_ss(leader, t_dk, desc_k(ds_at(x) + (e + kk / 4) * kBlockBytes + kk % 4 * 32), desc_mn(q_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
+                mma_ss(t_dk, desc_k(ds_at(x) + (e + kk / 4) * kBlockBytes + kk % 4 * 32), desc_mn(q_at(x) + e * (kBlockBytes / 2) + kk * 2048, kBlockBytes), id_kv,
                        acc || kk > 0);
         };
         // last group of pair x: its ds is there, so dk and dq can be completed; `more`: another pair of this key tile follows
@@ -261,11 +260,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (kOwnDq && more) dprobs(x + 1, 1);
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)
-                mma_ss(leader, t_dq, desc_mn(ds_at(x) + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
-            mma_commit(leader, &s.dq_full);
+                mma_ss(t_dq, desc_mn(ds_at(x) + kk * 2048, kBlockBytes), desc_mn(base + L::K + kk * 2048, kBlockBytes), id_dq, kk > 0);
+            mma_commit(&s.dq_full);
             add_dk(x, NE - 1, acc);
-            mma_commit(leader, &s.q_empty[x % NQ]);
-            mma_commit(leader, &s.ds_free[x % ND]);
+            mma_commit(&s.q_empty[x % NQ]);
+            mma_commit(&s.ds_free[x % ND]);
             if (!kOwnDq && more) {                              // dp of the next pair comes where dq is
                 ok = warp_wait(&s.g_full[(x + 1) % NG], ((x + 1) / NG) & 1, g) && warp_wait(&s.dq_free, x & 1, g);
                 if (!ok) return;
@@ -292,7 +291,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 if (!ok) break;
                 tc_fence_after();
                 add_dv(n, 0, t > 0);
-                if (NE == 1) mma_commit(leader, &s.g_empty[n % NG]);
+                if (NE == 1) mma_commit(&s.g_empty[n % NG]);
                 if (more) {
                     ok = warp_wait(&s.q_full[(n + 1) % NQ], ((n + 1) / NQ) & 1, g);
                     if (!ok) break;
@@ -313,16 +312,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     if (!ok) break;
                     tc_fence_after();
                     add_dv(n, 1, true);
-                    mma_commit(leader, &s.g_empty[n % NG]);
+                    mma_commit(&s.g_empty[n % NG]);
                     if (more) scores(n + 1, 1);
                 }
             }
             if (NE == 2) finish(n - 1, false, true);
-            if (ok) mma_commit(leader, &s.acc_full);
+            if (ok) mma_commit(&s.acc_full);
             ++w;
         }
         if (!ok) {                                              // products in flight end before the memory is freed
-            mma_commit(leader, &s.idle);
+            mma_commit(&s.idle);
             bar_drain(&s.idle, 0);
         }
         __syncwarp();

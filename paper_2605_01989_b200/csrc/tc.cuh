@@ -209,31 +209,26 @@ template <typename T> __host__ __device__ constexpr uint32_t mma_desc(int m, int
     return 1u << 4 | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7 | 1u << 10) : 0u) | (a_mn ? 1u << 15 : 0u) |
            (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
-// Products are issued by one lane of a warp that runs together: `leader` is 1 in that lane.  A branch on the lane instead
-// would make every operand a per-lane value and each product cost about 95 cycles to issue.
-__device__ __forceinline__ uint32_t elect_leader()
+// Products are issued by one lane of a warp that runs together, elected in the same statement (the same lane every time, so a
+// commit covers the products before it).  Operands, loops and branches around them have to be visibly uniform (`uniform`):
+// with a branch on the lane number each product cost about 95 cycles to issue.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
 {
-    uint32_t r;
-    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
-{
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
                  : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
 {
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
                  : "memory");
 }
-// The barrier completes a phase when every product issued before by this lane is done.
-__device__ __forceinline__ void mma_commit(uint32_t leader, uint64_t* bar)
+// The barrier completes a phase when every product issued before by this warp is done.
+__device__ __forceinline__ void mma_commit(uint64_t* bar)
 {
-    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n"
-                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_addr(bar)), "r"(leader)
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_addr(bar))
                  : "memory");
 }
 
