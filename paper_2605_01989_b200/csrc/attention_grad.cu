@@ -89,20 +89,20 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
 // ---- main ------------------------------------------------------------------------------------------------------------
 template <int DP> struct GradSmem {
     static constexpr int NS = DP / 64, TILE = NS * (int)kBlockBytes;
-    // stages of q (with its row values), of dout, of ds; dq leaves in pieces of 32 queries x 16 columns in fp32, four
-    // at a time for each of its warps
-    static constexpr int NQ = DP == 64 ? 3 : 2, NG = DP == 64 ? 2 : 1, ND = DP == 64 ? 2 : 1;
+    // stages of q (with its row values), of dout, of ds; dq leaves in pieces of 32 queries x 16 columns in fp32, CH
+    // at a time for each of its warps.  (With three stages of q the products waited for it in every pair.)
+    static constexpr int NQ = DP == 64 ? 4 : 2, NG = DP == 64 ? 2 : 1, ND = DP == 64 ? 2 : 1;
     static constexpr int K = 0, V = TILE, Q = 2 * TILE, G = Q + NQ * TILE, DS = G + NG * TILE, STAGE = DS + ND * 2 * (int)kBlockBytes;
-    static constexpr int ROWS = STAGE + 32768, BARS = ROWS + NQ * 1024, kBytes = BARS + 256;
+    static constexpr int CH = DP == 64 ? 2 : 4, ROWS = STAGE + 4 * CH * 2048, BARS = ROWS + NQ * 1024, kBytes = BARS + 320;
 };
 static_assert(GradSmem<64>::kBytes <= 232448 && GradSmem<128>::kBytes <= 232448, "");
 
 struct GradBars {
-    uint64_t kv_full, q_full[3], q_empty[3], g_full[2], g_empty[2], cut_full;
+    uint64_t kv_full, q_full[4], q_empty[4], g_full[4], g_empty[4], cut_full;
     uint64_t s_full[2], p_ready[2], dp_full[2], ds_ready[2], ds_free[2], dq_full, dq_free, acc_full, acc_free, idle;
     uint32_t tmem_slot, dead;
 };
-static_assert(sizeof(GradBars) <= 256, "");
+static_assert(sizeof(GradBars) <= 320, "");
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant__ GradArgs a)
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
     } else if (warp >= kDqWarp) {                               // ---- dq: tensor memory -> this share's buffer
         // Each warp takes 32 queries.  Pieces go through shared memory and are added by the memory system: adding from
         // registers kept the load/store unit busy and stalled every other warp behind it.
-        constexpr int CH = 4, PER = DP / 16;
+        constexpr int CH = L::CH, PER = DP / 16;
         const uint32_t quarter = warp & 3, lane_base = quarter << 21;
         float4* stage = reinterpret_cast<float4*>(smem + L::STAGE + quarter * CH * 2048);
         uint32_t n = 0;
