@@ -23,15 +23,16 @@ template <typename I>
 __device__ __forceinline__ int64_t token_at(const I* tokens, uint64_t i) { return (int64_t)tokens[i]; }
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
-// A row is `gpr` groups of G elements; consecutive threads take consecutive groups, and kLookUnroll groups a thread with
-// all table loads issued before the first store.
-constexpr int kLookUnroll = 4;
+// A row is `gpr` groups of G elements; consecutive threads take consecutive groups, and kLookUnrollOf groups (64 bytes)
+// a thread with all table loads issued before the first store.
+template <typename TI> constexpr int kLookUnrollOf = sizeof(TI) == 4 ? 2 : 4;
 
 template <typename I, typename TI, typename TO, int G>
 __global__ void __launch_bounds__(kEmbedThreads)
 k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restrict__ tokens, uint64_t n, int64_t padding,
         float scale, TO* __restrict__ out, int64_t os, FastDiv gpr, unsigned long long* bad)
 {
+    constexpr int kLookUnroll = kLookUnrollOf<TI>;
     // n * groups < 2^32 a launch (the host cuts longer lists): the division by the row's groups is a multiply and a shift
     const uint32_t items = (uint32_t)n * gpr.d, base = blockIdx.x * (kEmbedThreads * kLookUnroll) + threadIdx.x;
     uint32_t row[kLookUnroll];
@@ -264,6 +265,18 @@ k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys,
 constexpr uint32_t kTile = 32;
 constexpr int kGradWarps = 8;
 
+// G elements as they lie in memory: rows in flight are kept this way, half the registers of their fp32 values.
+template <typename T, int G> struct RawGroup {
+    Vec8<T> v;
+    __device__ __forceinline__ void load(const T* p) { v.load(p); }
+    __device__ __forceinline__ void get(float* x) const { v.get(x); }
+};
+template <typename T> struct RawGroup<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void get(float* x) const { x[0] = to_f32(v); }
+};
+
 template <typename T, int G>
 __device__ __forceinline__ void load_group(const T* p, float* x)
 {
@@ -351,12 +364,12 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
     for (int i = 0; i < G; ++i) acc[i] = 0.0f;
     uint32_t cur = __shfl_sync(0xFFFFFFFFu, key, 0);
     bool began = cur != prev;                                           // the current run begins inside this tile
-    float x[kAhead][G];
+    RawGroup<TI, G> x[kAhead];
     for (uint32_t r0 = 0; r0 < live; r0 += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const uint32_t a = __shfl_sync(0xFFFFFFFFu, at, (r0 + u) & 31);
-            if (in && r0 + u < live) load_group<TI, G>(dout + (int64_t)a * ds + c0, x[u]);
+            if (in && r0 + u < live) x[u].load(dout + (int64_t)a * ds + c0);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -377,8 +390,12 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
                     cur = k;
                     began = true;
                 }
+                if (in) {
+                    float y[G];
+                    x[u].get(y);
 #pragma unroll
-                for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], x[u][i]);
+                    for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], y[i]);
+                }
             }
         }
     }
@@ -589,9 +606,10 @@ extern "C" int dblp_embed(const void* table, int64_t table_stride, uint64_t rows
             using TO = decltype(to);
             auto launch = [&](auto id) -> int {
                 using I = decltype(id);
+                constexpr uint32_t per_block = kEmbedThreads * kLookUnrollOf<TI>;
                 for (uint64_t first = 0; first < n; first += most) {
                     const uint64_t m = n - first < most ? n - first : most;
-                    const unsigned grid = (unsigned)((m * gpr + kEmbedThreads * kLookUnroll - 1) / (kEmbedThreads * kLookUnroll));
+                    const unsigned grid = (unsigned)((m * gpr + per_block - 1) / per_block);
                     const I* tk = (const I*)tokens + first;
                     TO* o = (TO*)out + (int64_t)first * out_stride;
                     if (vec) k_embed<I, TI, TO, 8><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
