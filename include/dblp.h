@@ -421,7 +421,7 @@ int dblp_embed(const void* table, int64_t table_stride, uint64_t rows, uint32_t 
  *     dtable[v, :] = round(scale * sum of dout[i, :] over the i with tokens[i] = v, ascending [+ dtable[v, :]])
  * The sum is in fp32: the occurrences of all tokens, sorted by (token, i), are cut into tiles of 32; inside a tile a
  * row's terms are added one after the other, and a row that spans several tiles adds their partial sums in tile order
- * (from 65 partial sums on in 8 contiguous parts, joined in order).  Rows that no token names are written as zero.
+ * (from 17 partial sums on in 8 contiguous parts, joined in order).  Rows that no token names are written as zero.
  * flags: DBLP_ACCUMULATE adds to what dtable holds (rows that no token names are not touched), e.g. the output layer's
  * gradient of a tied table.  Padding and bad tokens contribute nothing (bad_tokens as above).
  * ws: dblp_embed_grad_workspace_bytes() bytes, 256-byte aligned, contents need not be preserved.  n < 2^31, rows < 2^31. */

@@ -314,7 +314,7 @@ __device__ __forceinline__ void finish_row(T* p, float* acc, float scale, bool a
     store_group<T, G>(p, acc);
 }
 
-// Warps from `sum_warps` on write zeros to the rows that no token names, kZeroRows rows each.
+// A warp's share of the rows that no token names: zeros.
 constexpr uint32_t kZeroRows = 4;
 
 template <typename TO, int G>
@@ -337,15 +337,18 @@ template <typename TI, typename TO, int G>
 __global__ void __launch_bounds__(kGradWarps * 32)
 k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
              uint32_t n, uint32_t rows, uint32_t width, uint32_t slabs, float scale, TO* __restrict__ dtable, int64_t ts,
-             uint32_t accumulate, float* __restrict__ part, const uint32_t* __restrict__ seen, uint64_t sum_warps)
+             uint32_t accumulate, float* __restrict__ part, const uint32_t* __restrict__ seen, uint32_t sum_blocks)
 {
     constexpr int kAhead = G == 8 ? (sizeof(TI) == 2 ? 8 : 4) : 16;     // rows in flight a lane
     after_start();
     wait_before();
     const uint32_t lane = threadIdx.x & 31;
-    const uint64_t w = (uint64_t)blockIdx.x * kGradWarps + (threadIdx.x >> 5);
-    if (w >= sum_warps) {
-        zero_rows<TO, G>((uint32_t)(w - sum_warps) * kZeroRows, seen, rows, width, dtable, ts);
+    // blocks that sum and blocks that write zeros take turns while there are both, so that reading and writing overlap
+    const uint32_t both = min(sum_blocks, gridDim.x - sum_blocks);
+    const bool sums = blockIdx.x < 2 * both ? blockIdx.x % 2 == 0 : sum_blocks > both;
+    const uint64_t w = (uint64_t)(blockIdx.x < 2 * both ? blockIdx.x / 2 : blockIdx.x - both) * kGradWarps + (threadIdx.x >> 5);
+    if (!sums) {
+        if (w < (rows + kZeroRows - 1) / kZeroRows) zero_rows<TO, G>((uint32_t)w * kZeroRows, seen, rows, width, dtable, ts);
         return;
     }
     const uint32_t tile = (uint32_t)(w / slabs), slab = (uint32_t)(w - (uint64_t)tile * slabs);
@@ -413,9 +416,9 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
 // Joining a run that crosses tiles: slot 1 of the tile in which it begins, then slot 0 of each tile that continues it, in
 // tile order.  A tile continues a run when its first key is the key before it.
 // Short runs (up to kLongRun - 1 partial sums): one warp a (tile, slab), which ends at once unless a run begins in its tile
-// and goes on.  Longer ones: a run of kLongRun or more sums continues over at least one tile whose number is a multiple of 64;
+// and goes on.  Longer ones: a run of kLongRun or more sums continues over at least one tile whose number is a multiple of 16;
 // the first such tile names the run, and a block adds it in 8 contiguous parts by 8 warps, joined in order.
-constexpr uint32_t kLongRun = 65;
+constexpr uint32_t kLongRun = 17;
 
 __device__ __forceinline__ bool continues(const uint32_t* __restrict__ keys, uint32_t tile, uint32_t tiles, uint32_t key)
 {
@@ -470,13 +473,11 @@ k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32
         finish_row<TO, G>(dtable + (int64_t)key * ts + c0, acc, scale, accumulate);
         return;
     }
-    const uint32_t at = blockIdx.x - short_blocks, u = (at / slabs + 1) * 64, slab = at % slabs, c0 = (slab * 32 + lane) * G;
+    const uint32_t at = blockIdx.x - short_blocks, u = (at / slabs + 1) * 16, slab = at % slabs, c0 = (slab * 32 + lane) * G;
     const uint32_t key = keys[(uint64_t)u * kTile];
-    if (key >= rows || !continues(keys, u, tiles, key) || continues(keys, u - 64, tiles, key)) return;
-    // u - 64 does not continue the run, so it begins in one of the 64 tiles before u
-    const uint32_t b0 = __ballot_sync(0xFFFFFFFFu, continues(keys, u - 1 - lane, tiles, key));
-    const uint32_t b1 = __ballot_sync(0xFFFFFFFFu, continues(keys, u - 33 - lane, tiles, key));
-    const uint32_t back = b0 != 0xFFFFFFFFu ? __ffs(~b0) - 1 : 32 + __ffs(~b1) - 1;
+    if (key >= rows || !continues(keys, u, tiles, key) || continues(keys, u - 16, tiles, key)) return;
+    // u - 16 does not continue the run, so it begins in one of the 16 tiles before u
+    const uint32_t back = __ffs(~__ballot_sync(0xFFFFFFFFu, lane < 16 && continues(keys, u - 1 - lane, tiles, key))) - 1;
     const uint32_t tile = u - back - 1, terms = 1 + back + continued(keys, u, tiles, key);
     if (terms < kLongRun) return;
     const uint32_t per = (terms + kGradWarps - 1) / kGradWarps, lo = min(terms, warp * per), hi = min(terms, lo + per);
@@ -552,13 +553,12 @@ static int launch_sums(const TI* dout, int64_t ds, const uint32_t* keys, const u
 {
     const uint32_t slabs = (width + 32 * G - 1) / (32 * G), tiles = (n + kTile - 1) / kTile;
     const uint64_t sums = (uint64_t)tiles * slabs, zeros = accumulate ? 0 : (rows + kZeroRows - 1) / kZeroRows;
-    const uint64_t sum_warps = (sums + kGradWarps - 1) / kGradWarps * kGradWarps;      // whole blocks of either kind
-    const uint64_t grid = (sum_warps + zeros + kGradWarps - 1) / kGradWarps;
+    const uint64_t sum_blocks = (sums + kGradWarps - 1) / kGradWarps, grid = sum_blocks + (zeros + kGradWarps - 1) / kGradWarps;
     DBLP_REQUIRE(grid < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
     DBLP_NEXT(launch_next(k_grad_tiles<TI, TO, G>, (unsigned)grid, kGradWarps * 32, 0, s, dout, ds, keys, pos, n, rows, width, slabs, scale, dtable,
-                          ts, accumulate, part, seen, sum_warps));
+                          ts, accumulate, part, seen, (uint32_t)sum_blocks));
     if (tiles > 1) {                                                   // a run can cross tiles
-        const uint64_t brief = ((tiles - 1ull) * slabs + kGradWarps - 1) / kGradWarps, lengthy = (uint64_t)((tiles - 1) / 64) * slabs;
+        const uint64_t brief = ((tiles - 1ull) * slabs + kGradWarps - 1) / kGradWarps, lengthy = (uint64_t)((tiles - 1) / 16) * slabs;
         DBLP_REQUIRE(brief + lengthy < (1ull << 31), DBLP_ECAPACITY, "embed_grad: too many tokens times columns");
         DBLP_NEXT(launch_next(k_grad_join<TO, G>, (unsigned)(brief + lengthy), kGradWarps * 32, 0, s, keys, n, rows, width, slabs, scale, dtable, ts,
                               accumulate, part, (uint32_t)brief));

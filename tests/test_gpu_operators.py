@@ -513,8 +513,8 @@ def test_no_wait_ran_out():
     assert dblp.dblp_wait_timeouts() == 0
 
 
-@pytest.mark.parametrize("first", [0, 1, 31, 32, 33, 63 * 32, 64 * 32, 64 * 32 + 1, 64 * 32 - 1])
-@pytest.mark.parametrize("length", [1, 32, 33, 63 * 32, 64 * 32, 64 * 32 + 40, 65 * 32, 130 * 32, 200 * 32 + 5])
+@pytest.mark.parametrize("first", [0, 1, 31, 32, 33, 15 * 32, 16 * 32 - 1, 16 * 32 + 1, 63 * 32, 64 * 32, 64 * 32 + 1, 64 * 32 - 1])
+@pytest.mark.parametrize("length", [1, 32, 33, 15 * 32, 16 * 32, 16 * 32 + 40, 17 * 32, 63 * 32, 64 * 32, 64 * 32 + 40, 65 * 32, 130 * 32, 200 * 32 + 5])
 def test_embed_grad_runs_of_every_length_at_every_place(first, length):
     """One long run between two others, beginning and ending around tile boundaries of the sorted list."""
     rows, width = 5, 16
