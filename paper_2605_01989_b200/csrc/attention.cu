@@ -1,8 +1,6 @@
 // dblp_attention, dblp_attention_grad: argument checks, tensor maps and the entry points.
 #include <math.h>
 
-#include <mutex>
-
 #include "attention.cuh"
 
 namespace dblp {

@@ -59,6 +59,12 @@ bool few_rows(const dblp_attention_t* a);
 size_t rows_space(const dblp_attention_t* a);
 int attention_rows(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                    const dblp_heads_t* out, float* lse, void* ws, cudaStream_t s);
+// dblp_attention_grad for few queries a key head (attention_rows.cu)
+bool few_grad_rows(const dblp_attention_t* a);
+size_t grad_rows_space(const dblp_attention_t* a);
+int attention_grad_rows(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
+                        const dblp_heads_t* out, const dblp_heads_t* dout, const float* lse, const dblp_heads_t* dq,
+                        const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, cudaStream_t s);
 int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                       const dblp_heads_t* out, float* lse, void* ws, cudaStream_t s);
 size_t attention_forward_space(const dblp_attention_t* a);

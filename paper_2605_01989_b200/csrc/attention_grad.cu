@@ -12,11 +12,16 @@
 //                 is done and are written once; shared key heads sum in the same accumulator.
 //   k_grad_dq     adds the shares' dq, scales and rounds; k_grad_dkv does the same for key heads whose query heads were
 //                 split into groups.
-// Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk, one thread per element: no
-// two blocks add to one place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
+// Order.  A block adds the dq of its key tiles to its own fp32 buffer, in the order of its walk: no two blocks add to one
+// place, so the sums do not depend on timing.  The number of shares R is chosen so that the shares
 // fill the machine; each costs a buffer of q's size in fp32.
 //   warps         0-15 p and ds, each thread one key and 32 queries, with head_dim up to 64 in two groups half a step apart;
 //                 16-19 dq to memory, 20 TMA, 21 products.
+// Bound.  A pair of 128 x 128 tiles with head_dim 64 costs 1280 cycles of products, 1024 of exponentials and, for its 32 KB of
+// dq at the 16 bytes a cycle and SM that the L2 adds in fp32, about 2000; the chain between them makes it about 3600.  With
+// 128, dq has no columns of its own and dp of the next pair waits until it has been read.
+//   measured      8 x 1024 tokens, 25 heads of 64, causal: 197 us (341 TFLOP/s), of which rows 16 and dq 25; 8192 tokens, 16 heads
+//                 of 128 on 4, causal: 1.05 to 1.1 ms (625 to 658 TFLOP/s); 8192 x 8192, 16 heads of 64: 1.2 ms (570 TFLOP/s).
 #include <math.h>
 
 #include "attention.cuh"
@@ -572,7 +577,7 @@ struct GradCut {
 };
 static GradCut cut_of(const dblp_attention_t* a)
 {
-    const uint64_t bk = (uint64_t)a->batch * a->kv_heads, kt = (a->k_tokens + 127) / 128, qt = (a->q_tokens + 127) / 128, sms = 148;
+    const uint64_t bk = (uint64_t)a->batch * a->kv_heads, kt = (a->k_tokens + 127) / 128, qt = (a->q_tokens + 127) / 128, sms = kSms;
     const uint32_t rep = a->q_heads / a->kv_heads;
     const double dp = a->head_dim <= 64 ? 64 : 128, pair_us = a->head_dim <= 64 ? 2.2 : 3.5, half = a->flags & DBLP_ATTENTION_CAUSAL ? 0.5 : 1.0;
     const double q_us = (double)a->batch * a->q_heads * qt * 128 * dp * 4 / 4e6, k_us = 2.0 * bk * kt * 128 * dp * 4 / 4e6;
@@ -605,7 +610,7 @@ struct GradSpaceA {
     }
 };
 
-size_t attention_backward_space(const dblp_attention_t* a) { return GradSpaceA(a).bytes; }
+size_t attention_backward_space(const dblp_attention_t* a) { return few_grad_rows(a) ? grad_rows_space(a) : GradSpaceA(a).bytes; }
 
 template <typename T, int DP>
 static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* lse, Heads dq, cudaStream_t s)
@@ -632,6 +637,7 @@ int attention_backward(const dblp_attention_t* a, const dblp_heads_t* q, const d
                        const dblp_heads_t* out, const dblp_heads_t* dout, const float* lse, const dblp_heads_t* dq,
                        const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, cudaStream_t s)
 {
+    if (few_grad_rows(a)) return attention_grad_rows(a, q, k, v, out, dout, lse, dq, dk, dv, ws, s);
     GradArgs r{};
     int rc = DBLP_OK;
     if (a->q_tokens) rc = make_source(&r.q, a, q, a->q_tokens, a->q_heads);

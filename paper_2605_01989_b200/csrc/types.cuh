@@ -9,6 +9,8 @@
 
 namespace dblp {
 
+constexpr unsigned kSms = 148;                // streaming multiprocessors of the device this library is built for
+
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }

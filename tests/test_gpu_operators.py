@@ -376,6 +376,21 @@ SHAPES = [
 ]
 
 
+FEW = [
+    (1, 1, 200, 4, 1, 40, F16, True, None, "plain"),
+    (2, 2, 300, 4, 2, 64, BF16, True, None, "heads_first"),
+    (1, 4, 1000, 2, 2, 96, BF16, True, None, "wide"),
+    (1, 4, 3, 2, 2, 64, BF16, True, None, "plain"),             # the first query sees nothing
+    (3, 2, 150, 2, 1, 128, BF16, False, ([2, 0, 1], [150, 60, 0]), "plain"),
+    (2, 3, 9000, 1, 1, 8, F16, True, ([3, 2], [9000, 4097]), "tokens_first"),
+    (1, 1, 5000, 8, 1, 128, BF16, True, None, "plain"),
+    (1, 8, 600, 1, 1, 64, BF16, True, None, "plain"),
+    (1, 9, 600, 1, 1, 64, BF16, True, None, "plain"),
+    (33, 1, 70, 25, 25, 64, BF16, True, None, "plain"),
+]
+SHAPES += FEW
+
+
 def lengths(lens):
     return (None, None) if lens is None else tuple(torch.tensor(x, dtype=torch.int32, device=DEV) for x in lens)
 
