@@ -1,7 +1,8 @@
 // dblp_dropout, dblp_dropout_grad: out = [u(i) >= t] * x * 65536 / (65536 - t) [+ residual], u(i) = 16 bits of a Philox
 // draw that eight consecutive elements share.
 //
-// Bound by HBM: 32768 x 6400 fp32 243 us (6.9 TB/s) in bursts, 278 us under sustained load; 8192 x 1600 bf16 with residual 13.9 us.
+// Bound by HBM: 32768 x 6400 fp32 243 us (6.9 TB/s) in bursts, 266 us (6.3) under sustained load, 295 with two 16-byte
+// accesses in place of one of 32; 8192 x 1600 bf16 with residual 13.9 us.
 // Nothing is kept between forward and backward: the mask costs ten Philox rounds per eight elements (about five
 // instructions an element) instead of a byte or bit each to write and read.
 #include <math.h>

@@ -67,15 +67,30 @@ template <typename T> struct Vec8 {
 };
 template <> struct Vec8<float> {
     float4 a, b;
+    // One 32-byte access where the address allows it (rows of torch tensors do): two of 16 bytes at a stride of 32 touch every
+    // sector twice.
     __device__ __forceinline__ void load(const float* p)
     {
-        a = *reinterpret_cast<const float4*>(p);
-        b = *reinterpret_cast<const float4*>(p + 4);
+        if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+            asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w), "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w)
+                         : "l"(p)
+                         : "memory");
+        } else {
+            a = *reinterpret_cast<const float4*>(p);
+            b = *reinterpret_cast<const float4*>(p + 4);
+        }
     }
     __device__ __forceinline__ void store(float* p) const
     {
-        *reinterpret_cast<float4*>(p) = a;
-        *reinterpret_cast<float4*>(p + 4) = b;
+        if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+            asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w), "f"(b.x),
+                         "f"(b.y), "f"(b.z), "f"(b.w)
+                         : "memory");
+        } else {
+            *reinterpret_cast<float4*>(p) = a;
+            *reinterpret_cast<float4*>(p + 4) = b;
+        }
     }
     __device__ __forceinline__ void get(float* x) const
     {
