@@ -13,8 +13,8 @@
 //      the launch write zeros to the rows that do not occur, so that reading dout and writing the table overlap;
 //   3. k_grad_join: joins the partial sums of crossing runs in tile order.
 // The floor is reading dout once and writing the table once.  Measured: 32768 x 1600 fp32 into 50257 rows 110 us (4.8 TB/s over
-// all), 8192 x 1024 bf16 into 30522 rows 34 us, where the chain of launches is the time; 29 tokens into 30522 x 1600 fp32
-// 30 us (6.5 TB/s).  The lookup: 8192 x 1600 fp32 13.6 us (5.5 TB/s), one token 1.8 us.
+// all), 8192 x 1024 bf16 into 30522 rows 32 us, where the chain of launches is the time; 29 tokens into 30522 x 1600 fp32
+// 30 us (6.5 TB/s).  The lookup: 8192 x 1600 fp32 14 us (5.3 TB/s), one token 1.8 us.
 #include "types.cuh"
 
 namespace dblp {
@@ -25,11 +25,11 @@ template <typename I>
 __device__ __forceinline__ int64_t token_at(const I* tokens, uint64_t i) { return (int64_t)tokens[i]; }
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
-// A row is `gpr` groups of G elements; consecutive threads take consecutive groups, and kLookUnrollOf groups (64 bytes)
+// A row is `gpr` groups of 8 elements; consecutive threads take consecutive groups, and kLookUnrollOf groups (64 bytes)
 // a thread with all table loads issued before the first store.
 template <typename TI> constexpr int kLookUnrollOf = sizeof(TI) == 4 ? 2 : 4;
 
-template <typename I, typename TI, typename TO, int G>
+template <typename I, typename TI, typename TO>
 __global__ void __launch_bounds__(kEmbedThreads)
 k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restrict__ tokens, uint64_t n, int64_t padding,
         float scale, TO* __restrict__ out, int64_t os, FastDiv gpr, unsigned long long* bad)
@@ -47,42 +47,54 @@ k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restr
         grp[u] = it - row[u] * gpr.d;
         tok[u] = it < items ? token_at(tokens, row[u]) : -1;
     }
-    if constexpr (G == 8) {
-        Vec8<TI> v[kLookUnroll];
-        float x[8];
+    Vec8<TI> v[kLookUnroll];
+    float x[8];
 #pragma unroll
-        for (int u = 0; u < kLookUnroll; ++u)
-            if (tok[u] >= 0 && tok[u] < rows && tok[u] != padding) v[u].load(table + tok[u] * ts + grp[u] * 8);
+    for (int u = 0; u < kLookUnroll; ++u)
+        if (tok[u] >= 0 && tok[u] < rows && tok[u] != padding) v[u].load(table + tok[u] * ts + grp[u] * 8);
 #pragma unroll
-        for (int u = 0; u < kLookUnroll; ++u) {
-            if (base + u * kEmbedThreads >= items) break;
-            const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
-            if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
-            Vec8<TO> o;
-            if (live) {
-                v[u].get(x);
+    for (int u = 0; u < kLookUnroll; ++u) {
+        if (base + u * kEmbedThreads >= items) break;
+        const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
+        if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
+        Vec8<TO> o;
+        if (live) {
+            v[u].get(x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], scale);
-            } else {
+            for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], scale);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-            }
-            o.set(x);
-            o.store(out + (int64_t)row[u] * os + grp[u] * 8);
+            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
         }
-    } else {
-        TI v[kLookUnroll];
-#pragma unroll
-        for (int u = 0; u < kLookUnroll; ++u)
-            if (tok[u] >= 0 && tok[u] < rows && tok[u] != padding) v[u] = table[tok[u] * ts + grp[u]];
-#pragma unroll
-        for (int u = 0; u < kLookUnroll; ++u) {
-            if (base + u * kEmbedThreads >= items) break;
-            const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
-            if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
-            out[(int64_t)row[u] * os + grp[u]] = from_f32<TO>(live ? __fmul_rn(to_f32(v[u]), scale) : 0.0f);
-        }
+        o.set(x);
+        o.store(out + (int64_t)row[u] * os + grp[u] * 8);
     }
+}
+
+// Any width, stride and alignment: one warp a row and slab of 256 columns, 8 a lane 32 apart, so that the token and the row's
+// place are worked out once (element by element with a division each: 33 us for 20000 x 769 bf16).
+constexpr int kAnyCols = 8;
+
+template <typename I, typename TI, typename TO>
+__global__ void __launch_bounds__(kEmbedThreads)
+k_embed_any(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restrict__ tokens, uint32_t n, int64_t padding,
+            float scale, TO* __restrict__ out, int64_t os, uint32_t width, FastDiv slabs, unsigned long long* bad)
+{
+    const uint32_t lane = threadIdx.x & 31, w = blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5), row = slabs.div(w), slab = w - row * slabs.d;
+    if (row >= n) return;
+    const int64_t tok = token_at(tokens, row);
+    const bool live = tok >= 0 && tok < rows && tok != padding;
+    if (!live && bad && tok != padding && slab == 0 && lane == 0) atomicAdd(bad, 1ull);
+    const uint32_t c0 = slab * (32 * kAnyCols) + lane;
+    const TI* src = table + (live ? tok : 0) * ts + c0;
+    TO* dst = out + (int64_t)row * os + c0;
+    TI v[kAnyCols];
+#pragma unroll
+    for (int i = 0; i < kAnyCols; ++i)
+        if (live && c0 + 32 * i < width) v[i] = src[32 * i];
+#pragma unroll
+    for (int i = 0; i < kAnyCols; ++i)
+        if (c0 + 32 * i < width) dst[32 * i] = from_f32<TO>(live ? __fmul_rn(to_f32(v[i]), scale) : 0.0f);
 }
 
 // ---- sort ------------------------------------------------------------------------------------------------------------
@@ -262,59 +274,75 @@ k_radix_scatter(const I* __restrict__ tokens, const uint32_t* __restrict__ keys,
 }
 
 // ---- sums ------------------------------------------------------------------------------------------------------------
-// One warp sums one tile of 32 sorted positions over one slab of 32 * G columns.  G = 8 elements a lane (vector loads) or 1
-// (any width, stride and alignment).  part: [tiles][2][width]: slot 0 is the tile's share of a run that began before the
-// tile, slot 1 of a run that begins here and goes on.
+// One warp sums one tile of 32 sorted positions over one slab of 32 * G columns.  G = 8: a lane's columns lie side by side (vector
+// loads); G = 4: they are 32 apart, for any width, stride and alignment.  part: [tiles][2][width]: slot 0 is the tile's share
+// of a run that began before the tile, slot 1 of a run that begins here and goes on.
 constexpr uint32_t kTile = 32;
 constexpr int kGradWarps = 8;
 
-// G elements as they lie in memory: rows in flight are kept this way, half the registers of their fp32 values.
-template <typename T, int G> struct RawGroup {
-    Vec8<T> v;
-    __device__ __forceinline__ void load(const T* p) { v.load(p); }
-    __device__ __forceinline__ void get(float* x) const { v.get(x); }
-};
-template <typename T> struct RawGroup<T, 1> {
-    T v;
-    __device__ __forceinline__ void load(const T* p) { v = *p; }
-    __device__ __forceinline__ void get(float* x) const { x[0] = to_f32(v); }
-};
-
-template <typename T, int G>
-__device__ __forceinline__ void load_group(const T* p, float* x)
+template <int G> __device__ __forceinline__ uint32_t first_column(uint32_t slab, uint32_t lane)
 {
-    if constexpr (G == 8) {
-        Vec8<T> v;
-        v.load(p);
-        v.get(x);
-    } else {
-        x[0] = to_f32(*p);
-    }
+    return G == 8 ? (slab * 32 + lane) * 8 : slab * (32 * G) + lane;
 }
 
-template <typename T, int G>
-__device__ __forceinline__ void store_group(T* p, const float* x)
-{
-    if constexpr (G == 8) {
-        Vec8<T> v;
+// A lane's elements as they lie in memory: rows in flight are kept this way, half the registers of their fp32 values.  `left`:
+// columns from the first one to the row's end.
+template <typename T, int G> struct RawGroup {
+    T v[G];
+    __device__ __forceinline__ void load(const T* p, uint32_t left)
+    {
+#pragma unroll
+        for (int i = 0; i < G; ++i) v[i] = 32u * i < left ? p[32 * i] : T();
+    }
+    __device__ __forceinline__ void get(float* x) const
+    {
+#pragma unroll
+        for (int i = 0; i < G; ++i) x[i] = to_f32(v[i]);
+    }
+    __device__ __forceinline__ void put(const float* x, T* p, uint32_t left) const
+    {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (32u * i < left) p[32 * i] = from_f32<T>(x[i]);
+    }
+};
+template <typename T> struct RawGroup<T, 8> {
+    Vec8<T> v;
+    __device__ __forceinline__ void load(const T* p, uint32_t) { v.load(p); }
+    __device__ __forceinline__ void get(float* x) const { v.get(x); }
+    __device__ __forceinline__ void put(const float* x, T* p, uint32_t)
+    {
         v.set(x);
         v.store(p);
-    } else {
-        *p = from_f32<T>(x[0]);
     }
+};
+
+template <typename T, int G>
+__device__ __forceinline__ void load_group(const T* p, uint32_t left, float* x)
+{
+    RawGroup<T, G> v;
+    v.load(p, left);
+    v.get(x);
 }
 
 template <typename T, int G>
-__device__ __forceinline__ void finish_row(T* p, float* acc, float scale, bool accumulate)
+__device__ __forceinline__ void store_group(T* p, uint32_t left, const float* x)
+{
+    RawGroup<T, G> v;
+    v.put(x, p, left);
+}
+
+template <typename T, int G>
+__device__ __forceinline__ void finish_row(T* p, uint32_t left, float* acc, float scale, bool accumulate)
 {
     float old[G];
-    if (accumulate) load_group<T, G>(p, old);
+    if (accumulate) load_group<T, G>(p, left, old);
 #pragma unroll
     for (int i = 0; i < G; ++i) {
         acc[i] = __fmul_rn(acc[i], scale);
         if (accumulate) acc[i] = __fadd_rn(acc[i], old[i]);
     }
-    store_group<T, G>(p, acc);
+    store_group<T, G>(p, left, acc);
 }
 
 // Zeros to row `row` if no token names it; one row a warp (4 rows a warp: 51 instead of 47 us for 30522 x 1600 fp32 with 29
@@ -339,7 +367,7 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
              uint32_t n, uint32_t rows, uint32_t width, uint32_t slabs, float scale, TO* __restrict__ dtable, int64_t ts,
              uint32_t accumulate, float* __restrict__ part, const uint32_t* __restrict__ seen, uint32_t sum_blocks)
 {
-    constexpr int kAhead = G == 8 ? (sizeof(TI) == 2 ? 8 : 4) : 16;     // rows in flight a lane
+    constexpr int kAhead = G == 8 && sizeof(TI) == 4 ? 4 : 8;     // rows in flight a lane
     after_start();
     wait_before();
     const uint32_t lane = threadIdx.x & 31;
@@ -360,8 +388,8 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
     const uint32_t live = __popc(__ballot_sync(0xFFFFFFFFu, key < rows));      // keys >= rows are at the end
     if (live == 0) return;
 
-    const uint32_t c0 = (slab * 32 + lane) * G;
-    const bool in = c0 < width;
+    const uint32_t c0 = first_column<G>(slab, lane), left = c0 < width ? width - c0 : 0;
+    const bool in = left > 0;
     float acc[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) acc[i] = 0.0f;
@@ -372,7 +400,7 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const uint32_t a = __shfl_sync(0xFFFFFFFFu, at, (r0 + u) & 31);
-            if (in && r0 + u < live) x[u].load(dout + (int64_t)a * ds + c0);
+            if (in && r0 + u < live) x[u].load(dout + (int64_t)a * ds + c0, left);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -382,10 +410,9 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
                 if (k != cur) {                                         // the run of `cur` ended with the row before
                     if (in) {
                         if (began) {
-                            finish_row<TO, G>(dtable + (int64_t)cur * ts + c0, acc, scale, accumulate);
+                            finish_row<TO, G>(dtable + (int64_t)cur * ts + c0, left, acc, scale, accumulate);
                         } else {
-#pragma unroll
-                            for (int i = 0; i < G; ++i) part[((uint64_t)tile * 2) * width + c0 + i] = acc[i];
+                            store_group<float, G>(part + ((uint64_t)tile * 2) * width + c0, left, acc);
                         }
                     }
 #pragma unroll
@@ -405,11 +432,9 @@ k_grad_tiles(const TI* __restrict__ dout, int64_t ds, const uint32_t* __restrict
     if (!in) return;
     const bool goes_on = live == cnt && next == cur;
     if (began && !goes_on) {
-        finish_row<TO, G>(dtable + (int64_t)cur * ts + c0, acc, scale, accumulate);
+        finish_row<TO, G>(dtable + (int64_t)cur * ts + c0, left, acc, scale, accumulate);
     } else {
-        float* q = part + ((uint64_t)tile * 2 + (began ? 1 : 0)) * width + c0;
-#pragma unroll
-        for (int i = 0; i < G; ++i) q[i] = acc[i];
+        store_group<float, G>(part + ((uint64_t)tile * 2 + (began ? 1 : 0)) * width + c0, left, acc);
     }
 }
 
@@ -443,7 +468,7 @@ __device__ __forceinline__ void add_terms(const float* __restrict__ part, uint32
 #pragma unroll 8
     for (uint32_t m = lo; m < hi; ++m) {
         float x[G];
-        load_group<float, G>(part + ((uint64_t)(tile + m) * 2 + (m == 0 ? 1 : 0)) * width + c0, x);
+        load_group<float, G>(part + ((uint64_t)(tile + m) * 2 + (m == 0 ? 1 : 0)) * width + c0, width - c0, x);
 #pragma unroll
         for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], x[i]);
     }
@@ -462,7 +487,7 @@ k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32
     for (int i = 0; i < G; ++i) acc[i] = 0.0f;
     if (blockIdx.x < short_blocks) {
         const uint64_t w = (uint64_t)blockIdx.x * kGradWarps + warp;
-        const uint32_t tile = (uint32_t)(w / slabs), slab = (uint32_t)(w - (uint64_t)tile * slabs), c0 = (slab * 32 + lane) * G;
+        const uint32_t tile = (uint32_t)(w / slabs), slab = (uint32_t)(w - (uint64_t)tile * slabs), c0 = first_column<G>(slab, lane);
         if (tile + 1 >= tiles) return;                                  // nothing goes on from the last tile
         const uint64_t end = (uint64_t)(tile + 1) * kTile;
         const uint32_t key = keys[end - 1];
@@ -470,10 +495,10 @@ k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32
         const uint32_t terms = 1 + continued(keys, tile + 1, tiles, key);
         if (terms >= kLongRun || c0 >= width) return;
         add_terms<G>(part, tile, 0, terms, width, c0, acc);
-        finish_row<TO, G>(dtable + (int64_t)key * ts + c0, acc, scale, accumulate);
+        finish_row<TO, G>(dtable + (int64_t)key * ts + c0, width - c0, acc, scale, accumulate);
         return;
     }
-    const uint32_t at = blockIdx.x - short_blocks, u = (at / slabs + 1) * 16, slab = at % slabs, c0 = (slab * 32 + lane) * G;
+    const uint32_t at = blockIdx.x - short_blocks, u = (at / slabs + 1) * 16, slab = at % slabs, c0 = first_column<G>(slab, lane);
     const uint32_t key = keys[(uint64_t)u * kTile];
     if (key >= rows || !continues(keys, u, tiles, key) || continues(keys, u - 16, tiles, key)) return;
     // u - 16 does not continue the run, so it begins in one of the 16 tiles before u
@@ -489,7 +514,7 @@ k_grad_join(const uint32_t* __restrict__ keys, uint32_t n, uint32_t rows, uint32
     for (int p = 1; p < kGradWarps; ++p)
 #pragma unroll
         for (int i = 0; i < G; ++i) acc[i] = __fadd_rn(acc[i], s_part[p][lane * G + i]);
-    finish_row<TO, G>(dtable + (int64_t)key * ts + c0, acc, scale, accumulate);
+    finish_row<TO, G>(dtable + (int64_t)key * ts + c0, width - c0, acc, scale, accumulate);
 }
 
 // Places in the workspace, each on a 256-byte boundary.
@@ -598,24 +623,26 @@ extern "C" int dblp_embed(const void* table, int64_t table_stride, uint64_t rows
     const int tb = element_bytes(table_dtype), ob = element_bytes(out_dtype);
     DBLP_REQUIRE((uintptr_t)table % tb == 0 && (uintptr_t)out % ob == 0, DBLP_EALIGN, "embed: a pointer is not aligned to its type");
     const bool vec = width % 8 == 0 && vector_rows(table, table_stride, rows, tb) && vector_rows(out, out_stride, n, ob);
-    const uint32_t gpr = vec ? width / 8 : width;
-    const uint64_t most = 0xFFFF0000u / gpr;                            // tokens a launch: its items fit in 32 bits
+    // groups of 8 columns, a thread each, or slabs, a warp each; tokens a launch: their items fit in 32 bits
+    const uint32_t per_row = vec ? width / 8 : (width + 32 * kAnyCols - 1) / (32 * kAnyCols);
+    const uint64_t most = 0xFFFF0000u / per_row;
     return with_type(table_dtype, [&](auto ti) -> int {
         return with_type(out_dtype, [&](auto to) -> int {
             using TI = decltype(ti);
             using TO = decltype(to);
             auto launch = [&](auto id) -> int {
                 using I = decltype(id);
-                constexpr uint32_t per_block = kEmbedThreads * kLookUnrollOf<TI>;
+                const uint32_t per_block = vec ? kEmbedThreads * kLookUnrollOf<TI> : kEmbedThreads / 32;
                 for (uint64_t first = 0; first < n; first += most) {
                     const uint64_t m = n - first < most ? n - first : most;
-                    const unsigned grid = (unsigned)((m * gpr + per_block - 1) / per_block);
+                    const unsigned grid = (unsigned)((m * per_row + per_block - 1) / per_block);
                     const I* tk = (const I*)tokens + first;
                     TO* o = (TO*)out + (int64_t)first * out_stride;
-                    if (vec) k_embed<I, TI, TO, 8><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
-                        (const TI*)table, table_stride, (int64_t)rows, tk, m, padding, scale, o, out_stride, FastDiv(gpr), (unsigned long long*)bad_tokens);
-                    else k_embed<I, TI, TO, 1><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
-                        (const TI*)table, table_stride, (int64_t)rows, tk, m, padding, scale, o, out_stride, FastDiv(gpr), (unsigned long long*)bad_tokens);
+                    if (vec) k_embed<I, TI, TO><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
+                        (const TI*)table, table_stride, (int64_t)rows, tk, m, padding, scale, o, out_stride, FastDiv(per_row), (unsigned long long*)bad_tokens);
+                    else k_embed_any<I, TI, TO><<<grid, kEmbedThreads, 0, (cudaStream_t)stream>>>(
+                        (const TI*)table, table_stride, (int64_t)rows, tk, (uint32_t)m, padding, scale, o, out_stride, width, FastDiv(per_row),
+                        (unsigned long long*)bad_tokens);
                     DBLP_LAUNCHED();
                 }
                 return DBLP_OK;
@@ -671,7 +698,7 @@ extern "C" int dblp_embed_grad(const void* dout, int64_t dout_stride, int dout_d
             using TO = decltype(to);
             return vec ? launch_sums<TI, TO, 8>((const TI*)dout, dout_stride, keys, pos, (uint32_t)n, (uint32_t)rows, width, scale, (TO*)dtable,
                                                 dtable_stride, flags & DBLP_ACCUMULATE, (float*)(w + sp.part), seen, s)
-                       : launch_sums<TI, TO, 1>((const TI*)dout, dout_stride, keys, pos, (uint32_t)n, (uint32_t)rows, width, scale, (TO*)dtable,
+                       : launch_sums<TI, TO, 4>((const TI*)dout, dout_stride, keys, pos, (uint32_t)n, (uint32_t)rows, width, scale, (TO*)dtable,
                                                 dtable_stride, flags & DBLP_ACCUMULATE, (float*)(w + sp.part), seen, s);
         });
     });
