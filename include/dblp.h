@@ -405,6 +405,7 @@ int dblp_round_until_stop(const dblp_plan_t* plan, const dblp_loss_model_t* mode
  * gradient for token models: the embedding table and its gradient, dropout, attention and its gradient.  They need no
  * plan; they run on the current device, whose memory all device pointers are in, allocate nothing, only enqueue work
  * on the given stream, and the order of every floating-point addition is fixed by the arguments, so results repeat bit for bit.
+ * Calls can be captured in a graph; make a call of each kind once on a device before (it looks up symbols and sets limits).
  * dtype arguments are dblp_dtype_t; strides are in elements and may be anything that keeps rows apart (inputs may also
  * repeat: stride 0).  Zero-sized calls return DBLP_OK without touching memory. */
 

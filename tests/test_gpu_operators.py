@@ -524,6 +524,52 @@ def test_gradient_is_the_difference_quotient():
         assert abs((ends[0] - ends[1]) / (2 * eps) - along) <= noise
 
 
+@pytest.mark.parametrize("Sq", [1, 260])
+def test_attention_without_lse_and_without_a_workspace(Sq):
+    q, k, v, g, out, *_ = tensors(1, Sq, 700, 2, 2, 64, BF16)
+    run_attention(q, k, v, out)
+    want = out.clone()
+    need = dblp.dblp_attention_workspace_bytes(q, k)[0]
+    assert (need > 0) == (Sq == 1)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    out.fill_(7.0)
+    dblp.dblp_attention(q, k, v, out, None, ws)
+    assert torch.equal(out, want)
+    if need:
+        with pytest.raises(dblp.DblpError, match="workspace"):
+            dblp.dblp_attention(q, k, v, out)
+
+
+def test_calls_replay_from_a_graph():
+    q, k, v, g, out, dq, dk, dv = tensors(2, 200, 200, 2, 2, 64, BF16)
+    one = torch.empty_like(q[:, :1])
+    lse, lse1 = run_attention(q, k, v, out, causal=True), run_attention(q[:, :1], k, v, one)
+    run_grad(q, k, v, out, g, lse, dq, dk, dv, causal=True)
+    tokens, dout = token_list(9000, 500, "power", 3), randn((9000, 64), F32, 4)
+    table = torch.empty((500, 64), device=DEV)
+    ws = torch.empty(max(dblp.dblp_embed_grad_workspace_bytes(9000, 500, 64), *dblp.dblp_attention_workspace_bytes(q, k, True)), dtype=torch.uint8, device=DEV)
+    ws1 = torch.empty(dblp.dblp_attention_workspace_bytes(q[:, :1], k)[0], dtype=torch.uint8, device=DEV)
+
+    def calls():
+        dblp.dblp_attention(q, k, v, out, lse, ws, causal=True)
+        dblp.dblp_attention_grad(q, k, v, out, g, lse, dq, dk, dv, ws, causal=True)
+        dblp.dblp_embed_grad(dout, tokens, table, ws)
+        dblp.dblp_attention(q[:, :1], k, v, one, lse1, ws1)
+
+    calls()
+    want = [t.clone() for t in (out, lse, dq, dk, dv, table, one, lse1)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for t in (out, lse, dq, dk, dv, table, one, lse1):
+        t.fill_(3.0)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, (out, lse, dq, dk, dv, table, one, lse1)):
+        assert torch.equal(bits(a), bits(b.clone()))
+
+
 def test_no_wait_ran_out():
     assert dblp.dblp_wait_timeouts() == 0
 
