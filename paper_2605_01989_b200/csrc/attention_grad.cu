@@ -20,7 +20,7 @@
 // Bound.  A pair of 128 x 128 tiles with head_dim 64 costs 1280 cycles of products, 1024 of exponentials and, for its 32 KB of
 // dq at the 16 bytes a cycle and SM that the L2 adds in fp32, about 2000; the chain between them makes it about 3600.  With
 // 128, dq has no columns of its own and dp of the next pair waits until it has been read.
-//   measured      8 x 1024 tokens, 25 heads of 64, causal: 197 us (341 TFLOP/s), of which rows 16 and dq 25; 8192 tokens, 16 heads
+//   measured      8 x 1024 tokens, 25 heads of 64, causal: 192 us (349 TFLOP/s), of which rows 15 and dq 23; 8192 tokens, 16 heads
 //                 of 128 on 4, causal: 1.05 to 1.1 ms (625 to 658 TFLOP/s); 8192 x 8192, 16 heads of 64: 1.2 ms (570 TFLOP/s).
 #include <math.h>
 
@@ -57,37 +57,53 @@ __device__ __forceinline__ uint32_t first_query_tile(uint32_t j, uint32_t lq, ui
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
-// A warp takes four rows at a time, eight lanes a row, 16 bytes a load.
+// A block takes one tile of 128 rows, a warp 16 of them: eight lanes a row, 16 bytes a load, four rows a thread with their loads
+// in front (200 heads of 1024 x 64, caches cold: 15.5 us, one row a thread 16.6).
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict__ rows, AttnShape s, uint32_t q_tiles)
 {
+    constexpr int R = 4;
     after_start();
     const uint32_t lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z, lq = length_of(s.q_lens, b, s.Sq), lk = length_of(s.k_lens, b, s.Sk);
-    const uint32_t i = blockIdx.x * 32 + (threadIdx.x >> 5) * 4 + (lane >> 3);
-    const bool live = keys_of(i, lq, lk, s.causal) > 0;
-    float d = 0.0f;
-    if (live) {
-        const T* po = (const T*)o.p + (int64_t)b * o.sb + (int64_t)i * o.st + (int64_t)h * o.sh;
-        const T* pg = (const T*)go.p + (int64_t)b * go.sb + (int64_t)i * go.st + (int64_t)h * go.sh;
-        for (uint32_t c = (lane & 7) * 8; c < s.D; c += 64) {
-            Vec8<T> vo, vg;
-            float x[8], y[8];
-            vo.load(po + c);
-            vg.load(pg + c);
-            vo.get(x);
-            vg.get(y);
+    const uint32_t in_tile = (threadIdx.x >> 5) * (4 * R) + (lane >> 3), i0 = blockIdx.x * 128 + in_tile;
+    const T* po = (const T*)o.p + (int64_t)b * o.sb + (int64_t)i0 * o.st + (int64_t)h * o.sh;
+    const T* pg = (const T*)go.p + (int64_t)b * go.sb + (int64_t)i0 * go.st + (int64_t)h * go.sh;
+    bool live[R];
+    float d[R];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) d += x[t] * y[t];
-        }
+    for (int r = 0; r < R; ++r) {
+        live[r] = keys_of(i0 + 4 * r, lq, lk, s.causal) > 0;
+        d[r] = 0.0f;
     }
+    for (uint32_t c = (lane & 7) * 8; c < s.D; c += 64) {
+        Vec8<T> vo[R], vg[R];
 #pragma unroll
-    for (int t = 4; t; t >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, t);
-    if ((lane & 7) == 0 && i < q_tiles * 128) {
-        float* r = rows + (((uint64_t)b * s.Hq + h) * q_tiles + i / 128) * 256 + i % 128;
-        // rows that see nothing: 2^(s - infinity) = 0
-        r[0] = live ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i] * -1.4426950408889634f : -INFINITY;
-        r[128] = live ? -d : 0.0f;
+        for (int r = 0; r < R; ++r)
+            if (live[r]) {
+                vo[r].load(po + (int64_t)(4 * r) * o.st + c);
+                vg[r].load(pg + (int64_t)(4 * r) * go.st + c);
+            }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (live[r]) {
+                float x[8], y[8];
+                vo[r].get(x);
+                vg[r].get(y);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) d[r] += x[t] * y[t];
+            }
+    }
+    float* dst = rows + (((uint64_t)b * s.Hq + h) * q_tiles + blockIdx.x) * 256 + in_tile;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int t = 4; t; t >>= 1) d[r] += __shfl_xor_sync(0xFFFFFFFFu, d[r], t);
+        if ((lane & 7) == 0) {
+            // rows that see nothing: 2^(s - infinity) = 0
+            dst[4 * r] = live[r] ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i0 + 4 * r] * -1.4426950408889634f : -INFINITY;
+            dst[128 + 4 * r] = live[r] ? -d[r] : 0.0f;
+        }
     }
 }
 
@@ -514,7 +530,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 }
 
 // ---- dq --------------------------------------------------------------------------------------------------------------
-// Thread: one query, 8 of its columns at a time.  Share r has a part of query tile i iff its first key tile, r, meets it.
+// Thread: one query, 32 of its columns at a time (200 heads of 1024 x 64, two shares, caches cold: 22.8 us, 8 columns 25.9).  Share r has a part of query tile i iff its first key tile, r, meets it.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part, Heads dq, AttnShape s, float scale, uint32_t q_tiles, uint32_t shares)
 {
@@ -526,20 +542,30 @@ __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part
     T* dst = (T*)dq.p + (int64_t)b * dq.sb + (int64_t)token * dq.st + (int64_t)h * dq.sh;
     const uint64_t stride = (uint64_t)s.B * s.Hq * q_tiles * (DP / 4) * 128;
     const float4* src = part + (((uint64_t)b * s.Hq + h) * q_tiles + i) * (DP / 4) * 128 + row / 32 * (DP / 4) * 32 + row % 32;
-#pragma unroll 4
-    for (uint32_t c = (threadIdx.x >> 7) * 8; c < s.D; c += 16) {
-        const uint32_t at = c / 4 * 32;
-        float y[8] = {};
+    // 32 columns at a time, all loads of a share before their additions
+#pragma unroll
+    for (int c0 = 0; c0 < DP; c0 += 64) {
+        const int first = c0 + (threadIdx.x >> 7) * 32;
+        if ((uint32_t)first >= s.D) break;
+        float y[32] = {};
         for (uint32_t r = 0; r < parts; ++r) {
-            const float4 u = src[r * stride + at], v = src[r * stride + at + 32];
-            y[0] += u.x; y[1] += u.y; y[2] += u.z; y[3] += u.w;
-            y[4] += v.x; y[5] += v.y; y[6] += v.z; y[7] += v.w;
+            float4 u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = src[r * stride + (first / 4 + e) * 32];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[4 * e] += u[e].x; y[4 * e + 1] += u[e].y; y[4 * e + 2] += u[e].z; y[4 * e + 3] += u[e].w;
+            }
         }
 #pragma unroll
-        for (int t = 0; t < 8; ++t) y[t] *= scale;
-        Vec8<T> o;
-        o.set(y);
-        o.store(dst + c);
+        for (int e = 0; e < 4; ++e) {
+            Vec8<T> o;
+            float z[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) z[t] = y[8 * e + t] * scale;
+            o.set(z);
+            if ((uint32_t)(first + 8 * e) < s.D) o.store(dst + first + 8 * e);
+        }
     }
 }
 
@@ -617,7 +643,7 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
 {
     const AttnShape& sh = r.s;
     if (sh.Sq) {
-        k_grad_rows<T><<<dim3(r.q_tiles * 4, sh.Hq, sh.B), 256, 0, s>>>(o, go, lse, (float*)r.rows, sh, r.q_tiles);
+        k_grad_rows<T><<<dim3(r.q_tiles, sh.Hq, sh.B), 256, 0, s>>>(o, go, lse, (float*)r.rows, sh, r.q_tiles);
         DBLP_LAUNCHED();
     }
     if (sh.Sk) {
