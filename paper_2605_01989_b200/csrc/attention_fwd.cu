@@ -299,6 +299,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         for (int i = 0; i < DP / 32; ++i) {
             uint32_t y32[32];
             if (nh) {
+                __syncwarp();                                   // the stores before went by the lane
                 tmem_ld32(t_o + lane_base + i * 32, y32);
                 tmem_wait_ld<32>(y32);
                 if (i + 1 == DP / 32) {

@@ -371,6 +371,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 #pragma unroll
                 for (int c = 0; c < PER; ++c) {
                     uint32_t x[16];
+                    __syncwarp();                               // lane 0 alone waited or sent: together again for the load
                     tmem_ld16(t_dq + lane_base + c * 16, x);
                     if (lane == 0) bulk_wait_read<CH - 1>();    // the piece that was here has left
                     __syncwarp();
@@ -496,6 +497,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 const int c = c0 + cc;
                 uint32_t x[16];
                 if (pairs) {
+                    __syncwarp();                               // the stores before went by the lane
                     tmem_ld16((is_dk ? t_dk : t_dv) + lane_base + c, x);
                     tmem_wait_ld<16>(x);
                 }

@@ -120,6 +120,9 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
 // ---- tensor memory ---------------------------------------------------------------------------------------------------
+// Everything here is .sync.aligned: all 32 lanes execute the same instruction together, anything else is undefined.  After code
+// that only some lanes went through (a copy issued by lane 0, a store under a lane's bound) a __syncwarp() or a warp_wait comes
+// first.
 template <int COLS> __device__ __forceinline__ void tmem_alloc(uint32_t* slot)
 {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "n"(COLS) : "memory");
