@@ -167,8 +167,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                         bar_expect(&cut_full, L::TILE);
                         load_tile<NS>(dst, a.v, &cut_full, j * 128, hk, it.b);
                     }
-                    bar_drain(&cut_full, cuts++ & 1);
-                    __syncwarp();
+                    ok = warp_wait(&cut_full, cuts++ & 1, g);
+                    if (!ok) break;
                     clear_rows<NS>(dst, lk & 127);
                     __syncwarp();
                     if (lane == 0) bar_arrive(&full[st]);
@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         }
         if (lane == 0) {                                        // every copy lands before the block may end
             if (w) bar_drain(&q_full, (w - 1) & 1);
+            if (cuts) bar_drain(&cut_full, (cuts - 1) & 1);
             for (uint32_t x = n > (uint32_t)STAGES ? n - STAGES : 0; x < n; ++x) bar_drain(&full[x % STAGES], (x / STAGES) & 1);
         }
     } else if (warp == 5) {                                     // ---- products

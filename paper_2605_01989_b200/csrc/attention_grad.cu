@@ -177,15 +177,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         uint32_t n = 0, w = 0, cuts = 0;                        // pairs, key tiles with work, tiles that were cleared
         bool ok = true;
         // a tile whose rows from `first` on do not count but may hold anything
-        auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t first) {
+        auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t first) -> bool {
             if (lane == 0) {
                 bar_expect(&s.cut_full, L::TILE);
                 load_tile<NS>(dst, src, &s.cut_full, token, head, b);
             }
-            bar_drain(&s.cut_full, cuts++ & 1);
-            __syncwarp();
+            if (!warp_wait(&s.cut_full, cuts++ & 1, g)) return false;
             clear_rows<NS>(dst, first);
             __syncwarp();
+            return true;
         };
         for (uint32_t m = 0; ok; ++m) {
             const uint32_t j = share_tile(share, m, a.shares);
@@ -195,7 +195,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (w) ok = warp_wait(&s.acc_full, (w - 1) & 1, g);   // products of the tile before are done
             if (!ok) break;
             const bool kcut = j * 128 + 128 > lk && lk < a.s.Sk;
-            if (kcut) load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
+            if (kcut) ok = load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
+            if (!ok) break;
             if (lane == 0) {
                 bar_expect(&s.kv_full, kcut ? L::TILE : 2 * L::TILE);
                 if (!kcut) load_tile<NS>(smem + L::K, a.k, &s.kv_full, j * 128, hk, b);
@@ -209,15 +210,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                 if (n >= NQ) ok = warp_wait(&s.q_empty[sq], (n / NQ - 1) & 1, g);
                 if (!ok) break;
                 uint8_t *dq_ = smem + L::Q + sq * L::TILE, *dg = smem + L::G + sg * L::TILE;
-                if (cut) load_cut(dq_, a.q, i * 128, h, lq - i * 128);
+                if (cut) ok = load_cut(dq_, a.q, i * 128, h, lq - i * 128);
+                if (!ok) break;
                 if (lane == 0) {
                     bar_expect(&s.q_full[sq], (cut ? 0 : L::TILE) + 1024);
                     if (!cut) load_tile<NS>(dq_, a.q, &s.q_full[sq], i * 128, h, b);
                     bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &s.q_full[sq]);
                 }
                 if (n >= NG) ok = warp_wait(&s.g_empty[sg], (n / NG - 1) & 1, g);
+                if (ok && cut) ok = load_cut(dg, a.go, i * 128, h, lq - i * 128);
                 if (!ok) { if (lane == 0) bar_drain(&s.q_full[sq], (n / NQ) & 1); break; }
-                if (cut) load_cut(dg, a.go, i * 128, h, lq - i * 128);
                 if (lane == 0) {
                     if (cut) {
                         bar_arrive(&s.g_full[sg]);
@@ -231,6 +233,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         }
         if (lane == 0) {                                        // every copy lands before the block may end
             if (w) bar_drain(&s.kv_full, (w - 1) & 1);
+            if (cuts) bar_drain(&s.cut_full, (cuts - 1) & 1);
             for (uint32_t x = n > NQ ? n - NQ : 0; x < n; ++x) bar_drain(&s.q_full[x % NQ], (x / NQ) & 1);
             for (uint32_t x = n > NG ? n - NG : 0; x < n; ++x) bar_drain(&s.g_full[x % NG], (x / NG) & 1);
         }

@@ -78,7 +78,8 @@ __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, const Gu
 {
     return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, g));
 }
-// For copies that were issued and must land before the block ends: bounded by itself, whatever the flag says.
+// For copies and products that were issued and must be done before the block ends, and for nothing else: it tells nobody when
+// it gives up.  Bounded by itself, whatever the flag says.
 __device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
 {
     const long long t0 = clock64();
