@@ -229,10 +229,9 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             count += nh;
             ++w;
         }
-        if (!ok) {                                              // products in flight end before the memory is freed
-            mma_commit(&idle);
-            bar_drain(&idle, 0);
-        }
+        __syncwarp();
+        mma_commit(&idle);                                      // products in flight end before the memory is freed, whoever gave up
+        bar_drain(&idle, 0);
         __syncwarp();
     } else {                                                    // ---- softmax: one thread a row
         const uint32_t lane_base = warp << 21;                  // lane 32 * warp

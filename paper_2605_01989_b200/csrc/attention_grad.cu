@@ -344,10 +344,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (ok) mma_commit(&s.acc_full);
             ++w;
         }
-        if (!ok) {                                              // products in flight end before the memory is freed
-            mma_commit(&s.idle);
-            bar_drain(&s.idle, 0);
-        }
+        __syncwarp();
+        mma_commit(&s.idle);                                    // products in flight end before the memory is freed, whoever gave up
+        bar_drain(&s.idle, 0);
         __syncwarp();
     } else if (warp >= kDqWarp) {                               // ---- dq: tensor memory -> this share's buffer
         // Each warp takes 32 queries.  Pieces go through shared memory and are added by the memory system: adding from
