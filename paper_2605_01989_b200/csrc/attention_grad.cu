@@ -653,7 +653,13 @@ static int launch_backward(const GradArgs& r, Heads o, Heads go, const float* ls
     if (sh.Sk) {
         const cudaError_t e = allow_shared<k_grad<T, DP>>(GradSmem<DP>::kBytes);
         DBLP_CUDA(e);
-        DBLP_NEXT(launch_next(k_grad<T, DP>, dim3(r.shares * r.groups, sh.Hkv, sh.B), kGradThreads, GradSmem<DP>::kBytes, s, r));
+        const dim3 grid(r.shares * r.groups, sh.Hkv, sh.B);
+        if (sh.Sq) {
+            DBLP_NEXT(launch_next(k_grad<T, DP>, grid, kGradThreads, GradSmem<DP>::kBytes, s, r));
+        } else {                                                // the call's first kernel: it reads the lengths before it waits
+            k_grad<T, DP><<<grid, kGradThreads, GradSmem<DP>::kBytes, s>>>(r);
+            DBLP_LAUNCHED();
+        }
         if (r.dkv)
             DBLP_NEXT(launch_next(k_grad_dkv<T, DP>, dim3((sh.Sk * (DP / 8) + 255) / 256, sh.Hkv, sh.B * 2), 256, 0, s, r.dkv, r.dk, r.dv, sh,
                                   r.k_tiles * 128, r.groups));
