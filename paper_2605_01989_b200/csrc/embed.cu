@@ -122,7 +122,7 @@ k_rank_sort(const I* __restrict__ tokens, uint32_t n, int64_t rows, int64_t padd
             uint32_t* __restrict__ pos, uint32_t* __restrict__ seen, uint32_t seen_words, unsigned long long* bad)
 {
     after_start();
-    extern __shared__ uint32_t s_key[];                        // all n keys, padded to a multiple of 32 with all-ones
+    extern __shared__ __align__(16) uint32_t s_key[];          // all n keys, padded to a multiple of 32 with all-ones; read 16 bytes at a time
     __shared__ uint32_t s_cnt[8][32], s_seen[kSeenWords];
     const uint32_t n32 = (n + 31) & ~31u, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = blockIdx.x * 32 + lane;
     for (uint32_t i = threadIdx.x; i < n32; i += 256)
