@@ -118,8 +118,8 @@ using namespace dblp;
 extern "C" int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes)
 {
     DBLP_TRY(check_shape("attention_workspace_bytes", a));
-    if (fwd_bytes) *fwd_bytes = attention_forward_space(a);
-    if (grad_bytes) *grad_bytes = attention_backward_space(a);
+    if (fwd_bytes) *fwd_bytes = a->batch ? attention_forward_space(a) : 0;     // the rules that cut the work divide by the batch
+    if (grad_bytes) *grad_bytes = a->batch ? attention_backward_space(a) : 0;
     return DBLP_OK;
 }
 

@@ -1,0 +1,31 @@
+"""Worker-side entry points at the ends of their ranges, before anything touches a device: empty batches, sizes whose products
+leave 64 bits."""
+import ctypes as C
+
+import pytest
+import torch
+
+import test_operators_refusals as refusals
+from paper_2605_01989_b200 import binding as dblp
+
+EINVAL, EALIGN, ECAPACITY = -1, -2, -3
+
+
+def workspace(**kw):
+    s = dblp.dblp_attention_t(**{**refusals.SHAPE, **kw})
+    f, g = C.c_size_t(77), C.c_size_t(77)
+    rc, text = refusals.call("dblp_attention_workspace_bytes", C.byref(s), C.byref(f), C.byref(g))
+    return rc, f.value, g.value, text
+
+
+@pytest.mark.parametrize("q_tokens", [0, 1, 2, 16, 300])
+@pytest.mark.parametrize("k_tokens", [0, 1, 300])
+def test_an_empty_batch_needs_no_workspace(q_tokens, k_tokens):
+    assert workspace(batch=0, q_tokens=q_tokens, k_tokens=k_tokens)[:3] == (0, 0, 0)
+
+
+@pytest.mark.parametrize("q_tokens", [0, 1, 2, 16, 300])
+@pytest.mark.parametrize("k_tokens", [0, 1, 300])
+def test_the_workspace_query_knows_every_small_shape(q_tokens, k_tokens):
+    rc, f, g, _ = workspace(q_tokens=q_tokens, k_tokens=k_tokens)
+    assert rc == 0 and f % 4 == 0 and g % 4 == 0 and max(f, g) < 1 << 24
