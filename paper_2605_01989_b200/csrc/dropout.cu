@@ -138,7 +138,7 @@ extern "C" int dblp_dropout(const void* x, int64_t x_stride, const void* residua
     DBLP_REQUIRE(site < (1u << 24), DBLP_EINVAL, "dropout: site %u does not fit in 24 bits", site);
     if (rows == 0 || cols == 0) return DBLP_OK;
     DBLP_REQUIRE(x && out, DBLP_EINVAL, "dropout: null pointer");
-    DBLP_REQUIRE(rows < (1ull << 40) && rows * cols < (1ull << 41), DBLP_ECAPACITY, "dropout: more than 2^41 elements");
+    DBLP_REQUIRE(rows <= ((1ull << 41) - 1) / cols, DBLP_ECAPACITY, "dropout: 2^41 elements or more");
     DBLP_REQUIRE(rows == 1 || out_stride >= (int64_t)cols || out_stride <= -(int64_t)cols, DBLP_EINVAL,
                  "dropout: rows of the output overlap (stride %lld, %u columns)", (long long)out_stride, cols);
     const uint64_t es = element_bytes(dtype);

@@ -29,3 +29,10 @@ def test_an_empty_batch_needs_no_workspace(q_tokens, k_tokens):
 def test_the_workspace_query_knows_every_small_shape(q_tokens, k_tokens):
     rc, f, g, _ = workspace(q_tokens=q_tokens, k_tokens=k_tokens)
     assert rc == 0 and f % 4 == 0 and g % 4 == 0 and max(f, g) < 1 << 24
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 39, 1 << 31), (1 << 33, 1 << 31), ((1 << 33) + 1, 1 << 31), ((1 << 40) - 1, 0xFFFFFFFF),
+                                       (1 << 40, 2), (1 << 41, 1), (1 << 63, 2), ((1 << 64) - 1, 1)])
+def test_dropout_counts_its_elements_beyond_64_bits(rows, cols):
+    rc, text = refusals.dropout(rows=rows, cols=cols, xs=cols, os=cols)
+    assert rc == ECAPACITY and "elements" in text
