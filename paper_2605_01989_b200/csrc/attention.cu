@@ -118,8 +118,10 @@ using namespace dblp;
 extern "C" int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes)
 {
     DBLP_TRY(check_shape("attention_workspace_bytes", a));
-    if (fwd_bytes) *fwd_bytes = a->batch ? attention_forward_space(a) : 0;     // the rules that cut the work divide by the batch
-    if (grad_bytes) *grad_bytes = a->batch ? attention_backward_space(a) : 0;
+    const size_t grad = a->batch ? attention_backward_space(a) : 0;            // the rules that cut the work divide by the batch
+    DBLP_REQUIRE(grad < 1ull << 62, DBLP_ECAPACITY, "attention_workspace_bytes: the gradient's workspace passes 2^62 bytes");
+    if (fwd_bytes) *fwd_bytes = a->batch ? attention_forward_space(a) : 0;
+    if (grad_bytes) *grad_bytes = grad;
     return DBLP_OK;
 }
 

@@ -625,6 +625,7 @@ static GradCut cut_of(const dblp_attention_t* a)
 }
 
 struct GradSpaceA {
+    static constexpr uint64_t kTooLarge = ~0ull;
     uint64_t rows, dq, dkv, bytes;
     GradCut cut;
     explicit GradSpaceA(const dblp_attention_t* a) : cut{0, 1}
@@ -632,11 +633,13 @@ struct GradSpaceA {
         const uint64_t tiles = (uint64_t)a->batch * a->q_heads * ((a->q_tokens + 127) / 128), dp = a->head_dim <= 64 ? 64 : 128;
         rows = 0;
         dq = tiles * 1024;
-        dkv = bytes = dq;
+        dkv = dq;
+        bytes = tiles >= 1ull << 40 ? kTooLarge : dq;           // sizes that no tensor has can pass 64 bits
         if (!a->k_tokens) return;
         cut = cut_of(a);
         dkv = dq + cut.shares * tiles * 128 * dp * 4;
-        bytes = dkv + (cut.groups > 1 ? cut.groups * 2ull * a->batch * a->kv_heads * ((a->k_tokens + 127) / 128) * 128 * dp * 4 : 0);
+        const uint64_t kv = cut.groups > 1 ? cut.groups * 2ull * a->batch * a->kv_heads * ((a->k_tokens + 127) / 128) : 0;
+        if (bytes != kTooLarge) bytes = kv >= 1ull << 40 ? kTooLarge : dkv + kv * 128 * dp * 4;
     }
 };
 

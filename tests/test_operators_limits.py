@@ -36,3 +36,18 @@ def test_the_workspace_query_knows_every_small_shape(q_tokens, k_tokens):
 def test_dropout_counts_its_elements_beyond_64_bits(rows, cols):
     rc, text = refusals.dropout(rows=rows, cols=cols, xs=cols, os=cols)
     assert rc == ECAPACITY and "elements" in text
+
+
+@pytest.mark.parametrize("kw", [dict(batch=65535, q_heads=65535, kv_heads=65535, q_tokens=(1 << 30) - 1, k_tokens=1 << 29),
+                                dict(batch=65535, q_heads=65535, kv_heads=65535, q_tokens=(1 << 30) - 1, k_tokens=0),
+                                dict(batch=65535, q_heads=65535, kv_heads=1, q_tokens=(1 << 30) - 1, k_tokens=1 << 29, head_dim=128)])
+def test_a_workspace_beyond_64_bits_is_refused(kw):
+    rc, _, _, text = workspace(**kw)
+    assert rc == ECAPACITY and "workspace" in text
+
+
+def test_a_large_workspace_is_counted_in_full():
+    """One sequence of 2^29 tokens, 8 heads of 128: at least one fp32 copy of q and 8 bytes a row."""
+    n = 1 << 29
+    rc, _, g, _ = workspace(batch=1, q_heads=8, kv_heads=8, q_tokens=n, k_tokens=n, head_dim=128)
+    assert rc == 0 and g >= n * 8 * (128 * 4 + 8)
