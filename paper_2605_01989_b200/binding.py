@@ -457,6 +457,13 @@ def _require(ok, what):
         raise ValueError(what)
 
 
+def _u32(x, name):
+    """x itself where it fits the 32 bits that the call has for it (a larger one would arrive cut off)."""
+    if not 0 <= x < 1 << 32:
+        raise ValueError("%s = %d does not fit in 32 bits" % (name, x))
+    return x
+
+
 def _rows(t, name):
     """(address, row stride, rows, columns) of a 2-D tensor whose elements within a row are contiguous."""
     if t.dim() != 2:
@@ -496,13 +503,13 @@ def dblp_embed(table, tokens, out, scale=1.0, padding=-1, bad_tokens=None, strea
     kp, kb, n = _flat_tokens(tokens)
     if m != n or w != width:
         raise ValueError("out: one row of the table's width per token")
-    _check(lib().dblp_embed(tp, ts, rows, width, _dtype(table), kp, kb, n, padding, scale, op, os_, _dtype(out),
+    _check(lib().dblp_embed(tp, ts, rows, _u32(width, "width"), _dtype(table), kp, kb, n, padding, scale, op, os_, _dtype(out),
                             _counter(bad_tokens), _raw_stream(stream)), "dblp_embed")
 
 
 def dblp_embed_grad_workspace_bytes(n, rows, width):
     b = C.c_size_t()
-    _check(lib().dblp_embed_grad_workspace_bytes(n, rows, width, C.byref(b)), "dblp_embed_grad_workspace_bytes")
+    _check(lib().dblp_embed_grad_workspace_bytes(n, rows, _u32(width, "width"), C.byref(b)), "dblp_embed_grad_workspace_bytes")
     return int(b.value)
 
 
@@ -515,7 +522,7 @@ def dblp_embed_grad(dout, tokens, dtable, ws, scale=1.0, padding=-1, accumulate=
     if m != n or w != width:
         raise ValueError("dout: one row of the table's width per token")
     wp, wb = _scratch(ws)
-    _check(lib().dblp_embed_grad(dp, ds, _dtype(dout), kp, kb, n, padding, scale, tp, ts, rows, width, _dtype(dtable),
+    _check(lib().dblp_embed_grad(dp, ds, _dtype(dout), kp, kb, n, padding, scale, tp, ts, rows, _u32(width, "width"), _dtype(dtable),
                                  DBLP_ACCUMULATE if accumulate else 0, _counter(bad_tokens), wp, wb, _raw_stream(stream)),
            "dblp_embed_grad")
 
@@ -532,8 +539,8 @@ def dblp_dropout(x, out, p, seed, step, site, residual=None, stream=None):
         same = same and m == rows and w == cols and residual.dtype == x.dtype
     if not same:
         raise ValueError("x, residual and out: one shape and dtype")
-    _check(lib().dblp_dropout(xp, xs, rp, rs or 0, op, os_, rows, cols, _dtype(x), p, seed, step, site, _raw_stream(stream)),
-           "dblp_dropout")
+    _check(lib().dblp_dropout(xp, xs, rp, rs or 0, op, os_, rows, _u32(cols, "columns"), _dtype(x), p, seed, _u32(step, "step"),
+                              _u32(site, "site"), _raw_stream(stream)), "dblp_dropout")
 
 
 def dblp_dropout_grad(dout, dx, p, seed, step, site, stream=None):
@@ -543,8 +550,8 @@ def dblp_dropout_grad(dout, dx, p, seed, step, site, stream=None):
     xp, xs, m, w = _rows(dx, "dx")
     if m != rows or w != cols or dx.dtype != dout.dtype:
         raise ValueError("dout and dx: one shape and dtype")
-    _check(lib().dblp_dropout_grad(gp, gs, xp, xs, rows, cols, _dtype(dx), p, seed, step, site, _raw_stream(stream)),
-           "dblp_dropout_grad")
+    _check(lib().dblp_dropout_grad(gp, gs, xp, xs, rows, _u32(cols, "columns"), _dtype(dx), p, seed, _u32(step, "step"),
+                                   _u32(site, "site"), _raw_stream(stream)), "dblp_dropout_grad")
 
 
 def _heads(t, name, dtype, shape):
@@ -567,6 +574,8 @@ def _attention(q, k, causal, scale, q_lens, k_lens):
             raise ValueError("lengths: int32, one per sequence")
     if scale is None:
         scale = D ** -0.5 if D else 0.0
+    if max(B, Sq, ks[1], Hq, ks[2], D) >= 1 << 32:
+        raise ValueError("an extent of q or k does not fit in 32 bits")
     return dblp_attention_t(B, Sq, ks[1], Hq, ks[2], D, _dtype(q), DBLP_ATTENTION_CAUSAL if causal else 0, scale,
                             None if q_lens is None else q_lens.data_ptr(), None if k_lens is None else k_lens.data_ptr()), qs, ks
 

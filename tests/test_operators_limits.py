@@ -51,3 +51,33 @@ def test_a_large_workspace_is_counted_in_full():
     n = 1 << 29
     rc, _, g, _ = workspace(batch=1, q_heads=8, kv_heads=8, q_tokens=n, k_tokens=n, head_dim=128)
     assert rc == 0 and g >= n * 8 * (128 * 4 + 8)
+
+
+# Calls through the binding with tensors that have shapes and no memory: they end in a refusal, the binding's or the library's
+# for the null address.
+@pytest.fixture
+def anywhere(monkeypatch):
+    monkeypatch.setattr(dblp, "_on_device", lambda *t: None)
+
+
+def meta(*shape, dtype=torch.bfloat16):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+WIDE = (1 << 32) + 8
+
+
+@pytest.mark.parametrize("call", [
+    lambda: dblp.dblp_dropout(meta(1, WIDE), meta(1, WIDE), 0.1, 1, 2, 3, stream=0),
+    lambda: dblp.dblp_dropout_grad(meta(1, WIDE), meta(1, WIDE), 0.1, 1, 2, 3, stream=0),
+    lambda: dblp.dblp_dropout(meta(4, 8), meta(4, 8), 0.1, 1, 1 << 32, 3, stream=0),
+    lambda: dblp.dblp_dropout(meta(4, 8), meta(4, 8), 0.1, 1, -1, 3, stream=0),
+    lambda: dblp.dblp_dropout(meta(4, 8), meta(4, 8), 0.1, 1, 2, (1 << 32) + 3, stream=0),
+    lambda: dblp.dblp_dropout_grad(meta(4, 8), meta(4, 8), 0.1, 1, 2, (1 << 32) + 3, stream=0),
+    lambda: dblp.dblp_embed(meta(4, WIDE), meta(2, dtype=torch.int32), meta(2, WIDE), stream=0),
+    lambda: dblp.dblp_embed_grad(meta(2, WIDE), meta(2, dtype=torch.int32), meta(4, WIDE), None, stream=0),
+    lambda: dblp.dblp_embed_grad_workspace_bytes(5, 5, WIDE),
+    lambda: dblp.dblp_attention_workspace_bytes(meta(1, 5, 2, 64), meta(1, WIDE, 2, 64))])
+def test_what_does_not_fit_in_32_bits_is_refused(anywhere, call):
+    with pytest.raises(ValueError, match="32 bits"):
+        call()
