@@ -412,7 +412,7 @@ int dblp_round_until_stop(const dblp_plan_t* plan, const dblp_loss_model_t* mode
 /* dblp_embed: out[i, :] = scale * table[tokens[i], :], an fp32 multiply rounded once to out_dtype.
  * table: rows x width, row stride table_stride.  tokens: n ids of token_bytes (4 or 8) bytes each, signed.  out: n rows,
  * row stride out_stride.  A token equal to `padding` (any value outside [0, rows) = no padding id) gives a zero row.  A
- * token outside [0, rows) that is not the padding id gives a zero row too and is counted in *bad_tokens (u64, device,
+ * token outside [0, rows) gives a zero row too, whatever `padding` is, and is counted in *bad_tokens (u64, device,
  * accumulates; NULL = not counted); it never faults. */
 int dblp_embed(const void* table, int64_t table_stride, uint64_t rows, uint32_t width, int table_dtype,
                const void* tokens, uint32_t token_bytes, uint64_t n, int64_t padding, float scale, void* out,

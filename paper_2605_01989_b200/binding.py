@@ -496,7 +496,8 @@ def _scratch(ws):
 
 
 def dblp_embed(table, tokens, out, scale=1.0, padding=-1, bad_tokens=None, stream=None):
-    """out[i] = scale * table[tokens[i]]; a zero row for the padding id and for ids outside the table."""
+    """out[i] = scale * table[tokens[i]]; a zero row for the padding id (none if outside the table) and for ids outside the
+    table, which bad_tokens counts."""
     _on_device(table, tokens, out, bad_tokens)
     tp, ts, rows, width = _rows(table, "table")
     op, os_, m, w = _rows(out, "out")

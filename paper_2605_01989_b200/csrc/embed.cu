@@ -55,8 +55,8 @@ k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restr
 #pragma unroll
     for (int u = 0; u < kLookUnroll; ++u) {
         if (base + u * kEmbedThreads >= items) break;
-        const bool live = tok[u] >= 0 && tok[u] < rows && tok[u] != padding;
-        if (!live && bad && tok[u] != padding && grp[u] == 0) atomicAdd(bad, 1ull);
+        const bool inside = tok[u] >= 0 && tok[u] < rows, live = inside && tok[u] != padding;
+        if (!inside && bad && grp[u] == 0) atomicAdd(bad, 1ull);
         Vec8<TO> o;
         if (live) {
             v[u].get(x);
@@ -83,8 +83,8 @@ k_embed_any(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __r
     const uint32_t lane = threadIdx.x & 31, w = blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5), row = slabs.div(w), slab = w - row * slabs.d;
     if (row >= n) return;
     const int64_t tok = token_at(tokens, row);
-    const bool live = tok >= 0 && tok < rows && tok != padding;
-    if (!live && bad && tok != padding && slab == 0 && lane == 0) atomicAdd(bad, 1ull);
+    const bool inside = tok >= 0 && tok < rows, live = inside && tok != padding;
+    if (!inside && bad && slab == 0 && lane == 0) atomicAdd(bad, 1ull);
     const uint32_t c0 = slab * (32 * kAnyCols) + lane;
     const TI* src = table + (live ? tok : 0) * ts + c0;
     TO* dst = out + (int64_t)row * os + c0;
@@ -103,12 +103,11 @@ template <typename I>
 __device__ __forceinline__ uint32_t key_of(const I* tokens, uint64_t i, int64_t rows, int64_t padding, unsigned long long* bad)
 {
     const int64_t t = token_at(tokens, i);
-    if (t == padding) return (uint32_t)rows;
-    if (t < 0 || t >= rows) {
+    if (t < 0 || t >= rows) {                                  // before the padding id, which is one only inside the table
         if (bad) atomicAdd(bad, 1ull);
         return (uint32_t)rows;
     }
-    return (uint32_t)t;
+    return t == padding ? (uint32_t)rows : (uint32_t)t;
 }
 
 // Stable rank by counting: a block takes 32 tokens, its 8 warps an eighth of all keys each, and lane l counts for token l
