@@ -42,7 +42,7 @@ template <int N> __device__ __forceinline__ void join_sums(float& m, float& l, f
 template <typename T>
 __device__ __forceinline__ void finish_query(const RowsArgs& a, uint32_t b, uint32_t i, uint32_t h, uint32_t c, const float* acc, float m, float l)
 {
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (c < a.s.D) {
         float y[8];
 #pragma unroll
@@ -51,7 +51,7 @@ __device__ __forceinline__ void finish_query(const RowsArgs& a, uint32_t b, uint
         w.set(y);
         w.store((T*)a.o.p + (int64_t)b * a.o.sb + (int64_t)i * a.o.st + (int64_t)h * a.o.sh + c);
     }
-    if (c == 0 && a.lse) a.lse[((uint64_t)b * a.s.Hq + h) * a.s.Sq + i] = l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
+    if (c == 0 && a.lse) a.lse[((uint64_t)b * a.s.Hq + h) * a.s.Sq + i] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;  // NaN stays
 }
 
 template <typename T, int LPK, int NR>

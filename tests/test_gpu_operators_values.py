@@ -1,0 +1,71 @@
+"""Attention and its gradient where scores are NaN or infinite, in every place of the groups that the kernels take them in."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_operators as op
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BF16, F16 = torch.bfloat16, torch.float16
+NAN, INF = math.nan, math.inf
+
+
+def case(Sq, D, dtype, B=1, Sk=200, H=2, seed=1):
+    """Tensors whose first column makes infinite scores on demand: q has a one there, k a zero."""
+    ts = [t.clone() for t in op.tensors(B, Sq, Sk, H, H, D, dtype, seed=seed)]
+    ts[0][..., 0] = 1.0
+    ts[1][..., 0] = 0.0
+    return ts
+
+
+# One head's key at each place of eight, in both halves of a tile and in the last one.
+@pytest.mark.parametrize("Sq", [3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("at", list(range(8)) + [70, 71, 133, 198, 199])
+def test_a_score_that_is_no_number_reaches_its_rows(Sq, D, dtype, bad, at):
+    q, k, v, g, out, dq, dk, dv = case(Sq, D, dtype)
+    clean = torch.empty_like(out)
+    lse0 = op.run_attention(q, k, v, clean)
+    k[:, at, 0, 0] = bad                               # of head 0 alone
+    lse = op.run_attention(q, k, v, out)
+    assert torch.isnan(out[:, :, 0]).all()
+    assert (torch.isnan(lse[:, 0]) | (lse[:, 0] == INF)).all()
+    assert torch.equal(op.bits(out[:, :, 1]), op.bits(clean[:, :, 1])) and torch.equal(lse[:, 1], lse0[:, 1])
+    op.run_grad(q, k, v, out, g, lse, dq, dk, dv)
+    for t in (dq, dk, dv):
+        assert torch.isnan(t[:, :, 0]).all() and torch.isfinite(t[:, :, 1]).all()
+
+
+@pytest.mark.parametrize("Sq", [4])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("at", list(range(8)) + [70, 71, 133, 149])
+def test_a_query_that_is_no_number_reaches_every_key_it_sees(Sq, D, dtype, at):
+    at = at % Sq
+    q, k, v, g, out, dq, dk, dv = case(Sq, D, dtype)
+    q[:, at, 0, 3] = NAN
+    lse = op.run_attention(q, k, v, out)
+    assert torch.isnan(out[:, at, 0]).all() and torch.isnan(lse[:, 0, at]).all()
+    others = [i for i in range(Sq) if i != at]
+    assert torch.isfinite(out[:, others]).all() and torch.isfinite(lse[:, :, others]).all() and torch.isfinite(out[:, :, 1]).all()
+    op.run_grad(q, k, v, out, g, lse, dq, dk, dv)
+    assert torch.isnan(dq[:, at, 0]).all() and torch.isnan(dk[:, :, 0]).all() and torch.isnan(dv[:, :, 0]).all()
+    assert torch.isfinite(dq[:, others]).all()
+    for t in (dq, dk, dv):
+        assert torch.isfinite(t[:, :, 1]).all()
+
+
+@pytest.mark.parametrize("Sq", [3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", list(range(8)) + [133, 199])
+def test_a_score_of_minus_infinity_is_a_key_of_no_weight(Sq, D, at):
+    q, k, v, g, out, dq, dk, dv = case(Sq, D, BF16)
+    k[:, at, :, 0] = -INF
+    lse = op.run_attention(q, k, v, out)
+    rest = [j for j in range(k.shape[1]) if j != at]
+    op.check_forward(q, k[:, rest], v[:, rest], out, lse)
