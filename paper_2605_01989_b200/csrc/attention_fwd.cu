@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             tc_fence_after();
             ++w;
         }
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;                  // l = NaN: so is the row
         T* o = (T*)a.o.p + (int64_t)it.b * a.o.sb + (int64_t)row * a.o.st + (int64_t)it.h * a.o.sh;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i) {

@@ -259,23 +259,30 @@ __device__ __forceinline__ float exp2_fast(float x)
     return r;
 }
 
+__device__ __forceinline__ float max_nan(float a, float b)      // NaN if either is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // 2^x of two values on the FMA and integer units, for x < 128: x = n + f with n the nearest integer, 2^f by a polynomial of
-// degree 4 fitted here to the least largest relative error on [-1/2, 1/2] (2.7e-6, evaluated in fp32), 2^n by adding n to the
-// exponent; what falls below the exponent's range, -infinity too, gives 0.  The special function unit gives 16 results a cycle and SM,
-// which is what bounds the softmax; a part of them computed this way shortens it.
+// degree 4 fitted here to the least largest relative error on [-1/2, 1/2] (2.7e-6, evaluated in fp32), times 2^n made of its bits;
+// n = -127 makes the bits of 0, so what falls below the exponent's range, -infinity too, gives 0.  NaN stays NaN and +infinity
+// becomes NaN: both pass through f.  The special function unit gives 16 results a cycle and SM; a part of them computed this way
+// shortens a softmax.
 __device__ __forceinline__ float2 exp2_pair(float2 x)
 {
     constexpr float kShift = 12582912.0f;                       // 1.5 * 2^23: adding it rounds to an integer in the low bits
-    x.x = fmaxf(x.x, -200.0f);
-    x.y = fmaxf(x.y, -200.0f);
+    x.x = max_nan(x.x, -127.0f);
+    x.y = max_nan(x.y, -127.0f);
     const float2 t = add2(x, make_float2(kShift, kShift)), n = add2(t, make_float2(-kShift, -kShift));
     const float2 f = fma2(n, make_float2(-1.0f, -1.0f), x);
     float2 p = fma2(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
     p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
     p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
     p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    return make_float2(__int_as_float(max(__float_as_int(p.x) + (__float_as_int(t.x) << 23), 0)),
-                       __int_as_float(max(__float_as_int(p.y) + (__float_as_int(t.y) << 23), 0)));
+    return mul2(p, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3F800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3F800000)));
 }
 
 }  // namespace dblp

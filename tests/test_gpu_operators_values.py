@@ -1,4 +1,5 @@
-"""Attention and its gradient where scores are NaN or infinite, in every place of the groups that the kernels take them in."""
+"""Attention and its gradient where scores are NaN, infinite or very large, in every place of the groups that the kernels take
+them in; the exponential by itself."""
 import math
 
 import pytest
@@ -21,8 +22,8 @@ def case(Sq, D, dtype, B=1, Sk=200, H=2, seed=1):
     return ts
 
 
-# One head's key at each place of eight, in both halves of a tile and in the last one.
-@pytest.mark.parametrize("Sq", [3])
+# One head's key at each place of eight, in both halves of a tile and in the last one; Sq = 3: few rows a key head, 150: tiles.
+@pytest.mark.parametrize("Sq", [3, 150])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("bad", [NAN, INF])
@@ -41,7 +42,7 @@ def test_a_score_that_is_no_number_reaches_its_rows(Sq, D, dtype, bad, at):
         assert torch.isnan(t[:, :, 0]).all() and torch.isfinite(t[:, :, 1]).all()
 
 
-@pytest.mark.parametrize("Sq", [4])
+@pytest.mark.parametrize("Sq", [4, 150])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("at", list(range(8)) + [70, 71, 133, 149])
@@ -60,7 +61,7 @@ def test_a_query_that_is_no_number_reaches_every_key_it_sees(Sq, D, dtype, at):
         assert torch.isfinite(t[:, :, 1]).all()
 
 
-@pytest.mark.parametrize("Sq", [3])
+@pytest.mark.parametrize("Sq", [3, 150])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("at", list(range(8)) + [133, 199])
 def test_a_score_of_minus_infinity_is_a_key_of_no_weight(Sq, D, at):
@@ -69,3 +70,29 @@ def test_a_score_of_minus_infinity_is_a_key_of_no_weight(Sq, D, at):
     lse = op.run_attention(q, k, v, out)
     rest = [j for j in range(k.shape[1]) if j != at]
     op.check_forward(q, k[:, rest], v[:, rest], out, lse)
+
+
+def exponents(dtype):
+    """Every exponent from 0 down to -7 in steps of 1/256 (both types hold those below -4 in steps of 1/64 and more alike)."""
+    x = -torch.arange(0, 7 * 256 + 1, dtype=torch.float64) / 256
+    return x.to(dtype).unique()
+
+
+@pytest.mark.parametrize("place", range(8))
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_exponential_by_itself(place, D):
+    """Two keys count: one with score 0, one with score x ln 2, so that exp(lse) - 1 is the kernel's 2^x.  log2f and the product with
+    ln 2 are off by about 2^-23 of values up to 1, exp(lse) doubles that; the polynomial is off by 2.7e-6, ex2 by 2^-22."""
+    x = exponents(F16)
+    B, Sq, Sk = x.numel(), 9, 64
+    q, k = torch.zeros((B, Sq, 1, D), dtype=F16, device=DEV), torch.zeros((B, Sk, 1, D), dtype=F16, device=DEV)
+    q[..., 0] = 1.0
+    k[..., 0] = -1000.0
+    k[:, 8, 0, 0] = 0.0
+    k[:, 16 + place, 0, 0] = x.to(DEV)
+    v, out = torch.zeros_like(k), torch.empty_like(q)
+    lse = op.run_attention(q, k, v, out, scale=math.log(2))
+    got = torch.expm1(lse[:, 0, 0].double()).cpu()
+    want = torch.exp2(x.double())
+    assert ((got - want).abs() <= 3e-6 * want + 4 * 2.0 ** -23).all(), ((got - want).abs() / want).max()
+    assert (lse == lse[:, :, :1]).all()
