@@ -100,9 +100,10 @@ k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict_
 #pragma unroll
         for (int t = 4; t; t >>= 1) d[r] += __shfl_xor_sync(0xFFFFFFFFu, d[r], t);
         if ((lane & 7) == 0) {
-            // rows that see nothing: 2^(s - infinity) = 0
-            dst[4 * r] = live[r] ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i0 + 4 * r] * -1.4426950408889634f : -INFINITY;
-            dst[128 + 4 * r] = live[r] ? -d[r] : 0.0f;
+            // rows that see nothing, or nothing but scores of -infinity: 2^(s - infinity) = 0
+            const float l = live[r] ? lse[((uint64_t)b * s.Hq + h) * s.Sq + i0 + 4 * r] : -INFINITY;
+            dst[4 * r] = l == -INFINITY ? l : l * -1.4426950408889634f;
+            dst[128 + 4 * r] = l == -INFINITY ? 0.0f : -d[r];
         }
     }
 }

@@ -276,12 +276,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_grad_few(const __grid_const
     for (int r = 0; r < NR; ++r) {                              // row r: query r / rep of head hk * rep + r % rep
         const uint32_t i = r / a.s.rep, h = hk * a.s.rep + r % a.s.rep;
         sees[r] = (uint32_t)r < rows ? keys_of(i, lq, lk, a.s.causal) : 0;
-        most = max(most, sees[r]);
         lse[r] = 0.0f;
         float d = 0.0f;
 #pragma unroll
         for (int t = 0; t < 8; ++t) q[r][t] = g[r][t] = dq[r][t] = 0.0f;
         if (sees[r]) lse[r] = a.lse[((uint64_t)b * a.s.Hq + h) * a.s.Sq + i] * 1.4426950408889634f;
+        if (lse[r] == -INFINITY) sees[r] = 0;                   // nothing but scores of -infinity: as a row that sees no key
+        most = max(most, sees[r]);
         if (sees[r] && live) {
             Vec8<T> w;
             float o[8];

@@ -72,6 +72,30 @@ def test_a_score_of_minus_infinity_is_a_key_of_no_weight(Sq, D, at):
     op.check_forward(q, k[:, rest], v[:, rest], out, lse)
 
 
+@pytest.mark.parametrize("Sq", [3, 150])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_rows_whose_scores_are_all_minus_infinity_weigh_nothing(Sq, D, causal):
+    """Such a row has no largest score: out = 0 and lse = -infinity as for a row that sees no key, and so the gradient."""
+    q, k, v, g, out, dq, dk, dv = case(Sq, D, BF16)
+    rows = list(range(0, Sq, 2))
+    q[..., 0] = 0.0
+    q[:, rows, :, 0] = -1e30                           # finite, the products are not
+    k[..., 0] = 1e30
+    lse = op.run_attention(q, k, v, out, causal=causal)
+    assert (out[:, rows] == 0).all() and (lse[:, :, rows] == -INF).all()
+    op.run_grad(q, k, v, out, g, lse, dq, dk, dv, causal=causal)
+    assert (dq[:, rows] == 0).all()
+    got = [t.clone() for t in (dk, dv)]
+    q[:, rows, :, 0] = 0.0                             # what the other rows give, with no dout for these
+    g[:, rows] = 0
+    lse = op.run_attention(q, k, v, out, causal=causal)
+    out[:, rows] = 0
+    op.run_grad(q, k, v, out, g, lse, dq, dk, dv, causal=causal)
+    assert torch.isfinite(got[0]).all() and torch.isfinite(got[1]).all()
+    assert torch.equal(got[0], dk) and torch.equal(got[1], dv)
+
+
 def exponents(dtype):
     """Every exponent from 0 down to -7 in steps of 1/256 (both types hold those below -4 in steps of 1/64 and more alike)."""
     x = -torch.arange(0, 7 * 256 + 1, dtype=torch.float64) / 256
