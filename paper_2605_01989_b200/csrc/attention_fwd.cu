@@ -6,7 +6,9 @@
 // registers, so nothing of size queries x keys exists.
 //   scores     x = scale * log2(e) * s, p = 2^(x - m), m any value near the row's maximum so far: out and the sum use the
 //              same m, so it cancels.  m moves only when the maximum has grown by more than 2^8, and only then is the
-//              accumulator rescaled; p stays below 2^8, exact enough in 16 bits and far from overflow.
+//              accumulator rescaled; p stays below 2^8, exact enough in 16 bits and far from overflow.  x - m is one fused
+//              multiply-add with m rounded, off by up to 2^-24 |m| for the whole row alike; from |m| = kFar on, where that would show
+//              when m moves and in the end overflow, m is taken from s first, which is exact where it matters.
 //   warps      0-3 softmax and epilogue, 4 TMA, 5 products.  Two blocks share an SM (96 KB of shared memory and 256 columns
 //              of tensor memory each), so that one's products run beside the other's exponentials.  The blocks are persistent:
 //              q and the first k and v of the next item are loaded, and its first scores computed, while the last item's
@@ -30,7 +32,7 @@ struct FwdArgs {
     Heads o;
     float* lse;
     AttnShape s;
-    float scale_log2;
+    float scale, scale_log2;
     uint32_t q_tiles, items, heads_together;
     unsigned long long* timeouts;
 };
@@ -66,6 +68,8 @@ template <int N> __device__ __forceinline__ void hide_from(uint32_t* x, uint32_t
     for (int i = 0; i < N; ++i)
         if ((uint32_t)i >= left) x[i] = 0xFF800000u;
 }
+
+constexpr float kFar = 4096.0f;
 
 template <int N> __device__ __forceinline__ float largest(const uint32_t* x)
 {
@@ -244,6 +248,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         const uint32_t nh = key_halves(a, q0, lq, lk);
         const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal);
         float m = -INFINITY, l = 0.0f;
+        bool far = false;                                       // the same in all lanes
         for (uint32_t h = 0; h < nh; ++h, ++count) {
             const uint32_t buf = count & 1, my_s = t_s + lane_base + buf * 64;
             ok = warp_wait(&s_full[buf], (count >> 1) & 1, g);
@@ -260,6 +265,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float alpha = move ? exp2_fast((m - top) * c) : 1.0f;                         // m = -infinity: 0
                 if (move) m = top;
+                far = __any_sync(0xFFFFFFFFu, m != -INFINITY && fabsf(m * c) > kFar);
                 l *= alpha;
                 if (h > 0) {                                    // the product of the half before still adds to the accumulator
                     ok = warp_wait(&pv_done, (count - 1) & 1, g);
@@ -276,7 +282,13 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                     }
                 }
             }
-            const float mc = m == -INFINITY ? 0.0f : -m * c;
+            float mc = m == -INFINITY ? 0.0f : -m * c;
+            if (far) {
+                const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int t = 0; t < 64; ++t) s[t] = __float_as_uint(__uint_as_float(s[t]) - base);
+                mc = 0.0f;
+            }
             const float2 c2 = make_float2(c, c), mc2 = make_float2(mc, mc);
             float2 sum = make_float2(0.0f, 0.0f);
             probabilities<T, DP>(s, c2, mc2, sum, my_s);            // p(h) over s(h), which is in registers by now
@@ -318,7 +330,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             }
         }
         if (a.lse && row < a.s.Sq)
-            a.lse[((uint64_t)it.b * a.s.Hq + it.h) * a.s.Sq + row] = seen ? (m * c + log2f(l)) * 0.693147180559945309f : -INFINITY;
+            a.lse[((uint64_t)it.b * a.s.Hq + it.h) * a.s.Sq + row] =
+                !seen ? -INFINITY : far ? fmaf(log2f(l), 0.693147180559945309f, m * a.scale) : (m * c + log2f(l)) * 0.693147180559945309f;
         }
     }
     __syncthreads();
@@ -352,6 +365,7 @@ int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const db
     r.o = heads(out);
     r.lse = lse;
     r.s = shape_of(a);
+    r.scale = a->scale;
     r.scale_log2 = (float)(a->scale * 1.4426950408889634);
     r.q_tiles = (a->q_tokens + 127) / 128;
     const uint64_t items = (uint64_t)r.q_tiles * a->q_heads * a->batch, kv_bytes = (uint64_t)a->k_tokens * a->head_dim * 4 + 1;

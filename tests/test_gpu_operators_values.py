@@ -96,6 +96,34 @@ def test_rows_whose_scores_are_all_minus_infinity_weigh_nothing(Sq, D, causal):
     assert torch.equal(got[0], dk) and torch.equal(got[1], dv)
 
 
+# Scores q0 k0 are exact: q0 a small number, k0 a power of two.  Up to 2^28 in f16, to 2^100 in bf16.
+@pytest.mark.parametrize("Sq", [3, 150])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,power", [(F16, 10), (F16, 14), (BF16, 10), (BF16, 14), (BF16, 22), (BF16, 27), (BF16, 31), (BF16, 50), (BF16, 100)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("scale", [0.125, 0.7])
+def test_very_large_scores_choose_the_largest(Sq, D, dtype, power, sign, scale):
+    """Rows of q0 in (1, 2), keys of k0 = +-2^power or, the ones that win, of a quarter more or less; the exact
+    result is the mean of the winners' values."""
+    head = 2.0 ** 14 if dtype == F16 else 1.0          # f16: a part of the exponent in q
+    q, k, v, g, out, *_ = case(Sq, D, dtype)
+    q.zero_()
+    q[:, :, 0, 0] = (1 + torch.arange(Sq, device=DEV).remainder(128) / 128) * head
+    q[:, :, 1, 0] = q[:, :, 0, 0]
+    k.zero_()
+    k[..., 0] = sign * 2.0 ** power
+    winners = [5, 6, 71, 134]
+    k[:, winners, 0, 0] = sign * 2.0 ** power * (1.25 if sign > 0 else 0.75)          # head 1: all keys alike
+    lse = op.run_attention(q, k, v, out, scale=scale)
+    u, x = op.U[dtype], v[0].double()
+    for h, who in ((0, winners), (1, list(range(k.shape[1])))):
+        want = x[who, h].mean(0)
+        op.within(out[0, :, h], want.expand(Sq, D), (u + op.EXP) * x[who, h].abs().mean(0) + 1.01 * u * want.abs(), "head %d" % h)
+        s = q[0, :, h, 0].double() * k[0, who[0], h, 0].double() * float(torch.tensor(scale, dtype=torch.float32))
+        want = s + math.log(len(who))
+        assert ((lse[0, h].double() - want).abs() <= 2.0 ** -21 * want.abs() + op.EXP).all()
+
+
 def exponents(dtype):
     """Every exponent from 0 down to -7 in steps of 1/256 (both types hold those below -4 in steps of 1/64 and more alike)."""
     x = -torch.arange(0, 7 * 256 + 1, dtype=torch.float64) / 256
