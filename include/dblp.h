@@ -44,7 +44,7 @@ typedef enum {
     DBLP_EALIGN = -2,    /* pointer or payload size not 16-byte aligned */
     DBLP_ECAPACITY = -3, /* a limit above is exceeded, or the workspace is too small */
     DBLP_ECUDA = -4,     /* a CUDA runtime call failed; text in dblp_last_error() */
-    DBLP_ETIMEOUT = -5   /* reserved: no call in this library waits on the device */
+    DBLP_ETIMEOUT = -5   /* reserved: waits inside kernels are bounded and counted, see dblp_wait_timeouts */
 } dblp_status_t;
 
 typedef enum { DBLP_F32 = 0, DBLP_BF16 = 1, DBLP_F16 = 2 } dblp_dtype_t; /* F16: worker-side operators only, not plans */

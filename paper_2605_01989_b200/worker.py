@@ -104,7 +104,7 @@ def train(rounds, workers=4, rows=512, heads=4, head_dim=64, batch=4, tokens=128
     g = torch.Generator(device=device)
     g.manual_seed(1)
     follow = torch.randperm(rows, generator=g, device=device, dtype=torch.int32)
-    losses = []
+    losses, gave_up = [], dblp.dblp_wait_timeouts()
     for r in range(1, rounds + 1):
         seen = []
         for w in ws:
@@ -115,6 +115,8 @@ def train(rounds, workers=4, rows=512, heads=4, head_dim=64, batch=4, tokens=128
         losses.append(torch.stack(seen).mean())
     out = [float(x) for x in losses]
     plan.close()
+    if dblp.dblp_wait_timeouts() != gave_up:
+        raise RuntimeError("a kernel gave up waiting: the gradients of some round are incomplete")
     return out
 
 
