@@ -8,7 +8,8 @@
 //              same m, so it cancels.  m moves only when the maximum has grown by more than 2^8, and only then is the
 //              accumulator rescaled; p stays below 2^8, exact enough in 16 bits and far from overflow.  x - m is one fused
 //              multiply-add with m rounded, off by up to 2^-24 |m| for the whole row alike; from |m| = kFar on, where that would show
-//              when m moves and in the end overflow, m is taken from s first, which is exact where it matters.
+//              when m moves and in the end overflow, scores are taken relative to m before the scale, which is exact where
+//              it matters (a half tile in which m then moves is read twice; having the case costs others 0 to 1.5 %).
 //   warps      0-3 softmax and epilogue, 4 TMA, 5 products.  Two blocks share an SM (96 KB of shared memory and 256 columns
 //              of tensor memory each), so that one's products run beside the other's exponentials.  The blocks are persistent:
 //              q and the first k and v of the next item are loaded, and its first scores computed, while the last item's
@@ -32,7 +33,7 @@ struct FwdArgs {
     Heads o;
     float* lse;
     AttnShape s;
-    float scale, scale_log2;
+    float scale_log2;
     uint32_t q_tiles, items, heads_together;
     unsigned long long* timeouts;
 };
@@ -70,6 +71,14 @@ template <int N> __device__ __forceinline__ void hide_from(uint32_t* x, uint32_t
 }
 
 constexpr float kFar = 4096.0f;
+
+// Scores relative to m, unless that is -infinity.
+template <int N> __device__ __forceinline__ void take_from(uint32_t* x, float m)
+{
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) - base);
+}
 
 template <int N> __device__ __forceinline__ float largest(const uint32_t* x)
 {
@@ -247,9 +256,11 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
         const uint32_t q0 = it.qt * 128, lq = uniform(length_of(a.s.q_lens, it.b, a.s.Sq)), lk = uniform(length_of(a.s.k_lens, it.b, a.s.Sk));
         const uint32_t nh = key_halves(a, q0, lq, lk);
         const uint32_t row = q0 + tid, seen = keys_of(row, lq, lk, a.s.causal);
-        float m = -INFINITY, l = 0.0f;
-        bool far = false;                                       // the same in all lanes
-        for (uint32_t h = 0; h < nh; ++h, ++count) {
+        // m: the row's reference.  Once far, the same in all lanes, scores are taken relative to it: it then counts as 0 (ref) and
+        // nothing is left to subtract (mc).
+        float m = -INFINITY, l = 0.0f, ref = -INFINITY, mc = 0.0f;
+        bool far = false;
+        for (uint32_t h = 0; h < nh;) {
             const uint32_t buf = count & 1, my_s = t_s + lane_base + buf * 64;
             ok = warp_wait(&s_full[buf], (count >> 1) & 1, g);
             if (!ok) break;
@@ -259,13 +270,19 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             tmem_ld32(my_s + 32, s + 32);
             tmem_wait_ld<64>(s);
             const uint32_t left = seen > h * 64 ? seen - h * 64 : 0;
-            if (__any_sync(0xFFFFFFFFu, left < 64)) hide_from<64>(s, left);
+            if (__any_sync(0xFFFFFFFFu, left < 64 || far)) {
+                hide_from<64>(s, left);
+                if (far) take_from<64>(s, m);
+            }
             const float top = largest<64>(s);
-            const bool move = top > m + grow;                   // also from -infinity
+            const bool move = top > ref + grow;                 // also from -infinity
             if (__any_sync(0xFFFFFFFFu, move)) {
-                const float alpha = move ? exp2_fast((m - top) * c) : 1.0f;                         // m = -infinity: 0
-                if (move) m = top;
-                far = __any_sync(0xFFFFFFFFu, m != -INFINITY && fabsf(m * c) > kFar);
+                const float before = m;
+                if (move) m = far && m != -INFINITY ? m + top : top;
+                const float alpha = move ? exp2_fast((before - m) * c) : 1.0f;                      // before = -infinity: 0
+                far = far || __any_sync(0xFFFFFFFFu, m != -INFINITY && fabsf(m * c) > kFar);
+                ref = far && m != -INFINITY ? 0.0f : m;
+                mc = far || m == -INFINITY ? 0.0f : -m * c;
                 l *= alpha;
                 if (h > 0) {                                    // the product of the half before still adds to the accumulator
                     ok = warp_wait(&pv_done, (count - 1) & 1, g);
@@ -281,13 +298,10 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                         tmem_st16(t_o + lane_base + i * 16, o);
                     }
                 }
-            }
-            float mc = m == -INFINITY ? 0.0f : -m * c;
-            if (far) {
-                const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-                for (int t = 0; t < 64; ++t) s[t] = __float_as_uint(__uint_as_float(s[t]) - base);
-                mc = 0.0f;
+                if (far) {                                      // this half again, relative to the new m (m only grows, to the largest score
+                    tmem_wait_st();                             // at the latest with the third reading)
+                    continue;
+                }
             }
             const float2 c2 = make_float2(c, c), mc2 = make_float2(mc, mc);
             float2 sum = make_float2(0.0f, 0.0f);
@@ -297,6 +311,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             tmem_wait_st();
             tc_fence_before();
             warp_arrive(&p_ready[buf]);
+            ++h;
+            ++count;
         }
         if (!ok) break;
         if (nh) {
@@ -330,8 +346,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
             }
         }
         if (a.lse && row < a.s.Sq)
-            a.lse[((uint64_t)it.b * a.s.Hq + it.h) * a.s.Sq + row] =
-                !seen ? -INFINITY : far ? fmaf(log2f(l), 0.693147180559945309f, m * a.scale) : (m * c + log2f(l)) * 0.693147180559945309f;
+            a.lse[((uint64_t)it.b * a.s.Hq + it.h) * a.s.Sq + row] = seen ? (m * c + log2f(l)) * 0.693147180559945309f : -INFINITY;
         }
     }
     __syncthreads();
@@ -365,7 +380,6 @@ int attention_forward(const dblp_attention_t* a, const dblp_heads_t* q, const db
     r.o = heads(out);
     r.lse = lse;
     r.s = shape_of(a);
-    r.scale = a->scale;
     r.scale_log2 = (float)(a->scale * 1.4426950408889634);
     r.q_tiles = (a->q_tokens + 127) / 128;
     const uint64_t items = (uint64_t)r.q_tiles * a->q_heads * a->batch, kv_bytes = (uint64_t)a->k_tokens * a->head_dim * 4 + 1;

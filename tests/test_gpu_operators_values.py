@@ -124,6 +124,26 @@ def test_very_large_scores_choose_the_largest(Sq, D, dtype, power, sign, scale):
         assert ((lse[0, h].double() - want).abs() <= 2.0 ** -21 * want.abs() + op.EXP).all()
 
 
+@pytest.mark.parametrize("Sq", [3, 150])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [8, 12, 16, 24, 31, 50, 100])
+@pytest.mark.parametrize("start", [-1.0, 1.0])
+def test_very_large_scores_that_rise_from_tile_to_tile(Sq, D, power, start):
+    """The largest score grows with every 32 keys, from small or from far below zero; the last eight keys win."""
+    q, k, v, g, out, *_ = case(Sq, D, BF16)
+    q.zero_()
+    q[..., 0] = (1 + torch.arange(Sq, device=DEV).remainder(128) / 128)[None, :, None]
+    k.zero_()
+    j = torch.arange(k.shape[1], device=DEV)
+    k[..., 0] = ((start + (j // 32) / 8) * 2.0 ** power)[None, :, None]
+    lse = op.run_attention(q, k, v, out, scale=0.7)
+    u, x = op.U[BF16], v[0, 192:].double()
+    want = x.mean(0)
+    op.within(out[0], want.expand(Sq, 2, D), (u + op.EXP) * x.abs().mean(0) + 1.01 * u * want.abs(), "out")
+    want = q[0, :, 0, 0].double() * k[0, 199, 0, 0].double() * float(torch.tensor(0.7, dtype=torch.float32)) + math.log(8)
+    assert ((lse[0].double() - want).abs() <= 2.0 ** -21 * want.abs() + op.EXP).all()
+
+
 def exponents(dtype):
     """Every exponent from 0 down to -7 in steps of 1/256 (both types hold those below -4 in steps of 1/64 and more alike)."""
     x = -torch.arange(0, 7 * 256 + 1, dtype=torch.float64) / 256
