@@ -492,7 +492,10 @@ def _counter(t):
 
 
 def _scratch(ws):
-    return (None, 0) if ws is None or ws.numel() == 0 else (ws.data_ptr(), ws.nbytes)
+    if ws is None or ws.numel() == 0:
+        return None, 0
+    _require(ws.is_contiguous(), "workspace: contiguous")
+    return ws.data_ptr(), ws.nbytes
 
 
 def dblp_embed(table, tokens, out, scale=1.0, padding=-1, bad_tokens=None, stream=None):

@@ -81,3 +81,14 @@ WIDE = (1 << 32) + 8
 def test_what_does_not_fit_in_32_bits_is_refused(anywhere, call):
     with pytest.raises(ValueError, match="32 bits"):
         call()
+
+
+@pytest.mark.parametrize("call", [
+    lambda ws: dblp.dblp_embed_grad(meta(2, 8), meta(2, dtype=torch.int32), meta(4, 8), ws, stream=0),
+    lambda ws: dblp.dblp_attention(*(meta(1, 5, 2, 64) for _ in range(4)), ws=ws, stream=0),
+    lambda ws: dblp.dblp_attention_grad(*(meta(1, 5, 2, 64) for _ in range(5)), meta(1, 2, 5, dtype=torch.float32),
+                                        *(meta(1, 5, 2, 64) for _ in range(3)), ws, stream=0)])
+def test_a_workspace_with_gaps_is_refused(anywhere, call):
+    """What lies in the gaps is not the workspace's to write."""
+    with pytest.raises(ValueError, match="workspace"):
+        call(meta(1 << 20, 2, dtype=torch.uint8)[:, 0])
