@@ -1,4 +1,4 @@
-"""Which tokens are padding, which are bad, and which count."""
+"""Which tokens are padding, which are bad, and which count; runs of a token in rows that no vector access may touch."""
 import pytest
 import torch
 
@@ -44,3 +44,17 @@ def test_only_a_row_of_the_table_is_a_padding_id(padding, dtype, n, width):
     want, tol = op.grad_and_bound(dout, tokens.long(), ROWS, 1.0, F32, padding=p)
     op.within(dtable, want, tol, "dtable")
     assert int(bad) == int((~inside).sum())
+
+
+@pytest.mark.parametrize("first", [0, 31, 32, 33, 16 * 32 - 1, 16 * 32, 16 * 32 + 1, 64 * 32 + 1])
+@pytest.mark.parametrize("length", [1, 32, 33, 16 * 32, 17 * 32, 33 * 32 + 5, 130 * 32])
+@pytest.mark.parametrize("width,dtype", [(7, F32), (129, BF16)])
+def test_embed_grad_runs_at_odd_widths(first, length, width, dtype):
+    """One long run between two others, around the boundaries of tiles of 32 and of groups of 16 tiles."""
+    rows = 5
+    tokens = torch.cat([torch.full((c,), v, dtype=torch.int32) for v, c in ((1, first), (2, length), (4, 50))])
+    tokens = tokens[torch.randperm(tokens.numel(), generator=torch.Generator().manual_seed(first + length))].to(DEV)
+    dout = op.randn((tokens.numel(), width), dtype, 78)
+    dtable = op.embed_grad(dout, tokens, rows, torch.full((rows, width), 5.0, dtype=dtype, device=DEV))
+    want, tol = op.grad_and_bound(dout, tokens, rows, 1.0, dtype)
+    op.within(dtable, want, tol, "dtable")
