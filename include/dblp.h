@@ -472,9 +472,11 @@ typedef struct {
  *     s_ij = scale * <q_i, k_j>,  i < lq, j < lk, with DBLP_ATTENTION_CAUSAL also j <= i + lk - lq (the last query
  *                                 sees every key)
  *     lse_i = log sum_j exp(s_ij),  out_i = sum_j exp(s_ij - lse_i) v_j
- * A query that sees no key, lies beyond lq, or has no score above -infinity, gets out = 0 and lse = -infinity, and has no part in
- * any gradient.  A score of NaN or +infinity makes its row of out NaN.  lse: fp32 [batch, q_heads, q_tokens], contiguous
- * (NULL = not wanted).
+ * A query that sees no key or lies beyond lq gets out = 0 and lse = -infinity and has no part in any gradient, whatever its q
+ * and dout hold; so does one with finite q and dout that has no score above -infinity.  A score of NaN or +infinity makes its
+ * row of out NaN, and its gradients.  What is not finite can, as 0 * NaN, reach more than the formulas say where only the
+ * causal mask is between: v_j the rows of out before j, q_i and dout_i the gradients of keys after i.
+ * lse: fp32 [batch, q_heads, q_tokens], contiguous (NULL = not wanted).
  * dblp_attention_grad: with D_i = <dout_i, out_i>, p_ij = exp(s_ij - lse_i) computed again from q, k and lse,
  *     ds_ij = p_ij (<dout_i, v_j> - D_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
  *     dv_j = sum_i p_ij dout_i;  shared key heads sum over their query heads.

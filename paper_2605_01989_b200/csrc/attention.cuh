@@ -42,13 +42,13 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const TileSource& src, u
         tma_tile(dst + s * kBlockBytes, &src.map, bar, s * 64, (int)token, (int)head * src.mh, (int)b * src.mb);
 }
 
-// Rows from `first` on of a 128-row tile become zero: what lies beyond a sequence may hold anything, and 0 * NaN is NaN
-// inside a product.  Called by one whole warp, for tiles that hold a sequence's end only.
+// Rows first .. last - 1 of a 128-row tile become zero: what lies beyond a sequence, or sees nothing, may hold anything, and
+// 0 * NaN is NaN inside a product.  Called by one whole warp, for tiles that hold such a boundary only.
 template <int NS>
-__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t first)
+__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t first, uint32_t last)
 {
     const uint32_t lane = threadIdx.x & 31;
-    for (uint32_t i = first * 8 + lane; i < 128 * 8; i += 32)
+    for (uint32_t i = first * 8 + lane; i < last * 8; i += 32)
 #pragma unroll
         for (int s = 0; s < NS; ++s) *reinterpret_cast<uint4*>(tile + s * kBlockBytes + i * 16) = make_uint4(0, 0, 0, 0);
     fence_async_smem();

@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_attention(const __grid_const
                     }
                     ok = warp_wait(&cut_full, cuts++ & 1, g);
                     if (!ok) break;
-                    clear_rows<NS>(dst, lk & 127);
+                    clear_rows<NS>(dst, lk & 127, 128);
                     __syncwarp();
                     if (lane == 0) bar_arrive(&full[st]);
                 }

@@ -176,15 +176,17 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 
     if (warp == kTmaWarp) {                                       // ---- TMA
         uint32_t n = 0, w = 0, cuts = 0;                        // pairs, key tiles with work, tiles that were cleared
+        const uint32_t unseeing = a.s.causal && lq > lk ? lq - lk : 0;          // queries before this one see no key
         bool ok = true;
-        // a tile whose rows from `first` on do not count but may hold anything
-        auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t first) -> bool {
+        // a tile of which only the rows of tokens from .. to - 1 count and the others may hold anything
+        auto load_cut = [&](uint8_t* dst, const TileSource& src, uint32_t token, uint32_t head, uint32_t from, uint32_t to) -> bool {
             if (lane == 0) {
                 bar_expect(&s.cut_full, L::TILE);
                 load_tile<NS>(dst, src, &s.cut_full, token, head, b);
             }
             if (!warp_wait(&s.cut_full, cuts++ & 1, g)) return false;
-            clear_rows<NS>(dst, first);
+            if (from > token) clear_rows<NS>(dst, 0, from - token);
+            if (to < token + 128) clear_rows<NS>(dst, to - token, 128);
             __syncwarp();
             return true;
         };
@@ -196,7 +198,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             if (w) ok = warp_wait(&s.acc_full, (w - 1) & 1, g);   // products of the tile before are done
             if (!ok) break;
             const bool kcut = j * 128 + 128 > lk && lk < a.s.Sk;
-            if (kcut) ok = load_cut(smem + L::K, a.k, j * 128, hk, lk - j * 128);
+            if (kcut) ok = load_cut(smem + L::K, a.k, j * 128, hk, 0, lk);
             if (!ok) break;
             if (lane == 0) {
                 bar_expect(&s.kv_full, kcut ? L::TILE : 2 * L::TILE);
@@ -206,12 +208,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
             ++w;
             for (uint32_t t = 0; t < per_head * heads && ok; ++t, ++n) {
                 const uint32_t h = h0 + t / per_head, i = nq - per_head + t % per_head;
-                const bool cut = i * 128 + 128 > lq && lq < a.s.Sq;
+                const bool cut = (i * 128 + 128 > lq && lq < a.s.Sq) || i * 128 < unseeing;
                 const uint32_t sq = n % NQ, sg = n % NG;
                 if (n >= NQ) ok = warp_wait(&s.q_empty[sq], (n / NQ - 1) & 1, g);
                 if (!ok) break;
                 uint8_t *dq_ = smem + L::Q + sq * L::TILE, *dg = smem + L::G + sg * L::TILE;
-                if (cut) ok = load_cut(dq_, a.q, i * 128, h, lq - i * 128);
+                if (cut) ok = load_cut(dq_, a.q, i * 128, h, unseeing, lq);
                 if (!ok) break;
                 if (lane == 0) {
                     bar_expect(&s.q_full[sq], (cut ? 0 : L::TILE) + 1024);
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
                     bulk_load(smem + L::ROWS + sq * 1024, a.rows + (((uint64_t)b * a.s.Hq + h) * a.q_tiles + i) * 256, 1024, &s.q_full[sq]);
                 }
                 if (n >= NG) ok = warp_wait(&s.g_empty[sg], (n / NG - 1) & 1, g);
-                if (ok && cut) ok = load_cut(dg, a.go, i * 128, h, lq - i * 128);
+                if (ok && cut) ok = load_cut(dg, a.go, i * 128, h, unseeing, lq);
                 if (!ok) { if (lane == 0) bar_drain(&s.q_full[sq], (n / NQ) & 1); break; }
                 if (lane == 0) {
                     if (cut) {

@@ -144,6 +144,28 @@ def test_very_large_scores_that_rise_from_tile_to_tile(Sq, D, power, start):
     assert ((lse[0].double() - want).abs() <= 2.0 ** -21 * want.abs() + op.EXP).all()
 
 
+@pytest.mark.parametrize("Sq,Sk,lens", [(4, 3, None), (300, 200, None), (260, 1, None), (130, 2, None), (400, 128, None), (300, 400, ([300, 200, 257, 40], [100, 200, 1, 0]))])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_that_see_nothing_may_hold_anything(Sq, Sk, lens, D):
+    """Causal, more queries than keys: the first ones see no key, and what they hold reaches neither result nor gradient."""
+    B = len(lens[0]) if lens else 2
+    q, k, v, g, out, dq, dk, dv = case(Sq, D, BF16, B=B, Sk=Sk)
+    kw = dict(causal=True, lens=op.lengths(lens))
+    got = []
+    for poison in (0.0, NAN, INF):
+        for b in range(B):
+            lq, lk = (lens[0][b], lens[1][b]) if lens else (Sq, Sk)
+            for t in (q, g):
+                t[b, :max(0, lq - lk)] = poison
+        lse = op.run_attention(q, k, v, out, **kw)
+        op.run_grad(q, k, v, out, g, lse, dq, dk, dv, **kw)
+        got.append([t.clone() for t in (out, lse, dq, dk, dv)])
+    assert all(torch.isfinite(t).all() for t in got[0] if t.dtype == BF16)
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(op.bits(a), op.bits(b))
+
+
 def exponents(dtype):
     """Every exponent from 0 down to -7 in steps of 1/256 (both types hold those below -4 in steps of 1/64 and more alike)."""
     x = -torch.arange(0, 7 * 256 + 1, dtype=torch.float64) / 256
