@@ -485,8 +485,12 @@ typedef struct {
  * out and lse are dblp_attention's for the same arguments.  Every element of dq, dk and dv is written (zero where
  * nothing contributes).  Scores, statistics and accumulators are fp32; p and ds are rounded to dtype where they enter a
  * product.
+ * With DBLP_F16, p or ds below 2^-25 vanishes where it is rounded: scale the loss so that dout is not tiny.
  * ws: dblp_attention_workspace_bytes() bytes (fwd for dblp_attention, grad for dblp_attention_grad; either may be 0),
- * 256-byte aligned, contents need not be preserved. */
+ * 256-byte aligned, contents need not be preserved.  The gradient's holds 8 bytes a query row and 1 to 32 copies of dq in
+ * fp32, head_dim rounded up to 64 or 128: one a share of the keys, as many as make the heads fill the device; where query heads
+ * share key heads also up to q_heads / kv_heads copies of dk and dv.  (1 sequence, 8192 tokens, 16 heads on 4 of 128: 672 MB; 131072
+ * tokens, 8 heads of 128: 9.7 GB.) */
 int dblp_attention_workspace_bytes(const dblp_attention_t* a, size_t* fwd_bytes, size_t* grad_bytes);
 int dblp_attention(const dblp_attention_t* a, const dblp_heads_t* q, const dblp_heads_t* k, const dblp_heads_t* v,
                    const dblp_heads_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);

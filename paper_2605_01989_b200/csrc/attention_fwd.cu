@@ -15,11 +15,13 @@
 //              q and the first k and v of the next item are loaded, and its first scores computed, while the last item's
 //              softmax and output are still under way.
 //   memory     k and v tiles pass through one ring, in the order in which the products use them.
-//   bound      with head_dim 64 the exponentials: 1024 cycles of the special function unit for 128 x 128 scores against 512 of
-//              the tensor cores; with 128 both alike.
-//   measured   8 x 1024 tokens, 25 heads of 64, causal: 57 to 59 us (460 TFLOP/s of what is not masked); 8192 x 8192, 16 heads
-//              of 64: 381 us (722 TFLOP/s); 8192 tokens, 16 heads of 128, causal: 254 us (1083 TFLOP/s).  With whole tiles of 128
-//              keys, one buffer: 73, 447 and 290 us.
+//   bound      with head_dim 64 no unit: special function unit 41 % busy, issue 49 %, tensor pipe 26 % (8 x 1024 tokens, 25 heads,
+//              causal).  128 x 128 scores cost 1024 cycles of the special function unit, 768 with a quarter taken off it, and 512
+//              of the tensor cores; what takes longer is the one softmax warp group a block, which waits, loads, reduces,
+//              exponentiates, stores and writes the output in turn.  With 128 columns both units are half busy.
+//   measured   8 x 1024 tokens, 25 heads of 64, causal: 58 us (461 TFLOP/s of what is not masked); 8192 x 8192, 16 heads of 64:
+//              375 to 386 us (712 to 733 TFLOP/s); 8192 tokens, 16 heads on 4 of 128, causal: 269 to 298 us (920 to 1020 TFLOP/s, by
+//              the clock that power allows).  When half tiles in two buffers replaced whole tiles in one, the first took 12 % less.
 #include <math.h>
 
 #include "attention.cuh"
@@ -94,9 +96,9 @@ template <int N> __device__ __forceinline__ float largest(const uint32_t* x)
 }
 
 // 32 scores -> 16 words of probabilities in tensor memory; their fp32 sum is added to `sum`.  Rounded to 16 bits because
-// that is the type of the product with v.  With head_dim up to 64 the exponentials bound the kernel and a quarter of them is
-// computed off the special function unit (8192 x 8192, 16 heads: 438 us with none, 414 an eighth, 400 a quarter, 453 half);
-// with 128 the products do, and the extra instructions cost (271 -> 276 us causal on 4 key heads).
+// that is the type of the product with v.  With head_dim up to 64 a quarter of them is computed off the special function unit
+// (8192 x 8192, 16 heads, measured when it came: none 10 % slower, an eighth 4 %, half 13 %); with 128 that unit has time while the
+// products run, and the extra instructions cost 2 % (causal, on 4 key heads).
 template <typename T, int DP>
 __device__ __forceinline__ void probabilities(const uint32_t* x, float2 c2, float2 mc2, float2& sum, uint32_t dst)
 {

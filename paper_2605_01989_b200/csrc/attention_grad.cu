@@ -17,11 +17,13 @@
 // fill the machine; each costs a buffer of q's size in fp32.
 //   warps         0-15 p and ds, each thread one key and 32 queries, with head_dim up to 64 in two groups half a step apart;
 //                 16-19 dq to memory, 20 TMA, 21 products.
-// Bound.  A pair of 128 x 128 tiles with head_dim 64 costs 1280 cycles of products, 1024 of exponentials and, for its 32 KB of
-// dq at the 16 bytes a cycle and SM that the L2 adds in fp32, about 2000; the chain between them makes it about 3600.  With
-// 128, dq has no columns of its own and dp of the next pair waits until it has been read.
-//   measured      8 x 1024 tokens, 25 heads of 64, causal: 192 us (349 TFLOP/s), of which rows 15 and dq 23; 8192 tokens, 16 heads
-//                 of 128 on 4, causal: 1.05 to 1.1 ms (625 to 658 TFLOP/s); 8192 x 8192, 16 heads of 64: 1.2 ms (570 TFLOP/s).
+// Bound.  A pair of 128 x 128 tiles with head_dim 64 costs 1280 cycles of products, 768 of exponentials (1024 without the quarter
+// that is taken off the special function unit) and, for its 32 KB of dq at the 16 bytes a cycle and SM that the L2 was measured to add
+// in fp32, about 2050; the chain between them makes it about 3600.  With 128, dq has no columns of its own and dp of the next
+// pair waits until it has been read.
+//   measured      8 x 1024 tokens, 25 heads of 64, causal: 188 us (357 TFLOP/s), of which rows and dq about 40; 8192 tokens, 16
+//                 heads of 128 on 4, causal: 1.05 to 1.12 ms (615 to 655 TFLOP/s); 8192 x 8192, 16 heads of 64: 1.14 to 1.17 ms
+//                 (585 to 602 TFLOP/s).
 #include <math.h>
 
 #include "attention.cuh"
@@ -58,7 +60,7 @@ __device__ __forceinline__ uint32_t first_query_tile(uint32_t j, uint32_t lq, ui
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
 // A block takes one tile of 128 rows, a warp 16 of them: eight lanes a row, 16 bytes a load, four rows a thread with their loads
-// in front (200 heads of 1024 x 64, caches cold: 15.5 us, one row a thread 16.6).
+// in front (200 heads of 1024 x 64, caches cold: 7 % less time than one row a thread).
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_grad_rows(Heads o, Heads go, const float* __restrict__ lse, float* __restrict__ rows, AttnShape s, uint32_t q_tiles)
@@ -245,7 +247,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
         // one computes p while the other computes ds.  The order below follows them: p of the first half, ds of the second
         // half of the pair before, ds of the first half, p of the second.  With 128 there is no room for that: dq takes the
         // columns of dp, so that dp of the next pair waits for dq in any case, and all warps take the whole pair together (8192
-        // tokens, 16 heads on 4, causal: 1.40 ms in halves).
+        // tokens, 16 heads on 4, causal: halves took 21 % longer).
         constexpr uint32_t id_kk = mma_desc<T>(128, 128 / NE, false, false);    // s, dp of a group
         constexpr uint32_t id_kv = mma_desc<T>(128, DP, false, true);           // dv, dk: right operand across its rows
         constexpr uint32_t id_dq = mma_desc<T>(128, DP, true, true);            // dq: both across their rows
@@ -537,7 +539,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const __grid_constant_
 }
 
 // ---- dq --------------------------------------------------------------------------------------------------------------
-// Thread: one query, 32 of its columns at a time (200 heads of 1024 x 64, two shares, caches cold: 22.8 us, 8 columns 25.9).  Share r has a part of query tile i iff its first key tile, r, meets it.
+// Thread: one query, 32 of its columns at a time (200 heads of 1024 x 64, two shares, caches cold: 12 % less time than 8 columns).  Share r
+// has a part of query tile i iff its first key tile, r, meets it.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_grad_dq(const float4* __restrict__ part, Heads dq, AttnShape s, float scale, uint32_t q_tiles, uint32_t shares)
 {

@@ -10,8 +10,9 @@
 // The gradient goes the same way with up to 4 rows: everything about a key (p, ds, and with them its dk and dv) is known to
 // the lanes that hold it, so dk and dv are written once and only dq is joined (k_grad_few_join).
 //
-// Measured: 8 sequences x 25 heads of 64, 1 query, 1024 keys (52 MB): 15.5 us, 3.4 TB/s; one wave of blocks whose 8 dependent
-// loads are the time.  The tensor-core kernel takes 27 us there, and 135 us for 8192 keys of 4 heads (here 13).
+// Measured: 8 sequences x 25 heads of 64, 1 query, 1024 keys (52 MB): 16 us, 3.3 TB/s; one wave of blocks whose 8 dependent
+// loads are the time.  The tensor-core kernel took 27 us there, and 135 us for 8192 keys, 16 heads on 4 of 128 (here 13).  The gradient
+// of 4 sequences, 16 heads on 4 of 128, 1 query, 4096 keys: 32 us, 90 in tiles.
 #include <math.h>
 
 #include "attention.cuh"

@@ -1,7 +1,7 @@
 // dblp_dropout, dblp_dropout_grad: out = [u(i) >= t] * x * 65536 / (65536 - t) [+ residual], u(i) = 16 bits of a Philox
 // draw that eight consecutive elements share.
 //
-// Bound by HBM: 32768 x 6400 fp32 243 us (6.9 TB/s) in bursts, 266 us (6.3) under sustained load, 295 with two 16-byte
+// Bound by HBM: 32768 x 6400 fp32 244 us (6.9 TB/s) in bursts, 264 us (6.4) under sustained load, 295 with two 16-byte
 // accesses in place of one of 32; 8192 x 1600 bf16 with residual 13.9 us.
 // Nothing is kept between forward and backward: the mask costs ten Philox rounds per eight elements (about five
 // instructions an element) instead of a byte or bit each to write and read.
@@ -32,7 +32,7 @@ __device__ __forceinline__ float drop_one(const DropKey& k, uint32_t bits, float
 
 // A thread takes kGroups<T> groups of eight elements of contiguous rows (cols % 8 == 0 and 16-byte aligned rows, or
 // everything one row of n elements), all loads before the first draw: one 16-byte load a thread leaves too few bytes in
-// flight (32768 x 6400 bf16: 176 us with one group, DRAM-bound with two).  The last group of the one-row form may be short.
+// flight (32768 x 6400 bf16: 176 us with one group, 153 with two, where DRAM is the bound).  The last group of the one-row form may be short.
 template <typename T> constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
 
 template <typename T, bool RES>

@@ -12,9 +12,10 @@
 //      crosses a tile's end leaves a partial sum.  Other warps of
 //      the launch write zeros to the rows that do not occur, so that reading dout and writing the table overlap;
 //   3. k_grad_join: joins the partial sums of crossing runs in tile order.
-// The floor is reading dout once and writing the table once.  Measured: 32768 x 1600 fp32 into 50257 rows 110 us (4.8 TB/s over
-// all), 8192 x 1024 bf16 into 30522 rows 32 us, where the chain of launches is the time; 29 tokens into 30522 x 1600 fp32
-// 30 us (6.5 TB/s).  The lookup: 8192 x 1600 fp32 14 us (5.3 TB/s), one token 1.8 us.
+// The floor is reading dout once and writing the table once.  Measured: 32768 x 1600 fp32 into 50257 rows 113 us (4.7 TB/s over
+// all; 101 us when it is added to what the table holds), 8192 x 1024 bf16 into 30522 rows 31 us, where the chain of launches is the
+// time; 29 tokens into 30522 x 1600 fp32 30 to 34 us (5.8 to 6.5 TB/s).  The lookup: 8192 x 1600 fp32 14 us (5.3 TB/s), one token
+// 1.9 us; 20000 x 769 bf16, rows that no vector access may touch, 17 us and the gradient 50.
 #include "types.cuh"
 
 namespace dblp {
@@ -72,7 +73,7 @@ k_embed(const TI* __restrict__ table, int64_t ts, int64_t rows, const I* __restr
 }
 
 // Any width, stride and alignment: one warp a row and slab of 256 columns, 8 a lane 32 apart, so that the token and the row's
-// place are worked out once (element by element with a division each: 33 us for 20000 x 769 bf16).
+// place are worked out once (element by element with a division each took twice the time for 20000 x 769 bf16).
 constexpr int kAnyCols = 8;
 
 template <typename I, typename TI, typename TO>
@@ -344,8 +345,8 @@ __device__ __forceinline__ void finish_row(T* p, uint32_t left, float* acc, floa
     store_group<T, G>(p, left, acc);
 }
 
-// Zeros to row `row` if no token names it; one row a warp (4 rows a warp: 51 instead of 47 us for 30522 x 1600 fp32 with 29
-// tokens, the last blocks run alone for longer).  A warp's store covers 512 bytes in one piece.
+// Zeros to row `row` if no token names it; one row a warp (4 rows a warp, with the stores of that time: 9 % slower for 30522 x 1600
+// fp32 with 29 tokens, the last blocks run alone for longer).  A warp's store covers 512 bytes in one piece.
 template <typename TO, int G>
 __device__ __forceinline__ void zero_row(uint32_t row, const uint32_t* __restrict__ seen, uint32_t width, TO* __restrict__ dtable, int64_t ts)
 {
