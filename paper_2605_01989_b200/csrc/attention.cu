@@ -71,6 +71,7 @@ static int check_shape(const char* who, const dblp_attention_t* a)
                  "%s: %u key heads do not divide %u query heads", who, a->kv_heads, a->q_heads);
     DBLP_REQUIRE((a->flags & ~(uint32_t)DBLP_ATTENTION_CAUSAL) == 0, DBLP_EINVAL, "%s: unknown flags %u", who, a->flags);
     DBLP_REQUIRE(a->scale > 0.0f && a->scale < INFINITY, DBLP_EINVAL, "%s: scale %g is not finite and positive", who, a->scale);
+    DBLP_REQUIRE(((uintptr_t)a->q_lens & 3) == 0 && ((uintptr_t)a->k_lens & 3) == 0, DBLP_EALIGN, "%s: lengths are not aligned to their type", who);
     DBLP_REQUIRE(a->batch < 65536 && a->q_heads < 65536 && a->q_tokens < (1u << 30) && a->k_tokens < (1u << 30), DBLP_ECAPACITY,
                  "%s: batch and heads below 65536, tokens below 2^30", who);
     return DBLP_OK;
@@ -144,6 +145,7 @@ extern "C" int dblp_attention(const dblp_attention_t* a, const dblp_heads_t* q, 
         DBLP_TRY(check_heads("attention", "k", a, k, a->k_tokens, a->kv_heads, false));
         DBLP_TRY(check_heads("attention", "v", a, v, a->k_tokens, a->kv_heads, false));
     }
+    DBLP_REQUIRE(((uintptr_t)lse & 3) == 0, DBLP_EALIGN, "attention: lse is not aligned to its type");
     DBLP_TRY(check_space("attention", ws, ws_bytes, attention_forward_space(a)));
     return attention_forward(a, q, k, v, out, lse, ws, (cudaStream_t)stream);
 }
@@ -160,6 +162,7 @@ extern "C" int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t
         DBLP_TRY(check_heads("attention_grad", "dout", a, dout, a->q_tokens, a->q_heads, false));
         DBLP_TRY(check_heads("attention_grad", "dq", a, dq, a->q_tokens, a->q_heads, true));
         DBLP_REQUIRE(lse, DBLP_EINVAL, "attention_grad: lse is null");
+        DBLP_REQUIRE(((uintptr_t)lse & 3) == 0, DBLP_EALIGN, "attention_grad: lse is not aligned to its type");
     }
     if (a->k_tokens) {
         DBLP_TRY(check_heads("attention_grad", "k", a, k, a->k_tokens, a->kv_heads, false));

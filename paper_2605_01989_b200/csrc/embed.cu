@@ -600,11 +600,12 @@ static bool vector_rows(const void* p, int64_t stride, uint64_t nrows, int es)
 
 using namespace dblp;
 
-static int check_tokens(const char* who, const void* tokens, uint32_t token_bytes, uint64_t rows, uint32_t width, int ta, int tb)
+static int check_tokens(const char* who, const void* tokens, uint32_t token_bytes, const void* bad, uint64_t rows, uint32_t width, int ta, int tb)
 {
     DBLP_REQUIRE(known_dtype(ta) && known_dtype(tb), DBLP_EINVAL, "%s: unknown dtype %d or %d", who, ta, tb);
     DBLP_REQUIRE(token_bytes == 4 || token_bytes == 8, DBLP_EINVAL, "%s: tokens of %u bytes (4 or 8)", who, token_bytes);
     DBLP_REQUIRE((uintptr_t)tokens % token_bytes == 0, DBLP_EALIGN, "%s: tokens are not aligned to their type", who);
+    DBLP_REQUIRE((uintptr_t)bad % 8 == 0, DBLP_EALIGN, "%s: bad_tokens is not aligned to its type", who);
     DBLP_REQUIRE(rows < (1ull << 31) && width < (1u << 30), DBLP_ECAPACITY, "%s: 2^31 rows or 2^30 columns or more", who);
     return DBLP_OK;
 }
@@ -613,7 +614,7 @@ extern "C" int dblp_embed(const void* table, int64_t table_stride, uint64_t rows
                           const void* tokens, uint32_t token_bytes, uint64_t n, int64_t padding, float scale, void* out,
                           int64_t out_stride, int out_dtype, uint64_t* bad_tokens, void* stream)
 {
-    const int rc = check_tokens("embed", tokens, token_bytes, rows, width, table_dtype, out_dtype);
+    const int rc = check_tokens("embed", tokens, token_bytes, bad_tokens, rows, width, table_dtype, out_dtype);
     if (rc != DBLP_OK) return rc;
     if (n == 0 || width == 0) return DBLP_OK;
     DBLP_REQUIRE(tokens && out && (table || rows == 0), DBLP_EINVAL, "embed: null pointer");
@@ -666,7 +667,7 @@ extern "C" int dblp_embed_grad(const void* dout, int64_t dout_stride, int dout_d
                                uint32_t width, int dtable_dtype, uint32_t flags, uint64_t* bad_tokens, void* ws, size_t ws_bytes,
                                void* stream)
 {
-    const int rc = check_tokens("embed_grad", tokens, token_bytes, rows, width, dout_dtype, dtable_dtype);
+    const int rc = check_tokens("embed_grad", tokens, token_bytes, bad_tokens, rows, width, dout_dtype, dtable_dtype);
     if (rc != DBLP_OK) return rc;
     DBLP_REQUIRE((flags & ~(uint32_t)DBLP_ACCUMULATE) == 0, DBLP_EINVAL, "embed_grad: unknown flags %u", flags);
     DBLP_REQUIRE(n < (1ull << 31), DBLP_ECAPACITY, "embed_grad: 2^31 tokens or more");

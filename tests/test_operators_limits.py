@@ -53,6 +53,30 @@ def test_a_large_workspace_is_counted_in_full():
     assert rc == 0 and g >= n * 8 * (128 * 4 + 8)
 
 
+A = refusals.A
+
+
+@pytest.mark.parametrize("name,args", [
+    ("dblp_embed", (A, 64, 10, 64, 0, A, 4, 5, -1, 1.0, A, 64, 0, A + 4, None)),
+    ("dblp_embed_grad", (A, 64, 0, A, 4, 5, -1, 1.0, A, 64, 10, 64, 0, 0, A + 4, A, 1 << 30, None))])
+def test_a_counter_off_its_boundary_is_refused(name, args):
+    rc, text = refusals.call(name, *args)
+    assert rc == EALIGN and "bad_tokens" in text
+
+
+@pytest.mark.parametrize("which", ["q_lens", "k_lens"])
+def test_lengths_off_their_boundary_are_refused(which):
+    for rc, text in (refusals.attention(**{which: A + 2}), refusals.attention_grad(**{which: A + 2})):
+        assert rc == EALIGN and "lengths" in text
+
+
+def test_lse_off_its_boundary_is_refused():
+    s, h = dblp.dblp_attention_t(**refusals.SHAPE), refusals.heads
+    forward = refusals.call("dblp_attention", C.byref(s), h(), h(), h(), h(), A + 2, None, 0, None)
+    for rc, text in (forward, refusals.attention_grad(lse=A + 1)):
+        assert rc == EALIGN and "lse" in text
+
+
 # Calls through the binding with tensors that have shapes and no memory: they end in a refusal, the binding's or the library's
 # for the null address.
 @pytest.fixture
