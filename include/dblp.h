@@ -498,6 +498,104 @@ int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t* q, const 
                         const dblp_heads_t* out, const dblp_heads_t* dout, const float* lse, const dblp_heads_t* dq,
                         const dblp_heads_t* dk, const dblp_heads_t* dv, void* ws, size_t ws_bytes, void* stream);
 
+/* dblp_norm_rotate: what stands between a projection and dblp_attention.  For every token and head of q, and of k,
+ *     r = 1 / sqrt(mean of x_i^2 over the head's head_dim elements + eps),  y_i = x_i r weight_i
+ * and the first rotary_dim columns of y are turned, pair by pair: pair i (i < rotary_dim / 2) is columns (i, i +
+ * rotary_dim / 2), with DBLP_ROTATE_INTERLEAVED columns (2 i, 2 i + 1), and
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * freqs[i].
+ * The angle is a 64-bit product reduced to one turn before it is rounded, so far positions lose nothing; the rest is fp32,
+ * rounded once.  The squares of a head must not add up beyond fp32 (elements up to about 10^18).  Heads are as for
+ * dblp_attention (data and strides multiples of 16 bytes); q_out may be q and k_out may be k (the same data and strides).
+ * dblp_norm_rotate_grad: with d = the gradient of the output turned back by -t,
+ *     dx_i = r weight_i d_i - x_i r^3 / head_dim * sum_j weight_j d_j x_j,  dweight_i = sum over tokens and heads of d_i x_i r,
+ * from the inputs of the forward call; dq may be dq_out and dk may be dk_out.  With DBLP_ACCUMULATE dweight is added to.
+ * Sums over tokens are fp32, in an order that the shapes fix; dweight is rounded once to weight_dtype.
+ * ws: dblp_norm_rotate_grad_workspace_bytes() bytes, 256-byte aligned, contents need not be preserved. */
+enum { DBLP_ROTATE_INTERLEAVED = 2 };
+typedef struct {
+    uint32_t batch, tokens;         /* batch * tokens * heads < 2^31 */
+    uint32_t q_heads, k_heads;      /* k_heads 0: no k, its pointers are not looked at */
+    uint32_t head_dim;              /* a multiple of 8, at most 256 */
+    uint32_t rotary_dim;            /* <= head_dim; a multiple of 16, interleaved of 2; 0 = no rotation */
+    int dtype, weight_dtype;        /* any */
+    uint32_t flags;                 /* DBLP_ROTATE_INTERLEAVED, for the gradient also DBLP_ACCUMULATE */
+    float eps;                      /* > 0, finite */
+    const int32_t* positions;       /* device; token t of sequence b is at positions[b * position_stride + t] */
+    int64_t position_stride;
+    const double* freqs;            /* device, rotary_dim / 2 angles in radians a position */
+} dblp_norm_rotate_t;
+/* weights: contiguous, head_dim elements; NULL = all ones */
+int dblp_norm_rotate(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* q_out,
+                     const dblp_heads_t* k, const void* k_weight, const dblp_heads_t* k_out, void* stream);
+int dblp_norm_rotate_grad_workspace_bytes(const dblp_norm_rotate_t* a, size_t* bytes);
+/* dq_weight, dk_weight NULL = not wanted (both NULL: no workspace needed) */
+int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* dq_out,
+                          const dblp_heads_t* dq, void* dq_weight, const dblp_heads_t* k, const void* k_weight,
+                          const dblp_heads_t* dk_out, const dblp_heads_t* dk, void* dk_weight, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* A matrix: element (r, c) at data + r * row_stride + c * col_stride, in elements.  "Rows" means col_stride = 1. */
+typedef struct {
+    void* data;
+    int64_t row_stride, col_stride;
+} dblp_matrix_t;
+
+typedef enum { DBLP_ACT_NONE = 0, DBLP_ACT_RELU = 1, DBLP_ACT_GELU = 2, DBLP_ACT_GELU_TANH = 3, DBLP_ACT_SILU = 4 } dblp_activation_t;
+typedef struct {
+    uint32_t rows, in, out;     /* x is rows x in, w is in x out; each below 2^31, workspaces below 2^62 bytes */
+    int dtype;                  /* DBLP_BF16 or DBLP_F16: of x, w, pre, dy, dx, and the residual of dx */
+    int out_dtype;              /* of out and its residual, for the gradient of dw: dtype or DBLP_F32 */
+    int bias_dtype;             /* of bias, for the gradient of dbias: any */
+    int activation;             /* dblp_activation_t */
+    uint32_t flags;             /* the gradient: 0 or DBLP_ACCUMULATE (dw and dbias are added to) */
+} dblp_linear_t;
+
+/* dblp_linear: z = x w + bias, out = act(z) + residual; pre = z, for the backward pass.  x, residual, pre, out: rows; w: one
+ * of its two strides is 1 (weights held as [out, in] are the transposed view).  bias: contiguous.  bias, residual, pre:
+ * NULL = none.  out may be the residual.  The product's operands are 16-bit, everything after that is fp32 and rounded
+ * once.  relu: max(z, 0), NaN stays; gelu: z Phi(z); gelu_tanh: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))); silu:
+ * z / (1 + exp(-z)).
+ * dblp_linear_grad: dx = (dy w^T + residual) * act'(pre), dw = x^T dy, dbias = sum of dy's rows.  `pre` belongs to the
+ * layer BEFORE: where x = act(pre) was that layer's output, dx is the gradient of its pre-activation, ready to be its dy;
+ * without an activation pre is NULL.  residual (of dx, NULL = none): the gradient that reaches x on another way.  relu' is
+ * 0 at 0 and NaN at NaN.  dx, dw, dbias: NULL = not wanted; dx may be the residual or pre.  dw: one of its strides is 1.
+ * Every sum over the rows or columns is fp32, in an order that the shapes, types and alignments fix.
+ * ws: dblp_linear_workspace_bytes() bytes for the same x, w and dy (NULL: forward only), 256-byte aligned, contents need not
+ * be preserved.  It holds copies of operands whose data or strides are not multiples of 16 bytes, and partial sums where
+ * few rows or a long sum are split over the device. */
+int dblp_linear_workspace_bytes(const dblp_linear_t* l, const dblp_matrix_t* x, const dblp_matrix_t* w, const dblp_matrix_t* dy,
+                                size_t* fwd_bytes, size_t* grad_bytes);
+int dblp_linear(const dblp_linear_t* l, const dblp_matrix_t* x, const dblp_matrix_t* w, const void* bias,
+                const dblp_matrix_t* residual, const dblp_matrix_t* pre, const dblp_matrix_t* out, void* ws, size_t ws_bytes,
+                void* stream);
+int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, const dblp_matrix_t* w,
+                     const dblp_matrix_t* residual, const dblp_matrix_t* pre, const dblp_matrix_t* dx, const dblp_matrix_t* dw,
+                     void* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* dblp_orthogonalize: an update whose singular values are brought near 1 by Newton-Schulz products, matrix by matrix:
+ *     X = x / (|x|_F + eps);  for each (a, b, c):  A = X X^T, X = a X + (b A + c A A) X;  out = scale X
+ * (with X^T X and X (b A + c A A) where x is taller than wide: the products are always those of the shorter side).
+ * Used on the mean of a round (Algorithm 3) before the weights are updated.
+ * The norm is summed in 64 bits.  X and A enter the products scaled by powers of two (1024 and 256) and rounded to f16; X itself is
+ * kept in two f16 words (22 bits), so that what rounding adds is not amplified with the small singular values.  With
+ * out_dtype BF16 each product is one of f16 operands: the result is off by about 2e-3 of its norm at most, as much as
+ * its rounding.  With out_dtype F32 or F16 the products are of both words (three products each): about 2e-5.
+ * Coefficients must keep the entries of X below 63 and those of A and b A + c A A below 255 (singular values up to about 2 do), beyond
+ * which they become infinite.  An x of zeros gives zeros.  NaN or infinity in a matrix spreads over that matrix alone.
+ * ws: dblp_orthogonalize_workspace_bytes() bytes, 256-byte aligned, contents need not be preserved. */
+enum { DBLP_ORTHOGONALIZE_STEPS = 16 };
+typedef struct {
+    uint32_t batch, rows, cols;         /* rows, cols <= 32768; batch < 65536 */
+    int x_dtype, out_dtype;             /* any */
+    uint32_t steps;                     /* 1 .. DBLP_ORTHOGONALIZE_STEPS */
+    const float* coefficients;          /* HOST, steps times (a, b, c), finite */
+    float eps;                          /* >= 0 */
+    float scale;                        /* finite */
+    int64_t x_batch_stride, x_row_stride, out_batch_stride, out_row_stride;  /* in elements */
+} dblp_orthogonalize_t;
+int dblp_orthogonalize_workspace_bytes(const dblp_orthogonalize_t* a, size_t* bytes);
+int dblp_orthogonalize(const dblp_orthogonalize_t* a, const void* x, void* out, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- diagnostics -----------------------------------------------------------------------------------------------*/
 const char* dblp_strerror(int status);
 const char* dblp_last_error(void);  /* HOST string, valid until the calling thread's next failing call */

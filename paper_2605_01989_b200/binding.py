@@ -14,7 +14,10 @@ LIB_PATH = os.path.join(HERE, "libdblp.so")
 DBLP_F32, DBLP_BF16, DBLP_F16 = 0, 1, 2
 DBLP_LOSS_NONE, DBLP_LOSS_IID, DBLP_LOSS_GE, DBLP_LOSS_MICROBURST = 0, 1, 2, 3
 DBLP_SUM, DBLP_MEAN, DBLP_OUT_BF16 = 0, 1, 2
-DBLP_ACCUMULATE, DBLP_ATTENTION_CAUSAL = 1, 1
+DBLP_ACCUMULATE, DBLP_ATTENTION_CAUSAL, DBLP_ROTATE_INTERLEAVED = 1, 1, 2
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+DBLP_ORTHOGONALIZE_STEPS = 16
+MUON_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5        # a published choice: singular values to within about 0.7 .. 1.2
 LOSS_KINDS = {"none": DBLP_LOSS_NONE, "iid": DBLP_LOSS_IID, "ge": DBLP_LOSS_GE, "microburst": DBLP_LOSS_MICROBURST}
 HDR_BYTES = 32
 COUNTER_FIELDS = ("n_arrived", "n_accepted", "n_dup", "n_stale", "n_invalid", "n_late")
@@ -57,6 +60,27 @@ class dblp_attention_t(C.Structure):
         ("dtype", C.c_int), ("flags", C.c_uint32), ("scale", C.c_float), ("q_lens", C.c_void_p), ("k_lens", C.c_void_p)]
 
 
+class dblp_norm_rotate_t(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("batch", "tokens", "q_heads", "k_heads", "head_dim", "rotary_dim")] + [
+        ("dtype", C.c_int), ("weight_dtype", C.c_int), ("flags", C.c_uint32), ("eps", C.c_float), ("positions", C.c_void_p),
+        ("position_stride", C.c_int64), ("freqs", C.c_void_p)]
+
+
+class dblp_matrix_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("col_stride", C.c_int64)]
+
+
+class dblp_linear_t(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("rows", "in_", "out")] + [
+        (n, C.c_int) for n in ("dtype", "out_dtype", "bias_dtype", "activation")] + [("flags", C.c_uint32)]
+
+
+class dblp_orthogonalize_t(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("batch", "rows", "cols")] + [("x_dtype", C.c_int), ("out_dtype", C.c_int),
+                ("steps", C.c_uint32), ("coefficients", C.POINTER(C.c_float)), ("eps", C.c_float), ("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("x_batch_stride", "x_row_stride", "out_batch_stride", "out_row_stride")]
+
+
 class RoundMarks:
     """Timing events for the stages of a whole-round call (torch events; the library records them)."""
 
@@ -89,6 +113,9 @@ EXPORTS = ("dblp_plan_create", "dblp_plan_destroy", "dblp_plan_query", "dblp_pla
            "dblp_select_bound", "dblp_round_send", "dblp_round_receive", "dblp_round_device", "dblp_round_host",
            "dblp_embed", "dblp_embed_grad_workspace_bytes", "dblp_embed_grad", "dblp_dropout", "dblp_dropout_grad",
            "dblp_attention_workspace_bytes", "dblp_attention", "dblp_attention_grad", "dblp_wait_timeouts",
+           "dblp_norm_rotate", "dblp_norm_rotate_grad_workspace_bytes", "dblp_norm_rotate_grad",
+           "dblp_linear_workspace_bytes", "dblp_linear", "dblp_linear_grad",
+           "dblp_orthogonalize_workspace_bytes", "dblp_orthogonalize",
            "dblp_strerror", "dblp_last_error", "dblp_launch_count")
 
 
@@ -119,6 +146,15 @@ def lib():
         L.dblp_attention_workspace_bytes.argtypes = [at, sz, sz]
         L.dblp_attention.argtypes = [at, hd, hd, hd, hd, vp, vp, C.c_size_t, vp]
         L.dblp_attention_grad.argtypes = [at] + [hd] * 5 + [vp] + [hd] * 3 + [vp, C.c_size_t, vp]
+        nr, ln, mx, og = (C.POINTER(t) for t in (dblp_norm_rotate_t, dblp_linear_t, dblp_matrix_t, dblp_orthogonalize_t))
+        L.dblp_norm_rotate.argtypes = [nr, hd, vp, hd, hd, vp, hd, vp]
+        L.dblp_norm_rotate_grad_workspace_bytes.argtypes = [nr, sz]
+        L.dblp_norm_rotate_grad.argtypes = [nr, hd, vp, hd, hd, vp, hd, vp, hd, hd, vp, vp, C.c_size_t, vp]
+        L.dblp_linear_workspace_bytes.argtypes = [ln, mx, mx, mx, sz, sz]
+        L.dblp_linear.argtypes = [ln, mx, mx, vp, mx, mx, mx, vp, C.c_size_t, vp]
+        L.dblp_linear_grad.argtypes = [ln] + [mx] * 7 + [vp, vp, C.c_size_t, vp]
+        L.dblp_orthogonalize_workspace_bytes.argtypes = [og, sz]
+        L.dblp_orthogonalize.argtypes = [og, vp, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -620,6 +656,180 @@ def dblp_attention_grad(q, k, v, out, dout, lse, dq, dk, dv, ws, causal=False, s
                                      _heads(out, "out", dt, qs), _heads(dout, "dout", dt, qs), _lse(lse, qs),
                                      _heads(dq, "dq", dt, qs), _heads(dk, "dk", dt, ks), _heads(dv, "dv", dt, ks), wp, wb,
                                      _raw_stream(stream)), "dblp_attention_grad")
+
+
+def _norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps, flags):
+    """(the call's description, q's shape, k's shape or None)"""
+    _require(q.dim() == 4 and (k is None or k.dim() == 4), "q and k: [batch, tokens, heads, head_dim]")
+    qs, ks = q.shape, None if k is None else k.shape
+    B, T, Hq, D = qs
+    if k is not None:
+        _require(ks[0] == B and ks[1] == T and ks[3] == D and k.dtype == q.dtype, "q and k: one batch, length, head_dim and dtype")
+    w = q_weight if q_weight is not None else k_weight
+    for t in (q_weight, k_weight):
+        if t is not None and not (t.dtype == w.dtype and t.shape == (D,) and t.is_contiguous()):
+            raise ValueError("weights: contiguous, one per column of a head, of one dtype")
+    if max(B, T, Hq, D, 0 if ks is None else ks[2]) >= 1 << 32:
+        raise ValueError("an extent of q or k does not fit in 32 bits")
+    n = 0 if freqs is None else freqs.numel()
+    pp = fp = None
+    stride = 0
+    if n:
+        _require(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(), "freqs: 1-D, contiguous, float64")
+        _require(positions is not None and positions.dtype == torch.int32 and positions.shape == (B, T)
+                 and (T <= 1 or positions.stride(1) == 1), "positions: int32 [batch, tokens], the tokens of a sequence contiguous")
+        pp, fp, stride = positions.data_ptr(), freqs.data_ptr(), positions.stride(0)
+    return dblp_norm_rotate_t(B, T, Hq, 0 if ks is None else ks[2], D, _u32(2 * n, "rotary_dim"), _dtype(q),
+                              DBLP_F32 if w is None else _dtype(w), flags, eps, pp, stride, fp), qs, ks
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _pair(t, name, dtype, shape):
+    if shape is None:
+        _require(t is None, "%s: there is no k" % name)
+        return None
+    _require(t is not None, "%s: missing" % name)
+    return _heads(t, name, dtype, shape)
+
+
+def dblp_norm_rotate(q, k, q_weight, k_weight, positions, freqs, q_out, k_out, eps=1e-6, interleaved=False, stream=None):
+    """Norm of every head of q and k [batch, tokens, heads, head_dim] and rotation of the first 2 len(freqs) columns by
+    positions [batch, tokens] (int32) times freqs (float64, radians a position).  k, k_weight and k_out may be None; weights None
+    = ones; freqs None = no rotation."""
+    _on_device(q, k, q_weight, k_weight, positions, freqs, q_out, k_out)
+    a, qs, ks = _norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps, DBLP_ROTATE_INTERLEAVED if interleaved else 0)
+    dt = q.dtype
+    _check(lib().dblp_norm_rotate(C.byref(a), _heads(q, "q", dt, qs), _address(q_weight), _heads(q_out, "q_out", dt, qs),
+                                  _pair(k, "k", dt, ks), _address(k_weight), _pair(k_out, "k_out", dt, ks), _raw_stream(stream)),
+           "dblp_norm_rotate")
+
+
+def dblp_norm_rotate_grad_workspace_bytes(q, k):
+    b = C.c_size_t()
+    a = _norm_rotate(q, k, None, None, None, None, 1.0, 0)[0]
+    _check(lib().dblp_norm_rotate_grad_workspace_bytes(C.byref(a), C.byref(b)), "dblp_norm_rotate_grad_workspace_bytes")
+    return int(b.value)
+
+
+def dblp_norm_rotate_grad(q, k, q_weight, k_weight, positions, freqs, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None,
+                          ws=None, eps=1e-6, interleaved=False, accumulate=False, stream=None):
+    """Gradients of dblp_norm_rotate's q, k and weights, from its inputs and the gradients of its outputs."""
+    _on_device(q, k, q_weight, k_weight, positions, freqs, dq_out, dk_out, dq, dk, dq_weight, dk_weight, ws)
+    flags = (DBLP_ROTATE_INTERLEAVED if interleaved else 0) | (DBLP_ACCUMULATE if accumulate else 0)
+    a, qs, ks = _norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps, flags)
+    dt = q.dtype
+    for t in (dq_weight, dk_weight):
+        if t is None:
+            continue
+        if q_weight is None and k_weight is None:
+            _require(dq_weight is None or dk_weight is None or dq_weight.dtype == dk_weight.dtype, "gradients of the weights: one dtype")
+            a.weight_dtype = _dtype(t)
+        elif _dtype(t) != a.weight_dtype:
+            raise ValueError("gradients of the weights: the weights' dtype")
+        _require(t.shape == (qs[3],) and t.is_contiguous(), "gradients of the weights: contiguous, one per column of a head")
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_norm_rotate_grad(C.byref(a), _heads(q, "q", dt, qs), _address(q_weight), _heads(dq_out, "dq_out", dt, qs),
+                                       _heads(dq, "dq", dt, qs), _address(dq_weight), _pair(k, "k", dt, ks), _address(k_weight),
+                                       _pair(dk_out, "dk_out", dt, ks), _pair(dk, "dk", dt, ks), _address(dk_weight), wp, wb,
+                                       _raw_stream(stream)), "dblp_norm_rotate_grad")
+
+
+def _matrix(t, name, rows, cols, dtype):
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise ValueError("%s: %d x %d, %s" % (name, rows, cols, dtype))
+    rs, cs = t.stride()
+    return C.byref(dblp_matrix_t(t.data_ptr(), rs, cs))
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError("activation %r: one of %s" % (name, ", ".join(map(repr, ACTIVATIONS))))
+    return ACTIVATIONS[name]
+
+
+def _linear(x, w, out_dtype, bias, activation, flags):
+    _require(x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[0], "x and w: rows x in, in x out")
+    n, i, o = x.shape[0], x.shape[1], w.shape[1]
+    _require(w.dtype == x.dtype, "x and w: one dtype")
+    if max(n, i, o) >= 1 << 32:
+        raise ValueError("an extent does not fit in 32 bits")
+    if bias is not None and not (bias.shape == (o,) and bias.is_contiguous()):
+        raise ValueError("bias and its gradient: contiguous, one per column of w")
+    dt = _dtype(x)
+    return dblp_linear_t(n, i, o, dt, dt if out_dtype is None else _DTYPES.get(out_dtype, -1), DBLP_F32 if bias is None else _dtype(bias),
+                         _activation(activation), flags), n, i, o
+
+
+def dblp_linear_workspace_bytes(x, w, dy=None):
+    """(bytes for dblp_linear, bytes for dblp_linear_grad) with these tensors; the second is 0 without dy."""
+    l, n, i, o = _linear(x, w, None, None, None, 0)
+    f, g = C.c_size_t(), C.c_size_t()
+    _check(lib().dblp_linear_workspace_bytes(C.byref(l), _matrix(x, "x", n, i, x.dtype), _matrix(w, "w", i, o, x.dtype),
+                                             None if dy is None else _matrix(dy, "dy", n, o, x.dtype), C.byref(f), C.byref(g)),
+           "dblp_linear_workspace_bytes")
+    return int(f.value), int(g.value)
+
+
+def dblp_linear(x, w, out, ws=None, bias=None, residual=None, pre=None, activation=None, stream=None):
+    """out = act(x w + bias) + residual, pre = x w + bias; x [rows, in], w [in, out] (or the transposed view of [out, in])."""
+    _on_device(x, w, out, ws, bias, residual, pre)
+    l, n, i, o = _linear(x, w, out.dtype, bias, activation, 0)
+    dt, od = x.dtype, out.dtype
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_linear(C.byref(l), _matrix(x, "x", n, i, dt), _matrix(w, "w", i, o, dt), _address(bias),
+                             None if residual is None else _matrix(residual, "residual", n, o, od),
+                             None if pre is None else _matrix(pre, "pre", n, o, dt), _matrix(out, "out", n, o, od), wp, wb,
+                             _raw_stream(stream)), "dblp_linear")
+
+
+def dblp_linear_grad(dy, x, w, dx=None, dw=None, dbias=None, ws=None, residual=None, pre=None, activation=None, accumulate=False,
+                     stream=None):
+    """dx = (dy w^T + residual) act'(pre), with pre and the activation those of the layer that made x; dw = x^T dy; dbias = sum of
+    dy's rows.  With accumulate, dw and dbias are added to."""
+    _on_device(dy, x, w, dx, dw, dbias, ws, residual, pre)
+    l, n, i, o = _linear(x, w, None if dw is None else dw.dtype, dbias, activation, DBLP_ACCUMULATE if accumulate else 0)
+    dt = x.dtype
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_linear_grad(C.byref(l), _matrix(dy, "dy", n, o, dt), _matrix(x, "x", n, i, dt), _matrix(w, "w", i, o, dt),
+                                  None if residual is None else _matrix(residual, "residual", n, i, dt),
+                                  None if pre is None else _matrix(pre, "pre", n, i, dt),
+                                  None if dx is None else _matrix(dx, "dx", n, i, dt),
+                                  None if dw is None else _matrix(dw, "dw", i, o, dw.dtype), _address(dbias), wp, wb,
+                                  _raw_stream(stream)), "dblp_linear_grad")
+
+
+def _orthogonalize(x, out, coefficients, eps, scale):
+    _require(x.dim() in (2, 3) and x.shape == out.shape, "x and out: one shape, [rows, cols] or [batch, rows, cols]")
+    b = x.shape[0] if x.dim() == 3 else 1
+    m, n = x.shape[-2:]
+    if max(b, m, n) >= 1 << 32:
+        raise ValueError("an extent does not fit in 32 bits")
+    for t, name in ((x, "x"), (out, "out")):
+        _require(n <= 1 or t.stride(-1) == 1, "%s: contiguous within a row" % name)
+    flat = [float(v) for abc in coefficients for v in abc]
+    _require(len(flat) == 3 * len(coefficients), "coefficients: triples (a, b, c)")
+    each = [t.stride(0) if x.dim() == 3 else 0 for t in (x, out)]
+    return dblp_orthogonalize_t(b, m, n, _dtype(x), _dtype(out), len(coefficients), (C.c_float * max(1, len(flat)))(*flat), eps, scale,
+                                each[0], x.stride(-2), each[1], out.stride(-2))
+
+
+def dblp_orthogonalize_workspace_bytes(x, out):
+    b = C.c_size_t()
+    a = _orthogonalize(x, out, MUON_COEFFICIENTS, 0.0, 1.0)
+    _check(lib().dblp_orthogonalize_workspace_bytes(C.byref(a), C.byref(b)), "dblp_orthogonalize_workspace_bytes")
+    return int(b.value)
+
+
+def dblp_orthogonalize(x, out, ws, coefficients=MUON_COEFFICIENTS, eps=1e-7, scale=1.0, stream=None):
+    """out = scale times x with its singular values brought near 1, by one Newton-Schulz product a X + b X X^T X + c (X X^T)^2 X per
+    triple; x [rows, cols] or [batch, rows, cols].  out may be x."""
+    _on_device(x, out, ws)
+    a = _orthogonalize(x, out, coefficients, eps, scale)
+    wp, wb = _scratch(ws)
+    _check(lib().dblp_orthogonalize(C.byref(a), x.data_ptr(), out.data_ptr(), wp, wb, _raw_stream(stream)), "dblp_orthogonalize")
 
 
 def dblp_wait_timeouts():

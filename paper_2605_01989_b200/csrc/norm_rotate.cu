@@ -1,0 +1,523 @@
+// dblp_norm_rotate, dblp_norm_rotate_grad: root-mean-square norm of every head of q and k, and the rotation by position.
+//
+// A head's row of D elements belongs to L = D / 8 lanes (rounded up to a power of two), eight elements each: the norm is a
+// shuffle reduction, the other half of a rotated pair is in the same lane (interleaved) or comes from lane +- R / 16.
+// Cosines and sines of a block's tokens are computed once per block into shared memory: the angle, pos * freq / 2 pi, in
+// 64 bits, less its nearest integer, then one fp32 sincospi.
+// The backward pass recomputes r from x instead of reading a stored one: x is needed anyway.
+#include <math.h>
+
+#include "types.cuh"
+
+namespace dblp {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotRows = 4;                      // rows in flight per lane group
+
+struct RotHeads {
+    const void* p;
+    int64_t sb, st, sh;
+};
+
+// q or k: rows number token * heads + head
+struct RotSide {
+    RotHeads x, d;                               // input; gradient of the output
+    RotHeads y;                                  // output; gradient of the input
+    const void* weight;
+    uint32_t heads, rows, blocks;
+    FastDiv by_heads;
+    float* partial;                              // [blocks][D] sums of the weight's gradient, or null
+};
+
+struct RotArgs {
+    RotSide side[2];
+    uint32_t tokens, D, R, L, weight_dtype, table_tokens;
+    FastDiv by_tokens;
+    float eps, inv_d;
+    const int32_t* positions;
+    int64_t position_stride;
+    const double* freqs;
+};
+
+template <typename T> __device__ __forceinline__ Vec8<T> shuffle8(const Vec8<T>& v, uint32_t from)
+{
+    constexpr int W = sizeof(Vec8<T>) / 4;
+    Vec8<T> r;
+    const uint32_t* a = reinterpret_cast<const uint32_t*>(&v);
+    uint32_t* b = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+    for (int i = 0; i < W; ++i) b[i] = __shfl_sync(0xFFFFFFFFu, a[i], from);
+    return r;
+}
+
+__device__ __forceinline__ void load_weight(const void* w, uint32_t dtype, uint32_t c, uint32_t D, float* out)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float v = 1.0f;
+        if (w && c + i < D)
+            v = dtype == DBLP_F32 ? ((const float*)w)[c + i]
+                                  : (dtype == DBLP_BF16 ? to_f32(((const __nv_bfloat16*)w)[c + i]) : to_f32(((const __half*)w)[c + i]));
+        out[i] = v;
+    }
+}
+
+// (cos, sin) of the angles of tokens first .. first + n - 1 (of batch * tokens in all), R / 2 each.
+__device__ __forceinline__ void fill_angles(const RotArgs& a, float2* table, uint32_t first, uint32_t n)
+{
+    const uint32_t half = a.R / 2;
+    for (uint32_t i = threadIdx.x; i < n * half; i += kRotThreads) {
+        const uint32_t j = i / half, f = i - j * half, t = first + j, b = a.by_tokens.div(t);
+        const double turns = (double)a.positions[(int64_t)b * a.position_stride + (t - b * a.tokens)] * a.freqs[f] * 0.15915494309189533577;
+        float s, c;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        table[i] = make_float2(c, s);
+    }
+}
+
+// Columns c .. c + 7 of a row turned: mine holds them, other the other members of their pairs (not used when interleaved);
+// dir = 1 forward, -1 back.
+template <bool INTER>
+__device__ __forceinline__ void turn(float* mine, const float* other, const float2* angles, uint32_t c, uint32_t R, float dir)
+{
+    if (INTER) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (c + 2 * i >= R) break;
+            const float2 cs = angles[c / 2 + i];
+            const float x = mine[2 * i], y = mine[2 * i + 1], s = dir * cs.y;
+            mine[2 * i] = x * cs.x - y * s;
+            mine[2 * i + 1] = x * s + y * cs.x;
+        }
+    } else if (c < R) {
+        const uint32_t half = R / 2;
+        const float s = c < half ? -dir : dir;
+        const float4* at = reinterpret_cast<const float4*>(angles + (c < half ? c : c - half));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 v = at[i];
+            mine[2 * i] = mine[2 * i] * v.x + other[2 * i] * (s * v.y);
+            mine[2 * i + 1] = mine[2 * i + 1] * v.z + other[2 * i + 1] * (s * v.w);
+        }
+    }
+}
+
+struct RotRow {
+    bool live;
+    uint32_t token, b, t, h;
+};
+__device__ __forceinline__ RotRow row_of(const RotArgs& a, const RotSide& s, uint32_t row)
+{
+    RotRow r;
+    r.live = row < s.rows;
+    const uint32_t x = r.live ? row : 0;
+    r.token = s.by_heads.div(x);
+    r.h = x - r.token * s.heads;
+    r.b = a.by_tokens.div(r.token);
+    r.t = r.token - r.b * a.tokens;
+    return r;
+}
+__device__ __forceinline__ int64_t place(const RotHeads& h, const RotRow& r) { return (int64_t)r.b * h.sb + (int64_t)r.t * h.st + (int64_t)r.h * h.sh; }
+
+// Forward: a block takes kRotRows * kRotThreads / L rows of one side, once.
+template <typename T, bool INTER> __global__ void __launch_bounds__(kRotThreads) k_norm_rotate(const __grid_constant__ RotArgs a)
+{
+    extern __shared__ float2 table[];
+    const bool second = blockIdx.x >= a.side[0].blocks;
+    const RotSide& s = a.side[second];
+    const uint32_t block = blockIdx.x - (second ? a.side[0].blocks : 0), L = a.L, per = kRotThreads / L;
+    const uint32_t lane = threadIdx.x & 31, sub = threadIdx.x & (L - 1), c = sub * 8, group = threadIdx.x / L;
+    const uint32_t r0 = block * per * kRotRows;
+    const bool has = c < a.D;
+
+    Vec8<T> x[kRotRows];
+    RotRow row[kRotRows];
+#pragma unroll
+    for (int u = 0; u < kRotRows; ++u) {
+        row[u] = row_of(a, s, r0 + u * per + group);
+        row[u].live = row[u].live && has;
+        if (row[u].live) x[u].load((const T*)s.x.p + place(s.x, row[u]) + c);
+        else {
+            const float zero[8] = {};
+            x[u].set(zero);
+        }
+    }
+    const uint32_t first = s.by_heads.div(r0), last = s.by_heads.div(min(r0 + per * kRotRows, s.rows) - 1);
+    if (a.R) fill_angles(a, table, first, last - first + 1);
+    const uint32_t half = a.R / 2, from = c < half ? lane + a.R / 16 : (c < a.R ? lane - a.R / 16 : lane);
+    float w[8], wo[8];
+    load_weight(s.weight, a.weight_dtype, c, a.D, w);
+    if (!INTER) load_weight(s.weight, a.weight_dtype, c < half ? c + half : (c < a.R ? c - half : c), a.D, wo);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kRotRows; ++u) {
+        float v[8], o[8], ss = 0.0f;
+        x[u].get(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss += v[i] * v[i];
+        for (uint32_t m = L / 2; m; m >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
+        const float r = rsqrtf(ss * a.inv_d + a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= r * w[i];
+        if (!INTER && a.R) {
+            shuffle8<T>(x[u], from).get(o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] *= r * wo[i];
+        }
+        if (row[u].live) {
+            if (a.R) turn<INTER>(v, o, table + (row[u].token - first) * half, c, a.R, 1.0f);
+            Vec8<T> y;
+            y.set(v);
+            y.store((T*)s.y.p + place(s.y, row[u]) + c);
+        }
+    }
+}
+
+// Backward: a block walks over rows of one side, a stride of the side's blocks apart, and keeps its share of the weight's
+// gradient in registers; one barrier a step, since the angles of two steps alternate between two tables.
+template <typename T, bool INTER> __global__ void __launch_bounds__(kRotThreads) k_norm_rotate_grad(const __grid_constant__ RotArgs a)
+{
+    extern __shared__ float2 tables[];
+    after_start();
+    const bool second = blockIdx.x >= a.side[0].blocks;
+    const RotSide& s = a.side[second];
+    const uint32_t block = blockIdx.x - (second ? a.side[0].blocks : 0), L = a.L, per = kRotThreads / L;
+    const uint32_t lane = threadIdx.x & 31, sub = threadIdx.x & (L - 1), c = sub * 8, group = threadIdx.x / L;
+    const uint32_t half = a.R / 2, from = c < half ? lane + a.R / 16 : (c < a.R ? lane - a.R / 16 : lane);
+    const bool has = c < a.D;
+    float w[8], dw[8] = {};
+    load_weight(s.weight, a.weight_dtype, c, a.D, w);
+
+    constexpr int U = kRotRows / 2;
+    uint32_t step = 0;
+    for (uint64_t r0 = (uint64_t)block * per * U; r0 < s.rows; r0 += (uint64_t)s.blocks * per * U, ++step) {
+        Vec8<T> x[U], g[U];
+        RotRow row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row[u] = row_of(a, s, (uint32_t)r0 + u * per + group);
+            row[u].live = row[u].live && has;
+            if (row[u].live) {
+                x[u].load((const T*)s.x.p + place(s.x, row[u]) + c);
+                g[u].load((const T*)s.d.p + place(s.d, row[u]) + c);
+            } else {
+                const float zero[8] = {};
+                x[u].set(zero);
+                g[u].set(zero);
+            }
+        }
+        float2* table = tables + (step & 1) * a.table_tokens * half;
+        const uint32_t first = s.by_heads.div((uint32_t)r0), last = s.by_heads.div(min((uint32_t)r0 + per * U, s.rows) - 1);
+        if (a.R) fill_angles(a, table, first, last - first + 1);
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[8], d[8], o[8], ss = 0.0f, dot = 0.0f;
+            x[u].get(v);
+            g[u].get(d);
+            if (!INTER && a.R) shuffle8<T>(g[u], from).get(o);
+            if (row[u].live && a.R) turn<INTER>(d, o, table + (row[u].token - first) * half, c, a.R, -1.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                ss += v[i] * v[i];
+                dot += w[i] * d[i] * v[i];
+            }
+            for (uint32_t m = L / 2; m; m >>= 1) {
+                ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
+                dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+            }
+            const float r = rsqrtf(ss * a.inv_d + a.eps), q = dot * a.inv_d * r * r * r;
+            if (row[u].live) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dw[i] += d[i] * v[i] * r;
+                    y[i] = r * w[i] * d[i] - v[i] * q;
+                }
+                Vec8<T> out;
+                out.set(y);
+                out.store((T*)s.y.p + place(s.y, row[u]) + c);
+            }
+        }
+    }
+    if (!s.partial) return;
+    // the block's sum of its lane groups, in their order
+    __syncthreads();
+    float* sum = reinterpret_cast<float*>(tables);                      // kRotThreads * 8 floats
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[(group * L + sub) * 8 + i] = dw[i];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < a.D; i += kRotThreads) {
+        float t = 0.0f;
+        for (uint32_t k = 0; k < per; ++k) t += sum[k * L * 8 + i];
+        s.partial[(size_t)block * a.D + i] = t;
+    }
+}
+
+// The weights' gradients from the blocks' sums: 8 threads a column take every eighth block, then add up in order.
+struct RotJoin {
+    const float* partial[2];
+    void* dw[2];
+    uint32_t blocks[2], D, dtype, accumulate;
+};
+__global__ void __launch_bounds__(256) k_rotate_join(RotJoin j)
+{
+    __shared__ float part[8][32];
+    const int side = blockIdx.y;
+    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    float t = 0.0f;
+    wait_before();
+    after_start();
+    if (!j.dw[side]) return;
+    if (c < j.D)
+        for (uint32_t b = y; b < j.blocks[side]; b += 8) t += j.partial[side][(size_t)b * j.D + c];
+    part[y][x] = t;
+    __syncthreads();
+    if (y || c >= j.D) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += part[i][x];
+    if (j.dtype == DBLP_F32) {
+        float* p = (float*)j.dw[side] + c;
+        *p = j.accumulate ? *p + t : t;
+    } else if (j.dtype == DBLP_BF16) {
+        __nv_bfloat16* p = (__nv_bfloat16*)j.dw[side] + c;
+        *p = from_f32<__nv_bfloat16>(j.accumulate ? to_f32(*p) + t : t);
+    } else {
+        __half* p = (__half*)j.dw[side] + c;
+        *p = from_f32<__half>(j.accumulate ? to_f32(*p) + t : t);
+    }
+}
+
+static int check_rotate(const char* who, const dblp_norm_rotate_t* a, bool grad)
+{
+    DBLP_REQUIRE(a, DBLP_EINVAL, "%s: null argument", who);
+    DBLP_REQUIRE(known_dtype(a->dtype) && known_dtype(a->weight_dtype), DBLP_EINVAL, "%s: unknown dtype %d or %d", who, a->dtype, a->weight_dtype);
+    DBLP_REQUIRE(a->head_dim >= 8 && a->head_dim <= 256 && a->head_dim % 8 == 0, DBLP_EINVAL,
+                 "%s: head_dim %u is not a multiple of 8 up to 256", who, a->head_dim);
+    const uint32_t known = DBLP_ROTATE_INTERLEAVED | (grad ? DBLP_ACCUMULATE : 0);
+    DBLP_REQUIRE((a->flags & ~known) == 0, DBLP_EINVAL, "%s: unknown flags %u", who, a->flags);
+    const uint32_t unit = a->flags & DBLP_ROTATE_INTERLEAVED ? 2 : 16;
+    DBLP_REQUIRE(a->rotary_dim <= a->head_dim && a->rotary_dim % unit == 0, DBLP_EINVAL, "%s: rotary_dim %u is not a multiple of %u up to head_dim %u",
+                 who, a->rotary_dim, unit, a->head_dim);
+    DBLP_REQUIRE(a->eps > 0.0f && a->eps < INFINITY, DBLP_EINVAL, "%s: eps %g is not finite and positive", who, a->eps);
+    const uint64_t heads = a->q_heads > a->k_heads ? a->q_heads : a->k_heads, tokens = (uint64_t)a->batch * a->tokens;
+    DBLP_REQUIRE(tokens < (1ull << 31) && heads < (1ull << 31) && tokens * heads < (1ull << 31), DBLP_ECAPACITY, "%s: 2^31 heads or more", who);
+    return DBLP_OK;
+}
+
+static int check_positions(const char* who, const dblp_norm_rotate_t* a)
+{
+    if (a->rotary_dim == 0) return DBLP_OK;
+    DBLP_REQUIRE(a->positions && a->freqs, DBLP_EINVAL, "%s: positions or freqs are null", who);
+    DBLP_REQUIRE(((uintptr_t)a->positions & 3) == 0 && ((uintptr_t)a->freqs & 7) == 0, DBLP_EALIGN, "%s: positions or freqs are not aligned to their type", who);
+    return DBLP_OK;
+}
+
+static int check_side(const char* who, const char* name, const dblp_norm_rotate_t* a, const dblp_heads_t* h, uint32_t nheads, bool output)
+{
+    DBLP_REQUIRE(h && h->data, DBLP_EINVAL, "%s: %s is null", who, name);
+    const int64_t unit = 16 / element_bytes(a->dtype);
+    const struct { int64_t stride; uint64_t extent; } dim[3] = {{h->batch_stride, a->batch}, {h->token_stride, a->tokens}, {h->head_stride, nheads}};
+    bool aligned = aligned16(h->data);
+    for (auto& d : dim) {
+        if (d.extent <= 1) continue;
+        aligned = aligned && d.stride % unit == 0;
+        DBLP_REQUIRE(d.stride >= 0 && d.stride < (1ll << 39), DBLP_EINVAL, "%s: %s has a stride of %lld", who, name, (long long)d.stride);
+    }
+    DBLP_REQUIRE(aligned, DBLP_EALIGN, "%s: %s has data or a stride that is not a multiple of 16 bytes", who, name);
+    if (output) {                                   // sorted by stride, each dimension must clear the ones below it
+        uint64_t reach = a->head_dim;
+        bool used[3] = {false, false, false};
+        for (int r = 0; r < 3; ++r) {
+            int best = -1;
+            for (int i = 0; i < 3; ++i)
+                if (!used[i] && dim[i].extent > 1 && (best < 0 || dim[i].stride < dim[best].stride)) best = i;
+            if (best < 0) break;
+            used[best] = true;
+            DBLP_REQUIRE((uint64_t)dim[best].stride >= reach, DBLP_EINVAL, "%s: sections of %s overlap", who, name);
+            reach = (uint64_t)dim[best].stride * (dim[best].extent - 1) + reach;
+        }
+    }
+    return DBLP_OK;
+}
+
+static uint32_t lanes_of(uint32_t head_dim)
+{
+    uint32_t l = 1;
+    while (l * 8 < head_dim) l *= 2;
+    return l;
+}
+
+// Blocks that walk over the rows of one side in the backward pass: at most 4 a multiprocessor for both sides together, by
+// their share of the rows.
+static uint32_t grad_blocks(const dblp_norm_rotate_t* a, uint32_t heads)
+{
+    const uint64_t rows = (uint64_t)a->batch * a->tokens * heads, per = kRotThreads / lanes_of(a->head_dim) * (kRotRows / 2);
+    const uint64_t steps = (rows + per - 1) / per, all = a->q_heads + (uint64_t)a->k_heads;
+    uint64_t share = all ? (4ull * kSms * heads + all - 1) / all : 1;
+    if (share < 1) share = 1;
+    return (uint32_t)(steps < share ? steps : share);
+}
+
+static size_t partial_bytes(const dblp_norm_rotate_t* a, uint32_t heads)
+{
+    return ((size_t)grad_blocks(a, heads) * a->head_dim * 4 + 255) & ~(size_t)255;
+}
+
+static RotHeads rot_heads(const dblp_heads_t* h) { return RotHeads{h->data, h->batch_stride, h->token_stride, h->head_stride}; }
+
+static RotArgs rot_args(const dblp_norm_rotate_t* a)
+{
+    RotArgs r{};
+    r.tokens = a->tokens;
+    r.by_tokens = FastDiv(a->tokens);
+    r.D = a->head_dim;
+    r.R = a->rotary_dim;
+    r.L = lanes_of(a->head_dim);
+    r.weight_dtype = a->weight_dtype;
+    r.eps = a->eps;
+    r.inv_d = 1.0f / a->head_dim;
+    r.positions = a->positions;
+    r.position_stride = a->position_stride;
+    r.freqs = a->freqs;
+    return r;
+}
+
+static RotSide rot_side(const dblp_norm_rotate_t* a, const dblp_heads_t* x, const void* weight, const dblp_heads_t* y, uint32_t heads)
+{
+    RotSide s{};
+    s.heads = heads;
+    s.by_heads = FastDiv(heads ? heads : 1);
+    s.rows = a->batch * a->tokens * heads;
+    if (heads) {
+        s.x = rot_heads(x);
+        s.y = rot_heads(y);
+        s.weight = weight;
+    }
+    return s;
+}
+
+// Tokens that `rows` consecutive rows of a side can touch.
+static uint32_t tokens_of(uint32_t rows, uint32_t heads) { return heads ? (heads == 1 ? rows : rows / heads + 2) : 0; }
+
+static int check_weight(const char* who, const char* name, const void* w, int dtype)
+{
+    DBLP_REQUIRE((uintptr_t)w % element_bytes(dtype) == 0, DBLP_EALIGN, "%s: %s is not aligned to its type", who, name);
+    return DBLP_OK;
+}
+
+}  // namespace dblp
+
+using namespace dblp;
+
+#define DBLP_TRY(call)                      \
+    do {                                    \
+        const int rc_ = (call);             \
+        if (rc_ != DBLP_OK) return rc_;     \
+    } while (0)
+
+extern "C" int dblp_norm_rotate(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* q_out,
+                                const dblp_heads_t* k, const void* k_weight, const dblp_heads_t* k_out, void* stream)
+{
+    DBLP_TRY(check_rotate("norm_rotate", a, false));
+    if (a->batch == 0 || a->tokens == 0 || a->q_heads + a->k_heads == 0) return DBLP_OK;
+    DBLP_TRY(check_positions("norm_rotate", a));
+    if (a->q_heads) {
+        DBLP_TRY(check_side("norm_rotate", "q", a, q, a->q_heads, false));
+        DBLP_TRY(check_side("norm_rotate", "q_out", a, q_out, a->q_heads, true));
+        DBLP_TRY(check_weight("norm_rotate", "q_weight", q_weight, a->weight_dtype));
+    }
+    if (a->k_heads) {
+        DBLP_TRY(check_side("norm_rotate", "k", a, k, a->k_heads, false));
+        DBLP_TRY(check_side("norm_rotate", "k_out", a, k_out, a->k_heads, true));
+        DBLP_TRY(check_weight("norm_rotate", "k_weight", k_weight, a->weight_dtype));
+    }
+    RotArgs r = rot_args(a);
+    r.side[0] = rot_side(a, q, q_weight, q_out, a->q_heads);
+    r.side[1] = rot_side(a, k, k_weight, k_out, a->k_heads);
+    const uint32_t per = kRotThreads / r.L * kRotRows;
+    for (RotSide& s : r.side) {
+        s.blocks = (s.rows + per - 1) / per;
+        r.table_tokens = max(r.table_tokens, tokens_of(per, s.heads));
+    }
+    const size_t smem = (size_t)r.table_tokens * (r.R / 2) * sizeof(float2);
+    return with_type(a->dtype, [&](auto tag) -> int {
+        using T = decltype(tag);
+        const auto kernel = a->flags & DBLP_ROTATE_INTERLEAVED ? k_norm_rotate<T, true> : k_norm_rotate<T, false>;
+        kernel<<<r.side[0].blocks + r.side[1].blocks, kRotThreads, smem, (cudaStream_t)stream>>>(r);
+        DBLP_LAUNCHED();
+        return DBLP_OK;
+    });
+}
+
+extern "C" int dblp_norm_rotate_grad_workspace_bytes(const dblp_norm_rotate_t* a, size_t* bytes)
+{
+    DBLP_TRY(check_rotate("norm_rotate_grad_workspace_bytes", a, true));
+    DBLP_REQUIRE(bytes, DBLP_EINVAL, "norm_rotate_grad_workspace_bytes: null output");
+    *bytes = partial_bytes(a, a->q_heads) + partial_bytes(a, a->k_heads);
+    return DBLP_OK;
+}
+
+extern "C" int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* dq_out,
+                                     const dblp_heads_t* dq, void* dq_weight, const dblp_heads_t* k, const void* k_weight,
+                                     const dblp_heads_t* dk_out, const dblp_heads_t* dk, void* dk_weight, void* ws, size_t ws_bytes,
+                                     void* stream)
+{
+    const char* who = "norm_rotate_grad";
+    DBLP_TRY(check_rotate(who, a, true));
+    if (a->q_heads + a->k_heads == 0) return DBLP_OK;
+    const bool empty = a->batch == 0 || a->tokens == 0;
+    if (!empty) DBLP_TRY(check_positions(who, a));
+    if (!empty && a->q_heads) {
+        DBLP_TRY(check_side(who, "q", a, q, a->q_heads, false));
+        DBLP_TRY(check_side(who, "dq_out", a, dq_out, a->q_heads, false));
+        DBLP_TRY(check_side(who, "dq", a, dq, a->q_heads, true));
+        DBLP_TRY(check_weight(who, "q_weight", q_weight, a->weight_dtype));
+    }
+    if (!empty && a->k_heads) {
+        DBLP_TRY(check_side(who, "k", a, k, a->k_heads, false));
+        DBLP_TRY(check_side(who, "dk_out", a, dk_out, a->k_heads, false));
+        DBLP_TRY(check_side(who, "dk", a, dk, a->k_heads, true));
+        DBLP_TRY(check_weight(who, "k_weight", k_weight, a->weight_dtype));
+    }
+    if (a->q_heads == 0) dq_weight = nullptr;
+    if (a->k_heads == 0) dk_weight = nullptr;
+    DBLP_TRY(check_weight(who, "dq_weight", dq_weight, a->weight_dtype));
+    DBLP_TRY(check_weight(who, "dk_weight", dk_weight, a->weight_dtype));
+    const bool join = dq_weight || dk_weight;
+    if (empty && !join) return DBLP_OK;
+    const size_t q_bytes = partial_bytes(a, a->q_heads), need = join ? q_bytes + partial_bytes(a, a->k_heads) : 0;
+    if (need) {
+        DBLP_REQUIRE(ws, DBLP_EINVAL, "%s: the workspace is null", who);
+        DBLP_REQUIRE(((uintptr_t)ws & 255) == 0, DBLP_EALIGN, "%s: the workspace is not 256-byte aligned", who);
+        DBLP_REQUIRE(ws_bytes >= need, DBLP_ECAPACITY, "%s: workspace of %zu bytes, needs %zu", who, ws_bytes, need);
+    }
+    float* const partial[2] = {(float*)ws, (float*)((char*)ws + q_bytes)};
+    RotArgs r = rot_args(a);
+    if (!empty) {
+        r.side[0] = rot_side(a, q, q_weight, dq, a->q_heads);
+        r.side[1] = rot_side(a, k, k_weight, dk, a->k_heads);
+        if (a->q_heads) r.side[0].d = rot_heads(dq_out);
+        if (a->k_heads) r.side[1].d = rot_heads(dk_out);
+        const uint32_t per = kRotThreads / r.L * (kRotRows / 2);
+        for (int i = 0; i < 2; ++i) {
+            RotSide& s = r.side[i];
+            s.blocks = s.rows ? grad_blocks(a, s.heads) : 0;
+            s.partial = (i ? dk_weight : dq_weight) ? partial[i] : nullptr;
+            r.table_tokens = max(r.table_tokens, tokens_of(per, s.heads));
+        }
+        const size_t smem = max((size_t)r.table_tokens * r.R * sizeof(float2), (size_t)kRotThreads * 8 * 4);
+        DBLP_TRY(with_type(a->dtype, [&](auto tag) -> int {
+            using T = decltype(tag);
+            const auto kernel = a->flags & DBLP_ROTATE_INTERLEAVED ? k_norm_rotate_grad<T, true> : k_norm_rotate_grad<T, false>;
+            kernel<<<r.side[0].blocks + r.side[1].blocks, kRotThreads, smem, (cudaStream_t)stream>>>(r);
+            DBLP_LAUNCHED();
+            return DBLP_OK;
+        }));
+    }
+    if (!join) return DBLP_OK;
+    RotJoin j{{partial[0], partial[1]}, {dq_weight, dk_weight}, {r.side[0].blocks, r.side[1].blocks}, a->head_dim, (uint32_t)a->weight_dtype,
+              a->flags & (uint32_t)DBLP_ACCUMULATE};
+    DBLP_NEXT(launch_next(k_rotate_join, dim3((a->head_dim + 31) / 32, 2), 256, 0, (cudaStream_t)stream, j));
+    return DBLP_OK;
+}
