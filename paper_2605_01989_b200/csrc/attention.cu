@@ -22,12 +22,7 @@ unsigned long long* timeout_counter()
     return (unsigned long long*)p;
 }
 
-// The driver's encoder of tensor maps, looked up through the runtime (the library does not link the driver).
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiled encoder()
+EncodeTiled map_encoder()
 {
     static std::atomic<void*> fn{nullptr};
     void* f = fn.load(std::memory_order_acquire);
@@ -44,7 +39,7 @@ static EncodeTiled encoder()
 // Boxes of 128 tokens x 64 columns; what lies outside the tensor reads as zero.
 int make_source(TileSource* t, const dblp_attention_t* a, const dblp_heads_t* h, uint32_t tokens, uint32_t nheads)
 {
-    const EncodeTiled encode = encoder();
+    const EncodeTiled encode = map_encoder();
     DBLP_REQUIRE(encode, DBLP_ECUDA, "attention: the driver has no cuTensorMapEncodeTiled");
     const cuuint64_t unused = (cuuint64_t)a->head_dim * 2;
     const bool hb = nheads > 1 && h->head_stride == 0, bb = a->batch > 1 && h->batch_stride == 0;

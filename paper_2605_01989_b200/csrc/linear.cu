@@ -248,7 +248,7 @@ extern "C" int dblp_linear(const dblp_linear_t* l, const dblp_matrix_t* x, const
     if (bias) e.bias = rows_of(bias, 0, 1, l->bias_dtype);
     e.act = l->activation;
     const dblp_matrix_t none{nullptr, 1, 1};
-    return run_product(l->in ? forward_product(l, x, w) : forward_product(l, &none, &none), e, ws, (cudaStream_t)stream);
+    return run_product(l->in ? forward_product(l, x, w) : forward_product(l, &none, &none), e, ws, false, (cudaStream_t)stream);
 }
 
 extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, const dblp_matrix_t* w,
@@ -287,7 +287,7 @@ extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy,
         EpiStore e{};
         e.out = rows_of(dw->data, by_rows ? dw->row_stride : dw->col_stride, by_rows ? l->in : l->out, l->out_dtype);
         e.accumulate = l->flags & DBLP_ACCUMULATE;
-        DBLP_TRY(run_product(pw, e, ws, s));
+        DBLP_TRY(run_product(pw, e, ws, false, s));
     }
     if (want_dx) {
         EpiGradX e{};
@@ -295,7 +295,7 @@ extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy,
         if (residual) e.residual = rows_of(residual->data, residual->row_stride, l->rows, l->dtype);
         if (pre) e.pre = rows_of(pre->data, pre->row_stride, l->rows, l->dtype);
         e.act = l->activation;
-        DBLP_TRY(run_product(px, e, ws, s));
+        DBLP_TRY(run_product(px, e, ws, false, s));
     }
     return DBLP_OK;
 }

@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
         load8(x, r, c, left, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * f);
-        a.out.store(b, r, c, left, v);
+        a.out.store(b, r, c, v);
     }
 }
 
@@ -255,19 +255,19 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
         EpiPoly e{};
         e.out = w.a;
         e.alpha = kScaleA / (float)(kScaleX * kScaleX);
-        DBLP_TRY(run_product(gram_product(u, p, now), e, w.products, s));
+        DBLP_TRY(run_product(gram_product(u, p, now), e, w.products, true, s));
         e.out = w.b;
         e.add = w.a;
         e.alpha = c / kScaleA;
         e.beta = b;
-        DBLP_TRY(run_product(square_product(u, p, w.a), e, w.products, s));
+        DBLP_TRY(run_product(square_product(u, p, w.a), e, w.products, true, s));
         const Product last = step_product(u, p, w.b, now);
         if (i + 1 < u->steps) {
             e.out = next;
             e.add = now;
             e.alpha = 1.0f / kScaleA;
             e.beta = a;
-            DBLP_TRY(run_product(last, e, w.products, s));
+            DBLP_TRY(run_product(last, e, w.products, true, s));
             const Words t = now;
             now = next;
             next = t;
@@ -280,7 +280,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
             const float back = u->scale / (float)kScaleX;
             f.alpha = back / kScaleA;
             f.beta = back * a;
-            DBLP_TRY(run_product(last, f, w.products, s));
+            DBLP_TRY(run_product(last, f, w.products, true, s));
         }
     }
     return DBLP_OK;

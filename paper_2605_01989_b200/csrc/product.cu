@@ -1,44 +1,482 @@
-// Matrix products, first form: one thread a row and eight columns, fp32.
+// Matrix products on the tensor cores, with an epilogue that works on eight columns of a row at a time.
+//
+// A work item is a tile of the result: 128 rows a block (256 for a pair of blocks, which share B's columns) by up to 256
+// columns, or a part of the summed dimension of such a tile.  A block is persistent and walks over items; one warp loads (TMA, 64 of
+// the summed dimension a stage), one issues the products, eight write the sums of the item before out of the other half of
+// tensor memory.
+//   operands   either dimension of an operand may be the contiguous one: the shared-memory layout serves both ways, so x w, dy w^T
+//              and x^T dy read the same tensors without a transposed copy.  Rows that TMA cannot address (not on 16 bytes) are
+//              copied first.
+//   epilogue   a warp brings 32 x 32 sums through shared memory, so that a lane has eight columns of one row and everything it
+//              reads and writes is whole sectors.  Read the other way, the same piece is a piece of the transposed result: this is how
+//              the mirror of a symmetric result is written, and how few rows are computed (as columns of the tile).
+//   parts      where there are too few tiles for the machine, the summed dimension is cut; the parts' sums are added in order
+//              by a second kernel with the same epilogue.
 #include "product.cuh"
+#include "tc.cuh"
 
 namespace dblp {
 
-template <typename T> __device__ __forceinline__ float word(const Operand& o, uint32_t b, uint32_t r, uint32_t k)
-{
-    const int64_t at = b * o.each + (o.mn ? (int64_t)k * o.stride + r : (int64_t)r * o.stride + k);
-    return to_f32(((const T*)o.p)[at]) + (o.lo ? to_f32(((const T*)o.lo)[at]) : 0.0f);
-}
+constexpr int kProdThreads = 320, kProdWriters = 8;             // warps 0 .. 7 write, 8 loads, 9 issues products
+constexpr uint32_t kStep = 64;                                  // of the summed dimension a stage
+constexpr uint32_t kMaxStages = 8;
+constexpr uint32_t kPieceStride = 36;                           // floats: rows of 144 bytes, no bank conflicts either way
+constexpr uint32_t kPieceBytes = 32 * kPieceStride * 4;
+constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
 
-template <typename T, typename E> __global__ void __launch_bounds__(256) k_product(const __grid_constant__ Product p, const __grid_constant__ E e)
+struct ProductArgs {
+    CUtensorMap a[2], b[2];                                     // first and second words
+    uint32_t M, N, bn, mt, nt;                                  // tiles of 128 (256) x bn
+    uint32_t steps, per, parts, items;                          // stages in all (terms together), of a part; parts of a tile; items in all
+    uint32_t term_steps, group, tiles;                          // stages of a term; tile rows walked together; tiles of one product
+    uint32_t stages, stage_bytes, b_bytes, acc_cols, idesc;
+    uint32_t a_mn, b_mn, symmetric, turned;
+    unsigned long long* timeouts;
+};
+
+struct ProdItem {
+    uint32_t i, j, b, out, k0, k1;                              // tile, product, number of the sums, stages
+};
+
+template <int CG> __host__ __device__ __forceinline__ ProdItem prod_item(const ProductArgs& a, uint32_t x)
 {
-    const uint32_t n = (blockIdx.x * 32 + threadIdx.x) * 8, m = blockIdx.y * 8 + threadIdx.y, b = blockIdx.z;
-    if (m >= p.M || n >= p.N) return;
-    const uint32_t left = min(8u, p.N - n);
-    float v[8] = {};
-    for (uint32_t k = 0; k < p.K; ++k) {
-        const float x = word<T>(p.a, b, m, k);
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (i < left) v[i] = fmaf(x, word<T>(p.b, b, n + i, k), v[i]);
+    ProdItem t;
+    const uint32_t q = x / a.tiles;
+    uint32_t y = x - q * a.tiles;
+    t.out = q;
+    t.b = q / a.parts;
+    const uint32_t part = q - t.b * a.parts;
+    t.k0 = part * a.per;
+    t.k1 = min(t.k0 + a.per, a.steps);
+    if (a.symmetric) {                                          // tiles that reach the diagonal or lie above it, row by row
+        uint32_t i = 0, first = 0;
+        while (y >= a.nt - first) {
+            y -= a.nt - first;
+            ++i;
+            first = i * 128 * CG / a.bn;
+        }
+        t.i = i;
+        t.j = first + y;
+    } else {                                                    // `group` tile rows together, column by column: operands stay in L2
+        const uint32_t all = a.group * a.nt, g = y / all, first = g * a.group, rows = min(a.group, a.mt - first), r = y - g * all;
+        t.j = r / rows;
+        t.i = first + r - t.j * rows;
     }
-    e.apply(b, m, n, left, v);
+    return t;
 }
 
-size_t product_space(const Product&) { return 0; }
-
-template <typename E> int run_product(const Product& p, const E& e, void*, cudaStream_t s)
+template <int CG, typename E>
+__global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_constant__ ProductArgs a, const __grid_constant__ E e)
 {
-    const dim3 grid((p.N + 255) / 256, (p.M + 7) / 8, p.batch), block(32, 8);
-    if (p.dtype == DBLP_BF16) k_product<__nv_bfloat16, E><<<grid, block, 0, s>>>(p, e);
-    else k_product<__half, E><<<grid, block, 0, s>>>(p, e);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_free[2], idle;
+    __shared__ uint32_t tmem_slot, dead;
+    uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0, first_item = blockIdx.x / CG, item_stride = gridDim.x / CG;
+
+    if (tid == 0) {
+        dead = 0;
+        for (uint32_t i = 0; i < a.stages; ++i) { bar_init(&full[i], 1); bar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(&acc_full[i], 1); bar_init(&acc_free[i], kProdWriters * CG); }
+        bar_init(&idle, 1);
+        fence_bar_init();
+    }
+    if (warp == 9) tmem_alloc_cols<CG>(&tmem_slot, 2 * a.acc_cols);
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = uniform(tmem_slot);
+    const Guard g{&dead, a.timeouts};
+    wait_before();
+    after_start();
+
+    if (warp == 8) {                                            // ---- loads
+        uint32_t st = 0, round = 0, total = 0;
+        bool ok = true;
+        for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
+            const ProdItem t = prod_item<CG>(a, x);
+            const int row = (int)((t.i * CG + rank) * 128), col = (int)(t.j * a.bn + rank * (a.bn / CG));
+            for (uint32_t k = t.k0; k < t.k1; ++k, ++total) {
+                if (round) ok = warp_wait(&empty[st], (round - 1) & 1, g);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t term = k / a.term_steps, at = (k - term * a.term_steps) * kStep;
+                    const CUtensorMap *ma = &a.a[term == 2], *mb = &a.b[term == 1];
+                    uint8_t *da = ring + st * a.stage_bytes, *db = da + 128 * 128;
+                    const uint32_t bar = CG == 2 ? in_block(&full[st], 0) : smem_addr(&full[st]);
+                    if (rank == 0) bar_expect(&full[st], CG * a.stage_bytes);
+                    if (a.a_mn) {
+                        tma_tile3<CG>(da, ma, bar, row, (int)at, (int)t.b);
+                        tma_tile3<CG>(da + 8192, ma, bar, row + 64, (int)at, (int)t.b);
+                    } else {
+                        tma_tile3<CG>(da, ma, bar, (int)at, row, (int)t.b);
+                    }
+                    if (a.b_mn)
+                        for (uint32_t c = 0; c < a.b_bytes / 8192; ++c) tma_tile3<CG>(db + c * 8192, mb, bar, col + (int)c * 64, (int)at, (int)t.b);
+                    else
+                        tma_tile3<CG>(db, mb, bar, (int)at, col, (int)t.b);
+                }
+                __syncwarp();
+                if (++st == a.stages) { st = 0; ++round; }
+            }
+        }
+        if (lane == 0 && rank == 0) {                           // every copy lands before the block (its pair) may end
+            for (uint32_t i = 0; i < min(total, a.stages); ++i) {
+                const uint32_t n = total - 1 - i;
+                bar_drain(&full[n % a.stages], (n / a.stages) & 1);
+            }
+        }
+    } else if (warp == 9) {                                     // ---- products
+        if (rank == 0) {
+            uint32_t st = 0, phase = 0, w = 0;
+            bool ok = true;
+            const uint32_t base = smem_addr(ring);
+            for (uint32_t x = first_item; x < a.items && ok; x += item_stride, ++w) {
+                const ProdItem t = prod_item<CG>(a, x);
+                const uint32_t acc = tmem + (w & 1) * a.acc_cols, n = uniform(t.k1 - t.k0);
+                if (w >= 2) ok = warp_wait(&acc_free[w & 1], ((w >> 1) - 1) & 1, g);
+                if (!ok) break;
+                tc_fence_after();
+                for (uint32_t k = 0; k < n; ++k) {
+                    ok = warp_wait(&full[st], phase, g);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t pa = uniform(base + st * a.stage_bytes), pb = pa + 128 * 128;
+#pragma unroll
+                    for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
+                        const uint64_t da = a.a_mn ? desc_mn(pa + kk * 2048, 8192) : desc_k(pa + kk * 32);
+                        const uint64_t db = a.b_mn ? desc_mn(pb + kk * 2048, 8192) : desc_k(pb + kk * 32);
+                        mma_cg<CG>(acc, da, db, a.idesc, k > 0 || kk > 0);
+                    }
+                    commit_cg<CG>(&empty[st]);
+                    if (++st == a.stages) { st = 0; phase ^= 1; }
+                }
+                if (ok) commit_cg<CG>(&acc_full[w & 1]);
+            }
+            __syncwarp();
+            mma_commit_idle<CG>(&idle);                         // products in flight end before the memory is freed, whoever gave up
+            bar_drain(&idle, 0);
+        }
+    } else {                                                    // ---- sums to their places
+        float* piece = (float*)(ring + a.stages * a.stage_bytes + warp * kPieceBytes);
+        const uint32_t lanes = (warp & 3) * 32, M = a.M, N = a.N;
+        uint32_t w = 0;
+        bool ok = true;
+        for (uint32_t x = first_item; x < a.items && ok; x += item_stride, ++w) {
+            const ProdItem t = prod_item<CG>(a, x);
+            const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, acc = tmem + (w & 1) * a.acc_cols + (lanes << 16);
+            ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
+            if (!ok) break;
+            tc_fence_after();
+            if (r0 < M) {
+                for (uint32_t c = (warp >> 2) * 32; c < a.bn; c += 64) {
+                    const uint32_t c0 = t.j * a.bn + c;
+                    if (c0 >= N || (a.symmetric && c0 < r0)) continue;
+                    typename E::Fetched f[4];
+                    const bool plain = !a.turned, mirror = a.turned || (a.symmetric && c0 > r0);
+                    const uint32_t pr = r0 + lane / 4, pc = c0 + (lane & 3) * 8, pl = pc < N ? min(8u, N - pc) : 0;
+                    if (plain)
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i)
+                            if (pl && pr + 8 * i < M) e.fetch(t.out, pr + 8 * i, pc, pl, f[i]);
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_ld32(acc + c, v);
+                    tmem_wait_ld<32>(v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4*>(piece + lane * kPieceStride + 4 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    __syncwarp();
+                    if (plain)
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            if (!pl || pr + 8 * i >= M) continue;
+                            const float4* s = reinterpret_cast<const float4*>(piece + (lane / 4 + 8 * i) * kPieceStride + (lane & 3) * 8);
+                            const float4 lo = s[0], hi = s[1];
+                            float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                            e.apply(t.out, pr + 8 * i, pc, pl, f[i], y);
+                        }
+                    if (mirror && c0 + lane < N) {              // column `lane` of the piece is a row of the transposed result
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i)
+                            if (r0 + 8 * i < M) e.fetch(t.out, c0 + lane, r0 + 8 * i, min(8u, M - r0 - 8 * i), f[i]);
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            if (r0 + 8 * i >= M) continue;
+                            float y[8];
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) y[r] = piece[(8 * i + r) * kPieceStride + lane];
+                            e.apply(t.out, c0 + lane, r0 + 8 * i, min(8u, M - r0 - 8 * i), f[i], y);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            tc_fence_before();
+            if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
+            else warp_arrive(&acc_free[w & 1]);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    tc_fence_after();
+    if (warp == 9) tmem_free_cols<CG>(tmem, 2 * a.acc_cols);
+}
+
+// Sums of the parts, in order, and the epilogue; parts = 0: sums of nothing.
+template <typename E>
+__global__ void __launch_bounds__(256) k_product_join(const __grid_constant__ E e, EpiPartial from, uint32_t parts, uint32_t M, uint32_t N, uint32_t batch)
+{
+    wait_before();
+    after_start();
+    const uint32_t per_row = (N + 7) / 8;
+    const uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = x / per_row;
+    const uint32_t n = (uint32_t)(x - row * per_row) * 8, b = (uint32_t)(row / M), m = (uint32_t)(row - (uint64_t)b * M);
+    if (b >= batch) return;
+    typename E::Fetched f;
+    const uint32_t left = min(8u, N - n);
+    e.fetch(b, m, n, left, f);
+    float v[8] = {};
+    const float* p = from.p + (uint64_t)b * parts * from.each + (int64_t)m * from.stride + n;
+    for (uint32_t s = 0; s < parts; ++s) {
+        const float4 lo = *reinterpret_cast<const float4*>(p + s * from.each), hi = *reinterpret_cast<const float4*>(p + s * from.each + 4);
+        const float t[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += t[i];
+    }
+    e.apply(b, m, n, left, f, v);
+}
+
+// Rows of any stride and alignment -> rows of `to` elements, a multiple of eight.
+__global__ void __launch_bounds__(256) k_repack(const uint16_t* src, int64_t stride, uint16_t* dst, uint32_t to, uint32_t rows, uint32_t cols)
+{
+    after_start();
+    const uint32_t per_row = to / 8;
+    const uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x, r = x / per_row;
+    if (r >= rows) return;
+    const uint32_t c = (uint32_t)(x - r * per_row) * 8;
+    const uint16_t* p = src + (int64_t)r * stride + c;
+    uint32_t w[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+        w[i] = (c + 2 * i < cols ? p[2 * i] : 0u) | (c + 2 * i + 1 < cols ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    *reinterpret_cast<uint4*>(dst + r * to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+struct ProductPlan {
+    int cg;
+    uint32_t bn, mt, nt, tiles, parts, per, steps, term_steps;
+    bool turned;                                                // A and B change places
+    bool copy_a, copy_b;
+    uint32_t a_to, b_to;                                        // rows of the copies
+    size_t a_bytes, b_bytes, partial_bytes;                     // in workspace
+    uint32_t partial_stride;
+};
+
+static bool tma_reads(const Operand& o, uint32_t outer, uint32_t inner, uint32_t batch)
+{
+    if (!aligned16(o.p) || (o.lo && !aligned16(o.lo))) return false;
+    if (outer > 1 && (o.stride % 8 != 0 || o.stride < (int64_t)inner || o.stride >= (1ll << 38))) return false;
+    return batch <= 1 || o.each % 8 == 0;
+}
+
+static uint32_t count_tiles(bool symmetric, uint32_t tm, uint32_t bn, uint32_t mt, uint32_t nt)
+{
+    if (!symmetric) return mt * nt;
+    uint64_t n = 0;
+    for (uint32_t i = 0; i < mt; ++i) n += nt - (uint32_t)((uint64_t)i * tm / bn);
+    return (uint32_t)n;
+}
+
+static ProductPlan plan_product(const Product& p)
+{
+    ProductPlan r{};
+    auto padded = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    const uint32_t ai = p.a.mn ? p.M : p.K, ao = p.a.mn ? p.K : p.M, bi = p.b.mn ? p.N : p.K, bo = p.b.mn ? p.K : p.N;
+    r.copy_a = !tma_reads(p.a, ao, ai, p.batch);
+    r.copy_b = !tma_reads(p.b, bo, bi, p.batch);
+    r.a_to = (ai + 7) & ~7u;
+    r.b_to = (bi + 7) & ~7u;
+    r.a_bytes = r.copy_a ? padded((size_t)ao * r.a_to * 2) : 0;
+    r.b_bytes = r.copy_b ? padded((size_t)bo * r.b_to * 2) : 0;
+    r.term_steps = (p.K + kStep - 1) / kStep;
+    r.steps = r.term_steps * p.terms;
+    // Few rows become the columns of narrow tiles, which read B (weights) once and waste no products on rows that are not there.
+    r.turned = !p.symmetric && p.M <= 128 && p.M < p.N && !p.a.mn;
+    const uint32_t M = r.turned ? p.N : p.M, N = r.turned ? p.M : p.N;
+    double best = 1e300;
+    const struct { int cg; uint32_t bn; double step; } shapes[] = {{2, 256, 512}, {2, 128, 300}, {1, 256, 560}, {1, 128, 300}, {1, 64, 240}, {1, 32, 220}, {1, 16, 200}};
+    for (const auto& c : shapes) {
+        if (r.turned ? (c.cg == 2 || (c.bn >= 2 * N && c.bn > 16)) : c.bn < 64) continue;
+        if (r.turned && c.bn < N && c.bn < 128) continue;
+        const uint32_t tm = 128 * c.cg, mt = (uint32_t)(((uint64_t)M + tm - 1) / tm), nt = (N + c.bn - 1) / c.bn, tiles = count_tiles(p.symmetric, tm, c.bn, mt, nt);
+        const uint32_t slots = kSms / c.cg;
+        for (uint32_t parts = 1; parts <= 16 && parts <= r.steps; ++parts) {
+            const uint32_t per = (r.steps + parts - 1) / parts;
+            if ((r.steps + per - 1) / per != parts) continue;
+            const uint64_t items = (uint64_t)tiles * parts * p.batch, waves = (items + slots - 1) / slots;
+            // cycles: stages of the longest block, its first loads and last output, the parts written and read again
+            double t = (double)waves * per * c.step + 2500 + 10.0 * c.bn;
+            if (parts > 1) t += 5000 + (double)parts * p.batch * M * N * 8 / 2500;
+            if (t < best) {
+                best = t;
+                r.cg = c.cg;
+                r.bn = c.bn;
+                r.mt = mt;
+                r.nt = nt;
+                r.tiles = tiles;
+                r.parts = parts;
+                r.per = per;
+            }
+        }
+    }
+    r.partial_stride = (p.N + 7) & ~7u;
+    r.partial_bytes = r.parts > 1 ? padded((size_t)r.parts * p.batch * p.M * r.partial_stride * 4) : 0;
+    return r;
+}
+
+size_t product_space(const Product& p)
+{
+    const ProductPlan r = plan_product(p);
+    return r.a_bytes + r.b_bytes + r.partial_bytes;
+}
+
+// Boxes of `box` rows x 64 of the summed dimension, or of 64 rows x 64 where the rows are contiguous; zero outside.
+static int make_map(CUtensorMap* map, const void* data, int64_t stride, const Operand& o, uint32_t rows, uint32_t K, uint32_t batch, uint32_t box, int dtype)
+{
+    const EncodeTiled encode = map_encoder();
+    DBLP_REQUIRE(encode, DBLP_ECUDA, "product: the driver has no cuTensorMapEncodeTiled");
+    const uint32_t inner = o.mn ? rows : K, outer = o.mn ? K : rows;
+    const cuuint64_t unused = ((cuuint64_t)inner + 7) / 8 * 16;
+    const cuuint64_t dims[3] = {inner, outer, batch}, strides[2] = {outer > 1 ? (cuuint64_t)stride * 2 : unused, batch > 1 ? (cuuint64_t)o.each * 2 : unused};
+    const cuuint32_t boxes[3] = {64, o.mn ? 64 : box, 1}, ones[3] = {1, 1, 1};
+    const CUresult rc = encode(map, dtype == DBLP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)data, dims, strides,
+                               boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    DBLP_REQUIRE(rc == CUDA_SUCCESS, DBLP_ECUDA, "product: tensor map refused (driver error %d)", (int)rc);
+    return DBLP_OK;
+}
+
+template <int CG, typename E> static int launch_product(const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
+{
+    constexpr auto kernel = k_product<CG, E>;
+    DBLP_CUDA(allow_shared<kernel>(kProdSmem));
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg{};
+    const uint32_t slots = kSms / CG;
+    cfg.gridDim = dim3((a.items < slots ? a.items : slots) * CG);
+    cfg.blockDim = dim3(kProdThreads);
+    cfg.dynamicSmemBytes = 1024 + a.stages * a.stage_bytes + kProdWriters * kPieceBytes;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    if (CG == 2) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = 2;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (chained) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+    DBLP_NEXT(cudaLaunchKernelEx(&cfg, kernel, a, e));
+    return DBLP_OK;
+}
+
+template <typename E> static int launch_join(const E& e, const EpiPartial& from, uint32_t parts, const Product& p, bool chained, cudaStream_t s)
+{
+    const uint64_t groups = (uint64_t)p.batch * p.M * ((p.N + 7) / 8), blocks = (groups + 255) / 256;
+    DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^42 elements or more");
+    if (chained) {
+        DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)blocks), 256, 0, s, e, from, parts, p.M, p.N, p.batch));
+    } else {
+        k_product_join<E><<<(unsigned)blocks, 256, 0, s>>>(e, from, parts, p.M, p.N, p.batch);
+        DBLP_LAUNCHED();
+    }
+    return DBLP_OK;
+}
+
+static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, uint32_t inner, cudaStream_t s)
+{
+    const uint64_t blocks = ((uint64_t)outer * (stride / 8) + 255) / 256;
+    DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: an operand of 2^42 elements or more");
+    k_repack<<<(unsigned)blocks, 256, 0, s>>>((const uint16_t*)o.p, o.stride, (uint16_t*)to, stride, outer, inner);
     DBLP_LAUNCHED();
     return DBLP_OK;
 }
 
-template int run_product(const Product&, const EpiLinear&, void*, cudaStream_t);
-template int run_product(const Product&, const EpiGradX&, void*, cudaStream_t);
-template int run_product(const Product&, const EpiStore&, void*, cudaStream_t);
-template int run_product(const Product&, const EpiPoly&, void*, cudaStream_t);
-template int run_product(const Product&, const EpiLast&, void*, cudaStream_t);
+template <typename E> int run_product(const Product& p, const E& e, void* ws, bool chained, cudaStream_t s)
+{
+    if (p.K == 0) return launch_join(e, EpiPartial{}, 0, p, chained, s);
+    const ProductPlan r = plan_product(p);
+    DBLP_REQUIRE((uint64_t)r.tiles * r.parts * p.batch < 1ull << 31, DBLP_ECAPACITY, "product: 2^31 tiles or more");
+    unsigned long long* timeouts = timeout_counter();
+    DBLP_REQUIRE(timeouts, DBLP_ECUDA, "product: no device counter: %s", cudaGetErrorString(cudaGetLastError()));
+    Operand oa = p.a, ob = p.b;
+    char* at = (char*)ws;
+    if (r.copy_a) {
+        if (int rc = repack(oa, at, r.a_to, oa.mn ? p.K : p.M, oa.mn ? p.M : p.K, s)) return rc;
+        oa.p = at;
+        oa.stride = r.a_to;
+        at += r.a_bytes;
+        chained = false;
+    }
+    if (r.copy_b) {
+        if (int rc = repack(ob, at, r.b_to, ob.mn ? p.K : p.N, ob.mn ? p.N : p.K, s)) return rc;
+        ob.p = at;
+        ob.stride = r.b_to;
+        at += r.b_bytes;
+        chained = false;
+    }
+    if (r.turned) {
+        const Operand t = oa;
+        oa = ob;
+        ob = t;
+    }
+    ProductArgs a{};
+    a.M = r.turned ? p.N : p.M;
+    a.N = r.turned ? p.M : p.N;
+    for (int i = 0; i < (p.terms > 1 ? 2 : 1); ++i) {
+        if (int rc = make_map(&a.a[i], i ? oa.lo : oa.p, oa.stride, oa, a.M, p.K, p.batch, 128, p.dtype)) return rc;
+        if (int rc = make_map(&a.b[i], i ? ob.lo : ob.p, ob.stride, ob, a.N, p.K, p.batch, r.bn / r.cg, p.dtype)) return rc;
+    }
+    a.bn = r.bn;
+    a.mt = r.mt;
+    a.nt = r.nt;
+    a.steps = r.steps;
+    a.per = r.per;
+    a.parts = r.parts;
+    a.tiles = r.tiles;
+    a.items = r.tiles * r.parts * p.batch;
+    a.term_steps = r.term_steps;
+    a.group = 8 / r.cg;
+    a.a_mn = oa.mn;
+    a.b_mn = ob.mn;
+    a.symmetric = p.symmetric;
+    a.turned = r.turned;
+    a.b_bytes = (r.bn / r.cg) * 128;
+    a.stage_bytes = 128 * 128 + a.b_bytes;
+    const uint32_t room = (kProdSmem - 1024 - kProdWriters * kPieceBytes) / a.stage_bytes;
+    a.stages = room < kMaxStages ? room : kMaxStages;
+    a.acc_cols = r.bn < 32 ? 32 : r.bn;
+    a.idesc = p.dtype == DBLP_BF16 ? mma_desc<__nv_bfloat16>(128 * r.cg, r.bn, oa.mn, ob.mn) : mma_desc<__half>(128 * r.cg, r.bn, oa.mn, ob.mn);
+    a.timeouts = timeouts;
+    if (r.parts == 1) return r.cg == 2 ? launch_product<2>(a, e, chained, s) : launch_product<1>(a, e, chained, s);
+    const EpiPartial sums{(float*)at, (int64_t)p.M * r.partial_stride, r.partial_stride};
+    if (int rc = r.cg == 2 ? launch_product<2>(a, sums, chained, s) : launch_product<1>(a, sums, chained, s)) return rc;
+    return launch_join(e, sums, r.parts, p, true, s);
+}
+
+template int run_product(const Product&, const EpiLinear&, void*, bool, cudaStream_t);
+template int run_product(const Product&, const EpiGradX&, void*, bool, cudaStream_t);
+template int run_product(const Product&, const EpiStore&, void*, bool, cudaStream_t);
+template int run_product(const Product&, const EpiPoly&, void*, bool, cudaStream_t);
+template int run_product(const Product&, const EpiLast&, void*, bool, cudaStream_t);
 
 }  // namespace dblp

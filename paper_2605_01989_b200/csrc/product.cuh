@@ -23,6 +23,7 @@ struct Product {
 };
 
 size_t product_space(const Product& p);          // bytes of workspace
-template <typename E> int run_product(const Product& p, const E& epilogue, void* ws, cudaStream_t s);
+// chained: the kernels before it on the stream belong to the same call and let this one be set up while they run
+template <typename E> int run_product(const Product& p, const E& epilogue, void* ws, bool chained, cudaStream_t s);
 
 }  // namespace dblp

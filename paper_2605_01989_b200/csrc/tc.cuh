@@ -285,4 +285,110 @@ __device__ __forceinline__ float2 exp2_pair(float2 x)
     return mul2(p, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3F800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3F800000)));
 }
 
+// ---- pairs of blocks ---------------------------------------------------------------------------------------------------
+// Two blocks of a cluster on neighbouring multiprocessors compute one product of 256 rows: each holds its own 128 rows of A and of
+// the accumulator and half of B's columns; the first one issues the products, which read both blocks' shared memory at the
+// same offsets.  Loads of both blocks are counted on the first one's barrier.
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address, in the cluster's window, of the same place in block `rank`.
+__device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void warp_arrive_in(uint32_t cluster_bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// bar: in the cluster's window.  A pair's loads may count on the barrier of either block.
+template <int CG> __device__ __forceinline__ void tma_tile3(void* dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2)
+{
+    if (CG == 2)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                     : "memory");
+}
+// cols: a power of two from 32 to 512; by one warp of each block
+template <int CG> __device__ __forceinline__ void tmem_alloc_cols(uint32_t* slot, uint32_t cols)
+{
+    if (CG == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG> __device__ __forceinline__ void tmem_free_cols(uint32_t addr, uint32_t cols)
+{
+    if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+}
+template <int CG> __device__ __forceinline__ void mma_cg(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    if (CG == 2)
+        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                     "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+                     : "memory");
+    else
+        mma_ss(d, a, b, idesc, acc);
+}
+// As mma_commit; a pair's arrives on the barriers of both blocks.
+template <int CG> __device__ __forceinline__ void commit_cg(uint64_t* bar)
+{
+    if (CG == 2)
+        asm volatile("{\n.reg .pred q;\n.reg .b16 m;\nmov.b16 m, 3;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                     "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n}" ::"r"(smem_addr(bar))
+                     : "memory");
+    else
+        mma_commit(bar);
+}
+// On the issuing block's barrier alone.
+template <int CG> __device__ __forceinline__ void mma_commit_idle(uint64_t* bar)
+{
+    if (CG == 2)
+        asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                     "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(in_block(bar, 0))
+                     : "memory");
+    else
+        mma_commit(bar);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------
+// Lets kernel K use `bytes` of shared memory on the current device; asked of the runtime once per kernel and device.
+template <auto K> inline cudaError_t allow_shared(int bytes)
+{
+    static std::atomic<unsigned long long> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_acq_rel);
+    return e;
+}
+
+unsigned long long* timeout_counter();     // of the current device; null after a CUDA error
+
+// The driver's encoder of tensor maps, looked up through the runtime (the library does not link the driver); null if missing.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled map_encoder();
+
 }  // namespace dblp
