@@ -166,6 +166,7 @@ static Product product_of(const dblp_linear_t* l, const Operand& a, const Operan
     p.batch = 1;
     p.dtype = l->dtype;
     p.terms = 1;
+    p.runs = l->out_dtype == DBLP_F32;
     return p;
 }
 
@@ -176,7 +177,9 @@ static Product forward_product(const dblp_linear_t* l, const dblp_matrix_t* x, c
 }
 static Product dx_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* w)
 {
-    return product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out);
+    Product p = product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out);
+    p.runs = false;
+    return p;
 }
 static Product dw_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, bool by_rows)
 {

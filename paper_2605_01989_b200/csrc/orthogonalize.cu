@@ -66,18 +66,20 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
     __shared__ double part[kUpdThreads / 32];
     wait_before();
     after_start();
-    const uint32_t per_row = (a.cols + 7) / 8, b = blockIdx.y;
+    const uint32_t per_row = (a.cols + 15) / 16, b = blockIdx.y;
     const uint64_t groups = (uint64_t)a.rows * per_row;
     const double norm = sqrt(block_sum(threadIdx.x < a.parts ? a.squares[(size_t)b * a.parts + threadIdx.x] : 0.0, part)) + (double)a.eps;
     const double f = norm == 0.0 ? 0.0 : kScaleX / norm;
     Rows x = a.x;
     x.p = (char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
     for (uint64_t g = (uint64_t)blockIdx.x * kUpdThreads + threadIdx.x; g < groups; g += (uint64_t)gridDim.x * kUpdThreads) {
-        const uint32_t r = (uint32_t)(g / per_row), c = (uint32_t)(g - (uint64_t)r * per_row) * 8, left = min(8u, a.cols - c);
-        float v[8];
-        load8(x, r, c, left, v);
+        const uint32_t r = (uint32_t)(g / per_row), c = (uint32_t)(g - (uint64_t)r * per_row) * 16, left = min(16u, a.cols - c);
+        Raw w;
+        float v[16];
+        fetch16(x, r, c, left, w);
+        use16(x, left, w, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * f);
+        for (int i = 0; i < 16; ++i) v[i] = (float)((double)v[i] * f);
         a.out.store(b, r, c, v);
     }
 }
@@ -96,8 +98,8 @@ static UpdPlan plan_update(const dblp_orthogonalize_t* u)
     p.tall = u->rows > u->cols;
     p.low = p.tall ? u->cols : u->rows;
     p.precise = u->out_dtype != DBLP_BF16;
-    p.xs = (u->cols + 7) & ~7u;
-    p.as = (p.low + 7) & ~7u;
+    p.xs = (u->cols + 15) & ~15u;
+    p.as = (p.low + 15) & ~15u;
     auto padded = [](size_t b) { return (b + 255) & ~(size_t)255; };
     p.x_bytes = padded((size_t)u->batch * u->rows * p.xs * 2);
     p.a_bytes = padded((size_t)u->batch * p.low * p.as * 2);
@@ -117,6 +119,7 @@ static Product gram_product(const dblp_orthogonalize_t* u, const UpdPlan& p, con
     g.batch = u->batch;
     g.dtype = DBLP_F16;
     g.terms = p.precise ? 3 : 1;
+    g.runs = p.precise;
     g.symmetric = true;
     return g;
 }
@@ -170,6 +173,14 @@ static UpdSpace space_of(const dblp_orthogonalize_t* u, const UpdPlan& p, void* 
     for (const Product& g : {gram_product(u, p, s.x), square_product(u, p, s.a), step_product(u, p, s.b, s.x)}) most = max(most, product_space(g));
     s.bytes = (size_t)(at - (char*)ws) + most;
     return s;
+}
+
+// Rows of the first matrix, with accesses that all of them allow.
+static Rows batched(const void* p, int64_t row_stride, int64_t batch_stride, const dblp_orthogonalize_t* u, int dtype)
+{
+    Rows r = rows_of(p, row_stride, u->rows, dtype);
+    while (u->batch > 1 && r.vec && batch_stride * element_bytes(dtype) % r.vec) r.vec = r.vec == 32 ? 16 : 0;
+    return r;
 }
 
 static int check_update(const char* who, const dblp_orthogonalize_t* u)
@@ -235,9 +246,8 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     const cudaStream_t s = (cudaStream_t)stream;
 
     UpdIn in{};
-    in.x = rows_of(x, u->x_row_stride, u->rows, u->x_dtype);
+    in.x = batched(x, u->x_row_stride, u->x_batch_stride, u, u->x_dtype);
     in.each = u->x_batch_stride;
-    in.x.vec = in.x.vec && (u->batch == 1 || u->x_batch_stride % (16 / element_bytes(u->x_dtype)) == 0);
     in.rows = u->rows;
     in.cols = u->cols;
     in.parts = p.parts;
@@ -246,7 +256,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     in.out = w.x;
     k_squares<<<dim3(p.parts, u->batch), kUpdThreads, 0, s>>>(in);
     DBLP_LAUNCHED();
-    const uint64_t groups = (uint64_t)u->rows * ((u->cols + 7) / 8), blocks = (groups + 2 * kUpdThreads - 1) / (2 * kUpdThreads);
+    const uint64_t groups = (uint64_t)u->rows * ((u->cols + 15) / 16), blocks = (groups + kUpdThreads - 1) / kUpdThreads;
     DBLP_NEXT(launch_next(k_normalize, dim3((unsigned)(blocks < 1024 ? blocks : 1024), u->batch), kUpdThreads, 0, s, in));
 
     Words now = w.x, next = w.y;
@@ -273,8 +283,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
             next = t;
         } else {
             EpiLast f{};
-            f.out = rows_of(out, u->out_row_stride, u->rows, u->out_dtype);
-            f.out.vec = f.out.vec && (u->batch == 1 || u->out_batch_stride % (16 / element_bytes(u->out_dtype)) == 0);
+            f.out = batched(out, u->out_row_stride, u->out_batch_stride, u, u->out_dtype);
             f.each = u->out_batch_stride;
             f.add = now;
             const float back = u->scale / (float)kScaleX;

@@ -1,8 +1,8 @@
 // Matrix products on the tensor cores, with an epilogue that works on eight columns of a row at a time.
 //
 // A work item is a tile of the result: 128 rows a block (256 for a pair of blocks, which share B's columns) by up to 256
-// columns, or a part of the summed dimension of such a tile.  A block is persistent and walks over items; one warp loads (TMA, 64 of
-// the summed dimension a stage), one issues the products, eight write the sums of the item before out of the other half of
+// columns, or a part of the summed dimension of such a tile.  A block is persistent and walks over items; two warps load (TMA, 64
+// of the summed dimension a stage), one issues the products, eight write the sums of the item before out of the other half of
 // tensor memory.
 //   operands   either dimension of an operand may be the contiguous one: the shared-memory layout serves both ways, so x w, dy w^T
 //              and x^T dy read the same tensors without a transposed copy.  Rows that TMA cannot address (not on 16 bytes) are
@@ -17,11 +17,11 @@
 
 namespace dblp {
 
-constexpr int kProdThreads = 320, kProdWriters = 8;             // warps 0 .. 7 write, 8 loads, 9 issues products
+constexpr int kProdThreads = 384, kProdWriters = 8;             // warps 0 .. 7 write, 8 and 10 load A and B, 9 issues products, 11 idles
 constexpr uint32_t kStep = 64;                                  // of the summed dimension a stage
 constexpr uint32_t kMaxStages = 8;
-constexpr uint32_t kPieceStride = 36;                           // floats: rows of 144 bytes, no bank conflicts either way
-constexpr uint32_t kPieceBytes = 32 * kPieceStride * 4;
+constexpr uint32_t kPieceBytes = 32 * 32 * 4;                   // what a writing warp brings through shared memory at a time
+constexpr uint32_t kRun = 4;                                    // stages that the tensor cores add up by themselves (RUNS)
 constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
 
 struct ProductArgs {
@@ -30,7 +30,7 @@ struct ProductArgs {
     uint32_t steps, per, parts, items;                          // stages in all (terms together), of a part; parts of a tile; items in all
     uint32_t term_steps, group, tiles;                          // stages of a term; tile rows walked together; tiles of one product
     uint32_t stages, stage_bytes, b_bytes, acc_cols, idesc;
-    uint32_t a_mn, b_mn, symmetric, turned;
+    uint32_t a_mn, b_mn, symmetric, turned, direct;
     unsigned long long* timeouts;
 };
 
@@ -65,7 +65,69 @@ template <int CG> __host__ __device__ __forceinline__ ProdItem prod_item(const P
     return t;
 }
 
-template <int CG, typename E>
+// 32 x 32 sums, a row a lane, from (r0, c0) on: what the epilogue reads is fetched, then `sums` brings v, then it is applied.  Rows
+// whose matrices allow 32-byte accesses are written from the lane that has them.  The others, and results written by columns, go
+// through 4 KB of shared memory, where the 16-byte chunk c of row r is at place c ^ (r % 8): no bank conflicts in any of the
+// three ways.
+template <typename E, typename F>
+__device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, uint32_t b, uint32_t r0, uint32_t c0, float* v, uint8_t* piece, const F& sums)
+{
+    const uint32_t M = a.M, N = a.N, lane = threadIdx.x & 31;
+    if (r0 >= M || c0 >= N || (a.symmetric && c0 < r0)) return;
+    const bool mirror = a.turned || (a.symmetric && c0 > r0), plain = !a.turned, direct = plain && a.direct;
+    typename E::Fetched f[2];
+    // lane's part of the piece: direct one row, two groups of columns; through shared memory one group of two rows
+    const uint32_t row = direct ? r0 + lane : r0 + lane / 2, dr = direct ? 0 : 16, col = direct ? c0 : c0 + (lane & 1) * 16, dc = direct ? 16 : 0;
+    auto left = [&](uint32_t i) { return col + i * dc < N ? min(16u, N - col - i * dc) : 0u; };
+    auto live = [&](uint32_t i) { return plain && row + i * dr < M && left(i) > 0; };
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i)
+        if (live(i)) e.fetch(b, row + i * dr, col + i * dc, left(i), f[i]);
+    sums();
+    if (!direct || mirror) {
+        __syncwarp();
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            *reinterpret_cast<float4*>(piece + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        __syncwarp();
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        if (!live(i)) continue;
+        float y[16];
+        if (direct) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] = v[16 * i + k];
+        } else {
+            const uint32_t r = lane / 2 + 16 * i;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                const float4 q = *reinterpret_cast<const float4*>(piece + r * 128 + ((((lane & 1) * 4 + k) ^ (r & 7)) << 4));
+                y[4 * k] = q.x; y[4 * k + 1] = q.y; y[4 * k + 2] = q.z; y[4 * k + 3] = q.w;
+            }
+        }
+        e.apply(b, row + i * dr, col + i * dc, left(i), f[i], y);
+    }
+    if (mirror && c0 + lane < N) {                              // column `lane` of the piece is part of a row of the transposed result
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            if (r0 + 16 * i < M) e.fetch(b, c0 + lane, r0 + 16 * i, min(16u, M - r0 - 16 * i), f[i]);
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            if (r0 + 16 * i >= M) continue;
+            float y[16];
+#pragma unroll
+            for (uint32_t k = 0; k < 16; ++k) {
+                const uint32_t r = 16 * i + k;
+                y[k] = *reinterpret_cast<const float*>(piece + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+            }
+            e.apply(b, c0 + lane, r0 + 16 * i, min(16u, M - r0 - 16 * i), f[i], y);
+        }
+    }
+    __syncwarp();
+}
+
+template <int CG, bool RUNS, typename E>
 __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_constant__ ProductArgs a, const __grid_constant__ E e)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -92,131 +154,135 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
     wait_before();
     after_start();
 
-    if (warp == 8) {                                            // ---- loads
-        uint32_t st = 0, round = 0, total = 0;
+    // With runs a writer holds 128 sums.  Registers of a thread: 168 at launch, then 224 in two warpgroups and 56 in the third, the same
+    // 64512 in all.
+    if (warp >= kProdWriters) {
+        if (RUNS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8 || warp == 10) {                              // ---- loads: A by one warp, B by another
+            const bool is_a = warp == 8, mn = is_a ? a.a_mn : a.b_mn;
+            const CUtensorMap* words = is_a ? a.a : a.b;
+            const uint32_t boxes = is_a ? 2 : a.b_bytes / 8192, tile = is_a ? 128 * CG : a.bn, mine = rank * (tile / CG);
+            const uint32_t full_at = uniform(smem_addr(full)), full_to = CG == 2 ? uniform(in_block(full, 0)) : full_at;
+            const uint32_t dst0 = uniform(smem_addr(ring)) + (is_a ? 0 : 128 * 128), end = a.term_steps * kStep;
+            uint32_t st = 0, phase = 1, total = 0;                  // the first round of waits passes at once
+            bool ok = true, ready = true;
+            for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
+                const ProdItem t = prod_item<CG>(a, x);
+                const int at_row = (int)((is_a ? t.i : t.j) * tile + mine), b = (int)t.b;
+                uint32_t term = t.k0 / a.term_steps, at = (t.k0 - term * a.term_steps) * kStep, left = t.k1 - t.k0;
+                const CUtensorMap* map = &words[is_a ? term == 2 : term == 1];
+                for (; left; --left, ++total) {
+                    if (!__all_sync(0xFFFFFFFFu, ready)) ok = warp_wait(&empty[st], phase, g);
+                    if (!ok) break;
+                    const uint32_t dst = dst0 + st * a.stage_bytes, bar = full_to + st * 8;
+                    if (is_a && rank == 0) warp_expect(full_at + st * 8, CG * a.stage_bytes);
+                    if (++st == a.stages) { st = 0; phase ^= 1; }
+                    ready = bar_try(&empty[st], phase);             // the next stage's, beside this one's loads
+                    if (mn)
+                        for (uint32_t c = 0; c < boxes; ++c) warp_tma3<CG>(dst + c * 8192, map, bar, at_row + (int)c * 64, (int)at, b);
+                    else
+                        warp_tma3<CG>(dst, map, bar, (int)at, at_row, b);
+                    if ((at += kStep) == end) {
+                        at = 0;
+                        ++term;
+                        map = &words[is_a ? term == 2 : term == 1];
+                    }
+                }
+            }
+            if (is_a && rank == 0 && lane == 0) {                   // every copy lands before the block (its pair) may end
+                for (uint32_t i = 0; i < min(total, a.stages); ++i) {
+                    const uint32_t n = total - 1 - i;
+                    bar_drain(&full[n % a.stages], (n / a.stages) & 1);
+                }
+            }
+        } else if (warp == 9) {                                     // ---- products
+            if (rank == 0) {
+                uint32_t st = 0, phase = 0, w = 0;
+                bool ok = true, ready = false;
+                const uint64_t a0 = a.a_mn ? desc_mn(smem_addr(ring), 8192) : desc_k(smem_addr(ring));
+                const uint64_t b0 = a.b_mn ? desc_mn(smem_addr(ring) + 128 * 128, 8192) : desc_k(smem_addr(ring) + 128 * 128);
+                const uint32_t a_step = a.a_mn ? 2048 / 16 : 32 / 16, b_step = a.b_mn ? 2048 / 16 : 32 / 16, stage = a.stage_bytes / 16;
+                for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
+                    const ProdItem t = prod_item<CG>(a, x);
+                    const uint32_t n = uniform(t.k1 - t.k0);
+                    uint32_t acc = 0;
+                    for (uint32_t k = 0, run = 0; k < n; ++k) {
+                        if (run == 0) {                             // a run of stages whose sums are taken together
+                            if (w >= 2) ok = warp_wait(&acc_free[w & 1], ((w >> 1) - 1) & 1, g);
+                            if (!ok) break;
+                            acc = tmem + (w & 1) * a.acc_cols;
+                        }
+                        if (!__all_sync(0xFFFFFFFFu, ready)) ok = warp_wait(&full[st], phase, g);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t now = st;
+                        if (++st == a.stages) { st = 0; phase ^= 1; }
+                        ready = bar_try(&full[st], phase);          // the next stage's, beside this one's products
+                        mma4_commit<CG>(acc, a0 + uniform(now * stage), b0 + uniform(now * stage), a_step, b_step, a.idesc, run > 0, &empty[now]);
+                        if (++run == (RUNS ? kRun : n) || k + 1 == n) {
+                            commit_cg<CG>(&acc_full[w & 1]);
+                            ++w;
+                            run = 0;
+                        }
+                    }
+                }
+                __syncwarp();
+                mma_commit_idle<CG>(&idle);                         // products in flight end before the memory is freed, whoever gave up
+                bar_drain(&idle, 0);
+            }
+        }
+    } else {                                                    // ---- sums to their places
+        if (RUNS) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        uint8_t* piece = ring + a.stages * a.stage_bytes + warp * kPieceBytes;
+        const uint32_t lanes = (warp & 3) * 32, half = (warp >> 2) * 32;
+        uint32_t w = 0;
         bool ok = true;
         for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
             const ProdItem t = prod_item<CG>(a, x);
-            const int row = (int)((t.i * CG + rank) * 128), col = (int)(t.j * a.bn + rank * (a.bn / CG));
-            for (uint32_t k = t.k0; k < t.k1; ++k, ++total) {
-                if (round) ok = warp_wait(&empty[st], (round - 1) & 1, g);
-                if (!ok) break;
-                if (lane == 0) {
-                    const uint32_t term = k / a.term_steps, at = (k - term * a.term_steps) * kStep;
-                    const CUtensorMap *ma = &a.a[term == 2], *mb = &a.b[term == 1];
-                    uint8_t *da = ring + st * a.stage_bytes, *db = da + 128 * 128;
-                    const uint32_t bar = CG == 2 ? in_block(&full[st], 0) : smem_addr(&full[st]);
-                    if (rank == 0) bar_expect(&full[st], CG * a.stage_bytes);
-                    if (a.a_mn) {
-                        tma_tile3<CG>(da, ma, bar, row, (int)at, (int)t.b);
-                        tma_tile3<CG>(da + 8192, ma, bar, row + 64, (int)at, (int)t.b);
-                    } else {
-                        tma_tile3<CG>(da, ma, bar, (int)at, row, (int)t.b);
-                    }
-                    if (a.b_mn)
-                        for (uint32_t c = 0; c < a.b_bytes / 8192; ++c) tma_tile3<CG>(db + c * 8192, mb, bar, col + (int)c * 64, (int)at, (int)t.b);
-                    else
-                        tma_tile3<CG>(db, mb, bar, (int)at, col, (int)t.b);
-                }
-                __syncwarp();
-                if (++st == a.stages) { st = 0; ++round; }
-            }
-        }
-        if (lane == 0 && rank == 0) {                           // every copy lands before the block (its pair) may end
-            for (uint32_t i = 0; i < min(total, a.stages); ++i) {
-                const uint32_t n = total - 1 - i;
-                bar_drain(&full[n % a.stages], (n / a.stages) & 1);
-            }
-        }
-    } else if (warp == 9) {                                     // ---- products
-        if (rank == 0) {
-            uint32_t st = 0, phase = 0, w = 0;
-            bool ok = true;
-            const uint32_t base = smem_addr(ring);
-            for (uint32_t x = first_item; x < a.items && ok; x += item_stride, ++w) {
-                const ProdItem t = prod_item<CG>(a, x);
-                const uint32_t acc = tmem + (w & 1) * a.acc_cols, n = uniform(t.k1 - t.k0);
-                if (w >= 2) ok = warp_wait(&acc_free[w & 1], ((w >> 1) - 1) & 1, g);
-                if (!ok) break;
-                tc_fence_after();
-                for (uint32_t k = 0; k < n; ++k) {
-                    ok = warp_wait(&full[st], phase, g);
+            const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, c0 = t.j * a.bn + half;
+            if (RUNS) {
+                float2 sums[4][16] = {};
+                const uint32_t n = t.k1 - t.k0;
+                for (uint32_t k = 0; k < n; k += kRun, ++w) {
+                    ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t pa = uniform(base + st * a.stage_bytes), pb = pa + 128 * 128;
+                    const uint32_t acc = tmem + (w & 1) * a.acc_cols + (lanes << 16) + half;
 #pragma unroll
-                    for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
-                        const uint64_t da = a.a_mn ? desc_mn(pa + kk * 2048, 8192) : desc_k(pa + kk * 32);
-                        const uint64_t db = a.b_mn ? desc_mn(pb + kk * 2048, 8192) : desc_k(pb + kk * 32);
-                        mma_cg<CG>(acc, da, db, a.idesc, k > 0 || kk > 0);
+                    for (uint32_t p = 0; p < 4; ++p) {
+                        if (half + 64 * p >= a.bn) continue;
+                        uint32_t v[32];
+                        tmem_ld32(acc + 64 * p, v);
+                        tmem_wait_ld<32>(v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sums[p][i] = add2(sums[p][i], pair(v[2 * i], v[2 * i + 1]));
                     }
-                    commit_cg<CG>(&empty[st]);
-                    if (++st == a.stages) { st = 0; phase ^= 1; }
+                    tc_fence_before();
+                    if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
+                    else warp_arrive(&acc_free[w & 1]);
                 }
-                if (ok) commit_cg<CG>(&acc_full[w & 1]);
-            }
-            __syncwarp();
-            mma_commit_idle<CG>(&idle);                         // products in flight end before the memory is freed, whoever gave up
-            bar_drain(&idle, 0);
-        }
-    } else {                                                    // ---- sums to their places
-        float* piece = (float*)(ring + a.stages * a.stage_bytes + warp * kPieceBytes);
-        const uint32_t lanes = (warp & 3) * 32, M = a.M, N = a.N;
-        uint32_t w = 0;
-        bool ok = true;
-        for (uint32_t x = first_item; x < a.items && ok; x += item_stride, ++w) {
-            const ProdItem t = prod_item<CG>(a, x);
-            const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, acc = tmem + (w & 1) * a.acc_cols + (lanes << 16);
-            ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
-            if (!ok) break;
-            tc_fence_after();
-            if (r0 < M) {
-                for (uint32_t c = (warp >> 2) * 32; c < a.bn; c += 64) {
-                    const uint32_t c0 = t.j * a.bn + c;
-                    if (c0 >= N || (a.symmetric && c0 < r0)) continue;
-                    typename E::Fetched f[4];
-                    const bool plain = !a.turned, mirror = a.turned || (a.symmetric && c0 > r0);
-                    const uint32_t pr = r0 + lane / 4, pc = c0 + (lane & 3) * 8, pl = pc < N ? min(8u, N - pc) : 0;
-                    if (plain)
+                if (!ok) break;
 #pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i)
-                            if (pl && pr + 8 * i < M) e.fetch(t.out, pr + 8 * i, pc, pl, f[i]);
-                    uint32_t v[32];
-                    __syncwarp();
-                    tmem_ld32(acc + c, v);
-                    tmem_wait_ld<32>(v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4*>(piece + lane * kPieceStride + 4 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                    __syncwarp();
-                    if (plain)
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) {
-                            if (!pl || pr + 8 * i >= M) continue;
-                            const float4* s = reinterpret_cast<const float4*>(piece + (lane / 4 + 8 * i) * kPieceStride + (lane & 3) * 8);
-                            const float4 lo = s[0], hi = s[1];
-                            float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                            e.apply(t.out, pr + 8 * i, pc, pl, f[i], y);
-                        }
-                    if (mirror && c0 + lane < N) {              // column `lane` of the piece is a row of the transposed result
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i)
-                            if (r0 + 8 * i < M) e.fetch(t.out, c0 + lane, r0 + 8 * i, min(8u, M - r0 - 8 * i), f[i]);
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) {
-                            if (r0 + 8 * i >= M) continue;
-                            float y[8];
-#pragma unroll
-                            for (int r = 0; r < 8; ++r) y[r] = piece[(8 * i + r) * kPieceStride + lane];
-                            e.apply(t.out, c0 + lane, r0 + 8 * i, min(8u, M - r0 - 8 * i), f[i], y);
-                        }
-                    }
-                    __syncwarp();
+                for (uint32_t p = 0; p < 4; ++p)
+                    if (half + 64 * p < a.bn) write_piece(a, e, t.out, r0, c0 + 64 * p, reinterpret_cast<float*>(sums[p]), piece, [] {});
+            } else {
+                ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t acc = tmem + (w & 1) * a.acc_cols + (lanes << 16) + half;
+                for (uint32_t c = 0; half + c < a.bn; c += 64) {
+                    float v[32];
+                    write_piece(a, e, t.out, r0, c0 + c, v, piece, [&] {
+                        __syncwarp();
+                        tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(v));
+                        tmem_wait_ld<32>(reinterpret_cast<uint32_t*>(v));
+                    });
                 }
+                tc_fence_before();
+                if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
+                else warp_arrive(&acc_free[w & 1]);
+                ++w;
             }
-            tc_fence_before();
-            if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
-            else warp_arrive(&acc_free[w & 1]);
         }
     }
     __syncwarp();
@@ -228,25 +294,27 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
 }
 
 // Sums of the parts, in order, and the epilogue; parts = 0: sums of nothing.
+constexpr int kJoinThreads = 64;
 template <typename E>
-__global__ void __launch_bounds__(256) k_product_join(const __grid_constant__ E e, EpiPartial from, uint32_t parts, uint32_t M, uint32_t N, uint32_t batch)
+__global__ void __launch_bounds__(kJoinThreads) k_product_join(const __grid_constant__ E e, EpiPartial from, uint32_t parts, uint32_t M, uint32_t N, uint32_t batch)
 {
     wait_before();
     after_start();
-    const uint32_t per_row = (N + 7) / 8;
-    const uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = x / per_row;
-    const uint32_t n = (uint32_t)(x - row * per_row) * 8, b = (uint32_t)(row / M), m = (uint32_t)(row - (uint64_t)b * M);
+    const uint32_t per_row = (N + 15) / 16;
+    const uint64_t x = (uint64_t)blockIdx.x * kJoinThreads + threadIdx.x, row = x / per_row;
+    const uint32_t n = (uint32_t)(x - row * per_row) * 16, b = (uint32_t)(row / M), m = (uint32_t)(row - (uint64_t)b * M);
     if (b >= batch) return;
     typename E::Fetched f;
-    const uint32_t left = min(8u, N - n);
+    const uint32_t left = min(16u, N - n);
     e.fetch(b, m, n, left, f);
-    float v[8] = {};
+    float v[16] = {};
     const float* p = from.p + (uint64_t)b * parts * from.each + (int64_t)m * from.stride + n;
     for (uint32_t s = 0; s < parts; ++s) {
-        const float4 lo = *reinterpret_cast<const float4*>(p + s * from.each), hi = *reinterpret_cast<const float4*>(p + s * from.each + 4);
-        const float t[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        uint32_t t[16];
+        load32(p + s * from.each, t);
+        load32(p + s * from.each + 8, t + 8);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += t[i];
+        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(t[i]);
     }
     e.apply(b, m, n, left, f, v);
 }
@@ -335,7 +403,7 @@ static ProductPlan plan_product(const Product& p)
             }
         }
     }
-    r.partial_stride = (p.N + 7) & ~7u;
+    r.partial_stride = (p.N + 15) & ~15u;
     r.partial_bytes = r.parts > 1 ? padded((size_t)r.parts * p.batch * p.M * r.partial_stride * 4) : 0;
     return r;
 }
@@ -362,10 +430,19 @@ static int make_map(CUtensorMap* map, const void* data, int64_t stride, const Op
     return DBLP_OK;
 }
 
-template <int CG, typename E> static int launch_product(const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
+template <int CG, bool RUNS, typename E> static int launch_product(const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
 {
-    constexpr auto kernel = k_product<CG, E>;
+    constexpr auto kernel = k_product<CG, RUNS, E>;
     DBLP_CUDA(allow_shared<kernel>(kProdSmem));
+    if (RUNS) {                                                 // the split of registers inside counts on this
+        static std::atomic<int> regs{0};
+        if (regs.load(std::memory_order_acquire) == 0) {
+            cudaFuncAttributes fa;
+            DBLP_CUDA(cudaFuncGetAttributes(&fa, kernel));
+            regs.store(fa.numRegs, std::memory_order_release);
+        }
+        DBLP_REQUIRE(regs.load(std::memory_order_acquire) == 168, DBLP_ECUDA, "product: built with %d registers a thread, not 168", regs.load());
+    }
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg{};
     const uint32_t slots = kSms / CG;
@@ -389,14 +466,21 @@ template <int CG, typename E> static int launch_product(const ProductArgs& a, co
     return DBLP_OK;
 }
 
+template <typename E> static int launch_product(int cg, bool runs, const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
+{
+    if constexpr (!std::is_same<E, EpiGradX>::value)            // dx is never fp32
+        if (runs) return cg == 2 ? launch_product<2, true>(a, e, chained, s) : launch_product<1, true>(a, e, chained, s);
+    return cg == 2 ? launch_product<2, false>(a, e, chained, s) : launch_product<1, false>(a, e, chained, s);
+}
+
 template <typename E> static int launch_join(const E& e, const EpiPartial& from, uint32_t parts, const Product& p, bool chained, cudaStream_t s)
 {
-    const uint64_t groups = (uint64_t)p.batch * p.M * ((p.N + 7) / 8), blocks = (groups + 255) / 256;
+    const uint64_t groups = (uint64_t)p.batch * p.M * ((p.N + 15) / 16), blocks = (groups + kJoinThreads - 1) / kJoinThreads;
     DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^42 elements or more");
     if (chained) {
-        DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)blocks), 256, 0, s, e, from, parts, p.M, p.N, p.batch));
+        DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)blocks), kJoinThreads, 0, s, e, from, parts, p.M, p.N, p.batch));
     } else {
-        k_product_join<E><<<(unsigned)blocks, 256, 0, s>>>(e, from, parts, p.M, p.N, p.batch);
+        k_product_join<E><<<(unsigned)blocks, kJoinThreads, 0, s>>>(e, from, parts, p.M, p.N, p.batch);
         DBLP_LAUNCHED();
     }
     return DBLP_OK;
@@ -467,9 +551,11 @@ template <typename E> int run_product(const Product& p, const E& e, void* ws, bo
     a.acc_cols = r.bn < 32 ? 32 : r.bn;
     a.idesc = p.dtype == DBLP_BF16 ? mma_desc<__nv_bfloat16>(128 * r.cg, r.bn, oa.mn, ob.mn) : mma_desc<__half>(128 * r.cg, r.bn, oa.mn, ob.mn);
     a.timeouts = timeouts;
-    if (r.parts == 1) return r.cg == 2 ? launch_product<2>(a, e, chained, s) : launch_product<1>(a, e, chained, s);
+    a.direct = e.sectors();
+    if (r.parts == 1) return launch_product(r.cg, p.runs, a, e, chained, s);
     const EpiPartial sums{(float*)at, (int64_t)p.M * r.partial_stride, r.partial_stride};
-    if (int rc = r.cg == 2 ? launch_product<2>(a, sums, chained, s) : launch_product<1>(a, sums, chained, s)) return rc;
+    a.direct = true;
+    if (int rc = launch_product(r.cg, p.runs, a, sums, chained, s)) return rc;
     return launch_join(e, sums, r.parts, p, true, s);
 }
 

@@ -19,6 +19,7 @@ struct Product {
     uint32_t M, N, K, batch;
     int dtype;                  // of both operands
     int terms;                  // 1, or 3: hi hi + hi lo + lo hi
+    bool runs;                  // the result is wanted to fp32's precision: the tensor cores' sums, which truncate, are taken in short runs
     bool symmetric;             // M = N and the result equals its transpose: computed once, written twice
 };
 

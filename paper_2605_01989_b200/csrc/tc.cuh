@@ -311,17 +311,26 @@ __device__ __forceinline__ void warp_arrive_in(uint32_t cluster_bar)
     __syncwarp();
     if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// bar: in the cluster's window.  A pair's loads may count on the barrier of either block.
-template <int CG> __device__ __forceinline__ void tma_tile3(void* dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2)
+// A tile load by one lane of a warp that runs together, elected in the same statement, with addresses that are visibly uniform (as
+// for products: by a branch on the lane number a load took 150 cycles to issue).  bar: in the cluster's window; a pair's loads
+// may count on the barrier of either block.
+template <int CG> __device__ __forceinline__ void warp_tma3(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2)
 {
     if (CG == 2)
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
-                     ::"r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                     "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];\n}"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                      : "memory");
     else
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                     ::"r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n"
+                     "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                      : "memory");
+}
+__device__ __forceinline__ void warp_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar), "r"(bytes)
+                 : "memory");
 }
 // cols: a power of two from 32 to 512; by one warp of each block
 template <int CG> __device__ __forceinline__ void tmem_alloc_cols(uint32_t* slot, uint32_t cols)
@@ -339,14 +348,24 @@ template <int CG> __device__ __forceinline__ void tmem_free_cols(uint32_t addr, 
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
 }
-template <int CG> __device__ __forceinline__ void mma_cg(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+// Four products along the summed dimension, 16 each, descriptors `a_step` and `b_step` apart, and their commit to `bar` (of both
+// blocks of a pair): one statement, one election (apart, an election each, they cost 330 cycles a stage to issue).
+template <int CG>
+__device__ __forceinline__ void mma4_commit(uint32_t d, uint64_t a, uint64_t b, uint32_t a_step, uint32_t b_step, uint32_t idesc, uint32_t acc, uint64_t* bar)
 {
-    if (CG == 2)
-        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xFFFFFFFF;\n"
-                     "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
-                     : "memory");
-    else
-        mma_ss(d, a, b, idesc, acc);
+#define DBLP_MMA4(CGS, COMMIT)                                                                                                   \
+    asm volatile("{\n.reg .pred p, q, t;\n.reg .b64 a, b, x, y;\n.reg .b16 m;\nmov.b16 m, 3;\ncvt.u64.u32 x, %3;\ncvt.u64.u32 y, %4;\n" \
+                 "setp.ne.b32 p, %6, 0;\nsetp.eq.b32 t, %6, %6;\nelect.sync _|q, 0xFFFFFFFF;\n"                                   \
+                 "@q tcgen05.mma.cta_group::" CGS ".kind::f16 [%0], %1, %2, %5, p;\nadd.u64 a, %1, x;\nadd.u64 b, %2, y;\n"      \
+                 "@q tcgen05.mma.cta_group::" CGS ".kind::f16 [%0], a, b, %5, t;\nadd.u64 a, a, x;\nadd.u64 b, b, y;\n"          \
+                 "@q tcgen05.mma.cta_group::" CGS ".kind::f16 [%0], a, b, %5, t;\nadd.u64 a, a, x;\nadd.u64 b, b, y;\n"          \
+                 "@q tcgen05.mma.cta_group::" CGS ".kind::f16 [%0], a, b, %5, t;\n"                                               \
+                 "@q tcgen05.commit.cta_group::" CGS ".mbarrier::arrive::one.shared::cluster" COMMIT ";\n}" ::"r"(d),            \
+                 "l"(a), "l"(b), "r"(a_step), "r"(b_step), "r"(idesc), "r"(acc), "r"(smem_addr(bar))                               \
+                 : "memory")
+    if (CG == 2) DBLP_MMA4("2", ".multicast::cluster.b64 [%7], m");
+    else DBLP_MMA4("1", ".b64 [%7]");
+#undef DBLP_MMA4
 }
 // As mma_commit; a pair's arrives on the barriers of both blocks.
 template <int CG> __device__ __forceinline__ void commit_cg(uint64_t* bar)
