@@ -2,7 +2,7 @@
 // 16-bit matrix (two accesses of 16 bytes at a stride of 32 touch every sector twice).
 #pragma once
 
-#include "types.cuh"
+#include "tc.cuh"
 
 namespace dblp {
 
@@ -156,29 +156,30 @@ __device__ __forceinline__ float reciprocal(float x)            // 0 of infinity
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float exp2_approx(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 // 1 / (1 + e^-x), 0 and 1 at the ends.
-__device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + exp2_approx(-1.4426950408889634f * x)); }
+__device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + exp2_fast(-1.4426950408889634f * x)); }
 
 // gelu_tanh(z) = z logistic(2 u), 2 u = sqrt(8 / pi) (z + 0.044715 z^3): the same function without a tanh.
 __device__ __forceinline__ float tanh_arg(float z) { return 1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f); }
 
-// The normal distribution's integral up to z, and e^(-z^2 / 2).  With x = |z| / sqrt 2 and t = 1 / (1 + 0.46 x), the tail erfc(x) / 2 is
-// e^(-x^2) t P(t): P of degree 7 was fitted here to the least largest relative error over x >= 0 (7e-7), so that far tails keep
-// their digits.  (CUDA's erfcf in its place: 8192 x 1600 -> 6400 with gelu 431 us instead of 148 without, the epilogue outlasted
-// the products.)
-__device__ __forceinline__ float normal_cdf(float z, float& e)
+// The normal distribution's integral up to z, and e^(-z^2 / 2), of two values.  With x = |z| / sqrt 2 and t = 1 / (1 + 0.46 x), the tail
+// erfc(x) / 2 is e^(-x^2) t P(t): P of degree 7 was fitted here to the least largest relative error over x >= 0 (7e-7), so that far
+// tails keep their digits.  (CUDA's erfcf in its place: 8192 x 1600 -> 6400 with bias and gelu 431 us instead of 184.)
+__device__ __forceinline__ float2 normal_cdf(float2 z, float2& e)
 {
-    const float x = fabsf(z), t = reciprocal(fmaf(0.32526912f, x, 1.0f));
-    e = exp2_approx(-0.72134752f * z * z);
-    float p = fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(0.0338571332f, t, -0.113314494f), t, 0.0845952928f), t, 0.0263054594f), t, 0.0934238359f), t, 0.115590952f), t, 0.129778638f), t, 0.129763529f);
-    p = p * t * e;
-    return z > 0.0f ? 1.0f - p : p;
+    auto two = [](float x) { return make_float2(x, x); };
+    const float2 d = fma2(make_float2(fabsf(z.x), fabsf(z.y)), two(0.32526912f), two(1.0f)), t = make_float2(reciprocal(d.x), reciprocal(d.y));
+    const float2 x = mul2(mul2(z, two(-0.72134752f)), z);
+    e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+    float2 p = fma2(two(0.0338571332f), t, two(-0.113314494f));
+    p = fma2(p, t, two(0.0845952928f));
+    p = fma2(p, t, two(0.0263054594f));
+    p = fma2(p, t, two(0.0934238359f));
+    p = fma2(p, t, two(0.115590952f));
+    p = fma2(p, t, two(0.129778638f));
+    p = mul2(mul2(fma2(p, t, two(0.129763529f)), t), e);
+    const float2 q = fma2(p, two(-1.0f), two(1.0f));
+    return make_float2(z.x > 0.0f ? q.x : p.x, z.y > 0.0f ? q.y : p.y);
 }
 
 template <int N> __device__ __forceinline__ void activate(int act, float* z)
@@ -190,9 +191,11 @@ template <int N> __device__ __forceinline__ void activate(int act, float* z)
         break;
     case DBLP_ACT_GELU:
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float e;
-            z[i] *= normal_cdf(z[i], e);
+        for (int i = 0; i < N; i += 2) {
+            float2 e;
+            const float2 x = make_float2(z[i], z[i + 1]), y = mul2(x, normal_cdf(x, e));
+            z[i] = y.x;
+            z[i + 1] = y.y;
         }
         break;
     case DBLP_ACT_GELU_TANH:
@@ -217,10 +220,11 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
         break;
     case DBLP_ACT_GELU:
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float e;
-            const float c = normal_cdf(z[i], e);
-            y[i] *= fmaf(z[i] * 0.39894228040143268f, e, c);
+        for (int i = 0; i < N; i += 2) {
+            float2 e;
+            const float2 x = make_float2(z[i], z[i + 1]), c = normal_cdf(x, e), d = fma2(mul2(x, make_float2(0.39894228f, 0.39894228f)), e, c);
+            y[i] *= d.x;
+            y[i + 1] *= d.y;
         }
         break;
     case DBLP_ACT_GELU_TANH:
@@ -247,18 +251,17 @@ struct EpiLinear {                        // out = act(z) + residual, pre = z = 
     Rows out, residual, pre, bias;
     int act;
     bool sectors() const { return whole(out) && whole(residual) && whole(pre); }
-    struct Fetched { Raw residual; };
+    struct Fetched { Raw bias, residual; };
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, uint32_t left, Fetched& f) const
     {
+        if (bias) fetch16(bias, 0, n, left, f.bias);
         if (residual) fetch16(residual, m, n, left, f.residual);
     }
     __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, uint32_t left, const Fetched& f, float* v) const
     {
         float t[16];
         if (bias) {
-            Raw b;
-            fetch16(bias, 0, n, left, b);
-            use16(bias, left, b, t);
+            use16(bias, left, f.bias, t);
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] += t[i];
         }
@@ -317,20 +320,6 @@ struct EpiStore {                         // out = v [+ out]
             for (int i = 0; i < 16; ++i) v[i] += t[i];
         }
         store16(out, m, n, left, v);
-    }
-};
-
-// The sums themselves, fp32, one matrix of M x stride per (product, part of the summed dimension): b numbers them.
-struct EpiPartial {
-    float* p;
-    int64_t each;
-    uint32_t stride;                      // a multiple of sixteen
-    struct Fetched {};
-    bool sectors() const { return true; }
-    __device__ __forceinline__ void fetch(uint32_t, uint32_t, uint32_t, uint32_t, Fetched&) const {}
-    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, uint32_t, const Fetched&, float* v) const
-    {
-        store16(p + b * each + (int64_t)m * stride + n, 16, 32, v);           // rows are padded: whole groups always fit
     }
 };
 

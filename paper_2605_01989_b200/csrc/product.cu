@@ -26,42 +26,59 @@ constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block 
 
 struct ProductArgs {
     CUtensorMap a[2], b[2];                                     // first and second words
-    uint32_t M, N, bn, mt, nt;                                  // tiles of 128 (256) x bn
-    uint32_t steps, per, parts, items;                          // stages in all (terms together), of a part; parts of a tile; items in all
-    uint32_t term_steps, group, tiles;                          // stages of a term; tile rows walked together; tiles of one product
+    uint32_t M, N, tm, bn, mt, nt;                              // tiles of tm = 128 (256) rows x bn columns
+    uint32_t steps, term_steps;                                 // stages of a tile (terms together), of a term
+    uint32_t whole, rest, parts, per, items;                    // tiles done whole; tiles done in parts of `per` stages; items in all
+    uint32_t group, tiles;                                      // tile rows walked together; tiles of one product
+    FastDiv by_tiles, by_rest, by_all, by_group, by_last;
     uint32_t stages, stage_bytes, b_bytes, acc_cols, idesc;
     uint32_t a_mn, b_mn, symmetric, turned, direct;
+    float* partial;                                             // [rest][parts][tm][bn]
     unsigned long long* timeouts;
 };
 
 struct ProdItem {
-    uint32_t i, j, b, out, k0, k1;                              // tile, product, number of the sums, stages
+    uint32_t i, j, b, k0, k1;                                   // tile, product, stages
+    uint32_t slot;                                              // where its sums go in `partial`; kWhole: to the epilogue
 };
+constexpr uint32_t kWhole = 0xFFFFFFFFu;
 
-template <int CG> __host__ __device__ __forceinline__ ProdItem prod_item(const ProductArgs& a, uint32_t x)
+// Tile number g of all products.
+__host__ __device__ __forceinline__ void place_tile(const ProductArgs& a, uint32_t g, ProdItem& t)
 {
-    ProdItem t;
-    const uint32_t q = x / a.tiles;
-    uint32_t y = x - q * a.tiles;
-    t.out = q;
-    t.b = q / a.parts;
-    const uint32_t part = q - t.b * a.parts;
-    t.k0 = part * a.per;
-    t.k1 = min(t.k0 + a.per, a.steps);
+    t.b = a.by_tiles.div(g);
+    uint32_t y = g - t.b * a.tiles;
     if (a.symmetric) {                                          // tiles that reach the diagonal or lie above it, row by row
         uint32_t i = 0, first = 0;
         while (y >= a.nt - first) {
             y -= a.nt - first;
             ++i;
-            first = i * 128 * CG / a.bn;
+            first = i * a.tm / a.bn;
         }
         t.i = i;
         t.j = first + y;
     } else {                                                    // `group` tile rows together, column by column: operands stay in L2
-        const uint32_t all = a.group * a.nt, g = y / all, first = g * a.group, rows = min(a.group, a.mt - first), r = y - g * all;
-        t.j = r / rows;
-        t.i = first + r - t.j * rows;
+        const uint32_t q = a.by_all.div(y), first = q * a.group, r = y - q * a.group * a.nt;
+        const bool last = first + a.group > a.mt;
+        t.j = last ? a.by_last.div(r) : a.by_group.div(r);
+        t.i = first + r - t.j * (last ? a.mt - first : a.group);
     }
+}
+
+__host__ __device__ __forceinline__ ProdItem prod_item(const ProductArgs& a, uint32_t x)
+{
+    ProdItem t;
+    t.k0 = 0;
+    t.k1 = a.steps;
+    t.slot = kWhole;
+    if (x >= a.whole) {
+        const uint32_t y = x - a.whole, part = a.by_rest.div(y), n = y - part * a.rest;
+        t.k0 = part * a.per;
+        t.k1 = t.k0 + a.per < a.steps ? t.k0 + a.per : a.steps;
+        t.slot = n * a.parts + part;
+        x = a.whole + n;
+    }
+    place_tile(a, x, t);
     return t;
 }
 
@@ -127,6 +144,18 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
     __syncwarp();
 }
 
+// The same sums as they are, for the join.
+template <typename F>
+__device__ __forceinline__ void write_partial(const ProductArgs& a, const ProdItem& t, uint32_t r0, uint32_t c0, float* v, const F& sums)
+{
+    if (r0 >= a.M || c0 >= a.N || (a.symmetric && c0 < r0)) return;
+    sums();
+    float* p = a.partial + ((size_t)t.slot * a.tm + (r0 - t.i * a.tm) + (threadIdx.x & 31)) * a.bn + (c0 - t.j * a.bn);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+        if (8 * i < a.bn) store32(p + 8 * i, reinterpret_cast<const uint32_t*>(v) + 8 * i);
+}
+
 template <int CG, bool RUNS, typename E>
 __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_constant__ ProductArgs a, const __grid_constant__ E e)
 {
@@ -167,7 +196,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             uint32_t st = 0, phase = 1, total = 0;                  // the first round of waits passes at once
             bool ok = true, ready = true;
             for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
-                const ProdItem t = prod_item<CG>(a, x);
+                const ProdItem t = prod_item(a, x);
                 const int at_row = (int)((is_a ? t.i : t.j) * tile + mine), b = (int)t.b;
                 uint32_t term = t.k0 / a.term_steps, at = (t.k0 - term * a.term_steps) * kStep, left = t.k1 - t.k0;
                 const CUtensorMap* map = &words[is_a ? term == 2 : term == 1];
@@ -203,7 +232,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                 const uint64_t b0 = a.b_mn ? desc_mn(smem_addr(ring) + 128 * 128, 8192) : desc_k(smem_addr(ring) + 128 * 128);
                 const uint32_t a_step = a.a_mn ? 2048 / 16 : 32 / 16, b_step = a.b_mn ? 2048 / 16 : 32 / 16, stage = a.stage_bytes / 16;
                 for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
-                    const ProdItem t = prod_item<CG>(a, x);
+                    const ProdItem t = prod_item(a, x);
                     const uint32_t n = uniform(t.k1 - t.k0);
                     uint32_t acc = 0;
                     for (uint32_t k = 0, run = 0; k < n; ++k) {
@@ -238,7 +267,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
         uint32_t w = 0;
         bool ok = true;
         for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
-            const ProdItem t = prod_item<CG>(a, x);
+            const ProdItem t = prod_item(a, x);
             const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, c0 = t.j * a.bn + half;
             if (RUNS) {
                 float2 sums[4][16] = {};
@@ -264,7 +293,11 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                 if (!ok) break;
 #pragma unroll
                 for (uint32_t p = 0; p < 4; ++p)
-                    if (half + 64 * p < a.bn) write_piece(a, e, t.out, r0, c0 + 64 * p, reinterpret_cast<float*>(sums[p]), piece, [] {});
+                    if (half + 64 * p < a.bn) {
+                        float* v = reinterpret_cast<float*>(sums[p]);
+                        if (t.slot == kWhole) write_piece(a, e, t.b, r0, c0 + 64 * p, v, piece, [] {});
+                        else write_partial(a, t, r0, c0 + 64 * p, v, [] {});
+                    }
             } else {
                 ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
                 if (!ok) break;
@@ -272,11 +305,13 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                 const uint32_t acc = tmem + (w & 1) * a.acc_cols + (lanes << 16) + half;
                 for (uint32_t c = 0; half + c < a.bn; c += 64) {
                     float v[32];
-                    write_piece(a, e, t.out, r0, c0 + c, v, piece, [&] {
+                    auto sums = [&] {
                         __syncwarp();
                         tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(v));
                         tmem_wait_ld<32>(reinterpret_cast<uint32_t*>(v));
-                    });
+                    };
+                    if (t.slot == kWhole) write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
+                    else write_partial(a, t, r0, c0 + c, v, sums);
                 }
                 tc_fence_before();
                 if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
@@ -293,29 +328,46 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
     if (warp == 9) tmem_free_cols<CG>(tmem, 2 * a.acc_cols);
 }
 
-// Sums of the parts, in order, and the epilogue; parts = 0: sums of nothing.
-constexpr int kJoinThreads = 64;
-template <typename E>
-__global__ void __launch_bounds__(kJoinThreads) k_product_join(const __grid_constant__ E e, EpiPartial from, uint32_t parts, uint32_t M, uint32_t N, uint32_t batch)
+// Tiles that were done in parts: their sums, in order, and the epilogue; a warp a piece of 32 x 32.
+constexpr int kJoinWarps = 4;
+template <typename E> __global__ void __launch_bounds__(32 * kJoinWarps) k_product_join(const __grid_constant__ ProductArgs a, const __grid_constant__ E e)
+{
+    __shared__ __align__(128) uint8_t pieces[kJoinWarps][kPieceBytes];
+    wait_before();
+    after_start();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, across = (a.bn + 31) / 32, each = a.tm / 32 * across;
+    const uint32_t x = blockIdx.x * kJoinWarps + warp, n = x / each, y = x - n * each, pr = y / across, pc = y - pr * across;
+    if (n >= a.rest) return;
+    ProdItem t;
+    place_tile(a, a.whole + n, t);
+    float2 v[16] = {};
+    write_piece(a, e, t.b, t.i * a.tm + pr * 32, t.j * a.bn + pc * 32, reinterpret_cast<float*>(v), pieces[warp], [&] {
+        const float* p = a.partial + ((size_t)n * a.parts * a.tm + pr * 32 + lane) * a.bn + pc * 32;
+        for (uint32_t s = 0; s < a.parts; ++s, p += (size_t)a.tm * a.bn) {
+            uint32_t w[32];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                if (8 * i < a.bn) load32(p + 8 * i, w + 8 * i);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                if (2 * i < a.bn) v[i] = add2(v[i], pair(w[2 * i], w[2 * i + 1]));
+        }
+    });
+}
+
+// Nothing to sum: the epilogue of zeros.
+template <typename E> __global__ void __launch_bounds__(64) k_product_none(const __grid_constant__ E e, uint32_t M, uint32_t N, uint32_t batch)
 {
     wait_before();
     after_start();
     const uint32_t per_row = (N + 15) / 16;
-    const uint64_t x = (uint64_t)blockIdx.x * kJoinThreads + threadIdx.x, row = x / per_row;
+    const uint64_t x = (uint64_t)blockIdx.x * 64 + threadIdx.x, row = x / per_row;
     const uint32_t n = (uint32_t)(x - row * per_row) * 16, b = (uint32_t)(row / M), m = (uint32_t)(row - (uint64_t)b * M);
     if (b >= batch) return;
     typename E::Fetched f;
     const uint32_t left = min(16u, N - n);
-    e.fetch(b, m, n, left, f);
     float v[16] = {};
-    const float* p = from.p + (uint64_t)b * parts * from.each + (int64_t)m * from.stride + n;
-    for (uint32_t s = 0; s < parts; ++s) {
-        uint32_t t[16];
-        load32(p + s * from.each, t);
-        load32(p + s * from.each + 8, t + 8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(t[i]);
-    }
+    e.fetch(b, m, n, left, f);
     e.apply(b, m, n, left, f, v);
 }
 
@@ -338,12 +390,11 @@ __global__ void __launch_bounds__(256) k_repack(const uint16_t* src, int64_t str
 // ---- host ------------------------------------------------------------------------------------------------------------------
 struct ProductPlan {
     int cg;
-    uint32_t bn, mt, nt, tiles, parts, per, steps, term_steps;
+    uint32_t bn, mt, nt, tiles, whole, rest, parts, per, steps, term_steps;
     bool turned;                                                // A and B change places
     bool copy_a, copy_b;
     uint32_t a_to, b_to;                                        // rows of the copies
     size_t a_bytes, b_bytes, partial_bytes;                     // in workspace
-    uint32_t partial_stride;
 };
 
 static bool tma_reads(const Operand& o, uint32_t outer, uint32_t inner, uint32_t batch)
@@ -377,20 +428,23 @@ static ProductPlan plan_product(const Product& p)
     // Few rows become the columns of narrow tiles, which read B (weights) once and waste no products on rows that are not there.
     r.turned = !p.symmetric && p.M <= 128 && p.M < p.N && !p.a.mn;
     const uint32_t M = r.turned ? p.N : p.M, N = r.turned ? p.M : p.N;
+    // The shape and the cut with the shortest estimate, in cycles: `step` is what a stage was measured to take (64 x 8192 x 8192 and the
+    // like), by issue for small tiles and by L2 for large ones.  Tiles fill the machine in rounds; those of the last, incomplete
+    // round (all, where there is no other) may be done in parts, which cost a second kernel and their way through memory.
     double best = 1e300;
-    const struct { int cg; uint32_t bn; double step; } shapes[] = {{2, 256, 512}, {2, 128, 300}, {1, 256, 560}, {1, 128, 300}, {1, 64, 240}, {1, 32, 220}, {1, 16, 200}};
+    const struct { int cg; uint32_t bn; double step; } shapes[] = {{2, 256, 560}, {2, 128, 360}, {1, 256, 720}, {1, 128, 490}, {1, 64, 360}, {1, 32, 340}, {1, 16, 320}};
     for (const auto& c : shapes) {
         if (r.turned ? (c.cg == 2 || (c.bn >= 2 * N && c.bn > 16)) : c.bn < 64) continue;
         if (r.turned && c.bn < N && c.bn < 128) continue;
         const uint32_t tm = 128 * c.cg, mt = (uint32_t)(((uint64_t)M + tm - 1) / tm), nt = (N + c.bn - 1) / c.bn, tiles = count_tiles(p.symmetric, tm, c.bn, mt, nt);
-        const uint32_t slots = kSms / c.cg;
+        const uint64_t slots = kSms / c.cg, all = (uint64_t)tiles * p.batch, last = all % slots;
         for (uint32_t parts = 1; parts <= 16 && parts <= r.steps; ++parts) {
+            if (parts > 1 && last == 0) break;
             const uint32_t per = (r.steps + parts - 1) / parts;
             if ((r.steps + per - 1) / per != parts) continue;
-            const uint64_t items = (uint64_t)tiles * parts * p.batch, waves = (items + slots - 1) / slots;
-            // cycles: stages of the longest block, its first loads and last output, the parts written and read again
-            double t = (double)waves * per * c.step + 2500 + 10.0 * c.bn;
-            if (parts > 1) t += 5000 + (double)parts * p.batch * M * N * 8 / 2500;
+            const uint64_t rounds = all / slots, cut = (last * parts + slots - 1) / slots;
+            double t = (double)(rounds * r.steps + cut * per) * c.step + 4000 + 10.0 * c.bn;
+            if (parts > 1) t += 5000 + (double)last * parts * tm * c.bn * 8 / 2500;
             if (t < best) {
                 best = t;
                 r.cg = c.cg;
@@ -400,11 +454,12 @@ static ProductPlan plan_product(const Product& p)
                 r.tiles = tiles;
                 r.parts = parts;
                 r.per = per;
+                r.rest = parts > 1 ? (uint32_t)last : 0;
+                r.whole = (uint32_t)(all - r.rest);
             }
         }
     }
-    r.partial_stride = (p.N + 15) & ~15u;
-    r.partial_bytes = r.parts > 1 ? padded((size_t)r.parts * p.batch * p.M * r.partial_stride * 4) : 0;
+    r.partial_bytes = padded((size_t)r.rest * r.parts * 128 * r.cg * r.bn * 4);
     return r;
 }
 
@@ -473,19 +528,6 @@ template <typename E> static int launch_product(int cg, bool runs, const Product
     return cg == 2 ? launch_product<2, false>(a, e, chained, s) : launch_product<1, false>(a, e, chained, s);
 }
 
-template <typename E> static int launch_join(const E& e, const EpiPartial& from, uint32_t parts, const Product& p, bool chained, cudaStream_t s)
-{
-    const uint64_t groups = (uint64_t)p.batch * p.M * ((p.N + 15) / 16), blocks = (groups + kJoinThreads - 1) / kJoinThreads;
-    DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^42 elements or more");
-    if (chained) {
-        DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)blocks), kJoinThreads, 0, s, e, from, parts, p.M, p.N, p.batch));
-    } else {
-        k_product_join<E><<<(unsigned)blocks, kJoinThreads, 0, s>>>(e, from, parts, p.M, p.N, p.batch);
-        DBLP_LAUNCHED();
-    }
-    return DBLP_OK;
-}
-
 static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, uint32_t inner, cudaStream_t s)
 {
     const uint64_t blocks = ((uint64_t)outer * (stride / 8) + 255) / 256;
@@ -497,9 +539,15 @@ static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, u
 
 template <typename E> int run_product(const Product& p, const E& e, void* ws, bool chained, cudaStream_t s)
 {
-    if (p.K == 0) return launch_join(e, EpiPartial{}, 0, p, chained, s);
+    if (p.K == 0) {
+        const uint64_t blocks = ((uint64_t)p.batch * p.M * ((p.N + 15) / 16) + 63) / 64;
+        DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^41 elements or more");
+        k_product_none<E><<<(unsigned)blocks, 64, 0, s>>>(e, p.M, p.N, p.batch);
+        DBLP_LAUNCHED();
+        return DBLP_OK;
+    }
     const ProductPlan r = plan_product(p);
-    DBLP_REQUIRE((uint64_t)r.tiles * r.parts * p.batch < 1ull << 31, DBLP_ECAPACITY, "product: 2^31 tiles or more");
+    DBLP_REQUIRE((uint64_t)r.tiles * p.batch + (uint64_t)r.rest * r.parts < 1ull << 31, DBLP_ECAPACITY, "product: 2^31 tiles or more");
     unsigned long long* timeouts = timeout_counter();
     DBLP_REQUIRE(timeouts, DBLP_ECUDA, "product: no device counter: %s", cudaGetErrorString(cudaGetLastError()));
     Operand oa = p.a, ob = p.b;
@@ -530,16 +578,24 @@ template <typename E> int run_product(const Product& p, const E& e, void* ws, bo
         if (int rc = make_map(&a.a[i], i ? oa.lo : oa.p, oa.stride, oa, a.M, p.K, p.batch, 128, p.dtype)) return rc;
         if (int rc = make_map(&a.b[i], i ? ob.lo : ob.p, ob.stride, ob, a.N, p.K, p.batch, r.bn / r.cg, p.dtype)) return rc;
     }
+    a.tm = 128 * r.cg;
     a.bn = r.bn;
     a.mt = r.mt;
     a.nt = r.nt;
     a.steps = r.steps;
-    a.per = r.per;
-    a.parts = r.parts;
-    a.tiles = r.tiles;
-    a.items = r.tiles * r.parts * p.batch;
     a.term_steps = r.term_steps;
+    a.whole = r.whole;
+    a.rest = r.rest;
+    a.parts = r.parts;
+    a.per = r.per;
+    a.items = r.whole + r.rest * r.parts;
     a.group = 8 / r.cg;
+    a.tiles = r.tiles;
+    a.by_tiles = FastDiv(r.tiles);
+    a.by_rest = FastDiv(r.rest ? r.rest : 1);
+    a.by_all = FastDiv(a.group * r.nt);
+    a.by_group = FastDiv(a.group);
+    a.by_last = FastDiv(r.mt % a.group ? r.mt % a.group : a.group);
     a.a_mn = oa.mn;
     a.b_mn = ob.mn;
     a.symmetric = p.symmetric;
@@ -552,11 +608,12 @@ template <typename E> int run_product(const Product& p, const E& e, void* ws, bo
     a.idesc = p.dtype == DBLP_BF16 ? mma_desc<__nv_bfloat16>(128 * r.cg, r.bn, oa.mn, ob.mn) : mma_desc<__half>(128 * r.cg, r.bn, oa.mn, ob.mn);
     a.timeouts = timeouts;
     a.direct = e.sectors();
-    if (r.parts == 1) return launch_product(r.cg, p.runs, a, e, chained, s);
-    const EpiPartial sums{(float*)at, (int64_t)p.M * r.partial_stride, r.partial_stride};
-    a.direct = true;
-    if (int rc = launch_product(r.cg, p.runs, a, sums, chained, s)) return rc;
-    return launch_join(e, sums, r.parts, p, true, s);
+    a.partial = (float*)at;
+    if (int rc = launch_product(r.cg, p.runs, a, e, chained, s)) return rc;
+    if (r.rest == 0) return DBLP_OK;
+    const uint64_t pieces = (uint64_t)r.rest * (a.tm / 32) * ((r.bn + 31) / 32);
+    DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)((pieces + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, s, a, e));
+    return DBLP_OK;
 }
 
 template int run_product(const Product&, const EpiLinear&, void*, bool, cudaStream_t);

@@ -117,9 +117,9 @@ struct FastDiv {
         s1 = l > 1 ? 1 : l;
         s2 = l > 0 ? l - 1 : 0;
     }
-    __device__ __forceinline__ uint32_t div(uint32_t x) const
+    __host__ __device__ __forceinline__ uint32_t div(uint32_t x) const
     {
-        const uint32_t t = __umulhi(m, x);
+        const uint32_t t = (uint32_t)((uint64_t)m * x >> 32);
         return (t + ((x - t) >> s1)) >> s2;
     }
 };
