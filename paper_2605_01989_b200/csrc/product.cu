@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                     const uint32_t dst = dst0 + st * a.stage_bytes, bar = full_to + st * 8;
                     if (is_a && rank == 0) warp_expect(full_at + st * 8, CG * a.stage_bytes);
                     if (++st == a.stages) { st = 0; phase ^= 1; }
-                    ready = bar_try(&empty[st], phase);             // the next stage's, beside this one's loads
+                    ready = bar_test(&empty[st], phase);             // the next stage's, beside this one's loads
                     if (mn)
                         for (uint32_t c = 0; c < boxes; ++c) warp_tma3<CG>(dst + c * 8192, map, bar, at_row + (int)c * 64, (int)at, b);
                     else
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                         tc_fence_after();
                         const uint32_t now = st;
                         if (++st == a.stages) { st = 0; phase ^= 1; }
-                        ready = bar_try(&full[st], phase);          // the next stage's, beside this one's products
+                        ready = bar_test(&full[st], phase);          // the next stage's, beside this one's products
                         mma4_commit<CG>(acc, a0 + uniform(now * stage), b0 + uniform(now * stage), a_step, b_step, a.idesc, run > 0, &empty[now]);
                         if (++run == (RUNS ? kRun : n) || k + 1 == n) {
                             commit_cg<CG>(&acc_full[w & 1]);

@@ -46,6 +46,17 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
     return ok != 0;
 }
 
+// The same without waiting at all: try_wait may sleep for microseconds before it says no.
+__device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok)
+                 : "r"(smem_addr(b)), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+
 // Every wait is bounded: after about two seconds the waiting thread raises the block's flag, which ends all other waits of
 // the block at once; the block then skips its work, lets its copies land, frees its tensor memory and returns.  The results
 // of such a launch are incomplete, and the device's count of timeouts (dblp_wait_timeouts) says so.
