@@ -1,27 +1,11 @@
-// What is done with a matrix product's fp32 sums: sixteen consecutive columns of one row at a time, whole 32-byte sectors of a
-// 16-bit matrix (two accesses of 16 bytes at a stride of 32 touch every sector twice).
+// What is done with a matrix product's fp32 sums: sixteen consecutive columns of one row at a time where all matrices allow 32-byte
+// accesses (whole sectors of a 16-bit matrix; two accesses of 16 bytes at a stride of 32 touch every sector twice), else one
+// element a lane.
 #pragma once
 
 #include "tc.cuh"
 
 namespace dblp {
-
-// A row-major matrix that an epilogue reads or writes.  vec: bytes that an access at a column that is a multiple of sixteen may
-// have, 32 or 16; 0 = element by element.
-struct Rows {
-    void* p;
-    int64_t stride;
-    int dtype, vec;
-    __device__ __forceinline__ explicit operator bool() const { return p != nullptr; }
-};
-inline Rows rows_of(const void* p, int64_t stride, uint64_t rows, int dtype)
-{
-    if (rows <= 1) stride = 0;
-    const uint64_t at = (uintptr_t)p | (uint64_t)stride * element_bytes(dtype);
-    return Rows{(void*)p, stride, dtype, at % 32 == 0 ? 32 : (at % 16 == 0 ? 16 : 0)};
-}
-
-inline bool whole(const Rows& r) { return r.p == nullptr || r.vec == 32; }
 
 __device__ __forceinline__ void load32(const void* p, uint32_t* w)
 {
@@ -36,117 +20,56 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w)
                  "r"(w[6]), "r"(w[7])
                  : "memory");
 }
-// 32 bytes, in one access or two.
-__device__ __forceinline__ void load_words(const void* p, int vec, uint32_t* w)
-{
-    if (vec == 32) {
-        load32(p, w);
-    } else {
-        const uint4 a = ((const uint4*)p)[0], b = ((const uint4*)p)[1];
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-    }
-}
-__device__ __forceinline__ void store_words(void* p, int vec, const uint32_t* w)
-{
-    if (vec == 32) {
-        store32(p, w);
-    } else {
-        ((uint4*)p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        ((uint4*)p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-}
 
-// Sixteen elements on their way: as loaded where whole vectors were (in the first eight words those of a 16-bit type), else as
-// fp32.  What an epilogue reads is fetched before the sums it belongs to are there.
-struct Raw {
-    uint32_t w[16];
+// Sixteen elements as they lie in memory.
+template <typename T> struct Raw {
+    uint32_t w[sizeof(T) * 4];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        load32(p, w);
+        if (sizeof(T) == 4) load32((const char*)p + 32, w + (sizeof(T) == 4 ? 8 : 0));
+    }
+    __device__ __forceinline__ float2 get(int i) const           // elements 2 i and 2 i + 1
+    {
+        if constexpr (sizeof(T) == 4) return pair(w[2 * i], w[2 * i + 1]);
+        else return unpack2<T>(w[i]);
+    }
 };
-__device__ __forceinline__ void fetch16(const Rows& r, uint32_t m, uint32_t n, uint32_t left, Raw& x)
+template <typename T> __device__ __forceinline__ void store16(T* p, const float* x)
 {
-    const int64_t at = (int64_t)m * r.stride + n;
-    if (r.vec && left >= 16) {
-        const char* p = (const char*)r.p + at * (r.dtype == DBLP_F32 ? 4 : 2);
-        load_words(p, r.vec, x.w);
-        if (r.dtype == DBLP_F32) load_words(p + 32, r.vec, x.w + 8);
+    if constexpr (sizeof(T) == 4) {
+        store32(p, reinterpret_cast<const uint32_t*>(x));
+        store32(p + 8, reinterpret_cast<const uint32_t*>(x) + 8);
     } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) {
-            float t = 0.0f;
-            if (i < left)
-                t = r.dtype == DBLP_F32 ? ((const float*)r.p)[at + i]
-                                        : (r.dtype == DBLP_BF16 ? to_f32(((const __nv_bfloat16*)r.p)[at + i]) : to_f32(((const __half*)r.p)[at + i]));
-            x.w[i] = __float_as_uint(t);
-        }
-    }
-}
-template <typename T> __device__ __forceinline__ void widen16(const uint32_t* w, float* x)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 f = unpack2<T>(w[i]);
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
-}
-__device__ __forceinline__ void use16(const Rows& r, uint32_t left, const Raw& x, float* t)
-{
-    if (r.dtype == DBLP_F32 || !r.vec || left < 16) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t[i] = __uint_as_float(x.w[i]);
-    } else if (r.dtype == DBLP_BF16) widen16<__nv_bfloat16>(x.w, t);
-    else widen16<__half>(x.w, t);
-}
-template <typename T> __device__ __forceinline__ void store16(T* p, uint32_t left, int vec, const float* x)
-{
-    if (vec && left >= 16) {
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-        store_words(p, vec, w);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i)
-            if (i < left) p[i] = from_f32<T>(x[i]);
+        store32(p, w);
     }
-}
-template <> __device__ __forceinline__ void store16<float>(float* p, uint32_t left, int vec, const float* x)
-{
-    if (vec && left >= 16) {
-        store_words(p, vec, reinterpret_cast<const uint32_t*>(x));
-        store_words(p + 8, vec, reinterpret_cast<const uint32_t*>(x) + 8);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i)
-            if (i < left) p[i] = x[i];
-    }
-}
-__device__ __forceinline__ void store16(const Rows& r, uint32_t m, uint32_t n, uint32_t left, const float* x)
-{
-    const int64_t at = (int64_t)m * r.stride + n;
-    if (r.dtype == DBLP_F32) store16((float*)r.p + at, left, r.vec, x);
-    else if (r.dtype == DBLP_BF16) store16((__nv_bfloat16*)r.p + at, left, r.vec, x);
-    else store16((__half*)r.p + at, left, r.vec, x);
 }
 
-// Eight elements, for the kernels around the products.
-__device__ __forceinline__ void load8(const Rows& r, uint32_t m, uint32_t n, uint32_t left, float* x)
-{
-    const int64_t at = (int64_t)m * r.stride + n;
-    auto go = [&](auto tag) {
-        using T = decltype(tag);
-        const T* p = (const T*)r.p + at;
-        if (r.vec && left >= 8) {
-            Vec8<T> v;
-            v.load(p);
-            v.get(x);
-        } else {
+// A row-major matrix that an epilogue reads or writes.
+template <typename T> struct Rows {
+    T* p;
+    int64_t stride;
+    __device__ __forceinline__ explicit operator bool() const { return p != nullptr; }
+    __device__ __forceinline__ T* at(uint32_t m, uint32_t n) const { return p + (int64_t)m * stride + n; }
+    __device__ __forceinline__ void add(const Raw<T>& r, float* v) const
+    {
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) x[i] = i < left ? to_f32(p[i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const float2 t = add2(make_float2(v[2 * i], v[2 * i + 1]), r.get(i));
+            v[2 * i] = t.x;
+            v[2 * i + 1] = t.y;
         }
-    };
-    if (r.dtype == DBLP_F32) go(float());
-    else if (r.dtype == DBLP_BF16) go(__nv_bfloat16());
-    else go(__half());
+    }
+    bool whole() const { return p == nullptr || (((uintptr_t)p | (uint64_t)stride * sizeof(T)) % 32 == 0); }
+};
+template <typename T> inline Rows<T> rows_of(const void* p, int64_t stride, uint64_t rows) { return Rows<T>{(T*)p, rows <= 1 ? 0 : stride}; }
+
+__device__ __forceinline__ float element(const void* p, int dtype, uint64_t i)
+{
+    return dtype == DBLP_F32 ? ((const float*)p)[i] : (dtype == DBLP_BF16 ? to_f32(((const __nv_bfloat16*)p)[i]) : to_f32(((const __half*)p)[i]));
 }
 
 // ---- activations -----------------------------------------------------------------------------------------------------
@@ -246,80 +169,108 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 }
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
-// v holds the sums of row m, columns n .. n + 15 (left of them inside the matrix) of product b; what `fetch` loaded for them is in f.
-struct EpiLinear {                        // out = act(z) + residual, pre = z = v + bias
-    Rows out, residual, pre, bias;
-    int act;
-    bool sectors() const { return whole(out) && whole(residual) && whole(pre); }
-    struct Fetched { Raw bias, residual; };
-    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, uint32_t left, Fetched& f) const
+// Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
+// padding behind a row); apply1 one.  What `fetch` loaded is in f.  sectors(): all matrices allow 32-byte accesses.
+template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
+    Rows<O> out, residual;
+    Rows<T> pre;
+    const void* bias;
+    int bias_dtype, act;
+    static constexpr bool kPadded = false;
+    bool sectors() const { return out.whole() && residual.whole() && pre.whole() && (uintptr_t)bias % 32 == 0; }
+    struct Fetched { Raw<O> residual; };
+    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
-        if (bias) fetch16(bias, 0, n, left, f.bias);
-        if (residual) fetch16(residual, m, n, left, f.residual);
+        if (residual) f.residual.load(residual.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, uint32_t left, const Fetched& f, float* v) const
+    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
-        float t[16];
-        if (bias) {
-            use16(bias, left, f.bias, t);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += t[i];
+        if (bias) {                                             // the same sixteen for all lanes
+            if (bias_dtype == DBLP_F32) {
+                Raw<float> r;
+                r.load((const float*)bias + n);
+                Rows<float>().add(r, v);
+            } else if (bias_dtype == DBLP_BF16) {
+                Raw<__nv_bfloat16> r;
+                r.load((const __nv_bfloat16*)bias + n);
+                Rows<__nv_bfloat16>().add(r, v);
+            } else {
+                Raw<__half> r;
+                r.load((const __half*)bias + n);
+                Rows<__half>().add(r, v);
+            }
         }
-        if (pre) store16(pre, m, n, left, v);
+        if (pre) store16(pre.at(m, n), v);
         activate<16>(act, v);
-        if (residual) {
-            use16(residual, left, f.residual, t);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += t[i];
-        }
-        store16(out, m, n, left, v);
+        if (residual) residual.add(f.residual, v);
+        store16(out.at(m, n), v);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    {
+        float v[2] = {bias ? x + element(bias, bias_dtype, n) : x, 0.0f};
+        if (pre) *pre.at(m, n) = from_f32<T>(v[0]);
+        activate<2>(act, v);
+        if (residual) v[0] += to_f32(*residual.at(m, n));
+        *out.at(m, n) = from_f32<O>(v[0]);
     }
 };
 
-struct EpiGradX {                         // dx = (v + residual) act'(pre)
-    Rows out, residual, pre;
+template <typename T> struct EpiGradX {                         // dx = (v + residual) act'(pre)
+    Rows<T> out, residual, pre;
     int act;
-    bool sectors() const { return whole(out) && whole(residual) && whole(pre); }
-    struct Fetched { Raw residual, pre; };
-    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, uint32_t left, Fetched& f) const
+    static constexpr bool kPadded = false;
+    bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
+    struct Fetched { Raw<T> residual, pre; };
+    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
-        if (residual) fetch16(residual, m, n, left, f.residual);
-        if (pre) fetch16(pre, m, n, left, f.pre);
+        if (residual) f.residual.load(residual.at(m, n));
+        if (pre) f.pre.load(pre.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, uint32_t left, const Fetched& f, float* v) const
+    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
-        float t[16];
-        if (residual) {
-            use16(residual, left, f.residual, t);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += t[i];
-        }
+        if (residual) residual.add(f.residual, v);
         if (pre) {
-            use16(pre, left, f.pre, t);
-            activate_grad<16>(act, t, v);
+            float z[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float2 t = f.pre.get(i);
+                z[2 * i] = t.x;
+                z[2 * i + 1] = t.y;
+            }
+            activate_grad<16>(act, z, v);
         }
-        store16(out, m, n, left, v);
+        store16(out.at(m, n), v);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    {
+        float v[2] = {residual ? x + to_f32(*residual.at(m, n)) : x, 0.0f};
+        if (pre) {
+            const float z[2] = {to_f32(*pre.at(m, n)), 0.0f};
+            activate_grad<2>(act, z, v);
+        }
+        *out.at(m, n) = from_f32<T>(v[0]);
     }
 };
 
-struct EpiStore {                         // out = v [+ out]
-    Rows out;
+template <typename O> struct EpiStore {                         // out = v [+ out]
+    Rows<O> out;
     bool accumulate;
-    bool sectors() const { return whole(out); }
-    struct Fetched { Raw out; };
-    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, uint32_t left, Fetched& f) const
+    static constexpr bool kPadded = false;
+    bool sectors() const { return out.whole(); }
+    struct Fetched { Raw<O> out; };
+    __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
-        if (accumulate) fetch16(out, m, n, left, f.out);
+        if (accumulate) f.out.load(out.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, uint32_t left, const Fetched& f, float* v) const
+    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
-        if (accumulate) {
-            float t[16];
-            use16(out, left, f.out, t);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += t[i];
-        }
-        store16(out, m, n, left, v);
+        if (accumulate) out.add(f.out, v);
+        store16(out.at(m, n), v);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    {
+        O* p = out.at(m, n);
+        *p = from_f32<O>(accumulate ? x + to_f32(*p) : x);
     }
 };
 
@@ -329,23 +280,30 @@ struct Words {
     __half *hi, *lo;
     int64_t each;
     uint32_t stride;
-    struct Fetched { uint32_t hi[8], lo[8]; };
+    struct Fetched { Raw<__half> hi, lo; };
     __device__ __forceinline__ int64_t at(uint32_t b, uint32_t m, uint32_t n) const { return b * each + (int64_t)m * stride + n; }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (!hi) return;
-        load32(hi + at(b, m, n), f.hi);
-        if (lo) load32(lo + at(b, m, n), f.lo);
+        f.hi.load(hi + at(b, m, n));
+        if (lo) f.lo.load(lo + at(b, m, n));
     }
-    __device__ __forceinline__ void use(const Fetched& f, float* x) const
+    // v = alpha v + beta (the words)
+    __device__ __forceinline__ void combine(const Fetched& f, float alpha, float beta, float* v) const
     {
-        widen16<__half>(f.hi, x);
-        if (lo) {
-            float t[16];
-            widen16<__half>(f.lo, t);
+        const float2 a = make_float2(alpha, alpha), b = make_float2(beta, beta);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] += t[i];
+        for (int i = 0; i < 8; ++i) {
+            float2 t = mul2(make_float2(v[2 * i], v[2 * i + 1]), a);
+            if (hi) t = fma2(lo ? add2(f.hi.get(i), f.lo.get(i)) : f.hi.get(i), b, t);
+            v[2 * i] = t.x;
+            v[2 * i + 1] = t.y;
         }
+    }
+    __device__ __forceinline__ float value(uint32_t b, uint32_t m, uint32_t n) const
+    {
+        const int64_t i = at(b, m, n);
+        return hi ? to_f32(hi[i]) + (lo ? to_f32(lo[i]) : 0.0f) : 0.0f;
     }
     __device__ __forceinline__ void store(uint32_t b, uint32_t m, uint32_t n, const float* x) const
     {
@@ -364,39 +322,38 @@ struct Words {
     }
 };
 
-struct EpiPoly {                          // out = alpha v [+ beta add], both in words
+struct EpiPoly {                                                // out = alpha v [+ beta add], both in words
     Words out, add;
     float alpha, beta;
+    static constexpr bool kPadded = true;
     bool sectors() const { return true; }
     using Fetched = Words::Fetched;
-    __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, uint32_t, Fetched& f) const { add.fetch(b, m, n, f); }
-    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, uint32_t, const Fetched& f, float* v) const
+    __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
+    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
-        float t[16] = {};
-        if (add.hi) add.use(f, t);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = fmaf(beta, t[i], alpha * v[i]);
+        add.combine(f, alpha, beta, v);
         out.store(b, m, n, v);
     }
 };
 
-struct EpiLast {                          // the caller's out = alpha v + beta add
-    Rows out;
+template <typename O> struct EpiLast {                          // the caller's out = alpha v + beta add
+    Rows<O> out;
     int64_t each;
     Words add;
     float alpha, beta;
-    bool sectors() const { return whole(out); }
+    bool aligned;                                               // of all products of the batch
+    static constexpr bool kPadded = false;
+    bool sectors() const { return aligned; }
     using Fetched = Words::Fetched;
-    __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, uint32_t, Fetched& f) const { add.fetch(b, m, n, f); }
-    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, uint32_t left, const Fetched& f, float* v) const
+    __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
+    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
-        float t[16];
-        add.use(f, t);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = fmaf(beta, t[i], alpha * v[i]);
-        Rows o = out;
-        o.p = (char*)o.p + b * each * (o.dtype == DBLP_F32 ? 4 : 2);
-        store16(o, m, n, left, v);
+        add.combine(f, alpha, beta, v);
+        store16(out.at(m, n) + b * each, v);
+    }
+    __device__ __forceinline__ void apply1(uint32_t b, uint32_t m, uint32_t n, float x) const
+    {
+        out.at(m, n)[b * each] = from_f32<O>(fmaf(beta, add.value(b, m, n), alpha * x));
     }
 };
 

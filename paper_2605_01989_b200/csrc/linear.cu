@@ -11,7 +11,7 @@ namespace dblp {
 constexpr int kSumThreads = 256;
 
 struct SumArgs {
-    Rows dy;
+    Source dy;
     uint32_t rows, cols, slices;
     float* partial;                     // [slices][cols]
     void* out;
@@ -82,7 +82,7 @@ static size_t sum_bytes(const dblp_linear_t* l) { return l->out ? ((size_t)sum_s
 static int column_sums(const dblp_linear_t* l, const dblp_matrix_t* dy, void* dbias, void* ws, cudaStream_t s)
 {
     SumArgs a{};
-    if (l->rows) a.dy = rows_of(dy->data, dy->row_stride, l->rows, l->dtype);
+    if (l->rows) a.dy = source_of(dy->data, dy->row_stride, l->rows, l->dtype);
     a.rows = l->rows;
     a.cols = l->out;
     a.slices = sum_slices(l->rows, l->out);
@@ -166,7 +166,7 @@ static Product product_of(const dblp_linear_t* l, const Operand& a, const Operan
     p.batch = 1;
     p.dtype = l->dtype;
     p.terms = 1;
-    p.runs = l->out_dtype == DBLP_F32;
+    p.few = true;
     return p;
 }
 
@@ -177,9 +177,7 @@ static Product forward_product(const dblp_linear_t* l, const dblp_matrix_t* x, c
 }
 static Product dx_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* w)
 {
-    Product p = product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out);
-    p.runs = false;
-    return p;
+    return product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out);
 }
 static Product dw_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, bool by_rows)
 {
@@ -244,14 +242,22 @@ extern "C" int dblp_linear(const dblp_linear_t* l, const dblp_matrix_t* x, const
     if (pre) DBLP_TRY(check_matrix(who, "pre", pre, l->rows, l->out, l->dtype, false, true));
     DBLP_TRY(check_vector(who, "bias", bias, l->bias_dtype));
     DBLP_TRY(check_space(who, ws, ws_bytes, forward_bytes(l, x, w)));
-    EpiLinear e{};
-    e.out = rows_of(out->data, out->row_stride, l->rows, l->out_dtype);
-    if (residual) e.residual = rows_of(residual->data, residual->row_stride, l->rows, l->out_dtype);
-    if (pre) e.pre = rows_of(pre->data, pre->row_stride, l->rows, l->dtype);
-    if (bias) e.bias = rows_of(bias, 0, 1, l->bias_dtype);
-    e.act = l->activation;
     const dblp_matrix_t none{nullptr, 1, 1};
-    return run_product(l->in ? forward_product(l, x, w) : forward_product(l, &none, &none), e, ws, false, (cudaStream_t)stream);
+    const Product p = l->in ? forward_product(l, x, w) : forward_product(l, &none, &none);
+    auto go = [&](auto t, auto o) -> int {
+        using T = decltype(t);
+        using O = decltype(o);
+        EpiLinear<T, O> e{};
+        e.out = rows_of<O>(out->data, out->row_stride, l->rows);
+        if (residual) e.residual = rows_of<O>(residual->data, residual->row_stride, l->rows);
+        if (pre) e.pre = rows_of<T>(pre->data, pre->row_stride, l->rows);
+        e.bias = bias;
+        e.bias_dtype = l->bias_dtype;
+        e.act = l->activation;
+        return run_product<sizeof(O) == 4>(p, e, ws, false, (cudaStream_t)stream);
+    };
+    if (l->dtype == DBLP_BF16) return l->out_dtype == DBLP_F32 ? go(__nv_bfloat16(), float()) : go(__nv_bfloat16(), __nv_bfloat16());
+    return l->out_dtype == DBLP_F32 ? go(__half(), float()) : go(__half(), __half());
 }
 
 extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, const dblp_matrix_t* w,
@@ -286,19 +292,23 @@ extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy,
 
     // dw before dx: dx may be written over pre or the residual, never over x or dy
     if (want_db) DBLP_TRY(column_sums(l, dy, dbias, ws, s));
-    if (want_dw) {
-        EpiStore e{};
-        e.out = rows_of(dw->data, by_rows ? dw->row_stride : dw->col_stride, by_rows ? l->in : l->out, l->out_dtype);
-        e.accumulate = l->flags & DBLP_ACCUMULATE;
-        DBLP_TRY(run_product(pw, e, ws, false, s));
-    }
-    if (want_dx) {
-        EpiGradX e{};
-        e.out = rows_of(dx->data, dx->row_stride, l->rows, l->dtype);
-        if (residual) e.residual = rows_of(residual->data, residual->row_stride, l->rows, l->dtype);
-        if (pre) e.pre = rows_of(pre->data, pre->row_stride, l->rows, l->dtype);
+    if (want_dw)
+        DBLP_TRY(with_type(l->out_dtype, [&](auto t) -> int {
+            using O = decltype(t);
+            EpiStore<O> e{};
+            e.out = rows_of<O>(dw->data, by_rows ? dw->row_stride : dw->col_stride, by_rows ? l->in : l->out);
+            e.accumulate = l->flags & DBLP_ACCUMULATE;
+            return run_product<sizeof(O) == 4>(pw, e, ws, false, s);
+        }));
+    if (!want_dx) return DBLP_OK;
+    auto go = [&](auto t) -> int {
+        using T = decltype(t);
+        EpiGradX<T> e{};
+        e.out = rows_of<T>(dx->data, dx->row_stride, l->rows);
+        if (residual) e.residual = rows_of<T>(residual->data, residual->row_stride, l->rows);
+        if (pre) e.pre = rows_of<T>(pre->data, pre->row_stride, l->rows);
         e.act = l->activation;
-        DBLP_TRY(run_product(px, e, ws, false, s));
-    }
-    return DBLP_OK;
+        return run_product<false>(px, e, ws, false, s);
+    };
+    return l->dtype == DBLP_BF16 ? go(__nv_bfloat16()) : go(__half());
 }

@@ -18,7 +18,7 @@ constexpr double kScaleX = 1024.0;
 constexpr float kScaleA = 256.0f;
 
 struct UpdIn {
-    Rows x;
+    Source x;
     int64_t each;
     uint32_t rows, cols, parts;
     double* squares;                             // [batch][parts]
@@ -46,8 +46,8 @@ __global__ void __launch_bounds__(kUpdThreads) k_squares(const __grid_constant__
     const uint32_t per_row = (a.cols + 7) / 8, b = blockIdx.y;
     const uint64_t groups = (uint64_t)a.rows * per_row, share = (groups + a.parts - 1) / a.parts;
     const uint64_t g0 = blockIdx.x * share, g1 = min(groups, g0 + share);
-    Rows x = a.x;
-    x.p = (char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
+    Source x = a.x;
+    x.p = (const char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
     double t = 0.0;
     for (uint64_t g = g0 + threadIdx.x; g < g1; g += kUpdThreads) {
         const uint32_t r = (uint32_t)(g / per_row), c = (uint32_t)(g - (uint64_t)r * per_row) * 8;
@@ -70,14 +70,13 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
     const uint64_t groups = (uint64_t)a.rows * per_row;
     const double norm = sqrt(block_sum(threadIdx.x < a.parts ? a.squares[(size_t)b * a.parts + threadIdx.x] : 0.0, part)) + (double)a.eps;
     const double f = norm == 0.0 ? 0.0 : kScaleX / norm;
-    Rows x = a.x;
-    x.p = (char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
+    Source x = a.x;
+    x.p = (const char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
     for (uint64_t g = (uint64_t)blockIdx.x * kUpdThreads + threadIdx.x; g < groups; g += (uint64_t)gridDim.x * kUpdThreads) {
         const uint32_t r = (uint32_t)(g / per_row), c = (uint32_t)(g - (uint64_t)r * per_row) * 16, left = min(16u, a.cols - c);
-        Raw w;
         float v[16];
-        fetch16(x, r, c, left, w);
-        use16(x, left, w, v);
+        load8(x, r, c, min(8u, left), v);
+        load8(x, r, c + 8, left > 8 ? left - 8 : 0, v + 8);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = (float)((double)v[i] * f);
         a.out.store(b, r, c, v);
@@ -119,7 +118,6 @@ static Product gram_product(const dblp_orthogonalize_t* u, const UpdPlan& p, con
     g.batch = u->batch;
     g.dtype = DBLP_F16;
     g.terms = p.precise ? 3 : 1;
-    g.runs = p.precise;
     g.symmetric = true;
     return g;
 }
@@ -175,12 +173,16 @@ static UpdSpace space_of(const dblp_orthogonalize_t* u, const UpdPlan& p, void* 
     return s;
 }
 
-// Rows of the first matrix, with accesses that all of them allow.
-static Rows batched(const void* p, int64_t row_stride, int64_t batch_stride, const dblp_orthogonalize_t* u, int dtype)
+static bool whole(const void* p, int64_t row_stride, int64_t batch_stride, const dblp_orthogonalize_t* u, int dtype, uint32_t bytes)
 {
-    Rows r = rows_of(p, row_stride, u->rows, dtype);
-    while (u->batch > 1 && r.vec && batch_stride * element_bytes(dtype) % r.vec) r.vec = r.vec == 32 ? 16 : 0;
-    return r;
+    const uint64_t es = element_bytes(dtype), rows = u->rows > 1 ? row_stride * es : 0, batches = u->batch > 1 ? batch_stride * es : 0;
+    return ((uintptr_t)p | rows | batches) % bytes == 0;
+}
+
+// The products of bf16 results are of one word, the others of both, their sums in short runs.
+template <typename E> static int product(const UpdPlan& plan, const Product& p, const E& e, void* ws, cudaStream_t s)
+{
+    return plan.precise ? run_product<true>(p, e, ws, true, s) : run_product<false>(p, e, ws, true, s);
 }
 
 static int check_update(const char* who, const dblp_orthogonalize_t* u)
@@ -246,7 +248,8 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     const cudaStream_t s = (cudaStream_t)stream;
 
     UpdIn in{};
-    in.x = batched(x, u->x_row_stride, u->x_batch_stride, u, u->x_dtype);
+    in.x = source_of(x, u->x_row_stride, u->rows, u->x_dtype);
+    in.x.vec = whole(x, u->x_row_stride, u->x_batch_stride, u, u->x_dtype, 16);
     in.each = u->x_batch_stride;
     in.rows = u->rows;
     in.cols = u->cols;
@@ -265,31 +268,35 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
         EpiPoly e{};
         e.out = w.a;
         e.alpha = kScaleA / (float)(kScaleX * kScaleX);
-        DBLP_TRY(run_product(gram_product(u, p, now), e, w.products, true, s));
+        DBLP_TRY(product(p, gram_product(u, p, now), e, w.products, s));
         e.out = w.b;
         e.add = w.a;
         e.alpha = c / kScaleA;
         e.beta = b;
-        DBLP_TRY(run_product(square_product(u, p, w.a), e, w.products, true, s));
+        DBLP_TRY(product(p, square_product(u, p, w.a), e, w.products, s));
         const Product last = step_product(u, p, w.b, now);
         if (i + 1 < u->steps) {
             e.out = next;
             e.add = now;
             e.alpha = 1.0f / kScaleA;
             e.beta = a;
-            DBLP_TRY(run_product(last, e, w.products, true, s));
+            DBLP_TRY(product(p, last, e, w.products, s));
             const Words t = now;
             now = next;
             next = t;
         } else {
-            EpiLast f{};
-            f.out = batched(out, u->out_row_stride, u->out_batch_stride, u, u->out_dtype);
-            f.each = u->out_batch_stride;
-            f.add = now;
-            const float back = u->scale / (float)kScaleX;
-            f.alpha = back / kScaleA;
-            f.beta = back * a;
-            DBLP_TRY(run_product(last, f, w.products, true, s));
+            DBLP_TRY(with_type(u->out_dtype, [&](auto t) -> int {
+                using O = decltype(t);
+                EpiLast<O> f{};
+                f.out = rows_of<O>(out, u->out_row_stride, u->rows);
+                f.each = u->out_batch_stride;
+                f.add = now;
+                const float back = u->scale / (float)kScaleX;
+                f.alpha = back / kScaleA;
+                f.beta = back * a;
+                f.aligned = whole(out, u->out_row_stride, u->out_batch_stride, u, u->out_dtype, 32);
+                return run_product<!std::is_same<O, __nv_bfloat16>::value>(last, f, w.products, true, s);
+            }));
         }
     }
     return DBLP_OK;

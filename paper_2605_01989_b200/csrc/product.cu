@@ -82,64 +82,74 @@ __host__ __device__ __forceinline__ ProdItem prod_item(const ProductArgs& a, uin
     return t;
 }
 
-// 32 x 32 sums, a row a lane, from (r0, c0) on: what the epilogue reads is fetched, then `sums` brings v, then it is applied.  Rows
-// whose matrices allow 32-byte accesses are written from the lane that has them.  The others, and results written by columns, go
-// through 4 KB of shared memory, where the 16-byte chunk c of row r is at place c ^ (r % 8): no bank conflicts in any of the
-// three ways.
+// 32 x 32 sums, a row a lane, from (r0, c0) on.  Whole pieces of matrices that allow 32-byte accesses are written from the lane that has
+// the row; what the epilogue reads is fetched before `sums` brings v.  The others, and results written by columns, go through
+// 4 KB of shared memory, where the 16-byte chunk c of row r is at place c ^ (r % 8): no bank conflicts in any direction.  Edges and
+// unaligned matrices are written an element a lane, a row at a time.
 template <typename E, typename F>
 __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, uint32_t b, uint32_t r0, uint32_t c0, float* v, uint8_t* piece, const F& sums)
 {
     const uint32_t M = a.M, N = a.N, lane = threadIdx.x & 31;
     if (r0 >= M || c0 >= N || (a.symmetric && c0 < r0)) return;
-    const bool mirror = a.turned || (a.symmetric && c0 > r0), plain = !a.turned, direct = plain && a.direct;
-    typename E::Fetched f[2];
-    // lane's part of the piece: direct one row, two groups of columns; through shared memory one group of two rows
-    const uint32_t row = direct ? r0 + lane : r0 + lane / 2, dr = direct ? 0 : 16, col = direct ? c0 : c0 + (lane & 1) * 16, dc = direct ? 16 : 0;
-    auto left = [&](uint32_t i) { return col + i * dc < N ? min(16u, N - col - i * dc) : 0u; };
-    auto live = [&](uint32_t i) { return plain && row + i * dr < M && left(i) > 0; };
-#pragma unroll
-    for (uint32_t i = 0; i < 2; ++i)
-        if (live(i)) e.fetch(b, row + i * dr, col + i * dc, left(i), f[i]);
-    sums();
-    if (!direct || mirror) {
-        __syncwarp();
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            *reinterpret_cast<float4*>(piece + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        __syncwarp();
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
-        if (!live(i)) continue;
-        float y[16];
-        if (direct) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) y[k] = v[16 * i + k];
-        } else {
-            const uint32_t r = lane / 2 + 16 * i;
-#pragma unroll
-            for (uint32_t k = 0; k < 4; ++k) {
-                const float4 q = *reinterpret_cast<const float4*>(piece + r * 128 + ((((lane & 1) * 4 + k) ^ (r & 7)) << 4));
-                y[4 * k] = q.x; y[4 * k + 1] = q.y; y[4 * k + 2] = q.z; y[4 * k + 3] = q.w;
-            }
-        }
-        e.apply(b, row + i * dr, col + i * dc, left(i), f[i], y);
-    }
-    if (mirror && c0 + lane < N) {                              // column `lane` of the piece is part of a row of the transposed result
+    auto value = [&](uint32_t r, uint32_t c) { return *reinterpret_cast<const float*>(piece + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4); };
+    const bool direct = a.direct && !a.turned && (E::kPadded || (r0 + 32 <= M && c0 + 32 <= N)), mirror = E::kPadded && a.symmetric && c0 > r0;
+    if (direct) {
+        typename E::Fetched f[2];
+        const bool in = r0 + lane < M;
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i)
-            if (r0 + 16 * i < M) e.fetch(b, c0 + lane, r0 + 16 * i, min(16u, M - r0 - 16 * i), f[i]);
+            if (in && c0 + 16 * i < N) e.fetch(b, r0 + lane, c0 + 16 * i, f[i]);
+        sums();
+        float y[32];
 #pragma unroll
-        for (uint32_t i = 0; i < 2; ++i) {
-            if (r0 + 16 * i >= M) continue;
-            float y[16];
+        for (int i = 0; i < 32; ++i) y[i] = v[i];
 #pragma unroll
-            for (uint32_t k = 0; k < 16; ++k) {
-                const uint32_t r = 16 * i + k;
-                y[k] = *reinterpret_cast<const float*>(piece + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+        for (uint32_t i = 0; i < 2; ++i)
+            if (in && c0 + 16 * i < N) e.apply(b, r0 + lane, c0 + 16 * i, f[i], y + 16 * i);
+        if (!mirror) return;
+    } else {
+        sums();
+    }
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+        *reinterpret_cast<float4*>(piece + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    __syncwarp();
+    if constexpr (E::kPadded) {                                 // mirror: column `lane` of the piece is part of a row of the transposed result
+        if (c0 + lane < N) {
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                if (r0 + 16 * i >= M) continue;
+                typename E::Fetched f;
+                float y[16];
+                e.fetch(b, c0 + lane, r0 + 16 * i, f);
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) y[k] = value(16 * i + k, lane);
+                e.apply(b, c0 + lane, r0 + 16 * i, f, y);
             }
-            e.apply(b, c0 + lane, r0 + 16 * i, min(16u, M - r0 - 16 * i), f[i], y);
         }
+    } else if (a.turned) {                                      // rows of the result are the piece's columns
+        const uint32_t n = min(32u, N - c0);
+        if (a.direct && r0 + 32 <= M && n > 4) {
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t c = lane / 2 + 16 * i, first = (lane & 1) * 16;
+                if (c >= n) continue;
+                typename E::Fetched f;
+                float y[16];
+                e.fetch(b, c0 + c, r0 + first, f);
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) y[k] = value(first + k, c);
+                e.apply(b, c0 + c, r0 + first, f, y);
+            }
+        } else if (r0 + lane < M)
+#pragma unroll 2
+            for (uint32_t c = 0; c < n; ++c) e.apply1(b, c0 + c, r0 + lane, value(lane, c));
+    } else {
+        const uint32_t n = min(32u, M - r0);
+        if (c0 + lane < N)
+#pragma unroll 2
+            for (uint32_t r = 0; r < n; ++r) e.apply1(b, r0 + r, c0 + lane, value(r, lane));
     }
     __syncwarp();
 }
@@ -356,19 +366,10 @@ template <typename E> __global__ void __launch_bounds__(32 * kJoinWarps) k_produ
 }
 
 // Nothing to sum: the epilogue of zeros.
-template <typename E> __global__ void __launch_bounds__(64) k_product_none(const __grid_constant__ E e, uint32_t M, uint32_t N, uint32_t batch)
+template <typename E> __global__ void __launch_bounds__(256) k_product_none(const __grid_constant__ E e, uint32_t M, uint32_t N)
 {
-    wait_before();
-    after_start();
-    const uint32_t per_row = (N + 15) / 16;
-    const uint64_t x = (uint64_t)blockIdx.x * 64 + threadIdx.x, row = x / per_row;
-    const uint32_t n = (uint32_t)(x - row * per_row) * 16, b = (uint32_t)(row / M), m = (uint32_t)(row - (uint64_t)b * M);
-    if (b >= batch) return;
-    typename E::Fetched f;
-    const uint32_t left = min(16u, N - n);
-    float v[16] = {};
-    e.fetch(b, m, n, left, f);
-    e.apply(b, m, n, left, f, v);
+    const uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x, m = x / N;
+    if (m < M) e.apply1(0, (uint32_t)m, (uint32_t)(x - m * N), 0.0f);
 }
 
 // Rows of any stride and alignment -> rows of `to` elements, a multiple of eight.
@@ -426,7 +427,7 @@ static ProductPlan plan_product(const Product& p)
     r.term_steps = (p.K + kStep - 1) / kStep;
     r.steps = r.term_steps * p.terms;
     // Few rows become the columns of narrow tiles, which read B (weights) once and waste no products on rows that are not there.
-    r.turned = !p.symmetric && p.M <= 128 && p.M < p.N && !p.a.mn;
+    r.turned = p.few && p.M <= 128 && p.M < p.N && !p.a.mn;
     const uint32_t M = r.turned ? p.N : p.M, N = r.turned ? p.M : p.N;
     // The shape and the cut with the shortest estimate, in cycles: `step` is what a stage was measured to take (64 x 8192 x 8192 and the
     // like), by issue for small tiles and by L2 for large ones.  Tiles fill the machine in rounds; those of the last, incomplete
@@ -521,13 +522,6 @@ template <int CG, bool RUNS, typename E> static int launch_product(const Product
     return DBLP_OK;
 }
 
-template <typename E> static int launch_product(int cg, bool runs, const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
-{
-    if constexpr (!std::is_same<E, EpiGradX>::value)            // dx is never fp32
-        if (runs) return cg == 2 ? launch_product<2, true>(a, e, chained, s) : launch_product<1, true>(a, e, chained, s);
-    return cg == 2 ? launch_product<2, false>(a, e, chained, s) : launch_product<1, false>(a, e, chained, s);
-}
-
 static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, uint32_t inner, cudaStream_t s)
 {
     const uint64_t blocks = ((uint64_t)outer * (stride / 8) + 255) / 256;
@@ -537,12 +531,12 @@ static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, u
     return DBLP_OK;
 }
 
-template <typename E> int run_product(const Product& p, const E& e, void* ws, bool chained, cudaStream_t s)
+template <bool RUNS, typename E> int run_product(const Product& p, const E& e, void* ws, bool chained, cudaStream_t s)
 {
-    if (p.K == 0) {
-        const uint64_t blocks = ((uint64_t)p.batch * p.M * ((p.N + 15) / 16) + 63) / 64;
-        DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^41 elements or more");
-        k_product_none<E><<<(unsigned)blocks, 64, 0, s>>>(e, p.M, p.N, p.batch);
+    if constexpr (!E::kPadded) if (p.K == 0) {
+        const uint64_t blocks = ((uint64_t)p.M * p.N + 255) / 256;
+        DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^39 elements or more");
+        k_product_none<E><<<(unsigned)blocks, 256, 0, s>>>(e, p.M, p.N);
         DBLP_LAUNCHED();
         return DBLP_OK;
     }
@@ -609,17 +603,27 @@ template <typename E> int run_product(const Product& p, const E& e, void* ws, bo
     a.timeouts = timeouts;
     a.direct = e.sectors();
     a.partial = (float*)at;
-    if (int rc = launch_product(r.cg, p.runs, a, e, chained, s)) return rc;
+    if (int rc = r.cg == 2 ? launch_product<2, RUNS>(a, e, chained, s) : launch_product<1, RUNS>(a, e, chained, s)) return rc;
     if (r.rest == 0) return DBLP_OK;
     const uint64_t pieces = (uint64_t)r.rest * (a.tm / 32) * ((r.bn + 31) / 32);
     DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)((pieces + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, s, a, e));
     return DBLP_OK;
 }
 
-template int run_product(const Product&, const EpiLinear&, void*, bool, cudaStream_t);
-template int run_product(const Product&, const EpiGradX&, void*, bool, cudaStream_t);
-template int run_product(const Product&, const EpiStore&, void*, bool, cudaStream_t);
-template int run_product(const Product&, const EpiPoly&, void*, bool, cudaStream_t);
-template int run_product(const Product&, const EpiLast&, void*, bool, cudaStream_t);
+#define DBLP_PRODUCT(RUNS, ...) template int run_product<RUNS>(const Product&, const __VA_ARGS__&, void*, bool, cudaStream_t)
+DBLP_PRODUCT(false, EpiLinear<__nv_bfloat16, __nv_bfloat16>);
+DBLP_PRODUCT(false, EpiLinear<__half, __half>);
+DBLP_PRODUCT(true, EpiLinear<__nv_bfloat16, float>);
+DBLP_PRODUCT(true, EpiLinear<__half, float>);
+DBLP_PRODUCT(false, EpiGradX<__nv_bfloat16>);
+DBLP_PRODUCT(false, EpiGradX<__half>);
+DBLP_PRODUCT(false, EpiStore<__nv_bfloat16>);
+DBLP_PRODUCT(false, EpiStore<__half>);
+DBLP_PRODUCT(true, EpiStore<float>);
+DBLP_PRODUCT(false, EpiPoly);
+DBLP_PRODUCT(true, EpiPoly);
+DBLP_PRODUCT(false, EpiLast<__nv_bfloat16>);
+DBLP_PRODUCT(true, EpiLast<__half>);
+DBLP_PRODUCT(true, EpiLast<float>);
 
 }  // namespace dblp
