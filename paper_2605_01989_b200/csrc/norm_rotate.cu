@@ -1,18 +1,20 @@
 // dblp_norm_rotate, dblp_norm_rotate_grad: root-mean-square norm of every head of q and k, and the rotation by position.
 //
-// A head's row of D elements belongs to L = D / 8 lanes (rounded up to a power of two), eight elements each: the norm is a
-// shuffle reduction, the other half of a rotated pair is in the same lane (interleaved) or comes from lane +- R / 16.
-// Cosines and sines of a block's tokens are computed once per block into shared memory: the angle, pos * freq / 2 pi, in
-// 64 bits, less its nearest integer, then one fp32 sincospi.
+// A lane holds sixteen elements of a head's row as two groups of eight, chosen so that both members of a rotated pair are its own:
+// columns u .. u + 7 and R / 2 + u .. (interleaved, and behind the rotated part: sixteen in a row).  L lanes, a power of two, make
+// a row; the norm is a shuffle reduction, the rotation needs none.  (One group a lane, the other member by shuffles: 39 us for
+// 8 x 1024 tokens, 25 + 25 heads of 64, bf16, bound by instructions.)
+// Cosines and sines of a step's tokens are computed once per block into shared memory: the angle, pos * freq / 2 pi, in 64 bits,
+// less its nearest integer, then one fp32 sincospi.
 // The backward pass recomputes r from x instead of reading a stored one: x is needed anyway.
 #include <math.h>
 
-#include "types.cuh"
+#include "tc.cuh"
 
 namespace dblp {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotRows = 4;                      // rows in flight per lane group
+constexpr int kRotRows = 2;                      // rows in flight per lane group
 
 struct RotHeads {
     const void* p;
@@ -39,31 +41,21 @@ struct RotArgs {
     const double* freqs;
 };
 
-template <typename T> __device__ __forceinline__ Vec8<T> shuffle8(const Vec8<T>& v, uint32_t from)
+// Columns of a lane's two groups: a .. a + 7 and b .. b + 7; from D on a group is empty.
+struct RotPlace {
+    uint32_t a, b;
+    bool turns;                                  // part of the rotated columns (interleaved: a may be, b need not)
+};
+template <bool INTER> __device__ __forceinline__ RotPlace place_of(uint32_t unit, uint32_t R)
 {
-    constexpr int W = sizeof(Vec8<T>) / 4;
-    Vec8<T> r;
-    const uint32_t* a = reinterpret_cast<const uint32_t*>(&v);
-    uint32_t* b = reinterpret_cast<uint32_t*>(&r);
-#pragma unroll
-    for (int i = 0; i < W; ++i) b[i] = __shfl_sync(0xFFFFFFFFu, a[i], from);
-    return r;
+    if (INTER) return {unit * 16, unit * 16 + 8, unit * 16 < R};
+    const uint32_t turning = R / 16;
+    if (unit < turning) return {unit * 8, R / 2 + unit * 8, true};
+    return {R + (unit - turning) * 16, R + (unit - turning) * 16 + 8, false};
 }
 
-__device__ __forceinline__ void load_weight(const void* w, uint32_t dtype, uint32_t c, uint32_t D, float* out)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float v = 1.0f;
-        if (w && c + i < D)
-            v = dtype == DBLP_F32 ? ((const float*)w)[c + i]
-                                  : (dtype == DBLP_BF16 ? to_f32(((const __nv_bfloat16*)w)[c + i]) : to_f32(((const __half*)w)[c + i]));
-        out[i] = v;
-    }
-}
-
-// (cos, sin) of the angles of tokens first .. first + n - 1 (of batch * tokens in all), R / 2 each.
-__device__ __forceinline__ void fill_angles(const RotArgs& a, float2* table, uint32_t first, uint32_t n)
+// (cos, sin) of the angles of tokens first .. first + n - 1 (of batch * tokens in all): R / 2 cosines, then R / 2 sines a token.
+__device__ __forceinline__ void fill_angles(const RotArgs& a, float* table, uint32_t first, uint32_t n)
 {
     const uint32_t half = a.R / 2;
     for (uint32_t i = threadIdx.x; i < n * half; i += kRotThreads) {
@@ -71,33 +63,36 @@ __device__ __forceinline__ void fill_angles(const RotArgs& a, float2* table, uin
         const double turns = (double)a.positions[(int64_t)b * a.position_stride + (t - b * a.tokens)] * a.freqs[f] * 0.15915494309189533577;
         float s, c;
         sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        table[i] = make_float2(c, s);
+        table[j * a.R + f] = c;
+        table[j * a.R + half + f] = s;
     }
 }
 
-// Columns c .. c + 7 of a row turned: mine holds them, other the other members of their pairs (not used when interleaved);
-// dir = 1 forward, -1 back.
-template <bool INTER>
-__device__ __forceinline__ void turn(float* mine, const float* other, const float2* angles, uint32_t c, uint32_t R, float dir)
+__device__ __forceinline__ float2 neg2(float2 x) { return make_float2(-x.x, -x.y); }
+
+// A lane's sixteen values (a in the first four pairs, b in the last) turned by +t, BACK by -t; angles of its token.
+template <bool INTER, bool BACK> __device__ __forceinline__ void turn(float2* v, const float* angles, const RotPlace& p, uint32_t R)
 {
+    const uint32_t half = R / 2;
     if (INTER) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (c + 2 * i >= R) break;
-            const float2 cs = angles[c / 2 + i];
-            const float x = mine[2 * i], y = mine[2 * i + 1], s = dir * cs.y;
-            mine[2 * i] = x * cs.x - y * s;
-            mine[2 * i + 1] = x * s + y * cs.x;
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t at = p.a / 2 + i;
+            if (at >= half) break;
+            const float c = angles[at], s = BACK ? -angles[half + at] : angles[half + at];
+            v[i] = make_float2(v[i].x * c - v[i].y * s, v[i].x * s + v[i].y * c);
         }
-    } else if (c < R) {
-        const uint32_t half = R / 2;
-        const float s = c < half ? -dir : dir;
-        const float4* at = reinterpret_cast<const float4*>(angles + (c < half ? c : c - half));
+    } else if (p.turns) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 v = at[i];
-            mine[2 * i] = mine[2 * i] * v.x + other[2 * i] * (s * v.y);
-            mine[2 * i + 1] = mine[2 * i + 1] * v.z + other[2 * i + 1] * (s * v.w);
+        for (int q = 0; q < 2; ++q) {
+            const float4 c = *reinterpret_cast<const float4*>(angles + p.a + 4 * q), s = *reinterpret_cast<const float4*>(angles + half + p.a + 4 * q);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float2 cc = h ? make_float2(c.z, c.w) : make_float2(c.x, c.y), ss = h ? make_float2(s.z, s.w) : make_float2(s.x, s.y);
+                const float2 x = v[2 * q + h], y = v[4 + 2 * q + h], up = BACK ? neg2(ss) : ss;
+                v[2 * q + h] = fma2(y, neg2(up), mul2(x, cc));
+                v[4 + 2 * q + h] = fma2(x, up, mul2(y, cc));
+            }
         }
     }
 }
@@ -117,140 +112,141 @@ __device__ __forceinline__ RotRow row_of(const RotArgs& a, const RotSide& s, uin
     r.t = r.token - r.b * a.tokens;
     return r;
 }
-__device__ __forceinline__ int64_t place(const RotHeads& h, const RotRow& r) { return (int64_t)r.b * h.sb + (int64_t)r.t * h.st + (int64_t)r.h * h.sh; }
+__device__ __forceinline__ int64_t offset(const RotHeads& h, const RotRow& r) { return (int64_t)r.b * h.sb + (int64_t)r.t * h.st + (int64_t)r.h * h.sh; }
 
-// Forward: a block takes kRotRows * kRotThreads / L rows of one side, once.
-template <typename T, bool INTER> __global__ void __launch_bounds__(kRotThreads) k_norm_rotate(const __grid_constant__ RotArgs a)
-{
-    extern __shared__ float2 table[];
-    const bool second = blockIdx.x >= a.side[0].blocks;
-    const RotSide& s = a.side[second];
-    const uint32_t block = blockIdx.x - (second ? a.side[0].blocks : 0), L = a.L, per = kRotThreads / L;
-    const uint32_t lane = threadIdx.x & 31, sub = threadIdx.x & (L - 1), c = sub * 8, group = threadIdx.x / L;
-    const uint32_t r0 = block * per * kRotRows;
-    const bool has = c < a.D;
-
-    Vec8<T> x[kRotRows];
-    RotRow row[kRotRows];
-#pragma unroll
-    for (int u = 0; u < kRotRows; ++u) {
-        row[u] = row_of(a, s, r0 + u * per + group);
-        row[u].live = row[u].live && has;
-        if (row[u].live) x[u].load((const T*)s.x.p + place(s.x, row[u]) + c);
-        else {
-            const float zero[8] = {};
-            x[u].set(zero);
+// A lane's part of a row; zeros where there is none.
+template <typename T> struct RotData {
+    Vec8<T> a, b;
+    __device__ __forceinline__ void load(const T* p, const RotPlace& at, bool has_a, bool has_b)
+    {
+        const float zero[8] = {};
+        if (has_a) a.load(p + at.a);
+        else a.set(zero);
+        if (has_b) b.load(p + at.b);
+        else b.set(zero);
+    }
+    __device__ __forceinline__ void get(float2* v) const
+    {
+        a.get(reinterpret_cast<float*>(v));
+        b.get(reinterpret_cast<float*>(v + 4));
+    }
+    __device__ __forceinline__ static void put(T* p, const RotPlace& at, bool has_a, bool has_b, const float2* v)
+    {
+        Vec8<T> w;
+        if (has_a) {
+            w.set(reinterpret_cast<const float*>(v));
+            w.store(p + at.a);
+        }
+        if (has_b) {
+            w.set(reinterpret_cast<const float*>(v + 4));
+            w.store(p + at.b);
         }
     }
-    const uint32_t first = s.by_heads.div(r0), last = s.by_heads.div(min(r0 + per * kRotRows, s.rows) - 1);
-    if (a.R) fill_angles(a, table, first, last - first + 1);
-    const uint32_t half = a.R / 2, from = c < half ? lane + a.R / 16 : (c < a.R ? lane - a.R / 16 : lane);
-    float w[8], wo[8];
-    load_weight(s.weight, a.weight_dtype, c, a.D, w);
-    if (!INTER) load_weight(s.weight, a.weight_dtype, c < half ? c + half : (c < a.R ? c - half : c), a.D, wo);
-    __syncthreads();
+};
+
+__device__ __forceinline__ void load_weight(const RotArgs& a, const void* w, const RotPlace& at, float2* out)
+{
 #pragma unroll
-    for (int u = 0; u < kRotRows; ++u) {
-        float v[8], o[8], ss = 0.0f;
-        x[u].get(v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss += v[i] * v[i];
-        for (uint32_t m = L / 2; m; m >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-        const float r = rsqrtf(ss * a.inv_d + a.eps);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= r * w[i];
-        if (!INTER && a.R) {
-            shuffle8<T>(x[u], from).get(o);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] *= r * wo[i];
-        }
-        if (row[u].live) {
-            if (a.R) turn<INTER>(v, o, table + (row[u].token - first) * half, c, a.R, 1.0f);
-            Vec8<T> y;
-            y.set(v);
-            y.store((T*)s.y.p + place(s.y, row[u]) + c);
-        }
+    for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t c = i < 8 ? at.a + i : at.b + i - 8;
+        float v = 1.0f;
+        if (w && c < a.D)
+            v = a.weight_dtype == DBLP_F32 ? ((const float*)w)[c]
+                                           : (a.weight_dtype == DBLP_BF16 ? to_f32(((const __nv_bfloat16*)w)[c]) : to_f32(((const __half*)w)[c]));
+        if (i & 1) out[i / 2].y = v;
+        else out[i / 2].x = v;
     }
 }
 
-// Backward: a block walks over rows of one side, a stride of the side's blocks apart, and keeps its share of the weight's
-// gradient in registers; one barrier a step, since the angles of two steps alternate between two tables.
-template <typename T, bool INTER> __global__ void __launch_bounds__(kRotThreads) k_norm_rotate_grad(const __grid_constant__ RotArgs a)
+// A block walks over rows of one side, a stride of the side's blocks apart.  The rows of the next step are on their way while this
+// step's are worked on; one barrier a step, since the angles of two steps alternate between two tables.  GRAD keeps the block's
+// share of the weight's gradient in registers.
+template <typename T, bool INTER, bool GRAD> __global__ void __launch_bounds__(kRotThreads, GRAD ? 2 : 3) k_norm_rotate(const __grid_constant__ RotArgs a)
 {
-    extern __shared__ float2 tables[];
-    after_start();
+    constexpr int U = GRAD ? 1 : kRotRows;
+    extern __shared__ __align__(16) float tables[];
+    if (GRAD) after_start();
     const bool second = blockIdx.x >= a.side[0].blocks;
     const RotSide& s = a.side[second];
-    const uint32_t block = blockIdx.x - (second ? a.side[0].blocks : 0), L = a.L, per = kRotThreads / L;
-    const uint32_t lane = threadIdx.x & 31, sub = threadIdx.x & (L - 1), c = sub * 8, group = threadIdx.x / L;
-    const uint32_t half = a.R / 2, from = c < half ? lane + a.R / 16 : (c < a.R ? lane - a.R / 16 : lane);
-    const bool has = c < a.D;
-    float w[8], dw[8] = {};
-    load_weight(s.weight, a.weight_dtype, c, a.D, w);
-
-    constexpr int U = kRotRows / 2;
-    uint32_t step = 0;
-    for (uint64_t r0 = (uint64_t)block * per * U; r0 < s.rows; r0 += (uint64_t)s.blocks * per * U, ++step) {
-        Vec8<T> x[U], g[U];
-        RotRow row[U];
+    const uint32_t block = blockIdx.x - (second ? a.side[0].blocks : 0), L = a.L, per = kRotThreads / L, group = threadIdx.x / L;
+    const RotPlace at = place_of<INTER>(threadIdx.x & (L - 1), a.R);
+    const bool has_a = at.a < a.D, has_b = at.b < a.D;
+    RotData<T> x[U], g[U];
+    auto bring = [&](uint64_t r0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            row[u] = row_of(a, s, (uint32_t)r0 + u * per + group);
-            row[u].live = row[u].live && has;
-            if (row[u].live) {
-                x[u].load((const T*)s.x.p + place(s.x, row[u]) + c);
-                g[u].load((const T*)s.d.p + place(s.d, row[u]) + c);
-            } else {
-                const float zero[8] = {};
-                x[u].set(zero);
-                g[u].set(zero);
-            }
+            const RotRow row = row_of(a, s, r0 < s.rows ? (uint32_t)r0 + u * per + group : s.rows);
+            x[u].load((const T*)s.x.p + offset(s.x, row), at, row.live && has_a, row.live && has_b);
+            if (GRAD) g[u].load((const T*)s.d.p + offset(s.d, row), at, row.live && has_a, row.live && has_b);
         }
-        float2* table = tables + (step & 1) * a.table_tokens * half;
+    };
+    const uint64_t stride = (uint64_t)s.blocks * per * U;
+    bring((uint64_t)block * per * U);
+    float2 w[8], dw[8] = {};
+    load_weight(a, s.weight, at, w);
+    uint32_t step = 0;
+    for (uint64_t r0 = (uint64_t)block * per * U; r0 < s.rows; r0 += stride, ++step) {
+        float* table = tables + (step & 1) * a.table_tokens * a.R;
         const uint32_t first = s.by_heads.div((uint32_t)r0), last = s.by_heads.div(min((uint32_t)r0 + per * U, s.rows) - 1);
-        if (a.R) fill_angles(a, table, first, last - first + 1);
-        __syncthreads();
+        if (a.R) {
+            fill_angles(a, table, first, last - first + 1);
+            __syncthreads();
+        }
+        float2 vs[U][8], ds[U][8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float v[8], d[8], o[8], ss = 0.0f, dot = 0.0f;
-            x[u].get(v);
-            g[u].get(d);
-            if (!INTER && a.R) shuffle8<T>(g[u], from).get(o);
-            if (row[u].live && a.R) turn<INTER>(d, o, table + (row[u].token - first) * half, c, a.R, -1.0f);
+            x[u].get(vs[u]);
+            if (GRAD) g[u].get(ds[u]);
+        }
+        bring(r0 + stride);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                ss += v[i] * v[i];
-                dot += w[i] * d[i] * v[i];
+        for (int u = 0; u < U; ++u) {
+            const RotRow row = row_of(a, s, (uint32_t)r0 + u * per + group);
+            const float* angles = table + (row.live ? row.token - first : 0) * a.R;
+            float2 *v = vs[u], *d = ds[u], sum = make_float2(0.0f, 0.0f), along = sum;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fma2(v[i], v[i], sum);
+            if (GRAD) {
+                if (a.R) turn<INTER, true>(d, angles, at, a.R);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) along = fma2(mul2(w[i], d[i]), v[i], along);
             }
+            float ss = sum.x + sum.y, dot = along.x + along.y;
             for (uint32_t m = L / 2; m; m >>= 1) {
                 ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-                dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+                if (GRAD) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
             }
-            const float r = rsqrtf(ss * a.inv_d + a.eps), q = dot * a.inv_d * r * r * r;
-            if (row[u].live) {
-                float y[8];
+            const float r = rsqrtf(ss * a.inv_d + a.eps);
+            const float2 rr = make_float2(r, r);
+            if (GRAD) {
+                const float q = -dot * a.inv_d * r * r * r;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    dw[i] += d[i] * v[i] * r;
-                    y[i] = r * w[i] * d[i] - v[i] * q;
+                    if (row.live) dw[i] = fma2(mul2(d[i], v[i]), rr, dw[i]);
+                    v[i] = fma2(v[i], make_float2(q, q), mul2(mul2(w[i], d[i]), rr));
                 }
-                Vec8<T> out;
-                out.set(y);
-                out.store((T*)s.y.p + place(s.y, row[u]) + c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], mul2(w[i], rr));
+                if (a.R) turn<INTER, false>(v, angles, at, a.R);
             }
+            RotData<T>::put((T*)s.y.p + offset(s.y, row), at, row.live && has_a, row.live && has_b, v);
         }
     }
-    if (!s.partial) return;
-    // the block's sum of its lane groups, in their order
+    if (!GRAD || !s.partial) return;
+    // the block's sum of its lane groups, in their order: a row of sixteen places a unit
     __syncthreads();
-    float* sum = reinterpret_cast<float*>(tables);                      // kRotThreads * 8 floats
+    float* sum = tables;                                                // kRotThreads * 16 floats
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[(group * L + sub) * 8 + i] = dw[i];
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<float2*>(sum + threadIdx.x * 16 + 2 * i) = dw[i];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < a.D; i += kRotThreads) {
+    for (uint32_t i = threadIdx.x; i < L * 16; i += kRotThreads) {
+        const RotPlace p = place_of<INTER>(i / 16, a.R);
+        const uint32_t c = (i & 8) ? p.b + (i & 7) : p.a + (i & 7);
+        if (c >= a.D) continue;
         float t = 0.0f;
-        for (uint32_t k = 0; k < per; ++k) t += sum[k * L * 8 + i];
-        s.partial[(size_t)block * a.D + i] = t;
+        for (uint32_t k = 0; k < per; ++k) t += sum[k * L * 16 + i];
+        s.partial[(size_t)block * a.D + c] = t;
     }
 }
 
@@ -344,24 +340,23 @@ static int check_side(const char* who, const char* name, const dblp_norm_rotate_
 static uint32_t lanes_of(uint32_t head_dim)
 {
     uint32_t l = 1;
-    while (l * 8 < head_dim) l *= 2;
+    while (l * 16 < head_dim) l *= 2;
     return l;
 }
 
-// Blocks that walk over the rows of one side in the backward pass: at most 4 a multiprocessor for both sides together, by
-// their share of the rows.
-static uint32_t grad_blocks(const dblp_norm_rotate_t* a, uint32_t heads)
+// Blocks that walk over the rows of one side: as many as the device holds for both sides together, by their share of the rows.
+static uint32_t blocks_of(const dblp_norm_rotate_t* a, uint32_t heads, bool grad)
 {
-    const uint64_t rows = (uint64_t)a->batch * a->tokens * heads, per = kRotThreads / lanes_of(a->head_dim) * (kRotRows / 2);
+    const uint64_t rows = (uint64_t)a->batch * a->tokens * heads, per = kRotThreads / lanes_of(a->head_dim) * (grad ? 1 : kRotRows);
     const uint64_t steps = (rows + per - 1) / per, all = a->q_heads + (uint64_t)a->k_heads;
-    uint64_t share = all ? (4ull * kSms * heads + all - 1) / all : 1;
+    uint64_t share = all ? (grad ? 2 : 3) * (uint64_t)kSms * heads / all : 1;
     if (share < 1) share = 1;
     return (uint32_t)(steps < share ? steps : share);
 }
 
 static size_t partial_bytes(const dblp_norm_rotate_t* a, uint32_t heads)
 {
-    return ((size_t)grad_blocks(a, heads) * a->head_dim * 4 + 255) & ~(size_t)255;
+    return ((size_t)blocks_of(a, heads, true) * a->head_dim * 4 + 255) & ~(size_t)255;
 }
 
 static RotHeads rot_heads(const dblp_heads_t* h) { return RotHeads{h->data, h->batch_stride, h->token_stride, h->head_stride}; }
@@ -395,6 +390,16 @@ static RotSide rot_side(const dblp_norm_rotate_t* a, const dblp_heads_t* x, cons
         s.weight = weight;
     }
     return s;
+}
+
+// Two tables of angles take up to 64 KB (a single head of a full rotation), 10 KB with 25 heads of 64.
+template <typename T, bool INTER, bool GRAD> static int launch_rotate(const RotArgs& r, size_t smem, cudaStream_t s)
+{
+    constexpr auto kernel = k_norm_rotate<T, INTER, GRAD>;
+    DBLP_CUDA(allow_shared<kernel>(65536));
+    kernel<<<r.side[0].blocks + r.side[1].blocks, kRotThreads, smem, s>>>(r);
+    DBLP_LAUNCHED();
+    return DBLP_OK;
 }
 
 // Tokens that `rows` consecutive rows of a side can touch.
@@ -437,16 +442,14 @@ extern "C" int dblp_norm_rotate(const dblp_norm_rotate_t* a, const dblp_heads_t*
     r.side[1] = rot_side(a, k, k_weight, k_out, a->k_heads);
     const uint32_t per = kRotThreads / r.L * kRotRows;
     for (RotSide& s : r.side) {
-        s.blocks = (s.rows + per - 1) / per;
+        s.blocks = s.rows ? blocks_of(a, s.heads, false) : 0;
         r.table_tokens = max(r.table_tokens, tokens_of(per, s.heads));
     }
-    const size_t smem = (size_t)r.table_tokens * (r.R / 2) * sizeof(float2);
+    const size_t smem = (size_t)r.table_tokens * r.R * 2 * sizeof(float);
     return with_type(a->dtype, [&](auto tag) -> int {
         using T = decltype(tag);
-        const auto kernel = a->flags & DBLP_ROTATE_INTERLEAVED ? k_norm_rotate<T, true> : k_norm_rotate<T, false>;
-        kernel<<<r.side[0].blocks + r.side[1].blocks, kRotThreads, smem, (cudaStream_t)stream>>>(r);
-        DBLP_LAUNCHED();
-        return DBLP_OK;
+        return a->flags & DBLP_ROTATE_INTERLEAVED ? launch_rotate<T, true, false>(r, smem, (cudaStream_t)stream)
+                                                  : launch_rotate<T, false, false>(r, smem, (cudaStream_t)stream);
     });
 }
 
@@ -499,20 +502,18 @@ extern "C" int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_hea
         r.side[1] = rot_side(a, k, k_weight, dk, a->k_heads);
         if (a->q_heads) r.side[0].d = rot_heads(dq_out);
         if (a->k_heads) r.side[1].d = rot_heads(dk_out);
-        const uint32_t per = kRotThreads / r.L * (kRotRows / 2);
+        const uint32_t per = kRotThreads / r.L;
         for (int i = 0; i < 2; ++i) {
             RotSide& s = r.side[i];
-            s.blocks = s.rows ? grad_blocks(a, s.heads) : 0;
+            s.blocks = s.rows ? blocks_of(a, s.heads, true) : 0;
             s.partial = (i ? dk_weight : dq_weight) ? partial[i] : nullptr;
             r.table_tokens = max(r.table_tokens, tokens_of(per, s.heads));
         }
-        const size_t smem = max((size_t)r.table_tokens * r.R * sizeof(float2), (size_t)kRotThreads * 8 * 4);
+        const size_t smem = max((size_t)r.table_tokens * r.R * 2 * sizeof(float), (size_t)kRotThreads * 16 * sizeof(float));
         DBLP_TRY(with_type(a->dtype, [&](auto tag) -> int {
             using T = decltype(tag);
-            const auto kernel = a->flags & DBLP_ROTATE_INTERLEAVED ? k_norm_rotate_grad<T, true> : k_norm_rotate_grad<T, false>;
-            kernel<<<r.side[0].blocks + r.side[1].blocks, kRotThreads, smem, (cudaStream_t)stream>>>(r);
-            DBLP_LAUNCHED();
-            return DBLP_OK;
+            return a->flags & DBLP_ROTATE_INTERLEAVED ? launch_rotate<T, true, true>(r, smem, (cudaStream_t)stream)
+                                                      : launch_rotate<T, false, true>(r, smem, (cudaStream_t)stream);
         }));
     }
     if (!join) return DBLP_OK;
