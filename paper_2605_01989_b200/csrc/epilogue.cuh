@@ -170,7 +170,7 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
-// padding behind a row); apply1 one.  What `fetch` loaded is in f.  sectors(): all matrices allow 32-byte accesses.
+// padding behind a row); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
@@ -205,13 +205,16 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
         if (residual) residual.add(f.residual, v);
         store16(out.at(m, n), v);
     }
-    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
-        float v[2] = {bias ? x + element(bias, bias_dtype, n) : x, 0.0f};
+        return make_float2(bias ? element(bias, bias_dtype, n) : 0.0f, residual ? to_f32(*residual.at(m, n)) : 0.0f);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float2 f, float x) const
+    {
+        float v[2] = {bias ? x + f.x : x, 0.0f};
         if (pre) *pre.at(m, n) = from_f32<T>(v[0]);
         activate<2>(act, v);
-        if (residual) v[0] += to_f32(*residual.at(m, n));
-        *out.at(m, n) = from_f32<O>(v[0]);
+        *out.at(m, n) = from_f32<O>(residual ? v[0] + f.y : v[0]);
     }
 };
 
@@ -241,11 +244,15 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
         }
         store16(out.at(m, n), v);
     }
-    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
-        float v[2] = {residual ? x + to_f32(*residual.at(m, n)) : x, 0.0f};
+        return make_float2(residual ? to_f32(*residual.at(m, n)) : 0.0f, pre ? to_f32(*pre.at(m, n)) : 0.0f);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float2 f, float x) const
+    {
+        float v[2] = {residual ? x + f.x : x, 0.0f};
         if (pre) {
-            const float z[2] = {to_f32(*pre.at(m, n)), 0.0f};
+            const float z[2] = {f.y, 0.0f};
             activate_grad<2>(act, z, v);
         }
         *out.at(m, n) = from_f32<T>(v[0]);
@@ -267,10 +274,13 @@ template <typename O> struct EpiStore {                         // out = v [+ ou
         if (accumulate) out.add(f.out, v);
         store16(out.at(m, n), v);
     }
-    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float x) const
+    __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
-        O* p = out.at(m, n);
-        *p = from_f32<O>(accumulate ? x + to_f32(*p) : x);
+        return make_float2(accumulate ? to_f32(*out.at(m, n)) : 0.0f, 0.0f);
+    }
+    __device__ __forceinline__ void apply1(uint32_t, uint32_t m, uint32_t n, float2 f, float x) const
+    {
+        *out.at(m, n) = from_f32<O>(accumulate ? x + f.x : x);
     }
 };
 
@@ -351,9 +361,10 @@ template <typename O> struct EpiLast {                          // the caller's 
         add.combine(f, alpha, beta, v);
         store16(out.at(m, n) + b * each, v);
     }
-    __device__ __forceinline__ void apply1(uint32_t b, uint32_t m, uint32_t n, float x) const
+    __device__ __forceinline__ float2 fetch1(uint32_t b, uint32_t m, uint32_t n) const { return make_float2(add.value(b, m, n), 0.0f); }
+    __device__ __forceinline__ void apply1(uint32_t b, uint32_t m, uint32_t n, float2 f, float x) const
     {
-        out.at(m, n)[b * each] = from_f32<O>(fmaf(beta, add.value(b, m, n), alpha * x));
+        out.at(m, n)[b * each] = from_f32<O>(fmaf(beta, f.x, alpha * x));
     }
 };
 

@@ -21,7 +21,7 @@ constexpr int kProdThreads = 384, kProdWriters = 8;             // warps 0 .. 7 
 constexpr uint32_t kStep = 64;                                  // of the summed dimension a stage
 constexpr uint32_t kMaxStages = 8;
 constexpr uint32_t kPieceBytes = 32 * 32 * 4;                   // what a writing warp brings through shared memory at a time
-constexpr uint32_t kRun = 4;                                    // stages that the tensor cores add up by themselves (RUNS)
+constexpr uint32_t kRun = 8;                                    // stages that the tensor cores add up by themselves (RUNS)
 constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
 
 struct ProductArgs {
@@ -80,6 +80,20 @@ __host__ __device__ __forceinline__ ProdItem prod_item(const ProductArgs& a, uin
     }
     place_tile(a, x, t);
     return t;
+}
+
+// Elements 0 .. n - 1 by one lane, what eight of them read fetched together.
+template <typename F, typename A> __device__ __forceinline__ void one_by_one(uint32_t n, const F& fetch, const A& apply)
+{
+    for (uint32_t i = 0; i < n; i += 8) {
+        float2 f[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+            if (i + k < n) f[k] = fetch(i + k);
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+            if (i + k < n) apply(i + k, f[k]);
+    }
 }
 
 // 32 x 32 sums, a row a lane, from (r0, c0) on.  Whole pieces of matrices that allow 32-byte accesses are written from the lane that has
@@ -142,14 +156,13 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
                 for (uint32_t k = 0; k < 16; ++k) y[k] = value(first + k, c);
                 e.apply(b, c0 + c, r0 + first, f, y);
             }
-        } else if (r0 + lane < M)
-#pragma unroll 2
-            for (uint32_t c = 0; c < n; ++c) e.apply1(b, c0 + c, r0 + lane, value(lane, c));
-    } else {
-        const uint32_t n = min(32u, M - r0);
-        if (c0 + lane < N)
-#pragma unroll 2
-            for (uint32_t r = 0; r < n; ++r) e.apply1(b, r0 + r, c0 + lane, value(r, lane));
+        } else if (r0 + lane < M) {
+            one_by_one(n, [&](uint32_t c) { return e.fetch1(b, c0 + c, r0 + lane); },
+                       [&](uint32_t c, float2 f) { e.apply1(b, c0 + c, r0 + lane, f, value(lane, c)); });
+        }
+    } else if (c0 + lane < N) {
+        one_by_one(min(32u, M - r0), [&](uint32_t r) { return e.fetch1(b, r0 + r, c0 + lane); },
+                   [&](uint32_t r, float2 f) { e.apply1(b, r0 + r, c0 + lane, f, value(r, lane)); });
     }
     __syncwarp();
 }
@@ -184,6 +197,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
         fence_bar_init();
     }
     if (warp == 9) tmem_alloc_cols<CG>(&tmem_slot, 2 * a.acc_cols);
+    if (warp == 8 || warp == 10) prefetch_map(warp == 8 ? a.a : a.b);
     tc_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync();
@@ -369,7 +383,8 @@ template <typename E> __global__ void __launch_bounds__(32 * kJoinWarps) k_produ
 template <typename E> __global__ void __launch_bounds__(256) k_product_none(const __grid_constant__ E e, uint32_t M, uint32_t N)
 {
     const uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x, m = x / N;
-    if (m < M) e.apply1(0, (uint32_t)m, (uint32_t)(x - m * N), 0.0f);
+    const uint32_t n = (uint32_t)(x - m * N);
+    if (m < M) e.apply1(0, (uint32_t)m, n, e.fetch1(0, (uint32_t)m, n), 0.0f);
 }
 
 // Rows of any stride and alignment -> rows of `to` elements, a multiple of eight.

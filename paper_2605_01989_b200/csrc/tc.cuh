@@ -338,6 +338,7 @@ template <int CG> __device__ __forceinline__ void warp_tma3(uint32_t dst, const 
                      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                      : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void warp_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xFFFFFFFF;\n@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar), "r"(bytes)
