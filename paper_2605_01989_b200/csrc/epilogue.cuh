@@ -21,6 +21,28 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w)
                  : "memory");
 }
 
+// 128 bytes of shared memory per lane, 16-byte chunk c of lane l at l * 128 + ((c ^ l % 8) * 16): no bank conflicts.  What an epilogue
+// reads of a row (32 columns) is copied there while the piece before is worked on, and read back by the lane that asked for it.
+__device__ __forceinline__ uint8_t* chunk(uint8_t* piece, uint32_t c)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    return piece + lane * 128 + ((c ^ (lane & 7)) << 4);
+}
+template <int N> __device__ __forceinline__ void stage(uint8_t* piece, uint32_t c0, const void* from)
+{
+#pragma unroll
+    for (uint32_t c = 0; c < N; ++c)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(chunk(piece, c0 + c))), "l"((const char*)from + 16 * c) : "memory");
+}
+template <int N> __device__ __forceinline__ void staged(uint8_t* piece, uint32_t c0, uint32_t* w)
+{
+#pragma unroll
+    for (uint32_t c = 0; c < N; ++c) {
+        const uint4 q = *reinterpret_cast<const uint4*>(chunk(piece, c0 + c));
+        w[4 * c] = q.x; w[4 * c + 1] = q.y; w[4 * c + 2] = q.z; w[4 * c + 3] = q.w;
+    }
+}
+
 // Sixteen elements as they lie in memory.
 template <typename T> struct Raw {
     uint32_t w[sizeof(T) * 4];
@@ -170,7 +192,8 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
-// padding behind a row); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
+// padding behind a row); fetch1 and apply1 one.  ask and take: the same
+// as fetch for 32 columns, by way of the warp's piece of shared memory; reads(): there is something to fetch.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
@@ -179,6 +202,13 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole() && (uintptr_t)bias % 32 == 0; }
     struct Fetched { Raw<O> residual; };
+    __device__ __forceinline__ bool reads() const { return (bool)residual; }
+    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const { stage<2 * sizeof(O)>(piece, 0, residual.at(m, n)); }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
+    {
+        staged<sizeof(O)>(piece, 0, f[0].residual.w);
+        staged<sizeof(O)>(piece, sizeof(O), f[1].residual.w);
+    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (residual) f.residual.load(residual.at(m, n));
@@ -224,6 +254,20 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     struct Fetched { Raw<T> residual, pre; };
+    __device__ __forceinline__ bool reads() const { return residual || pre; }
+    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const
+    {
+        if (residual) stage<4>(piece, 0, residual.at(m, n));
+        if (pre) stage<4>(piece, 4, pre.at(m, n));
+    }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            staged<2>(piece, 2 * i, f[i].residual.w);
+            staged<2>(piece, 4 + 2 * i, f[i].pre.w);
+        }
+    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (residual) f.residual.load(residual.at(m, n));
@@ -265,6 +309,13 @@ template <typename O> struct EpiStore {                         // out = v [+ ou
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole(); }
     struct Fetched { Raw<O> out; };
+    __device__ __forceinline__ bool reads() const { return accumulate; }
+    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const { stage<2 * sizeof(O)>(piece, 0, out.at(m, n)); }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
+    {
+        staged<sizeof(O)>(piece, 0, f[0].out.w);
+        staged<sizeof(O)>(piece, sizeof(O), f[1].out.w);
+    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (accumulate) f.out.load(out.at(m, n));
@@ -291,6 +342,19 @@ struct Words {
     int64_t each;
     uint32_t stride;
     struct Fetched { Raw<__half> hi, lo; };
+    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const
+    {
+        stage<4>(piece, 0, hi + at(b, m, n));
+        if (lo) stage<4>(piece, 4, lo + at(b, m, n));
+    }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            staged<2>(piece, 2 * i, f[i].hi.w);
+            staged<2>(piece, 4 + 2 * i, f[i].lo.w);
+        }
+    }
     __device__ __forceinline__ int64_t at(uint32_t b, uint32_t m, uint32_t n) const { return b * each + (int64_t)m * stride + n; }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const
     {
@@ -338,6 +402,9 @@ struct EpiPoly {                                                // out = alpha v
     static constexpr bool kPadded = true;
     bool sectors() const { return true; }
     using Fetched = Words::Fetched;
+    __device__ __forceinline__ bool reads() const { return add.hi != nullptr; }
+    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const { add.ask(b, m, n, piece); }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const { add.take(piece, f); }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
     __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {
@@ -355,6 +422,9 @@ template <typename O> struct EpiLast {                          // the caller's 
     static constexpr bool kPadded = false;
     bool sectors() const { return aligned; }
     using Fetched = Words::Fetched;
+    __device__ __forceinline__ bool reads() const { return add.hi != nullptr; }
+    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const { add.ask(b, m, n, piece); }
+    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const { add.take(piece, f); }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
     __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
     {

@@ -21,6 +21,7 @@ struct UpdIn {
     Source x;
     int64_t each;
     uint32_t rows, cols, parts;
+    FastDiv by_row;                              // groups of eight in a row; rows * groups < 2^32
     double* squares;                             // [batch][parts]
     float eps;
     Words out;
@@ -49,12 +50,19 @@ __global__ void __launch_bounds__(kUpdThreads) k_squares(const __grid_constant__
     Source x = a.x;
     x.p = (const char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
     double t = 0.0;
-    for (uint64_t g = g0 + threadIdx.x; g < g1; g += kUpdThreads) {
-        const uint32_t r = (uint32_t)(g / per_row), c = (uint32_t)(g - (uint64_t)r * per_row) * 8;
-        float v[8];
-        load8(x, r, c, min(8u, a.cols - c), v);
+    for (uint64_t g = g0 + threadIdx.x; g < g1; g += 4 * kUpdThreads) {             // four groups on their way
+        float v[4][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t = fma((double)v[i], (double)v[i], t);
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint64_t h = min(g + u * kUpdThreads, groups - 1);
+            const uint32_t r = a.by_row.div((uint32_t)h), c = ((uint32_t)h - r * per_row) * 8;
+            load8(x, r, c, min(8u, a.cols - c), v[u]);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+            if (g + u * kUpdThreads < g1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t = fma((double)v[u][i], (double)v[u][i], t);
     }
     t = block_sum(t, part);
     if (threadIdx.x == 0) a.squares[(size_t)b * a.parts + blockIdx.x] = t;
@@ -254,6 +262,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     in.rows = u->rows;
     in.cols = u->cols;
     in.parts = p.parts;
+    in.by_row = FastDiv((u->cols + 7) / 8);
     in.squares = w.squares;
     in.eps = u->eps;
     in.out = w.x;

@@ -293,6 +293,29 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
         for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
             const ProdItem t = prod_item(a, x);
             const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, c0 = t.j * a.bn + half;
+            // Whole pieces whose epilogue reads something have it brought ahead (not beside a mirror, which needs the same memory).
+            const bool ahead = a.direct && !a.turned && !a.symmetric && t.slot == kWhole && e.reads() && r0 + 32 <= a.M;
+            auto asked = [&](uint32_t c) { return ahead && half + c < a.bn && c0 + c + 32 <= a.N; };
+            auto ask = [&](uint32_t c) {
+                if (asked(c)) e.ask(t.b, r0 + (tid & 31), c0 + c, piece);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            auto write = [&](uint32_t c, float* v, const auto& sums) {
+                if (t.slot != kWhole) {
+                    write_partial(a, t, r0, c0 + c, v, sums);
+                } else if (asked(c)) {
+                    typename E::Fetched f[2];
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    e.take(piece, f);
+                    ask(c + 64);
+                    sums();
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i) e.apply(t.b, r0 + (tid & 31), c0 + c + 16 * i, f[i], v + 16 * i);
+                } else {
+                    write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
+                }
+            };
+            if (!RUNS) ask(0);
             if (RUNS) {
                 float2 sums[4][16] = {};
                 const uint32_t n = t.k1 - t.k0;
@@ -315,13 +338,10 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                     else warp_arrive(&acc_free[w & 1]);
                 }
                 if (!ok) break;
+                ask(0);
 #pragma unroll
                 for (uint32_t p = 0; p < 4; ++p)
-                    if (half + 64 * p < a.bn) {
-                        float* v = reinterpret_cast<float*>(sums[p]);
-                        if (t.slot == kWhole) write_piece(a, e, t.b, r0, c0 + 64 * p, v, piece, [] {});
-                        else write_partial(a, t, r0, c0 + 64 * p, v, [] {});
-                    }
+                    if (half + 64 * p < a.bn) write(64 * p, reinterpret_cast<float*>(sums[p]), [] {});
             } else {
                 ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
                 if (!ok) break;
@@ -334,8 +354,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                         tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(v));
                         tmem_wait_ld<32>(reinterpret_cast<uint32_t*>(v));
                     };
-                    if (t.slot == kWhole) write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
-                    else write_partial(a, t, r0, c0 + c, v, sums);
+                    write(c, v, sums);
                 }
                 tc_fence_before();
                 if (CG == 2) warp_arrive_in(in_block(&acc_free[w & 1], 0));
@@ -344,6 +363,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             }
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -352,22 +372,25 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
     if (warp == 9) tmem_free_cols<CG>(tmem, 2 * a.acc_cols);
 }
 
-// Tiles that were done in parts: their sums, in order, and the epilogue; a warp a piece of 32 x 32.
-constexpr int kJoinWarps = 4;
+// Tiles that were done in parts: a block a piece of 32 x 32.  Warp i adds up parts i, i + 8, ..., the first warp the eight sums, in
+// order, and writes.  (One warp a piece, part after part: 10 us for 10 parts, a trip to memory each.)
+constexpr int kJoinWarps = 8;
 template <typename E> __global__ void __launch_bounds__(32 * kJoinWarps) k_product_join(const __grid_constant__ ProductArgs a, const __grid_constant__ E e)
 {
-    __shared__ __align__(128) uint8_t pieces[kJoinWarps][kPieceBytes];
+    __shared__ __align__(128) float4 sums[kJoinWarps][8][32];
     wait_before();
     after_start();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, across = (a.bn + 31) / 32, each = a.tm / 32 * across;
-    const uint32_t x = blockIdx.x * kJoinWarps + warp, n = x / each, y = x - n * each, pr = y / across, pc = y - pr * across;
-    if (n >= a.rest) return;
+    const uint32_t n = blockIdx.x / each, y = blockIdx.x - n * each, pr = y / across, pc = y - pr * across;
     ProdItem t;
     place_tile(a, a.whole + n, t);
-    float2 v[16] = {};
-    write_piece(a, e, t.b, t.i * a.tm + pr * 32, t.j * a.bn + pc * 32, reinterpret_cast<float*>(v), pieces[warp], [&] {
-        const float* p = a.partial + ((size_t)n * a.parts * a.tm + pr * 32 + lane) * a.bn + pc * 32;
-        for (uint32_t s = 0; s < a.parts; ++s, p += (size_t)a.tm * a.bn) {
+    const uint32_t r0 = t.i * a.tm + pr * 32, c0 = t.j * a.bn + pc * 32;
+    if (r0 >= a.M || c0 >= a.N || (a.symmetric && c0 < r0)) return;
+    if (warp < a.parts) {
+        const float* p = a.partial + ((size_t)(n * a.parts + warp) * a.tm + pr * 32 + lane) * a.bn + pc * 32;
+        float2 v[16] = {};
+#pragma unroll 2
+        for (uint32_t s = warp; s < a.parts; s += kJoinWarps, p += (size_t)kJoinWarps * a.tm * a.bn) {
             uint32_t w[32];
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i)
@@ -375,6 +398,22 @@ template <typename E> __global__ void __launch_bounds__(32 * kJoinWarps) k_produ
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i)
                 if (2 * i < a.bn) v[i] = add2(v[i], pair(w[2 * i], w[2 * i + 1]));
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) sums[warp][i][lane] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+    }
+    __syncthreads();
+    if (warp) return;
+    float v[32];
+    write_piece(a, e, t.b, r0, c0, v, (uint8_t*)sums, [&] {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            float4 x = sums[0][i][lane];
+            for (uint32_t k = 1; k < min(a.parts, (uint32_t)kJoinWarps); ++k) {
+                const float4 q = sums[k][i][lane];
+                x = make_float4(x.x + q.x, x.y + q.y, x.z + q.z, x.w + q.w);
+            }
+            v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
         }
     });
 }
@@ -621,7 +660,7 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
     if (int rc = r.cg == 2 ? launch_product<2, RUNS>(a, e, chained, s) : launch_product<1, RUNS>(a, e, chained, s)) return rc;
     if (r.rest == 0) return DBLP_OK;
     const uint64_t pieces = (uint64_t)r.rest * (a.tm / 32) * ((r.bn + 31) / 32);
-    DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)((pieces + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, s, a, e));
+    DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)pieces), 32 * kJoinWarps, 0, s, a, e));
     return DBLP_OK;
 }
 
