@@ -21,28 +21,6 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w)
                  : "memory");
 }
 
-// 128 bytes of shared memory per lane, 16-byte chunk c of lane l at l * 128 + ((c ^ l % 8) * 16): no bank conflicts.  What an epilogue
-// reads of a row (32 columns) is copied there while the piece before is worked on, and read back by the lane that asked for it.
-__device__ __forceinline__ uint8_t* chunk(uint8_t* piece, uint32_t c)
-{
-    const uint32_t lane = threadIdx.x & 31;
-    return piece + lane * 128 + ((c ^ (lane & 7)) << 4);
-}
-template <int N> __device__ __forceinline__ void stage(uint8_t* piece, uint32_t c0, const void* from)
-{
-#pragma unroll
-    for (uint32_t c = 0; c < N; ++c)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(chunk(piece, c0 + c))), "l"((const char*)from + 16 * c) : "memory");
-}
-template <int N> __device__ __forceinline__ void staged(uint8_t* piece, uint32_t c0, uint32_t* w)
-{
-#pragma unroll
-    for (uint32_t c = 0; c < N; ++c) {
-        const uint4 q = *reinterpret_cast<const uint4*>(chunk(piece, c0 + c));
-        w[4 * c] = q.x; w[4 * c + 1] = q.y; w[4 * c + 2] = q.z; w[4 * c + 3] = q.w;
-    }
-}
-
 // Sixteen elements as they lie in memory.
 template <typename T> struct Raw {
     uint32_t w[sizeof(T) * 4];
@@ -57,6 +35,39 @@ template <typename T> struct Raw {
         else return unpack2<T>(w[i]);
     }
 };
+// Where sixteen results of a row go: to memory, or into a piece of 32 x 32 in shared memory that one TMA store takes from there.
+// (Stores from the lanes, a row each, took 100 cycles an instruction: 32 lines.)  Rows of 64 bytes are laid out as TMA's 64-byte swizzle
+// has them, chunk c of row r at c ^ (r / 2 % 4), rows of 128 as its 128-byte swizzle, c ^ (r % 8): no bank conflicts.
+struct ToMemory {
+    template <typename T> __device__ __forceinline__ void put(int, T* p, const float* x) const;
+};
+struct ToPiece {
+    uint8_t* piece;
+    uint32_t first;                       // 0: columns 0 .. 15 of the piece, 16: the others
+    template <typename T> __device__ __forceinline__ void put(int output, T*, const float* x) const
+    {
+        const uint32_t r = threadIdx.x & 31;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (uint32_t c = 0; c < 4; ++c)
+                *reinterpret_cast<float4*>(piece + r * 128 + (((first / 4 + c) ^ (r & 7)) << 4)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+        } else {
+#pragma unroll
+            for (uint32_t c = 0; c < 2; ++c)
+                *reinterpret_cast<uint4*>(piece + output * 2048 + r * 64 + (((first / 8 + c) ^ (r >> 1 & 3)) << 4)) =
+                    make_uint4(pack2<T>(x[8 * c], x[8 * c + 1]), pack2<T>(x[8 * c + 2], x[8 * c + 3]), pack2<T>(x[8 * c + 4], x[8 * c + 5]),
+                               pack2<T>(x[8 * c + 6], x[8 * c + 7]));
+        }
+    }
+};
+
+// A result that TMA can store: null where the epilogue has none.
+struct Output {
+    void* p;
+    int64_t stride, each;                 // rows; products of a batch
+    int bytes;                            // of an element
+};
+
 template <typename T> __device__ __forceinline__ void store16(T* p, const float* x)
 {
     if constexpr (sizeof(T) == 4) {
@@ -69,6 +80,8 @@ template <typename T> __device__ __forceinline__ void store16(T* p, const float*
         store32(p, w);
     }
 }
+
+template <typename T> __device__ __forceinline__ void ToMemory::put(int, T* p, const float* x) const { store16(p, x); }
 
 // A row-major matrix that an epilogue reads or writes.
 template <typename T> struct Rows {
@@ -192,8 +205,7 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
-// padding behind a row); fetch1 and apply1 one.  ask and take: the same
-// as fetch for 32 columns, by way of the warp's piece of shared memory; reads(): there is something to fetch.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
+// padding behind a row); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
@@ -201,19 +213,13 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
     int bias_dtype, act;
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole() && (uintptr_t)bias % 32 == 0; }
+    Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{pre.p, pre.stride, 0, 2}; }
     struct Fetched { Raw<O> residual; };
-    __device__ __forceinline__ bool reads() const { return (bool)residual; }
-    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const { stage<2 * sizeof(O)>(piece, 0, residual.at(m, n)); }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
-    {
-        staged<sizeof(O)>(piece, 0, f[0].residual.w);
-        staged<sizeof(O)>(piece, sizeof(O), f[1].residual.w);
-    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (residual) f.residual.load(residual.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
+    template <typename S> __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
         if (bias) {                                             // the same sixteen for all lanes
             if (bias_dtype == DBLP_F32) {
@@ -230,10 +236,10 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
                 Rows<__half>().add(r, v);
             }
         }
-        if (pre) store16(pre.at(m, n), v);
+        if (pre) to.put(0, pre.at(m, n), v);
         activate<16>(act, v);
         if (residual) residual.add(f.residual, v);
-        store16(out.at(m, n), v);
+        to.put(1, out.at(m, n), v);
     }
     __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
@@ -253,27 +259,14 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
     int act;
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
+    Output output(int k) const { return k ? Output{out.p, out.stride, 0, 2} : Output{}; }
     struct Fetched { Raw<T> residual, pre; };
-    __device__ __forceinline__ bool reads() const { return residual || pre; }
-    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const
-    {
-        if (residual) stage<4>(piece, 0, residual.at(m, n));
-        if (pre) stage<4>(piece, 4, pre.at(m, n));
-    }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            staged<2>(piece, 2 * i, f[i].residual.w);
-            staged<2>(piece, 4 + 2 * i, f[i].pre.w);
-        }
-    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (residual) f.residual.load(residual.at(m, n));
         if (pre) f.pre.load(pre.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
+    template <typename S> __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
         if (residual) residual.add(f.residual, v);
         if (pre) {
@@ -286,7 +279,7 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
             }
             activate_grad<16>(act, z, v);
         }
-        store16(out.at(m, n), v);
+        to.put(1, out.at(m, n), v);
     }
     __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
@@ -308,22 +301,16 @@ template <typename O> struct EpiStore {                         // out = v [+ ou
     bool accumulate;
     static constexpr bool kPadded = false;
     bool sectors() const { return out.whole(); }
+    Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{}; }
     struct Fetched { Raw<O> out; };
-    __device__ __forceinline__ bool reads() const { return accumulate; }
-    __device__ __forceinline__ void ask(uint32_t, uint32_t m, uint32_t n, uint8_t* piece) const { stage<2 * sizeof(O)>(piece, 0, out.at(m, n)); }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
-    {
-        staged<sizeof(O)>(piece, 0, f[0].out.w);
-        staged<sizeof(O)>(piece, sizeof(O), f[1].out.w);
-    }
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
     {
         if (accumulate) f.out.load(out.at(m, n));
     }
-    __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v) const
+    template <typename S> __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
         if (accumulate) out.add(f.out, v);
-        store16(out.at(m, n), v);
+        to.put(1, out.at(m, n), v);
     }
     __device__ __forceinline__ float2 fetch1(uint32_t, uint32_t m, uint32_t n) const
     {
@@ -342,19 +329,6 @@ struct Words {
     int64_t each;
     uint32_t stride;
     struct Fetched { Raw<__half> hi, lo; };
-    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const
-    {
-        stage<4>(piece, 0, hi + at(b, m, n));
-        if (lo) stage<4>(piece, 4, lo + at(b, m, n));
-    }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            staged<2>(piece, 2 * i, f[i].hi.w);
-            staged<2>(piece, 4 + 2 * i, f[i].lo.w);
-        }
-    }
     __device__ __forceinline__ int64_t at(uint32_t b, uint32_t m, uint32_t n) const { return b * each + (int64_t)m * stride + n; }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const
     {
@@ -379,20 +353,17 @@ struct Words {
         const int64_t i = at(b, m, n);
         return hi ? to_f32(hi[i]) + (lo ? to_f32(lo[i]) : 0.0f) : 0.0f;
     }
-    __device__ __forceinline__ void store(uint32_t b, uint32_t m, uint32_t n, const float* x) const
+    template <typename S> __device__ __forceinline__ void store(uint32_t b, uint32_t m, uint32_t n, float* x, const S& to) const
     {
-        uint32_t w[8];
+        to.put(0, hi + at(b, m, n), x);
+        if (!lo) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = pack2<__half>(x[2 * i], x[2 * i + 1]);
-        store32(hi + at(b, m, n), w);
-        if (lo) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 t = unpack2<__half>(w[i]);
-                w[i] = pack2<__half>(x[2 * i] - t.x, x[2 * i + 1] - t.y);
-            }
-            store32(lo + at(b, m, n), w);
+        for (int i = 0; i < 8; ++i) {
+            const float2 t = unpack2<__half>(pack2<__half>(x[2 * i], x[2 * i + 1]));
+            x[2 * i] -= t.x;
+            x[2 * i + 1] -= t.y;
         }
+        to.put(1, lo + at(b, m, n), x);
     }
 };
 
@@ -401,15 +372,13 @@ struct EpiPoly {                                                // out = alpha v
     float alpha, beta;
     static constexpr bool kPadded = true;
     bool sectors() const { return true; }
+    Output output(int k) const { return Output{k ? out.lo : out.hi, out.stride, out.each, 2}; }
     using Fetched = Words::Fetched;
-    __device__ __forceinline__ bool reads() const { return add.hi != nullptr; }
-    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const { add.ask(b, m, n, piece); }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const { add.take(piece, f); }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
-    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
+    template <typename S> __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
         add.combine(f, alpha, beta, v);
-        out.store(b, m, n, v);
+        out.store(b, m, n, v, to);
     }
 };
 
@@ -421,15 +390,13 @@ template <typename O> struct EpiLast {                          // the caller's 
     bool aligned;                                               // of all products of the batch
     static constexpr bool kPadded = false;
     bool sectors() const { return aligned; }
+    Output output(int k) const { return k ? Output{out.p, out.stride, each, (int)sizeof(O)} : Output{}; }
     using Fetched = Words::Fetched;
-    __device__ __forceinline__ bool reads() const { return add.hi != nullptr; }
-    __device__ __forceinline__ void ask(uint32_t b, uint32_t m, uint32_t n, uint8_t* piece) const { add.ask(b, m, n, piece); }
-    __device__ __forceinline__ void take(uint8_t* piece, Fetched* f) const { add.take(piece, f); }
     __device__ __forceinline__ void fetch(uint32_t b, uint32_t m, uint32_t n, Fetched& f) const { add.fetch(b, m, n, f); }
-    __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v) const
+    template <typename S> __device__ __forceinline__ void apply(uint32_t b, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
         add.combine(f, alpha, beta, v);
-        store16(out.at(m, n) + b * each, v);
+        to.put(1, out.at(m, n) + b * each, v);
     }
     __device__ __forceinline__ float2 fetch1(uint32_t b, uint32_t m, uint32_t n) const { return make_float2(add.value(b, m, n), 0.0f); }
     __device__ __forceinline__ void apply1(uint32_t b, uint32_t m, uint32_t n, float2 f, float x) const

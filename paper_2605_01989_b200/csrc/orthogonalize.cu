@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
         load8(x, r, c + 8, left > 8 ? left - 8 : 0, v + 8);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = (float)((double)v[i] * f);
-        a.out.store(b, r, c, v);
+        a.out.store(b, r, c, v, ToMemory());
     }
 }
 

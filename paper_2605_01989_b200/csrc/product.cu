@@ -25,14 +25,14 @@ constexpr uint32_t kRun = 8;                                    // stages that t
 constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
 
 struct ProductArgs {
-    CUtensorMap a[2], b[2];                                     // first and second words
+    CUtensorMap a[2], b[2], o[2];                               // first and second words; results, pieces of 32 x 32
     uint32_t M, N, tm, bn, mt, nt;                              // tiles of tm = 128 (256) rows x bn columns
     uint32_t steps, term_steps;                                 // stages of a tile (terms together), of a term
     uint32_t whole, rest, parts, per, items;                    // tiles done whole; tiles done in parts of `per` stages; items in all
     uint32_t group, tiles;                                      // tile rows walked together; tiles of one product
     FastDiv by_tiles, by_rest, by_all, by_group, by_last;
     uint32_t stages, stage_bytes, b_bytes, acc_cols, idesc;
-    uint32_t a_mn, b_mn, symmetric, turned, direct;
+    uint32_t a_mn, b_mn, symmetric, turned, direct, bulk;       // bulk: bit k, result k goes by TMA (bit 2: it is fp32); 0: none does
     float* partial;                                             // [rest][parts][tm][bn]
     unsigned long long* timeouts;
 };
@@ -105,6 +105,10 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
 {
     const uint32_t M = a.M, N = a.N, lane = threadIdx.x & 31;
     if (r0 >= M || c0 >= N || (a.symmetric && c0 < r0)) return;
+    if (a.bulk) {                                               // the piece may still be on its way out
+        if (lane == 0) bulk_wait_read<0>();
+        __syncwarp();
+    }
     auto value = [&](uint32_t r, uint32_t c) { return *reinterpret_cast<const float*>(piece + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4); };
     const bool direct = a.direct && !a.turned && (E::kPadded || (r0 + 32 <= M && c0 + 32 <= N)), mirror = E::kPadded && a.symmetric && c0 > r0;
     if (direct) {
@@ -119,7 +123,7 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
         for (int i = 0; i < 32; ++i) y[i] = v[i];
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i)
-            if (in && c0 + 16 * i < N) e.apply(b, r0 + lane, c0 + 16 * i, f[i], y + 16 * i);
+            if (in && c0 + 16 * i < N) e.apply(b, r0 + lane, c0 + 16 * i, f[i], y + 16 * i, ToMemory());
         if (!mirror) return;
     } else {
         sums();
@@ -139,7 +143,7 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
                 e.fetch(b, c0 + lane, r0 + 16 * i, f);
 #pragma unroll
                 for (uint32_t k = 0; k < 16; ++k) y[k] = value(16 * i + k, lane);
-                e.apply(b, c0 + lane, r0 + 16 * i, f, y);
+                e.apply(b, c0 + lane, r0 + 16 * i, f, y, ToMemory());
             }
         }
     } else if (a.turned) {                                      // rows of the result are the piece's columns
@@ -154,7 +158,7 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
                 e.fetch(b, c0 + c, r0 + first, f);
 #pragma unroll
                 for (uint32_t k = 0; k < 16; ++k) y[k] = value(first + k, c);
-                e.apply(b, c0 + c, r0 + first, f, y);
+                e.apply(b, c0 + c, r0 + first, f, y, ToMemory());
             }
         } else if (r0 + lane < M) {
             one_by_one(n, [&](uint32_t c) { return e.fetch1(b, c0 + c, r0 + lane); },
@@ -163,6 +167,29 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
     } else if (c0 + lane < N) {
         one_by_one(min(32u, M - r0), [&](uint32_t r) { return e.fetch1(b, r0 + r, c0 + lane); },
                    [&](uint32_t r, float2 f) { e.apply1(b, r0 + r, c0 + lane, f, value(r, lane)); });
+    }
+    __syncwarp();
+}
+
+// A whole piece by way of shared memory and TMA.
+template <typename E, typename F>
+__device__ __forceinline__ void write_bulk(const ProductArgs& a, const E& e, uint32_t b, uint32_t r0, uint32_t c0, float* v, uint8_t* piece, const F& sums)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    typename E::Fetched f[2];
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) e.fetch(b, r0 + lane, c0 + 16 * i, f[i]);
+    sums();
+    if (lane == 0) bulk_wait_read<0>();                         // the last piece has left
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) e.apply(b, r0 + lane, c0 + 16 * i, f[i], v + 16 * i, ToPiece{piece, 16 * i});
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+        if (a.bulk & 1) tma_store3(&a.o[0], piece, (int)c0, (int)r0, (int)b);
+        if (a.bulk & 2) tma_store3(&a.o[1], piece + (a.bulk & 4 ? 0 : 2048), (int)c0, (int)r0, (int)b);
+        bulk_commit();
     }
     __syncwarp();
 }
@@ -293,29 +320,11 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
         for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
             const ProdItem t = prod_item(a, x);
             const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, c0 = t.j * a.bn + half;
-            // Whole pieces whose epilogue reads something have it brought ahead (not beside a mirror, which needs the same memory).
-            const bool ahead = a.direct && !a.turned && !a.symmetric && t.slot == kWhole && e.reads() && r0 + 32 <= a.M;
-            auto asked = [&](uint32_t c) { return ahead && half + c < a.bn && c0 + c + 32 <= a.N; };
-            auto ask = [&](uint32_t c) {
-                if (asked(c)) e.ask(t.b, r0 + (tid & 31), c0 + c, piece);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            };
             auto write = [&](uint32_t c, float* v, const auto& sums) {
-                if (t.slot != kWhole) {
-                    write_partial(a, t, r0, c0 + c, v, sums);
-                } else if (asked(c)) {
-                    typename E::Fetched f[2];
-                    asm volatile("cp.async.wait_group 0;" ::: "memory");
-                    e.take(piece, f);
-                    ask(c + 64);
-                    sums();
-#pragma unroll
-                    for (uint32_t i = 0; i < 2; ++i) e.apply(t.b, r0 + (tid & 31), c0 + c + 16 * i, f[i], v + 16 * i);
-                } else {
-                    write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
-                }
+                if (t.slot != kWhole) write_partial(a, t, r0, c0 + c, v, sums);
+                else if (a.bulk && r0 + 32 <= a.M && c0 + c + 32 <= a.N) write_bulk(a, e, t.b, r0, c0 + c, v, piece, sums);
+                else write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
             };
-            if (!RUNS) ask(0);
             if (RUNS) {
                 float2 sums[4][16] = {};
                 const uint32_t n = t.k1 - t.k0;
@@ -338,7 +347,6 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                     else warp_arrive(&acc_free[w & 1]);
                 }
                 if (!ok) break;
-                ask(0);
 #pragma unroll
                 for (uint32_t p = 0; p < 4; ++p)
                     if (half + 64 * p < a.bn) write(64 * p, reinterpret_cast<float*>(sums[p]), [] {});
@@ -363,7 +371,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             }
         }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (lane == 0) bulk_wait<0>();
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -540,6 +548,21 @@ static int make_map(CUtensorMap* map, const void* data, int64_t stride, const Op
     return DBLP_OK;
 }
 
+// Pieces of 32 x 32 of a result.
+static int make_store_map(CUtensorMap* map, const Output& o, const Product& p)
+{
+    const EncodeTiled encode = map_encoder();
+    DBLP_REQUIRE(encode, DBLP_ECUDA, "product: the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t unused = ((cuuint64_t)p.N * o.bytes + 15) / 16 * 16;
+    const cuuint64_t dims[3] = {p.N, p.M, p.batch}, strides[2] = {p.M > 1 ? (cuuint64_t)o.stride * o.bytes : unused, p.batch > 1 ? (cuuint64_t)o.each * o.bytes : unused};
+    const cuuint32_t boxes[3] = {32, 32, 1}, ones[3] = {1, 1, 1};
+    const CUresult rc = encode(map, o.bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, o.p, dims, strides, boxes, ones,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, o.bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    DBLP_REQUIRE(rc == CUDA_SUCCESS, DBLP_ECUDA, "product: tensor map of a result refused (driver error %d)", (int)rc);
+    return DBLP_OK;
+}
+
 template <int CG, bool RUNS, typename E> static int launch_product(const ProductArgs& a, const E& e, bool chained, cudaStream_t s)
 {
     constexpr auto kernel = k_product<CG, RUNS, E>;
@@ -656,6 +679,18 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
     a.idesc = p.dtype == DBLP_BF16 ? mma_desc<__nv_bfloat16>(128 * r.cg, r.bn, oa.mn, ob.mn) : mma_desc<__half>(128 * r.cg, r.bn, oa.mn, ob.mn);
     a.timeouts = timeouts;
     a.direct = e.sectors();
+    // Results by TMA where blocks have several tiles: for one tile a block its latency (1.5 us) is longer than what it saves.
+    if (a.direct && !r.turned && !p.symmetric && a.items > (uint32_t)kSms / r.cg) {
+        const Output o[2] = {e.output(0), e.output(1)};
+        const bool down = p.M <= 1 || ((!o[0].p || o[0].stride > 0) && (!o[1].p || o[1].stride > 0));      // TMA knows no negative strides
+        if (down && !(o[0].p && o[1].p && o[1].bytes == 4)) {   // a 16-bit and an fp32 piece together are more than there is room for
+            for (int k = 0; k < 2; ++k) {
+                if (!o[k].p) continue;
+                if (int rc = make_store_map(&a.o[k], o[k], p)) return rc;
+                a.bulk |= 1u << k | (o[k].bytes == 4 ? 4u : 0u);
+            }
+        }
+    }
     a.partial = (float*)at;
     if (int rc = r.cg == 2 ? launch_product<2, RUNS>(a, e, chained, s) : launch_product<1, RUNS>(a, e, chained, s)) return rc;
     if (r.rest == 0) return DBLP_OK;

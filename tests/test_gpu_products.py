@@ -139,6 +139,22 @@ def test_linear_strides_broadcasts_and_places(n, i, o):
     within(res, y, tol, "over the residual")
 
 
+def test_rows_in_reverse():
+    """Negative row strides, which the header allows (a tensor cannot have them: raw addresses)."""
+    import ctypes as C
+    n, i, o = 300, 64, 96
+    x, w = randn((n, i), BF16, 1), randn((i, o), BF16, 2, i ** -0.5)
+    out, plain = torch.zeros((n, o), dtype=BF16, device=DEV), linear(x, w, BF16)
+    m = lambda t, rows: C.byref(dblp.dblp_matrix_t(t.data_ptr() + (rows - 1) * t.stride(0) * 2, -t.stride(0), 1))
+    l = dblp.dblp_linear_t(n, i, o, 1, 1, 0, 0, 0)
+    f = C.c_size_t()
+    assert dblp.lib().dblp_linear_workspace_bytes(C.byref(l), m(x, n), C.byref(dblp.dblp_matrix_t(w.data_ptr(), o, 1)), None, C.byref(f), None) == 0
+    ws = space(f.value)
+    rc = dblp.lib().dblp_linear(C.byref(l), m(x, n), C.byref(dblp.dblp_matrix_t(w.data_ptr(), o, 1)), None, None, None, m(out, n), ws.data_ptr(), f.value,
+                                torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(out, plain)
+
+
 def test_linear_without_input_columns_or_rows():
     bias, res = randn((40,), F32, 1), randn((9, 40), F32, 2)
     x, w = torch.empty((9, 0), dtype=BF16, device=DEV), torch.empty((0, 40), dtype=BF16, device=DEV)
