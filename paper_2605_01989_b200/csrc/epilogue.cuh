@@ -205,13 +205,14 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
-// padding behind a row); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
+// padding behind a row; kFewRows: A may have few; kMirror: the result
+// may equal its transpose and be computed by half); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
     const void* bias;
     int bias_dtype, act;
-    static constexpr bool kPadded = false;
+    static constexpr bool kPadded = false, kFewRows = true, kMirror = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole() && (uintptr_t)bias % 32 == 0; }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{pre.p, pre.stride, 0, 2}; }
     struct Fetched { Raw<O> residual; };
@@ -257,7 +258,7 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
 template <typename T> struct EpiGradX {                         // dx = (v + residual) act'(pre)
     Rows<T> out, residual, pre;
     int act;
-    static constexpr bool kPadded = false;
+    static constexpr bool kPadded = false, kFewRows = true, kMirror = false;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, 2} : Output{}; }
     struct Fetched { Raw<T> residual, pre; };
@@ -299,7 +300,7 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
 template <typename O> struct EpiStore {                         // out = v [+ out]
     Rows<O> out;
     bool accumulate;
-    static constexpr bool kPadded = false;
+    static constexpr bool kPadded = false, kFewRows = false, kMirror = false;
     bool sectors() const { return out.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{}; }
     struct Fetched { Raw<O> out; };
@@ -367,10 +368,10 @@ struct Words {
     }
 };
 
-struct EpiPoly {                                                // out = alpha v [+ beta add], both in words
+template <bool SYMMETRIC> struct EpiPoly {                      // out = alpha v [+ beta add], both in words
     Words out, add;
     float alpha, beta;
-    static constexpr bool kPadded = true;
+    static constexpr bool kPadded = true, kFewRows = false, kMirror = SYMMETRIC;
     bool sectors() const { return true; }
     Output output(int k) const { return Output{k ? out.lo : out.hi, out.stride, out.each, 2}; }
     using Fetched = Words::Fetched;
@@ -388,7 +389,7 @@ template <typename O> struct EpiLast {                          // the caller's 
     Words add;
     float alpha, beta;
     bool aligned;                                               // of all products of the batch
-    static constexpr bool kPadded = false;
+    static constexpr bool kPadded = false, kFewRows = false, kMirror = false;
     bool sectors() const { return aligned; }
     Output output(int k) const { return k ? Output{out.p, out.stride, each, (int)sizeof(O)} : Output{}; }
     using Fetched = Words::Fetched;

@@ -192,6 +192,11 @@ static Product product_of(const dblp_linear_t* l, const Operand& a, const Operan
     p.batch = 1;
     p.dtype = l->dtype;
     p.terms = 1;
+    return p;
+}
+
+static Product few(Product p)
+{
     p.few = true;
     return p;
 }
@@ -199,11 +204,11 @@ static Product product_of(const dblp_linear_t* l, const Operand& a, const Operan
 // The three products.  x w, dy w^T, x^T dy (or its transpose, where dw is held that way).
 static Product forward_product(const dblp_linear_t* l, const dblp_matrix_t* x, const dblp_matrix_t* w)
 {
-    return product_of(l, operand(x, l->rows, l->in, false), operand(w, l->in, l->out, true), l->rows, l->out, l->in);
+    return few(product_of(l, operand(x, l->rows, l->in, false), operand(w, l->in, l->out, true), l->rows, l->out, l->in));
 }
 static Product dx_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* w)
 {
-    return product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out);
+    return few(product_of(l, operand(dy, l->rows, l->out, false), operand(w, l->in, l->out, false), l->rows, l->in, l->out));
 }
 static Product dw_product(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp_matrix_t* x, bool by_rows)
 {

@@ -274,7 +274,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     Words now = w.x, next = w.y;
     for (uint32_t i = 0; i < u->steps; ++i) {
         const float a = u->coefficients[3 * i], b = u->coefficients[3 * i + 1], c = u->coefficients[3 * i + 2];
-        EpiPoly e{};
+        EpiPoly<true> e{};
         e.out = w.a;
         e.alpha = kScaleA / (float)(kScaleX * kScaleX);
         DBLP_TRY(product(p, gram_product(u, p, now), e, w.products, s));
@@ -285,11 +285,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
         DBLP_TRY(product(p, square_product(u, p, w.a), e, w.products, s));
         const Product last = step_product(u, p, w.b, now);
         if (i + 1 < u->steps) {
-            e.out = next;
-            e.add = now;
-            e.alpha = 1.0f / kScaleA;
-            e.beta = a;
-            DBLP_TRY(product(p, last, e, w.products, s));
+            DBLP_TRY(product(p, last, EpiPoly<false>{next, now, 1.0f / kScaleA, a}, w.products, s));
             const Words t = now;
             now = next;
             next = t;

@@ -21,7 +21,6 @@ constexpr int kProdThreads = 384, kProdWriters = 8;             // warps 0 .. 7 
 constexpr uint32_t kStep = 64;                                  // of the summed dimension a stage
 constexpr uint32_t kMaxStages = 8;
 constexpr uint32_t kPieceBytes = 32 * 32 * 4;                   // what a writing warp brings through shared memory at a time
-constexpr uint32_t kRun = 8;                                    // stages that the tensor cores add up by themselves (RUNS)
 constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
 
 struct ProductArgs {
@@ -32,6 +31,7 @@ struct ProductArgs {
     uint32_t group, tiles;                                      // tile rows walked together; tiles of one product
     FastDiv by_tiles, by_rest, by_all, by_group, by_last;
     uint32_t stages, stage_bytes, b_bytes, acc_cols, idesc;
+    uint32_t run;                                               // stages that the tensor cores add up by themselves (RUNS)
     uint32_t a_mn, b_mn, symmetric, turned, direct, bulk;       // bulk: bit k, result k goes by TMA (bit 2: it is fp32); 0: none does
     float* partial;                                             // [rest][parts][tm][bn]
     unsigned long long* timeouts;
@@ -105,12 +105,12 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
 {
     const uint32_t M = a.M, N = a.N, lane = threadIdx.x & 31;
     if (r0 >= M || c0 >= N || (a.symmetric && c0 < r0)) return;
-    if (a.bulk) {                                               // the piece may still be on its way out
+    if (!E::kMirror && a.bulk) {                                // the piece may still be on its way out
         if (lane == 0) bulk_wait_read<0>();
         __syncwarp();
     }
     auto value = [&](uint32_t r, uint32_t c) { return *reinterpret_cast<const float*>(piece + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4); };
-    const bool direct = a.direct && !a.turned && (E::kPadded || (r0 + 32 <= M && c0 + 32 <= N)), mirror = E::kPadded && a.symmetric && c0 > r0;
+    const bool direct = a.direct && !a.turned && (E::kPadded || (r0 + 32 <= M && c0 + 32 <= N)), mirror = E::kMirror && a.symmetric && c0 > r0;
     if (direct) {
         typename E::Fetched f[2];
         const bool in = r0 + lane < M;
@@ -118,9 +118,12 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
         for (uint32_t i = 0; i < 2; ++i)
             if (in && c0 + 16 * i < N) e.fetch(b, r0 + lane, c0 + 16 * i, f[i]);
         sums();
-        float y[32];
+        float copy[32], *y = v;                                 // the mirror needs the sums as they are
+        if constexpr (E::kMirror) {
+            y = copy;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) y[i] = v[i];
+            for (int i = 0; i < 32; ++i) y[i] = v[i];
+        }
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i)
             if (in && c0 + 16 * i < N) e.apply(b, r0 + lane, c0 + 16 * i, f[i], y + 16 * i, ToMemory());
@@ -133,7 +136,7 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
     for (uint32_t i = 0; i < 8; ++i)
         *reinterpret_cast<float4*>(piece + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
     __syncwarp();
-    if constexpr (E::kPadded) {                                 // mirror: column `lane` of the piece is part of a row of the transposed result
+    if constexpr (E::kMirror) {                                 // column `lane` of the piece is part of a row of the transposed result
         if (c0 + lane < N) {
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i) {
@@ -146,6 +149,7 @@ __device__ __forceinline__ void write_piece(const ProductArgs& a, const E& e, ui
                 e.apply(b, c0 + lane, r0 + 16 * i, f, y, ToMemory());
             }
         }
+    } else if constexpr (E::kPadded) {
     } else if (a.turned) {                                      // rows of the result are the piece's columns
         const uint32_t n = min(32u, N - c0);
         if (a.direct && r0 + 32 <= M && n > 4) {
@@ -299,7 +303,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                         if (++st == a.stages) { st = 0; phase ^= 1; }
                         ready = bar_test(&full[st], phase);          // the next stage's, beside this one's products
                         mma4_commit<CG>(acc, a0 + uniform(now * stage), b0 + uniform(now * stage), a_step, b_step, a.idesc, run > 0, &empty[now]);
-                        if (++run == (RUNS ? kRun : n) || k + 1 == n) {
+                        if (++run == (RUNS ? a.run : n) || k + 1 == n) {
                             commit_cg<CG>(&acc_full[w & 1]);
                             ++w;
                             run = 0;
@@ -322,13 +326,13 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             const uint32_t r0 = (t.i * CG + rank) * 128 + lanes, c0 = t.j * a.bn + half;
             auto write = [&](uint32_t c, float* v, const auto& sums) {
                 if (t.slot != kWhole) write_partial(a, t, r0, c0 + c, v, sums);
-                else if (a.bulk && r0 + 32 <= a.M && c0 + c + 32 <= a.N) write_bulk(a, e, t.b, r0, c0 + c, v, piece, sums);
+                else if (!E::kMirror && a.bulk && r0 + 32 <= a.M && c0 + c + 32 <= a.N) write_bulk(a, e, t.b, r0, c0 + c, v, piece, sums);
                 else write_piece(a, e, t.b, r0, c0 + c, v, piece, sums);
             };
             if (RUNS) {
                 float2 sums[4][16] = {};
                 const uint32_t n = t.k1 - t.k0;
-                for (uint32_t k = 0; k < n; k += kRun, ++w) {
+                for (uint32_t k = 0; k < n; k += a.run, ++w) {
                     ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
@@ -450,6 +454,119 @@ __global__ void __launch_bounds__(256) k_repack(const uint16_t* src, int64_t str
     *reinterpret_cast<uint4*>(dst + r * to + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// ---- up to four rows -------------------------------------------------------------------------------------------------------
+// No tensor cores: B (the weights) passes once, 16 bytes a lane, through fp32 multiply-adds with A's rows; bound by the memory's
+// latency and rate.  (1 x 1600 -> 6400 with bias and gelu: 10.0 us as columns of a tile.)
+constexpr int kRowThreads = 256;
+constexpr uint32_t kRowMax = 4, kRowCols = 64, kRowLoads = 8;
+struct RowsArgs {
+    const void *x, *w;
+    int64_t xs, ws;
+    uint32_t M, N, K, splits, per;              // per: of the summed dimension a block, where it is cut
+};
+
+template <typename T> __device__ __forceinline__ void fma8(const uint4& w, float x, float2* acc)
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = fma2(unpack2<T>(u[i]), make_float2(x, x), acc[i]);
+}
+
+// B's columns are contiguous: a block takes 64 of them, eight lanes a line of 128 bytes, 32 lines at once.  The blocks of a cluster
+// share the summed dimension; the first adds their sums in order.
+template <typename T, int M, typename E> __global__ void __launch_bounds__(kRowThreads) k_rows_wide(const __grid_constant__ RowsArgs a, const __grid_constant__ E e)
+{
+    __shared__ float part[32][M][kRowCols + 4], sums[8][M][kRowCols];
+    const uint32_t g = threadIdx.x & 7, line = threadIdx.x >> 3, rank = a.splits > 1 ? cluster_rank() : 0, first = blockIdx.x / a.splits * kRowCols;
+    const uint32_t n = first + g * 8, k0 = rank * a.per, k1 = min(a.K, k0 + a.per);
+    const T *w = (const T*)a.w + n, *x = (const T*)a.x;
+    float2 acc[M][4] = {};
+    if (n < a.N)
+        for (uint32_t k = k0 + line; k < k1; k += 32 * kRowLoads) {
+            uint4 q[kRowLoads];
+            float f[kRowLoads][M];
+#pragma unroll
+            for (uint32_t u = 0; u < kRowLoads; ++u) {
+                const uint32_t r = min(k + 32 * u, k1 - 1);
+                q[u] = __ldg(reinterpret_cast<const uint4*>(w + (int64_t)r * a.ws));
+#pragma unroll
+                for (int m = 0; m < M; ++m) f[u][m] = k + 32 * u < k1 && (uint32_t)m < a.M ? to_f32(x[m * a.xs + r]) : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kRowLoads; ++u)
+                if (k + 32 * u < k1)
+#pragma unroll
+                    for (int m = 0; m < M; ++m) fma8<T>(q[u], f[u][m], acc[m]);
+        }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(&part[line][m][g * 8 + 2 * i]) = acc[m][i];
+    __syncthreads();
+    if (a.splits > 1) cluster_sync();                           // the first block is there before anything is written to it
+    for (uint32_t i = threadIdx.x; i < M * kRowCols; i += kRowThreads) {
+        float t = 0.0f;
+#pragma unroll
+        for (int l = 0; l < 32; ++l) t += part[l][i / kRowCols][i % kRowCols];
+        if (a.splits > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(in_block(&sums[rank][i / kRowCols][i % kRowCols], 0)), "f"(t) : "memory");
+        else sums[0][i / kRowCols][i % kRowCols] = t;
+    }
+    if (a.splits > 1) cluster_sync();
+    else __syncthreads();
+    if (rank) return;
+    for (uint32_t i = threadIdx.x; i < a.M * kRowCols; i += kRowThreads) {
+        const uint32_t m = i / kRowCols, c = i % kRowCols;
+        if (first + c >= a.N) continue;
+        float t = sums[0][m][c];
+        for (uint32_t r = 1; r < a.splits; ++r) t += sums[r][m][c];
+        e.apply1(0, m, first + c, e.fetch1(0, m, first + c), t);
+    }
+}
+
+// The summed dimension is contiguous: a warp takes two of B's rows.
+template <typename T, int M, typename E> __global__ void __launch_bounds__(kRowThreads) k_rows_long(const __grid_constant__ RowsArgs a, const __grid_constant__ E e)
+{
+    const uint32_t lane = threadIdx.x & 31, n0 = (blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5)) * 2;
+    if (n0 >= a.N) return;
+    const T *w[2] = {(const T*)a.w + (int64_t)n0 * a.ws, (const T*)a.w + (int64_t)min(n0 + 1, a.N - 1) * a.ws}, *x = (const T*)a.x;
+    float2 acc[2][M] = {};
+    for (uint32_t k = lane * 8; k < a.K; k += 1024) {
+        uint4 q[2][4], f[M][4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t at = k + 256 * u;
+            const bool in = at < a.K;                           // K is a multiple of 8
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) q[j][u] = in ? __ldg(reinterpret_cast<const uint4*>(w[j] + at)) : zero;
+#pragma unroll
+            for (int m = 0; m < M; ++m) f[m][u] = in && (uint32_t)m < a.M ? __ldg(reinterpret_cast<const uint4*>(x + m * a.xs + at)) : zero;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t ww[4] = {q[j][u].x, q[j][u].y, q[j][u].z, q[j][u].w}, xx[4] = {f[m][u].x, f[m][u].y, f[m][u].z, f[m][u].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][m] = fma2(unpack2<T>(ww[i]), unpack2<T>(xx[i]), acc[j][m]);
+                }
+    }
+    float mine = 0.0f;
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float t = acc[j][m].x + acc[j][m].y;
+#pragma unroll
+            for (int s = 16; s; s >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, s);
+            if (lane == (uint32_t)(m * 2 + j)) mine = t;
+        }
+    const uint32_t m = lane / 2, n = n0 + (lane & 1);
+    if (m < a.M && n < a.N) e.apply1(0, m, n, e.fetch1(0, m, n), mine);
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------------
 struct ProductPlan {
     int cg;
@@ -467,12 +584,12 @@ static bool tma_reads(const Operand& o, uint32_t outer, uint32_t inner, uint32_t
     return batch <= 1 || o.each % 8 == 0;
 }
 
-static uint32_t count_tiles(bool symmetric, uint32_t tm, uint32_t bn, uint32_t mt, uint32_t nt)
+static uint64_t count_tiles(bool symmetric, uint32_t tm, uint32_t bn, uint32_t mt, uint32_t nt)
 {
-    if (!symmetric) return mt * nt;
+    if (!symmetric) return (uint64_t)mt * nt;
     uint64_t n = 0;
     for (uint32_t i = 0; i < mt; ++i) n += nt - (uint32_t)((uint64_t)i * tm / bn);
-    return (uint32_t)n;
+    return n;
 }
 
 static ProductPlan plan_product(const Product& p)
@@ -499,8 +616,9 @@ static ProductPlan plan_product(const Product& p)
     for (const auto& c : shapes) {
         if (r.turned ? (c.cg == 2 || (c.bn >= 2 * N && c.bn > 16)) : c.bn < 64) continue;
         if (r.turned && c.bn < N && c.bn < 128) continue;
-        const uint32_t tm = 128 * c.cg, mt = (uint32_t)(((uint64_t)M + tm - 1) / tm), nt = (N + c.bn - 1) / c.bn, tiles = count_tiles(p.symmetric, tm, c.bn, mt, nt);
-        const uint64_t slots = kSms / c.cg, all = (uint64_t)tiles * p.batch, last = all % slots;
+        const uint32_t tm = 128 * c.cg, mt = (uint32_t)(((uint64_t)M + tm - 1) / tm), nt = (N + c.bn - 1) / c.bn;
+        const uint64_t tiles = count_tiles(p.symmetric, tm, c.bn, mt, nt), slots = kSms / c.cg, all = tiles * p.batch, last = all % slots;
+        if (all >= 1ull << 30) continue;
         for (uint32_t parts = 1; parts <= 16 && parts <= r.steps; ++parts) {
             if (parts > 1 && last == 0) break;
             const uint32_t per = (r.steps + parts - 1) / parts;
@@ -514,7 +632,7 @@ static ProductPlan plan_product(const Product& p)
                 r.bn = c.bn;
                 r.mt = mt;
                 r.nt = nt;
-                r.tiles = tiles;
+                r.tiles = (uint32_t)tiles;
                 r.parts = parts;
                 r.per = per;
                 r.rest = parts > 1 ? (uint32_t)last : 0;
@@ -526,8 +644,53 @@ static ProductPlan plan_product(const Product& p)
     return r;
 }
 
+// Whether the kernels for up to four rows take it: B in whole 16-byte groups of one of its rows; where the summed dimension is the
+// contiguous one, in whole groups altogether, and A aligned like it.
+static bool rows_take(const Product& p)
+{
+    if (!p.few || p.M > kRowMax || p.a.mn || p.K == 0) return false;
+    if (p.b.mn) return p.N % 8 == 0 && tma_reads(p.b, p.K, p.N, 1);
+    return p.K % 8 == 0 && tma_reads(p.b, p.N, p.K, 1) && tma_reads(p.a, p.M, p.K, 1);
+}
+
+template <typename T, int M, typename E> static int launch_rows(const Product& p, const E& e, cudaStream_t s)
+{
+    RowsArgs a{p.a.p, p.b.p, p.a.stride, p.b.stride, p.M, p.N, p.K, 1, p.K};
+    if (!p.b.mn) {
+        k_rows_long<T, M, E><<<(p.N + 15) / 16, kRowThreads, 0, s>>>(a, e);
+        DBLP_LAUNCHED();
+        return DBLP_OK;
+    }
+    const uint32_t blocks = (p.N + kRowCols - 1) / kRowCols;
+    while (a.splits < 8 && blocks * a.splits < 2 * kSms && p.K / (a.splits * 2) >= 32 * kRowLoads / 2) a.splits *= 2;
+    a.per = (p.K + a.splits - 1) / a.splits;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks * a.splits);
+    cfg.blockDim = dim3(kRowThreads);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.splits > 1 ? 1 : 0;
+    const auto kernel = k_rows_wide<T, M, E>;
+    DBLP_NEXT(cudaLaunchKernelEx(&cfg, kernel, a, e));
+    return DBLP_OK;
+}
+template <typename E> static int product_rows(const Product& p, const E& e, cudaStream_t s)
+{
+    if (p.dtype == DBLP_BF16) {
+        if (p.M == 1) return launch_rows<__nv_bfloat16, 1>(p, e, s);
+        return p.M == 2 ? launch_rows<__nv_bfloat16, 2>(p, e, s) : launch_rows<__nv_bfloat16, 4>(p, e, s);
+    }
+    if (p.M == 1) return launch_rows<__half, 1>(p, e, s);
+    return p.M == 2 ? launch_rows<__half, 2>(p, e, s) : launch_rows<__half, 4>(p, e, s);
+}
+
 size_t product_space(const Product& p)
 {
+    if (rows_take(p)) return 0;
     const ProductPlan r = plan_product(p);
     return r.a_bytes + r.b_bytes + r.partial_bytes;
 }
@@ -617,7 +780,10 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
         DBLP_LAUNCHED();
         return DBLP_OK;
     }
+    if constexpr (E::kFewRows)
+        if (rows_take(p)) return product_rows(p, e, s);
     const ProductPlan r = plan_product(p);
+    DBLP_REQUIRE(r.cg, DBLP_ECAPACITY, "product: 2^31 tiles or more");
     DBLP_REQUIRE((uint64_t)r.tiles * p.batch + (uint64_t)r.rest * r.parts < 1ull << 31, DBLP_ECAPACITY, "product: 2^31 tiles or more");
     unsigned long long* timeouts = timeout_counter();
     DBLP_REQUIRE(timeouts, DBLP_ECUDA, "product: no device counter: %s", cudaGetErrorString(cudaGetLastError()));
@@ -655,6 +821,8 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
     a.nt = r.nt;
     a.steps = r.steps;
     a.term_steps = r.term_steps;
+    // Error of 8192 products of random signs: 9.1e-6 of the result in one run, 4.7e-7 in runs of 512, 2.4e-7 of 256; plain fp32 9.6e-7.
+    a.run = p.terms == 3 ? 4 : 8;
     a.whole = r.whole;
     a.rest = r.rest;
     a.parts = r.parts;
@@ -709,8 +877,10 @@ DBLP_PRODUCT(false, EpiGradX<__half>);
 DBLP_PRODUCT(false, EpiStore<__nv_bfloat16>);
 DBLP_PRODUCT(false, EpiStore<__half>);
 DBLP_PRODUCT(true, EpiStore<float>);
-DBLP_PRODUCT(false, EpiPoly);
-DBLP_PRODUCT(true, EpiPoly);
+DBLP_PRODUCT(false, EpiPoly<true>);
+DBLP_PRODUCT(true, EpiPoly<true>);
+DBLP_PRODUCT(false, EpiPoly<false>);
+DBLP_PRODUCT(true, EpiPoly<false>);
 DBLP_PRODUCT(false, EpiLast<__nv_bfloat16>);
 DBLP_PRODUCT(true, EpiLast<__half>);
 DBLP_PRODUCT(true, EpiLast<float>);

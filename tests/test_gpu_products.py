@@ -72,7 +72,7 @@ def expected(x, w, out_dtype, bias, residual, f):
     return y, (tol + U[out_dtype] * (y.abs() + tol) + TINY[out_dtype]), z, ez + U[x.dtype] * (z.abs() + ez) + TINY[x.dtype]
 
 
-SIZES = [(1, 1, 1), (1, 64, 128), (2, 1600, 6400), (3, 257, 129), (7, 33, 260), (8, 4096, 1000), (17, 100, 7), (31, 1601, 515), (64, 512, 1024),
+SIZES = [(1, 1, 1), (1, 64, 128), (2, 1600, 6400), (3, 257, 129), (4, 512, 1000), (1, 6400, 1600), (3, 40, 72), (4, 8, 8), (7, 33, 260), (8, 4096, 1000), (17, 100, 7), (31, 1601, 515), (64, 512, 1024),
          (65, 40, 129), (100, 1, 300), (127, 129, 1), (128, 64, 64), (129, 520, 260), (300, 72, 2050), (777, 1601, 499), (1100, 1000, 1530),
          (4100, 192, 768)]
 
