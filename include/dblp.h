@@ -579,9 +579,10 @@ int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp
  * The norm is summed in 64 bits.  X and A enter the products scaled by powers of two (1024 and 256) and rounded to f16; X itself is
  * kept in two f16 words (22 bits), so that what rounding adds is not amplified with the small singular values.  With
  * out_dtype BF16 each product is one of f16 operands: the result is off by about 2e-3 of its norm at most, as much as
- * its rounding.  With out_dtype F32 or F16 the products are of both words (three products each): about 2e-5.
+ * its rounding.  With out_dtype F32 or F16 the products are of both words (three products each): about 6e-6, what the iteration in fp32 has.
  * Coefficients must keep the entries of X below 63 and those of A and b A + c A A below 255 (singular values up to about 2 do), beyond
  * which they become infinite.  An x of zeros gives zeros.  NaN or infinity in a matrix spreads over that matrix alone.
+ * out may be x (the same place, strides and dtype).
  * ws: dblp_orthogonalize_workspace_bytes() bytes, 256-byte aligned, contents need not be preserved. */
 enum { DBLP_ORTHOGONALIZE_STEPS = 16 };
 typedef struct {

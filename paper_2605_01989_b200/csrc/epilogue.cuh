@@ -212,8 +212,9 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
     Rows<T> pre;
     const void* bias;
     int bias_dtype, act;
+    bool bias_whole;                                            // it allows 32-byte accesses (a view of a flat vector may not)
     static constexpr bool kPadded = false, kFewRows = true, kMirror = false;
-    bool sectors() const { return out.whole() && residual.whole() && pre.whole() && (uintptr_t)bias % 32 == 0; }
+    bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{pre.p, pre.stride, 0, 2}; }
     struct Fetched { Raw<O> residual; };
     __device__ __forceinline__ void fetch(uint32_t, uint32_t m, uint32_t n, Fetched& f) const
@@ -222,7 +223,10 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
     }
     template <typename S> __device__ __forceinline__ void apply(uint32_t, uint32_t m, uint32_t n, const Fetched& f, float* v, const S& to) const
     {
-        if (bias) {                                             // the same sixteen for all lanes
+        if (bias && !bias_whole) {                              // the same sixteen for all lanes
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += element(bias, bias_dtype, n + i);
+        } else if (bias) {
             if (bias_dtype == DBLP_F32) {
                 Raw<float> r;
                 r.load((const float*)bias + n);

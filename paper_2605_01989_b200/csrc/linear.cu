@@ -284,6 +284,7 @@ extern "C" int dblp_linear(const dblp_linear_t* l, const dblp_matrix_t* x, const
         if (pre) e.pre = rows_of<T>(pre->data, pre->row_stride, l->rows);
         e.bias = bias;
         e.bias_dtype = l->bias_dtype;
+        e.bias_whole = (uintptr_t)bias % 32 == 0;
         e.act = l->activation;
         return run_product<sizeof(O) == 4>(p, e, ws, false, (cudaStream_t)stream);
     };

@@ -139,6 +139,37 @@ def test_linear_strides_broadcasts_and_places(n, i, o):
     within(res, y, tol, "over the residual")
 
 
+@pytest.mark.parametrize("n,i,o", [(2, 64, 96), (50, 64, 96), (700, 64, 544)])
+@pytest.mark.parametrize("bias_dtype", [F32, BF16, F16])
+def test_bias_anywhere_in_a_flat_vector(n, i, o, bias_dtype):
+    x, w, flat = randn((n, i), BF16, 1), randn((i, o), BF16, 2, i ** -0.5), randn((o + 3,), bias_dtype, 3)
+    for at in (0, 1, 3):
+        out = linear(x, w, BF16, bias=flat[at:at + o], activation="silu")
+        y, tol, _, _ = expected(x, w, BF16, flat[at:at + o], None, "silu")
+        within(out, y, tol, at)
+
+
+def test_many_tiles_a_block_and_edges_of_them():
+    """More tiles than blocks: results by TMA, with rows and columns that end inside a piece, beside untouched neighbours."""
+    n, i, o = 4111, 72, 2600
+    x, w = randn((n, i), BF16, 1), randn((i, o), BF16, 2, i ** -0.5)
+    for odt in (BF16, F32):
+        buf, pre = torch.full((n + 1, o + 40), 9.0, dtype=odt, device=DEV), torch.full((n, o), 5.0, dtype=BF16, device=DEV)
+        res = randn((n, o), odt, 3)
+        linear(x, w, odt, out=buf[:n, :o], residual=res, pre=pre if odt == BF16 else None, activation="gelu")
+        y, tol, z, ez = expected(x, w, odt, None, res, "gelu")
+        within(buf[:n, :o], y, tol, "out")
+        assert (buf[n] == 9).all() and (buf[:, o:] == 9).all()
+        if odt == BF16:
+            within(pre, z, ez, "pre")
+    dy, dw = randn((n, o), BF16, 4), torch.empty((i, o), device=DEV)
+    dx, keep = randn((n, i), BF16, 5), randn((n, i), BF16, 6)
+    dblp.dblp_linear_grad(dy, x, w, dx=dx, dw=dw, ws=space(dblp.dblp_linear_workspace_bytes(x, w, dy)[1]), residual=keep)
+    want, mass = dy.double() @ w.double().t() + keep.double(), dy.double().abs() @ w.double().abs().t() + keep.double().abs()
+    tol = (o + 2) * 2.0 ** -23 * mass
+    within(dx, want, tol + U[BF16] * (want.abs() + tol), "dx")
+
+
 def test_rows_in_reverse():
     """Negative row strides, which the header allows (a tensor cannot have them: raw addresses)."""
     import ctypes as C
