@@ -250,15 +250,16 @@ template <typename T, bool INTER, bool GRAD> __global__ void __launch_bounds__(k
     }
 }
 
-// The weights' gradients from the blocks' sums: 8 threads a column take every eighth block, then add up in order.
+// The weights' gradients from the blocks' sums: 32 threads a column take every 32nd block, all their loads at once, then add up in
+// order.  (8 threads, a load after the other: 11 us of 49 for 296 blocks.)
 struct RotJoin {
     const float* partial[2];
     void* dw[2];
     uint32_t blocks[2], D, dtype, accumulate;
 };
-__global__ void __launch_bounds__(256) k_rotate_join(RotJoin j)
+__global__ void __launch_bounds__(1024) k_rotate_join(RotJoin j)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[32][32];
     const int side = blockIdx.y;
     const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float t = 0.0f;
@@ -266,12 +267,13 @@ __global__ void __launch_bounds__(256) k_rotate_join(RotJoin j)
     after_start();
     if (!j.dw[side]) return;
     if (c < j.D)
-        for (uint32_t b = y; b < j.blocks[side]; b += 8) t += j.partial[side][(size_t)b * j.D + c];
+#pragma unroll 16
+        for (uint32_t b = y; b < j.blocks[side]; b += 32) t += j.partial[side][(size_t)b * j.D + c];
     part[y][x] = t;
     __syncthreads();
     if (y || c >= j.D) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t += part[i][x];
+    for (int i = 1; i < 32; ++i) t += part[i][x];
     if (j.dtype == DBLP_F32) {
         float* p = (float*)j.dw[side] + c;
         *p = j.accumulate ? *p + t : t;
@@ -519,6 +521,6 @@ extern "C" int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_hea
     if (!join) return DBLP_OK;
     RotJoin j{{partial[0], partial[1]}, {dq_weight, dk_weight}, {r.side[0].blocks, r.side[1].blocks}, a->head_dim, (uint32_t)a->weight_dtype,
               a->flags & (uint32_t)DBLP_ACCUMULATE};
-    DBLP_NEXT(launch_next(k_rotate_join, dim3((a->head_dim + 31) / 32, 2), 256, 0, (cudaStream_t)stream, j));
+    DBLP_NEXT(launch_next(k_rotate_join, dim3((a->head_dim + 31) / 32, 2), 1024, 0, (cudaStream_t)stream, j));
     return DBLP_OK;
 }

@@ -78,6 +78,7 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
     const uint64_t groups = (uint64_t)a.rows * per_row;
     const double norm = sqrt(block_sum(threadIdx.x < a.parts ? a.squares[(size_t)b * a.parts + threadIdx.x] : 0.0, part)) + (double)a.eps;
     const double f = norm == 0.0 ? 0.0 : kScaleX / norm;
+    const bool plain = f > 1e-30 && f < 1e30;        // an fp32 factor and fp32 products (2^-24) are enough for 22 bits
     Source x = a.x;
     x.p = (const char*)x.p + b * a.each * (x.dtype == DBLP_F32 ? 4 : 2);
     for (uint64_t g = (uint64_t)blockIdx.x * kUpdThreads + threadIdx.x; g < groups; g += (uint64_t)gridDim.x * kUpdThreads) {
@@ -85,8 +86,13 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
         float v[16];
         load8(x, r, c, min(8u, left), v);
         load8(x, r, c + 8, left > 8 ? left - 8 : 0, v + 8);
+        if (plain) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = (float)((double)v[i] * f);
+            for (int i = 0; i < 16; ++i) v[i] *= (float)f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = (float)((double)v[i] * f);
+        }
         a.out.store(b, r, c, v, ToMemory());
     }
 }
