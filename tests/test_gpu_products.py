@@ -170,6 +170,22 @@ def test_many_tiles_a_block_and_edges_of_them():
     within(dx, want, tol + U[BF16] * (want.abs() + tol), "dx")
 
 
+def test_elements_beyond_32_bits():
+    n, i, o = 43000, 16, 50264
+    x, w = randn((n, i), BF16, 1), randn((i, o), BF16, 2, i ** -0.5)
+    out = torch.empty((n, o), dtype=BF16, device=DEV)
+    assert out.numel() > 1 << 31
+    linear(x, w, BF16, out=out, activation="relu")
+    for rows in (slice(0, 40), slice(n // 2, n // 2 + 40), slice(n - 40, n)):
+        y, tol, _, _ = expected(x[rows], w, BF16, None, None, "relu")
+        within(out[rows], y, tol, rows)
+    dx = torch.empty((n, i), dtype=BF16, device=DEV)
+    dblp.dblp_linear_grad(out, x, w, dx=dx, ws=space(dblp.dblp_linear_workspace_bytes(x, w, out)[1]))
+    rows = slice(n - 40, n)
+    want, mass = out[rows].double() @ w.double().t(), out[rows].double().abs() @ w.double().abs().t()
+    within(dx[rows], want, (o + 2) * 2.0 ** -23 * mass + U[BF16] * (want.abs() + mass * 2.0 ** -8), "dx")
+
+
 def test_rows_in_reverse():
     """Negative row strides, which the header allows (a tensor cannot have them: raw addresses)."""
     import ctypes as C
