@@ -659,28 +659,35 @@ def dblp_attention_grad(q, k, v, out, dout, lse, dq, dk, dv, ws, causal=False, s
 
 
 def _norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps, flags):
-    """(the call's description, q's shape, k's shape or None)"""
-    _require(q.dim() == 4 and (k is None or k.dim() == 4), "q and k: [batch, tokens, heads, head_dim]")
-    qs, ks = q.shape, None if k is None else k.shape
+    """(the call's description, q's shape, k's shape or None); plain comparisons, since a call of a few tokens waits for them"""
+    qs, ks, dt = q.shape, None if k is None else k.shape, q.dtype
+    if len(qs) != 4 or (ks is not None and len(ks) != 4):
+        raise ValueError("q and k: [batch, tokens, heads, head_dim]")
     B, T, Hq, D = qs
-    if k is not None:
-        _require(ks[0] == B and ks[1] == T and ks[3] == D and k.dtype == q.dtype, "q and k: one batch, length, head_dim and dtype")
+    Hk = 0
+    if ks is not None:
+        if ks[0] != B or ks[1] != T or ks[3] != D or k.dtype is not dt:
+            raise ValueError("q and k: one batch, length, head_dim and dtype")
+        Hk = ks[2]
     w = q_weight if q_weight is not None else k_weight
-    for t in (q_weight, k_weight):
-        if t is not None and not (t.dtype == w.dtype and t.shape == (D,) and t.is_contiguous()):
-            raise ValueError("weights: contiguous, one per column of a head, of one dtype")
-    if max(B, T, Hq, D, 0 if ks is None else ks[2]) >= 1 << 32:
+    if w is not None:
+        wt = w.dtype
+        for t in (q_weight, k_weight):
+            if t is not None and (t.dtype is not wt or t.dim() != 1 or t.shape[0] != D or not t.is_contiguous()):
+                raise ValueError("weights: contiguous, one per column of a head, of one dtype")
+    if B >= 1 << 32 or T >= 1 << 32 or Hq >= 1 << 32 or D >= 1 << 32 or Hk >= 1 << 32:
         raise ValueError("an extent of q or k does not fit in 32 bits")
     n = 0 if freqs is None else freqs.numel()
     pp = fp = None
     stride = 0
     if n:
-        _require(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(), "freqs: 1-D, contiguous, float64")
-        _require(positions is not None and positions.dtype == torch.int32 and positions.shape == (B, T)
-                 and (T <= 1 or positions.stride(1) == 1), "positions: int32 [batch, tokens], the tokens of a sequence contiguous")
+        if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+            raise ValueError("freqs: 1-D, contiguous, float64")
+        if positions is None or positions.dtype is not torch.int32 or positions.shape != (B, T) or (T > 1 and positions.stride(1) != 1):
+            raise ValueError("positions: int32 [batch, tokens], the tokens of a sequence contiguous")
         pp, fp, stride = positions.data_ptr(), freqs.data_ptr(), positions.stride(0)
-    return dblp_norm_rotate_t(B, T, Hq, 0 if ks is None else ks[2], D, _u32(2 * n, "rotary_dim"), _dtype(q),
-                              DBLP_F32 if w is None else _dtype(w), flags, eps, pp, stride, fp), qs, ks
+    return dblp_norm_rotate_t(B, T, Hq, Hk, D, _u32(2 * n, "rotary_dim"), _dtype(q), DBLP_F32 if w is None else _dtype(w), flags, eps, pp,
+                              stride, fp), qs, ks
 
 
 def _address(t):
@@ -751,15 +758,18 @@ def _activation(name):
 
 
 def _linear(x, w, out_dtype, bias, activation, flags):
-    _require(x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[0], "x and w: rows x in, in x out")
-    n, i, o = x.shape[0], x.shape[1], w.shape[1]
-    _require(w.dtype == x.dtype, "x and w: one dtype")
-    if max(n, i, o) >= 1 << 32:
+    xs, ws, dt = x.shape, w.shape, x.dtype
+    if len(xs) != 2 or len(ws) != 2 or xs[1] != ws[0]:
+        raise ValueError("x and w: rows x in, in x out")
+    (n, i), o = xs, ws[1]
+    if w.dtype is not dt:
+        raise ValueError("x and w: one dtype")
+    if n >= 1 << 32 or i >= 1 << 32 or o >= 1 << 32:
         raise ValueError("an extent does not fit in 32 bits")
-    if bias is not None and not (bias.shape == (o,) and bias.is_contiguous()):
+    if bias is not None and (bias.dim() != 1 or bias.shape[0] != o or not bias.is_contiguous()):
         raise ValueError("bias and its gradient: contiguous, one per column of w")
-    dt = _dtype(x)
-    return dblp_linear_t(n, i, o, dt, dt if out_dtype is None else _DTYPES.get(out_dtype, -1), DBLP_F32 if bias is None else _dtype(bias),
+    code = _dtype(x)
+    return dblp_linear_t(n, i, o, code, code if out_dtype is None else _DTYPES.get(out_dtype, -1), DBLP_F32 if bias is None else _dtype(bias),
                          _activation(activation), flags), n, i, o
 
 

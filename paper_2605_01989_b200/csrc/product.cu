@@ -19,7 +19,7 @@
 //              multiprocessor from L2, about what it gives: five stages instead of six cost 10 %, four 30 %); tiles of 128 columns by
 //              the 340 cycles that a stage takes to issue; with bias, gelu and a second result by the writing warps: 22 900
 //              cycles a tile of 1600 before edges left their code, 12 800 of products.
-//   measured   8192 x 8192 x 8192 bf16 691 to 760 us (1.45 to 1.59 PFLOP/s; the library's 649 to 690 on the same boxes), 8192 x 1600 -> 6400
+//   measured   8192 x 8192 x 8192 bf16 691 to 760 us (1.45 to 1.59 PFLOP/s; the library's 649 to 690 on the same machines), 8192 x 1600 -> 6400
 //              110 us (1.52), with bias, gelu and pre-activation 135 us (1.25).
 #include "product.cuh"
 #include "tc.cuh"
