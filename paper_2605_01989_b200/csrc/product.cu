@@ -105,6 +105,13 @@ template <typename F, typename A> __device__ __forceinline__ void one_by_one(uin
     }
 }
 
+// Where the run of stages that begins at stage k ends: the tensor cores add up a run by themselves.  The second and third terms are
+// smaller than the first by 2^-11, and so is what truncation takes from them: they are one run.
+__device__ __forceinline__ uint32_t run_end(const ProductArgs& a, uint32_t k, uint32_t k1)
+{
+    return min(k < a.term_steps ? min(k + a.run, a.term_steps) : a.steps, k1);
+}
+
 // 32 x 32 sums, a row a lane, from (r0, c0) on.  Whole pieces of matrices that allow 32-byte accesses are written from the lane that has
 // the row; what the epilogue reads is fetched before `sums` brings v.  The others, and results written by columns, go through
 // 4 KB of shared memory, where the 16-byte chunk c of row r is at place c ^ (r % 8): no bank conflicts in any direction.  Edges and
@@ -297,25 +304,26 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
                 const uint32_t a_step = a.a_mn ? 2048 / 16 : 32 / 16, b_step = a.b_mn ? 2048 / 16 : 32 / 16, stage = a.stage_bytes / 16;
                 for (uint32_t x = first_item; x < a.items && ok; x += item_stride) {
                     const ProdItem t = prod_item(a, x);
-                    const uint32_t n = uniform(t.k1 - t.k0);
-                    uint32_t acc = 0;
-                    for (uint32_t k = 0, run = 0; k < n; ++k) {
-                        if (run == 0) {                             // a run of stages whose sums are taken together
+                    const uint32_t k0 = uniform(t.k0), k1 = uniform(t.k1);
+                    uint32_t acc = 0, end = k0;
+                    for (uint32_t k = k0; k < k1; ++k) {
+                        const bool start = k == end;
+                        if (start) {
                             if (w >= 2) ok = warp_wait(&acc_free[w & 1], ((w >> 1) - 1) & 1, g);
                             if (!ok) break;
                             acc = tmem + (w & 1) * a.acc_cols;
+                            end = RUNS ? run_end(a, k, k1) : k1;
                         }
                         if (!__all_sync(0xFFFFFFFFu, ready)) ok = warp_wait(&full[st], phase, g);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t now = st;
                         if (++st == a.stages) { st = 0; phase ^= 1; }
-                        ready = bar_test(&full[st], phase);          // the next stage's, beside this one's products
-                        mma4_commit<CG>(acc, a0 + uniform(now * stage), b0 + uniform(now * stage), a_step, b_step, a.idesc, run > 0, &empty[now]);
-                        if (++run == (RUNS ? a.run : n) || k + 1 == n) {
+                        ready = bar_test(&full[st], phase);         // the next stage's, beside this one's products
+                        mma4_commit<CG>(acc, a0 + uniform(now * stage), b0 + uniform(now * stage), a_step, b_step, a.idesc, !start, &empty[now]);
+                        if (k + 1 == end) {
                             commit_cg<CG>(&acc_full[w & 1]);
                             ++w;
-                            run = 0;
                         }
                     }
                 }
@@ -340,8 +348,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             };
             if (RUNS) {
                 float2 sums[4][16] = {};
-                const uint32_t n = t.k1 - t.k0;
-                for (uint32_t k = 0; k < n; k += a.run, ++w) {
+                for (uint32_t k = t.k0; k < t.k1; k = run_end(a, k, t.k1), ++w) {
                     ok = warp_wait(&acc_full[w & 1], (w >> 1) & 1, g);
                     if (!ok) break;
                     tc_fence_after();
