@@ -367,7 +367,7 @@ static RotArgs rot_args(const dblp_norm_rotate_t* a)
 {
     RotArgs r{};
     r.tokens = a->tokens;
-    r.by_tokens = FastDiv(a->tokens);
+    r.by_tokens = FastDiv(a->tokens ? a->tokens : 1);           // without tokens only the weights' gradients are written
     r.D = a->head_dim;
     r.R = a->rotary_dim;
     r.L = lanes_of(a->head_dim);
