@@ -206,14 +206,16 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
 // padding behind a row; kFewRows: A may have few; kMirror: the result
-// may equal its transpose and be computed by half); fetch1 and apply1 one.  What was fetched is in f.  sectors(): all matrices allow 32-byte accesses.
+// may equal its transpose and be computed by half; kNothing: the sum may have no terms); fetch1 and apply1 one.  What was fetched is in f.
+// In: the operands' type, where A may have few rows.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
     const void* bias;
     int bias_dtype, act;
     bool bias_whole;                                            // it allows 32-byte accesses (a view of a flat vector may not)
-    static constexpr bool kPadded = false, kFewRows = true, kMirror = false;
+    using In = T;
+    static constexpr bool kPadded = false, kFewRows = true, kMirror = false, kNothing = true;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{pre.p, pre.stride, 0, 2}; }
     struct Fetched { Raw<O> residual; };
@@ -262,7 +264,8 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
 template <typename T> struct EpiGradX {                         // dx = (v + residual) act'(pre)
     Rows<T> out, residual, pre;
     int act;
-    static constexpr bool kPadded = false, kFewRows = true, kMirror = false;
+    using In = T;
+    static constexpr bool kPadded = false, kFewRows = true, kMirror = false, kNothing = true;
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, 2} : Output{}; }
     struct Fetched { Raw<T> residual, pre; };
@@ -304,7 +307,7 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
 template <typename O> struct EpiStore {                         // out = v [+ out]
     Rows<O> out;
     bool accumulate;
-    static constexpr bool kPadded = false, kFewRows = false, kMirror = false;
+    static constexpr bool kPadded = false, kFewRows = false, kMirror = false, kNothing = true;
     bool sectors() const { return out.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{}; }
     struct Fetched { Raw<O> out; };
@@ -375,7 +378,7 @@ struct Words {
 template <bool SYMMETRIC> struct EpiPoly {                      // out = alpha v [+ beta add], both in words
     Words out, add;
     float alpha, beta;
-    static constexpr bool kPadded = true, kFewRows = false, kMirror = SYMMETRIC;
+    static constexpr bool kPadded = true, kFewRows = false, kMirror = SYMMETRIC, kNothing = false;
     bool sectors() const { return true; }
     Output output(int k) const { return Output{k ? out.lo : out.hi, out.stride, out.each, 2}; }
     using Fetched = Words::Fetched;
@@ -393,7 +396,7 @@ template <typename O> struct EpiLast {                          // the caller's 
     Words add;
     float alpha, beta;
     bool aligned;                                               // of all products of the batch
-    static constexpr bool kPadded = false, kFewRows = false, kMirror = false;
+    static constexpr bool kPadded = false, kFewRows = false, kMirror = false, kNothing = false;
     bool sectors() const { return aligned; }
     Output output(int k) const { return k ? Output{out.p, out.stride, each, (int)sizeof(O)} : Output{}; }
     using Fetched = Words::Fetched;

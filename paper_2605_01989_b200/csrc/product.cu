@@ -696,12 +696,9 @@ template <typename T, int M, typename E> static int launch_rows(const Product& p
 }
 template <typename E> static int product_rows(const Product& p, const E& e, cudaStream_t s)
 {
-    if (p.dtype == DBLP_BF16) {
-        if (p.M == 1) return launch_rows<__nv_bfloat16, 1>(p, e, s);
-        return p.M == 2 ? launch_rows<__nv_bfloat16, 2>(p, e, s) : launch_rows<__nv_bfloat16, 4>(p, e, s);
-    }
-    if (p.M == 1) return launch_rows<__half, 1>(p, e, s);
-    return p.M == 2 ? launch_rows<__half, 2>(p, e, s) : launch_rows<__half, 4>(p, e, s);
+    using T = typename E::In;
+    if (p.M == 1) return launch_rows<T, 1>(p, e, s);
+    return p.M == 2 ? launch_rows<T, 2>(p, e, s) : launch_rows<T, 4>(p, e, s);
 }
 
 size_t product_space(const Product& p)
@@ -789,7 +786,7 @@ static int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, u
 
 template <bool RUNS, typename E> int run_product(const Product& p, const E& e, void* ws, bool chained, cudaStream_t s)
 {
-    if constexpr (!E::kPadded) if (p.K == 0) {
+    if constexpr (E::kNothing) if (p.K == 0) {
         const uint64_t blocks = ((uint64_t)p.M * p.N + 255) / 256;
         DBLP_REQUIRE(blocks < 1ull << 31, DBLP_ECAPACITY, "product: 2^39 elements or more");
         k_product_none<E><<<(unsigned)blocks, 256, 0, s>>>(e, p.M, p.N);
