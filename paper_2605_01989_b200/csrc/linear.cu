@@ -1,4 +1,4 @@
-// dblp_linear, dblp_linear_grad: argument checks, the sums of dbias, and the products they are made of (product.cu).
+// dblp_linear, dblp_linear_grad: argument checks, the sums of dbias, and the products they are made of (product_kernels.cuh).
 #include <math.h>
 
 #include "product.cuh"

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "epilogue.cuh"
+#include "product_plan.h"
 
 namespace dblp {
 
@@ -37,27 +38,14 @@ __device__ __forceinline__ void load8(const Source& r, uint32_t m, uint32_t n, u
     else go(__half());
 }
 
-// A 16-bit operand: its rows (m of A, n of B) and the summed dimension, one of which is contiguous.
-struct Operand {
-    const void* p;
-    const void* lo;             // second word of each element (terms = 3), or null
-    int64_t stride;             // of the other dimension, in elements
-    int64_t each;               // from one product of a batch to the next
-    bool mn;                    // the rows are contiguous, not the summed dimension
-};
-
-struct Product {
-    Operand a, b;
-    uint32_t M, N, K, batch;
-    int dtype;                  // of both operands
-    int terms;                  // 1, or 3: hi hi + hi lo + lo hi
-    bool few;                   // few rows (M) may be computed as columns
-    bool symmetric;             // M = N and the result equals its transpose: computed once, written twice
-};
-
 size_t product_space(const Product& p);          // bytes of workspace
 // chained: the kernels before it on the stream belong to the same call and let this one be set up while they run
 // RUNS: the result is wanted to fp32's precision (the tensor cores' own sums truncate).
 template <bool RUNS, typename E> int run_product(const Product& p, const E& epilogue, void* ws, bool chained, cudaStream_t s);
+
+// parts of it that are the same for every epilogue
+int make_map(CUtensorMap* map, const void* data, int64_t stride, const Operand& o, uint32_t rows, uint32_t K, uint32_t batch, uint32_t box, int dtype);
+int make_store_map(CUtensorMap* map, const Output& o, const Product& p);
+int repack(const Operand& o, void* to, uint32_t stride, uint32_t outer, uint32_t inner, cudaStream_t s);
 
 }  // namespace dblp

@@ -6,10 +6,9 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "device.h"
 
 namespace dblp {
-
-constexpr unsigned kSms = 148;                // streaming multiprocessors of the device this library is built for
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
