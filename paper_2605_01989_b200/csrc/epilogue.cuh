@@ -3,6 +3,8 @@
 // element a lane.
 #pragma once
 
+#include <type_traits>
+
 #include "tc.cuh"
 
 namespace dblp {
@@ -203,11 +205,17 @@ template <int N> __device__ __forceinline__ void activate_grad(int act, const fl
     }
 }
 
+// ---- precision of the sums ------------------------------------------------------------------------------------------------
+// The tensor cores' own sums truncate: sums of one sign lose up to 6e-9 of themselves a term (f16; 64 Ki terms: 4e-4).  Where that
+// passes an eighth of half a step of the result's type they are taken out every 512 terms and added in fp32.
+constexpr uint32_t kAnyTerms = 0xFFFFFFFFu;
+template <typename O> constexpr uint32_t run_terms() { return sizeof(O) == 4 ? 0 : (std::is_same<O, __half>::value ? 8192 : 65536); }
+
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // Of the sums of row m, column n of product b: fetch and apply take columns n .. n + 15, all of them inside (kPadded: or in the
 // padding behind a row; kFewRows: A may have few; kMirror: the result
 // may equal its transpose and be computed by half; kNothing: the sum may have no terms); fetch1 and apply1 one.  What was fetched is in f.
-// In: the operands' type, where A may have few rows.  sectors(): all matrices allow 32-byte accesses.
+// In: the operands' type, where A may have few rows.  kTerms: how many terms the tensor cores may add up by themselves.  sectors(): all matrices allow 32-byte accesses.
 template <typename T, typename O> struct EpiLinear {            // out = act(z) + residual, pre = z = v + bias
     Rows<O> out, residual;
     Rows<T> pre;
@@ -216,6 +224,7 @@ template <typename T, typename O> struct EpiLinear {            // out = act(z) 
     bool bias_whole;                                            // it allows 32-byte accesses (a view of a flat vector may not)
     using In = T;
     static constexpr bool kPadded = false, kFewRows = true, kMirror = false, kNothing = true;
+    static constexpr uint32_t kTerms = run_terms<O>();
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{pre.p, pre.stride, 0, 2}; }
     struct Fetched { Raw<O> residual; };
@@ -266,6 +275,7 @@ template <typename T> struct EpiGradX {                         // dx = (v + res
     int act;
     using In = T;
     static constexpr bool kPadded = false, kFewRows = true, kMirror = false, kNothing = true;
+    static constexpr uint32_t kTerms = run_terms<T>();
     bool sectors() const { return out.whole() && residual.whole() && pre.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, 2} : Output{}; }
     struct Fetched { Raw<T> residual, pre; };
@@ -308,6 +318,7 @@ template <typename O> struct EpiStore {                         // out = v [+ ou
     Rows<O> out;
     bool accumulate;
     static constexpr bool kPadded = false, kFewRows = false, kMirror = false, kNothing = true;
+    static constexpr uint32_t kTerms = run_terms<O>();
     bool sectors() const { return out.whole(); }
     Output output(int k) const { return k ? Output{out.p, out.stride, 0, (int)sizeof(O)} : Output{}; }
     struct Fetched { Raw<O> out; };
@@ -379,6 +390,7 @@ template <bool SYMMETRIC> struct EpiPoly {                      // out = alpha v
     Words out, add;
     float alpha, beta;
     static constexpr bool kPadded = true, kFewRows = false, kMirror = SYMMETRIC, kNothing = false;
+    static constexpr uint32_t kTerms = run_terms<__half>();
     bool sectors() const { return true; }
     Output output(int k) const { return Output{k ? out.lo : out.hi, out.stride, out.each, 2}; }
     using Fetched = Words::Fetched;
@@ -397,6 +409,7 @@ template <typename O> struct EpiLast {                          // the caller's 
     float alpha, beta;
     bool aligned;                                               // of all products of the batch
     static constexpr bool kPadded = false, kFewRows = false, kMirror = false, kNothing = false;
+    static constexpr uint32_t kTerms = std::is_same<O, __nv_bfloat16>::value ? kAnyTerms : run_terms<O>();     // 32768 at most
     bool sectors() const { return aligned; }
     Output output(int k) const { return k ? Output{out.p, out.stride, each, (int)sizeof(O)} : Output{}; }
     using Fetched = Words::Fetched;

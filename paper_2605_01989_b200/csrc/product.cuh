@@ -40,7 +40,7 @@ __device__ __forceinline__ void load8(const Source& r, uint32_t m, uint32_t n, u
 
 size_t product_space(const Product& p);          // bytes of workspace
 // chained: the kernels before it on the stream belong to the same call and let this one be set up while they run
-// RUNS: the result is wanted to fp32's precision (the tensor cores' own sums truncate).
+// RUNS: the result is wanted to fp32's precision (the tensor cores' own sums truncate); without it long sums alone are taken in runs.
 template <bool RUNS, typename E> int run_product(const Product& p, const E& epilogue, void* ws, bool chained, cudaStream_t s);
 
 // parts of it that are the same for every epilogue

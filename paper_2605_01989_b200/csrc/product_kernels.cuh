@@ -13,8 +13,8 @@
 //              computed (as columns of the tile).
 //   parts      tiles of the last, incomplete round are cut along the summed dimension; the parts' sums are added in order by a
 //              second kernel with the same epilogue.
-//   fp32       the tensor cores' sums truncate; where the result is fp32 they are taken out every 512 (three-term products: 256) and
-//              added up in registers.
+//   fp32       the tensor cores' sums truncate; where the result is fp32, and where a sum is long, they are taken out every 512
+//              (three-term products: 256) and added up in registers.
 //   bound      256 x 256 tiles by the tensor pipe under the power cap, like the library's product (a pair needs 64 bytes a cycle and
 //              multiprocessor from L2, about what it gives: five stages instead of six cost 10 %, four 30 %); tiles of 128 columns by
 //              the 340 cycles that a stage takes to issue; with bias, gelu and a second result by the writing warps: 22 900
@@ -724,7 +724,15 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
         }
     }
     a.partial = (float*)at;
-    if (int rc = r.cg == 2 ? launch_product<2, RUNS>(a, e, chained, s) : launch_product<1, RUNS>(a, e, chained, s)) return rc;
+    auto launch = [&](auto runs) -> int {
+        constexpr bool R = decltype(runs)::value;
+        return r.cg == 2 ? launch_product<2, R>(a, e, chained, s) : launch_product<1, R>(a, e, chained, s);
+    };
+    int rc = 0;
+    if constexpr (RUNS) rc = launch(std::true_type());
+    else if constexpr (E::kTerms == kAnyTerms) rc = launch(std::false_type());
+    else rc = (uint64_t)r.longest * kStep > E::kTerms ? launch(std::true_type()) : launch(std::false_type());
+    if (rc) return rc;
     if (r.rest == 0) return DBLP_OK;
     const uint64_t pieces = (uint64_t)r.rest * (a.tm / 32) * ((r.bn + 31) / 32);
     DBLP_NEXT(launch_next(k_product_join<E>, dim3((unsigned)pieces), 32 * kJoinWarps, 0, s, a, e));

@@ -37,6 +37,7 @@ struct ProductPlan {
     uint32_t a_to, b_to;                                        // rows of the copies
     size_t a_bytes, b_bytes, partial_bytes;                     // in workspace
     uint32_t items;                                             // whole tiles and parts
+    uint32_t longest;                                           // stages of the longest item
     bool several;                                               // blocks have several items: results may go by TMA
 };
 
@@ -104,6 +105,7 @@ inline ProductPlan plan_product(const Product& p)
         }
     }
     r.items = r.whole + r.rest * r.parts;
+    r.longest = r.whole ? r.steps : r.per;
     // For one tile a block TMA's latency (1.5 us) is longer than what it saves.
     r.several = r.cg && !r.turned && !p.symmetric && r.items > kSms / r.cg;
     r.partial_bytes = padded((size_t)r.rest * r.parts * 128 * r.cg * r.bn * 4);
