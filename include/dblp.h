@@ -552,13 +552,15 @@ typedef struct {
 
 /* dblp_linear: z = x w + bias, out = act(z) + residual; pre = z, for the backward pass.  x, residual, pre, out: rows; w: one
  * of its two strides is 1 (weights held as [out, in] are the transposed view).  bias: contiguous.  bias, residual, pre:
- * NULL = none.  out may be the residual.  The product's operands are 16-bit, everything after that is fp32 and rounded
+ * NULL = none.  out may be the residual (the same place and stride); apart from that out and pre lie over nothing else that is passed:
+ * an in-place step x += x w needs a second place.  The product's operands are 16-bit, everything after that is fp32 and rounded
  * once.  relu: max(z, 0), NaN stays; gelu: z Phi(z); gelu_tanh: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))); silu:
  * z / (1 + exp(-z)).
  * dblp_linear_grad: dx = (dy w^T + residual) * act'(pre), dw = x^T dy, dbias = sum of dy's rows.  `pre` belongs to the
  * layer BEFORE: where x = act(pre) was that layer's output, dx is the gradient of its pre-activation, ready to be its dy;
  * without an activation pre is NULL.  residual (of dx, NULL = none): the gradient that reaches x on another way.  relu' is
- * 0 at 0 and NaN at NaN.  dx, dw, dbias: NULL = not wanted; dx may be the residual or pre.  dw: one of its strides is 1.
+ * 0 at 0 and NaN at NaN.  dx, dw, dbias: NULL = not wanted; dx may be the residual or pre (the same place and stride)
+ * or lie over x, which is read before; no other result lies over an operand or another result.  dw: one of its strides is 1.
  * Every sum over the rows or columns is fp32, in an order that the shapes, types and alignments fix.
  * ws: dblp_linear_workspace_bytes() bytes for the same x, w and dy (NULL: forward only), 256-byte aligned, contents need not
  * be preserved.  It holds copies of operands whose data or strides are not multiples of 16 bytes, and partial sums where

@@ -170,6 +170,51 @@ static int check_space(const char* who, const void* ws, size_t ws_bytes, size_t 
     return DBLP_OK;
 }
 
+// Where a matrix (or a vector, a matrix of one row) lies: `lines` pieces of `bytes` bytes, `step` bytes apart.
+struct Extent {
+    intptr_t at;
+    int64_t lines, bytes;
+    __int128 step;
+};
+static Extent extent_of(const void* p, int64_t stride, uint64_t lines, uint64_t length, int dtype)
+{
+    const int64_t es = element_bytes(dtype);
+    Extent e{(intptr_t)p, lines > 1 && stride != 0 ? (int64_t)lines : 1, (int64_t)length * es, (__int128)stride * es};
+    if (e.lines > 1 && e.step < 0) {                            // from its lowest line on
+        e.at += (intptr_t)(e.step * (e.lines - 1));
+        e.step = -e.step;
+    }
+    return e;
+}
+static Extent extent_of(const dblp_matrix_t* m, uint32_t rows, uint32_t cols, int dtype)
+{
+    return is_by_rows(m, cols) || cols == 1 ? extent_of(m->data, m->row_stride, rows, cols, dtype) : extent_of(m->data, m->col_stride, cols, rows, dtype);
+}
+// Whether two of them certainly share a byte.  With one step between lines, or a single line on one side, this is exact; lines of
+// different steps that start apart are taken to lie between one another.
+static bool meet(const Extent& a, const Extent& b)
+{
+    if (a.at == b.at) return true;
+    const __int128 away = (__int128)b.at - a.at, step = a.lines > 1 ? a.step : (b.lines > 1 ? b.step : 1);
+    if (a.lines > 1 && b.lines > 1 && a.step != b.step) return false;
+    // line j of b and line i of a, k = j - i: they share a byte where -b.bytes < away + k step < a.bytes
+    const __int128 low = -b.bytes - away;
+    __int128 k = low >= 0 ? low / step + 1 : -((-low - 1) / step);
+    if (k < 1 - a.lines) k = 1 - a.lines;
+    return k < b.lines && away + k * step < a.bytes;
+}
+static int check_apart(const char* who, const char* x, const Extent& a, const char* y, const Extent& b)
+{
+    DBLP_REQUIRE(!meet(a, b), DBLP_EINVAL, "%s: %s lies over %s", who, x, y);
+    return DBLP_OK;
+}
+// what is read element by element where it is written: the same matrix, or apart from it
+static int check_same_or_apart(const char* who, const char* x, const dblp_matrix_t* a, const Extent& ea, const char* y, const dblp_matrix_t* b, const Extent& eb)
+{
+    if (a->data == b->data && ea.lines == eb.lines && (ea.lines == 1 || ea.step == eb.step) && ea.bytes == eb.bytes) return DBLP_OK;
+    return check_apart(who, x, ea, y, eb);
+}
+
 // The matrix as an operand whose rows are its rows (summed over the columns), or turned: its columns (summed over the rows).
 static Operand operand(const dblp_matrix_t* m, uint32_t rows, uint32_t cols, bool turned)
 {
@@ -273,6 +318,24 @@ extern "C" int dblp_linear(const dblp_linear_t* l, const dblp_matrix_t* x, const
     if (pre) DBLP_TRY(check_matrix(who, "pre", pre, l->rows, l->out, l->dtype, false, true));
     DBLP_TRY(check_vector(who, "bias", bias, l->bias_dtype));
     DBLP_TRY(check_space(who, ws, ws_bytes, forward_bytes(l, x, w)));
+    {                                                           // blocks write while others still read x, w and bias
+        const Extent eo = extent_of(out, l->rows, l->out, l->out_dtype), ep = pre ? extent_of(pre, l->rows, l->out, l->dtype) : Extent{};
+        if (l->in) {
+            const Extent ex = extent_of(x, l->rows, l->in, l->dtype), ew = extent_of(w, l->in, l->out, l->dtype);
+            DBLP_TRY(check_apart(who, "out", eo, "x", ex));
+            DBLP_TRY(check_apart(who, "out", eo, "w", ew));
+            if (pre) DBLP_TRY(check_apart(who, "pre", ep, "x", ex));
+            if (pre) DBLP_TRY(check_apart(who, "pre", ep, "w", ew));
+        }
+        if (bias) DBLP_TRY(check_apart(who, "out", eo, "bias", extent_of(bias, 0, 1, l->out, l->bias_dtype)));
+        if (bias && pre) DBLP_TRY(check_apart(who, "pre", ep, "bias", extent_of(bias, 0, 1, l->out, l->bias_dtype)));
+        if (pre) DBLP_TRY(check_apart(who, "pre", ep, "out", eo));
+        if (residual) {
+            const Extent er = extent_of(residual, l->rows, l->out, l->out_dtype);
+            DBLP_TRY(check_same_or_apart(who, "out", out, eo, "residual", residual, er));
+            if (pre) DBLP_TRY(check_apart(who, "pre", ep, "residual", er));
+        }
+    }
     const dblp_matrix_t none{nullptr, 1, 1};
     const Product p = l->in ? forward_product(l, x, w) : forward_product(l, &none, &none);
     auto go = [&](auto t, auto o) -> int {
@@ -321,6 +384,31 @@ extern "C" int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy,
     if (want_dx && l->out) need = max(need, product_space(px));
     if (want_dw && l->rows) need = max(need, product_space(pw));
     DBLP_TRY(check_space(who, ws, ws_bytes, need));
+    {                                                           // what a result may lie over: nothing that is read after its first block has written
+        Extent out[3], in[5];
+        const char *out_name[3], *in_name[5];
+        int outs = 0, ins = 0;
+        auto output = [&](const char* name, const Extent& e) { out_name[outs] = name; out[outs++] = e; };
+        auto input = [&](const char* name, const Extent& e) { in_name[ins] = name; in[ins++] = e; };
+        if (l->rows && l->out && (want_dx || want_dw || want_db)) input("dy", extent_of(dy, l->rows, l->out, l->dtype));
+        if (want_dx && l->out) input("w", extent_of(w, l->in, l->out, l->dtype));
+        const int for_dx = ins;                                 // dx comes last: x, read for dw, may lie under it
+        if (want_dw && l->rows) input("x", extent_of(x, l->rows, l->in, l->dtype));
+        if (want_dx && residual) input("residual", extent_of(residual, l->rows, l->in, l->dtype));
+        if (want_dx && pre) input("pre", extent_of(pre, l->rows, l->in, l->dtype));
+        if (want_dw) output("dw", extent_of(dw, l->in, l->out, l->out_dtype));
+        if (want_db) output("dbias", extent_of(dbias, 0, 1, l->out, l->bias_dtype));
+        for (int i = 0; i < outs; ++i)
+            for (int j = 0; j < ins; ++j) DBLP_TRY(check_apart(who, out_name[i], out[i], in_name[j], in[j]));
+        if (outs == 2) DBLP_TRY(check_apart(who, "dw", out[0], "dbias", out[1]));
+        if (want_dx) {
+            const Extent ex = extent_of(dx, l->rows, l->in, l->dtype);
+            for (int i = 0; i < outs; ++i) DBLP_TRY(check_apart(who, "dx", ex, out_name[i], out[i]));
+            for (int j = 0; j < for_dx; ++j) DBLP_TRY(check_apart(who, "dx", ex, in_name[j], in[j]));
+            if (residual) DBLP_TRY(check_same_or_apart(who, "dx", dx, ex, "residual", residual, extent_of(residual, l->rows, l->in, l->dtype)));
+            if (pre) DBLP_TRY(check_same_or_apart(who, "dx", dx, ex, "pre", pre, extent_of(pre, l->rows, l->in, l->dtype)));
+        }
+    }
 
     // dw before dx: dx may be written over pre or the residual, never over x or dy
     if (want_db) DBLP_TRY(column_sums(l, dy, dbias, ws, s));
