@@ -505,7 +505,8 @@ int dblp_attention_grad(const dblp_attention_t* a, const dblp_heads_t* q, const 
  *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * freqs[i].
  * The angle is a 64-bit product reduced to one turn before it is rounded, so far positions lose nothing; the rest is fp32,
  * rounded once.  The squares of a head must not add up beyond fp32 (elements up to about 10^18).  Heads are as for
- * dblp_attention (data and strides multiples of 16 bytes); q_out may be q and k_out may be k (the same data and strides).
+ * dblp_attention (data and strides multiples of 16 bytes); q_out may be q and k_out may be k (the same data and strides); nothing of
+ * q lies over anything of k where either is written.
  * dblp_norm_rotate_grad: with d = the gradient of the output turned back by -t,
  *     dx_i = r weight_i d_i - x_i r^3 / head_dim * sum_j weight_j d_j x_j,  dweight_i = sum over tokens and heads of d_i x_i r,
  * from the inputs of the forward call; dq may be dq_out and dk may be dk_out.  With DBLP_ACCUMULATE dweight is added to.
@@ -528,7 +529,8 @@ typedef struct {
 int dblp_norm_rotate(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* q_out,
                      const dblp_heads_t* k, const void* k_weight, const dblp_heads_t* k_out, void* stream);
 int dblp_norm_rotate_grad_workspace_bytes(const dblp_norm_rotate_t* a, size_t* bytes);
-/* dq_weight, dk_weight NULL = not wanted (both NULL: no workspace needed) */
+/* dq_weight, dk_weight NULL = not wanted (both NULL: no workspace needed); a weight that q and k share has two gradients, in two
+ * places, which the caller adds up */
 int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_heads_t* q, const void* q_weight, const dblp_heads_t* dq_out,
                           const dblp_heads_t* dq, void* dq_weight, const dblp_heads_t* k, const void* k_weight,
                           const dblp_heads_t* dk_out, const dblp_heads_t* dk, void* dk_weight, void* ws, size_t ws_bytes,

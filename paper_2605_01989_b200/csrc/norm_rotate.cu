@@ -339,6 +339,13 @@ static int check_side(const char* who, const char* name, const dblp_norm_rotate_
     return DBLP_OK;
 }
 
+// Blocks of one side write while blocks of the other still read and write: what begins in one place would mix.
+static int check_sides(const char* who, const char* x, const void* a, const char* y, const void* b)
+{
+    DBLP_REQUIRE(a != b, DBLP_EINVAL, "%s: %s lies over %s", who, x, y);
+    return DBLP_OK;
+}
+
 static uint32_t lanes_of(uint32_t head_dim)
 {
     uint32_t l = 1;
@@ -439,6 +446,11 @@ extern "C" int dblp_norm_rotate(const dblp_norm_rotate_t* a, const dblp_heads_t*
         DBLP_TRY(check_side("norm_rotate", "k_out", a, k_out, a->k_heads, true));
         DBLP_TRY(check_weight("norm_rotate", "k_weight", k_weight, a->weight_dtype));
     }
+    if (a->q_heads && a->k_heads) {
+        DBLP_TRY(check_sides("norm_rotate", "q_out", q_out->data, "k", k->data));
+        DBLP_TRY(check_sides("norm_rotate", "k_out", k_out->data, "q", q->data));
+        DBLP_TRY(check_sides("norm_rotate", "q_out", q_out->data, "k_out", k_out->data));
+    }
     RotArgs r = rot_args(a);
     r.side[0] = rot_side(a, q, q_weight, q_out, a->q_heads);
     r.side[1] = rot_side(a, k, k_weight, k_out, a->k_heads);
@@ -496,6 +508,17 @@ extern "C" int dblp_norm_rotate_grad(const dblp_norm_rotate_t* a, const dblp_hea
         DBLP_REQUIRE(ws, DBLP_EINVAL, "%s: the workspace is null", who);
         DBLP_REQUIRE(((uintptr_t)ws & 255) == 0, DBLP_EALIGN, "%s: the workspace is not 256-byte aligned", who);
         DBLP_REQUIRE(ws_bytes >= need, DBLP_ECAPACITY, "%s: workspace of %zu bytes, needs %zu", who, ws_bytes, need);
+    }
+    if (!empty && a->q_heads && a->k_heads) {
+        DBLP_TRY(check_sides(who, "dq", dq->data, "k", k->data));
+        DBLP_TRY(check_sides(who, "dq", dq->data, "dk_out", dk_out->data));
+        DBLP_TRY(check_sides(who, "dk", dk->data, "q", q->data));
+        DBLP_TRY(check_sides(who, "dk", dk->data, "dq_out", dq_out->data));
+        DBLP_TRY(check_sides(who, "dq", dq->data, "dk", dk->data));
+    }
+    if (dq_weight && dk_weight) {                               // each is a sum of its own: one place would hold either of them
+        const uintptr_t p = (uintptr_t)dq_weight, q0 = (uintptr_t)dk_weight, bytes = (uintptr_t)a->head_dim * element_bytes(a->weight_dtype);
+        DBLP_REQUIRE(p + bytes <= q0 || q0 + bytes <= p, DBLP_EINVAL, "%s: dq_weight lies over dk_weight", who);
     }
     float* const partial[2] = {(float*)ws, (float*)((char*)ws + q_bytes)};
     RotArgs r = rot_args(a);
