@@ -1,6 +1,7 @@
 """Builds libdblp.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
 import glob
 import os
+import re
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +19,22 @@ def _deps():
     return sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + [os.path.join(ROOT, "include", "dblp.h")]
 
 
+def registers(path=OUT):
+    """Registers a thread of every kernel in a library built here, by mangled name."""
+    tool = os.path.join(os.path.dirname(NVCC), "cuobjdump")
+    text = subprocess.run([tool, "--dump-resource-usage", path], check=True, capture_output=True, text=True).stdout
+    return {name: int(n) for name, n in re.findall(r"Function (\S+):\s+REG:(\d+)", text)}
+
+
+def check_registers(found):
+    """The products that sum in runs move registers between their warps, and refuse to start with another number than they count on."""
+    with open(os.path.join(CSRC, "product_kernels.cuh")) as f:
+        want = int(re.search(r"kRunRegs = (\d+)", f.read()).group(1))
+    wrong = {name: n for name, n in found.items() if re.search(r"k_productILi\dELb1E", name) and n != want}
+    if wrong:
+        raise RuntimeError("kernels that would refuse to start, built with other than %d registers a thread: %s" % (want, wrong))
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(OUT) and all(os.path.getmtime(OUT) >= os.path.getmtime(f) for f in _deps()):
         return OUT
@@ -25,7 +42,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
            "-Xcompiler", "-fPIC,-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", OUT]
     if verbose:
         cmd += ["-Xptxas", "-v"]
+    made = OUT[:-3] + ".new.so"
+    cmd[cmd.index(OUT)] = made
     subprocess.run(cmd + sources(), check=True)
+    check_registers(registers(made))
+    os.replace(made, OUT)
     return OUT
 
 

@@ -29,6 +29,11 @@
 namespace dblp {
 
 constexpr int kProdThreads = 384, kProdWriters = 8;             // warps 0 .. 7 write, 8 and 10 load A and B, 9 issues products, 11 idles
+// With runs a writer holds 128 sums: registers move to the writers' two warpgroups from the third.  An increase waits until the block's
+// own registers allow it, so the shares may not be more than what the block was launched with: 168 a thread, the most that 384
+// threads can have.  build.py looks at what the compiler gave.
+constexpr int kRunRegs = 168, kRunWriterRegs = 224, kRunOtherRegs = 56;
+static_assert(kProdWriters * 32 * kRunWriterRegs + (kProdThreads - kProdWriters * 32) * kRunOtherRegs == kProdThreads * kRunRegs, "registers of a block");
 constexpr uint32_t kMaxStages = 8;
 constexpr uint32_t kPieceBytes = 32 * 32 * 4;                   // what a writing warp brings through shared memory at a time
 constexpr uint32_t kProdSmem = 227 * 1024 - 512;                // what a block may use, less its barriers
@@ -255,10 +260,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
     wait_before();
     after_start();
 
-    // With runs a writer holds 128 sums.  Registers of a thread: 168 at launch, then 224 in two warpgroups and 56 in the third, the same
-    // 64512 in all.
     if (warp >= kProdWriters) {
-        if (RUNS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (RUNS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRunOtherRegs));
         if (warp == 8 || warp == 10) {                              // ---- loads: A by one warp, B by another
             const bool is_a = warp == 8, mn = is_a ? a.a_mn : a.b_mn;
             const CUtensorMap* words = is_a ? a.a : a.b;
@@ -334,7 +337,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) k_product(const __grid_consta
             }
         }
     } else {                                                    // ---- sums to their places
-        if (RUNS) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        if (RUNS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRunWriterRegs));
         uint8_t* piece = ring + a.stages * a.stage_bytes + warp * kPieceBytes;
         const uint32_t lanes = (warp & 3) * 32, half = (warp >> 2) * 32;
         uint32_t w = 0;
@@ -611,7 +614,7 @@ template <int CG, bool RUNS, typename E> static int launch_product(const Product
             DBLP_CUDA(cudaFuncGetAttributes(&fa, kernel));
             regs.store(fa.numRegs, std::memory_order_release);
         }
-        DBLP_REQUIRE(regs.load(std::memory_order_acquire) == 168, DBLP_ECUDA, "product: built with %d registers a thread, not 168", regs.load());
+        DBLP_REQUIRE(regs.load(std::memory_order_acquire) == kRunRegs, DBLP_ECUDA, "product: built with %d registers a thread, not %d", regs.load(), kRunRegs);
     }
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg{};
