@@ -651,8 +651,7 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
     if constexpr (E::kFewRows)
         if (rows_take(p)) return product_rows(p, e, s);
     const ProductPlan r = plan_product(p);
-    DBLP_REQUIRE(r.cg, DBLP_ECAPACITY, "product: 2^31 tiles or more");
-    DBLP_REQUIRE((uint64_t)r.tiles * p.batch + (uint64_t)r.rest * r.parts < 1ull << 31, DBLP_ECAPACITY, "product: 2^31 tiles or more");
+    DBLP_REQUIRE(r.cg, DBLP_ECAPACITY, "product: 2^30 tiles or more");
     unsigned long long* timeouts = timeout_counter();
     DBLP_REQUIRE(timeouts, DBLP_ECUDA, "product: no device counter: %s", cudaGetErrorString(cudaGetLastError()));
     Operand oa = p.a, ob = p.b;
