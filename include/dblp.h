@@ -581,9 +581,13 @@ int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp
  * (with X^T X and X (b A + c A A) where x is taller than wide: the products are always those of the shorter side).
  * Used on the mean of a round (Algorithm 3) before the weights are updated.
  * The norm is summed in 64 bits.  X and A enter the products scaled by powers of two (1024 and 256) and rounded to f16; X itself is
- * kept in two f16 words (22 bits), so that what rounding adds is not amplified with the small singular values.  With
- * out_dtype BF16 each product is one of f16 operands: the result is off by about 2e-3 of its norm at most, as much as
- * its rounding.  With out_dtype F32 or F16 the products are of both words (three products each): about 6e-6, what the iteration in fp32 has.
+ * kept in two f16 words (22 bits), so that what rounding adds is not amplified with the small singular values.  How far results are from
+ * the iteration in 64 bits, in parts of their norm, with five steps of the usual coefficients:
+ *   out_dtype BF16  from 64 on the shorter side each product is one of f16 operands: 1.7e-3 to 2.8e-3 (1.7e-3 of it is the result's own
+ *                   rounding), up to 5e-3 where all singular values are alike; below that as for F32, and the rounding.
+ *   F32 or F16      the products are of both words (three products each, about three times the work of large matrices): up to 6e-6, and up to 7e-5 for
+ *                   matrices of one or a few directions (iterated in fp32: 1.6e-4); F16 results are rounded besides.
+ * For a bf16 result as near as the fp32 iteration's take F32 and convert.
  * Coefficients must keep the entries of X below 63 and those of A and b A + c A A below 255 (singular values up to about 2 do), beyond
  * which they become infinite.  An x of zeros gives zeros.  NaN or infinity in a matrix spreads over that matrix alone.
  * out may be x (the same place, strides and dtype).

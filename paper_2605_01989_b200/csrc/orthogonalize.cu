@@ -3,9 +3,9 @@
 // f16 carries 11 bits where bf16 carries 8, and the entries' range is known: |X| is at most about 1.2 in every singular value, so
 // X scaled by 2^10 and A by 2^8 sit in the middle of f16's range.  What would still go wrong is the rounding of X itself: the
 // polynomial multiplies a small singular value by up to a per step (3.4^5 = 485 in five), noise as well as signal.  X is
-// therefore two f16 words (22 bits); the products read the first, and only the term a X, the one that amplifies what lies
-// outside the strong directions, reads both.  (In 64-bit simulation of a matrix of rank 8: 4e-2 of the result's norm with one
-// word, 5e-4 with two; one bf16 word 3e-1.)
+// therefore two f16 words (22 bits); for bf16 results the products read the first, and only the term a X, the one that amplifies what
+// lies outside the strong directions, reads both.  (In 64-bit simulation of a matrix of rank 8: 4e-2 of the result's norm with one
+// word, 5e-4 with two; one bf16 word 3e-1.)  For fp32 and f16 results, and small matrices, products read both words of X, A and B.
 #include <math.h>
 
 #include "product.cuh"
@@ -16,6 +16,10 @@ constexpr int kUpdThreads = 256;
 constexpr uint32_t kMaxSquares = 256;            // partial sums of squares a matrix
 constexpr double kScaleX = 1024.0;
 constexpr float kScaleA = 256.0f;
+// Bf16 results of matrices from here on (the shorter side) come of products of one word, whose roundings average out over rows and
+// columns: 1.7e-3 to 2.8e-3 of the norm with the result's own.  Below that single roundings show, up to 1.6e-2 for sides of two, so
+// these multiply both words: 1.7e-3; 16 x 16 takes 60 us instead of 45, 1 x 50 61 instead of 43.
+constexpr uint32_t kAverages = 64;
 
 struct UpdIn {
     Source x;
@@ -110,7 +114,7 @@ static UpdPlan plan_update(const dblp_orthogonalize_t* u)
     UpdPlan p{};
     p.tall = u->rows > u->cols;
     p.low = p.tall ? u->cols : u->rows;
-    p.precise = u->out_dtype != DBLP_BF16;
+    p.precise = u->out_dtype != DBLP_BF16 || p.low < kAverages;
     p.xs = (u->cols + 15) & ~15u;
     p.as = (p.low + 15) & ~15u;
     auto padded = [](size_t b) { return (b + 255) & ~(size_t)255; };
@@ -193,10 +197,12 @@ static bool whole(const void* p, int64_t row_stride, int64_t batch_stride, const
     return ((uintptr_t)p | rows | batches) % bytes == 0;
 }
 
-// The products of bf16 results are of one word, the others of both, their sums in short runs.
-template <typename E> static int product(const UpdPlan& plan, const Product& p, const E& e, void* ws, cudaStream_t s)
+// Products of both words take their sums in short runs; F32 and F16 results know no other.
+template <bool ONE_WORD, typename E> static int product(const UpdPlan& plan, const Product& p, const E& e, void* ws, cudaStream_t s)
 {
-    return plan.precise ? run_product<true>(p, e, ws, true, s) : run_product<false>(p, e, ws, true, s);
+    if constexpr (ONE_WORD)
+        if (!plan.precise) return run_product<false>(p, e, ws, true, s);
+    return run_product<true>(p, e, ws, true, s);
 }
 
 static int check_update(const char* who, const dblp_orthogonalize_t* u)
@@ -283,15 +289,15 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
         EpiPoly<true> e{};
         e.out = w.a;
         e.alpha = kScaleA / (float)(kScaleX * kScaleX);
-        DBLP_TRY(product(p, gram_product(u, p, now), e, w.products, s));
+        DBLP_TRY(product<true>(p, gram_product(u, p, now), e, w.products, s));
         e.out = w.b;
         e.add = w.a;
         e.alpha = c / kScaleA;
         e.beta = b;
-        DBLP_TRY(product(p, square_product(u, p, w.a), e, w.products, s));
+        DBLP_TRY(product<true>(p, square_product(u, p, w.a), e, w.products, s));
         const Product last = step_product(u, p, w.b, now);
         if (i + 1 < u->steps) {
-            DBLP_TRY(product(p, last, EpiPoly<false>{next, now, 1.0f / kScaleA, a}, w.products, s));
+            DBLP_TRY(product<true>(p, last, EpiPoly<false>{next, now, 1.0f / kScaleA, a}, w.products, s));
             const Words t = now;
             now = next;
             next = t;
@@ -306,7 +312,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
                 f.alpha = back / kScaleA;
                 f.beta = back * a;
                 f.aligned = whole(out, u->out_row_stride, u->out_batch_stride, u, u->out_dtype, 32);
-                return run_product<!std::is_same<O, __nv_bfloat16>::value>(last, f, w.products, true, s);
+                return product<std::is_same<O, __nv_bfloat16>::value>(p, last, f, w.products, s);
             }));
         }
     }

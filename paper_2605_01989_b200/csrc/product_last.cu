@@ -4,6 +4,7 @@
 namespace dblp {
 
 DBLP_PRODUCT(false, EpiLast<__nv_bfloat16>);
+DBLP_PRODUCT(true, EpiLast<__nv_bfloat16>);
 DBLP_PRODUCT(true, EpiLast<__half>);
 DBLP_PRODUCT(true, EpiLast<float>);
 

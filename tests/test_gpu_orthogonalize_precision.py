@@ -1,0 +1,85 @@
+"""How far dblp_orthogonalize's results are from the iteration in 64 bits, in parts of the result's norm, with the usual five steps.
+
+The bounds, from the scheme's own roundings:
+F32  X is held to 2^-23 of its entries.  Where the result fills the space (full rank) the error stays small; the tensor cores' runs of 256 terms of
+     one sign take 1.2e-6 from the diagonal of A, which the polynomial multiplies by up to |b| = 4.8, 6e-6: twice that.
+     Of a few directions only, what rounding leaves in the other directions grows by a = 3.4445 a step.  What is lost before step k of five
+     arrives 3.4445^(5 - k) times as large, 485 + 141 + 41 + 12 + 3 = 682 together, of an X that is up to 1.2 / 0.68 times the
+     result: 682 * 1.77 * 2^-23 = 1.44e-4.  (485 * 2^-23 = 5.8e-5, the first rounding alone and of a result as large as X, is passed:
+     7.3e-5.  The iteration in fp32 gives 3e-5 to 1.6e-4 for the same matrices.)
+F16  the same and the result's rounding, 2^-12.
+BF16 products of one f16 word.  Singular values that spread: roundings of random sign, 2.4e-3 at most from 64 on the shorter side by a 64-bit
+     simulation with the same words, and the result's rounding, 1.7e-3 for values that spread over a binade; together the root of the sum
+     of squares.  All alike: A and B are multiples of the identity but for noise, and every diagonal element is rounded the same way, by up to
+     d = 2^-11.  A step at s = 1.1 changes X by |b s^2 + c s^4| / (f / s) = 2.8 / 0.64 = 4.4 d for B; a step at 0.7 by 1.16 d for B and 0.86 d
+     for A, which the next step multiplies by |s f' / f| = 1.6, 3.2 d; the one before that 0.71 * 1.6 * 2 d = 2.3 d: 9.9 d = 4.8e-3
+     in all, and 1.3e-3 and 1.7e-3 of random sign, 5.3e-3."""
+import pytest
+import torch
+
+from paper_2605_01989_b200 import binding as dblp
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+FULL = {F32: 1.2e-5, F16: 1.2e-5 + 2.0 ** -12, BF16: 3e-3}
+FEW = {F32: 1.44e-4, F16: 1.44e-4 + 2.0 ** -12, BF16: 3e-3}
+ALIKE = {F32: 1.2e-5, F16: 1.2e-5 + 2.0 ** -12, BF16: 5.3e-3}
+
+
+def randn(shape, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device=DEV, dtype=torch.float64)
+
+
+def matrix(m, n, kind, seed):
+    if kind.startswith("rank"):
+        k = int(kind[4:])
+        return randn((m, k), seed) @ randn((k, n), seed + 1)
+    g = randn((m, n), seed)
+    if kind == "strong":
+        return randn((m, 3), seed + 1) @ randn((3, n), seed + 2) + 0.1 * g
+    if kind == "gradient":
+        return 0.5 * randn((m, 8), seed + 1) @ randn((8, n), seed + 2) + g
+    if kind == "alike":
+        return torch.linalg.qr(g)[0] if m >= n else torch.linalg.qr(g.T)[0].T
+    return g
+
+
+def iteration(x):
+    x = x.double()
+    x = x / (x.norm() + 1e-7)
+    tall = x.shape[0] > x.shape[1]
+    x = x.T if tall else x
+    for a, b, c in dblp.MUON_COEFFICIENTS:
+        A = x @ x.T
+        x = a * x + (b * A + c * A @ A) @ x
+    return x.T if tall else x
+
+
+@pytest.mark.parametrize("out_dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("kind", ["noise", "strong", "gradient", "alike", "rank1", "rank2", "rank8"])
+@pytest.mark.parametrize("m,n", [(64, 64), (129, 200), (700, 90), (384, 640), (1030, 520), (1600, 1600)])
+def test_the_result_is_as_near_as_the_header_says(m, n, kind, out_dtype):
+    x = (matrix(m, n, kind, m + n) * 1e-3).float().contiguous()
+    out = torch.empty((m, n), dtype=out_dtype, device=DEV)
+    dblp.dblp_orthogonalize(x, out, torch.empty(dblp.dblp_orthogonalize_workspace_bytes(x, out), dtype=torch.uint8, device=DEV))
+    want = iteration(x)
+    off = ((out.double() - want).norm() / want.norm()).item()
+    bound = (FEW if kind.startswith("rank") else ALIKE if kind == "alike" else FULL)[out_dtype]
+    assert off < bound, (off, bound)
+
+
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 50), (2, 1), (2, 3), (3, 2), (28, 2), (8, 8), (17, 40), (63, 63), (700, 33), (1, 4000)])
+def test_bf16_results_of_small_matrices_are_rounded_once(m, n):
+    """Element by element half a step of the result: 2^-8 of it, and what the products of both words are off by, 1.44e-4 of the norm at most."""
+    for seed in range(20):
+        x = randn((5, m, n), 100 + seed).float()
+        out = torch.empty((5, m, n), dtype=BF16, device=DEV)
+        dblp.dblp_orthogonalize(x, out, torch.empty(dblp.dblp_orthogonalize_workspace_bytes(x, out), dtype=torch.uint8, device=DEV))
+        for j in range(5):
+            want = iteration(x[j])
+            tol = 2.0 ** -8 * want.abs() + 1.44e-4 * want.norm()
+            assert ((out[j].double() - want).abs() <= tol).all(), (seed, j)
