@@ -585,8 +585,8 @@ int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp
  * the iteration in 64 bits, in parts of their norm, with five steps of the usual coefficients:
  *   out_dtype BF16  from 64 on the shorter side each product is one of f16 operands: 1.7e-3 to 2.8e-3 (1.7e-3 of it is the result's own
  *                   rounding), up to 5e-3 where all singular values are alike; below that as for F32, and the rounding.
- *   F32 or F16      the products are of both words (three products each, about three times the work of large matrices): up to 6e-6, and up to 7e-5 for
- *                   matrices of one or a few directions (iterated in fp32: 1.6e-4); F16 results are rounded besides.
+ *   F32 or F16      the products are of both words (three products each, about three times the work of large matrices): up to 5e-6, and up to 6e-5 for
+ *                   matrices of one or a few directions (iterated in fp32: 5e-6, 1.6e-4); F16 results are rounded besides.
  * For a bf16 result as near as the fp32 iteration's take F32 and convert.
  * Coefficients must keep the entries of X below 63 and those of A and b A + c A A below 255 (singular values up to about 2 do), beyond
  * which they become infinite.  An x of zeros gives zeros.  NaN or infinity in a matrix spreads over that matrix alone.

@@ -13,8 +13,8 @@
 //              computed (as columns of the tile).
 //   parts      tiles of the last, incomplete round are cut along the summed dimension; the parts' sums are added in order by a
 //              second kernel with the same epilogue.
-//   fp32       the tensor cores' sums truncate; where the result is fp32, and where a sum is long, they are taken out every 512
-//              (three-term products: 256) and added up in registers.
+//   fp32       the tensor cores' sums truncate; where the result is fp32, and where a sum is long, they are taken out in runs (run_stages) and
+//              added up in registers.
 //   bound      256 x 256 tiles by the tensor pipe under the power cap, like the library's product (a pair needs 64 bytes a cycle and
 //              multiprocessor from L2, about what it gives: five stages instead of six cost 10 %, four 30 %); tiles of 128 columns by
 //              the 340 cycles that a stage takes to issue; with bias, gelu and a second result by the writing warps: 22 900
@@ -688,8 +688,7 @@ template <bool RUNS, typename E> int run_product(const Product& p, const E& e, v
     a.nt = r.nt;
     a.steps = r.steps;
     a.term_steps = r.term_steps;
-    // Error of 8192 products of random signs: 9.1e-6 of the result in one run, 4.7e-7 in runs of 512, 2.4e-7 of 256; plain fp32 9.6e-7.
-    a.run = p.terms == 3 ? 4 : 8;
+    a.run = run_stages(p);
     a.whole = r.whole;
     a.rest = r.rest;
     a.parts = r.parts;

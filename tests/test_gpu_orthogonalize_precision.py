@@ -1,12 +1,12 @@
 """How far dblp_orthogonalize's results are from the iteration in 64 bits, in parts of the result's norm, with the usual five steps.
 
 The bounds, from the scheme's own roundings:
-F32  X is held to 2^-23 of its entries.  Where the result fills the space (full rank) the error stays small; the tensor cores' runs of 256 terms of
-     one sign take 1.2e-6 from the diagonal of A, which the polynomial multiplies by up to |b| = 4.8, 6e-6: twice that.
+F32  X is held to 2^-23 of its entries.  Where the result fills the space (full rank) the error stays small; the tensor cores' runs of 192 terms of
+     one sign at most take 1.2e-6 from the diagonal of A, which the polynomial multiplies by up to |b| = 4.8, 6e-6: twice that.
      Of a few directions only, what rounding leaves in the other directions grows by a = 3.4445 a step.  What is lost before step k of five
      arrives 3.4445^(5 - k) times as large, 485 + 141 + 41 + 12 + 3 = 682 together, of an X that is up to 1.2 / 0.68 times the
-     result: 682 * 1.77 * 2^-23 = 1.44e-4.  (485 * 2^-23 = 5.8e-5, the first rounding alone and of a result as large as X, is passed:
-     7.3e-5.  The iteration in fp32 gives 3e-5 to 1.6e-4 for the same matrices.)
+     result: 682 * 1.77 * 2^-23 = 1.44e-4.  (The iteration in fp32 gives 3e-5 to 1.6e-4 for the
+     same matrices.)
 F16  the same and the result's rounding, 2^-12.
 BF16 products of one f16 word.  Singular values that spread: roundings of random sign, 2.4e-3 at most from 64 on the shorter side by a 64-bit
      simulation with the same words, and the result's rounding, 1.7e-3 for values that spread over a binade; together the root of the sum
@@ -83,3 +83,21 @@ def test_bf16_results_of_small_matrices_are_rounded_once(m, n):
             want = iteration(x[j])
             tol = 2.0 ** -8 * want.abs() + 1.44e-4 * want.norm()
             assert ((out[j].double() - want).abs() <= tol).all(), (seed, j)
+
+
+@pytest.mark.parametrize("kind", ["noise", "gradient"])
+@pytest.mark.parametrize("m,n", [(129, 200), (200, 3000), (384, 640), (1030, 520), (700, 4000), (900, 4096), (1024, 2000), (1300, 4000), (6400, 1600)])
+def test_fp32_results_are_as_near_as_the_iteration_in_fp32(m, n, kind):
+    """Off by at most half as much again as the same iteration in plain fp32, on the same matrix."""
+    x = matrix(m, n, kind, m + n).float() * 1e-2
+    out = torch.empty_like(x)
+    dblp.dblp_orthogonalize(x, out, torch.empty(dblp.dblp_orthogonalize_workspace_bytes(x, out), dtype=torch.uint8, device=DEV))
+    want, plain = iteration(x), x / (x.norm() + 1e-7)
+    plain = plain.T if m > n else plain
+    assert not torch.backends.cuda.matmul.allow_tf32
+    for a, b, c in dblp.MUON_COEFFICIENTS:
+        A = plain @ plain.T
+        plain = a * plain + (b * A + c * (A @ A)) @ plain
+    plain = plain.T if m > n else plain
+    off, fp32 = (((t.double() - want).norm() / want.norm()).item() for t in (out, plain))
+    assert off <= 1.5 * fp32, (off, fp32)
