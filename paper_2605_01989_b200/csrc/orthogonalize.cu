@@ -5,7 +5,8 @@
 // polynomial multiplies a small singular value by up to a per step (3.4^5 = 485 in five), noise as well as signal.  X is
 // therefore two f16 words (22 bits); for bf16 results the products read the first, and only the term a X, the one that amplifies what
 // lies outside the strong directions, reads both.  (In 64-bit simulation of a matrix of rank 8: 4e-2 of the result's norm with one
-// word, 5e-4 with two; one bf16 word 3e-1.)  For fp32 and f16 results, and small matrices, products read both words of X, A and B.
+// word, 5e-4 with two; one bf16 word 3e-1.)  For fp32 and f16 results, and in the last steps
+// of small matrices, products read both words of X, A and B.
 #include <math.h>
 
 #include "product.cuh"
@@ -16,10 +17,12 @@ constexpr int kUpdThreads = 256;
 constexpr uint32_t kMaxSquares = 256;            // partial sums of squares a matrix
 constexpr double kScaleX = 1024.0;
 constexpr float kScaleA = 256.0f;
-// Bf16 results of matrices from here on (the shorter side) come of products of one word, whose roundings average out over rows and
-// columns: 1.7e-3 to 2.8e-3 of the norm with the result's own.  Below that single roundings show, up to 1.6e-2 for sides of two, so
-// these multiply both words: 1.7e-3; 16 x 16 takes 60 us instead of 45, 1 x 50 61 instead of 43.
-constexpr uint32_t kAverages = 64;
+// Bf16 results come of products of one word where single roundings average out over many rows and columns: from kAverages on the shorter
+// side 1.25 to 1.42 times as far from 64 bits as the result's rounding alone.  Smaller matrices multiply both words in their last
+// three steps, whose roundings reach the result (up to 1.6 times with one word, 1.0 to 1.1 with both: 129 x 200 78 and 99 us, 256 x 1024 90 and
+// 125 us), and in all steps below kFew, where single roundings show (sides of two: up to 1.6e-2 of the norm, with both 1.7e-3; 16 x 16 45 and
+// 60 us).
+constexpr uint32_t kAverages = 384, kFew = 64, kLastSteps = 3;
 
 struct UpdIn {
     Source x;
@@ -103,7 +106,8 @@ __global__ void __launch_bounds__(kUpdThreads) k_normalize(const __grid_constant
 
 struct UpdPlan {
     uint32_t low;                                // the shorter side
-    bool tall, precise;
+    bool tall;
+    bool one, both;                              // products of one word, of both, occur
     uint32_t xs, as;                             // row strides of X and of A, B
     size_t x_bytes, a_bytes, squares_bytes;      // one word of X, of A; sums
     uint32_t parts;
@@ -114,7 +118,8 @@ static UpdPlan plan_update(const dblp_orthogonalize_t* u)
     UpdPlan p{};
     p.tall = u->rows > u->cols;
     p.low = p.tall ? u->cols : u->rows;
-    p.precise = u->out_dtype != DBLP_BF16 || p.low < kAverages;
+    p.one = u->out_dtype == DBLP_BF16 && p.low >= kFew;
+    p.both = !p.one || p.low < kAverages;
     p.xs = (u->cols + 15) & ~15u;
     p.as = (p.low + 15) & ~15u;
     auto padded = [](size_t b) { return (b + 255) & ~(size_t)255; };
@@ -126,31 +131,31 @@ static UpdPlan plan_update(const dblp_orthogonalize_t* u)
     return p;
 }
 
-static Product gram_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& x)
+static Product gram_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& x, bool both)
 {
     Product g{};
-    g.a = Operand{x.hi, p.precise ? x.lo : nullptr, x.stride, x.each, p.tall};
+    g.a = Operand{x.hi, both ? x.lo : nullptr, x.stride, x.each, p.tall};
     g.b = g.a;
     g.M = g.N = p.low;
     g.K = p.tall ? u->rows : u->cols;
     g.batch = u->batch;
     g.dtype = DBLP_F16;
-    g.terms = p.precise ? 3 : 1;
+    g.terms = both ? 3 : 1;
     g.symmetric = true;
     return g;
 }
-static Product square_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& a)
+static Product square_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& a, bool both)
 {
-    Product g = gram_product(u, p, a);
-    g.a = g.b = Operand{a.hi, p.precise ? a.lo : nullptr, a.stride, a.each, false};
+    Product g = gram_product(u, p, a, both);
+    g.a = g.b = Operand{a.hi, both ? a.lo : nullptr, a.stride, a.each, false};
     g.K = p.low;
     return g;
 }
 // B X, or X B where X is tall
-static Product step_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& b, const Words& x)
+static Product step_product(const dblp_orthogonalize_t* u, const UpdPlan& p, const Words& b, const Words& x, bool both)
 {
-    Product g = square_product(u, p, b);
-    const Operand ox{x.hi, p.precise ? x.lo : nullptr, x.stride, x.each, !p.tall};
+    Product g = square_product(u, p, b, both);
+    const Operand ox{x.hi, both ? x.lo : nullptr, x.stride, x.each, !p.tall};
     if (p.tall) g.a = ox;
     else g.b = ox;
     g.M = u->rows;
@@ -181,12 +186,14 @@ static UpdSpace space_of(const dblp_orthogonalize_t* u, const UpdPlan& p, void* 
     };
     s.x = words(p.x_bytes, true, xe, p.xs);
     s.y = words(p.x_bytes, true, xe, p.xs);
-    s.a = words(p.a_bytes, p.precise, ae, p.as);
-    s.b = words(p.a_bytes, p.precise, ae, p.as);
+    s.a = words(p.a_bytes, p.both, ae, p.as);
+    s.b = words(p.a_bytes, p.both, ae, p.as);
     s.squares = (double*)take(p.squares_bytes);
     s.products = at;
     size_t most = 0;
-    for (const Product& g : {gram_product(u, p, s.x), square_product(u, p, s.a), step_product(u, p, s.b, s.x)}) most = max(most, product_space(g));
+    for (bool both : {false, true})
+        if (both ? p.both : p.one)
+            for (const Product& g : {gram_product(u, p, s.x, both), square_product(u, p, s.a, both), step_product(u, p, s.b, s.x, both)}) most = max(most, product_space(g));
     s.bytes = (size_t)(at - (char*)ws) + most;
     return s;
 }
@@ -198,10 +205,10 @@ static bool whole(const void* p, int64_t row_stride, int64_t batch_stride, const
 }
 
 // Products of both words take their sums in short runs; F32 and F16 results know no other.
-template <bool ONE_WORD, typename E> static int product(const UpdPlan& plan, const Product& p, const E& e, void* ws, cudaStream_t s)
+template <bool ONE_WORD, typename E> static int product(const Product& p, const E& e, void* ws, cudaStream_t s)
 {
     if constexpr (ONE_WORD)
-        if (!plan.precise) return run_product<false>(p, e, ws, true, s);
+        if (p.terms == 1) return run_product<false>(p, e, ws, true, s);
     return run_product<true>(p, e, ws, true, s);
 }
 
@@ -286,18 +293,21 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
     Words now = w.x, next = w.y;
     for (uint32_t i = 0; i < u->steps; ++i) {
         const float a = u->coefficients[3 * i], b = u->coefficients[3 * i + 1], c = u->coefficients[3 * i + 2];
+        const bool both = p.both && (!p.one || i + kLastSteps >= u->steps);
+        Words wa = w.a, wb = w.b;
+        if (!both) wa.lo = wb.lo = nullptr;
         EpiPoly<true> e{};
-        e.out = w.a;
+        e.out = wa;
         e.alpha = kScaleA / (float)(kScaleX * kScaleX);
-        DBLP_TRY(product<true>(p, gram_product(u, p, now), e, w.products, s));
-        e.out = w.b;
-        e.add = w.a;
+        DBLP_TRY(product<true>(gram_product(u, p, now, both), e, w.products, s));
+        e.out = wb;
+        e.add = wa;
         e.alpha = c / kScaleA;
         e.beta = b;
-        DBLP_TRY(product<true>(p, square_product(u, p, w.a), e, w.products, s));
-        const Product last = step_product(u, p, w.b, now);
+        DBLP_TRY(product<true>(square_product(u, p, wa, both), e, w.products, s));
+        const Product last = step_product(u, p, wb, now, both);
         if (i + 1 < u->steps) {
-            DBLP_TRY(product<true>(p, last, EpiPoly<false>{next, now, 1.0f / kScaleA, a}, w.products, s));
+            DBLP_TRY(product<true>(last, EpiPoly<false>{next, now, 1.0f / kScaleA, a}, w.products, s));
             const Words t = now;
             now = next;
             next = t;
@@ -312,7 +322,7 @@ extern "C" int dblp_orthogonalize(const dblp_orthogonalize_t* u, const void* x, 
                 f.alpha = back / kScaleA;
                 f.beta = back * a;
                 f.aligned = whole(out, u->out_row_stride, u->out_batch_stride, u, u->out_dtype, 32);
-                return product<std::is_same<O, __nv_bfloat16>::value>(p, last, f, w.products, s);
+                return product<std::is_same<O, __nv_bfloat16>::value>(last, f, w.products, s);
             }));
         }
     }

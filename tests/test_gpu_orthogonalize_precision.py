@@ -101,3 +101,32 @@ def test_fp32_results_are_as_near_as_the_iteration_in_fp32(m, n, kind):
     plain = plain.T if m > n else plain
     off, fp32 = (((t.double() - want).norm() / want.norm()).item() for t in (out, plain))
     assert off <= 1.5 * fp32, (off, fp32)
+
+
+@pytest.mark.parametrize("kind", ["noise", "gradient"])
+@pytest.mark.parametrize("m,n", [(64, 64), (64, 4000), (100, 3000), (129, 200), (300, 300), (383, 900), (384, 640), (512, 2048), (1030, 520), (1600, 1600)])
+def test_bf16_results_are_near_their_own_rounding(m, n, kind):
+    """Below 384 on the shorter side 1.2 times what rounding the exact result is off by (three last steps of both words), beyond 1.5 times."""
+    x = matrix(m, n, kind, m + n).float() * 1e-2
+    out = torch.empty((m, n), dtype=BF16, device=DEV)
+    dblp.dblp_orthogonalize(x, out, torch.empty(dblp.dblp_orthogonalize_workspace_bytes(x, out), dtype=torch.uint8, device=DEV))
+    want = iteration(x)
+    off, rounded = ((out.double() - want).norm().item(), (want.bfloat16().double() - want).norm().item())
+    assert off <= (1.2 if min(m, n) < 384 else 1.5) * rounded, off / rounded
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
+@pytest.mark.parametrize("m,n", [(40, 90), (200, 130), (400, 500)])
+def test_other_numbers_of_steps(m, n, steps):
+    """The workspace does not depend on the steps; which products read both words does."""
+    coefficients = ((1.5, -0.5, 0.0),) * steps
+    x = matrix(m, n, "noise", 7).float()
+    for out_dtype in (BF16, F32):
+        out = torch.empty((m, n), dtype=out_dtype, device=DEV)
+        ws = torch.full((dblp.dblp_orthogonalize_workspace_bytes(x, out),), 0xAB, dtype=torch.uint8, device=DEV)
+        dblp.dblp_orthogonalize(x, out, ws, coefficients=coefficients)
+        want = x.double() / (x.double().norm() + 1e-7)
+        for a, b, c in coefficients:
+            A = want @ want.T
+            want = a * want + (b * A + c * A @ A) @ want
+        assert ((out.double() - want).norm() / want.norm()).item() < FULL[out_dtype]
