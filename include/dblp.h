@@ -556,7 +556,8 @@ typedef struct {
  * of its two strides is 1 (weights held as [out, in] are the transposed view).  bias: contiguous.  bias, residual, pre:
  * NULL = none.  out may be the residual (the same place and stride); apart from that out and pre lie over nothing else that is passed:
  * an in-place step x += x w needs a second place.  The product's operands are 16-bit, everything after that is fp32 and rounded
- * once.  relu: max(z, 0), NaN stays; gelu: z Phi(z); gelu_tanh: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))); silu:
+ * once.  The tensor cores' own sums truncate: sums of one sign lose up to 2.8e-6 of themselves where the result is fp32 (taken in runs of 512
+ * terms), and an eighth of half a step where it has 16 bits.  relu: max(z, 0), NaN stays; gelu: z Phi(z); gelu_tanh: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))); silu:
  * z / (1 + exp(-z)).
  * dblp_linear_grad: dx = (dy w^T + residual) * act'(pre), dw = x^T dy, dbias = sum of dy's rows.  `pre` belongs to the
  * layer BEFORE: where x = act(pre) was that layer's output, dx is the gradient of its pre-activation, ready to be its dy;

@@ -124,7 +124,8 @@ __device__ __forceinline__ float tanh_arg(float z) { return 1.5957691216057308f 
 
 // The normal distribution's integral up to z, and e^(-z^2 / 2), of two values.  With x = |z| / sqrt 2 and t = 1 / (1 + 0.46 x), the tail
 // erfc(x) / 2 is e^(-x^2) t P(t): P of degree 7 was fitted here to the least largest relative error over x >= 0 (7e-7), so that far
-// tails keep their digits.  (CUDA's erfcf in its place: 8192 x 1600 -> 6400 with bias and gelu 431 us instead of 184.)
+// tails keep their digits.  (CUDA's erfcf in its place took 431 us for 8192 x 1600 -> 6400 with bias and gelu where this took 184, before
+// the epilogue around it was rewritten.)
 __device__ __forceinline__ float2 normal_cdf(float2 z, float2& e)
 {
     auto two = [](float x) { return make_float2(x, x); };

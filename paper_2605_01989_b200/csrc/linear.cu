@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) k_column_join(const __grid_constant__ Sum
     }
 }
 
-// Slices of at least 64 rows, as many as give about four blocks a multiprocessor.
+// At most one slice for every 64 rows begun, as many as give about four blocks a multiprocessor.
 static uint32_t sum_slices(uint32_t rows, uint32_t cols)
 {
     const uint32_t most = (rows + 63) / 64, want = 4 * kSms / ((cols + 255) / 256) + 1, s = most < want ? most : want;

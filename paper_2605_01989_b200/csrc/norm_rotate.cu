@@ -401,7 +401,8 @@ static RotSide rot_side(const dblp_norm_rotate_t* a, const dblp_heads_t* x, cons
     return s;
 }
 
-// Two tables of angles take up to 64 KB (a single head of a full rotation), 10 KB with 25 heads of 64.
+// Two tables of angles take up to 64 KB (a single head of a full rotation), 3.5 KB with 25 heads of 64; the gradient's sums, in the same
+// place, 16 KB.
 template <typename T, bool INTER, bool GRAD> static int launch_rotate(const RotArgs& r, size_t smem, cudaStream_t s)
 {
     constexpr auto kernel = k_norm_rotate<T, INTER, GRAD>;
