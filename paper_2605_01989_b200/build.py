@@ -20,8 +20,11 @@ def _deps():
 
 
 def registers(path=OUT):
-    """Registers a thread of every kernel in a library built here, by mangled name."""
+    """Registers a thread of every kernel in a library built here, by mangled name; none where the toolkit has no tool for it (the launch
+    looks as well)."""
     tool = os.path.join(os.path.dirname(NVCC), "cuobjdump")
+    if not os.path.exists(tool):
+        return {}
     text = subprocess.run([tool, "--dump-resource-usage", path], check=True, capture_output=True, text=True).stdout
     return {name: int(n) for name, n in re.findall(r"Function (\S+):\s+REG:(\d+)", text)}
 

@@ -38,16 +38,16 @@ int main()
 }
 """
 FIELDS = ("rows_take", "cg", "bn", "tiles", "whole", "rest", "parts", "per", "items", "turned", "several", "copies")
-_program = None
+_folder, _program = None, None
 
 
 def plans(products):
     """A dict per product; a product is a dict of M, N, K and, where they differ from 1, 1, 0, 0, 0, 0, 1: batch, terms, few, symmetric,
     a_mn, b_mn (the rows of an operand are contiguous, not the summed dimension) and whole (rows on 16 bytes)."""
-    global _program
+    global _folder, _program
     if _program is None:
-        folder = tempfile.mkdtemp()
-        source, _program = os.path.join(folder, "plans.cpp"), os.path.join(folder, "plans")
+        _folder = tempfile.TemporaryDirectory()
+        source, _program = os.path.join(_folder.name, "plans.cpp"), os.path.join(_folder.name, "plans")
         with open(source, "w") as f:
             f.write(PROGRAM)
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", lib_build.CSRC, "-o", _program, source], check=True)
