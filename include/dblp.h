@@ -584,9 +584,9 @@ int dblp_linear_grad(const dblp_linear_t* l, const dblp_matrix_t* dy, const dblp
  * The norm is summed in 64 bits.  X and A enter the products scaled by powers of two (1024 and 256) and rounded to f16; X itself is
  * kept in two f16 words (22 bits), so that what rounding adds is not amplified with the small singular values.  How far results are from
  * the iteration in 64 bits, in parts of their norm, with five steps of the usual coefficients:
- *   out_dtype BF16  the result's own rounding, 1.7e-3, up to 1.1 times that below 384 on the shorter side, where products read both words in
- *                   the last three steps (below 64 in all), and up to 1.45 times that for larger matrices, whose products are of one f16 word
- *                   each; up to 5e-3 where all singular values are alike.
+ *   out_dtype BF16  the result's own rounding, 1.7e-3, up to 1.1 times that below 512 on the shorter side, where products read both words in
+ *                   the last three steps (below 64 in all), and up to 1.5 times that for larger matrices, whose products are of one f16 word
+ *                   each (1.7 times where all singular values are alike).
  *   F32 or F16      the products are of both words (three products each, about three times the work of large matrices): up to 5e-6, and up to 6e-5 for
  *                   matrices of one or a few directions (iterated in fp32: 5e-6, 1.6e-4); F16 results are rounded besides.
  * For a bf16 result as near as the fp32 iteration's take F32 and convert.

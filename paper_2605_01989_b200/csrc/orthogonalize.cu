@@ -18,11 +18,11 @@ constexpr uint32_t kMaxSquares = 256;            // partial sums of squares a ma
 constexpr double kScaleX = 1024.0;
 constexpr float kScaleA = 256.0f;
 // Bf16 results come of products of one word where single roundings average out over many rows and columns: from kAverages on the shorter
-// side 1.25 to 1.42 times as far from 64 bits as the result's rounding alone.  Smaller matrices multiply both words in their last
-// three steps, whose roundings reach the result (up to 1.6 times with one word, 1.0 to 1.1 with both: 129 x 200 78 and 99 us, 256 x 1024 90 and
-// 125 us), and in all steps below kFew, where single roundings show (sides of two: up to 1.6e-2 of the norm, with both 1.7e-3; 16 x 16 45 and
+// side 1.1 to 1.5 times as far from 64 bits as the result's rounding alone (1.7 where all singular values are alike).  Smaller matrices multiply both words in their last
+// three steps, whose roundings reach the result (up to 1.6 times with one word, alike 2.8, with both 1.0 to 1.1: 129 x 200 78 and 99 us, 384 x
+// 640 92 and 134 us), and in all steps below kFew, where single roundings show (sides of two: up to 1.6e-2 of the norm, with both 1.7e-3; 16 x 16 45 and
 // 60 us).
-constexpr uint32_t kAverages = 384, kFew = 64, kLastSteps = 3;
+constexpr uint32_t kAverages = 512, kFew = 64, kLastSteps = 3;
 
 struct UpdIn {
     Source x;

@@ -32,12 +32,12 @@ int main()
         p.few = few;
         p.symmetric = symmetric;
         const ProductPlan r = plan_product(p);
-        printf("%d %d %u %u %u %u %u %u %u %d %d %d\n", (int)rows_take(p), r.cg, r.bn, r.tiles, r.whole, r.rest, r.parts, r.per, r.items, (int)r.turned,
-               (int)r.several, (int)(r.copy_a || r.copy_b));
+        printf("%d %d %u %u %u %u %u %u %u %d %d %d %u\n", (int)rows_take(p), r.cg, r.bn, r.tiles, r.whole, r.rest, r.parts, r.per, r.items, (int)r.turned,
+               (int)r.several, (int)(r.copy_a || r.copy_b), r.longest);
     }
 }
 """
-FIELDS = ("rows_take", "cg", "bn", "tiles", "whole", "rest", "parts", "per", "items", "turned", "several", "copies")
+FIELDS = ("rows_take", "cg", "bn", "tiles", "whole", "rest", "parts", "per", "items", "turned", "several", "copies", "longest")
 _folder, _program = None, None
 
 

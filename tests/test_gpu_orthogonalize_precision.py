@@ -8,12 +8,9 @@ F32  X is held to 2^-23 of its entries.  Where the result fills the space (full 
      result: 682 * 1.77 * 2^-23 = 1.44e-4.  (The iteration in fp32 gives 3e-5 to 1.6e-4 for the
      same matrices.)
 F16  the same and the result's rounding, 2^-12.
-BF16 products of one f16 word.  Singular values that spread: roundings of random sign, 2.4e-3 at most from 64 on the shorter side by a 64-bit
-     simulation with the same words, and the result's rounding, 1.7e-3 for values that spread over a binade; together the root of the sum
-     of squares.  All alike: A and B are multiples of the identity but for noise, and every diagonal element is rounded the same way, by up to
-     d = 2^-11.  A step at s = 1.1 changes X by |b s^2 + c s^4| / (f / s) = 2.8 / 0.64 = 4.4 d for B; a step at 0.7 by 1.16 d for B and 0.86 d
-     for A, which the next step multiplies by |s f' / f| = 1.6, 3.2 d; the one before that 0.71 * 1.6 * 2 d = 2.3 d: 9.9 d = 4.8e-3
-     in all, and 1.3e-3 and 1.7e-3 of random sign, 5.3e-3."""
+BF16 products of one f16 word from 512 on the shorter side: roundings of random sign, 2.4e-3 at most by a 64-bit simulation with the same words,
+     and the result's rounding, 1.7e-3 for values that spread over a binade; together the root of the sum of squares.  Smaller matrices,
+     with both words where it shows, stay within the same bound."""
 import pytest
 import torch
 
@@ -25,7 +22,7 @@ DEV = "cuda:0"
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 FULL = {F32: 1.2e-5, F16: 1.2e-5 + 2.0 ** -12, BF16: 3e-3}
 FEW = {F32: 1.44e-4, F16: 1.44e-4 + 2.0 ** -12, BF16: 3e-3}
-ALIKE = {F32: 1.2e-5, F16: 1.2e-5 + 2.0 ** -12, BF16: 5.3e-3}
+ALIKE = {F32: 1.2e-5, F16: 1.2e-5 + 2.0 ** -12, BF16: 3e-3}
 
 
 def randn(shape, seed):
@@ -104,19 +101,19 @@ def test_fp32_results_are_as_near_as_the_iteration_in_fp32(m, n, kind):
 
 
 @pytest.mark.parametrize("kind", ["noise", "gradient"])
-@pytest.mark.parametrize("m,n", [(64, 64), (64, 4000), (100, 3000), (129, 200), (300, 300), (383, 900), (384, 640), (512, 2048), (1030, 520), (1600, 1600)])
+@pytest.mark.parametrize("m,n", [(64, 64), (64, 4000), (100, 3000), (129, 200), (300, 300), (383, 900), (384, 640), (384, 4096), (511, 4096), (512, 2048), (512, 4096), (1030, 520), (1600, 1600)])
 def test_bf16_results_are_near_their_own_rounding(m, n, kind):
-    """Below 384 on the shorter side 1.2 times what rounding the exact result is off by (three last steps of both words), beyond 1.5 times."""
+    """Below 512 on the shorter side 1.2 times what rounding the exact result is off by (three last steps of both words), beyond 1.5 times."""
     x = matrix(m, n, kind, m + n).float() * 1e-2
     out = torch.empty((m, n), dtype=BF16, device=DEV)
     dblp.dblp_orthogonalize(x, out, torch.empty(dblp.dblp_orthogonalize_workspace_bytes(x, out), dtype=torch.uint8, device=DEV))
     want = iteration(x)
     off, rounded = ((out.double() - want).norm().item(), (want.bfloat16().double() - want).norm().item())
-    assert off <= (1.2 if min(m, n) < 384 else 1.5) * rounded, off / rounded
+    assert off <= (1.2 if min(m, n) < 512 else 1.5) * rounded, off / rounded
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
-@pytest.mark.parametrize("m,n", [(40, 90), (200, 130), (400, 500)])
+@pytest.mark.parametrize("m,n", [(40, 90), (200, 130), (400, 500), (600, 520)])
 def test_other_numbers_of_steps(m, n, steps):
     """The workspace does not depend on the steps; which products read both words does."""
     coefficients = ((1.5, -0.5, 0.0),) * steps

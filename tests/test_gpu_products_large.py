@@ -18,6 +18,7 @@ NEAR = {F32: 2.2e-5, BF16: 2.0 ** -9, F16: 2.0 ** -12}
 UPDATE = {F32: 1.2e-5, BF16: 3e-3}
 
 UPDATES = [(1, 1601, 3100), (1, 3100, 1590), (8, 803, 1109), (8, 1590, 1700), (1, 700, 4000), (1, 6400, 1600), (3, 1310, 1700)]
+LONG_UPDATES = [(1, 8200, 8250), (8, 2100, 12000)]       # sums of more than 8192 terms that are not cut
 ROWS, WIDE, NARROW = 4207, 6384, 1616                  # a down-projection: a ragged batch, widths that end inside a piece
 VOCABULARY = (520, 512, 50257)
 
@@ -32,6 +33,11 @@ def test_the_updates_reach_every_kind_of_tile():
         assert any(r["items"] > 74 and r["cg"] == 2 for r in symmetric)                             # several a pair
         assert sum(r["several"] and r["cg"] == 2 for r in steps) >= 5 and {r["bn"] for r in steps if r["several"]} >= {128, 256}
     assert any(r["rest"] and r["whole"] and r["several"] for r in steps)
+
+
+def test_the_long_updates_sum_in_runs():
+    for s in LONG_UPDATES:
+        assert max(r["longest"] for r in pl.plans(pl.update(*s, False))) * 64 > 8192, s
 
 
 def test_the_layers_reach_wide_pairs_in_runs_and_by_tma():
@@ -81,7 +87,7 @@ def iteration(x):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("out_dtype", [BF16, F32])
-@pytest.mark.parametrize("b,m,n", UPDATES)
+@pytest.mark.parametrize("b,m,n", UPDATES + LONG_UPDATES)
 def test_large_matrices_are_orthogonalised(b, m, n, out_dtype):
     x = randn((b, m, 8), F32, 1, 0.5) @ randn((b, 8, n), F32, 2) + randn((b, m, n), F32, 3)
     buf = torch.full((b, m + 3, (n + 47) // 16 * 16), 9.0, dtype=out_dtype, device=DEV)
