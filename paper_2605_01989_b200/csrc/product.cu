@@ -1,5 +1,5 @@
 // Matrix products: workspace, tensor maps and the copies of operands that TMA cannot address.  The kernels are in product_kernels.cuh,
-// built for their epilogues by product_linear.cu, product_grad.cu, product_poly.cu and product_last.cu.
+// built for their epilogues by product_linear_*.cu, product_dx.cu, product_dw.cu, product_poly.cu and product_last.cu.
 #include "product.cuh"
 
 namespace dblp {
